@@ -69,6 +69,7 @@ typedef enum bv_status {
 enum { BV_DTYPE_F32 = 0, BV_DTYPE_BF16 = 1 };
 enum { BV_MAX_GAMMA = 64 };
 enum { BV_NOALLOC_SCRATCH_BYTES = 8 * 1024 * 1024 };
+enum { BV_MAX_HEAD_DIM = 256 };
 
 /*
  * Block Verification: Algorithm 2 with Eq. "def_as" (p_0 = 1,
@@ -340,6 +341,95 @@ int bv_decode_loop(const void* target_table, const void* draft_table, const int3
                    const float* u_draft, const float* u_verify, int iterations, int B, int gamma, int V,
                    int dtype, float temperature, int algo, int32_t* out_tokens, int64_t* out_lengths,
                    int32_t* out_tau, int32_t* out_drafted, int32_t* out_fault, int32_t* work, void* stream);
+
+/*
+ * The key-value cache of a model whose blocks are verified here: the tokens of B sequences in pages that a table names.
+ * Token j of sequence b lies in page table[b, j / page_size], at row j % page_size of it; refs[p] counts the table entries that name
+ * page p, and a page is free where that is 0.  One iteration of Algorithm 3 on such a cache:
+ *   bv_pages_extend    room for the gamma + 1 tokens that are to be scored (pages that are shared are replaced: bv_pages_copy)
+ *   bv_cache_append    their keys and values, in each layer
+ *   bv_cache_attend    what they attend to, in each layer
+ *   bv_pages_truncate  after the verification, with its out_len: the tokens that were not accepted go
+ * The drafting model's steps are the same with one token.  Layers share table, lens and refs and differ in k and v.
+ *
+ * All pointers are DEVICE pointers.  Strides count elements and are 0 or more; the D elements of a row are contiguous.
+ * Calls enqueue on `stream` and return without synchronising; lengths and tables are read on the device, so calls of one shape may be
+ * captured and replayed.  Members that a call does not name are not looked at.
+ */
+typedef struct bv_cache {
+    void* k;               /* [num_pages, heads, page_size, D]  dtype, at k_stride between pages, heads, tokens */
+    void* v;               /* the same, at v_stride                                                             */
+    int32_t* table;        /* [B, width]  page numbers; entries at and beyond ceil(lens[b] / page_size) are not read */
+    int32_t* lens;         /* [B]         0 .. width page_size; anything else is a data fault of the sequence    */
+    int32_t* refs;         /* [num_pages] table entries that name the page (bv_pages_* but bv_pages_copy)        */
+    int64_t k_stride[3], v_stride[3];
+    int32_t B, width, num_pages, page_size, heads, D, dtype, reserved;
+} bv_cache;
+
+/*
+ * Attention of the newest tokens of every sequence over its pages:
+ *   out[b, t, h] = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale q[b, t, h] . k_j)
+ * over the positions j that token t, at position p = lens[b] - m_b + t, may see: j <= p, and with window > 0 only
+ * j > p - window or j < sinks.  m_b = n_new[b] held to 0 .. n (n_new null: n) tokens are the newest ones of the sequence and
+ * already in the cache; rows t >= m_b of out are left as they were.  Query head h uses key-value head h / (q_heads / heads).
+ * A row that sees nothing (a block longer than its sequence) is 0.  What a row does not see does not count, whatever it
+ * holds (infinities and NaN too).  A sequence with a length that is none, or with a page outside 0 .. num_pages - 1 among
+ * those it has to read, gets NaN; others are unaffected.
+ *   q, out  [B, n, q_heads, D] in the cache's dtype, at strides between sequences, tokens, heads; out must not overlap the inputs
+ * Arithmetic: scores, weights and sums in fp32.  16-bit values are multiplied by weights rounded to 16 bits (their sum is taken of the same
+ * rounded weights) where the tensor cores do it.  Results do not depend on the order in which CTAs finish.
+ * Any D up to BV_MAX_HEAD_DIM, any page size, any alignment; D a multiple of 8 up to 128 at 16-byte strides with
+ * pages of a multiple of 8 tokens, in bf16, goes through the tensor cores.
+ */
+int bv_cache_attend(const bv_cache* cache, const void* q, const int64_t* q_stride, const int32_t* n_new, int n, int q_heads,
+                    float scale, int window, int sinks, void* out, const int64_t* out_stride, void* stream);
+
+/*
+ * The keys and values of the newest tokens into their pages: row t < m_b (as above) of k_new, v_new [B, n, heads, D], at strides between
+ * sequences, tokens, heads, becomes position lens[b] - m_b + t of sequence b.  A position below 0, a length that is none and an entry of
+ * the table that is no page are passed over.
+ */
+int bv_cache_append(const bv_cache* cache, const void* k_new, const int64_t* k_new_stride, const void* v_new,
+                    const int64_t* v_new_stride, const int32_t* n_new, int n, void* stream);
+
+/*
+ * Lengthens the sequences by n_new[b] tokens each (null: by n; n_new[b] in 0 .. n).  The pages that takes are the lowest free ones, given out in
+ * the sequences' order; a last page that is partly filled and shared is replaced by one of its own.
+ *   out_new    [B]     n_new[b], or -1 for a sequence that is left as it was: n_new[b] out of range, too long for its table row, a length or a
+ *                      last page that is none, or not enough free pages for it and all before it (then no later one gets any either)
+ *   out_copies [B, 2]  the page that was replaced and the one in its place, which the caller fills with bv_pages_copy; else -1, -1
+ * Pages whose count falls to 0 by a replacement are free from the next call on.  out_new is what n_new of the calls that follow takes.
+ */
+int bv_pages_extend(const bv_cache* cache, const int32_t* n_new, int n, int32_t* out_new, int32_t* out_copies, void* stream);
+
+/*
+ * Of the m_b newest tokens of sequence b (m_b as in bv_cache_attend, at most lens[b]; n = 0: of all its tokens, n_new is not looked at) the first
+ * keep[b], held to 0 .. m_b, stay.  With keep = out_len of a verification and n = gamma + 1 that is what follows it: the last
+ * token and the accepted drafts stay (none of a block with a data fault, out_len = -1).  keep = 0 with n = 0 gives a sequence up.
+ * Pages that hold nothing any more are given back, their table entries become -1.
+ */
+int bv_pages_truncate(const bv_cache* cache, const int32_t* keep, const int32_t* n_new, int n, void* stream);
+
+/*
+ * Sequence dst[i] becomes a second copy of sequence src[i], on the same pages; what it held is given back.  Beyond the pages in use
+ * its table row becomes -1.  out_ok [forks]: 0, or -1 for a fork that is refused and changes nothing: an index outside 0 .. B-1, a length that is
+ * none, or a dst[i] that another fork names too, as its source or target, or that is its own source.
+ */
+int bv_pages_fork(const bv_cache* cache, const int32_t* src, const int32_t* dst, int forks, int32_t* out_ok, void* stream);
+
+/*
+ * Renumbers the pages so that the ones in use are 0 .. n-1: those beyond move, in order, to the free ones before, in order.
+ *   out_moves [num_pages / 2, 2]  source and destination of each move, then -1;  out_count [1]  how many
+ * Tables and counts are changed here; the contents are the caller's to move: bv_pages_copy with out_moves and out_count for every layer,
+ * before anything else uses the cache.
+ */
+int bv_pages_compact(const bv_cache* cache, int32_t* out_moves, int32_t* out_count, void* stream);
+
+/*
+ * Copies pages, keys and values: pairs [n_pairs, 2] of source and destination, of which the first *count are looked at (null: all).  A pair
+ * with a page outside 0 .. num_pages - 1, or with itself, is passed over.  No page may be the destination of one pair and named by another.
+ */
+int bv_pages_copy(const bv_cache* cache, const int32_t* pairs, int n_pairs, const int32_t* count, void* stream);
 
 /*
  * Waits for `stream` and reports whether a device-side wait of any call enqueued on it since the

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -20,7 +21,7 @@ DTYPE_BF16 = 1
 
 # every symbol include/bv.h declares
 EXPORTS = ["bv_verify", "tv_verify", "bv_verify_ex", "tv_verify_ex", "bv_verify_host",
-           "tv_verify_host", "bv_verify_noalloc", "bv_verify_lse", "bv_verify_lse_ex", "tv_verify_lse", "tv_verify_lse_ex", "gbv_verify", "gbv_verify_ex", "bv_verify_probs", "tv_verify_probs", "bv_sample_draft", "bv_draft_chain", "bv_decode_loop", "bv_stream_status", "bv_set_option", "bv_release", "bv_last_launch_count", "bv_last_kernel", "bv_last_cuda_error",
+           "tv_verify_host", "bv_verify_noalloc", "bv_verify_lse", "bv_verify_lse_ex", "tv_verify_lse", "tv_verify_lse_ex", "gbv_verify", "gbv_verify_ex", "bv_verify_probs", "tv_verify_probs", "bv_sample_draft", "bv_draft_chain", "bv_decode_loop", "bv_cache_attend", "bv_cache_append", "bv_pages_extend", "bv_pages_truncate", "bv_pages_fork", "bv_pages_compact", "bv_pages_copy", "bv_stream_status", "bv_set_option", "bv_release", "bv_last_launch_count", "bv_last_kernel", "bv_last_cuda_error",
            "bv_status_string", "bv_version"]
 
 
@@ -62,6 +63,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     for name in ("bv_verify_lse", "tv_verify_lse"):
         getattr(lib, name).argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, cf, vp, vp, vp]
         getattr(lib, name + "_ex").argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, cf, vp, vp, vp, vp, vp, vp, vp, vp]
+    # (bv_cache and the strides travel as packed bytes)
+    lib.bv_cache_attend.argtypes = [vp, vp, vp, vp, ci, ci, cf, ci, ci, vp, vp, vp]
+    lib.bv_cache_append.argtypes = [vp, vp, vp, vp, vp, vp, ci, vp]
+    lib.bv_pages_extend.argtypes = [vp, vp, ci, vp, vp, vp]
+    lib.bv_pages_truncate.argtypes = [vp, vp, vp, ci, vp]
+    lib.bv_pages_fork.argtypes = [vp, vp, vp, ci, vp, vp]
+    lib.bv_pages_compact.argtypes = [vp, vp, vp, vp]
+    lib.bv_pages_copy.argtypes = [vp, vp, ci, vp, vp]
     for name in EXPORTS:
         getattr(lib, name).restype = ci
     lib.bv_stream_status.argtypes = [vp]
@@ -429,3 +438,180 @@ def _lse_call(name, target_logits, draft_logits, draft_tokens, uniforms, draft_l
             return out_tokens, out_len, diag
         _check(getattr(lib, name)(*args, s))
     return out_tokens, out_len
+
+
+# ---- the paged key-value cache (include/bv.h, struct bv_cache) ----
+
+_CACHE = struct.Struct("@5Q6q8i")
+_STRIDES = struct.Struct("@3q")
+
+
+def _pool(t, name: str):
+    """Strides of a pool of pages [num_pages, heads, page_size, D]."""
+    if t.dim() != 4 or t.stride(3) != 1:
+        raise ValueError("%s must be [num_pages, heads, page_size, D] with contiguous rows of D" % name)
+    return t.stride()
+
+
+def _written(t, name: str) -> None:
+    """A tensor that is written must not have two elements in one place."""
+    if not t.is_contiguous() and any(st == 0 and n > 1 for st, n in zip(t.stride(), t.shape)):
+        raise ValueError("%s must not be an expanded tensor" % name)
+
+
+def _sequences(table, lens):
+    if table.dim() != 2 or lens.dim() != 1 or lens.shape[0] != table.shape[0] or table.dtype != torch.int32 or lens.dtype != torch.int32:
+        raise ValueError("table must be int32 [B, width] and lens int32 [B]")
+    if not (table.is_contiguous() and lens.is_contiguous()):
+        raise ValueError("table and lens must be contiguous")
+    dev = table.get_device()
+    if dev < 0 or lens.get_device() != dev:
+        raise ValueError("expected CUDA tensors on one device")
+    return table.shape
+
+
+def _counted(t, n: int, dev: int, name: str):
+    """Address of an int32 [n] on the cache's device (None: null)."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError("%s must be a contiguous int32 tensor [%d] on the cache's device" % (name, n))
+    return t.data_ptr()
+
+
+def _cache(k, v, table, lens) -> bytes:
+    ks, vs = _pool(k, "k"), _pool(v, "v")
+    B, width = _sequences(table, lens)
+    P, heads, page, D = k.shape
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("k and v must have one shape and dtype")
+    if not k.get_device() == v.get_device() == table.get_device():
+        raise ValueError("expected CUDA tensors on one device")
+    return _CACHE.pack(k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr(), 0, ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+                       B, width, P, page, heads, D, _dtype_code(k), 0)
+
+
+def _rows(t, n_heads, like, B: int, name: str):
+    """Checks [B, n, heads, D] of the cache's dtype on its device; (n, heads, packed strides)."""
+    if t.dim() != 4 or t.shape[0] != B or t.shape[3] != like.shape[3] or (n_heads and t.shape[2] != n_heads) or t.dtype != like.dtype:
+        raise ValueError("%s must be [B, n, heads, D] of the cache's dtype" % name)
+    st = t.stride()
+    if st[3] != 1 or t.get_device() != like.get_device():
+        raise ValueError("%s must have contiguous rows of D on the cache's device" % name)
+    return t.shape[1], t.shape[2], _STRIDES.pack(st[0], st[1], st[2])
+
+
+def bv_cache_attend(q, k, v, table, lens, n_new=None, scale: Optional[float] = None, window: int = 0, sinks: int = 0, out=None,
+                    stream=None):
+    """Attention of the newest tokens of each sequence over a paged key-value cache (see include/bv.h).
+
+    ``q`` [B, n, q_heads, D]; ``k``, ``v`` [num_pages, heads, page_size, D] (float32 or bfloat16, any strides with contiguous rows);
+    ``table`` int32 [B, width], ``lens`` int32 [B] (the newest tokens counted in), ``n_new`` int32 [B] or None: every sequence
+    brings n.  ``scale``: 1/sqrt(D) by default; ``window`` > 0: a token sees its last ``window`` positions and the first ``sinks``.
+    Returns ``out`` [B, n, q_heads, D] (rows beyond n_new[b] are not written: zero in a tensor made here)."""
+    B = table.shape[0]
+    blob = _cache(k, v, table, lens)
+    n, heads, qs = _rows(q, 0, k, B, "q")
+    dev = k.device
+    if out is None:
+        out = torch.empty((B, n, heads, k.shape[3]), dtype=k.dtype, device=dev) if n_new is None else \
+            torch.zeros((B, n, heads, k.shape[3]), dtype=k.dtype, device=dev)
+    else:
+        _written(out, "out")
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    os_ = _rows(out, heads, k, B, "out")[2]
+    new = _counted(n_new, B, dev.index, "n_new")
+    with _on(dev):
+        _check(load_library().bv_cache_attend(blob, q.data_ptr(), qs, new, n, heads, k.shape[3] ** -0.5 if scale is None else scale,
+                                              window, sinks, out.data_ptr(), os_, _raw_stream(dev, stream)))
+    return out
+
+
+def bv_cache_append(k_new, v_new, k, v, table, lens, n_new=None, stream=None) -> None:
+    """Stores the keys and values of the newest tokens [B, n, heads, D] in the pages of their positions (see include/bv.h)."""
+    B = table.shape[0]
+    blob = _cache(k, v, table, lens)
+    n, _, ks = _rows(k_new, k.shape[1], k, B, "k_new")
+    n_v, _, vs = _rows(v_new, k.shape[1], k, B, "v_new")
+    if n != n_v:
+        raise ValueError("k_new and v_new must have one shape")
+    _written(k, "k")
+    _written(v, "v")
+    dev = k.device
+    new = _counted(n_new, B, dev.index, "n_new")
+    with _on(dev):
+        _check(load_library().bv_cache_append(blob, k_new.data_ptr(), ks, v_new.data_ptr(), vs, new, n, _raw_stream(dev, stream)))
+
+
+def _book(table, lens, refs, page_size: int) -> bytes:
+    B, width = _sequences(table, lens)
+    if refs.dtype != torch.int32 or refs.dim() != 1 or not refs.is_contiguous() or refs.get_device() != table.get_device():
+        raise ValueError("refs must be a contiguous int32 tensor [num_pages] on the table's device")
+    return _CACHE.pack(0, 0, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), 0, 0, 0, 0, 0, 0, B, width, refs.shape[0], page_size, 0, 0, 0, 0)
+
+
+def bv_pages_extend(table, lens, refs, page_size: int, n: int, n_new=None, stream=None):
+    """Lengthens every sequence by n (or n_new[b] in 0 .. n) tokens, taking the lowest free pages (refs 0) in the sequences' order; table, lens and
+    refs change in place.  Returns (new int32 [B]: the tokens, or -1 for a sequence left as it was; copies int32 [B, 2]: the pages that
+    bv_pages_copy is to copy, or -1)."""
+    blob = _book(table, lens, refs, page_size)
+    dev, B = table.device, table.shape[0]
+    new, copies = table.new_empty((B,)), table.new_empty((B, 2))
+    given = _counted(n_new, B, dev.index, "n_new")
+    with _on(dev):
+        _check(load_library().bv_pages_extend(blob, given, n, new.data_ptr(), copies.data_ptr(), _raw_stream(dev, stream)))
+    return new, copies
+
+
+def bv_pages_truncate(table, lens, refs, page_size: int, keep, n: int = 0, n_new=None, stream=None) -> None:
+    """Keeps the first keep[b] of the n (or n_new[b]) newest tokens of each sequence, with n = 0 of all its tokens, and gives back the pages
+    that hold nothing any more.  ``keep`` may be the out_len of a verification."""
+    blob = _book(table, lens, refs, page_size)
+    dev, B = table.device, table.shape[0]
+    kept, given = _counted(keep, B, dev.index, "keep"), _counted(n_new, B, dev.index, "n_new")
+    with _on(dev):
+        _check(load_library().bv_pages_truncate(blob, kept, given, n, _raw_stream(dev, stream)))
+
+
+def bv_pages_fork(table, lens, refs, page_size: int, src, dst, stream=None):
+    """Makes sequence dst[i] a second copy of src[i] on the same pages.  Returns ok int32: 0, or -1 where a fork is refused."""
+    blob = _book(table, lens, refs, page_size)
+    dev, forks = table.device, src.shape[0]
+    s, d = _counted(src, forks, dev.index, "src"), _counted(dst, forks, dev.index, "dst")
+    ok = table.new_empty((forks,))
+    with _on(dev):
+        _check(load_library().bv_pages_fork(blob, s, d, forks, ok.data_ptr(), _raw_stream(dev, stream)))
+    return ok
+
+
+def bv_pages_compact(table, lens, refs, page_size: int, stream=None):
+    """Renumbers the pages so that those in use come first.  Returns (moves int32 [num_pages // 2, 2], count int32 [1]), which
+    bv_pages_copy takes for each layer before anything else uses the cache."""
+    blob = _book(table, lens, refs, page_size)
+    dev = table.device
+    moves, count = table.new_empty((refs.shape[0] // 2, 2)), table.new_empty((1,))
+    with _on(dev):
+        # (a pool of one page has no moves, and no place for them)
+        _check(load_library().bv_pages_compact(blob, moves.data_ptr() or count.data_ptr(), count.data_ptr(), _raw_stream(dev, stream)))
+    return moves, count
+
+
+def bv_pages_copy(k, v, pairs, count=None, stream=None) -> None:
+    """Copies pages, keys and values: pairs int32 [n, 2] of source and destination, of which the first count[0] are looked at."""
+    ks, vs = _pool(k, "k"), _pool(v, "v")
+    _written(k, "k")
+    _written(v, "v")
+    dev = k.device
+    if v.shape != k.shape or v.dtype != k.dtype or v.get_device() != k.get_device() or not k.is_cuda:
+        raise ValueError("k and v must have one shape, dtype and CUDA device")
+    if pairs.dtype != torch.int32 or pairs.dim() != 2 or pairs.shape[1] != 2 or not pairs.is_contiguous() or pairs.get_device() != dev.index:
+        raise ValueError("pairs must be a contiguous int32 tensor [n, 2] on the cache's device")
+    P, heads, page, D = k.shape
+    n = pairs.shape[0]
+    blob = _CACHE.pack(k.data_ptr(), v.data_ptr(), 0, 0, 0, ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], 0, 0, P, page, heads, D, _dtype_code(k), 0)
+    upto = _counted(count, 1, dev.index, "count")
+    if n == 0:
+        return
+    with _on(dev):
+        _check(load_library().bv_pages_copy(blob, pairs.data_ptr(), n, upto, _raw_stream(dev, stream)))

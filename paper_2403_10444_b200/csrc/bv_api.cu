@@ -70,7 +70,9 @@ constexpr long long kPhaseAllBytes[2] = {360LL << 20, 144LL << 20}, kPhaseAllByt
 constexpr long long kPhaseAllRows[2] = {2500000, 2200000}, kPhaseAllSmall = 1300000;
 constexpr size_t kSlotHead = 16384;   // first area of a stream's workspace: status word, barrier words, the phase kernel's counters
 constexpr size_t kSlotPhase = 256, kSlotSmall = 8192;    // ... the phase kernel's from here on, the small-batch kernel's counters of its sequences
-static_assert(kSlotPhase + bv::kPhaseCounterWords * sizeof(unsigned) <= kSlotSmall && kSlotSmall + bv::kSmallMaxB * sizeof(unsigned) <= kSlotHead, "the counters fit in the head");
+constexpr size_t kSlotCache = 12288;                     // ... the counters of the cache's attention
+static_assert(kSlotPhase + bv::kPhaseCounterWords * sizeof(unsigned) <= kSlotSmall && kSlotSmall + bv::kSmallMaxB * sizeof(unsigned) <= kSlotCache &&
+              kSlotCache + bv::kCacheCounters * sizeof(unsigned) <= kSlotHead, "the counters fit in the head");
 constexpr int kStreamSlots = 32;  // streams per device that keep a workspace of their own
 
 // Tuning and test options (bv_set_option); their first values come from the environment, read once.
@@ -700,6 +702,17 @@ int note_cuda_error(cudaError_t e) {
     return BV_ERR_CUDA;
 }
 void note_launches(int n) { t_last_launches = n; }
+int with_stream_work(cudaStream_t stream, size_t (*scratch)(int, const void*), int (*enqueue)(const StreamWork&, void*), void* ctx) {
+    std::call_once(g_opt_once, load_env_options);
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState* d = nullptr;
+    int rc = device_state(&d);
+    if (rc != BV_OK) return rc;
+    StreamSlot* s = nullptr;
+    if ((rc = stream_slot(*d, stream, 0, scratch(d->sm_count, ctx), &s)) != BV_OK) return rc;
+    return enqueue(StreamWork{reinterpret_cast<int*>(s->head.p), reinterpret_cast<unsigned*>(s->head.p + kSlotCache), s->scratch.p,
+                              d->sm_count, g_opt.wait_limit > 0 ? static_cast<unsigned>(g_opt.wait_limit) : 0u, g_opt.never_signal}, ctx);
+}
 bool small_takes_tables(int algo, bool lse, int B, int gamma, size_t row_bytes) {
     return small_fits(B, gamma) &&
            static_cast<long long>(B) * (2 * gamma + 1) * static_cast<long long>(row_bytes) <= kPhaseBytes[algo != kBlockVerify ? 0 : lse ? 2 : 1][0];

@@ -13,6 +13,20 @@ int check_verify_args(const void* tgt, const void* drf, const int32_t* tok, cons
                       int V, int dtype, float T, const int32_t* ot, const int32_t* ol);
 int note_cuda_error(cudaError_t e);
 void note_launches(int n);
+
+// The workspace of `stream` on the current device for a call of the cache (bv_cache.cu): the status word of the stream, kCacheCounters
+// counters that are zero between launches, `scratch` bytes of anything.  `enqueue` is called with it while nobody else can have it
+// (it belongs to the stream again when the library's lock is let go).  sm_count: SMs of the device.
+constexpr int kCacheCounters = 512;
+struct StreamWork {
+    int* status;
+    unsigned* counters;
+    char* scratch;
+    int sm_count;
+    unsigned wait_limit;
+    int never_signal;
+};
+int with_stream_work(cudaStream_t stream, size_t (*scratch)(int sm_count, const void* ctx), int (*enqueue)(const StreamWork& work, void* ctx), void* ctx);
 // One verification call on rows of two tables (Params::first): BV_OK, BV_ERR_UNSUPPORTED if no kernel takes it, or an error.
 // With `probe` only that is found out: nothing is launched.
 int run_tables(int algo, const void* tgt_table, const void* drf_table, const int32_t* first, const int32_t* tok, const float* uni,

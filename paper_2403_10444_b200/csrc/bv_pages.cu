@@ -1,0 +1,447 @@
+// The pages of a key-value cache: taking, sharing and giving them back, and moving the ones in use together (contracts in
+// include/bv.h).  A page is free where its count is 0; the lowest free pages are taken first, by the sequences in order.  So
+// nothing but the counts says what is free, giving back is an atomic decrement in any order, and the outcome of every call is the
+// same whatever the order in which its threads run.
+//
+// Taking needs the free pages' ranks: one cluster of up to 8 CTAs reads the counts in as many contiguous regions, the regions' sums
+// cross through distributed shared memory, and a second look at the counts hands out the pages.  (One CTA reads some 60 bytes a
+// clock: 100000 counts would take it 4 us twice, a cluster has them in one round of loads per CTA.)
+#include <cooperative_groups.h>
+
+#include "bv_cache.cuh"
+#include "bv_launch.h"
+
+namespace cg = cooperative_groups;
+
+namespace bv {
+namespace {
+
+constexpr int kThreads = 512, kEach = 16, kRound = kThreads * kEach;      // counts a thread, a CTA looks at in one go
+constexpr int kMaxSequences = 8192;                                       // of bv_pages_extend: their needs lie in shared memory
+constexpr int kMost = (1 << 22) - 2;                                      // pages of a cache, entries of a table's row
+
+struct PagesArgs {
+    int32_t* table;
+    int32_t* lens;
+    int32_t* refs;
+    const int32_t* n_new;
+    int B, n, page, num_pages, width;
+};
+
+__device__ __forceinline__ int pages_of(long long tokens, int page) { return static_cast<int>((tokens + page - 1) / page); }
+__device__ __forceinline__ bool length_ok(const PagesArgs& a, int len) { return len >= 0 && len <= static_cast<long long>(a.width) * a.page; }
+
+// The counts of pages first .. first + 15 of a region that ends at `end`, as bits: which are 0.
+__device__ __forceinline__ unsigned zero_bits(const int32_t* refs, int first, int end, bool vec) {
+    unsigned bits = 0;
+    if (vec && first + kEach <= end) {
+        int4 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __ldcg(reinterpret_cast<const int4*>(refs + first) + i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            bits |= (static_cast<unsigned>(x[i].x == 0) | static_cast<unsigned>(x[i].y == 0) << 1 | static_cast<unsigned>(x[i].z == 0) << 2 | static_cast<unsigned>(x[i].w == 0) << 3) << 4 * i;
+    } else {
+        for (int i = 0; i < kEach; ++i)
+            if (first + i < end && __ldcg(refs + first + i) == 0) bits |= 1u << i;
+    }
+    return bits;
+}
+struct ScanSmem {
+    int warp[kThreads / 32];
+    int pad;
+};
+// Sum over the CTA, and what lies before this thread.
+__device__ __forceinline__ int scan(ScanSmem& sm, int mine, int* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int upto = mine;
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+    }
+    __syncthreads();                          // (the last scan's readers)
+    if (lane == 31) sm.warp[warp] = upto;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        const int x = sm.warp[w];
+        before += w < warp ? x : 0;
+        all += x;
+    }
+    *total = all;
+    return before + upto - mine;
+}
+
+// A CTA's region of the counts: whole rounds of 16 but for the last.
+__device__ __forceinline__ void region(int num_pages, int rank, int ctas, int* begin, int* end) {
+    const int each = ((num_pages + ctas - 1) / ctas + kEach - 1) / kEach * kEach;
+    const long long b = static_cast<long long>(each) * rank;
+    *begin = b < num_pages ? static_cast<int>(b) : num_pages;
+    *end = b + each < num_pages ? static_cast<int>(b + each) : num_pages;
+}
+
+// ---- extend ------------------------------------------------------------------------------------------------------------
+
+struct ExtendSmem {
+    ScanSmem scan;
+    int free;                 // free pages of this CTA's region
+    int upto[kMaxSequences];  // pages needed by the sequences up to and including this one, at most one more than there are
+    int info[kMaxSequences];  // negative: refused whatever is free; else kReplace, kNeeds, and the first entry of its table row to be filled
+};
+enum : int { kReplace = 1, kNeeds = 2, kFirst = 4 };
+
+// What a sequence asks for: the number of pages, and its `info`.
+__device__ __forceinline__ int need_of(const PagesArgs& a, int b, int* info) {
+    const int len = __ldcg(a.lens + b);
+    const int m = a.n_new ? __ldg(a.n_new + b) : a.n;
+    const long long grown = static_cast<long long>(len) + m;
+    *info = -1;
+    if (m < 0 || m > a.n || !length_ok(a, len) || grown > static_cast<long long>(a.width) * a.page || grown > 0x7fffffff) return 0;
+    int first = pages_of(len, a.page), pages = pages_of(grown, a.page) - first, replace = 0;
+    if (m > 0 && len % a.page != 0) {
+        const int last = __ldcg(a.table + static_cast<long long>(b) * a.width + first - 1);
+        if (last < 0 || last >= a.num_pages) return 0;
+        if (__ldcg(a.refs + last) > 1) {      // shared and partly filled
+            replace = kReplace;
+            --first;
+            ++pages;
+        }
+    }
+    *info = first * kFirst + (pages > 0 ? kNeeds : 0) + replace;
+    return min(pages, a.num_pages + 1);
+}
+
+__global__ void __launch_bounds__(kThreads, 1) extend_pages_kernel(const PagesArgs a, int32_t* out_new, int32_t* out_copies, const int vec) {
+    extern __shared__ __align__(16) char raw[];
+    ExtendSmem& sm = *reinterpret_cast<ExtendSmem*>(raw);
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = static_cast<int>(cluster.block_rank()), ctas = static_cast<int>(cluster.num_blocks()), tid = threadIdx.x;
+    int begin, end;
+    region(a.num_pages, rank, ctas, &begin, &end);
+
+    // free pages of the region
+    int mine = 0, total;
+    for (int p = begin + tid * kEach; p < end; p += kRound) mine += __popc(zero_bits(a.refs, p, end, vec));
+    scan(sm.scan, mine, &total);
+    if (tid == 0) sm.free = total;
+    // what every sequence needs, summed up in their order (every CTA for itself: the pages it finds may be anybody's)
+    int sum = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+        const int b = b0 + tid;
+        int info = -1;
+        const int want = b < a.B ? need_of(a, b, &info) : 0;
+        int all;                              // (512 numbers of at most kMost + 1 each stay within 32 bits)
+        const int before = scan(sm.scan, want, &all);
+        if (b < a.B) {
+            sm.upto[b] = min(sum + before + want, a.num_pages + 1);
+            sm.info[b] = info;
+        }
+        sum = min(sum + all, a.num_pages + 1);
+    }
+    cluster.sync();                           // everything that decides has been read, and nothing changed so far
+    int before = 0, free = 0;
+    for (int r = 0; r < ctas; ++r) {
+        const int f = *cluster.map_shared_rank(&sm.free, r);
+        if (r < rank) before += f;
+        free += f;
+    }
+    // the region's free pages, by rank, to the sequences
+    const int wanted = min(sum, free);
+    int at = before;
+    for (int p0 = begin; p0 < end && at < wanted; p0 += kRound) {
+        const int p = p0 + tid * kEach;
+        unsigned bits = p < end ? zero_bits(a.refs, p, end, vec) : 0u;
+        int all;
+        int f = at + scan(sm.scan, __popc(bits), &all);
+        at += all;
+        for (; bits && f < wanted; bits &= bits - 1, ++f) {
+            const int page = p + __ffs(bits) - 1;
+            int lo = 0, hi = a.B - 1;         // the first sequence whose sum is above f
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                if (sm.upto[mid] > f) hi = mid; else lo = mid + 1;
+            }
+            if (sm.upto[lo] > free) continue; // it is not served, nor is any after it
+            const int slot = f - (lo > 0 ? sm.upto[lo - 1] : 0), info = sm.info[lo];
+            int32_t* entry = a.table + static_cast<long long>(lo) * a.width + info / kFirst + slot;
+            if (slot == 0 && (info & kReplace)) {
+                out_copies[2 * lo] = *entry;
+                out_copies[2 * lo + 1] = page;
+            }
+            *entry = page;
+            a.refs[page] = 1;
+        }
+    }
+    __threadfence();
+    cluster.sync();
+    // lengths, what was served, and the counts of the pages that were replaced (only now: one that comes to 0 is free for the next call)
+    for (int b = rank * kThreads + tid; b < a.B; b += ctas * kThreads) {
+        const int info = sm.info[b];
+        const bool ok = info >= 0 && (!(info & kNeeds) || sm.upto[b] <= free);
+        const int m = a.n_new ? __ldg(a.n_new + b) : a.n;
+        if (ok && (info & kReplace)) atomicSub(a.refs + __ldcg(out_copies + 2 * b), 1);
+        else out_copies[2 * b] = out_copies[2 * b + 1] = -1;
+        out_new[b] = ok ? m : -1;
+        if (ok) a.lens[b] += m;
+    }
+}
+
+// ---- truncate ----------------------------------------------------------------------------------------------------------
+
+// One use of a page less.  (A count that is not positive is none of ours to lower: it stays.)
+__device__ __forceinline__ void give_back(int32_t* refs, int num_pages, int page) {
+    if (page < 0 || page >= num_pages) return;
+    if (atomicSub(refs + page, 1) <= 0) atomicAdd(refs + page, 1);
+}
+
+// A CTA per sequence.
+__global__ void __launch_bounds__(128) truncate_pages_kernel(const PagesArgs a, const int32_t* keep) {
+    const int b = blockIdx.x;
+    const int len = __ldcg(a.lens + b);
+    if (!length_ok(a, len)) return;
+    int m = len;
+    if (a.n > 0) {
+        m = a.n_new ? __ldg(a.n_new + b) : a.n;
+        m = m < 0 ? 0 : m > len ? len : m;
+    }
+    int k = __ldg(keep + b);
+    k = k < 0 ? 0 : k > m ? m : k;
+    const int left = len - m + k;
+    int32_t* row = a.table + static_cast<long long>(b) * a.width;
+    for (int j = pages_of(left, a.page) + threadIdx.x; j < pages_of(len, a.page); j += 128) {
+        give_back(a.refs, a.num_pages, row[j]);
+        row[j] = -1;
+    }
+    __syncthreads();                          // (everybody has read the length)
+    if (threadIdx.x == 0) a.lens[b] = left;
+}
+
+// ---- fork --------------------------------------------------------------------------------------------------------------
+
+// A CTA per fork.  A fork whose target another one names, or that any one has as its source, is refused: those that are left change
+// rows that nobody else reads or changes, so they need no order.
+__global__ void __launch_bounds__(128) fork_pages_kernel(const PagesArgs a, const int32_t* src, const int32_t* dst, int forks, int32_t* out_ok) {
+    const int f = blockIdx.x;
+    const int s = __ldg(src + f), d = __ldg(dst + f);
+    bool bad = s < 0 || s >= a.B || d < 0 || d >= a.B;
+    for (int g = threadIdx.x; g < forks; g += 128) bad |= (g != f && __ldg(dst + g) == d) || __ldg(src + g) == d;
+    if (!__syncthreads_or(bad)) {
+        const int len = __ldcg(a.lens + s), old = __ldcg(a.lens + d);
+        bad = !length_ok(a, len) || !length_ok(a, old);
+        if (!bad) {
+            const int32_t* from = a.table + static_cast<long long>(s) * a.width;
+            int32_t* to = a.table + static_cast<long long>(d) * a.width;
+            const int take = pages_of(len, a.page), give = pages_of(old, a.page);
+            for (int j = threadIdx.x; j < a.width; j += 128) {
+                const int had = to[j];
+                const int page = j < take ? from[j] : -1;
+                if (page >= 0 && page < a.num_pages) atomicAdd(a.refs + page, 1);
+                if (j < give) give_back(a.refs, a.num_pages, had);
+                to[j] = page;
+            }
+            __syncthreads();
+            if (threadIdx.x == 0) a.lens[d] = len;
+        }
+    } else {
+        bad = true;
+    }
+    if (threadIdx.x == 0) out_ok[f] = bad ? -1 : 0;
+}
+
+// ---- compact -----------------------------------------------------------------------------------------------------------
+
+struct CompactSmem {
+    ScanSmem scan;
+    int used, holes, sources;
+};
+// The n pages in use are to lie at 0 .. n-1: those beyond move, in order, to the free pages before, in order.  Writes the moves, moves the
+// counts, and leaves in `to` where a page that moves goes, and n at to[num_pages].
+__global__ void __launch_bounds__(kThreads, 1) compact_pages_kernel(const PagesArgs a, int32_t* moves, int32_t* out_count, int32_t* to, const int vec) {
+    __shared__ CompactSmem sm;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = static_cast<int>(cluster.block_rank()), ctas = static_cast<int>(cluster.num_blocks()), tid = threadIdx.x;
+    int begin, end;
+    region(a.num_pages, rank, ctas, &begin, &end);
+    int mine = 0, all;
+    for (int p = begin + tid * kEach; p < end; p += kRound) mine += min(end - p, kEach) - __popc(zero_bits(a.refs, p, end, vec));
+    scan(sm.scan, mine, &all);
+    if (tid == 0) sm.used = all;
+    cluster.sync();
+    int live = 0;
+    for (int r = 0; r < ctas; ++r) live += *cluster.map_shared_rank(&sm.used, r);
+    // free pages before `live`, pages in use from there on, as bits
+    auto look = [&](int p, unsigned* holes, unsigned* sources) {
+        *holes = *sources = 0;
+        if (p >= end) return;
+        const unsigned zero = zero_bits(a.refs, p, end, vec), there = end - p >= kEach ? 0xffffu : (1u << (end - p)) - 1;
+        const unsigned before = live - p >= kEach ? 0xffffu : live <= p ? 0u : (1u << (live - p)) - 1;
+        *holes = zero & before;
+        *sources = ~zero & there & ~before;
+    };
+    int h = 0, s = 0;
+    for (int p = begin + tid * kEach; p < end; p += kRound) {
+        unsigned hb, sb;
+        look(p, &hb, &sb);
+        h += __popc(hb);
+        s += __popc(sb);
+    }
+    scan(sm.scan, h, &all);
+    if (tid == 0) sm.holes = all;
+    scan(sm.scan, s, &all);
+    if (tid == 0) sm.sources = all;
+    cluster.sync();
+    int hole_at = 0, source_at = 0, count = 0;
+    for (int r = 0; r < ctas; ++r) {
+        const int x = *cluster.map_shared_rank(&sm.holes, r), y = *cluster.map_shared_rank(&sm.sources, r);
+        if (r < rank) { hole_at += x; source_at += y; }
+        count += y;
+    }
+    for (int p0 = begin; p0 < end; p0 += kRound) {
+        const int p = p0 + tid * kEach;
+        unsigned hb, sb;
+        look(p, &hb, &sb);
+        int f = hole_at + scan(sm.scan, __popc(hb), &all);
+        hole_at += all;
+        int g = source_at + scan(sm.scan, __popc(sb), &all);
+        source_at += all;
+        for (; hb; hb &= hb - 1) moves[2 * f++ + 1] = p + __ffs(hb) - 1;
+        for (; sb; sb &= sb - 1) moves[2 * g++] = p + __ffs(sb) - 1;
+    }
+    __threadfence();
+    cluster.sync();
+    for (int i = rank * kThreads + tid; i < a.num_pages / 2; i += ctas * kThreads) {
+        if (i >= count) {
+            moves[2 * i] = moves[2 * i + 1] = -1;
+            continue;
+        }
+        const int from = __ldcg(moves + 2 * i), into = __ldcg(moves + 2 * i + 1);
+        a.refs[into] = __ldcg(a.refs + from);
+        a.refs[from] = 0;
+        to[from] = into;
+    }
+    if (rank == 0 && tid == 0) {
+        *out_count = count;
+        to[a.num_pages] = live;
+    }
+    cluster.sync();                           // (the others' shared memory is read above)
+}
+// Gives the pages of all tables their new numbers.
+__global__ void __launch_bounds__(256) rename_pages_kernel(const PagesArgs a, const int32_t* to) {
+    const int live = __ldg(to + a.num_pages);
+    const int len = __ldg(a.lens + blockIdx.y);
+    if (!length_ok(a, len)) return;
+    int32_t* row = a.table + static_cast<long long>(blockIdx.y) * a.width;
+    for (int j = blockIdx.x * 256 + threadIdx.x; j < pages_of(len, a.page); j += gridDim.x * 256) {
+        const int page = row[j];
+        if (page < live || page >= a.num_pages) continue;
+        const int now = __ldg(to + page);
+        if (now >= 0 && now < live) row[j] = now;     // (else no page in use: what it names was free)
+    }
+}
+
+// ---- launches ----------------------------------------------------------------------------------------------------------
+
+// One cluster, of as many CTAs as have a round of counts to look at.
+template <typename... P, typename... A>
+cudaError_t one_cluster(void (*kernel)(P...), int num_pages, size_t smem, cudaStream_t stream, A... args) {
+    int ctas = 1;
+    while (ctas < 8 && num_pages > ctas * kRound) ctas *= 2;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = ctas;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+bool on(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+int check(const bv_cache* c, PagesArgs* a) {
+    if (!c || !c->table || !c->lens || !c->refs || !on(c->table, 4) || !on(c->lens, 4) || !on(c->refs, 4)) return BV_ERR_INVALID_ARG;
+    if (c->B < 0 || c->width < 1 || c->num_pages < 1 || c->page_size < 1) return BV_ERR_INVALID_ARG;
+    if (c->num_pages > kMost || c->width > kMost || c->B > 0xffff) return BV_ERR_UNSUPPORTED;
+    *a = PagesArgs{c->table, c->lens, c->refs, nullptr, c->B, 0, c->page_size, c->num_pages, c->width};
+    note_launches(0);
+    return BV_OK;
+}
+int done(cudaError_t e, int launches) {
+    if (e != cudaSuccess) return note_cuda_error(e);
+    note_launches(launches);
+    return BV_OK;
+}
+
+struct CompactCall {
+    PagesArgs a;
+    int32_t* moves;
+    int32_t* count;
+    cudaStream_t stream;
+};
+size_t compact_scratch(int, const void* ctx) { return (static_cast<const CompactCall*>(ctx)->a.num_pages + 1) * sizeof(int32_t); }
+int enqueue_compact(const StreamWork& work, void* ctx) {
+    const CompactCall& c = *static_cast<const CompactCall*>(ctx);
+    int32_t* to = reinterpret_cast<int32_t*>(work.scratch);
+    cudaError_t e = one_cluster(compact_pages_kernel, c.a.num_pages, 0, c.stream, c.a, c.moves, c.count, to, static_cast<int>(on(c.a.refs, 16)));
+    if (e == cudaSuccess && c.a.B > 0) {
+        const int blocks = (c.a.width + 1023) / 1024;
+        rename_pages_kernel<<<dim3(blocks < 64 ? blocks : 64, c.a.B), 256, 0, c.stream>>>(c.a, to);
+        e = cudaGetLastError();
+    }
+    return done(e, c.a.B > 0 ? 2 : 1);
+}
+
+}  // namespace
+}  // namespace bv
+
+extern "C" int bv_pages_extend(const bv_cache* c, const int32_t* n_new, int n, int32_t* out_new, int32_t* out_copies, void* stream) {
+    bv::PagesArgs a;
+    const int rc = bv::check(c, &a);
+    if (rc != BV_OK) return rc;
+    if (n < 1 || !out_new || !out_copies || !bv::on(out_new, 4) || !bv::on(out_copies, 4) || (n_new && !bv::on(n_new, 4))) return BV_ERR_INVALID_ARG;
+    if (a.B > bv::kMaxSequences) return BV_ERR_UNSUPPORTED;
+    if (a.B == 0) return BV_OK;
+    a.n_new = n_new;
+    a.n = n;
+    cudaError_t e = cudaFuncSetAttribute(bv::extend_pages_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(bv::ExtendSmem)));
+    if (e == cudaSuccess)
+        e = bv::one_cluster(bv::extend_pages_kernel, a.num_pages, sizeof(bv::ExtendSmem), static_cast<cudaStream_t>(stream), a, out_new, out_copies,
+                            static_cast<int>(bv::on(a.refs, 16)));
+    return bv::done(e, 1);
+}
+
+extern "C" int bv_pages_truncate(const bv_cache* c, const int32_t* keep, const int32_t* n_new, int n, void* stream) {
+    bv::PagesArgs a;
+    const int rc = bv::check(c, &a);
+    if (rc != BV_OK) return rc;
+    if (n < 0 || !keep || !bv::on(keep, 4) || (n_new && !bv::on(n_new, 4))) return BV_ERR_INVALID_ARG;
+    if (a.B == 0) return BV_OK;
+    a.n_new = n_new;
+    a.n = n;
+    bv::truncate_pages_kernel<<<a.B, 128, 0, static_cast<cudaStream_t>(stream)>>>(a, keep);
+    return bv::done(cudaGetLastError(), 1);
+}
+
+extern "C" int bv_pages_fork(const bv_cache* c, const int32_t* src, const int32_t* dst, int forks, int32_t* out_ok, void* stream) {
+    bv::PagesArgs a;
+    const int rc = bv::check(c, &a);
+    if (rc != BV_OK) return rc;
+    if (forks < 0 || !src || !dst || !out_ok || !bv::on(src, 4) || !bv::on(dst, 4) || !bv::on(out_ok, 4)) return BV_ERR_INVALID_ARG;
+    if (forks == 0) return BV_OK;
+    bv::fork_pages_kernel<<<forks, 128, 0, static_cast<cudaStream_t>(stream)>>>(a, src, dst, forks, out_ok);
+    return bv::done(cudaGetLastError(), 1);
+}
+
+extern "C" int bv_pages_compact(const bv_cache* c, int32_t* out_moves, int32_t* out_count, void* stream) {
+    bv::CompactCall call{};
+    const int rc = bv::check(c, &call.a);
+    if (rc != BV_OK) return rc;
+    if (!out_moves || !out_count || !bv::on(out_moves, 4) || !bv::on(out_count, 4)) return BV_ERR_INVALID_ARG;
+    call.moves = out_moves;
+    call.count = out_count;
+    call.stream = static_cast<cudaStream_t>(stream);
+    return bv::with_stream_work(call.stream, bv::compact_scratch, bv::enqueue_compact, &call);
+}
