@@ -8,7 +8,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libbv_b200.so")
 SOURCES = ["bv_api.cu", "bv_stream.cu", "bv_cluster.cu", "bv_flow.cu", "bv_small.cu", "bv_phase.cu", "bv_noalloc.cu", "bv_sample.cu", "bv_loop.cu",
-           "bv_cache.cu", "bv_attend_rows.cu", "bv_pages.cu"]
+           "bv_cache.cu", "bv_attend_rows.cu", "bv_attend_tiles.cu", "bv_pages.cu"]
 HEADERS = ["bv_device.cuh", "bv_launch.h", "bv_flow_common.cuh", "bv_sample_row.cuh", "bv_cache.cuh", os.path.join("..", "..", "include", "bv.h")]
 
 NVCC_FLAGS = [

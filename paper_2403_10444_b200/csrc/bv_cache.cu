@@ -152,14 +152,28 @@ cudaError_t launch_copy(CopyArgs a, const bv_cache& c, cudaStream_t stream) {
 struct AttendCall {
     AttendArgs a;
     int dtype;
-    bool aligned;
-    int ctas;
+    bool aligned, q_vec, tiles;
     cudaStream_t stream;
 };
-int attend_ctas(const AttendCall&, int sm_count) { return sm_count < kCacheCounters ? sm_count : kCacheCounters; }
+// The kernel for every shape, or the one on the tensor cores.
+void plan(AttendCall* c, bool tiles) {
+    AttendArgs& a = c->a;
+    c->tiles = tiles;
+    const int rows = a.n * a.group;
+    if (tiles) {
+        a.rows = attend_tiles_rows(rows);
+        attend_tiles_plan(&a);
+    } else {
+        a.rows = attend_rows_tile(a.D, rows);
+        a.span = attend_rows_keys();
+        a.per_page = 1;
+    }
+}
+int attend_ctas(int sm_count) { return sm_count < kCacheCounters ? sm_count : kCacheCounters; }
 size_t attend_scratch(int sm_count, const void* ctx) {
     const AttendCall& c = *static_cast<const AttendCall*>(ctx);
-    return attend_ctas(c, sm_count) * 2 * part_floats(c.a.rows, c.a.D) * sizeof(float);
+    const int other = attend_rows_tile(c.a.D, c.a.n * c.a.group);         // (should the first kernel not take the call)
+    return attend_ctas(sm_count) * 2 * part_floats(c.a.rows > other ? c.a.rows : other, c.a.D) * sizeof(float);
 }
 int enqueue_attend(const StreamWork& work, void* ctx) {
     AttendCall& c = *static_cast<AttendCall*>(ctx);
@@ -168,7 +182,14 @@ int enqueue_attend(const StreamWork& work, void* ctx) {
     c.a.status = work.status;
     c.a.wait_limit = work.wait_limit;
     c.a.never_signal = work.never_signal;
-    return done(launch_attend_rows(c.a, c.dtype, c.aligned, attend_ctas(c, work.sm_count), c.stream), 1);
+    const int ctas = attend_ctas(work.sm_count);
+    if (c.tiles) {
+        bool taken = false;
+        const cudaError_t e = launch_attend_tiles(c.a, c.q_vec, ctas, c.stream, &taken);
+        if (e != cudaSuccess || taken) return done(e, 1);
+        plan(&c, false);
+    }
+    return done(launch_attend_rows(c.a, c.dtype, c.aligned, ctas, c.stream), 1);
 }
 
 }  // namespace
@@ -237,12 +258,10 @@ extern "C" int bv_cache_attend(const bv_cache* c, const void* q, const int64_t* 
     a.kf = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634073599246810019);
     a.window = window;
     a.sinks = window > 0 ? sinks : 0;
-    a.rows = bv::attend_rows_tile(a.D, n * group);
-    a.row_tiles = (n * group + a.rows - 1) / a.rows;
-    a.span = bv::attend_rows_keys();
-    a.per_page = 1;
     call.dtype = c->dtype;
     call.aligned = bv::vectors(c->k, c->k_stride, c->D, es) && bv::vectors(c->v, c->v_stride, c->D, es);
+    call.q_vec = bv::vectors(q, q_stride, c->D, es);
+    bv::plan(&call, c->dtype == BV_DTYPE_BF16 && call.aligned && bv::attend_tiles_takes(a));
     call.stream = static_cast<cudaStream_t>(stream);
     return bv::with_stream_work(call.stream, bv::attend_scratch, bv::enqueue_attend, &call);
 }

@@ -30,7 +30,6 @@ struct AttendArgs {
     float kf;                 // scale log2(e)
     int window, sinks;
     int rows;                 // query rows of a unit, at most (row = token * group + head of the group)
-    int row_tiles;            // units a key-value head has: ceil(n * group / rows)
     int span;                 // keys of a tile; for pages that are several tiles those of a tile but the last of a page
     int per_page;             // tiles of a page, where a page is more than one (else 1)
     float* part;              // [gridDim.x][2] partial results of part_floats(rows, D)
@@ -266,6 +265,11 @@ __device__ __forceinline__ Leave leave_of(const AttendArgs& a, const Share& sh, 
 // The kernel for every shape (bv_attend_rows.cu): query rows of a unit, keys of a tile.
 int attend_rows_tile(int D, int rows);
 int attend_rows_keys();
+// The kernel on the tensor cores (bv_attend_tiles.cu), for calls that attend_tiles_takes; `taken` is false if no map of the pools could be had.
+bool attend_tiles_takes(const AttendArgs& a);
+int attend_tiles_rows(int rows);
+void attend_tiles_plan(AttendArgs* a);
+cudaError_t launch_attend_tiles(const AttendArgs& a, bool q_vec, int ctas, cudaStream_t stream, bool* taken);
 cudaError_t launch_attend_rows(const AttendArgs& a, int dtype, bool aligned, int ctas, cudaStream_t stream);
 
 }  // namespace bv
