@@ -34,8 +34,8 @@ struct RowsSmem {
     long long row[4][2][kKeys];            // element offsets of the keys' rows, of tiles i .. i+3 (negative: no page)
     float part[kWarps][R][NJ * 32 + 2];
     ShareSmem share;
+    JointSmem joint;
     int bad;
-    unsigned last;
 };
 
 template <typename T, int NJ, int R>
@@ -49,11 +49,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const AttendAr
     const int row_groups = a.rows / R;                     // 1, 2, 4 or 8
     const int key_slices = kWarps / row_groups;
     const int rg = warp % row_groups, ks = warp / row_groups;
-    const size_t part_stride = part_floats(a.rows, a.D);
 
     // (columns D .. kRow of the staged rows are never copied to: they stay zero)
     for (int x = tid; x < static_cast<int>(sizeof(sm.tile) / 16); x += kThreads) reinterpret_cast<uint4*>(&sm.tile[0][0][0])[x] = make_uint4(0, 0, 0, 0);
-    if (tid == 0) sm.bad = 0;
+    if (tid == 0) sm.bad = sm.joint.n = 0;
     const Share sh = find_share<kThreads>(a, sm.share);
     Walk w = walk_begin(a, sh);
 
@@ -223,8 +222,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const AttendAr
         }
         __syncthreads();
         const bool bad = w.s.bad || sm.bad;
-        const Leave lv = leave_of(a, sh, w);
-        float* part = lv.split ? a.part + (2 * static_cast<size_t>(blockIdx.x) + (static_cast<int>(blockIdx.x) == lv.first)) * part_stride : nullptr;
+        float* part = leave_unit(a, sh, w, count, sm.joint, tid);
         for (int x = tid; x < count * a.D; x += kThreads) {
             const int row = x / a.D, d = x - row * a.D;
             const int g = row / R, r = row - g * R;
@@ -246,17 +244,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const AttendAr
                 *dst = from_float<T>(sl == 0.f ? 0.f : so / sl);
             }
         }
-        if (lv.split) {
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                const unsigned n = lv.last - lv.first;
-                sm.last = atomicInc(a.counters + lv.first, n) == n;         // (back to zero with the last one)
-                __threadfence();
-            }
-            __syncthreads();
-            if (sm.last) join_unit<T>(a, w, lv.first, lv.last, tid, kThreads);
-        }
         __syncthreads();
         if (warp == 0) {
             if (lane == 0) sm.bad = 0;
@@ -264,6 +251,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const AttendAr
         }
         walk_next(a, w);
     }
+    join_units<T>(a, sm.joint, tid, kThreads);
 }
 
 template <typename T, int NJ, int R>
@@ -272,8 +260,7 @@ cudaError_t launch(const AttendArgs& a, bool aligned, int ctas, cudaStream_t str
     static_assert(bytes <= 227 * 1024, "fits an SM");
     const cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<T, NJ, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
-    attend_rows_kernel<T, NJ, R><<<ctas, kThreads, bytes, stream>>>(a, aligned);
-    return cudaGetLastError();
+    return launch_together(attend_rows_kernel<T, NJ, R>, ctas, kThreads, bytes, stream, a, static_cast<int>(aligned));
 }
 template <typename T>
 cudaError_t pick(const AttendArgs& a, bool aligned, int ctas, cudaStream_t stream) {

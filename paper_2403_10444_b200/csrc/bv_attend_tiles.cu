@@ -106,7 +106,7 @@ struct Shape {
     static constexpr int kSlot = kTile * 128 * NP;                       // bytes of a slot: NP panels of 128 rows of 64 columns
     static constexpr int kPanel = kTile * 128;
     static constexpr int kQ = NP * N * 128, kP = N * kTile * 2;
-    static constexpr int kRest = 3072;
+    static constexpr int kRest = N > 64 ? 4096 : 3072;
     static constexpr int kFit = (227 * 1024 - kRest - kQ - kP) / kSlot;
     static constexpr int kSlots = kFit < 8 ? kFit : 8;
     static constexpr int kColumns = 3 * N <= 64 ? 64 : 3 * N <= 128 ? 128 : 3 * N <= 256 ? 256 : 512;      // of tensor memory: S twice, O
@@ -126,7 +126,7 @@ struct __align__(1024) Smem {
     ShareSmem share;
     uint32_t tmem;
     int abort, fix;
-    unsigned last;
+    JointSmem joint;
 };
 
 struct Geometry {      // of a tile
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
         mbar_init(smem_u32(&sm.q_full), kSoft);
         mbar_init(smem_u32(&sm.drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        sm.abort = sm.fix = 0;
+        sm.abort = sm.fix = sm.joint.n = 0;
     }
     if (warp == kIssuer) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)), "n"(Sh::kColumns) : "memory");
@@ -302,7 +302,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
         __syncwarp();
     } else {
         // ---- weights
-        const size_t part_stride = part_floats(a.rows, a.D);
         const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
         const int key = tid;                   // of a tile
         // the element of O that this thread has: with 64 of them a warp has 16, in its lower lanes
@@ -500,8 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
             }
             bad = soft_any(bad || failed || gone);
             const bool fix = *static_cast<volatile int*>(&sm.fix) != 0;
-            const Leave lv = leave_of(a, sh, w);
-            float* part = lv.split ? a.part + (2 * static_cast<size_t>(blockIdx.x) + (static_cast<int>(blockIdx.x) == lv.first)) * part_stride : nullptr;
+            float* part = leave_unit(a, sh, w, count, sm.joint, tid);
             if (part && tid < count) {
                 part[tid] = -sm.nref[tid];
                 part[a.rows + tid] = bad ? NAN : sm.part[0][tid] + sm.part[1][tid] + sm.part[2][tid] + sm.part[3][tid];
@@ -548,17 +546,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
                 }
             }
             fence_before();
-            if (lv.split) {
-                __threadfence();
-                soft_sync();
-                if (tid == 0) {
-                    const unsigned n = lv.last - lv.first;
-                    sm.last = atomicInc(a.counters + lv.first, n) == n;         // (back to zero with the last one)
-                    __threadfence();
-                }
-                soft_sync();
-                if (sm.last) join_unit<__nv_bfloat16>(a, w, lv.first, lv.last, tid, kSoft);
-            }
             soft_sync();
             if (tid == 0) sm.fix = 0;
         }
@@ -567,6 +554,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
     __syncthreads();
     fence_after();
     if (warp == kIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Sh::kColumns) : "memory");
+    join_units<__nv_bfloat16>(a, sm.joint, tid, kThreads);
 }
 
 // ---- launch ------------------------------------------------------------------------------------------------------------
@@ -601,8 +589,7 @@ template <int NP, int N>
 cudaError_t launch(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, bool q_vec, int ctas, cudaStream_t stream) {
     const cudaError_t e = cudaFuncSetAttribute(attend_tiles_kernel<NP, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<NP, N>::kBytes);
     if (e != cudaSuccess) return e;
-    attend_tiles_kernel<NP, N><<<ctas, kThreads, Shape<NP, N>::kBytes, stream>>>(a, k, v, q_vec);
-    return cudaGetLastError();
+    return launch_together(attend_tiles_kernel<NP, N>, ctas, kThreads, Shape<NP, N>::kBytes, stream, a, k, v, static_cast<int>(q_vec));
 }
 template <int NP>
 cudaError_t pick(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, bool q_vec, int ctas, cudaStream_t stream) {

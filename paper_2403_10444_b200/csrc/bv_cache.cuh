@@ -33,7 +33,7 @@ struct AttendArgs {
     int span;                 // keys of a tile; for pages that are several tiles those of a tile but the last of a page
     int per_page;             // tiles of a page, where a page is more than one (else 1)
     float* part;              // [gridDim.x][2] partial results of part_floats(rows, D)
-    unsigned* counters;       // [gridDim.x] CTAs that have left their part of the unit that a CTA's last tiles belong to; zero between launches
+    unsigned* counters;       // [gridDim.x] by the first CTA of a unit that several have: those that have come, then gone; zero between launches
     int* status;              // set if a bounded wait gave up
     unsigned wait_limit;
     int never_signal;
@@ -212,7 +212,7 @@ __device__ __forceinline__ void walk_next(const AttendArgs& a, Walk& w) {
 }
 __device__ __forceinline__ int tile_at(const Span& u, int i) { return i < u.sink ? i : u.first + i - u.sink; }
 
-// Which CTAs hold tiles of the unit, the first and the last of them.
+// The CTA that holds a tile of the list.
 __device__ __forceinline__ int holder_of(const Share& sh, long long tile) {
     return static_cast<int>(((tile + 1) * sh.ctas - 1) / sh.total);
 }
@@ -223,43 +223,141 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(f
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// The unit's rows from the parts that CTAs `first` to `last` left: out = sum_c 2^{m_c - M} O_c / sum_c 2^{m_c - M} l_c, in the order of the
-// CTAs, so that the result does not depend on who finishes last.
-template <typename T>
-__device__ __forceinline__ void join_unit(const AttendArgs& a, const Walk& w, int first, int last, int tid, int threads) {
+// ---- units that several CTAs hold tiles of -----------------------------------------------------------------------------
+
+// Each CTA leaves what it has of such a unit (at most two: its first and its last) in `part`: per row the reference m and the sum l, then
+// O.  At its end it reports, waits until the unit's other CTAs have (their parts of the list are equal, so they end at about the same time;
+// the launch is cooperative, so they all run), and forms its share of the unit's elements from all parts:
+//   out = sum_c 2^{m_c - M} O_c / sum_c 2^{m_c - M} l_c,   M = max_c m_c,
+// in an order that does not depend on who came when.  (Joined by the last CTA alone, 148 parts of 36 rows took 2.5 ms, and the
+// two or three parts that most units of a batch are cut into 0.3 ms in all: one SM has too few loads under way.)
+struct Joint {
+    int b, h, r0, count;      // the unit
+    int first, last;          // the CTAs that have tiles of it
+};
+struct JointSmem {
+    Joint unit[2];
+    int n;                    // units left so far; zero at the start
+    int ok[2];
+};
+// Is the unit one of several CTAs?  Then where this one's part goes, and a note of it (by thread `tid` 0; visible to the CTA behind its next barrier).
+__device__ __forceinline__ float* leave_unit(const AttendArgs& a, const Share& sh, const Walk& w, int count, JointSmem& js, int tid) {
+    if (w.i == 0 && w.upto == w.u.tiles) return nullptr;
+    const int c = blockIdx.x;
+    const int first = w.i == 0 ? c : holder_of(sh, w.unit_at), last = w.upto == w.u.tiles ? c : holder_of(sh, w.unit_at + w.u.tiles - 1);
+    if (tid == 0) js.unit[js.n++] = Joint{w.b, w.h, w.r0, count, first, last};
+    return a.part + (2 * static_cast<size_t>(c) + (c == first)) * part_floats(a.rows, a.D);
+}
+
+template <typename T, int W>
+__device__ __forceinline__ void join_share(const AttendArgs& a, const Joint& u, int tid, int threads) {
+    const int parts = u.last - u.first + 1, k = blockIdx.x - u.first, per_row = a.D / W;
+    const int all = u.count * per_row;
+    const int e0 = static_cast<int>(static_cast<long long>(all) * k / parts), e1 = static_cast<int>(static_cast<long long>(all) * (k + 1) / parts);
+    // few elements and many parts: several lanes share an element, each with some of the parts
+    int lanes = 1;
+    while (lanes < 32 && 2 * lanes * (e1 - e0) <= threads && lanes < parts) lanes *= 2;
+    const int sub = tid & (lanes - 1);
     const size_t stride = part_floats(a.rows, a.D);
-    const int count = (w.r0 + a.rows < w.s.rows ? a.rows : w.s.rows - w.r0);
-    for (int x = tid; x < count * a.D; x += threads) {
-        const int row = x / a.D, d = x - row * a.D;
+    const float* const base = a.part + 2 * static_cast<size_t>(u.first) * stride;      // part c lies at 2 c, but that of the first CTA at 2 c + 1
+    for (int x = e0; x < e1; x += threads / lanes) {
+        const int e = x + tid / lanes;
+        const bool mine = e < e1;
+        const int row = mine ? e / per_row : 0, d = mine ? (e - row * per_row) * W : 0;
         float M = -INFINITY;
         bool nan = false;
-        for (int c = first; c <= last; ++c) {
-            const float m = __ldcg(a.part + (2 * static_cast<size_t>(c) + (c == first)) * stride + row);
+#pragma unroll 4
+        for (int c = sub; c < parts; c += lanes) {
+            const float m = __ldcg(base + (2 * c + (c == 0)) * stride + row);
             nan |= m != m;
             M = fmaxf(M, m);
         }
-        float l = 0.f, o = 0.f;
-        for (int c = first; c <= last; ++c) {
-            const float* p = a.part + (2 * static_cast<size_t>(c) + (c == first)) * stride;
-            const float m = __ldcg(p + row);
-            if (m == -INFINITY) { l += __ldcg(p + a.rows + row); continue; }       // (nothing visible there: zero; or a page that is none: NaN)
-            const float f = exp2f(m - M);
-            l += f * __ldcg(p + a.rows + row);
-            o += f * __ldcg(p + 2 * a.rows + static_cast<size_t>(row) * a.D + d);
+        for (int o = 1; o < lanes; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+        float l = 0.f, o[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) o[i] = 0.f;
+#pragma unroll 4
+        for (int c = sub; c < parts; c += lanes) {
+            const float* p = base + (2 * c + (c == 0)) * stride;
+            const float m = __ldcg(p + row), pl = __ldcg(p + a.rows + row);
+            const float f = m == -INFINITY ? 0.f : exp2f(m - M);
+            l += m == -INFINITY ? pl : f * pl;              // (nothing visible there: zero; a page that is none: NaN)
+            float v[W];
+            if constexpr (W == 4) {
+                const float4 x4 = __ldcg(reinterpret_cast<const float4*>(p + 2 * a.rows + static_cast<size_t>(row) * a.D + d));
+                v[0] = x4.x; v[1] = x4.y; v[2] = x4.z; v[3] = x4.w;
+            } else {
+                v[0] = __ldcg(p + 2 * a.rows + static_cast<size_t>(row) * a.D + d);
+            }
+#pragma unroll
+            for (int i = 0; i < W; ++i) o[i] += f * v[i];
         }
-        const int r = w.r0 + row, t = r / a.group, g = r - t * a.group;
-        T* dst = static_cast<T*>(a.out) + w.b * a.os[0] + t * a.os[1] + (w.h * a.group + g) * a.os[2] + d;
-        *dst = from_float<T>(nan ? NAN : l == 0.f ? 0.f : o / l);
+        if (nan) l = NAN;
+        for (int s = 1; s < lanes; s <<= 1) {
+            l += __shfl_xor_sync(0xffffffffu, l, s);
+#pragma unroll
+            for (int i = 0; i < W; ++i) o[i] += __shfl_xor_sync(0xffffffffu, o[i], s);
+        }
+        if (mine && sub == 0) {
+            const int r = u.r0 + row, t = r / a.group;
+            T* dst = static_cast<T*>(a.out) + u.b * a.os[0] + t * a.os[1] + (u.h * a.group + r - t * a.group) * a.os[2] + d;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+            for (int i = 0; i < W; ++i) dst[i] = from_float<T>(l == 0.f ? 0.f : o[i] * inv);
+        }
     }
 }
-// Who holds tiles of the unit: CTAs `first` to `last`; `split`: others than this one too.
-struct Leave { int first, last; bool split; };
-__device__ __forceinline__ Leave leave_of(const AttendArgs& a, const Share& sh, const Walk& w) {
-    Leave l;
-    l.split = w.i > 0 || w.upto < w.u.tiles;
-    l.first = holder_of(sh, w.unit_at);
-    l.last = holder_of(sh, w.unit_at + w.u.tiles - 1);
-    return l;
+// The end of a CTA: all its threads, its parts written.
+template <typename T>
+__device__ __forceinline__ void join_units(const AttendArgs& a, JointSmem& js, int tid, int threads) {
+    __syncthreads();
+    const int n = js.n;
+    if (n == 0) return;
+    unsigned* counter = nullptr;
+    unsigned parts = 0;
+    if (tid < n) {
+        counter = a.counters + js.unit[tid].first;
+        parts = js.unit[tid].last - js.unit[tid].first + 1;
+        __threadfence();
+        atomicInc(counter, 2 * parts - 1);    // `parts` have come, as many go: back to zero with the last one
+        const unsigned limit = a.wait_limit ? a.wait_limit : 1u << 22;
+        unsigned v = 0;
+        for (unsigned i = 0; i <= limit; ++i) {
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
+            if (v >= parts) break;
+        }
+        js.ok[tid] = v >= parts;
+        if (v < parts) atomicExch(a.status, 1);
+        __threadfence();
+    }
+    __syncthreads();
+    for (int j = 0; j < n; ++j) {
+        if (!js.ok[j]) continue;              // (the status says so: the outputs are not to be used)
+        if (a.D % 4 == 0) join_share<T, 4>(a, js.unit[j], tid, threads);
+        else join_share<T, 1>(a, js.unit[j], tid, threads);
+    }
+    __syncthreads();
+    if (tid < n) atomicInc(counter, 2 * parts - 1);
+}
+
+// A cooperative launch of as many of `ctas` CTAs as can run at once (a process that is given a part of the GPU has fewer).
+template <typename... P, typename... A>
+cudaError_t launch_together(void (*kernel)(P...), int ctas, int threads, size_t smem, cudaStream_t stream, A... args) {
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeCooperative;
+    at.val.cooperative = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    for (;; ctas /= 2) {
+        cfg.gridDim = dim3(ctas);
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+        if (e != cudaErrorCooperativeLaunchTooLarge || ctas == 1) return e;
+        cudaGetLastError();
+    }
 }
 
 // The kernel for every shape (bv_attend_rows.cu): query rows of a unit, keys of a tile.
