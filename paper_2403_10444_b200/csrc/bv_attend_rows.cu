@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const AttendAr
     // (columns D .. kRow of the staged rows are never copied to: they stay zero)
     for (int x = tid; x < static_cast<int>(sizeof(sm.tile) / 16); x += kThreads) reinterpret_cast<uint4*>(&sm.tile[0][0][0])[x] = make_uint4(0, 0, 0, 0);
     if (tid == 0) sm.bad = sm.joint.n = 0;
-    const Share sh = find_share<kThreads>(a, sm.share);
+    const Share sh = find_share(a, sm.share, kThreads);
     Walk w = walk_begin(a, sh);
 
     while (w.more) {
@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const AttendAr
         for (int r = 0; r < R; ++r) {
             const int row = w.r0 + rg * R + r;
             const bool valid = rg * R + r < count;
-            const int t = valid ? row / a.group : 0, g = valid ? row - t * a.group : 0;
+            const int t = valid ? a.by_group(row) : 0, g = valid ? row - t * a.group : 0;
             pos[r] = valid ? w.s.base + t : -1;
             low[r] = valid ? low_of(a, pos[r]) : 0;
             const T* src = static_cast<const T*>(a.q) + w.b * a.qs[0] + t * a.qs[1] + (w.h * a.group + g) * a.qs[2];
@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const AttendAr
             for (int x = 0; x < NJ * 4; ++x) acc[r][x] = 0.f;
         }
         // what all of the unit's rows see, and what none of them does
-        const int p0 = w.s.base + w.r0 / a.group, p1 = w.s.base + (w.r0 + count - 1) / a.group;
+        const int p0 = w.s.base + a.by_group(w.r0), p1 = w.s.base + a.by_group(w.r0 + count - 1);
         const int low0 = low_of(a, p0), low1 = low_of(a, p1);
 
         // the rows of tile i's keys (one warp; -1: beyond what anybody sees, -2: a page that is none)
@@ -96,10 +96,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const AttendAr
             if (i >= nt) return;
             const int p = tile_at(w.u, w.i + i) * kKeys + lane;
             if (p > p1 || !(p >= low0 || p < a.sinks)) return;
-            const int page = __ldg(a.table + static_cast<long long>(w.b) * a.width + p / a.page);
+            const int j = a.by_page(p);
+            const int page = __ldg(a.table + static_cast<long long>(w.b) * a.width + j);
             if (page < 0 || page >= a.num_pages) { ko = -2; return; }
-            ko = page * a.ks[0] + w.h * a.ks[1] + p % a.page * a.ks[2];
-            vo = page * a.vs[0] + w.h * a.vs[1] + p % a.page * a.vs[2];
+            ko = page * a.ks[0] + w.h * a.ks[1] + (p - j * a.page) * a.ks[2];
+            vo = page * a.vs[0] + w.h * a.vs[1] + (p - j * a.page) * a.vs[2];
         };
         auto put_rows = [&](int i, long long ko, long long vo) {
             sm.row[i & 3][0][lane] = ko;
@@ -239,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const AttendAr
                 part[2 * a.rows + static_cast<size_t>(row) * a.D + d] = so;
                 if (d == 0) { part[row] = M; part[a.rows + row] = sl; }
             } else {
-                const int at = w.r0 + row, t = at / a.group;
+                const int at = w.r0 + row, t = a.by_group(at);
                 T* dst = static_cast<T*>(a.out) + w.b * a.os[0] + t * a.os[1] + (w.h * a.group + at - t * a.group) * a.os[2] + d;
                 *dst = from_float<T>(sl == 0.f ? 0.f : so / sl);
             }

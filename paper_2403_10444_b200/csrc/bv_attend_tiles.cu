@@ -1,25 +1,26 @@
 // Attention over a paged cache in 16 bits on the tensor cores: bv_cache_attend for bf16, D a multiple of 8 up to 128, pages of a
 // multiple of 8 tokens, rows at 16-byte strides.
 //
-// A unit is one key-value head of a sequence with N query rows (the heads of its group times the block's tokens: 1 to some 100), a tile
-// 128 keys.  Keys are the large side, so they take the M side of the matrix instructions and nothing is padded but N to 16:
+// A unit is one key-value head of a sequence with up to N query rows (the heads of its group times the block's tokens), a tile
+// 128 keys.  Keys are the large side, so they take the M side of the matrix instructions and nothing is padded but N, to 16:
 //   S^T [128 keys, N] = K Q^T            K as it lies in its pages, K-major
 //   O^T [D, N]       += V^T P            V as it lies in its pages, M-major; P [128 keys, N] from shared memory
-// One warp loads (TMA, a box per page and 64 columns, 128-byte swizzle, a ring of slots that hold a tile's keys or its values), one thread
-// issues the matrix instructions, four warps turn S into P: a thread has one key and goes over the N rows, so the mask, the
-// exponential and the rounding need no other lane.  What softmax usually needs across lanes is avoided: each row has an integer
-// reference m in shared memory, weights are 2^{k s - m}, and only where some score exceeds its reference by more than 8 (a vote
-// per tile) the new maxima are formed, and O and the sums scaled by the power of two between the old and the new reference.
-// Sums stay per thread until a unit ends.  Weights are rounded to 16 bits for the second product, and the sums are taken of
-// the rounded weights: a row of one key is that key's value exactly, and the error of a row, 2^-9 of its terms at most, is that
-// of an output rounded once more.
-//
-// Bound: HBM.  A tile of D = 128 is 64 KB, 2850 clocks of an SM's share of the copy bandwidth; the two products take 8 instructions
-// each (S: 128 x N x 128), the four warps some 5 N instructions.  The ring holds up to 192 KB, three tiles.
+// Two warps load (TMA, a box per page and 64 columns, 128-byte swizzle, a ring of slots that hold a tile's keys or its values), one
+// thread issues the matrix instructions, four warps turn S into P: a thread has one key and goes over the N rows, so the
+// mask, the exponential and the rounding need no other lane.  What softmax usually needs across lanes is avoided: each row has an
+// integer reference m in shared memory, weights are 2^{k s - m}, and only where some score exceeds its reference by more than 8
+// (a vote per tile) the new maxima are formed, and O and the sums scaled by the power of two between the old and the new
+// reference.  Sums stay per thread until a unit ends.  Weights are rounded to 16 bits for the second product, and the sums are taken of the rounded weights: a row of one
+// key is that key's value exactly, and the error of a row, 2^-9 of its terms at most, is that of an output rounded once more.
+// The next unit's query rows come in while a unit is gone through, and its first scores before the unit's last products.
 //
 // What a row may not see is taken out twice: its weight is 0 whatever the score is, and rows of V that no row of the unit sees (or that were never
 // loaded) are set to 0 in shared memory, since 0 times an infinity is not 0.  Rows of V that some see and others do not keep their finite
 // elements there; the others are added where they belong when the unit ends, from global memory.
+//
+// Steps that a CTA takes once or a few times (first maxima, masks, ends of units) are loops of 16 rows rather than code for N: fetching
+// instructions that ran never before costs a CTA more than running them (with everything unrolled a unit of 80 rows took 65000
+// clocks beyond its tiles).
 #include <cuda.h>
 
 #include "bv_cache.cuh"
@@ -28,8 +29,8 @@
 namespace bv {
 namespace {
 
-constexpr int kThreads = 192, kSoft = 128, kTile = 128;
-constexpr int kProducer = 4, kIssuer = 5;                       // warps; 0 .. 3 are the softmax's
+constexpr int kThreads = 224, kSoft = 128, kTile = 128;
+constexpr int kKeys = 4, kValues = 5, kIssuer = 6;               // warps: loads of keys, of values, products; 0 .. 3 are the softmax's
 constexpr float kNone = -3.0e38f;                               // the reference of a row that has seen no score
 constexpr float kLag = 8.f;                                     // how far a score may exceed its reference
 
@@ -89,9 +90,13 @@ __device__ __forceinline__ float ex2(float x) {
 }
 
 // Shared-memory descriptors: start address, leading and stride byte offsets in units of 16 bytes, version 1, layout (2: 128-byte swizzle,
-// 0: none).
-__device__ __forceinline__ uint64_t describe(uint32_t addr, uint32_t lead, uint32_t stride, uint64_t layout) {
-    return static_cast<uint64_t>((addr & 0x3ffff) >> 4) | static_cast<uint64_t>(lead >> 4) << 16 | static_cast<uint64_t>(stride >> 4) << 32 | 1ull << 46 | layout << 61;
+// 0: none).  The start address is the low word's; the rest is known when compiling but for 14 bits of the leading offset.
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t lead) { return (addr & 0x3ffff) >> 4 | (lead >> 4) << 16; }
+__host__ __device__ constexpr uint32_t desc_high(uint32_t stride, uint32_t layout) { return stride >> 4 | 1u << 14 | layout << 29; }
+__device__ __forceinline__ uint64_t desc(uint32_t low, uint32_t high) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(low), "r"(high));
+    return d;
 }
 // Instruction descriptor: 32-bit sums, bf16 operands; which operands are M / N-major; the sizes.
 __host__ __device__ constexpr uint32_t instruction(int M, int N, bool a_m, bool b_n) {
@@ -103,49 +108,72 @@ __host__ __device__ constexpr uint32_t instruction(int M, int N, bool a_m, bool 
 
 template <int NP, int N>
 struct Shape {
-    static constexpr int kSlot = kTile * 128 * NP;                       // bytes of a slot: NP panels of 128 rows of 64 columns
-    static constexpr int kPanel = kTile * 128;
+    static constexpr int kPanel = kTile * 128, kSlot = NP * kPanel;      // a slot: NP panels of 128 rows of 64 columns
     static constexpr int kQ = NP * N * 128, kP = N * kTile * 2;
-    static constexpr int kRest = N > 64 ? 4096 : 3072;
-    static constexpr int kFit = (227 * 1024 - kRest - kQ - kP) / kSlot;
+    static constexpr int kRest = 3072;
+    // two buffers for the weights (the next tile's are formed while the last one's are multiplied) where that leaves five slots
+    static constexpr int kTwo = (227 * 1024 - kRest - 2 * kQ - 2 * kP) / kSlot;
+    static constexpr int kBuffers = kTwo >= 5 ? 2 : 1;
+    static constexpr int kFit = (227 * 1024 - kRest - 2 * kQ - kBuffers * kP) / kSlot;
     static constexpr int kSlots = kFit < 8 ? kFit : 8;
-    static constexpr int kColumns = 3 * N <= 64 ? 64 : 3 * N <= 128 ? 128 : 3 * N <= 256 ? 256 : 512;      // of tensor memory: S twice, O
-    static constexpr int kBytes = kSlots * kSlot + kQ + kP + kRest;
+    static constexpr int kColumns = 3 * N <= 64 ? 64 : 3 * N <= 128 ? 128 : 256;      // of tensor memory: S twice, O
+    static constexpr int kBytes = kSlots * kSlot + 2 * kQ + kBuffers * kP + kRest;
     static_assert(kSlots >= 4, "two tiles in flight");
 };
+constexpr int kUnits = 8;                      // units that may be in flight: no more than slots
 template <int NP, int N>
 struct __align__(1024) Smem {
     using Sh = Shape<NP, N>;
     char ring[Sh::kSlots][Sh::kSlot];
-    char q[Sh::kQ];
-    char p[Sh::kP];
-    float nref[N], factor[N];                  // minus the references; what the last move of the references scales by
-    float part[4][N];                          // maxima, at the end sums, by warp
-    int pos[N], low[N];                        // the rows' positions, and the first positions of their windows
-    unsigned long long full[8], empty[8], s_full[2], p_full, p_done, q_full, drain;
+    char q[2][Sh::kQ];
+    char p[Sh::kBuffers][Sh::kP];
+    float nref[N];                             // minus the references
+    float part[4][N];                          // maxima by warp; then in part[0] what the move of the references scales by
+    unsigned long long full[8], empty[8], s_full[2], p_full[2], p_done[2], q_full, drain;
     ShareSmem share;
+    JointSmem joint;
     uint32_t tmem;
     int abort, fix;
-    JointSmem joint;
+    int bad[kUnits];                           // units that name a page that is none
 };
 
-struct Geometry {      // of a tile
-    int start, keys;   // its first position, its keys
+// Sees of a unit: positions p0 to p1 are its rows', low0 and low1 the first positions of the first and the last row's windows.
+struct View {
+    int count, p0, p1, low0, low1;
+    int j0, j1, js;            // pages j0 .. j1, and those before js, hold what its rows see
 };
-__device__ __forceinline__ Geometry geometry(const AttendArgs& a, int tile) {
-    Geometry g;
-    g.start = tile_start(a, tile);
-    g.keys = a.span;
-    if (a.per_page > 1) {
-        const int left = a.page - tile % a.per_page * a.span;
-        if (left < g.keys) g.keys = left;
-    }
-    return g;
+__device__ __forceinline__ View view_of(const AttendArgs& a, const Walk& w) {
+    View v;
+    v.count = w.r0 + a.rows < w.s.rows ? a.rows : w.s.rows - w.r0;
+    v.p0 = w.s.base + a.by_group(w.r0);
+    v.p1 = w.s.base + a.by_group(w.r0 + v.count - 1);
+    v.low0 = low_of(a, v.p0);
+    v.low1 = low_of(a, v.p1);
+    v.j0 = a.by_page(v.low0);
+    v.j1 = v.p1 < 0 ? -1 : a.by_page(v.p1);
+    v.js = a.sinks > 0 ? a.by_page(a.sinks - 1) + 1 : 0;
+    return v;
 }
-// Is page j of a sequence one that the unit's rows see some of?
-__device__ __forceinline__ bool page_seen(const AttendArgs& a, int j, int p1, int low0) {
-    const long long begin = static_cast<long long>(j) * a.page;
-    return begin <= p1 && (begin + a.page > low0 || begin < a.sinks);
+__device__ __forceinline__ bool any_sees(const AttendArgs& a, const View& v, int p) { return p <= v.p1 && (p >= v.low0 || p < a.sinks); }
+__device__ __forceinline__ bool all_see(const AttendArgs& a, const View& v, int p) { return p <= v.p0 && (p >= v.low1 || p < a.sinks); }
+// Keys of a tile, its first position.
+__device__ __forceinline__ int tile_keys(const AttendArgs& a, int tile, int* start) {
+    *start = tile_start(a, tile);
+    if (a.per_page == 1) return a.span;
+    const int left = a.page - tile % a.per_page * a.span;
+    return left < a.span ? left : a.span;
+}
+__device__ __forceinline__ bool whole_tile(const AttendArgs& a, const View& v, int start, int keys) {
+    return start + keys - 1 <= v.p0 && (start >= v.low1 || start + keys <= a.sinks);
+}
+
+// The largest of the lanes' values (as integers that are in the order of the values).
+__device__ __forceinline__ float warp_max(float x) {
+    int i = __float_as_int(x);
+    i ^= (i >> 31) & 0x7fffffff;
+    i = __reduce_max_sync(0xffffffffu, i);
+    i ^= (i >> 31) & 0x7fffffff;
+    return __int_as_float(i);
 }
 
 // Sums over the lanes of 16 or 32 values each: lane x ends up with the sum of value x (of x % 16).
@@ -165,13 +193,161 @@ template <int W> __device__ __forceinline__ float across(float* v, int lane) {
     }
     return v[0];
 }
-// The largest of the lanes' values (as integers that are in the order of the values).
-__device__ __forceinline__ float warp_max(float x) {
-    int i = __float_as_int(x);
-    i ^= (i >> 31) & 0x7fffffff;
-    i = __reduce_max_sync(0xffffffffu, i);
-    i ^= (i >> 31) & 0x7fffffff;
-    return __int_as_float(i);
+
+// ---- the parts of a CTA ------------------------------------------------------------------------------------------------
+
+// Loads: the keys' warp fills the even slots of the ring's order, the values' warp the odd ones.
+template <int NP, int N>
+__device__ __forceinline__ void load_tiles(const AttendArgs& a, Smem<NP, N>& sm, Walk w, const CUtensorMap* map, int which, uint32_t limit) {
+    using Sh = Shape<NP, N>;
+    const int lane = threadIdx.x & 31;
+    const int rows = a.page < kTile ? a.page : kTile;                    // of a box
+    const int per = a.per_page > 1 ? 1 : a.by_page(a.span);              // pages of a tile
+    int x = which, unit = 0;                   // the slot's number in the ring's order
+    bool ok = true;
+#pragma unroll 1
+    for (; w.more && ok; walk_next(a, w), ++unit) {
+        const View v = view_of(a, w);
+        const int32_t* row = a.table + static_cast<long long>(w.b) * a.width;
+        auto entry = [&](int i) {              // this lane's page of tile i: -1 none to be seen, -2 none at all
+            if (i >= w.upto || lane >= per) return -1;
+            const int tile = tile_at(w.u, i);
+            const int j = a.per_page > 1 ? tile / a.per_page : tile * per + lane;
+            if (j > v.j1 || (j < v.j0 && j >= v.js)) return -1;
+            const int page = __ldg(row + j);
+            return page < 0 || page >= a.num_pages ? -2 : page;
+        };
+        int next = entry(w.i);
+#pragma unroll 1
+        for (int i = w.i; i < w.upto && ok; ++i, x += 2) {
+            const int page = next;
+            next = entry(i + 1);
+            const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
+            if (__any_sync(0xffffffffu, page == -2) && lane == 0) sm.bad[unit % kUnits] = 1;
+            const int slot = x % Sh::kSlots;
+            ok = __all_sync(0xffffffffu, mbar_wait_now(smem_u32(&sm.empty[slot]), (x / Sh::kSlots & 1) ^ 1, a.status, limit));
+            if (!ok) break;
+            const uint32_t bar = smem_u32(&sm.full[slot]);
+            if (lane == 0) mbar_arrive_expect(bar, __popc(there) * rows * 128 * NP);
+            __syncwarp();
+            if (page >= 0) {
+                const int token = a.per_page > 1 ? tile_at(w.u, i) % a.per_page * a.span : 0;
+#pragma unroll
+                for (int p = 0; p < NP; ++p) tma_load(smem_u32(sm.ring[slot]) + p * Sh::kPanel + lane * rows * 128, map, p * 64, token, w.h, page, bar);
+            }
+        }
+    }
+    // (a launch that gave up leaves when its copies are in)
+    if (!ok)
+        for (int y = x >= Sh::kSlots ? x - Sh::kSlots : which; y < x; ++y)
+            if ((y & 1) == which) mbar_wait_now(smem_u32(&sm.full[y % Sh::kSlots]), y / Sh::kSlots & 1, a.status, limit);
+}
+
+// The products, by one thread: S of a tile before O of the one before it.
+template <int NP, int N>
+__device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>& sm, Walk w, int total, uint32_t tmem, uint32_t limit) {
+    using Sh = Shape<NP, N>;
+    constexpr uint32_t qk = instruction(kTile, N, false, false), pv = instruction(64 * NP, N, true, true);
+    const uint32_t ring = smem_u32(sm.ring), o_at = tmem + 2 * N;
+    bool ok = true;
+    auto wait = [&](unsigned long long& bar, int phase) { ok = ok && mbar_wait_now(smem_u32(&bar), phase & 1, a.status, limit); };
+    int unit = 0, left = w.upto - w.i;         // of the tile whose scores come next
+    unsigned starts = 0;                       // bit t & 1: tile t is its unit's first
+    uint32_t q_low = 0;
+    auto scores = [&](int t) {
+        bool first = t == 0;
+        if (left == 0) {
+            walk_next(a, w);
+            left = w.upto - w.i;
+            ++unit;
+            first = true;
+        }
+        --left;
+        if (first) {
+            wait(sm.q_full, unit);
+            q_low = desc_low(smem_u32(sm.q[unit & 1]), 16);
+        }
+        starts = (starts & ~(1u << (t & 1))) | static_cast<unsigned>(first) << (t & 1);
+        const int slot = 2 * t % Sh::kSlots;
+        wait(sm.full[slot], 2 * t / Sh::kSlots);
+        if (!ok) return;
+        fence_after();
+        const uint32_t k_low = desc_low(ring + slot * Sh::kSlot, 16), s_at = tmem + (t & 1) * N;
+#pragma unroll
+        for (int i = 0; i < 4 * NP; ++i)
+            mma(s_at, desc(k_low + (i / 4 * Sh::kPanel + i % 4 * 32) / 16, desc_high(1024, 2)), desc(q_low + (i / 4 * N * 128 + i % 4 * 32) / 16, desc_high(1024, 2)), qk, i > 0);
+        commit(smem_u32(&sm.empty[slot]));
+        if (a.never_signal != 1) commit(smem_u32(&sm.s_full[t & 1]));
+    };
+    if (total > 0) scores(0);
+#pragma unroll 1
+    for (int g = 0; g < total && ok; ++g) {
+        if (g + 1 < total) scores(g + 1);
+        const int x = 2 * g + 1, slot = x % Sh::kSlots;
+        wait(sm.full[slot], x / Sh::kSlots);
+        const int buffer = g % Sh::kBuffers;
+        wait(sm.p_full[buffer], g / Sh::kBuffers);
+        if (!ok) break;
+        fence_after();
+        const uint32_t p_low = desc_low(smem_u32(sm.p[buffer]), 128);
+        const uint32_t v_low = desc_low(ring + slot * Sh::kSlot, Sh::kPanel);
+        const uint32_t add = !(starts >> (g & 1) & 1);
+#pragma unroll
+        for (int j = 0; j < kTile / 16; ++j) mma(o_at, desc(v_low + j * 128, desc_high(1024, 2)), desc(p_low + j * 16, desc_high(2048, 0)), pv, add || j > 0);
+        commit(smem_u32(&sm.empty[slot]));
+        commit(smem_u32(&sm.p_done[buffer]));
+    }
+    if (!ok) {
+        commit(smem_u32(&sm.drain));
+        mbar_wait_now(smem_u32(&sm.drain), 0, a.status, limit);
+    }
+}
+
+// A unit's query rows, swizzled like the keys; zero beyond its rows and beyond D.  They are there when the copies are (fetched_queries).
+template <int NP, int N>
+__device__ __forceinline__ void fetch_queries(const AttendArgs& a, char* to, const Walk& w, int count, int q_vec, int tid) {
+    constexpr int per_row = NP * 8;
+    const int c = tid % per_row;
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + w.b * a.qs[0] + w.h * a.group * a.qs[2] + c * 8;
+#pragma unroll 1
+    for (int row = tid / per_row; row < N; row += kSoft / per_row) {
+        const uint32_t dst = smem_u32(to) + c / 8 * (N * 128) + row * 128 + ((c % 8) ^ (row & 7)) * 16;
+        const int r = w.r0 + row, t = a.by_group(r);
+        const __nv_bfloat16* from = src + t * a.qs[1] + (r - t * a.group) * a.qs[2];
+        const bool there = row < count && c * 8 < a.D;
+        if (q_vec && there) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(from) : "memory");
+        } else {
+            uint4 val = make_uint4(0, 0, 0, 0);
+            if (there) {
+                const uint16_t* e = reinterpret_cast<const uint16_t*>(from);
+                val = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+            }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(val.x), "r"(val.y), "r"(val.z), "r"(val.w) : "memory");
+        }
+    }
+    cp_async_commit();
+}
+__device__ __forceinline__ void fetched_queries(unsigned long long& bar) {
+    cp_async_wait<0>();
+    fence_async();
+    mbar_arrive(smem_u32(&bar));
+}
+
+// 16 columns of k s - m, those outside [lo, hi) at -inf.
+__device__ __forceinline__ void weigh16(float* s, const float* nref, float kf, bool masked, int lo, int hi) {
+#pragma unroll
+    for (int c = 0; c < 16; c += 4) {
+        const float4 nr = *reinterpret_cast<const float4*>(nref + c);
+        s[c] = fmaf(s[c], kf, nr.x);
+        s[c + 1] = fmaf(s[c + 1], kf, nr.y);
+        s[c + 2] = fmaf(s[c + 2], kf, nr.z);
+        s[c + 3] = fmaf(s[c + 3], kf, nr.w);
+    }
+    if (masked) {
+#pragma unroll
+        for (int c = 0; c < 16; ++c) s[c] = c >= lo && c < hi ? s[c] : -INFINITY;
+    }
 }
 
 template <int NP, int N>
@@ -184,289 +360,199 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t limit = a.wait_limit ? a.wait_limit : 1u << 24;
 
-    // (rows of a slot that no page reaches are never written: they stay zero)
-    for (int x = tid; x < kSlots * Sh::kSlot / 16; x += kThreads)
-        if (x * 16 % Sh::kPanel / 128 >= a.span) reinterpret_cast<uint4*>(sm.ring)[x] = make_uint4(0, 0, 0, 0);
-    fence_async();
-    if (tid == 0) {
-        for (int i = 0; i < kSlots; ++i) {
-            mbar_init(smem_u32(&sm.full[i]), 1);
-            mbar_init(smem_u32(&sm.empty[i]), 1);
-        }
-        for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sm.s_full[i]), 1);
-        mbar_init(smem_u32(&sm.p_full), kSoft);
-        mbar_init(smem_u32(&sm.p_done), 1);
-        mbar_init(smem_u32(&sm.q_full), kSoft);
-        mbar_init(smem_u32(&sm.drain), 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        sm.abort = sm.fix = sm.joint.n = 0;
-    }
     if (warp == kIssuer) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)), "n"(Sh::kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         fence_before();
+    } else if (warp == kKeys && lane == 0) {
+        for (int i = 0; i < kSlots; ++i) {
+            mbar_init(smem_u32(&sm.full[i]), 1);
+            mbar_init(smem_u32(&sm.empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&sm.s_full[i]), 1);
+            mbar_init(smem_u32(&sm.p_full[i]), kSoft);
+            mbar_init(smem_u32(&sm.p_done[i]), 1);
+        }
+        mbar_init(smem_u32(&sm.q_full), kSoft);
+        mbar_init(smem_u32(&sm.drain), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int i = 0; i < kUnits; ++i) sm.bad[i] = 0;
+        sm.abort = sm.fix = sm.joint.n = 0;
+    } else if (warp < 4) {
+        // (rows of a slot that no page reaches are never written: they stay zero)
+        if (a.span < kTile) {
+            const int vecs = (kTile - a.span) * 8;
+            for (int x = tid; x < kSlots * NP * vecs; x += kSoft) {
+                const int panel = x / vecs;
+                reinterpret_cast<uint4*>(sm.ring[0] + panel * Sh::kPanel + a.span * 128)[x - panel * vecs] = make_uint4(0, 0, 0, 0);
+            }
+        }
+        fence_async();
     }
-    const Share sh = find_share<kThreads>(a, sm.share);
+    const Share sh = find_share(a, sm.share, kThreads);
     fence_after();
     const uint32_t tmem = sm.tmem;
-    auto s_at = [&](int g) { return tmem + (g & 1) * N; };
-    const uint32_t o_at = tmem + 2 * N;
     Walk w = walk_begin(a, sh);
 
-    if (warp == kProducer) {
-        // ---- loads
-        int x = 0;                             // slots filled
-        bool ok = true;
-        const int rows = a.page < kTile ? a.page : kTile;                // of a box
-        for (; w.more && ok; walk_next(a, w)) {
-            const int count = w.r0 + a.rows < w.s.rows ? a.rows : w.s.rows - w.r0;
-            const int p1 = w.s.base + (w.r0 + count - 1) / a.group, low0 = low_of(a, w.s.base + w.r0 / a.group);
-            const int per = a.per_page > 1 ? 1 : a.span / a.page;        // pages of a tile
-            auto entry = [&](int i) {          // the page of this lane in tile i, or -1
-                if (i >= w.upto || lane >= per) return -1;
-                const int tile = tile_at(w.u, i);
-                const int j = a.per_page > 1 ? tile / a.per_page : tile * per + lane;
-                if (!page_seen(a, j, p1, low0)) return -1;
-                const int page = __ldg(a.table + static_cast<long long>(w.b) * a.width + j);
-                return page < 0 || page >= a.num_pages ? -1 : page;
-            };
-            int next = entry(w.i);
-            for (int i = w.i; i < w.upto && ok; ++i) {
-                const int page = next;
-                next = entry(i + 1);
-                const int token = a.per_page > 1 ? tile_at(w.u, i) % a.per_page * a.span : 0;
-                const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
-#pragma unroll
-                for (int which = 0; which < 2; ++which, ++x) {
-                    const int slot = x % kSlots;
-                    ok = ok && mbar_wait_now(smem_u32(&sm.empty[slot]), (x / kSlots & 1) ^ 1, a.status, limit);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    const uint32_t bar = smem_u32(&sm.full[slot]);
-                    if (lane == 0) mbar_arrive_expect(bar, __popc(there) * rows * 128 * NP);
-                    __syncwarp();
-                    if (page >= 0) {
-#pragma unroll
-                        for (int p = 0; p < NP; ++p)
-                            tma_load(smem_u32(sm.ring[slot]) + p * Sh::kPanel + lane * rows * 128, which ? &v_map : &k_map, p * 64, token, w.h, page, bar);
-                    }
-                }
-            }
-        }
-        // (a launch that gave up leaves when its copies are in)
-        if (!ok)
-            for (int y = x < kSlots ? 0 : x - kSlots; y < x; ++y) mbar_wait_now(smem_u32(&sm.full[y % kSlots]), y / kSlots & 1, a.status, limit);
+    if (warp == kKeys || warp == kValues) {
+        load_tiles<NP, N>(a, sm, w, warp == kKeys ? &k_map : &v_map, warp == kValues, limit);
     } else if (warp == kIssuer) {
-        // ---- products
-        if (lane == 0) {
-            constexpr uint32_t qk = instruction(kTile, N, false, false), pv = instruction(64 * NP, N, true, true);
-            int g = 0, units = 0;              // tiles, units gone through
-            bool ok = true;
-            auto wait = [&](unsigned long long& bar, int phase) { ok = ok && mbar_wait_now(smem_u32(&bar), phase & 1, a.status, limit); };
-            auto scores = [&](int t) {
-                const int x = 2 * t;
-                wait(sm.full[x % kSlots], x / kSlots);
-                if (!ok) return;
-                fence_after();
-                const uint32_t k = smem_u32(sm.ring[x % kSlots]), q = smem_u32(sm.q);
-#pragma unroll
-                for (int i = 0; i < 4 * NP; ++i)
-                    mma(s_at(t), describe(k + i / 4 * Sh::kPanel + i % 4 * 32, 16, 1024, 2), describe(q + i / 4 * N * 128 + i % 4 * 32, 16, 1024, 2), qk, i > 0);
-                commit(smem_u32(&sm.empty[x % kSlots]));
-                if (a.never_signal != 1) commit(smem_u32(&sm.s_full[t & 1]));
-            };
-            for (; w.more && ok; walk_next(a, w), ++units) {
-                const int nt = w.upto - w.i;
-                wait(sm.q_full, units);
-                if (ok) scores(g);
-                for (int i = 0; i < nt && ok; ++i, ++g) {
-                    if (i + 1 < nt) scores(g + 1);
-                    const int x = 2 * g + 1;
-                    wait(sm.full[x % kSlots], x / kSlots);
-                    wait(sm.p_full, g);
-                    if (!ok) break;
-                    fence_after();
-                    const uint32_t v = smem_u32(sm.ring[x % kSlots]), p = smem_u32(sm.p);
-#pragma unroll
-                    for (int j = 0; j < kTile / 16; ++j)
-                        mma(o_at, describe(v + j * 2048, Sh::kPanel, 1024, 2), describe(p + j * 256, 128, 2048, 0), pv, i > 0 || j > 0);
-                    commit(smem_u32(&sm.empty[x % kSlots]));
-                    commit(smem_u32(&sm.p_done));
-                }
-            }
-            if (!ok) {
-                commit(smem_u32(&sm.drain));
-                mbar_wait_now(smem_u32(&sm.drain), 0, a.status, limit);
-            }
-        }
+        if (lane == 0) issue_products<NP, N>(a, sm, w, static_cast<int>(sh.end - sh.begin), tmem, limit);
         __syncwarp();
     } else {
         // ---- weights
-        const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
+        const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16, o_at = tmem + lanes + 2 * N;
         const int key = tid;                   // of a tile
         // the element of O that this thread has: with 64 of them a warp has 16, in its lower lanes
         const int dim = NP == 2 ? tid : warp * 16 + lane;
         const bool has_dim = dim < a.D && (NP == 2 || lane < 16);
-        char* const p_row = sm.p + key / 8 * 128 + key % 8 * 16;
-        int g = 0;
+        char* const p_row = sm.p[0] + key / 8 * 128 + key % 8 * 16;
+        int g = 0, unit = 0;
         // A wait that gives up: this thread asks for a vote from then on, and behind the vote all of them leave together (sm.abort is
         // set before a vote or after the barrier that follows the look at it, never between).
         bool failed = false, gone = false;
-        auto wait = [&](unsigned long long& bar, int phase) {
+        auto lane_wait = [&](unsigned long long& bar, int phase) {       // (for some lanes of a warp: no coming together in here)
             if (!mbar_wait_now(smem_u32(&bar), phase & 1, a.status, limit)) {
                 failed = true;
                 atomicExch(&sm.abort, 1);
             }
         };
-        for (; w.more; walk_next(a, w)) {
-            const int count = w.r0 + a.rows < w.s.rows ? a.rows : w.s.rows - w.r0;
-            const int p0 = w.s.base + w.r0 / a.group, p1 = w.s.base + (w.r0 + count - 1) / a.group;
-            const int low0 = low_of(a, p0), low1 = low_of(a, p1);
-            // the query rows, swizzled like the keys; zero beyond the unit's rows and beyond D
-            for (int y = tid; y < N * NP * 8; y += kSoft) {
-                const int row = y / (NP * 8), c = y - row * (NP * 8);
-                uint4 val = make_uint4(0, 0, 0, 0);
-                if (row < count && c * 8 < a.D) {
-                    const int r = w.r0 + row, t = r / a.group;
-                    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + w.b * a.qs[0] + t * a.qs[1] + (w.h * a.group + r - t * a.group) * a.qs[2] + c * 8;
-                    if (q_vec) {
-                        val = *reinterpret_cast<const uint4*>(src);
-                    } else {
-                        const uint16_t* e = reinterpret_cast<const uint16_t*>(src);
-                        val = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
-                    }
-                }
-                *reinterpret_cast<uint4*>(sm.q + c / 8 * N * 128 + row * 128 + ((c % 8) ^ (row & 7)) * 16) = val;
-            }
-            if (tid < N) {
-                const int t = (w.r0 + (tid < count ? tid : 0)) / a.group;
-                sm.pos[tid] = w.s.base + t;
-                sm.low[tid] = low_of(a, w.s.base + t);
-                sm.nref[tid] = -kNone;
-            }
-            fence_async();
-            mbar_arrive(smem_u32(&sm.q_full));
-            // (does the CTA's part of the unit read pages that are none?)
-            bool bad = w.s.bad;
-            {
-                const int t0 = tile_at(w.u, w.i), t1 = tile_at(w.u, w.upto - 1);
-                const int j0 = tile_start(a, t0) / a.page, j1 = min(tile_start(a, t1) + a.span - 1, p1) / a.page;
-                for (int j = j0 + tid; p1 >= 0 && j <= j1; j += kSoft) {
-                    if (!page_seen(a, j, p1, low0)) continue;
-                    const int page = __ldg(a.table + static_cast<long long>(w.b) * a.width + j);
-                    bad |= page < 0 || page >= a.num_pages;
-                }
-            }
+        auto wait = [&](unsigned long long& bar, int phase) {            // by whole warps
+            lane_wait(bar, phase);
+            __syncwarp();
+        };
+        auto products = [&](int t) { wait(sm.p_done[t % Sh::kBuffers], t / Sh::kBuffers); };      // until tile t's are done
+        View v{};
+        if (w.more) {
+            v = view_of(a, w);
+            fetch_queries<NP, N>(a, sm.q[0], w, v.count, q_vec, tid);
+            fetched_queries(sm.q_full);
+        }
+#pragma unroll 1
+        while (w.more) {
+            Walk next = w;
+            View nv{};
+            bool ahead = false;
+            auto look_ahead = [&] {
+                ahead = true;
+                walk_next(a, next);
+                if (next.more) nv = view_of(a, next);
+            };
             float l[N];
 #pragma unroll
             for (int c = 0; c < N; ++c) l[c] = 0.f;
-            soft_sync();                       // pos, low, nref
+            if (tid < N) sm.nref[tid] = -kNone;
+            soft_sync();
             const int nt = w.upto - w.i;
+#pragma unroll 1
             for (int i = 0; i < nt && !gone; ++i, ++g) {
-                const Geometry ge = geometry(a, tile_at(w.u, w.i + i));
-                const bool whole = ge.start + ge.keys - 1 <= p0 && (ge.start >= low1 || ge.start + ge.keys <= a.sinks) && ge.keys == kTile;
-                unsigned see[(N + 31) / 32];
+                int start;
+                const int keys = tile_keys(a, tile_at(w.u, w.i + i), &start);
+                const bool masked = keys < kTile || !whole_tile(a, v, start, keys);
+                int lo = 0, hi = N;            // the rows that see this thread's key
                 wait(sm.s_full[g & 1], g >> 1);
-                __syncwarp();
                 fence_after();
+                const uint32_t s_at = tmem + lanes + (g & 1) * N;
                 float s[N];
-#pragma unroll
-                for (int c = 0; c < N; c += 16) ld16(s_at(g) + lanes + c, s + c);
-                if (!whole) {
-                    const int p = ge.start + key;
-#pragma unroll
-                    for (int c = 0; c < N; ++c) {
-                        if (c % 32 == 0) see[c / 32] = 0;
-                        const bool x = key < ge.keys && p <= sm.pos[c] && (p >= sm.low[c] || p < a.sinks);
-                        see[c / 32] |= static_cast<unsigned>(x) << (c % 32);
+                if (masked) {
+                    const int p = start + key;
+                    const bool any = key < keys && any_sees(a, v, p), all = any && all_see(a, v, p);
+                    if (!any) {
+                        hi = 0;
+                    } else if (!all) {
+                        // rows are in the order of their positions: from the first token at or beyond p, to the last whose window reaches p
+                        const long long first = static_cast<long long>(p - w.s.base) * a.group - w.r0, last = first + static_cast<long long>(a.window) * a.group;
+                        lo = first > 0 ? static_cast<int>(first) : 0;
+                        if (a.window > 0 && p >= a.sinks && last < N) hi = static_cast<int>(last);
                     }
                     // the value's row: zero where nobody sees it, its finite elements where some do not
-                    const bool any = key < ge.keys && p <= p1 && (p >= low0 || p < a.sinks), all = any && p <= p0 && (p >= low1 || p < a.sinks);
-                    const int xv = 2 * g + 1;
-                    if (!all) wait(sm.full[xv % kSlots], xv / kSlots);
-                    char* row = sm.ring[xv % kSlots] + key * 128;
-                    if (!any) {
-#pragma unroll
-                        for (int e = 0; e < 8 * NP; ++e) *reinterpret_cast<uint4*>(row + e / 8 * Sh::kPanel + ((e + lane) % 8) * 16) = make_uint4(0, 0, 0, 0);
-                    } else if (!all) {
-                        for (int e = 0; e < 32 * NP; ++e) {
-                            uint32_t* at = reinterpret_cast<uint32_t*>(row + e / 32 * Sh::kPanel) + (e + lane) % 32;
-                            uint32_t v = *at;
-                            const uint32_t was = v;
-                            if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
-                            if ((v & 0x7f800000u) == 0x7f800000u) v &= 0xffffu;
-                            if (v != was) {
-                                *at = v;
+                    if (!all && key < a.span) {
+                        const int xv = 2 * g + 1;
+                        lane_wait(sm.full[xv % kSlots], xv / kSlots);
+                        char* row = sm.ring[xv % kSlots] + key * 128;
+#pragma unroll 1
+                        for (int e = 0; e < 8 * NP; ++e) {
+                            uint4* at = reinterpret_cast<uint4*>(row + e / 8 * Sh::kPanel + ((e + lane) % 8) * 16);
+                            uint4 val = make_uint4(0, 0, 0, 0);
+                            if (any) {
+                                val = *at;
+                                bool odd = false;
+                                auto finite = [&](uint32_t& x) {
+                                    if ((x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; odd = true; }
+                                    if ((x & 0x7f800000u) == 0x7f800000u) { x &= 0xffffu; odd = true; }
+                                };
+                                finite(val.x); finite(val.y); finite(val.z); finite(val.w);
+                                if (!odd) continue;
                                 sm.fix = 1;
                             }
+                            *at = val;
                         }
                     }
+                    __syncwarp();
                 }
-                __syncwarp();
-#pragma unroll
-                for (int c = 0; c < N; c += 16) wait_ld(s + c);
                 // k s - m, and whether any of them is too large
                 float most = -INFINITY;
 #pragma unroll
-                for (int c = 0; c < N; c += 4) {
-                    const float4 nr = *reinterpret_cast<const float4*>(sm.nref + c);
-                    s[c] = fmaf(s[c], a.kf, nr.x);
-                    s[c + 1] = fmaf(s[c + 1], a.kf, nr.y);
-                    s[c + 2] = fmaf(s[c + 2], a.kf, nr.z);
-                    s[c + 3] = fmaf(s[c + 3], a.kf, nr.w);
-                }
-                if (!whole) {
+                for (int c = 0; c < N; c += 16) ld16(s_at + c, s + c);
 #pragma unroll
-                    for (int c = 0; c < N; ++c) s[c] = see[c / 32] >> (c % 32) & 1 ? s[c] : -INFINITY;
-                }
+                for (int c = 0; c < N; c += 16) {
+                    wait_ld(s + c);
+                    weigh16(s + c, sm.nref + c, a.kf, masked, lo - c, hi - c);
 #pragma unroll
-                for (int c = 0; c < N; ++c) most = fmaxf(most, s[c]);
+                    for (int e = 0; e < 16; ++e) most = fmaxf(most, s[c + e]);
+                }
                 if (soft_any(most > kLag || failed)) {
-                    // (the scores once more: what is left of them next to a reference that is none is not exact)
+#pragma unroll 1
+                    for (int c = 0; c < N; c += 16) {
+                        float y[16];
+                        ld16(s_at + c, y);
+                        wait_ld(y);
+                        float mine = -INFINITY;
 #pragma unroll
-                    for (int c = 0; c < N; c += 16) ld16(s_at(g) + lanes + c, s + c);
-#pragma unroll
-                    for (int c = 0; c < N; c += 16) wait_ld(s + c);
-#pragma unroll
-                    for (int c = 0; c < N; ++c) {
-                        s[c] *= a.kf;
-                        if (!whole && !(see[c / 32] >> (c % 32) & 1)) s[c] = -INFINITY;
-                        const float x = warp_max(s[c]);
-                        if (lane == c % 32) sm.part[warp][c] = x;
+                        for (int e = 0; e < 16; ++e) {
+                            const float x = warp_max(c + e >= lo && c + e < hi ? y[e] * a.kf : -INFINITY);
+                            if (lane == e) mine = x;
+                        }
+                        if (lane < 16) sm.part[warp][c + lane] = mine;
                     }
                     soft_sync();
                     if (tid < N) {
                         const float top = fmaxf(fmaxf(sm.part[0][tid], sm.part[1][tid]), fmaxf(sm.part[2][tid], sm.part[3][tid]));
                         const float old = -sm.nref[tid];
                         const float now = top - old > kLag ? rintf(top) : old;
-                        sm.factor[tid] = now == old ? 1.f : exp2f(old - now);
+                        sm.part[0][tid] = now == old ? 1.f : exp2f(old - now);
                         sm.nref[tid] = -now;
                     }
                     gone = *static_cast<volatile int*>(&sm.abort) != 0;
                     soft_sync();
                     if (gone) break;
                     if (i > 0) {
-                        wait(sm.p_done, g - 1);
-                        __syncwarp();
+                        products(g - 1);
                         fence_after();
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < N; c += 16) {
                             float o[16];
-                            ld16(o_at + lanes + c, o);
+                            ld16(o_at + c, o);
                             wait_ld(o);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] *= sm.factor[c + e];
-                            st16(o_at + lanes + c, o);
+                            for (int e = 0; e < 16; ++e) o[e] *= sm.part[0][c + e];
+                            st16(o_at + c, o);
                         }
                         wait_st();
+#pragma unroll
+                        for (int c = 0; c < N; ++c) l[c] *= sm.part[0][c];
                     }
 #pragma unroll
-                    for (int c = 0; c < N; ++c) {
-                        l[c] *= sm.factor[c];
-                        s[c] += sm.nref[c];
+                    for (int c = 0; c < N; c += 16) ld16(s_at + c, s + c);
+#pragma unroll
+                    for (int c = 0; c < N; c += 16) {
+                        wait_ld(s + c);
+                        weigh16(s + c, sm.nref + c, a.kf, masked, lo - c, hi - c);
                     }
                 }
-                if (i > 0) wait(sm.p_done, g - 1);                       // (the last tile's weights have been read)
+                if (i >= Sh::kBuffers) products(g - Sh::kBuffers);       // (the weights that lie there have been multiplied)
+                char* const to = p_row + g % Sh::kBuffers * Sh::kP;
 #pragma unroll
                 for (int c = 0; c < N; c += 8) {
                     uint32_t pk[4];
@@ -477,77 +563,95 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
                         l[c + 2 * e] += __uint_as_float(pk[e] << 16);
                         l[c + 2 * e + 1] += __uint_as_float(pk[e] & 0xffff0000u);
                     }
-                    *reinterpret_cast<uint4*>(p_row + c / 8 * (kTile * 16)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                    *reinterpret_cast<uint4*>(to + c / 8 * (kTile * 16)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
                 }
                 fence_async();
                 fence_before();
-                mbar_arrive(smem_u32(&sm.p_full));
+                mbar_arrive(smem_u32(&sm.p_full[g % Sh::kBuffers]));
+                if (i == 0) {
+                    // the next unit's rows
+                    look_ahead();
+                    if (next.more) {
+                        fetch_queries<NP, N>(a, sm.q[(unit + 1) & 1], next, nv.count, q_vec, tid);
+                        fetched_queries(sm.q_full);
+                    }
+                }
             }
-            if (!gone) wait(sm.p_done, g - 1);
-            __syncwarp();
+            if (!gone) products(g - 1);
             fence_after();
-            // the sums
+            // the sums: over the lanes, then (in what follows) over the warps
 #pragma unroll
             for (int c = 0; c < N; c += 32) {
                 if (c + 32 <= N) {
-                    const float x = across<32>(l + c, lane);
-                    sm.part[warp][c + lane] = x;
+                    sm.part[warp][c + lane] = across<32>(l + c, lane);
                 } else {
                     const float x = across<16>(l + c, lane);
                     if (lane < 16) sm.part[warp][c + lane] = x;
                 }
             }
-            bad = soft_any(bad || failed || gone);
+            const bool bad = soft_any(w.s.bad || failed || gone) || *static_cast<volatile int*>(&sm.bad[unit % kUnits]) != 0;
             const bool fix = *static_cast<volatile int*>(&sm.fix) != 0;
-            float* part = leave_unit(a, sh, w, count, sm.joint, tid);
-            if (part && tid < count) {
-                part[tid] = -sm.nref[tid];
-                part[a.rows + tid] = bad ? NAN : sm.part[0][tid] + sm.part[1][tid] + sm.part[2][tid] + sm.part[3][tid];
+            float* part = leave_unit(a, sh, w, v.count, sm.joint, tid);
+            if (tid < N) {
+                const float sum = bad ? NAN : sm.part[0][tid] + sm.part[1][tid] + sm.part[2][tid] + sm.part[3][tid];
+                if (part && tid < v.count) {
+                    part[tid] = -sm.nref[tid];
+                    part[a.rows + tid] = sum;
+                }
+                sm.part[0][tid] = sum == 0.f ? 0.f : 1.f / sum;
             }
+            soft_sync();
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + w.b * a.os[0] + w.h * a.group * a.os[2] + dim;
 #pragma unroll 1
-            for (int c0 = 0; c0 < count; c0 += 16) {
+            for (int c0 = 0; c0 < v.count; c0 += 16) {
                 float o[16];
                 __syncwarp();
-                ld16(o_at + lanes + c0, o);
+                ld16(o_at + c0, o);
                 wait_ld(o);
                 if (fix && has_dim) {
                     // what is not finite among the values that some rows see and others do not
 #pragma unroll 1
                     for (int i = w.i; i < w.upto; ++i) {
-                        const Geometry ge = geometry(a, tile_at(w.u, i));
-                        if (ge.start + ge.keys - 1 <= p0 && (ge.start >= low1 || ge.start + ge.keys <= a.sinks)) continue;
-                        for (int x = 0; x < ge.keys; ++x) {
-                            const int p = ge.start + x;
-                            const bool any = p <= p1 && (p >= low0 || p < a.sinks), all = p <= p0 && (p >= low1 || p < a.sinks);
-                            if (!any || all) continue;
-                            const int page = __ldg(a.table + static_cast<long long>(w.b) * a.width + p / a.page);
+                        int start;
+                        const int keys = tile_keys(a, tile_at(w.u, i), &start);
+                        if (whole_tile(a, v, start, keys)) continue;
+#pragma unroll 1
+                        for (int x = 0; x < keys; ++x) {
+                            const int p = start + x;
+                            if (!any_sees(a, v, p) || all_see(a, v, p)) continue;
+                            const int j = a.by_page(p), page = __ldg(a.table + static_cast<long long>(w.b) * a.width + j);
                             if (page < 0 || page >= a.num_pages) continue;
-                            const float v = to_float((static_cast<const __nv_bfloat16*>(a.v) + page * a.vs[0] + w.h * a.vs[1] + p % a.page * a.vs[2])[dim]);
-                            if (isfinite(v)) continue;
+                            const float val = to_float((static_cast<const __nv_bfloat16*>(a.v) + page * a.vs[0] + w.h * a.vs[1] + (p - j * a.page) * a.vs[2])[dim]);
+                            if (isfinite(val)) continue;
 #pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (c0 + e < count && p <= sm.pos[c0 + e] && (p >= sm.low[c0 + e] || p < a.sinks)) o[e] += v;
+                            for (int e = 0; e < 16; ++e) {
+                                const int pos = w.s.base + a.by_group(w.r0 + c0 + e);
+                                if (p <= pos && (p >= low_of(a, pos) || p < a.sinks)) o[e] += val;
+                            }
                         }
                     }
                 }
+                if (part) {
+                    float* const at = part + 2 * a.rows + c0 * a.D + dim;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int row = c0 + e;
-                    if (row < count && has_dim) {
-                        if (part) {
-                            part[2 * a.rows + static_cast<size_t>(row) * a.D + dim] = o[e];
-                        } else {
-                            const float sum = sm.part[0][row] + sm.part[1][row] + sm.part[2][row] + sm.part[3][row];
-                            const int r = w.r0 + row, t = r / a.group;
-                            __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out) + w.b * a.os[0] + t * a.os[1] + (w.h * a.group + r - t * a.group) * a.os[2] + dim;
-                            *dst = __float2bfloat16_rn(bad ? NAN : sum == 0.f ? 0.f : o[e] / sum);
-                        }
+                    for (int e = 0; e < 16; ++e)
+                        if (c0 + e < v.count && has_dim) at[e * a.D] = o[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int r = w.r0 + c0 + e, t = a.by_group(r);
+                        const float val = o[e] * sm.part[0][c0 + e];
+                        if (c0 + e < v.count && has_dim) out[t * a.os[1] + (r - t * a.group) * a.os[2]] = __float2bfloat16_rn(val);
                     }
                 }
             }
+            if (!ahead) look_ahead();          // (a launch that gives up)
             fence_before();
             soft_sync();
-            if (tid == 0) sm.fix = 0;
+            if (tid == 0) sm.fix = sm.bad[unit % kUnits] = 0;
+            w = next;
+            v = nv;
+            ++unit;
         }
     }
     fence_before();

@@ -168,6 +168,9 @@ void plan(AttendCall* c, bool tiles) {
         a.span = attend_rows_keys();
         a.per_page = 1;
     }
+    a.by_group = divider(a.group);
+    a.by_page = divider(a.page);
+    a.by_span = divider(a.span);
 }
 int attend_ctas(int sm_count) { return sm_count < kCacheCounters ? sm_count : kCacheCounters; }
 size_t attend_scratch(int sm_count, const void* ctx) {

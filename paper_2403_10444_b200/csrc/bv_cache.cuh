@@ -11,6 +11,18 @@
 
 namespace bv {
 
+// Division of numbers below 2^31 by one that the host knows: (n mul / 2^32 + n) / 2^shift.  (A division of unknown integers is some
+// thirty instructions in a row, and the laying out of the work below is a chain of them.)
+struct Divider {
+    unsigned by, mul, shift;
+    __device__ __forceinline__ int operator()(int n) const { return static_cast<int>((__umulhi(static_cast<unsigned>(n), mul) + static_cast<unsigned>(n)) >> shift); }
+};
+inline Divider divider(unsigned by) {
+    unsigned shift = 0;
+    while ((1ull << shift) < by) ++shift;
+    return Divider{by, static_cast<unsigned>(((1ull << 32) * ((1ull << shift) - by)) / by + 1), shift};
+}
+
 // One call of bv_cache_attend.  Work is cut into units (sequence, key-value head, tile of query rows), a unit into tiles of
 // keys; all tiles of all units, in that order, are one list that is cut into gridDim.x equal contiguous parts.  A CTA goes
 // through its part; what a unit has in several CTAs is left in `part` and joined by the one that finishes last.
@@ -27,6 +39,7 @@ struct AttendArgs {
     long long qs[3], os[3];   // elements between sequences, tokens, heads
     long long ks[3], vs[3];   // elements between pages, heads, tokens
     int B, n, Hkv, group, D, page, num_pages, width;
+    Divider by_group, by_page, by_span;
     float kf;                 // scale log2(e)
     int window, sinks;
     int rows;                 // query rows of a unit, at most (row = token * group + head of the group)
@@ -42,10 +55,14 @@ struct AttendArgs {
 __host__ __device__ __forceinline__ size_t part_floats(int rows, int D) { return static_cast<size_t>(rows) * (D + 2); }
 
 __device__ __forceinline__ int tile_of(const AttendArgs& a, int pos) {
-    return a.per_page == 1 ? pos / a.span : pos / a.page * a.per_page + pos % a.page / a.span;
+    if (a.per_page == 1) return a.by_span(pos);
+    const int page = a.by_page(pos);
+    return page * a.per_page + a.by_span(pos - page * a.page);
 }
 __device__ __forceinline__ int tile_start(const AttendArgs& a, int tile) {
-    return a.per_page == 1 ? tile * a.span : tile / a.per_page * a.page + tile % a.per_page * a.span;
+    if (a.per_page == 1) return tile * a.span;
+    const int page = tile / a.per_page;
+    return page * a.page + (tile - page * a.per_page) * a.span;
 }
 
 // A sequence of the batch: its length and the tokens it brings.
@@ -79,7 +96,7 @@ struct Span {
     int sink, first, tiles;
 };
 __device__ __forceinline__ Span span_of(const AttendArgs& a, const Seq& s, int r0, int r1) {
-    const int p0 = s.base + r0 / a.group, p1 = s.base + r1 / a.group;
+    const int p0 = s.base + a.by_group(r0), p1 = s.base + a.by_group(r1);
     Span u{0, 0, 1};
     if (p1 < 0) return u;
     const int low = low_of(a, p0);
@@ -109,50 +126,64 @@ struct Share {
     long long begin, end;     // the CTA's part
     int b;                    // the sequence its first tile belongs to
     long long off;            // ... and how many of that sequence's tiles come before it
+    long long per_head;       // tiles of one head of it
 };
 struct ShareSmem {
-    long long sums[33];
-    long long off;
+    long long sums[32];
+    long long off, per_head;
     int b;
 };
-template <int THREADS>
-__device__ __forceinline__ Share find_share(const AttendArgs& a, ShareSmem& sm) {
+// total * c / n, in 32 bits where that is enough
+__device__ __forceinline__ long long part_of(long long total, int c, int n) {
+    const unsigned long long x = static_cast<unsigned long long>(total) * static_cast<unsigned>(c);
+    return x >> 32 ? static_cast<long long>(x / static_cast<unsigned>(n)) : static_cast<long long>(static_cast<unsigned>(x) / static_cast<unsigned>(n));
+}
+__device__ __forceinline__ Share find_share(const AttendArgs& a, ShareSmem& sm, int threads) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int each = (a.B + THREADS - 1) / THREADS;
+    const int each = a.B <= threads ? 1 : (a.B + threads - 1) / threads;
     const int b0 = tid * each < a.B ? tid * each : a.B, b1 = b0 + each < a.B ? b0 + each : a.B;
-    long long mine = 0;
-    for (int b = b0; b < b1; ++b) mine += a.Hkv * head_tiles(a, seq_of(a, b));
+    long long mine = 0, per_head = 0;
+#pragma unroll 1
+    for (int b = b0; b < b1; ++b) mine += a.Hkv * (per_head = head_tiles(a, seq_of(a, b)));
     long long upto = mine;
+#pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const long long x = __shfl_up_sync(0xffffffffu, upto, o);
         if (lane >= o) upto += x;
     }
     if (lane == 31) sm.sums[warp] = upto;
-    if (tid == 0) { sm.b = a.B; sm.off = 0; }
     __syncthreads();
     long long before = 0, total = 0;
-    for (int w = 0; w < THREADS / 32; ++w) {
-        if (w < warp) before += sm.sums[w];
-        total += sm.sums[w];
+#pragma unroll 1
+    for (int w = 0; w < threads / 32; ++w) {
+        const long long x = sm.sums[w];
+        before += w < warp ? x : 0;
+        total += x;
     }
     before += upto - mine;
     Share s;
     s.total = total;
     s.ctas = total < gridDim.x ? static_cast<int>(total) : gridDim.x;
     const int c = blockIdx.x;
-    s.begin = c < s.ctas ? total * c / s.ctas : total;
-    s.end = c < s.ctas ? total * (c + 1) / s.ctas : total;
+    s.begin = c < s.ctas ? part_of(total, c, s.ctas) : total;
+    s.end = c < s.ctas ? part_of(total, c + 1, s.ctas) : total;
     if (s.begin < s.end && before <= s.begin && s.begin < before + mine) {
-        long long at = before;
-        for (int b = b0; b < b1; ++b) {
-            const long long t = a.Hkv * head_tiles(a, seq_of(a, b));
-            if (s.begin < at + t) { sm.b = b; sm.off = s.begin - at; break; }
-            at += t;
+        int b = b0;
+        if (each > 1) {
+            for (;; ++b) {
+                per_head = head_tiles(a, seq_of(a, b));
+                if (s.begin < before + a.Hkv * per_head) break;
+                before += a.Hkv * per_head;
+            }
         }
+        sm.b = b;
+        sm.off = s.begin - before;
+        sm.per_head = per_head;
     }
     __syncthreads();
     s.b = sm.b;
     s.off = sm.off;
+    s.per_head = sm.per_head;
     return s;
 }
 
@@ -183,9 +214,14 @@ __device__ __forceinline__ Walk walk_begin(const AttendArgs& a, const Share& sh)
     if (!w.more) return w;
     w.b = sh.b;
     w.s = seq_of(a, w.b);
-    const long long per_head = head_tiles(a, w.s);
-    w.h = static_cast<int>(sh.off / per_head);
-    long long off = sh.off % per_head;
+    long long off;
+    if ((sh.off | sh.per_head) >> 31) {
+        w.h = static_cast<int>(sh.off / sh.per_head);
+        off = sh.off % sh.per_head;
+    } else {
+        w.h = static_cast<unsigned>(sh.off) / static_cast<unsigned>(sh.per_head);
+        off = static_cast<unsigned>(sh.off) % static_cast<unsigned>(sh.per_head);
+    }
     for (w.r0 = 0;; w.r0 += a.rows) {
         walk_unit(a, w);
         if (off < w.u.tiles) break;
@@ -214,7 +250,8 @@ __device__ __forceinline__ int tile_at(const Span& u, int i) { return i < u.sink
 
 // The CTA that holds a tile of the list.
 __device__ __forceinline__ int holder_of(const Share& sh, long long tile) {
-    return static_cast<int>(((tile + 1) * sh.ctas - 1) / sh.total);
+    const unsigned long long x = static_cast<unsigned long long>(tile + 1) * static_cast<unsigned>(sh.ctas) - 1;
+    return (x | sh.total) >> 32 ? static_cast<int>(x / sh.total) : static_cast<unsigned>(x) / static_cast<unsigned>(sh.total);
 }
 
 template <typename T> __device__ __forceinline__ T from_float(float x);
@@ -299,7 +336,7 @@ __device__ __forceinline__ void join_share(const AttendArgs& a, const Joint& u, 
             for (int i = 0; i < W; ++i) o[i] += __shfl_xor_sync(0xffffffffu, o[i], s);
         }
         if (mine && sub == 0) {
-            const int r = u.r0 + row, t = r / a.group;
+            const int r = u.r0 + row, t = a.by_group(r);
             T* dst = static_cast<T*>(a.out) + u.b * a.os[0] + t * a.os[1] + (u.h * a.group + r - t * a.group) * a.os[2] + d;
             const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
