@@ -6,8 +6,8 @@
 //   S^T [128 keys, N] = K Q^T            K as it lies in its pages, K-major
 //   O^T [D, N]       += V^T P            V as it lies in its pages, M-major; P [128 keys, N] from shared memory
 // Two warps load (TMA, a box per page and 64 columns, 128-byte swizzle, a ring of slots that hold a tile's keys or its values), one
-// thread issues the matrix instructions, four warps turn S into P: a thread has one key and goes over the N rows, so the
-// mask, the exponential and the rounding need no other lane.  What softmax usually needs across lanes is avoided: each row has an
+// thread issues the matrix instructions, four warps (for 48 rows and more eight, each four half of the rows) turn S into P: a thread has
+// one key and goes over the rows, so the mask, the exponential and the rounding need no other lane.  What softmax usually needs across lanes is avoided: each row has an
 // integer reference m in shared memory, weights are 2^{k s - m}, and only where some score exceeds its reference by more than 8
 // (a vote per tile) the new maxima are formed, and O and the sums scaled by the power of two between the old and the new
 // reference.  Sums stay per thread until a unit ends.  Weights are rounded to 16 bits for the second product, and the sums are taken of the rounded weights: a row of one
@@ -29,8 +29,7 @@
 namespace bv {
 namespace {
 
-constexpr int kThreads = 224, kSoft = 128, kTile = 128;
-constexpr int kKeys = 4, kValues = 5, kIssuer = 6;               // warps: loads of keys, of values, products; 0 .. 3 are the softmax's
+constexpr int kTile = 128;
 constexpr float kNone = -3.0e38f;                               // the reference of a row that has seen no score
 constexpr float kLag = 8.f;                                     // how far a score may exceed its reference
 
@@ -59,28 +58,39 @@ __device__ __forceinline__ void ld16(uint32_t addr, float* x) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(r[i]);
 }
-// (the values are not there before this; the operands keep the compiler from using them earlier)
-__device__ __forceinline__ void wait_ld(float* x) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]), "+f"(x[8]), "+f"(x[9]), "+f"(x[10]), "+f"(x[11]),
-                   "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15])::"memory");
+__device__ __forceinline__ void ld8(uint32_t addr, float* x) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(addr));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void st16(uint32_t addr, const float* x) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
-                 "r"(__float_as_uint(x[0])), "r"(__float_as_uint(x[1])), "r"(__float_as_uint(x[2])), "r"(__float_as_uint(x[3])), "r"(__float_as_uint(x[4])),
-                 "r"(__float_as_uint(x[5])), "r"(__float_as_uint(x[6])), "r"(__float_as_uint(x[7])), "r"(__float_as_uint(x[8])), "r"(__float_as_uint(x[9])),
-                 "r"(__float_as_uint(x[10])), "r"(__float_as_uint(x[11])), "r"(__float_as_uint(x[12])), "r"(__float_as_uint(x[13])), "r"(__float_as_uint(x[14])),
-                 "r"(__float_as_uint(x[15]))
+// (the values are not there before this; the operands keep the compiler from using them earlier)
+__device__ __forceinline__ void wait_ld8(float* x) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7])::"memory");
+}
+__device__ __forceinline__ void st8(uint32_t addr, const float* x) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), "r"(__float_as_uint(x[0])),
+                 "r"(__float_as_uint(x[1])), "r"(__float_as_uint(x[2])), "r"(__float_as_uint(x[3])), "r"(__float_as_uint(x[4])), "r"(__float_as_uint(x[5])),
+                 "r"(__float_as_uint(x[6])), "r"(__float_as_uint(x[7]))
                  : "memory");
+}
+// C columns, a multiple of 8.
+template <int C> __device__ __forceinline__ void load_columns(uint32_t addr, float* x) {
+#pragma unroll
+    for (int c = 0; c + 16 <= C; c += 16) ld16(addr + c, x + c);
+    if constexpr (C % 16 != 0) ld8(addr + C - 8, x + C - 8);
 }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // (a warp's lanes come together before what all of them have to execute at once)
-__device__ __forceinline__ void soft_sync() { __syncwarp(); asm volatile("bar.sync 1, 128;" ::: "memory"); }
-__device__ __forceinline__ bool soft_any(bool x) {
+template <int T> __device__ __forceinline__ void soft_sync() { __syncwarp(); asm volatile("bar.sync 1, %0;" ::"n"(T) : "memory"); }
+template <int T> __device__ __forceinline__ bool soft_any(bool x) {
     uint32_t r;
     __syncwarp();
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(static_cast<uint32_t>(x)) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(static_cast<uint32_t>(x)), "n"(T) : "memory");
     return r != 0;
 }
 __device__ __forceinline__ float ex2(float x) {
@@ -108,6 +118,9 @@ __host__ __device__ constexpr uint32_t instruction(int M, int N, bool a_m, bool 
 
 template <int NP, int N>
 struct Shape {
+    static constexpr int kHalves = N >= 48 ? 2 : 1, kColumnsEach = N / kHalves;      // the softmax's warps, four a half; rows of a half
+    static constexpr int kSoft = 128 * kHalves, kThreads = kSoft + 96;
+    static constexpr int kKeys = 4 * kHalves, kValues = kKeys + 1, kIssuer = kKeys + 2;      // warps: loads of keys, of values, products
     static constexpr int kPanel = kTile * 128, kSlot = NP * kPanel;      // a slot: NP panels of 128 rows of 64 columns
     static constexpr int kQ = NP * N * 128, kP = N * kTile * 2;
     static constexpr int kRest = 3072;
@@ -129,6 +142,7 @@ struct __align__(1024) Smem {
     char p[Sh::kBuffers][Sh::kP];
     float nref[N];                             // minus the references
     float part[4][N];                          // maxima by warp; then in part[0] what the move of the references scales by
+    long long off[N];                          // where the rows' results go
     unsigned long long full[8], empty[8], s_full[2], p_full[2], p_done[2], q_full, drain;
     ShareSmem share;
     JointSmem joint;
@@ -176,11 +190,12 @@ __device__ __forceinline__ float warp_max(float x) {
     return __int_as_float(i);
 }
 
-// Sums over the lanes of 16 or 32 values each: lane x ends up with the sum of value x (of x % 16).
+// Sums over the lanes of W = 8, 16 or 32 values each: lane x ends up with the sum of value x % W.
 template <int W> __device__ __forceinline__ float across(float* v, int lane) {
-    if (W == 16) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], 16);
+    for (int w = 16; w >= W; w >>= 1) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], w);
     }
 #pragma unroll
     for (int w = W / 2; w > 0; w >>= 1) {
@@ -304,13 +319,13 @@ __device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>&
 }
 
 // A unit's query rows, swizzled like the keys; zero beyond its rows and beyond D.  They are there when the copies are (fetched_queries).
-template <int NP, int N>
+template <int NP, int N, int T>
 __device__ __forceinline__ void fetch_queries(const AttendArgs& a, char* to, const Walk& w, int count, int q_vec, int tid) {
     constexpr int per_row = NP * 8;
     const int c = tid % per_row;
     const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + w.b * a.qs[0] + w.h * a.group * a.qs[2] + c * 8;
 #pragma unroll 1
-    for (int row = tid / per_row; row < N; row += kSoft / per_row) {
+    for (int row = tid / per_row; row < N; row += T / per_row) {
         const uint32_t dst = smem_u32(to) + c / 8 * (N * 128) + row * 128 + ((c % 8) ^ (row & 7)) * 16;
         const int r = w.r0 + row, t = a.by_group(r);
         const __nv_bfloat16* from = src + t * a.qs[1] + (r - t * a.group) * a.qs[2];
@@ -334,10 +349,10 @@ __device__ __forceinline__ void fetched_queries(unsigned long long& bar) {
     mbar_arrive(smem_u32(&bar));
 }
 
-// 16 columns of k s - m, those outside [lo, hi) at -inf.
-__device__ __forceinline__ void weigh16(float* s, const float* nref, float kf, bool masked, int lo, int hi) {
+// C columns of k s - m, those outside [lo, hi) at -inf.
+template <int C> __device__ __forceinline__ void weigh(float* s, const float* nref, float kf, bool masked, int lo, int hi) {
 #pragma unroll
-    for (int c = 0; c < 16; c += 4) {
+    for (int c = 0; c < C; c += 4) {
         const float4 nr = *reinterpret_cast<const float4*>(nref + c);
         s[c] = fmaf(s[c], kf, nr.x);
         s[c + 1] = fmaf(s[c + 1], kf, nr.y);
@@ -346,25 +361,25 @@ __device__ __forceinline__ void weigh16(float* s, const float* nref, float kf, b
     }
     if (masked) {
 #pragma unroll
-        for (int c = 0; c < 16; ++c) s[c] = c >= lo && c < hi ? s[c] : -INFINITY;
+        for (int c = 0; c < C; ++c) s[c] = c >= lo && c < hi ? s[c] : -INFINITY;
     }
 }
 
 template <int NP, int N>
-__global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const int q_vec) {
+__global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const int q_vec) {
     extern __shared__ __align__(1024) char raw[];
     using Sh = Shape<NP, N>;
     Smem<NP, N>& sm = *reinterpret_cast<Smem<NP, N>*>(raw);
     static_assert(sizeof(Smem<NP, N>) <= Sh::kBytes, "the rest fits");
-    constexpr int kSlots = Sh::kSlots;
+    constexpr int kSlots = Sh::kSlots, kSoft = Sh::kSoft, C = Sh::kColumnsEach;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t limit = a.wait_limit ? a.wait_limit : 1u << 24;
 
-    if (warp == kIssuer) {
+    if (warp == Sh::kIssuer) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)), "n"(Sh::kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         fence_before();
-    } else if (warp == kKeys && lane == 0) {
+    } else if (warp == Sh::kKeys && lane == 0) {
         for (int i = 0; i < kSlots; ++i) {
             mbar_init(smem_u32(&sm.full[i]), 1);
             mbar_init(smem_u32(&sm.empty[i]), 1);
@@ -379,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         for (int i = 0; i < kUnits; ++i) sm.bad[i] = 0;
         sm.abort = sm.fix = sm.joint.n = 0;
-    } else if (warp < 4) {
+    } else if (warp < Sh::kKeys) {
         // (rows of a slot that no page reaches are never written: they stay zero)
         if (a.span < kTile) {
             const int vecs = (kTile - a.span) * 8;
@@ -390,24 +405,25 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
         }
         fence_async();
     }
-    const Share sh = find_share(a, sm.share, kThreads);
+    const Share sh = find_share(a, sm.share, Sh::kThreads);
     fence_after();
     const uint32_t tmem = sm.tmem;
     Walk w = walk_begin(a, sh);
 
-    if (warp == kKeys || warp == kValues) {
-        load_tiles<NP, N>(a, sm, w, warp == kKeys ? &k_map : &v_map, warp == kValues, limit);
-    } else if (warp == kIssuer) {
+    if (warp == Sh::kKeys || warp == Sh::kValues) {
+        load_tiles<NP, N>(a, sm, w, warp == Sh::kKeys ? &k_map : &v_map, warp == Sh::kValues, limit);
+    } else if (warp == Sh::kIssuer) {
         if (lane == 0) issue_products<NP, N>(a, sm, w, static_cast<int>(sh.end - sh.begin), tmem, limit);
         __syncwarp();
     } else {
         // ---- weights
-        const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16, o_at = tmem + lanes + 2 * N;
-        const int key = tid;                   // of a tile
+        // the thread's key, its four warps' rows c0 .. c0 + C - 1
+        const int key = tid & (kTile - 1), quarter = warp & 3, half = warp >> 2, c0 = half * C;
+        const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16, o_at = tmem + lanes + 2 * N + c0;
         // the element of O that this thread has: with 64 of them a warp has 16, in its lower lanes
-        const int dim = NP == 2 ? tid : warp * 16 + lane;
+        const int dim = NP == 2 ? key : quarter * 16 + lane;
         const bool has_dim = dim < a.D && (NP == 2 || lane < 16);
-        char* const p_row = sm.p[0] + key / 8 * 128 + key % 8 * 16;
+        char* const p_row = sm.p[0] + c0 / 8 * (kTile * 16) + key / 8 * 128 + key % 8 * 16;
         int g = 0, unit = 0;
         // A wait that gives up: this thread asks for a vote from then on, and behind the vote all of them leave together (sm.abort is
         // set before a vote or after the barrier that follows the look at it, never between).
@@ -426,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
         View v{};
         if (w.more) {
             v = view_of(a, w);
-            fetch_queries<NP, N>(a, sm.q[0], w, v.count, q_vec, tid);
+            fetch_queries<NP, N, kSoft>(a, sm.q[0], w, v.count, q_vec, tid);
             fetched_queries(sm.q_full);
         }
 #pragma unroll 1
@@ -439,22 +455,26 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
                 walk_next(a, next);
                 if (next.more) nv = view_of(a, next);
             };
-            float l[N];
+            float l[C];
 #pragma unroll
-            for (int c = 0; c < N; ++c) l[c] = 0.f;
-            if (tid < N) sm.nref[tid] = -kNone;
-            soft_sync();
+            for (int c = 0; c < C; ++c) l[c] = 0.f;
+            if (tid < N) {
+                const int r = w.r0 + tid, t = a.by_group(r);
+                sm.nref[tid] = -kNone;
+                sm.off[tid] = t * a.os[1] + (r - t * a.group) * a.os[2];
+            }
+            soft_sync<kSoft>();
             const int nt = w.upto - w.i;
 #pragma unroll 1
             for (int i = 0; i < nt && !gone; ++i, ++g) {
                 int start;
                 const int keys = tile_keys(a, tile_at(w.u, w.i + i), &start);
                 const bool masked = keys < kTile || !whole_tile(a, v, start, keys);
-                int lo = 0, hi = N;            // the rows that see this thread's key
+                int lo = 0, hi = N;            // the rows that see this thread's key, from the first of its four warps on
                 wait(sm.s_full[g & 1], g >> 1);
                 fence_after();
-                const uint32_t s_at = tmem + lanes + (g & 1) * N;
-                float s[N];
+                const uint32_t s_at = tmem + lanes + (g & 1) * N + c0;
+                float s[C];
                 if (masked) {
                     const int p = start + key;
                     const bool any = key < keys && any_sees(a, v, p), all = any && all_see(a, v, p);
@@ -466,13 +486,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
                         lo = first > 0 ? static_cast<int>(first) : 0;
                         if (a.window > 0 && p >= a.sinks && last < N) hi = static_cast<int>(last);
                     }
+                    lo -= c0;
+                    hi -= c0;
                     // the value's row: zero where nobody sees it, its finite elements where some do not
                     if (!all && key < a.span) {
                         const int xv = 2 * g + 1;
                         lane_wait(sm.full[xv % kSlots], xv / kSlots);
                         char* row = sm.ring[xv % kSlots] + key * 128;
 #pragma unroll 1
-                        for (int e = 0; e < 8 * NP; ++e) {
+                        for (int e = half * 8 * NP / Sh::kHalves; e < (half + 1) * 8 * NP / Sh::kHalves; ++e) {
                             uint4* at = reinterpret_cast<uint4*>(row + e / 8 * Sh::kPanel + ((e + lane) % 8) * 16);
                             uint4 val = make_uint4(0, 0, 0, 0);
                             if (any) {
@@ -493,30 +515,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
                 }
                 // k s - m, and whether any of them is too large
                 float most = -INFINITY;
+                load_columns<C>(s_at, s);
 #pragma unroll
-                for (int c = 0; c < N; c += 16) ld16(s_at + c, s + c);
+                for (int c = 0; c < C; c += 8) wait_ld8(s + c);
+                weigh<C>(s, sm.nref + c0, a.kf, masked, lo, hi);
 #pragma unroll
-                for (int c = 0; c < N; c += 16) {
-                    wait_ld(s + c);
-                    weigh16(s + c, sm.nref + c, a.kf, masked, lo - c, hi - c);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) most = fmaxf(most, s[c + e]);
-                }
-                if (soft_any(most > kLag || failed)) {
+                for (int c = 0; c < C; ++c) most = fmaxf(most, s[c]);
+                if (soft_any<kSoft>(most > kLag || failed)) {
 #pragma unroll 1
-                    for (int c = 0; c < N; c += 16) {
-                        float y[16];
-                        ld16(s_at + c, y);
-                        wait_ld(y);
+                    for (int c = 0; c < C; c += 8) {
+                        float y[8];
+                        ld8(s_at + c, y);
+                        wait_ld8(y);
                         float mine = -INFINITY;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
+                        for (int e = 0; e < 8; ++e) {
                             const float x = warp_max(c + e >= lo && c + e < hi ? y[e] * a.kf : -INFINITY);
                             if (lane == e) mine = x;
                         }
-                        if (lane < 16) sm.part[warp][c + lane] = mine;
+                        if (lane < 8) sm.part[quarter][c0 + c + lane] = mine;
                     }
-                    soft_sync();
+                    soft_sync<kSoft>();
                     if (tid < N) {
                         const float top = fmaxf(fmaxf(sm.part[0][tid], sm.part[1][tid]), fmaxf(sm.part[2][tid], sm.part[3][tid]));
                         const float old = -sm.nref[tid];
@@ -525,36 +544,33 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
                         sm.nref[tid] = -now;
                     }
                     gone = *static_cast<volatile int*>(&sm.abort) != 0;
-                    soft_sync();
+                    soft_sync<kSoft>();
                     if (gone) break;
                     if (i > 0) {
                         products(g - 1);
                         fence_after();
 #pragma unroll 1
-                        for (int c = 0; c < N; c += 16) {
-                            float o[16];
-                            ld16(o_at + c, o);
-                            wait_ld(o);
+                        for (int c = 0; c < C; c += 8) {
+                            float o[8];
+                            ld8(o_at + c, o);
+                            wait_ld8(o);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] *= sm.part[0][c + e];
-                            st16(o_at + c, o);
+                            for (int e = 0; e < 8; ++e) o[e] *= sm.part[0][c0 + c + e];
+                            st8(o_at + c, o);
                         }
                         wait_st();
 #pragma unroll
-                        for (int c = 0; c < N; ++c) l[c] *= sm.part[0][c];
+                        for (int c = 0; c < C; ++c) l[c] *= sm.part[0][c0 + c];
                     }
+                    load_columns<C>(s_at, s);
 #pragma unroll
-                    for (int c = 0; c < N; c += 16) ld16(s_at + c, s + c);
-#pragma unroll
-                    for (int c = 0; c < N; c += 16) {
-                        wait_ld(s + c);
-                        weigh16(s + c, sm.nref + c, a.kf, masked, lo - c, hi - c);
-                    }
+                    for (int c = 0; c < C; c += 8) wait_ld8(s + c);
+                    weigh<C>(s, sm.nref + c0, a.kf, masked, lo, hi);
                 }
                 if (i >= Sh::kBuffers) products(g - Sh::kBuffers);       // (the weights that lie there have been multiplied)
                 char* const to = p_row + g % Sh::kBuffers * Sh::kP;
 #pragma unroll
-                for (int c = 0; c < N; c += 8) {
+                for (int c = 0; c < C; c += 8) {
                     uint32_t pk[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -572,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
                     // the next unit's rows
                     look_ahead();
                     if (next.more) {
-                        fetch_queries<NP, N>(a, sm.q[(unit + 1) & 1], next, nv.count, q_vec, tid);
+                        fetch_queries<NP, N, kSoft>(a, sm.q[(unit + 1) & 1], next, nv.count, q_vec, tid);
                         fetched_queries(sm.q_full);
                     }
                 }
@@ -580,16 +596,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
             if (!gone) products(g - 1);
             fence_after();
             // the sums: over the lanes, then (in what follows) over the warps
+            constexpr int c32 = C / 32 * 32, c16 = (C - c32) / 16 * 16, c8 = C - c32 - c16;
+            float* const sums = sm.part[quarter] + c0;
 #pragma unroll
-            for (int c = 0; c < N; c += 32) {
-                if (c + 32 <= N) {
-                    sm.part[warp][c + lane] = across<32>(l + c, lane);
-                } else {
-                    const float x = across<16>(l + c, lane);
-                    if (lane < 16) sm.part[warp][c + lane] = x;
-                }
+            for (int c = 0; c < c32; c += 32) sums[c + lane] = across<32>(l + c, lane);
+            if constexpr (c16 > 0) {
+                const float x = across<16>(l + c32, lane);
+                if (lane < 16) sums[c32 + lane] = x;
             }
-            const bool bad = soft_any(w.s.bad || failed || gone) || *static_cast<volatile int*>(&sm.bad[unit % kUnits]) != 0;
+            if constexpr (c8 > 0) {
+                const float x = across<8>(l + c32 + c16, lane);
+                if (lane < 8) sums[c32 + c16 + lane] = x;
+            }
+            const bool bad = soft_any<kSoft>(w.s.bad || failed || gone) || *static_cast<volatile int*>(&sm.bad[unit % kUnits]) != 0;
             const bool fix = *static_cast<volatile int*>(&sm.fix) != 0;
             float* part = leave_unit(a, sh, w, v.count, sm.joint, tid);
             if (tid < N) {
@@ -600,14 +619,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
                 }
                 sm.part[0][tid] = sum == 0.f ? 0.f : 1.f / sum;
             }
-            soft_sync();
+            soft_sync<kSoft>();
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + w.b * a.os[0] + w.h * a.group * a.os[2] + dim;
 #pragma unroll 1
-            for (int c0 = 0; c0 < v.count; c0 += 16) {
-                float o[16];
+            for (int c = 0; c < C && c0 + c < v.count; c += 8) {
+                float o[8];
                 __syncwarp();
-                ld16(o_at + c0, o);
-                wait_ld(o);
+                ld8(o_at + c, o);
+                wait_ld8(o);
                 if (fix && has_dim) {
                     // what is not finite among the values that some rows see and others do not
 #pragma unroll 1
@@ -624,30 +643,28 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
                             const float val = to_float((static_cast<const __nv_bfloat16*>(a.v) + page * a.vs[0] + w.h * a.vs[1] + (p - j * a.page) * a.vs[2])[dim]);
                             if (isfinite(val)) continue;
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                const int pos = w.s.base + a.by_group(w.r0 + c0 + e);
+                            for (int e = 0; e < 8; ++e) {
+                                const int pos = w.s.base + a.by_group(w.r0 + c0 + c + e);
                                 if (p <= pos && (p >= low_of(a, pos) || p < a.sinks)) o[e] += val;
                             }
                         }
                     }
                 }
+                const int left = has_dim ? v.count - c0 - c : 0;
                 if (part) {
-                    float* const at = part + 2 * a.rows + c0 * a.D + dim;
+                    float* const at = part + 2 * a.rows + (c0 + c) * a.D + dim;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (c0 + e < v.count && has_dim) at[e * a.D] = o[e];
+                    for (int e = 0; e < 8; ++e)
+                        if (e < left) at[e * a.D] = o[e];
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int r = w.r0 + c0 + e, t = a.by_group(r);
-                        const float val = o[e] * sm.part[0][c0 + e];
-                        if (c0 + e < v.count && has_dim) out[t * a.os[1] + (r - t * a.group) * a.os[2]] = __float2bfloat16_rn(val);
-                    }
+                    for (int e = 0; e < 8; ++e)
+                        if (e < left) out[sm.off[c0 + c + e]] = __float2bfloat16_rn(o[e] * sm.part[0][c0 + c + e]);
                 }
             }
             if (!ahead) look_ahead();          // (a launch that gives up)
             fence_before();
-            soft_sync();
+            soft_sync<kSoft>();
             if (tid == 0) sm.fix = sm.bad[unit % kUnits] = 0;
             w = next;
             v = nv;
@@ -657,8 +674,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const AttendA
     fence_before();
     __syncthreads();
     fence_after();
-    if (warp == kIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Sh::kColumns) : "memory");
-    join_units<__nv_bfloat16>(a, sm.joint, tid, kThreads);
+    if (warp == Sh::kIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Sh::kColumns) : "memory");
+    join_units<__nv_bfloat16>(a, sm.joint, tid, Sh::kThreads);
 }
 
 // ---- launch ------------------------------------------------------------------------------------------------------------
@@ -693,7 +710,7 @@ template <int NP, int N>
 cudaError_t launch(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, bool q_vec, int ctas, cudaStream_t stream) {
     const cudaError_t e = cudaFuncSetAttribute(attend_tiles_kernel<NP, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<NP, N>::kBytes);
     if (e != cudaSuccess) return e;
-    return launch_together(attend_tiles_kernel<NP, N>, ctas, kThreads, Shape<NP, N>::kBytes, stream, a, k, v, static_cast<int>(q_vec));
+    return launch_together(attend_tiles_kernel<NP, N>, ctas, Shape<NP, N>::kThreads, Shape<NP, N>::kBytes, stream, a, k, v, static_cast<int>(q_vec));
 }
 template <int NP>
 cudaError_t pick(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, bool q_vec, int ctas, cudaStream_t stream) {
