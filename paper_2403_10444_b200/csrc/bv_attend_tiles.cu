@@ -12,7 +12,7 @@
 // (a vote per tile) the new maxima are formed, and O and the sums scaled by the power of two between the old and the new
 // reference.  Sums stay per thread until a unit ends.  Weights are rounded to 16 bits for the second product, and the sums are taken of the rounded weights: a row of one
 // key is that key's value exactly, and the error of a row, 2^-9 of its terms at most, is that of an output rounded once more.
-// The next unit's query rows come in while a unit is gone through, and its first scores before the unit's last products.
+// The next unit's query rows come in, and its first scores are formed, while a unit is brought to its end.
 //
 // What a row may not see is taken out twice: its weight is 0 whatever the score is, and rows of V that no row of the unit sees (or that were never
 // loaded) are set to 0 in shared memory, since 0 times an infinity is not 0.  Rows of V that some see and others do not keep their finite
@@ -125,12 +125,12 @@ struct Shape {
     static constexpr int kQ = NP * N * 128, kP = N * kTile * 2;
     static constexpr int kRest = 3072;
     // two buffers for the weights (the next tile's are formed while the last one's are multiplied) where that leaves five slots
-    static constexpr int kTwo = (227 * 1024 - kRest - 2 * kQ - 2 * kP) / kSlot;
+    static constexpr int kTwo = (227 * 1024 - kRest - kQ - 2 * kP) / kSlot;
     static constexpr int kBuffers = kTwo >= 5 ? 2 : 1;
-    static constexpr int kFit = (227 * 1024 - kRest - 2 * kQ - kBuffers * kP) / kSlot;
+    static constexpr int kFit = (227 * 1024 - kRest - kQ - kBuffers * kP) / kSlot;
     static constexpr int kSlots = kFit < 8 ? kFit : 8;
     static constexpr int kColumns = 3 * N <= 64 ? 64 : 3 * N <= 128 ? 128 : 256;      // of tensor memory: S twice, O
-    static constexpr int kBytes = kSlots * kSlot + 2 * kQ + kBuffers * kP + kRest;
+    static constexpr int kBytes = kSlots * kSlot + kQ + kBuffers * kP + kRest;
     static_assert(kSlots >= 4, "two tiles in flight");
 };
 constexpr int kUnits = 8;                      // units that may be in flight: no more than slots
@@ -138,7 +138,7 @@ template <int NP, int N>
 struct __align__(1024) Smem {
     using Sh = Shape<NP, N>;
     char ring[Sh::kSlots][Sh::kSlot];
-    char q[2][Sh::kQ];
+    char q[Sh::kQ];
     char p[Sh::kBuffers][Sh::kP];
     float nref[N];                             // minus the references
     float part[4][N];                          // maxima by warp; then in part[0] what the move of the references scales by
@@ -258,7 +258,7 @@ __device__ __forceinline__ void load_tiles(const AttendArgs& a, Smem<NP, N>& sm,
             if ((y & 1) == which) mbar_wait_now(smem_u32(&sm.full[y % Sh::kSlots]), y / Sh::kSlots & 1, a.status, limit);
 }
 
-// The products, by one thread: S of a tile before O of the one before it.
+// The products, by one thread: S of a tile before O of the one before it, but at a unit's end.
 template <int NP, int N>
 __device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>& sm, Walk w, int total, uint32_t tmem, uint32_t limit) {
     using Sh = Shape<NP, N>;
@@ -268,7 +268,7 @@ __device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>&
     auto wait = [&](unsigned long long& bar, int phase) { ok = ok && mbar_wait_now(smem_u32(&bar), phase & 1, a.status, limit); };
     int unit = 0, left = w.upto - w.i;         // of the tile whose scores come next
     unsigned starts = 0;                       // bit t & 1: tile t is its unit's first
-    uint32_t q_low = 0;
+    const uint32_t q_low = desc_low(smem_u32(sm.q), 16);
     auto scores = [&](int t) {
         bool first = t == 0;
         if (left == 0) {
@@ -278,10 +278,7 @@ __device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>&
             first = true;
         }
         --left;
-        if (first) {
-            wait(sm.q_full, unit);
-            q_low = desc_low(smem_u32(sm.q[unit & 1]), 16);
-        }
+        if (first) wait(sm.q_full, unit);
         starts = (starts & ~(1u << (t & 1))) | static_cast<unsigned>(first) << (t & 1);
         const int slot = 2 * t % Sh::kSlots;
         wait(sm.full[slot], 2 * t / Sh::kSlots);
@@ -297,7 +294,9 @@ __device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>&
     if (total > 0) scores(0);
 #pragma unroll 1
     for (int g = 0; g < total && ok; ++g) {
-        if (g + 1 < total) scores(g + 1);
+        // (the next unit's rows take the place of this one's when its last scores are there: its end does not wait for them)
+        const bool last = left == 0;
+        if (g + 1 < total && !last) scores(g + 1);
         const int x = 2 * g + 1, slot = x % Sh::kSlots;
         wait(sm.full[slot], x / Sh::kSlots);
         const int buffer = g % Sh::kBuffers;
@@ -311,6 +310,7 @@ __device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>&
         for (int j = 0; j < kTile / 16; ++j) mma(o_at, desc(v_low + j * 128, desc_high(1024, 2)), desc(p_low + j * 16, desc_high(2048, 0)), pv, add || j > 0);
         commit(smem_u32(&sm.empty[slot]));
         commit(smem_u32(&sm.p_done[buffer]));
+        if (g + 1 < total && last) scores(g + 1);
     }
     if (!ok) {
         commit(smem_u32(&sm.drain));
@@ -413,7 +413,10 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
     if (warp == Sh::kKeys || warp == Sh::kValues) {
         load_tiles<NP, N>(a, sm, w, warp == Sh::kKeys ? &k_map : &v_map, warp == Sh::kValues, limit);
     } else if (warp == Sh::kIssuer) {
-        if (lane == 0) issue_products<NP, N>(a, sm, w, static_cast<int>(sh.end - sh.begin), tmem, limit);
+        // (the lane is elected, not chosen by its number, so that the compiler knows that it is one: a fourth less time an instruction)
+        uint32_t one;
+        asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+        if (one) issue_products<NP, N>(a, sm, w, static_cast<int>(sh.end - sh.begin), tmem, limit);
         __syncwarp();
     } else {
         // ---- weights
@@ -442,7 +445,7 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
         View v{};
         if (w.more) {
             v = view_of(a, w);
-            fetch_queries<NP, N, kSoft>(a, sm.q[0], w, v.count, q_vec, tid);
+            fetch_queries<NP, N, kSoft>(a, sm.q, w, v.count, q_vec, tid);
             fetched_queries(sm.q_full);
         }
 #pragma unroll 1
@@ -493,12 +496,17 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                         const int xv = 2 * g + 1;
                         lane_wait(sm.full[xv % kSlots], xv / kSlots);
                         char* row = sm.ring[xv % kSlots] + key * 128;
+                        if (!any) {
+#pragma unroll
+                            for (int e = 0; e < 8 * NP / Sh::kHalves; ++e) {
+                                const int x = half * 8 * NP / Sh::kHalves + e;
+                                *reinterpret_cast<uint4*>(row + x / 8 * Sh::kPanel + ((x + lane) % 8) * 16) = make_uint4(0, 0, 0, 0);
+                            }
+                        } else {
 #pragma unroll 1
-                        for (int e = half * 8 * NP / Sh::kHalves; e < (half + 1) * 8 * NP / Sh::kHalves; ++e) {
-                            uint4* at = reinterpret_cast<uint4*>(row + e / 8 * Sh::kPanel + ((e + lane) % 8) * 16);
-                            uint4 val = make_uint4(0, 0, 0, 0);
-                            if (any) {
-                                val = *at;
+                            for (int e = half * 8 * NP / Sh::kHalves; e < (half + 1) * 8 * NP / Sh::kHalves; ++e) {
+                                uint4* at = reinterpret_cast<uint4*>(row + e / 8 * Sh::kPanel + ((e + lane) % 8) * 16);
+                                uint4 val = *at;
                                 bool odd = false;
                                 auto finite = [&](uint32_t& x) {
                                     if ((x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; odd = true; }
@@ -507,8 +515,8 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                                 finite(val.x); finite(val.y); finite(val.z); finite(val.w);
                                 if (!odd) continue;
                                 sm.fix = 1;
+                                *at = val;
                             }
-                            *at = val;
                         }
                     }
                     __syncwarp();
@@ -584,16 +592,14 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                 fence_async();
                 fence_before();
                 mbar_arrive(smem_u32(&sm.p_full[g % Sh::kBuffers]));
-                if (i == 0) {
-                    // the next unit's rows
-                    look_ahead();
-                    if (next.more) {
-                        fetch_queries<NP, N, kSoft>(a, sm.q[(unit + 1) & 1], next, nv.count, q_vec, tid);
-                        fetched_queries(sm.q_full);
-                    }
-                }
             }
-            if (!gone) products(g - 1);
+            // the next unit's rows, now that this one's have their scores
+            if (!gone) {
+                look_ahead();
+                if (next.more) fetch_queries<NP, N, kSoft>(a, sm.q, next, nv.count, q_vec, tid);
+                products(g - 1);
+                if (next.more) fetched_queries(sm.q_full);
+            }
             fence_after();
             // the sums: over the lanes, then (in what follows) over the warps
             constexpr int c32 = C / 32 * 32, c16 = (C - c32) / 16 * 16, c8 = C - c32 - c16;
