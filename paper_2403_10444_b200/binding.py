@@ -441,16 +441,39 @@ def _lse_call(name, target_logits, draft_logits, draft_tokens, uniforms, draft_l
 
 
 # ---- the paged key-value cache (include/bv.h, struct bv_cache) ----
+#
+# A call of the cache takes some 10 us on the GPU and is made for every layer, so the checks are made on what each tensor is
+# asked once (an attribute costs 0.1 us); what a check finds wrong is put in words where it fails.
 
 _CACHE = struct.Struct("@5Q6q8i")
 _STRIDES = struct.Struct("@3q")
+_I32 = torch.int32
+_CODES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
 
 
-def _pool(t, name: str):
-    """Strides of a pool of pages [num_pages, heads, page_size, D]."""
-    if t.dim() != 4 or t.stride(3) != 1:
-        raise ValueError("%s must be [num_pages, heads, page_size, D] with contiguous rows of D" % name)
-    return t.stride()
+def _pools(k, v):
+    """(shape, strides of k, strides of v, dtype code, dtype, device) of two pools of pages [num_pages, heads, page_size, D]."""
+    shape, ks, vs, dtype, dev = k.shape, k.stride(), v.stride(), k.dtype, k.get_device()
+    if len(shape) != 4 or ks[3] != 1 or len(vs) != 4 or vs[3] != 1:
+        raise ValueError("k and v must be [num_pages, heads, page_size, D] with contiguous rows of D")
+    if v.shape != shape or v.dtype is not dtype:
+        raise ValueError("k and v must have one shape and dtype")
+    code = _CODES.get(dtype)
+    if code is None:
+        raise TypeError("keys and values must be float32 or bfloat16, got %s" % dtype)
+    return shape, ks, vs, code, dtype, dev
+
+
+def _table(table, lens):
+    """(B, width, device) of a table of pages and its lengths."""
+    shape, dev = table.shape, table.get_device()
+    if len(shape) != 2 or lens.shape != shape[:1] or table.dtype is not _I32 or lens.dtype is not _I32:
+        raise ValueError("table must be int32 [B, width] and lens int32 [B]")
+    if not (table.is_contiguous() and lens.is_contiguous()):
+        raise ValueError("table and lens must be contiguous")
+    if dev < 0 or lens.get_device() != dev:
+        raise ValueError("expected CUDA tensors on one device")
+    return shape[0], shape[1], dev
 
 
 def _written(t, name: str) -> None:
@@ -459,46 +482,33 @@ def _written(t, name: str) -> None:
         raise ValueError("%s must not be an expanded tensor" % name)
 
 
-def _sequences(table, lens):
-    if table.dim() != 2 or lens.dim() != 1 or lens.shape[0] != table.shape[0] or table.dtype != torch.int32 or lens.dtype != torch.int32:
-        raise ValueError("table must be int32 [B, width] and lens int32 [B]")
-    if not (table.is_contiguous() and lens.is_contiguous()):
-        raise ValueError("table and lens must be contiguous")
-    dev = table.get_device()
-    if dev < 0 or lens.get_device() != dev:
-        raise ValueError("expected CUDA tensors on one device")
-    return table.shape
-
-
 def _counted(t, n: int, dev: int, name: str):
     """Address of an int32 [n] on the cache's device (None: null)."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != dev:
+    if t.dtype is not _I32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != dev:
         raise ValueError("%s must be a contiguous int32 tensor [%d] on the cache's device" % (name, n))
     return t.data_ptr()
 
 
-def _cache(k, v, table, lens) -> bytes:
-    ks, vs = _pool(k, "k"), _pool(v, "v")
-    B, width = _sequences(table, lens)
-    P, heads, page, D = k.shape
-    if v.shape != k.shape or v.dtype != k.dtype:
-        raise ValueError("k and v must have one shape and dtype")
-    if not k.get_device() == v.get_device() == table.get_device():
+def _cache(k, v, table, lens):
+    """The packed cache, its B, heads, D, dtype and device."""
+    (P, heads, page, D), ks, vs, code, dtype, dev = _pools(k, v)
+    B, width, on = _table(table, lens)
+    if dev != on or v.get_device() != on:
         raise ValueError("expected CUDA tensors on one device")
     return _CACHE.pack(k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr(), 0, ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
-                       B, width, P, page, heads, D, _dtype_code(k), 0)
+                       B, width, P, page, heads, D, code, 0), B, heads, D, dtype, dev
 
 
-def _rows(t, n_heads, like, B: int, name: str):
-    """Checks [B, n, heads, D] of the cache's dtype on its device; (n, heads, packed strides)."""
-    if t.dim() != 4 or t.shape[0] != B or t.shape[3] != like.shape[3] or (n_heads and t.shape[2] != n_heads) or t.dtype != like.dtype:
+def _rows(t, B: int, heads: int, D: int, dtype, dev: int, name: str):
+    """(n, heads, packed strides) of a tensor [B, n, heads, D] that goes with the cache (heads = 0: any number)."""
+    shape, st = t.shape, t.stride()
+    if len(shape) != 4 or shape[0] != B or shape[3] != D or (heads and shape[2] != heads) or t.dtype is not dtype:
         raise ValueError("%s must be [B, n, heads, D] of the cache's dtype" % name)
-    st = t.stride()
-    if st[3] != 1 or t.get_device() != like.get_device():
+    if st[3] != 1 or t.get_device() != dev:
         raise ValueError("%s must have contiguous rows of D on the cache's device" % name)
-    return t.shape[1], t.shape[2], _STRIDES.pack(st[0], st[1], st[2])
+    return shape[1], shape[2], _STRIDES.pack(st[0], st[1], st[2])
 
 
 def bv_cache_attend(q, k, v, table, lens, n_new=None, scale: Optional[float] = None, window: int = 0, sinks: int = 0, out=None,
@@ -509,109 +519,123 @@ def bv_cache_attend(q, k, v, table, lens, n_new=None, scale: Optional[float] = N
     ``table`` int32 [B, width], ``lens`` int32 [B] (the newest tokens counted in), ``n_new`` int32 [B] or None: every sequence
     brings n.  ``scale``: 1/sqrt(D) by default; ``window`` > 0: a token sees its last ``window`` positions and the first ``sinks``.
     Returns ``out`` [B, n, q_heads, D] (rows beyond n_new[b] are not written: zero in a tensor made here)."""
-    B = table.shape[0]
-    blob = _cache(k, v, table, lens)
-    n, heads, qs = _rows(q, 0, k, B, "q")
-    dev = k.device
+    blob, B, _, D, dtype, dev = _cache(k, v, table, lens)
+    n, heads, qs = _rows(q, B, 0, D, dtype, dev, "q")
     if out is None:
-        out = torch.empty((B, n, heads, k.shape[3]), dtype=k.dtype, device=dev) if n_new is None else \
-            torch.zeros((B, n, heads, k.shape[3]), dtype=k.dtype, device=dev)
+        out = q.new_empty((B, n, heads, D)) if n_new is None else q.new_zeros((B, n, heads, D))
     else:
         _written(out, "out")
-        if out.shape != q.shape:
-            raise ValueError("out must have the shape of q")
-    os_ = _rows(out, heads, k, B, "out")[2]
-    new = _counted(n_new, B, dev.index, "n_new")
-    with _on(dev):
-        _check(load_library().bv_cache_attend(blob, q.data_ptr(), qs, new, n, heads, k.shape[3] ** -0.5 if scale is None else scale,
-                                              window, sinks, out.data_ptr(), os_, _raw_stream(dev, stream)))
+    n_out, _, os_ = _rows(out, B, heads, D, dtype, dev, "out")
+    if n_out != n:
+        raise ValueError("out must have the shape of q")
+    new = None if n_new is None else _counted(n_new, B, dev, "n_new")
+    lib = _lib or load_library()
+    with _on(q.device):
+        status = lib.bv_cache_attend(blob, q.data_ptr(), qs, new, n, heads, D ** -0.5 if scale is None else scale, window, sinks,
+                                     out.data_ptr(), os_, _raw_stream(q.device, stream))
+    if status:
+        _check(status)
     return out
 
 
 def bv_cache_append(k_new, v_new, k, v, table, lens, n_new=None, stream=None) -> None:
     """Stores the keys and values of the newest tokens [B, n, heads, D] in the pages of their positions (see include/bv.h)."""
-    B = table.shape[0]
-    blob = _cache(k, v, table, lens)
-    n, _, ks = _rows(k_new, k.shape[1], k, B, "k_new")
-    n_v, _, vs = _rows(v_new, k.shape[1], k, B, "v_new")
+    blob, B, heads, D, dtype, dev = _cache(k, v, table, lens)
+    n, _, ks = _rows(k_new, B, heads, D, dtype, dev, "k_new")
+    n_v, _, vs = _rows(v_new, B, heads, D, dtype, dev, "v_new")
     if n != n_v:
         raise ValueError("k_new and v_new must have one shape")
     _written(k, "k")
     _written(v, "v")
-    dev = k.device
-    new = _counted(n_new, B, dev.index, "n_new")
-    with _on(dev):
-        _check(load_library().bv_cache_append(blob, k_new.data_ptr(), ks, v_new.data_ptr(), vs, new, n, _raw_stream(dev, stream)))
+    new = None if n_new is None else _counted(n_new, B, dev, "n_new")
+    lib = _lib or load_library()
+    with _on(k.device):
+        status = lib.bv_cache_append(blob, k_new.data_ptr(), ks, v_new.data_ptr(), vs, new, n, _raw_stream(k.device, stream))
+    if status:
+        _check(status)
 
 
-def _book(table, lens, refs, page_size: int) -> bytes:
-    B, width = _sequences(table, lens)
-    if refs.dtype != torch.int32 or refs.dim() != 1 or not refs.is_contiguous() or refs.get_device() != table.get_device():
+def _book(table, lens, refs, page_size: int):
+    """The packed cache of a call that moves no keys, B and device."""
+    B, width, dev = _table(table, lens)
+    if refs.dtype is not _I32 or refs.dim() != 1 or not refs.is_contiguous() or refs.get_device() != dev:
         raise ValueError("refs must be a contiguous int32 tensor [num_pages] on the table's device")
-    return _CACHE.pack(0, 0, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), 0, 0, 0, 0, 0, 0, B, width, refs.shape[0], page_size, 0, 0, 0, 0)
+    return _CACHE.pack(0, 0, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), 0, 0, 0, 0, 0, 0, B, width, refs.shape[0], page_size, 0, 0, 0, 0), B, dev
 
 
 def bv_pages_extend(table, lens, refs, page_size: int, n: int, n_new=None, stream=None):
     """Lengthens every sequence by n (or n_new[b] in 0 .. n) tokens, taking the lowest free pages (refs 0) in the sequences' order; table, lens and
     refs change in place.  Returns (new int32 [B]: the tokens, or -1 for a sequence left as it was; copies int32 [B, 2]: the pages that
     bv_pages_copy is to copy, or -1)."""
-    blob = _book(table, lens, refs, page_size)
-    dev, B = table.device, table.shape[0]
+    blob, B, dev = _book(table, lens, refs, page_size)
+    given = None if n_new is None else _counted(n_new, B, dev, "n_new")
     new, copies = table.new_empty((B,)), table.new_empty((B, 2))
-    given = _counted(n_new, B, dev.index, "n_new")
-    with _on(dev):
-        _check(load_library().bv_pages_extend(blob, given, n, new.data_ptr(), copies.data_ptr(), _raw_stream(dev, stream)))
+    lib = _lib or load_library()
+    with _on(table.device):
+        status = lib.bv_pages_extend(blob, given, n, new.data_ptr(), copies.data_ptr(), _raw_stream(table.device, stream))
+    if status:
+        _check(status)
     return new, copies
 
 
 def bv_pages_truncate(table, lens, refs, page_size: int, keep, n: int = 0, n_new=None, stream=None) -> None:
     """Keeps the first keep[b] of the n (or n_new[b]) newest tokens of each sequence, with n = 0 of all its tokens, and gives back the pages
     that hold nothing any more.  ``keep`` may be the out_len of a verification."""
-    blob = _book(table, lens, refs, page_size)
-    dev, B = table.device, table.shape[0]
-    kept, given = _counted(keep, B, dev.index, "keep"), _counted(n_new, B, dev.index, "n_new")
-    with _on(dev):
-        _check(load_library().bv_pages_truncate(blob, kept, given, n, _raw_stream(dev, stream)))
+    blob, B, dev = _book(table, lens, refs, page_size)
+    kept, given = _counted(keep, B, dev, "keep"), None if n_new is None else _counted(n_new, B, dev, "n_new")
+    lib = _lib or load_library()
+    with _on(table.device):
+        status = lib.bv_pages_truncate(blob, kept, given, n, _raw_stream(table.device, stream))
+    if status:
+        _check(status)
 
 
 def bv_pages_fork(table, lens, refs, page_size: int, src, dst, stream=None):
     """Makes sequence dst[i] a second copy of src[i] on the same pages.  Returns ok int32: 0, or -1 where a fork is refused."""
-    blob = _book(table, lens, refs, page_size)
-    dev, forks = table.device, src.shape[0]
-    s, d = _counted(src, forks, dev.index, "src"), _counted(dst, forks, dev.index, "dst")
+    blob, _, dev = _book(table, lens, refs, page_size)
+    forks = src.shape[0] if src.dim() == 1 else -1
+    s, d = _counted(src, forks, dev, "src"), _counted(dst, forks, dev, "dst")
     ok = table.new_empty((forks,))
-    with _on(dev):
-        _check(load_library().bv_pages_fork(blob, s, d, forks, ok.data_ptr(), _raw_stream(dev, stream)))
+    if forks == 0:
+        return ok
+    lib = _lib or load_library()
+    with _on(table.device):
+        status = lib.bv_pages_fork(blob, s, d, forks, ok.data_ptr(), _raw_stream(table.device, stream))
+    if status:
+        _check(status)
     return ok
 
 
 def bv_pages_compact(table, lens, refs, page_size: int, stream=None):
     """Renumbers the pages so that those in use come first.  Returns (moves int32 [num_pages // 2, 2], count int32 [1]), which
     bv_pages_copy takes for each layer before anything else uses the cache."""
-    blob = _book(table, lens, refs, page_size)
-    dev = table.device
+    blob, _, _ = _book(table, lens, refs, page_size)
     moves, count = table.new_empty((refs.shape[0] // 2, 2)), table.new_empty((1,))
-    with _on(dev):
+    lib = _lib or load_library()
+    with _on(table.device):
         # (a pool of one page has no moves, and no place for them)
-        _check(load_library().bv_pages_compact(blob, moves.data_ptr() or count.data_ptr(), count.data_ptr(), _raw_stream(dev, stream)))
+        status = lib.bv_pages_compact(blob, moves.data_ptr() or count.data_ptr(), count.data_ptr(), _raw_stream(table.device, stream))
+    if status:
+        _check(status)
     return moves, count
 
 
 def bv_pages_copy(k, v, pairs, count=None, stream=None) -> None:
     """Copies pages, keys and values: pairs int32 [n, 2] of source and destination, of which the first count[0] are looked at."""
-    ks, vs = _pool(k, "k"), _pool(v, "v")
+    (P, heads, page, D), ks, vs, code, _, dev = _pools(k, v)
     _written(k, "k")
     _written(v, "v")
-    dev = k.device
-    if v.shape != k.shape or v.dtype != k.dtype or v.get_device() != k.get_device() or not k.is_cuda:
-        raise ValueError("k and v must have one shape, dtype and CUDA device")
-    if pairs.dtype != torch.int32 or pairs.dim() != 2 or pairs.shape[1] != 2 or not pairs.is_contiguous() or pairs.get_device() != dev.index:
+    if dev < 0 or v.get_device() != dev:
+        raise ValueError("expected CUDA tensors on one device")
+    shape = pairs.shape
+    if pairs.dtype is not _I32 or len(shape) != 2 or shape[1] != 2 or not pairs.is_contiguous() or pairs.get_device() != dev:
         raise ValueError("pairs must be a contiguous int32 tensor [n, 2] on the cache's device")
-    P, heads, page, D = k.shape
-    n = pairs.shape[0]
-    blob = _CACHE.pack(k.data_ptr(), v.data_ptr(), 0, 0, 0, ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], 0, 0, P, page, heads, D, _dtype_code(k), 0)
-    upto = _counted(count, 1, dev.index, "count")
-    if n == 0:
+    upto = None if count is None else _counted(count, 1, dev, "count")
+    if shape[0] == 0:
         return
-    with _on(dev):
-        _check(load_library().bv_pages_copy(blob, pairs.data_ptr(), n, upto, _raw_stream(dev, stream)))
+    blob = _CACHE.pack(k.data_ptr(), v.data_ptr(), 0, 0, 0, ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], 0, 0, P, page, heads, D, code, 0)
+    lib = _lib or load_library()
+    with _on(k.device):
+        status = lib.bv_pages_copy(blob, pairs.data_ptr(), shape[0], upto, _raw_stream(k.device, stream))
+    if status:
+        _check(status)

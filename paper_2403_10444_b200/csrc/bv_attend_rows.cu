@@ -259,7 +259,8 @@ template <typename T, int NJ, int R>
 cudaError_t launch(const AttendArgs& a, bool aligned, int ctas, cudaStream_t stream) {
     constexpr int bytes = static_cast<int>(sizeof(RowsSmem<T, NJ, R>));
     static_assert(bytes <= 227 * 1024, "fits an SM");
-    const cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<T, NJ, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    static std::atomic<unsigned long long> asked{0};
+    const cudaError_t e = allow_shared(attend_rows_kernel<T, NJ, R>, bytes, asked);
     if (e != cudaSuccess) return e;
     return launch_together(attend_rows_kernel<T, NJ, R>, ctas, kThreads, bytes, stream, a, static_cast<int>(aligned));
 }

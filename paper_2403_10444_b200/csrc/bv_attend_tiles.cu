@@ -714,7 +714,8 @@ bool encode(const AttendArgs& a, const void* pool, const long long* stride, CUte
 
 template <int NP, int N>
 cudaError_t launch(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, bool q_vec, int ctas, cudaStream_t stream) {
-    const cudaError_t e = cudaFuncSetAttribute(attend_tiles_kernel<NP, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<NP, N>::kBytes);
+    static std::atomic<unsigned long long> asked{0};
+    const cudaError_t e = allow_shared(attend_tiles_kernel<NP, N>, Shape<NP, N>::kBytes, asked);
     if (e != cudaSuccess) return e;
     return launch_together(attend_tiles_kernel<NP, N>, ctas, Shape<NP, N>::kThreads, Shape<NP, N>::kBytes, stream, a, k, v, static_cast<int>(q_vec));
 }

@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 #include "../../include/bv.h"
@@ -377,6 +378,16 @@ __device__ __forceinline__ void join_units(const AttendArgs& a, JointSmem& js, i
     if (tid < n) atomicInc(counter, 2 * parts - 1);
 }
 
+// Lets a kernel have `bytes` of shared memory: asked once per kernel and device (a call takes 1 us of host time).
+template <typename K>
+cudaError_t allow_shared(K* kernel, int bytes, std::atomic<unsigned long long>& devices) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (devices.load(std::memory_order_acquire) >> (dev & 63) & 1)) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) devices.fetch_or(1ull << (dev & 63), std::memory_order_release);
+    return e;
+}
 // A cooperative launch of as many of `ctas` CTAs as can run at once (a process that is given a part of the GPU has fewer).
 template <typename... P, typename... A>
 cudaError_t launch_together(void (*kernel)(P...), int ctas, int threads, size_t smem, cudaStream_t stream, A... args) {

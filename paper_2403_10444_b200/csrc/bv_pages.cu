@@ -406,7 +406,8 @@ extern "C" int bv_pages_extend(const bv_cache* c, const int32_t* n_new, int n, i
     if (a.B == 0) return BV_OK;
     a.n_new = n_new;
     a.n = n;
-    cudaError_t e = cudaFuncSetAttribute(bv::extend_pages_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(bv::ExtendSmem)));
+    static std::atomic<unsigned long long> asked{0};
+    cudaError_t e = bv::allow_shared(bv::extend_pages_kernel, static_cast<int>(sizeof(bv::ExtendSmem)), asked);
     if (e == cudaSuccess)
         e = bv::one_cluster(bv::extend_pages_kernel, a.num_pages, sizeof(bv::ExtendSmem), static_cast<cudaStream_t>(stream), a, out_new, out_copies,
                             static_cast<int>(bv::on(a.refs, 16)));
