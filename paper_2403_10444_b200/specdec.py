@@ -3,6 +3,8 @@ models whose next-token logits depend on the last token only (two [V, V] tables 
 
     python -m paper_2403_10444_b200.specdec [--V 32768] [--B 64] [--gammas 2,4,8] [--iterations 32]
 
+(With ``--context L`` the models attend to all of their context, prompts of up to L tokens, on the library's key-value cache: see cached.py.)
+
 Each iteration drafts gamma tokens autoregressively with ``bv_draft_chain`` (one launch; or gamma calls of
 ``bv_sample_draft``), which also leaves every draft row's log-normaliser, looks up the target rows along the drafted path (the stand-in for the
 parallel scoring pass of the large model), and verifies the block with ``bv_verify_lse`` (Block
@@ -162,6 +164,31 @@ def block_efficiency(result) -> float:
     return float(result["tau"].float().mean().item()) + 1.0
 
 
+def context_main(args):
+    """The loop for models that attend to their context."""
+    from . import cached
+    tw, dw = wl.attention_models(args.V, "bf16", args.seed, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(args.seed)
+    prompts = torch.randint(args.V, (args.B, args.context), dtype=torch.int32, device="cuda", generator=gen)
+    lens = torch.randint(max(1, args.context // 4), args.context + 1, (args.B,), dtype=torch.int32, device="cuda", generator=gen)
+    for gamma in [int(x) for x in args.gammas.split(",")]:
+        ud, uv = wl.loop_uniforms(args.iterations, args.B, gamma, args.seed + gamma, "cuda")
+        for algo in ALGOS:
+            spent = []
+            for n in (2, args.iterations):                                                                           # warm-up, then all
+                models = [cached.Decoder(w, args.B, args.context + n * (gamma + 1), window=args.window, sinks=args.sinks) for w in (tw, dw)]
+                torch.cuda.synchronize()
+                t0 = time.perf_counter()
+                res = cached.run(*models, prompts, lens, ud[:n], uv[:n], gamma, args.temperature, algo, args.graph)
+                torch.cuda.synchronize()
+                spent.append(time.perf_counter() - t0)
+            print(json.dumps({"V": args.V, "B": args.B, "gamma": gamma, "algo": algo, "context": args.context, "window": args.window or None,
+                              "iterations": args.iterations, "temperature": args.temperature, "graph": args.graph,
+                              "block_efficiency": round(block_efficiency(res), 4), "tokens": int(res["lengths"].sum().item()),
+                              "ms_per_iteration": round(spent[1] / args.iterations * 1e3, 3),
+                              "tokens_per_s": round(float(res["lengths"].sum().item()) / spent[1], 1)}), flush=True)
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--V", type=int, default=32768)
@@ -174,8 +201,13 @@ def main():
     ap.add_argument("--top-p", type=float, default=0.0, help="mask both models' rows to their top-p nucleus")
     ap.add_argument("--graph", action="store_true", help="replay one captured iteration as a CUDA graph")
     ap.add_argument("--no-chain", action="store_true", help="draft with gamma sampler calls instead of one chain launch")
+    ap.add_argument("--context", type=int, default=0, help="models that attend to prompts of up to this many tokens (and what follows) on a paged cache")
+    ap.add_argument("--window", type=int, default=0, help="with --context: how many positions a token sees (0: all)")
+    ap.add_argument("--sinks", type=int, default=0, help="with --window: first positions that stay visible")
     args = ap.parse_args()
     bv.load_library()
+    if args.context > 0:
+        return context_main(args)
     tt, dt = wl.markov_models(args.V, "bf16", args.seed, 2.0, args.draft_sigma, 1.1, "cuda")
     if args.top_p > 0:
         tt, dt = wl.top_p_mask(tt, args.top_p, args.temperature), wl.top_p_mask(dt, args.top_p, args.temperature)

@@ -123,6 +123,30 @@ def markov_models(V: int, dtype: str, seed: int, target_sigma: float = 2.0, draf
     return t.to(td), d.to(td)
 
 
+def attention_models(V: int, dtype: str, seed: int, layers: int = 2, heads: int = 8, kv_heads: int = 2, head_dim: int = 64,
+                     noise: float = 0.02, sharpness: float = 3.0, device="cpu"):
+    """Synthetic decoders for the decoding loop on a key-value cache: (target, draft) as dicts of weights, next-token logits
+    a function of all the context.  A layer is causal attention with ``heads`` query heads on ``kv_heads`` key-value heads; random
+    weights at the scales that keep activations near one, the draft's the target's plus ``noise`` times as much of others;
+    logits have a standard deviation of about ``sharpness``."""
+    dev = torch.device(device)
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(seed)
+    td = torch.float32 if dtype == "f32" else torch.bfloat16
+    width = heads * head_dim
+
+    def weight(rows, cols, scale):
+        w = torch.randn((rows, cols), generator=gen, device=dev) * scale
+        d = w + torch.randn((rows, cols), generator=gen, device=dev) * (scale * noise)
+        return w.to(td), d.to(td)
+
+    embed = weight(V, width, 1.0)
+    stack = [(weight(width, (heads + 2 * kv_heads) * head_dim, 1.5 * width ** -0.5), weight(width, width, width ** -0.5)) for _ in range(layers)]
+    unembed = weight(width, V, sharpness * (width * (1 + layers)) ** -0.5)
+    return tuple(dict(embed=embed[i], unembed=unembed[i], layers=[dict(qkv=qkv[i], out=out[i]) for qkv, out in stack],
+                      heads=heads, kv_heads=kv_heads, head_dim=head_dim) for i in (0, 1))
+
+
 def top_p_mask(table: torch.Tensor, top_p: float, temperature: float = 1.0) -> torch.Tensor:
     """Nucleus masking of every row of a [V, V] table of logits: the tokens of a row are kept in
     order of decreasing probability under softmax(row / temperature) until their mass reaches
