@@ -4,79 +4,204 @@
 // One pass over the keys with a running reference m and sum l per row:  p = 2^{k q.k - m},  l += p,  O += p v,  and where a score
 // exceeds m by more than 8 (first of all where m is still -inf)  m <- that score, l and O scaled by 2^{m_old - m}.  A reference
 // that lags by up to 8 costs nothing in 32 bits (terms of up to 256 instead of 1) and saves nearly all of the scaling.
+// A weight of zero takes no value, whatever that is.
 //
-// A CTA stages tiles of 32 keys and their values in shared memory, three deep, with 16-byte asynchronous copies (element by
-// element where rows are not whole aligned vectors).  Eight lanes share a key: each holds every 8th group of four of the row's D elements, of R query
-// rows at a time, in registers, so a key costs 2 R D / 8 FMAs and 3 R shuffles a lane.  The eight warps take different query rows
-// (RG groups of R) and, where there are fewer rows than that, different keys of the tile.
+// Two kernels.  Few query rows (a token of a group of up to 8 heads): the call is a matter of reading the cache.  Eight lanes share
+// a key, each with every 8th group of four of its D elements, of 4 query rows at a time, in registers; a warp has 4 keys of each tile
+// of 32, and every thread copies what it will read itself into a ring of cells of its own, several tiles ahead, so no thread
+// waits for another until the unit ends.  More rows: the FMAs bound.  A tile of 64 keys lies in shared memory, and both products
+// are tiled in registers: S by 2 rows x 4 keys a thread, O by 8 rows x 4 columns.
 #include "bv_cache.cuh"
 #include "bv_launch.h"
 
 namespace bv {
 namespace {
 
-constexpr int kThreads = 256, kWarps = 8, kKeys = 32, kStages = 3;
+constexpr int kThreads = 256, kWarps = 8;
+constexpr float kLag = 8.f;
 
-template <typename T> __device__ __forceinline__ void load4(const T* p, float (&x)[4]);
-template <> __device__ __forceinline__ void load4<float>(const float* p, float (&x)[4]) {
+__device__ __forceinline__ void widen(const float* p, float (&x)[4]) {
     const float4 v = *reinterpret_cast<const float4*>(p);
     x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
 }
-template <> __device__ __forceinline__ void load4<__nv_bfloat16>(const __nv_bfloat16* p, float (&x)[4]) {
+__device__ __forceinline__ void widen(const __nv_bfloat16* p, float (&x)[4]) {
     const uint2 v = *reinterpret_cast<const uint2*>(p);
     x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u);
     x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u);
 }
+__device__ __forceinline__ void copy4(float* to, const float* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy4(__nv_bfloat16* to, const __nv_bfloat16* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+
+// What the unit's rows see: positions p0 to p1 are theirs, low0 and low1 the first positions of the first and the last row's windows.
+struct Sight {
+    int count, p0, p1, low0, low1;
+};
+__device__ __forceinline__ Sight sight_of(const AttendArgs& a, const Walk& w) {
+    Sight s;
+    s.count = w.r0 + a.rows < w.s.rows ? a.rows : w.s.rows - w.r0;
+    s.p0 = w.s.base + a.by_group(w.r0);
+    s.p1 = w.s.base + a.by_group(w.r0 + s.count - 1);
+    s.low0 = low_of(a, s.p0);
+    s.low1 = low_of(a, s.p1);
+    return s;
+}
+// Where a key's row lies in the pools: false if nobody sees it, `bad` if its page is none.
+__device__ __forceinline__ bool key_row(const AttendArgs& a, const Walk& w, const Sight& s, int p, long long* k, long long* v, bool* bad) {
+    if (p > s.p1 || !(p >= s.low0 || p < a.sinks)) return false;
+    const int j = a.by_page(p), page = __ldg(a.table + static_cast<long long>(w.b) * a.width + j);
+    if (page < 0 || page >= a.num_pages) {
+        *bad = true;
+        return false;
+    }
+    const int row = p - j * a.page;
+    *k = page * a.ks[0] + w.h * a.ks[1] + row * a.ks[2];
+    *v = page * a.vs[0] + w.h * a.vs[1] + row * a.vs[2];
+    return true;
+}
+__device__ __forceinline__ bool whole_tile(const AttendArgs& a, const Sight& s, int start, int keys) {
+    return start + keys - 1 <= s.p0 && (start >= s.low1 || start + keys <= a.sinks);
+}
+__device__ __forceinline__ float factor_of(float m, float M) { return m == -INFINITY ? 0.f : exp2f(m - M); }
+
+// Elements d .. d + 3 of the unit's row `row` from their sums, to `out` or to the CTA's part of the unit.
+template <typename T>
+__device__ __forceinline__ void put(const AttendArgs& a, const Walk& w, float* part, int row, int d, float m, float l, const float (&o)[4]) {
+    if (part) {
+        float* const to = part + 2 * a.rows + row * a.D + d;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (d + e < a.D) to[e] = o[e];
+        if (d == 0) {
+            part[row] = m;
+            part[a.rows + row] = l;
+        }
+    } else {
+        const int r = w.r0 + row, t = a.by_group(r);
+        T* const to = static_cast<T*>(a.out) + w.b * a.os[0] + t * a.os[1] + (w.h * a.group + r - t * a.group) * a.os[2] + d;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (d + e < a.D) to[e] = from_float<T>(l == 0.f ? 0.f : o[e] / l);
+    }
+}
+
+// ---- few rows ----------------------------------------------------------------------------------------------------------
+
+constexpr int kFewKeys = 32;
 
 template <typename T, int NJ, int R>
-struct RowsSmem {
-    T tile[kStages][2][kKeys * NJ * 32];
-    long long row[4][2][kKeys];            // element offsets of the keys' rows, of tiles i .. i+3 (negative: no page)
+struct FewSmem {
+    static constexpr int kDepth = NJ <= 4 ? 5 : 3;                 // tiles ahead
+    T ring[kDepth][2 * NJ][kThreads][4];
     float part[kWarps][R][NJ * 32 + 2];
     ShareSmem share;
     JointSmem joint;
-    int bad;
 };
 
 template <typename T, int NJ, int R>
-__global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const AttendArgs a, const int aligned) {
-    extern __shared__ char smem_raw[];
-    using Smem = RowsSmem<T, NJ, R>;
-    Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
-    constexpr int kRow = NJ * 32;
+__global__ void __launch_bounds__(kThreads, 1) attend_few_kernel(const AttendArgs a, const int aligned, const int q_vec) {
+    extern __shared__ __align__(16) char raw[];
+    using Smem = FewSmem<T, NJ, R>;
+    Smem& sm = *reinterpret_cast<Smem*>(raw);
+    constexpr int kRow = NJ * 32, kDepth = Smem::kDepth;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int group8 = lane >> 3, l8 = lane & 7;
-    const int row_groups = a.rows / R;                     // 1, 2, 4 or 8
-    const int key_slices = kWarps / row_groups;
-    const int rg = warp % row_groups, ks = warp / row_groups;
-
-    // (columns D .. kRow of the staged rows are never copied to: they stay zero)
-    for (int x = tid; x < static_cast<int>(sizeof(sm.tile) / 16); x += kThreads) reinterpret_cast<uint4*>(&sm.tile[0][0][0])[x] = make_uint4(0, 0, 0, 0);
-    if (tid == 0) sm.bad = sm.joint.n = 0;
+    const int group8 = lane >> 3, l8 = lane & 7, mine = warp * 4 + group8;             // its key of a tile
+    if (a.D < kRow) {                          // (a thread's cells beyond D are never copied to: they stay zero)
+        for (int x = 0; x < kDepth * 2 * NJ; ++x)
+            for (int e = 0; e < 4; ++e) sm.ring[x / (2 * NJ)][x % (2 * NJ)][tid][e] = from_float<T>(0.f);
+    }
+    if (tid == 0) sm.joint.n = 0;
     const Share sh = find_share(a, sm.share, kThreads);
     Walk w = walk_begin(a, sh);
-
+#pragma unroll 1
     while (w.more) {
-        const int count = w.r0 + a.rows < w.s.rows ? a.rows : w.s.rows - w.r0;
+        const Sight v = sight_of(a, w);
         const int nt = w.upto - w.i;
-        // a row's position, and the positions it sees: low .. pos, and those below `sinks`
+        bool bad = w.s.bad;
+        // the page of the key that is fetched next, asked for a tile before that
+        int page = 0, row = 0;
+        bool seen = false;
+        auto find = [&](int i) {
+            const int p = i < nt ? tile_at(w.u, w.i + i) * kFewKeys + mine : 0, j = a.by_page(p);
+            seen = i < nt && p <= v.p1 && (p >= v.low0 || p < a.sinks);
+            row = p - j * a.page;
+            if (seen) page = __ldg(a.table + static_cast<long long>(w.b) * a.width + j);
+        };
+        auto fetch = [&](int i) {
+            const bool there = seen && page >= 0 && page < a.num_pages;
+            bad |= seen && !there;
+            if (there) {
+                T(*cell)[kThreads][4] = sm.ring[i % kDepth];
+                const T* k = static_cast<const T*>(a.k) + page * a.ks[0] + w.h * a.ks[1] + row * a.ks[2] + l8 * 4;
+                const T* vv = static_cast<const T*>(a.v) + page * a.vs[0] + w.h * a.vs[1] + row * a.vs[2] + l8 * 4;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    if (aligned) {
+                        if (j * 32 + l8 * 4 < a.D) {
+                            copy4(cell[2 * j][tid], k + j * 32);
+                            copy4(cell[2 * j + 1][tid], vv + j * 32);
+                        }
+                    } else {
+                        for (int e = 0; e < 4; ++e) {
+                            if (j * 32 + l8 * 4 + e < a.D) {
+                                cell[2 * j][tid][e] = k[j * 32 + e];
+                                cell[2 * j + 1][tid][e] = vv[j * 32 + e];
+                            }
+                        }
+                    }
+                }
+            }
+            cp_async_commit();
+        };
+        {
+            // (the first tiles' pages are asked for all at once)
+            int pages[kDepth - 1];
+            unsigned sees = 0;
+#pragma unroll
+            for (int i = 0; i < kDepth - 1; ++i) {
+                find(i);
+                pages[i] = page;
+                sees |= static_cast<unsigned>(seen) << i;
+            }
+#pragma unroll 1
+            for (int i = 0; i < kDepth - 1; ++i) {
+                const int p = i < nt ? tile_at(w.u, w.i + i) * kFewKeys + mine : 0;
+                row = p - a.by_page(p) * a.page;
+                seen = sees >> i & 1;
+                page = pages[0];
+#pragma unroll
+                for (int x = 0; x + 1 < kDepth - 1; ++x) pages[x] = pages[x + 1];
+                fetch(i);
+            }
+            find(kDepth - 1);
+        }
         float q[R][NJ * 4];
         int pos[R], low[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int row = w.r0 + rg * R + r;
-            const bool valid = rg * R + r < count;
-            const int t = valid ? a.by_group(row) : 0, g = valid ? row - t * a.group : 0;
+            const bool valid = r < v.count;
+            const int row = w.r0 + r, t = valid ? a.by_group(row) : 0;
             pos[r] = valid ? w.s.base + t : -1;
             low[r] = valid ? low_of(a, pos[r]) : 0;
-            const T* src = static_cast<const T*>(a.q) + w.b * a.qs[0] + t * a.qs[1] + (w.h * a.group + g) * a.qs[2];
+            const T* src = static_cast<const T*>(a.q) + w.b * a.qs[0] + t * a.qs[1] + (w.h * a.group + (valid ? row - t * a.group : 0)) * a.qs[2] + l8 * 4;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
+            for (int j = 0; j < NJ; ++j) {
+                float x[4] = {0.f, 0.f, 0.f, 0.f};
+                if (valid && j * 32 + l8 * 4 < a.D) {
+                    if (q_vec) {
+                        widen(src + j * 32, x);
+                    } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int d = j * 32 + l8 * 4 + e;
-                    q[r][j * 4 + e] = valid && d < a.D ? to_float(src[d]) * a.kf : 0.f;
+                        for (int e = 0; e < 4; ++e)
+                            if (j * 32 + l8 * 4 + e < a.D) x[e] = to_float(src[j * 32 + e]);
+                    }
                 }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) q[r][j * 4 + e] = x[e] * a.kf;
+            }
         }
         float m[R], l[R], acc[R][NJ * 4];
 #pragma unroll
@@ -86,206 +211,416 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const AttendAr
 #pragma unroll
             for (int x = 0; x < NJ * 4; ++x) acc[r][x] = 0.f;
         }
-        // what all of the unit's rows see, and what none of them does
-        const int p0 = w.s.base + a.by_group(w.r0), p1 = w.s.base + a.by_group(w.r0 + count - 1);
-        const int low0 = low_of(a, p0), low1 = low_of(a, p1);
-
-        // the rows of tile i's keys (one warp; -1: beyond what anybody sees, -2: a page that is none)
-        auto find_rows = [&](int i, long long& ko, long long& vo) {
-            ko = vo = -1;
-            if (i >= nt) return;
-            const int p = tile_at(w.u, w.i + i) * kKeys + lane;
-            if (p > p1 || !(p >= low0 || p < a.sinks)) return;
-            const int j = a.by_page(p);
-            const int page = __ldg(a.table + static_cast<long long>(w.b) * a.width + j);
-            if (page < 0 || page >= a.num_pages) { ko = -2; return; }
-            ko = page * a.ks[0] + w.h * a.ks[1] + (p - j * a.page) * a.ks[2];
-            vo = page * a.vs[0] + w.h * a.vs[1] + (p - j * a.page) * a.vs[2];
-        };
-        auto put_rows = [&](int i, long long ko, long long vo) {
-            sm.row[i & 3][0][lane] = ko;
-            sm.row[i & 3][1][lane] = vo;
-            if (ko == -2) sm.bad = 1;
-        };
-        auto fetch = [&](int i) {
-            if (i < nt) {
-                T* dst = sm.tile[i % kStages][0];
-                if (aligned) {
-                    const int vecs = a.D * static_cast<int>(sizeof(T)) / 16;
-                    for (int x = tid; x < 2 * kKeys * vecs; x += kThreads) {
-                        const int which = x / (kKeys * vecs), y = x - which * kKeys * vecs, key = y / vecs, c = y - key * vecs;
-                        const long long off = sm.row[i & 3][which][key];
-                        if (off >= 0) {
-                            const T* src = static_cast<const T*>(which ? a.v : a.k) + off + c * (16 / sizeof(T));
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst + (which * kKeys + key) * kRow + c * (16 / sizeof(T)))), "l"(src) : "memory");
-                        }
-                    }
-                } else {
-                    for (int x = tid; x < 2 * kKeys * a.D; x += kThreads) {
-                        const int which = x / (kKeys * a.D), y = x - which * kKeys * a.D, key = y / a.D, c = y - key * a.D;
-                        const long long off = sm.row[i & 3][which][key];
-                        if (off >= 0) dst[(which * kKeys + key) * kRow + c] = (static_cast<const T*>(which ? a.v : a.k) + off)[c];
-                    }
-                }
-            }
-            cp_async_commit();
-        };
-        if (warp == 0) {
-            long long ko, vo;
-            for (int i = 0; i < 3; ++i) { find_rows(i, ko, vo); put_rows(i, ko, vo); }
-        }
-        __syncthreads();
-        fetch(0);
-        fetch(1);
+#pragma unroll 1
         for (int i = 0; i < nt; ++i) {
-            fetch(i + 2);
-            long long ko = 0, vo = 0;
-            if (warp == 0) find_rows(i + 3, ko, vo);
-            cp_async_wait<2>();
-            __syncthreads();
-            const int start = tile_at(w.u, w.i + i) * kKeys;
-            const bool whole = start + kKeys - 1 <= p0 && (start >= low1 || start + kKeys <= a.sinks);
-            const T* kt = sm.tile[i % kStages][0];
-            const T* vt = sm.tile[i % kStages][1];
-            for (int key = ks * 4 + group8; key < kKeys; key += key_slices * 4) {
-                float s[R];
+            fetch(i + kDepth - 1);
+            find(i + kDepth);
+            cp_async_wait<kDepth - 1>();
+            T(*cell)[kThreads][4] = sm.ring[i % kDepth];
+            float s[R];
 #pragma unroll
-                for (int r = 0; r < R; ++r) s[r] = 0.f;
+            for (int r = 0; r < R; ++r) s[r] = 0.f;
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    float x[4];
-                    load4<T>(kt + key * kRow + j * 32 + l8 * 4, x);
+            for (int j = 0; j < NJ; ++j) {
+                float x[4];
+                widen(cell[2 * j][tid], x);
 #pragma unroll
-                    for (int r = 0; r < R; ++r)
+                for (int e = 0; e < 4; ++e)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[r] = fmaf(q[r][j * 4 + e], x[e], s[r]);
-                }
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    s[r] += __shfl_xor_sync(0xffffffffu, s[r], 4);
-                    s[r] += __shfl_xor_sync(0xffffffffu, s[r], 2);
-                    s[r] += __shfl_xor_sync(0xffffffffu, s[r], 1);
-                }
-                const int p = start + key;
-                const bool there = sm.row[i & 3][0][key] >= 0;
-                bool some[R];
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const bool see = there && (whole ? rg * R + r < count : p <= pos[r] && (p >= low[r] || p < a.sinks));
-                    some[r] = see && s[r] != -INFINITY;               // (a weight of zero takes no value, whatever that is)
-                    if (some[r] && s[r] > m[r] + 8.f) {
-                        const float f = exp2f(m[r] - s[r]);
-                        m[r] = s[r];
-                        l[r] *= f;
-#pragma unroll
-                        for (int x = 0; x < NJ * 4; ++x) acc[r][x] *= f;
-                    }
-                    s[r] = some[r] ? exp2f(s[r] - m[r]) : 0.f;
-                    l[r] += s[r];
-                }
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    float x[4];
-                    load4<T>(vt + key * kRow + j * 32 + l8 * 4, x);
-#pragma unroll
-                    for (int r = 0; r < R; ++r)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (some[r]) acc[r][j * 4 + e] = fmaf(s[r], x[e], acc[r][j * 4 + e]);
-                }
+                    for (int r = 0; r < R; ++r) s[r] = fmaf(q[r][j * 4 + e], x[e], s[r]);
             }
-            if (warp == 0) put_rows(i + 3, ko, vo);        // (tile i - 1's place: its readers are past the barrier above)
-            __syncthreads();
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1)
+#pragma unroll
+                for (int r = 0; r < R; ++r) s[r] += __shfl_xor_sync(0xffffffffu, s[r], o);
+            const int p = tile_at(w.u, w.i + i) * kFewKeys + mine;
+            bool some[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                some[r] = p <= pos[r] && (p >= low[r] || p < a.sinks) && s[r] != -INFINITY;
+                if (some[r] && s[r] > m[r] + kLag) {
+                    const float f = exp2f(m[r] - s[r]);
+                    m[r] = s[r];
+                    l[r] *= f;
+#pragma unroll
+                    for (int x = 0; x < NJ * 4; ++x) acc[r][x] *= f;
+                }
+                s[r] = some[r] ? exp2f(s[r] - m[r]) : 0.f;
+                l[r] += s[r];
+            }
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                float x[4];
+                widen(cell[2 * j + 1][tid], x);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (some[r]) acc[r][j * 4 + e] = fmaf(s[r], x[e], acc[r][j * 4 + e]);
+            }
         }
-        // lanes of one row, then warps of one row group
+        // a warp's keys, then the warps'
 #pragma unroll
         for (int r = 0; r < R; ++r) {
 #pragma unroll
             for (int o = 8; o <= 16; o <<= 1) {
                 const float om = __shfl_xor_sync(0xffffffffu, m[r], o), ol = __shfl_xor_sync(0xffffffffu, l[r], o);
-                const float M = fmaxf(m[r], om);
-                const float f = m[r] == -INFINITY ? 0.f : exp2f(m[r] - M), of = om == -INFINITY ? 0.f : exp2f(om - M);
+                const float M = fmaxf(m[r], om), f = factor_of(m[r], M), of = factor_of(om, M);
                 l[r] = l[r] * f + ol * of;
                 m[r] = M;
 #pragma unroll
-                for (int x = 0; x < NJ * 4; ++x) {
-                    const float oa = __shfl_xor_sync(0xffffffffu, acc[r][x], o);
-                    acc[r][x] = acc[r][x] * f + oa * of;
-                }
+                for (int x = 0; x < NJ * 4; ++x) acc[r][x] = acc[r][x] * f + __shfl_xor_sync(0xffffffffu, acc[r][x], o) * of;
             }
             if (group8 == 0) {
+                float* const to = sm.part[warp][r];
 #pragma unroll
                 for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sm.part[warp][r][j * 32 + l8 * 4 + e] = acc[r][j * 4 + e];
-                if (l8 == 0) { sm.part[warp][r][kRow] = m[r]; sm.part[warp][r][kRow + 1] = l[r]; }
+                    for (int e = 0; e < 4; ++e) to[j * 32 + l8 * 4 + e] = acc[r][j * 4 + e];
+                if (l8 == 0) {
+                    to[kRow] = m[r];
+                    to[kRow + 1] = l[r];
+                }
             }
         }
-        __syncthreads();
-        const bool bad = w.s.bad || sm.bad;
-        float* part = leave_unit(a, sh, w, count, sm.joint, tid);
-        for (int x = tid; x < count * a.D; x += kThreads) {
-            const int row = x / a.D, d = x - row * a.D;
-            const int g = row / R, r = row - g * R;
-            float M = -INFINITY, sl = 0.f, so = 0.f;
-            for (int s = 0; s < key_slices; ++s) M = fmaxf(M, sm.part[g + s * row_groups][r][kRow]);
-            for (int s = 0; s < key_slices; ++s) {
-                const float* p = sm.part[g + s * row_groups][r];
-                const float f = p[kRow] == -INFINITY ? 0.f : exp2f(p[kRow] - M);
-                sl += p[kRow + 1] * f;
-                so += p[d] * f;
+        bad = __syncthreads_or(bad);
+        float* const part = leave_unit(a, sh, w, v.count, sm.joint, tid);
+        static_assert(R * NJ * 8 <= kThreads, "a thread for every four elements");
+        const int at = tid / (NJ * 8), d = tid % (NJ * 8) * 4;
+        if (at < v.count && at < R && d < a.D) {
+            float M = -INFINITY, sl = 0.f, so[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < kWarps; ++s) M = fmaxf(M, sm.part[s][at][kRow]);
+#pragma unroll
+            for (int s = 0; s < kWarps; ++s) {
+                const float f = factor_of(sm.part[s][at][kRow], M);
+                sl += sm.part[s][at][kRow + 1] * f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) so[e] += sm.part[s][at][d + e] * f;
             }
-            if (bad) sl = NAN;
-            if (part) {
-                part[2 * a.rows + static_cast<size_t>(row) * a.D + d] = so;
-                if (d == 0) { part[row] = M; part[a.rows + row] = sl; }
-            } else {
-                const int at = w.r0 + row, t = a.by_group(at);
-                T* dst = static_cast<T*>(a.out) + w.b * a.os[0] + t * a.os[1] + (w.h * a.group + at - t * a.group) * a.os[2] + d;
-                *dst = from_float<T>(sl == 0.f ? 0.f : so / sl);
+            put<T>(a, w, part, at, d, M, bad ? NAN : sl, so);
+        }
+        cp_async_wait<0>();
+        __syncthreads();
+        walk_next(a, w);
+    }
+    join_units<T>(a, sm.joint, tid, kThreads);
+}
+
+// ---- more rows ---------------------------------------------------------------------------------------------------------
+
+template <int NJ>
+struct ManyShape {
+    static constexpr int kRows = 32, kKeys = NJ <= 4 ? 64 : 32, kRow = NJ * 32;
+    static constexpr int kVecs = NJ <= 2 ? 16 : NJ <= 4 ? 32 : 64;     // groups of four of a row, to a power of two
+    static constexpr int kEach = NJ <= 4 ? 1 : 2;                      // ... that a thread has of O
+    static constexpr int kLanes = kVecs / kEach;                       // threads that share a row of O: 16 or 32
+};
+template <int NJ>
+struct ManySmem {
+    using Sh = ManyShape<NJ>;
+    float k[2][Sh::kKeys][Sh::kRow + 4];
+    float v[2][Sh::kKeys][Sh::kRow];
+    float q[Sh::kRows][Sh::kRow + 4];
+    float p[Sh::kKeys][Sh::kRows + 4];
+    float m[Sh::kRows], l[Sh::kRows], factor[Sh::kRows];
+    long long row[3][2][Sh::kKeys];            // where the keys' rows lie, of tiles i .. i + 2 (negative: nowhere)
+    ShareSmem share;
+    JointSmem joint;
+};
+
+template <typename T, int NJ>
+__global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendArgs a, const int aligned, const int q_vec) {
+    extern __shared__ __align__(16) char raw[];
+    using Sh = ManyShape<NJ>;
+    ManySmem<NJ>& sm = *reinterpret_cast<ManySmem<NJ>*>(raw);
+    constexpr int KT = Sh::kKeys, kI = KT / 16, kEach = Sh::kEach;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // S: rows 2 ty, 2 ty + 1 and keys tx + 16 i;  O: rows of `rows8`, columns of `col`, every `kSplit`-th key
+    const int tx = lane & 15, ty = warp * 2 + (lane >> 4);
+    constexpr int kSplit = 2 * (32 / Sh::kLanes);
+    const int rows8 = (warp & 3) * 8, col = lane % Sh::kLanes, split = (warp >> 2) + 2 * (lane / Sh::kLanes);
+    const int quads = (a.D + 3) / 4;
+
+    if (a.D % 4 != 0)                          // (columns D to the next multiple of four stay zero)
+        for (int x = tid; x < 2 * KT * (Sh::kRow + 4); x += kThreads) (&sm.k[0][0][0])[x] = 0.f;
+    if (tid == 0) sm.joint.n = 0;
+    const Share sh = find_share(a, sm.share, kThreads);
+    Walk w = walk_begin(a, sh);
+#pragma unroll 1
+    while (w.more) {
+        const Sight v = sight_of(a, w);
+        const int nt = w.upto - w.i;
+        bool bad = w.s.bad;
+        auto find = [&](int i) {
+            if (tid < KT) {
+                long long ko = -1, vo = -1;
+                if (i < nt && !key_row(a, w, v, tile_at(w.u, w.i + i) * KT + tid, &ko, &vo, &bad)) ko = vo = -1;
+                sm.row[i % 3][0][tid] = ko;
+                sm.row[i % 3][1][tid] = vo;
+            }
+        };
+        auto fetch = [&](int i) {
+            if (i < nt) {
+#pragma unroll 2
+                for (int x = tid; x < 2 * KT * Sh::kVecs; x += kThreads) {
+                    const int c = x % Sh::kVecs, key = x / Sh::kVecs % KT, which = x / (Sh::kVecs * KT);
+                    const long long off = sm.row[i % 3][which][key];
+                    if (off < 0 || c >= quads) continue;
+                    const T* src = static_cast<const T*>(which ? a.v : a.k) + off + c * 4;
+                    float* dst = which ? &sm.v[i & 1][key][c * 4] : &sm.k[i & 1][key][c * 4];
+                    if constexpr (sizeof(T) == 4) {
+                        if (aligned) {
+                            copy4(dst, src);
+                            continue;
+                        }
+                    } else {
+                        if (aligned) {
+                            float y[4];
+                            widen(src, y);
+                            *reinterpret_cast<float4*>(dst) = make_float4(y[0], y[1], y[2], y[3]);
+                            continue;
+                        }
+                    }
+                    for (int e = 0; e < 4; ++e)
+                        if (c * 4 + e < a.D) dst[e] = to_float(src[e]);
+                }
+            }
+            cp_async_commit();
+        };
+        find(0);
+        find(1);
+#pragma unroll
+        for (int x0 = 0; x0 < Sh::kRows * Sh::kVecs; x0 += kThreads) {
+            const int row = (x0 + tid) / Sh::kVecs, c = (x0 + tid) % Sh::kVecs;
+            if (c < quads) {
+                float y[4] = {0.f, 0.f, 0.f, 0.f};
+                if (row < v.count) {
+                    const int r = w.r0 + row, t = a.by_group(r);
+                    const T* src = static_cast<const T*>(a.q) + w.b * a.qs[0] + t * a.qs[1] + (w.h * a.group + r - t * a.group) * a.qs[2] + c * 4;
+                    if (q_vec) {
+                        widen(src, y);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (c * 4 + e < a.D) y[e] = to_float(src[e]);
+                    }
+                }
+                *reinterpret_cast<float4*>(&sm.q[row][c * 4]) = make_float4(y[0] * a.kf, y[1] * a.kf, y[2] * a.kf, y[3] * a.kf);
             }
         }
+        if (tid < Sh::kRows) {
+            sm.m[tid] = -INFINITY;
+            sm.l[tid] = 0.f;
+        }
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        int pos[2], low[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const bool valid = 2 * ty + r < v.count;
+            pos[r] = valid ? w.s.base + a.by_group(w.r0 + 2 * ty + r) : -1;
+            low[r] = valid ? low_of(a, pos[r]) : 0;
+        }
+        float acc[8][4 * kEach];
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+#pragma unroll
+            for (int x = 0; x < 4 * kEach; ++x) acc[r][x] = 0.f;
         __syncthreads();
-        if (warp == 0) {
-            if (lane == 0) sm.bad = 0;
-            __syncwarp();                              // (this warp is the one that sets it)
+        fetch(0);
+#pragma unroll 1
+        for (int i = 0; i < nt; ++i) {
+            fetch(i + 1);
+            find(i + 2);
+            cp_async_wait<1>();
+            __syncthreads();
+            const int start = tile_at(w.u, w.i + i) * KT;
+            const bool whole = whole_tile(a, v, start, KT);
+            bool raised = false;
+            if (warp * 4 < v.count) {
+                float s[2][kI];
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int x = 0; x < kI; ++x) s[r][x] = 0.f;
+                const float* const kr = &sm.k[i & 1][tx][0];
+                const float* const qr = &sm.q[2 * ty][0];
+#pragma unroll 4
+                for (int d = 0; d < quads * 4; d += 4) {
+                    const float4 q0 = *reinterpret_cast<const float4*>(qr + d), q1 = *reinterpret_cast<const float4*>(qr + Sh::kRow + 4 + d);
+#pragma unroll
+                    for (int x = 0; x < kI; ++x) {
+                        const float4 k = *reinterpret_cast<const float4*>(kr + x * 16 * (Sh::kRow + 4) + d);
+                        s[0][x] = fmaf(q0.x, k.x, fmaf(q0.y, k.y, fmaf(q0.z, k.z, fmaf(q0.w, k.w, s[0][x]))));
+                        s[1][x] = fmaf(q1.x, k.x, fmaf(q1.y, k.y, fmaf(q1.z, k.z, fmaf(q1.w, k.w, s[1][x]))));
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int x = 0; x < kI; ++x) {
+                        const int p = start + tx + 16 * x;
+                        if (!whole && !(p <= pos[r] && (p >= low[r] || p < a.sinks))) s[r][x] = -INFINITY;
+                        top = fmaxf(top, s[r][x]);
+                    }
+#pragma unroll
+                    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    if (top > m[r] + kLag) {
+                        const float f = exp2f(m[r] - top);
+                        m[r] = top;
+                        l[r] *= f;
+                        if (tx == 0) sm.factor[2 * ty + r] = f;
+                        raised = true;
+                    } else if (tx == 0) {
+                        sm.factor[2 * ty + r] = 1.f;
+                    }
+#pragma unroll
+                    for (int x = 0; x < kI; ++x) {
+                        const float p = s[r][x] == -INFINITY ? 0.f : exp2f(s[r][x] - m[r]);
+                        l[r] += p;
+                        sm.p[tx + 16 * x][2 * ty + r] = p;
+                    }
+                }
+            }
+            raised = __syncthreads_or(raised);
+            if (rows8 < v.count) {
+                if (raised) {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        const float f = rows8 + r < v.count ? sm.factor[rows8 + r] : 1.f;
+#pragma unroll
+                        for (int x = 0; x < 4 * kEach; ++x) acc[r][x] *= f;
+                    }
+                }
+                auto add = [&](int key, bool guard) {
+                    const float4 pa = *reinterpret_cast<const float4*>(&sm.p[key][rows8]), pb = *reinterpret_cast<const float4*>(&sm.p[key][rows8 + 4]);
+                    const float p[8] = {pa.x, pa.y, pa.z, pa.w, pb.x, pb.y, pb.z, pb.w};
+#pragma unroll
+                    for (int c = 0; c < kEach; ++c) {
+                        const float4 val = *reinterpret_cast<const float4*>(&sm.v[i & 1][key][(col + c * Sh::kLanes) * 4 < Sh::kRow ? (col + c * Sh::kLanes) * 4 : 0]);
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) {
+                            if (guard && p[r] == 0.f) continue;
+                            acc[r][4 * c] = fmaf(p[r], val.x, acc[r][4 * c]);
+                            acc[r][4 * c + 1] = fmaf(p[r], val.y, acc[r][4 * c + 1]);
+                            acc[r][4 * c + 2] = fmaf(p[r], val.z, acc[r][4 * c + 2]);
+                            acc[r][4 * c + 3] = fmaf(p[r], val.w, acc[r][4 * c + 3]);
+                        }
+                    }
+                };
+                if (whole) {
+#pragma unroll 4
+                    for (int key = split; key < KT; key += kSplit) add(key, false);
+                } else {
+#pragma unroll 1
+                    for (int key = split; key < KT; key += kSplit) add(key, true);
+                }
+            }
+            __syncthreads();
+        }
+        // the sums of the rows, and the splits of O, which lie in the keys' place
+        cp_async_wait<0>();
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
+            if (tx == 0) {
+                sm.m[2 * ty + r] = m[r];
+                sm.l[2 * ty + r] = l[r];
+            }
+        }
+        float* const o_at = &sm.k[0][0][0];    // [kSplit][kRows][kRow]
+        static_assert(kSplit * Sh::kRows * Sh::kRow <= 2 * KT * (Sh::kRow + 4), "fits");
+        if (rows8 < v.count) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+#pragma unroll
+                for (int c = 0; c < kEach; ++c)
+                    if ((col + c * Sh::kLanes) * 4 < Sh::kRow)
+                        *reinterpret_cast<float4*>(o_at + (split * Sh::kRows + rows8 + r) * Sh::kRow + (col + c * Sh::kLanes) * 4) =
+                            make_float4(acc[r][4 * c], acc[r][4 * c + 1], acc[r][4 * c + 2], acc[r][4 * c + 3]);
+        }
+        bad = __syncthreads_or(bad);
+        float* const part = leave_unit(a, sh, w, v.count, sm.joint, tid);
+#pragma unroll 2
+        for (int x = tid; x < v.count * Sh::kVecs; x += kThreads) {
+            const int row = x / Sh::kVecs, c = x % Sh::kVecs;
+            if (c >= quads) continue;
+            float so[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < kSplit; ++s) {
+                const float4 y = *reinterpret_cast<const float4*>(o_at + (s * Sh::kRows + row) * Sh::kRow + c * 4);
+                so[0] += y.x; so[1] += y.y; so[2] += y.z; so[3] += y.w;
+            }
+            put<T>(a, w, part, row, c * 4, sm.m[row], bad ? NAN : sm.l[row], so);
+        }
+        __syncthreads();
+        if (a.D % 4 != 0) {                    // (the keys' columns beyond D are zero again)
+            for (int x = tid; x < 2 * KT * (Sh::kRow + 4); x += kThreads)
+                if (x % (Sh::kRow + 4) >= a.D) o_at[x] = 0.f;
         }
         walk_next(a, w);
     }
     join_units<T>(a, sm.joint, tid, kThreads);
 }
 
+// ---- launches ----------------------------------------------------------------------------------------------------------
+
 template <typename T, int NJ, int R>
-cudaError_t launch(const AttendArgs& a, bool aligned, int ctas, cudaStream_t stream) {
-    constexpr int bytes = static_cast<int>(sizeof(RowsSmem<T, NJ, R>));
+cudaError_t launch_few(const AttendArgs& a, bool aligned, bool q_vec, int ctas, cudaStream_t stream) {
+    constexpr int bytes = static_cast<int>(sizeof(FewSmem<T, NJ, R>));
     static_assert(bytes <= 227 * 1024, "fits an SM");
     static std::atomic<unsigned long long> asked{0};
-    const cudaError_t e = allow_shared(attend_rows_kernel<T, NJ, R>, bytes, asked);
+    const cudaError_t e = allow_shared(attend_few_kernel<T, NJ, R>, bytes, asked);
     if (e != cudaSuccess) return e;
-    return launch_together(attend_rows_kernel<T, NJ, R>, ctas, kThreads, bytes, stream, a, static_cast<int>(aligned));
+    return launch_together(attend_few_kernel<T, NJ, R>, ctas, kThreads, bytes, stream, a, static_cast<int>(aligned), static_cast<int>(q_vec));
 }
+template <typename T, int NJ>
+cudaError_t launch_many(const AttendArgs& a, bool aligned, bool q_vec, int ctas, cudaStream_t stream) {
+    constexpr int bytes = static_cast<int>(sizeof(ManySmem<NJ>));
+    static_assert(bytes <= 227 * 1024, "fits an SM");
+    static std::atomic<unsigned long long> asked{0};
+    const cudaError_t e = allow_shared(attend_many_kernel<T, NJ>, bytes, asked);
+    if (e != cudaSuccess) return e;
+    return launch_together(attend_many_kernel<T, NJ>, ctas, kThreads, bytes, stream, a, static_cast<int>(aligned), static_cast<int>(q_vec));
+}
+// Up to 8 rows (4 where D is beyond 128) are taken 4 (2) at a time by the kernel that reads; the others by the one that multiplies.
+constexpr int few_each(int D) { return D <= 128 ? 4 : 2; }
+bool few(int D, int rows) { return rows <= 2 * few_each(D); }
 template <typename T>
-cudaError_t pick(const AttendArgs& a, bool aligned, int ctas, cudaStream_t stream) {
+cudaError_t pick(const AttendArgs& a, bool aligned, bool q_vec, int ctas, cudaStream_t stream) {
     const int nj = (a.D + 31) / 32;
-    if (nj <= 2) return launch<T, 2, 4>(a, aligned, ctas, stream);
-    if (nj <= 3) return launch<T, 3, 4>(a, aligned, ctas, stream);
-    if (nj <= 4) return launch<T, 4, 4>(a, aligned, ctas, stream);
-    return launch<T, 8, 2>(a, aligned, ctas, stream);
+    if (a.rows <= 4) {
+        if (nj <= 2) return launch_few<T, 2, 4>(a, aligned, q_vec, ctas, stream);
+        if (nj <= 3) return launch_few<T, 3, 4>(a, aligned, q_vec, ctas, stream);
+        if (nj <= 4) return launch_few<T, 4, 4>(a, aligned, q_vec, ctas, stream);
+        return launch_few<T, 8, 2>(a, aligned, q_vec, ctas, stream);
+    }
+    if (nj <= 2) return launch_many<T, 2>(a, aligned, q_vec, ctas, stream);
+    if (nj <= 3) return launch_many<T, 3>(a, aligned, q_vec, ctas, stream);
+    if (nj <= 4) return launch_many<T, 4>(a, aligned, q_vec, ctas, stream);
+    return launch_many<T, 8>(a, aligned, q_vec, ctas, stream);
 }
 
 }  // namespace
 
-// Query rows of a unit: R a warp, times as many groups of warps as the call's rows fill.
-int attend_rows_tile(int D, int rows) {
-    const int R = D <= 128 ? 4 : 2;
-    int groups = 1;
-    while (groups < kWarps && groups * R < rows) groups *= 2;
-    return groups * R;
+void attend_rows_plan(AttendArgs* a) {
+    const int rows = a->n * a->group;
+    if (few(a->D, rows)) {
+        a->rows = few_each(a->D);
+        a->span = kFewKeys;
+    } else {
+        const int tiles = (rows + 31) / 32;
+        a->rows = ((rows + tiles - 1) / tiles + 7) / 8 * 8;
+        a->span = a->D <= 128 ? 64 : 32;
+    }
+    a->per_page = 1;
 }
-int attend_rows_keys() { return kKeys; }
+int attend_rows_most() { return 32; }
 
-cudaError_t launch_attend_rows(const AttendArgs& a, int dtype, bool aligned, int ctas, cudaStream_t stream) {
-    return dtype == BV_DTYPE_F32 ? pick<float>(a, aligned, ctas, stream) : pick<__nv_bfloat16>(a, aligned, ctas, stream);
+cudaError_t launch_attend_rows(const AttendArgs& a, int dtype, bool aligned, bool q_vec, int ctas, cudaStream_t stream) {
+    return dtype == BV_DTYPE_F32 ? pick<float>(a, aligned, q_vec, ctas, stream) : pick<__nv_bfloat16>(a, aligned, q_vec, ctas, stream);
 }
 
 }  // namespace bv

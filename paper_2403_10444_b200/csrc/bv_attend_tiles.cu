@@ -733,12 +733,10 @@ cudaError_t pick(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v
 }  // namespace
 
 bool attend_tiles_takes(const AttendArgs& a) { return a.D >= 16 && a.D <= 128 && a.D % 8 == 0 && a.page % 8 == 0 && a.page <= (1 << 20); }
-// The fewest tiles of rows, of sizes as even as multiples of 16 are.
-int attend_tiles_rows(int rows) {
-    const int tiles = (rows + 79) / 80;
-    return ((rows + tiles - 1) / tiles + 15) / 16 * 16;
-}
 void attend_tiles_plan(AttendArgs* a) {
+    // the fewest tiles of rows, of sizes as even as multiples of 16 are
+    const int rows = a->n * a->group, tiles = (rows + 79) / 80;
+    a->rows = ((rows + tiles - 1) / tiles + 15) / 16 * 16;
     a->span = a->page <= kTile ? kTile / a->page * a->page : kTile;
     a->per_page = a->page <= kTile ? 1 : (a->page + kTile - 1) / kTile;
 }

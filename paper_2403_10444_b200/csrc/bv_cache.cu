@@ -155,19 +155,12 @@ struct AttendCall {
     bool aligned, q_vec, tiles;
     cudaStream_t stream;
 };
-// The kernel for every shape, or the one on the tensor cores.
+// The kernels for every shape, or the one on the tensor cores.
 void plan(AttendCall* c, bool tiles) {
     AttendArgs& a = c->a;
     c->tiles = tiles;
-    const int rows = a.n * a.group;
-    if (tiles) {
-        a.rows = attend_tiles_rows(rows);
-        attend_tiles_plan(&a);
-    } else {
-        a.rows = attend_rows_tile(a.D, rows);
-        a.span = attend_rows_keys();
-        a.per_page = 1;
-    }
+    if (tiles) attend_tiles_plan(&a);
+    else attend_rows_plan(&a);
     a.by_group = divider(a.group);
     a.by_page = divider(a.page);
     a.by_span = divider(a.span);
@@ -175,7 +168,7 @@ void plan(AttendCall* c, bool tiles) {
 int attend_ctas(int sm_count) { return sm_count < kCacheCounters ? sm_count : kCacheCounters; }
 size_t attend_scratch(int sm_count, const void* ctx) {
     const AttendCall& c = *static_cast<const AttendCall*>(ctx);
-    const int other = attend_rows_tile(c.a.D, c.a.n * c.a.group);         // (should the first kernel not take the call)
+    const int other = attend_rows_most();                                 // (should the first kernel not take the call)
     return attend_ctas(sm_count) * 2 * part_floats(c.a.rows > other ? c.a.rows : other, c.a.D) * sizeof(float);
 }
 int enqueue_attend(const StreamWork& work, void* ctx) {
@@ -192,7 +185,7 @@ int enqueue_attend(const StreamWork& work, void* ctx) {
         if (e != cudaSuccess || taken) return done(e, 1);
         plan(&c, false);
     }
-    return done(launch_attend_rows(c.a, c.dtype, c.aligned, ctas, c.stream), 1);
+    return done(launch_attend_rows(c.a, c.dtype, c.aligned, c.q_vec, ctas, c.stream), 1);
 }
 
 }  // namespace

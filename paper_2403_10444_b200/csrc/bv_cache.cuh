@@ -408,14 +408,13 @@ cudaError_t launch_together(void (*kernel)(P...), int ctas, int threads, size_t 
     }
 }
 
-// The kernel for every shape (bv_attend_rows.cu): query rows of a unit, keys of a tile.
-int attend_rows_tile(int D, int rows);
-int attend_rows_keys();
+// The kernels for every shape (bv_attend_rows.cu): rows of a unit, keys of a tile; the most rows of a unit.
+void attend_rows_plan(AttendArgs* a);
+int attend_rows_most();
 // The kernel on the tensor cores (bv_attend_tiles.cu), for calls that attend_tiles_takes; `taken` is false if no map of the pools could be had.
 bool attend_tiles_takes(const AttendArgs& a);
-int attend_tiles_rows(int rows);
 void attend_tiles_plan(AttendArgs* a);
 cudaError_t launch_attend_tiles(const AttendArgs& a, bool q_vec, int ctas, cudaStream_t stream, bool* taken);
-cudaError_t launch_attend_rows(const AttendArgs& a, int dtype, bool aligned, int ctas, cudaStream_t stream);
+cudaError_t launch_attend_rows(const AttendArgs& a, int dtype, bool aligned, bool q_vec, int ctas, cudaStream_t stream);
 
 }  // namespace bv
