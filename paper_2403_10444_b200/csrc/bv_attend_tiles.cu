@@ -6,13 +6,14 @@
 //   S^T [128 keys, N] = K Q^T            K as it lies in its pages, K-major
 //   O^T [D, N]       += V^T P            V as it lies in its pages, M-major; P [128 keys, N] from shared memory
 // Two warps load (TMA, a box per page and 64 columns, 128-byte swizzle, a ring of slots that hold a tile's keys or its values), one
-// thread issues the matrix instructions, four warps (for 48 rows and more eight, each four half of the rows) turn S into P: a thread has
-// one key and goes over the rows, so the mask, the exponential and the rounding need no other lane.  What softmax usually needs across lanes is avoided: each row has an
+// thread issues the matrix instructions, eight warps turn S into P, four of them a tile's 128 keys: a thread has one key and goes over
+// the rows, so the mask, the exponential and the rounding need no other lane.  Up to 32 rows the two fours are two teams that take
+// units in turn, so that one unit's end and the next one's beginning overlap; from 48 rows on, where the exponentials bound (80 x 128 of
+// them are 640 clocks of an SM), each four has half of the rows.  What softmax usually needs across lanes is avoided: each row has an
 // integer reference m in shared memory, weights are 2^{k s - m}, and only where some score exceeds its reference by more than 8
 // (a vote per tile) the new maxima are formed, and O and the sums scaled by the power of two between the old and the new
 // reference.  Sums stay per thread until a unit ends.  Weights are rounded to 16 bits for the second product, and the sums are taken of the rounded weights: a row of one
 // key is that key's value exactly, and the error of a row, 2^-9 of its terms at most, is that of an output rounded once more.
-// The next unit's query rows come in, and its first scores are formed, while a unit is brought to its end.
 //
 // What a row may not see is taken out twice: its weight is 0 whatever the score is, and rows of V that no row of the unit sees (or that were never
 // loaded) are set to 0 in shared memory, since 0 times an infinity is not 0.  Rows of V that some see and others do not keep their finite
@@ -86,11 +87,11 @@ template <int C> __device__ __forceinline__ void load_columns(uint32_t addr, flo
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // (a warp's lanes come together before what all of them have to execute at once)
-template <int T> __device__ __forceinline__ void soft_sync() { __syncwarp(); asm volatile("bar.sync 1, %0;" ::"n"(T) : "memory"); }
-template <int T> __device__ __forceinline__ bool soft_any(bool x) {
+template <int T> __device__ __forceinline__ void team_sync(int bar) { __syncwarp(); asm volatile("bar.sync %0, %1;" ::"r"(bar), "n"(T) : "memory"); }
+template <int T> __device__ __forceinline__ bool team_any(int bar, bool x) {
     uint32_t r;
     __syncwarp();
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(static_cast<uint32_t>(x)), "n"(T) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(static_cast<uint32_t>(x)), "r"(bar), "n"(T) : "memory");
     return r != 0;
 }
 __device__ __forceinline__ float ex2(float x) {
@@ -118,19 +119,20 @@ __host__ __device__ constexpr uint32_t instruction(int M, int N, bool a_m, bool 
 
 template <int NP, int N>
 struct Shape {
-    static constexpr int kHalves = N >= 48 ? 2 : 1, kColumnsEach = N / kHalves;      // the softmax's warps, four a half; rows of a half
-    static constexpr int kSoft = 128 * kHalves, kThreads = kSoft + 96;
-    static constexpr int kKeys = 4 * kHalves, kValues = kKeys + 1, kIssuer = kKeys + 2;      // warps: loads of keys, of values, products
+    // the softmax's eight warps: teams that take units in turn, of halves that share a unit's rows
+    static constexpr int kHalves = N >= 48 ? 2 : 1, kTeams = 2 / kHalves, kColumnsEach = N / kHalves;
+    static constexpr int kTeam = 128 * kHalves, kSoft = kTeam * kTeams, kThreads = kSoft + 96;
+    static constexpr int kKeys = 8, kValues = 9, kIssuer = 10;           // warps: loads of keys, of values, products
     static constexpr int kPanel = kTile * 128, kSlot = NP * kPanel;      // a slot: NP panels of 128 rows of 64 columns
     static constexpr int kQ = NP * N * 128, kP = N * kTile * 2;
     static constexpr int kRest = 3072;
     // two buffers for the weights (the next tile's are formed while the last one's are multiplied) where that leaves five slots
-    static constexpr int kTwo = (227 * 1024 - kRest - kQ - 2 * kP) / kSlot;
+    static constexpr int kTwo = (227 * 1024 - kRest - kTeams * kQ - 2 * kP) / kSlot;
     static constexpr int kBuffers = kTwo >= 5 ? 2 : 1;
-    static constexpr int kFit = (227 * 1024 - kRest - kQ - kBuffers * kP) / kSlot;
+    static constexpr int kFit = (227 * 1024 - kRest - kTeams * kQ - kBuffers * kP) / kSlot;
     static constexpr int kSlots = kFit < 8 ? kFit : 8;
-    static constexpr int kColumns = 3 * N <= 64 ? 64 : 3 * N <= 128 ? 128 : 256;      // of tensor memory: S twice, O
-    static constexpr int kBytes = kSlots * kSlot + kQ + kBuffers * kP + kRest;
+    static constexpr int kUsed = (2 + kTeams) * N, kColumns = kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : 256;      // of tensor memory: S twice, O for each team
+    static constexpr int kBytes = kSlots * kSlot + kTeams * kQ + kBuffers * kP + kRest;
     static_assert(kSlots >= 4, "two tiles in flight");
 };
 constexpr int kUnits = 8;                      // units that may be in flight: no more than slots
@@ -138,16 +140,18 @@ template <int NP, int N>
 struct __align__(1024) Smem {
     using Sh = Shape<NP, N>;
     char ring[Sh::kSlots][Sh::kSlot];
-    char q[Sh::kQ];
+    char q[Sh::kTeams][Sh::kQ];
     char p[Sh::kBuffers][Sh::kP];
-    float nref[N];                             // minus the references
-    float part[4][N];                          // maxima by warp; then in part[0] what the move of the references scales by
-    long long off[N];                          // where the rows' results go
-    unsigned long long full[8], empty[8], s_full[2], p_full[2], p_done[2], q_full, drain;
+    struct __align__(16) {
+        float nref[N];                         // minus the references (read four at a time)
+        float part[4][N];                      // maxima by warp; then in part[0] what the move of the references scales by
+        long long off[N];                      // where the rows' results go
+        int abort, fix;
+    } team[Sh::kTeams];
+    unsigned long long full[8], empty[8], s_full[2], p_full[2], p_done[2], q_full[2], u_start[2], u_done[2], drain;
     ShareSmem share;
     JointSmem joint;
     uint32_t tmem;
-    int abort, fix;
     int bad[kUnits];                           // units that name a page that is none
 };
 
@@ -258,7 +262,7 @@ __device__ __forceinline__ void load_tiles(const AttendArgs& a, Smem<NP, N>& sm,
             if ((y & 1) == which) mbar_wait_now(smem_u32(&sm.full[y % Sh::kSlots]), y / Sh::kSlots & 1, a.status, limit);
 }
 
-// The products, by one thread: S of a tile before O of the one before it, but at a unit's end.
+// The products, by one thread: S of a tile before O of the one before it.
 template <int NP, int N>
 __device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>& sm, Walk w, int total, uint32_t tmem, uint32_t limit) {
     using Sh = Shape<NP, N>;
@@ -267,50 +271,57 @@ __device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>&
     bool ok = true;
     auto wait = [&](unsigned long long& bar, int phase) { ok = ok && mbar_wait_now(smem_u32(&bar), phase & 1, a.status, limit); };
     int unit = 0, left = w.upto - w.i;         // of the tile whose scores come next
-    unsigned starts = 0;                       // bit t & 1: tile t is its unit's first
-    const uint32_t q_low = desc_low(smem_u32(sm.q), 16);
+    unsigned starts = 0, ends = 0, teams = 0;  // bit t & 1: tile t is its unit's first, its last, its unit's team
     auto scores = [&](int t) {
-        bool first = t == 0;
+        const bool first = t == 0 || left == 0;
         if (left == 0) {
             walk_next(a, w);
             left = w.upto - w.i;
             ++unit;
-            first = true;
         }
         --left;
-        if (first) wait(sm.q_full, unit);
-        starts = (starts & ~(1u << (t & 1))) | static_cast<unsigned>(first) << (t & 1);
+        const int team = unit % Sh::kTeams, bit = t & 1;
+        if (first) wait(sm.q_full[team], unit / Sh::kTeams);
+        auto note = [&](unsigned& bits, bool x) { bits = (bits & ~(1u << bit)) | static_cast<unsigned>(x) << bit; };
+        note(starts, first);
+        note(ends, left == 0);
+        note(teams, team != 0);
         const int slot = 2 * t % Sh::kSlots;
         wait(sm.full[slot], 2 * t / Sh::kSlots);
         if (!ok) return;
         fence_after();
-        const uint32_t k_low = desc_low(ring + slot * Sh::kSlot, 16), s_at = tmem + (t & 1) * N;
+        const uint32_t k_low = desc_low(ring + slot * Sh::kSlot, 16), q_low = desc_low(smem_u32(sm.q[team]), 16), s_at = tmem + bit * N;
 #pragma unroll
         for (int i = 0; i < 4 * NP; ++i)
             mma(s_at, desc(k_low + (i / 4 * Sh::kPanel + i % 4 * 32) / 16, desc_high(1024, 2)), desc(q_low + (i / 4 * N * 128 + i % 4 * 32) / 16, desc_high(1024, 2)), qk, i > 0);
         commit(smem_u32(&sm.empty[slot]));
-        if (a.never_signal != 1) commit(smem_u32(&sm.s_full[t & 1]));
+        if (a.never_signal != 1) {
+            // (a team that waits for its turn may be many tiles early, too early to tell by a phase's parity: a unit's first scores are
+            // announced by a barrier of the team's own)
+            if (first) commit(smem_u32(&sm.u_start[team]));
+            commit(smem_u32(&sm.s_full[bit]));
+        }
     };
     if (total > 0) scores(0);
 #pragma unroll 1
     for (int g = 0; g < total && ok; ++g) {
-        // (the next unit's rows take the place of this one's when its last scores are there: its end does not wait for them)
-        const bool last = left == 0;
-        if (g + 1 < total && !last) scores(g + 1);
-        const int x = 2 * g + 1, slot = x % Sh::kSlots;
+        // (with one team the next unit's rows take the place of this one's when its last scores are there: its end does not wait for them)
+        const bool later = Sh::kTeams == 1 && left == 0;
+        if (g + 1 < total && !later) scores(g + 1);
+        const int x = 2 * g + 1, slot = x % Sh::kSlots, buffer = g % Sh::kBuffers, bit = g & 1, team = teams >> bit & 1;
         wait(sm.full[slot], x / Sh::kSlots);
-        const int buffer = g % Sh::kBuffers;
         wait(sm.p_full[buffer], g / Sh::kBuffers);
         if (!ok) break;
         fence_after();
         const uint32_t p_low = desc_low(smem_u32(sm.p[buffer]), 128);
         const uint32_t v_low = desc_low(ring + slot * Sh::kSlot, Sh::kPanel);
-        const uint32_t add = !(starts >> (g & 1) & 1);
+        const uint32_t add = !(starts >> bit & 1);
 #pragma unroll
-        for (int j = 0; j < kTile / 16; ++j) mma(o_at, desc(v_low + j * 128, desc_high(1024, 2)), desc(p_low + j * 16, desc_high(2048, 0)), pv, add || j > 0);
+        for (int j = 0; j < kTile / 16; ++j) mma(o_at + team * N, desc(v_low + j * 128, desc_high(1024, 2)), desc(p_low + j * 16, desc_high(2048, 0)), pv, add || j > 0);
         commit(smem_u32(&sm.empty[slot]));
         commit(smem_u32(&sm.p_done[buffer]));
-        if (g + 1 < total && last) scores(g + 1);
+        if (ends >> bit & 1) commit(smem_u32(&sm.u_done[team]));
+        if (g + 1 < total && later) scores(g + 1);
     }
     if (!ok) {
         commit(smem_u32(&sm.drain));
@@ -386,14 +397,17 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sm.s_full[i]), 1);
-            mbar_init(smem_u32(&sm.p_full[i]), kSoft);
+            mbar_init(smem_u32(&sm.p_full[i]), Sh::kTeam);
             mbar_init(smem_u32(&sm.p_done[i]), 1);
+            mbar_init(smem_u32(&sm.q_full[i]), Sh::kTeam);
+            mbar_init(smem_u32(&sm.u_start[i]), 1);
+            mbar_init(smem_u32(&sm.u_done[i]), 1);
         }
-        mbar_init(smem_u32(&sm.q_full), kSoft);
         mbar_init(smem_u32(&sm.drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         for (int i = 0; i < kUnits; ++i) sm.bad[i] = 0;
-        sm.abort = sm.fix = sm.joint.n = 0;
+        for (int i = 0; i < Sh::kTeams; ++i) sm.team[i].abort = sm.team[i].fix = 0;
+        sm.joint.n = 0;
     } else if (warp < Sh::kKeys) {
         // (rows of a slot that no page reaches are never written: they stay zero)
         if (a.span < kTile) {
@@ -421,20 +435,23 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
     } else {
         // ---- weights
         // the thread's key, its four warps' rows c0 .. c0 + C - 1
-        const int key = tid & (kTile - 1), quarter = warp & 3, half = warp >> 2, c0 = half * C;
-        const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16, o_at = tmem + lanes + 2 * N + c0;
+        constexpr int kTeam = Sh::kTeam;
+        const int key = tid & (kTile - 1), quarter = warp & 3, team = tid / kTeam, member = tid % kTeam, half = member >> 7, c0 = half * C;
+        auto& ts = sm.team[team];
+        const int bar = 1 + team;
+        const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16, o_at = tmem + lanes + (2 + team) * N + c0;
         // the element of O that this thread has: with 64 of them a warp has 16, in its lower lanes
         const int dim = NP == 2 ? key : quarter * 16 + lane;
         const bool has_dim = dim < a.D && (NP == 2 || lane < 16);
         char* const p_row = sm.p[0] + c0 / 8 * (kTile * 16) + key / 8 * 128 + key % 8 * 16;
         int g = 0, unit = 0;
-        // A wait that gives up: this thread asks for a vote from then on, and behind the vote all of them leave together (sm.abort is
+        // A wait that gives up: this thread asks for a vote from then on, and behind the vote all of them leave together (ts.abort is
         // set before a vote or after the barrier that follows the look at it, never between).
         bool failed = false, gone = false;
         auto lane_wait = [&](unsigned long long& bar, int phase) {       // (for some lanes of a warp: no coming together in here)
             if (!mbar_wait_now(smem_u32(&bar), phase & 1, a.status, limit)) {
                 failed = true;
-                atomicExch(&sm.abort, 1);
+                atomicExch(&ts.abort, 1);
             }
         };
         auto wait = [&](unsigned long long& bar, int phase) {            // by whole warps
@@ -442,31 +459,41 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
             __syncwarp();
         };
         auto products = [&](int t) { wait(sm.p_done[t % Sh::kBuffers], t / Sh::kBuffers); };      // until tile t's are done
+        // the team's first unit
         View v{};
+        for (; unit < team && w.more; ++unit) {
+            g += w.upto - w.i;
+            walk_next(a, w);
+        }
         if (w.more) {
             v = view_of(a, w);
-            fetch_queries<NP, N, kSoft>(a, sm.q, w, v.count, q_vec, tid);
-            fetched_queries(sm.q_full);
+            fetch_queries<NP, N, kTeam>(a, sm.q[team], w, v.count, q_vec, member);
+            fetched_queries(sm.q_full[team]);
         }
 #pragma unroll 1
         while (w.more) {
             Walk next = w;
             View nv{};
+            int skipped = 0;                   // tiles of the other team's unit
             bool ahead = false;
             auto look_ahead = [&] {
                 ahead = true;
                 walk_next(a, next);
+                if (Sh::kTeams > 1 && next.more) {
+                    skipped = next.upto - next.i;
+                    walk_next(a, next);
+                }
                 if (next.more) nv = view_of(a, next);
             };
             float l[C];
 #pragma unroll
             for (int c = 0; c < C; ++c) l[c] = 0.f;
-            if (tid < N) {
-                const int r = w.r0 + tid, t = a.by_group(r);
-                sm.nref[tid] = -kNone;
-                sm.off[tid] = t * a.os[1] + (r - t * a.group) * a.os[2];
+            if (member < N) {
+                const int r = w.r0 + member, t = a.by_group(r);
+                ts.nref[member] = -kNone;
+                ts.off[member] = t * a.os[1] + (r - t * a.group) * a.os[2];
             }
-            soft_sync<kSoft>();
+            team_sync<kTeam>(bar);
             const int nt = w.upto - w.i;
 #pragma unroll 1
             for (int i = 0; i < nt && !gone; ++i, ++g) {
@@ -474,7 +501,8 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                 const int keys = tile_keys(a, tile_at(w.u, w.i + i), &start);
                 const bool masked = keys < kTile || !whole_tile(a, v, start, keys);
                 int lo = 0, hi = N;            // the rows that see this thread's key, from the first of its four warps on
-                wait(sm.s_full[g & 1], g >> 1);
+                if (i == 0) wait(sm.u_start[team], unit / Sh::kTeams);
+                else wait(sm.s_full[g & 1], g >> 1);
                 fence_after();
                 const uint32_t s_at = tmem + lanes + (g & 1) * N + c0;
                 float s[C];
@@ -514,7 +542,7 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                                 };
                                 finite(val.x); finite(val.y); finite(val.z); finite(val.w);
                                 if (!odd) continue;
-                                sm.fix = 1;
+                                ts.fix = 1;
                                 *at = val;
                             }
                         }
@@ -526,10 +554,10 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                 load_columns<C>(s_at, s);
 #pragma unroll
                 for (int c = 0; c < C; c += 8) wait_ld8(s + c);
-                weigh<C>(s, sm.nref + c0, a.kf, masked, lo, hi);
+                weigh<C>(s, ts.nref + c0, a.kf, masked, lo, hi);
 #pragma unroll
                 for (int c = 0; c < C; ++c) most = fmaxf(most, s[c]);
-                if (soft_any<kSoft>(most > kLag || failed)) {
+                if (team_any<kTeam>(bar, most > kLag || failed)) {
 #pragma unroll 1
                     for (int c = 0; c < C; c += 8) {
                         float y[8];
@@ -541,18 +569,18 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                             const float x = warp_max(c + e >= lo && c + e < hi ? y[e] * a.kf : -INFINITY);
                             if (lane == e) mine = x;
                         }
-                        if (lane < 8) sm.part[quarter][c0 + c + lane] = mine;
+                        if (lane < 8) ts.part[quarter][c0 + c + lane] = mine;
                     }
-                    soft_sync<kSoft>();
-                    if (tid < N) {
-                        const float top = fmaxf(fmaxf(sm.part[0][tid], sm.part[1][tid]), fmaxf(sm.part[2][tid], sm.part[3][tid]));
-                        const float old = -sm.nref[tid];
+                    team_sync<kTeam>(bar);
+                    if (member < N) {
+                        const float top = fmaxf(fmaxf(ts.part[0][member], ts.part[1][member]), fmaxf(ts.part[2][member], ts.part[3][member]));
+                        const float old = -ts.nref[member];
                         const float now = top - old > kLag ? rintf(top) : old;
-                        sm.part[0][tid] = now == old ? 1.f : exp2f(old - now);
-                        sm.nref[tid] = -now;
+                        ts.part[0][member] = now == old ? 1.f : exp2f(old - now);
+                        ts.nref[member] = -now;
                     }
-                    gone = *static_cast<volatile int*>(&sm.abort) != 0;
-                    soft_sync<kSoft>();
+                    gone = *static_cast<volatile int*>(&ts.abort) != 0;
+                    team_sync<kTeam>(bar);
                     if (gone) break;
                     if (i > 0) {
                         products(g - 1);
@@ -563,19 +591,19 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                             ld8(o_at + c, o);
                             wait_ld8(o);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) o[e] *= sm.part[0][c0 + c + e];
+                            for (int e = 0; e < 8; ++e) o[e] *= ts.part[0][c0 + c + e];
                             st8(o_at + c, o);
                         }
                         wait_st();
 #pragma unroll
-                        for (int c = 0; c < C; ++c) l[c] *= sm.part[0][c0 + c];
+                        for (int c = 0; c < C; ++c) l[c] *= ts.part[0][c0 + c];
                     }
                     load_columns<C>(s_at, s);
 #pragma unroll
                     for (int c = 0; c < C; c += 8) wait_ld8(s + c);
-                    weigh<C>(s, sm.nref + c0, a.kf, masked, lo, hi);
+                    weigh<C>(s, ts.nref + c0, a.kf, masked, lo, hi);
                 }
-                if (i >= Sh::kBuffers) products(g - Sh::kBuffers);       // (the weights that lie there have been multiplied)
+                if (g >= Sh::kBuffers) products(g - Sh::kBuffers);       // (the weights that lie there have been multiplied)
                 char* const to = p_row + g % Sh::kBuffers * Sh::kP;
 #pragma unroll
                 for (int c = 0; c < C; c += 8) {
@@ -596,14 +624,14 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
             // the next unit's rows, now that this one's have their scores
             if (!gone) {
                 look_ahead();
-                if (next.more) fetch_queries<NP, N, kSoft>(a, sm.q, next, nv.count, q_vec, tid);
-                products(g - 1);
-                if (next.more) fetched_queries(sm.q_full);
+                if (next.more) fetch_queries<NP, N, kTeam>(a, sm.q[team], next, nv.count, q_vec, member);
+                wait(sm.u_done[team], unit / Sh::kTeams);
+                if (next.more) fetched_queries(sm.q_full[team]);
             }
             fence_after();
             // the sums: over the lanes, then (in what follows) over the warps
             constexpr int c32 = C / 32 * 32, c16 = (C - c32) / 16 * 16, c8 = C - c32 - c16;
-            float* const sums = sm.part[quarter] + c0;
+            float* const sums = ts.part[quarter] + c0;
 #pragma unroll
             for (int c = 0; c < c32; c += 32) sums[c + lane] = across<32>(l + c, lane);
             if constexpr (c16 > 0) {
@@ -614,18 +642,18 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                 const float x = across<8>(l + c32 + c16, lane);
                 if (lane < 8) sums[c32 + c16 + lane] = x;
             }
-            const bool bad = soft_any<kSoft>(w.s.bad || failed || gone) || *static_cast<volatile int*>(&sm.bad[unit % kUnits]) != 0;
-            const bool fix = *static_cast<volatile int*>(&sm.fix) != 0;
-            float* part = leave_unit(a, sh, w, v.count, sm.joint, tid);
-            if (tid < N) {
-                const float sum = bad ? NAN : sm.part[0][tid] + sm.part[1][tid] + sm.part[2][tid] + sm.part[3][tid];
-                if (part && tid < v.count) {
-                    part[tid] = -sm.nref[tid];
-                    part[a.rows + tid] = sum;
+            const bool bad = team_any<kTeam>(bar, w.s.bad || failed || gone) || *static_cast<volatile int*>(&sm.bad[unit % kUnits]) != 0;
+            const bool fix = *static_cast<volatile int*>(&ts.fix) != 0;
+            float* part = leave_unit(a, sh, w, v.count, sm.joint, member);
+            if (member < N) {
+                const float sum = bad ? NAN : ts.part[0][member] + ts.part[1][member] + ts.part[2][member] + ts.part[3][member];
+                if (part && member < v.count) {
+                    part[member] = -ts.nref[member];
+                    part[a.rows + member] = sum;
                 }
-                sm.part[0][tid] = sum == 0.f ? 0.f : 1.f / sum;
+                ts.part[0][member] = sum == 0.f ? 0.f : 1.f / sum;
             }
-            soft_sync<kSoft>();
+            team_sync<kTeam>(bar);
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + w.b * a.os[0] + w.h * a.group * a.os[2] + dim;
 #pragma unroll 1
             for (int c = 0; c < C && c0 + c < v.count; c += 8) {
@@ -665,16 +693,17 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (e < left) out[sm.off[c0 + c + e]] = __float2bfloat16_rn(o[e] * sm.part[0][c0 + c + e]);
+                        if (e < left) out[ts.off[c0 + c + e]] = __float2bfloat16_rn(o[e] * ts.part[0][c0 + c + e]);
                 }
             }
             if (!ahead) look_ahead();          // (a launch that gives up)
             fence_before();
-            soft_sync<kSoft>();
-            if (tid == 0) sm.fix = sm.bad[unit % kUnits] = 0;
+            team_sync<kTeam>(bar);
+            if (member == 0) ts.fix = sm.bad[unit % kUnits] = 0;
             w = next;
             v = nv;
-            ++unit;
+            g += skipped;
+            unit += Sh::kTeams;
         }
     }
     fence_before();

@@ -278,12 +278,12 @@ struct JointSmem {
     int n;                    // units left so far; zero at the start
     int ok[2];
 };
-// Is the unit one of several CTAs?  Then where this one's part goes, and a note of it (by thread `tid` 0; visible to the CTA behind its next barrier).
+// Is the unit one of several CTAs?  Then where this one's part goes, and a note of it (by one thread, whose `tid` is 0; visible to the CTA behind its next barrier).
 __device__ __forceinline__ float* leave_unit(const AttendArgs& a, const Share& sh, const Walk& w, int count, JointSmem& js, int tid) {
     if (w.i == 0 && w.upto == w.u.tiles) return nullptr;
     const int c = blockIdx.x;
     const int first = w.i == 0 ? c : holder_of(sh, w.unit_at), last = w.upto == w.u.tiles ? c : holder_of(sh, w.unit_at + w.u.tiles - 1);
-    if (tid == 0) js.unit[js.n++] = Joint{w.b, w.h, w.r0, count, first, last};
+    if (tid == 0) js.unit[atomicAdd(&js.n, 1)] = Joint{w.b, w.h, w.r0, count, first, last};
     return a.part + (2 * static_cast<size_t>(c) + (c == first)) * part_floats(a.rows, a.D);
 }
 
