@@ -451,6 +451,17 @@ _I32 = torch.int32
 _CODES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
 
 
+def _enqueue(fn, dev: int, stream, *args) -> None:
+    """Calls an entry point with device ``dev`` current (it nearly always is) and the stream as its last argument."""
+    if torch._C._cuda_getDevice() == dev:
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+    if status:
+        _check(status)
+
+
 def _pools(k, v):
     """(shape, strides of k, strides of v, dtype code, dtype, device) of two pools of pages [num_pages, heads, page_size, D]."""
     shape, ks, vs, dtype, dev = k.shape, k.stride(), v.stride(), k.dtype, k.get_device()
@@ -529,12 +540,7 @@ def bv_cache_attend(q, k, v, table, lens, n_new=None, scale: Optional[float] = N
     if n_out != n:
         raise ValueError("out must have the shape of q")
     new = None if n_new is None else _counted(n_new, B, dev, "n_new")
-    lib = _lib or load_library()
-    with _on(q.device):
-        status = lib.bv_cache_attend(blob, q.data_ptr(), qs, new, n, heads, D ** -0.5 if scale is None else scale, window, sinks,
-                                     out.data_ptr(), os_, _raw_stream(q.device, stream))
-    if status:
-        _check(status)
+    _enqueue((_lib or load_library()).bv_cache_attend, dev, stream, blob, q.data_ptr(), qs, new, n, heads, D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), os_)
     return out
 
 
@@ -548,11 +554,7 @@ def bv_cache_append(k_new, v_new, k, v, table, lens, n_new=None, stream=None) ->
     _written(k, "k")
     _written(v, "v")
     new = None if n_new is None else _counted(n_new, B, dev, "n_new")
-    lib = _lib or load_library()
-    with _on(k.device):
-        status = lib.bv_cache_append(blob, k_new.data_ptr(), ks, v_new.data_ptr(), vs, new, n, _raw_stream(k.device, stream))
-    if status:
-        _check(status)
+    _enqueue((_lib or load_library()).bv_cache_append, dev, stream, blob, k_new.data_ptr(), ks, v_new.data_ptr(), vs, new, n)
 
 
 def _book(table, lens, refs, page_size: int):
@@ -570,11 +572,7 @@ def bv_pages_extend(table, lens, refs, page_size: int, n: int, n_new=None, strea
     blob, B, dev = _book(table, lens, refs, page_size)
     given = None if n_new is None else _counted(n_new, B, dev, "n_new")
     new, copies = table.new_empty((B,)), table.new_empty((B, 2))
-    lib = _lib or load_library()
-    with _on(table.device):
-        status = lib.bv_pages_extend(blob, given, n, new.data_ptr(), copies.data_ptr(), _raw_stream(table.device, stream))
-    if status:
-        _check(status)
+    _enqueue((_lib or load_library()).bv_pages_extend, dev, stream, blob, given, n, new.data_ptr(), copies.data_ptr())
     return new, copies
 
 
@@ -583,11 +581,7 @@ def bv_pages_truncate(table, lens, refs, page_size: int, keep, n: int = 0, n_new
     that hold nothing any more.  ``keep`` may be the out_len of a verification."""
     blob, B, dev = _book(table, lens, refs, page_size)
     kept, given = _counted(keep, B, dev, "keep"), None if n_new is None else _counted(n_new, B, dev, "n_new")
-    lib = _lib or load_library()
-    with _on(table.device):
-        status = lib.bv_pages_truncate(blob, kept, given, n, _raw_stream(table.device, stream))
-    if status:
-        _check(status)
+    _enqueue((_lib or load_library()).bv_pages_truncate, dev, stream, blob, kept, given, n)
 
 
 def bv_pages_fork(table, lens, refs, page_size: int, src, dst, stream=None):
@@ -598,25 +592,17 @@ def bv_pages_fork(table, lens, refs, page_size: int, src, dst, stream=None):
     ok = table.new_empty((forks,))
     if forks == 0:
         return ok
-    lib = _lib or load_library()
-    with _on(table.device):
-        status = lib.bv_pages_fork(blob, s, d, forks, ok.data_ptr(), _raw_stream(table.device, stream))
-    if status:
-        _check(status)
+    _enqueue((_lib or load_library()).bv_pages_fork, dev, stream, blob, s, d, forks, ok.data_ptr())
     return ok
 
 
 def bv_pages_compact(table, lens, refs, page_size: int, stream=None):
     """Renumbers the pages so that those in use come first.  Returns (moves int32 [num_pages // 2, 2], count int32 [1]), which
     bv_pages_copy takes for each layer before anything else uses the cache."""
-    blob, _, _ = _book(table, lens, refs, page_size)
+    blob, _, dev = _book(table, lens, refs, page_size)
     moves, count = table.new_empty((refs.shape[0] // 2, 2)), table.new_empty((1,))
-    lib = _lib or load_library()
-    with _on(table.device):
-        # (a pool of one page has no moves, and no place for them)
-        status = lib.bv_pages_compact(blob, moves.data_ptr() or count.data_ptr(), count.data_ptr(), _raw_stream(table.device, stream))
-    if status:
-        _check(status)
+    # (a pool of one page has no moves, and no place for them)
+    _enqueue((_lib or load_library()).bv_pages_compact, dev, stream, blob, moves.data_ptr() or count.data_ptr(), count.data_ptr())
     return moves, count
 
 
@@ -634,8 +620,4 @@ def bv_pages_copy(k, v, pairs, count=None, stream=None) -> None:
     if shape[0] == 0:
         return
     blob = _CACHE.pack(k.data_ptr(), v.data_ptr(), 0, 0, 0, ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], 0, 0, P, page, heads, D, code, 0)
-    lib = _lib or load_library()
-    with _on(k.device):
-        status = lib.bv_pages_copy(blob, pairs.data_ptr(), shape[0], upto, _raw_stream(k.device, stream))
-    if status:
-        _check(status)
+    _enqueue((_lib or load_library()).bv_pages_copy, dev, stream, blob, pairs.data_ptr(), shape[0], upto)

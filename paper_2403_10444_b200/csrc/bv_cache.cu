@@ -43,32 +43,48 @@ struct AppendArgs {
     const int32_t* lens;
     const int32_t* n_new;
     int B, n, heads, page, num_pages, width, vecs;
+    Divider by_n, by_heads, by_vecs, by_page;
 };
 
 // A thread copies the same vector of a row's key and of its value: two loads in flight, then two stores.
 template <typename V, typename I>
 __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a, const I total) {
     for (I x = static_cast<I>(blockIdx.x) * 256 + threadIdx.x; x < total; x += static_cast<I>(gridDim.x) * 256) {
-        const I y = x / a.vecs, z = y / a.heads;
-        const int c = static_cast<int>(x - y * a.vecs), h = static_cast<int>(y - z * a.heads);
-        const int b = static_cast<int>(z / a.n), t = static_cast<int>(z - static_cast<I>(b) * a.n);
+        int b, t, h, c;
+        if constexpr (sizeof(I) == 4) {
+            const int y = a.by_vecs(x), z = a.by_heads(y);
+            b = a.by_n(z);
+            t = z - b * a.n;
+            h = y - z * a.heads;
+            c = x - y * a.vecs;
+        } else {
+            const I y = x / a.vecs, z = y / a.heads;
+            b = static_cast<int>(z / a.n);
+            t = static_cast<int>(z - static_cast<I>(b) * a.n);
+            h = static_cast<int>(y - z * a.heads);
+            c = static_cast<int>(x - y * a.vecs);
+        }
         const int len = __ldg(a.lens + b);
         int m = a.n_new ? __ldg(a.n_new + b) : a.n;
         if (m > a.n) m = a.n;
         const int pos = len - m + t;
         if (t >= m || pos < 0 || len > static_cast<long long>(a.width) * a.page) continue;
-        const int page = __ldg(a.table + static_cast<long long>(b) * a.width + pos / a.page);
+        const int j = a.by_page(pos), page = __ldg(a.table + static_cast<long long>(b) * a.width + j);
         if (page < 0 || page >= a.num_pages) continue;
         V val[2];
 #pragma unroll
         for (int w = 0; w < 2; ++w) val[w] = *reinterpret_cast<const V*>(a.src[w] + b * a.ss[w][0] + t * a.ss[w][1] + h * a.ss[w][2] + c * sizeof(V));
 #pragma unroll
-        for (int w = 0; w < 2; ++w) *reinterpret_cast<V*>(a.dst[w] + page * a.ds[w][0] + h * a.ds[w][1] + pos % a.page * a.ds[w][2] + c * sizeof(V)) = val[w];
+        for (int w = 0; w < 2; ++w) *reinterpret_cast<V*>(a.dst[w] + page * a.ds[w][0] + h * a.ds[w][1] + (pos - j * a.page) * a.ds[w][2] + c * sizeof(V)) = val[w];
     }
 }
 template <typename V>
 cudaError_t launch_append(AppendArgs a, int row_bytes, cudaStream_t stream) {
     a.vecs = row_bytes / static_cast<int>(sizeof(V));
+    a.by_n = divider(a.n);
+    a.by_heads = divider(a.heads);
+    a.by_vecs = divider(a.vecs);
+    a.by_page = divider(a.page);
     const long long total = static_cast<long long>(a.B) * a.n * a.heads * a.vecs;
     const long long blocks = (total + 255) / 256;
     const unsigned grid = static_cast<unsigned>(blocks < (1 << 20) ? blocks : (1 << 20));
@@ -85,65 +101,78 @@ struct CopyArgs {
     const int32_t* pairs;     // [n][2] source, destination
     const int32_t* count;     // how many of them count, or null: all
     int n, num_pages;
-    int tokens[2];            // tokens of a head that is one run of `vecs` vectors each (a dense page is one run)
-    int vecs[2];              // vectors of a run
-    int runs[2];              // vectors of a page
-    int chunks;               // pieces of a page that are handed out: ceil(max(runs) / (256 kCopyVecs))
+    bool run[2];              // a page is one run
+    int tokens, vecs, all;    // tokens of a head, vectors of a row, of a page
+    Divider by_chunks, by_vecs, by_tokens;
 };
 constexpr int kCopyVecs = 4;
 
-// Pieces of 16 KB of all pairs' pages, keys and values, are dealt out to the CTAs; a thread has four loads in flight.
+// An item is 16 KB of a pair's page, of its keys or of its values; a thread has four loads in flight.  As many CTAs as items as long as those
+// are few: they come and go as memory lets them, which carries 6.0 TB/s for 2048 pages of 64 KB where 8 CTAs an SM that take item after
+// item carry 5.4 (6.7 and 5.9 for 16384 pages).  With a count on the device most of the items may be none, so there are at most
+// kCopyCtas then, which go on.
+constexpr int kCopyCtas = 148 * 64;
 template <typename V>
-__global__ void __launch_bounds__(256) copy_kernel(const CopyArgs a) {
-    int n = a.n;
-    if (a.count) n = min(n, max(0, __ldg(a.count)));
-    const long long items = 2LL * n * a.chunks;
+__global__ void __launch_bounds__(256) copy_kernel(const CopyArgs a, const long long most) {
+    long long items = most;
+    if (a.count) {
+        const int n = __ldg(a.count);
+        const long long some = 2LL * (n < 0 ? 0 : n < a.n ? n : a.n) * a.by_chunks.by;
+        items = some < items ? some : items;
+    }
     for (long long x = blockIdx.x; x < items; x += gridDim.x) {
-        const long long y = x / a.chunks;
-        const int chunk = static_cast<int>(x - y * a.chunks), w = static_cast<int>(y & 1);
-        const int2 pair = make_int2(__ldg(a.pairs + (y & ~1LL)), __ldg(a.pairs + (y | 1)));
-        if (pair.x < 0 || pair.y < 0 || pair.x >= a.num_pages || pair.y >= a.num_pages || pair.x == pair.y) continue;
-        const char* src = a.pool[w] + pair.x * a.ps[w];
-        char* dst = a.pool[w] + pair.y * a.ps[w];
+        const long long y = x >> 31 ? x / a.by_chunks.by : a.by_chunks(static_cast<int>(x));
+        const int chunk = static_cast<int>(x - y * a.by_chunks.by), w = static_cast<int>(y & 1);
+        const int from = __ldg(a.pairs + (y & ~1LL)), into = __ldg(a.pairs + (y | 1));
+        if (from < 0 || into < 0 || from >= a.num_pages || into >= a.num_pages || from == into) continue;
+        const char* src = a.pool[w] + from * a.ps[w];
+        char* dst = a.pool[w] + into * a.ps[w];
+        const int first = chunk * kCopyVecs * 256 + threadIdx.x;
         V val[kCopyVecs];
-        long long off[kCopyVecs];
+        if (a.run[w]) {
+            src += static_cast<long long>(first) * sizeof(V);
+            dst += static_cast<long long>(first) * sizeof(V);
 #pragma unroll
-        for (int i = 0; i < kCopyVecs; ++i) {
-            const int z = (chunk * kCopyVecs + i) * 256 + threadIdx.x;
-            off[i] = -1;
-            if (z < a.runs[w]) {
-                const int run = z / a.vecs[w], c = z - run * a.vecs[w], h = run / a.tokens[w], t = run - h * a.tokens[w];
-                off[i] = h * a.hs[w] + t * a.ts[w] + static_cast<long long>(c) * sizeof(V);
-                val[i] = *reinterpret_cast<const V*>(src + off[i]);
+            for (int i = 0; i < kCopyVecs; ++i)
+                if (first + i * 256 < a.all) val[i] = *reinterpret_cast<const V*>(src + i * 256 * sizeof(V));
+#pragma unroll
+            for (int i = 0; i < kCopyVecs; ++i)
+                if (first + i * 256 < a.all) *reinterpret_cast<V*>(dst + i * 256 * sizeof(V)) = val[i];
+        } else {
+            long long off[kCopyVecs];
+#pragma unroll
+            for (int i = 0; i < kCopyVecs; ++i) {
+                const int z = first + i * 256, row = a.by_vecs(z), h = a.by_tokens(row);
+                off[i] = h * a.hs[w] + (row - h * a.tokens) * a.ts[w] + static_cast<long long>(z - row * a.vecs) * sizeof(V);
+                if (z < a.all) val[i] = *reinterpret_cast<const V*>(src + off[i]);
             }
-        }
 #pragma unroll
-        for (int i = 0; i < kCopyVecs; ++i)
-            if (off[i] >= 0) *reinterpret_cast<V*>(dst + off[i]) = val[i];
+            for (int i = 0; i < kCopyVecs; ++i)
+                if (first + i * 256 < a.all) *reinterpret_cast<V*>(dst + off[i]) = val[i];
+        }
     }
 }
 template <typename V>
 cudaError_t launch_copy(CopyArgs a, const bv_cache& c, cudaStream_t stream) {
     const int es = size_of(c.dtype);
-    a.chunks = 1;
     for (int w = 0; w < 2; ++w) {
         const int64_t* st = w ? c.v_stride : c.k_stride;
         // a page whose rows lie one after the other, heads or tokens first, is one run
-        const bool dense = (st[2] == c.D || c.page_size == 1) && (st[1] == static_cast<int64_t>(c.page_size) * c.D || c.heads == 1);
-        const bool other = (st[1] == c.D || c.heads == 1) && (st[2] == static_cast<int64_t>(c.heads) * c.D || c.page_size == 1);
-        const long long row = static_cast<long long>(c.D) * es / static_cast<int>(sizeof(V)), all = row * c.heads * c.page_size;
-        const bool one = dense || other;
-        a.tokens[w] = one ? 1 : c.page_size;
-        a.vecs[w] = static_cast<int>(one ? all : row);
-        a.runs[w] = static_cast<int>(all);
+        const bool heads = (st[2] == c.D || c.page_size == 1) && (st[1] == static_cast<int64_t>(c.page_size) * c.D || c.heads == 1);
+        const bool tokens = (st[1] == c.D || c.heads == 1) && (st[2] == static_cast<int64_t>(c.heads) * c.D || c.page_size == 1);
+        a.run[w] = heads || tokens;
         a.ps[w] = st[0] * es;
         a.hs[w] = st[1] * es;
         a.ts[w] = st[2] * es;
-        const int chunks = static_cast<int>((all + 256 * kCopyVecs - 1) / (256 * kCopyVecs));
-        if (chunks > a.chunks) a.chunks = chunks;
     }
-    const long long items = 2LL * a.n * a.chunks;
-    copy_kernel<V><<<static_cast<unsigned>(items < 148 * 8 ? items : 148 * 8), 256, 0, stream>>>(a);
+    a.tokens = c.page_size;
+    a.vecs = c.D * es / static_cast<int>(sizeof(V));
+    a.all = a.vecs * c.heads * c.page_size;
+    a.by_vecs = divider(a.vecs);
+    a.by_tokens = divider(a.tokens);
+    a.by_chunks = divider((a.all + 256 * kCopyVecs - 1) / (256 * kCopyVecs));
+    const long long items = 2LL * a.n * a.by_chunks.by, most = a.count ? kCopyCtas : 0x7fffffff;
+    copy_kernel<V><<<static_cast<unsigned>(items < most ? items : most), 256, 0, stream>>>(a, items);
     return cudaGetLastError();
 }
 
