@@ -65,7 +65,12 @@ __device__ __forceinline__ bool key_row(const AttendArgs& a, const Walk& w, cons
 __device__ __forceinline__ bool whole_tile(const AttendArgs& a, const Sight& s, int start, int keys) {
     return start + keys - 1 <= s.p0 && (start >= s.low1 || start + keys <= a.sinks);
 }
-__device__ __forceinline__ float factor_of(float m, float M) { return m == -INFINITY ? 0.f : exp2f(m - M); }
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float factor_of(float m, float M) { return m == -INFINITY ? 0.f : ex2(m - M); }
 
 // Elements d .. d + 3 of the unit's row `row` from their sums, to `out` or to the CTA's part of the unit.
 template <typename T>
@@ -239,13 +244,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_few_kernel(const AttendArg
             for (int r = 0; r < R; ++r) {
                 some[r] = p <= pos[r] && (p >= low[r] || p < a.sinks) && s[r] != -INFINITY;
                 if (some[r] && s[r] > m[r] + kLag) {
-                    const float f = exp2f(m[r] - s[r]);
+                    const float f = ex2(m[r] - s[r]);
                     m[r] = s[r];
                     l[r] *= f;
 #pragma unroll
                     for (int x = 0; x < NJ * 4; ++x) acc[r][x] *= f;
                 }
-                s[r] = some[r] ? exp2f(s[r] - m[r]) : 0.f;
+                s[r] = some[r] ? ex2(s[r] - m[r]) : 0.f;
                 l[r] += s[r];
             }
 #pragma unroll
@@ -362,28 +367,40 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
         };
         auto fetch = [&](int i) {
             if (i < nt) {
-#pragma unroll 2
-                for (int x = tid; x < 2 * KT * Sh::kVecs; x += kThreads) {
-                    const int c = x % Sh::kVecs, key = x / Sh::kVecs % KT, which = x / (Sh::kVecs * KT);
-                    const long long off = sm.row[i % 3][which][key];
-                    if (off < 0 || c >= quads) continue;
-                    const T* src = static_cast<const T*>(which ? a.v : a.k) + off + c * 4;
-                    float* dst = which ? &sm.v[i & 1][key][c * 4] : &sm.k[i & 1][key][c * 4];
-                    if constexpr (sizeof(T) == 4) {
-                        if (aligned) {
-                            copy4(dst, src);
-                            continue;
-                        }
-                    } else {
-                        if (aligned) {
-                            float y[4];
-                            widen(src, y);
-                            *reinterpret_cast<float4*>(dst) = make_float4(y[0], y[1], y[2], y[3]);
-                            continue;
+                // (a thread has one group of four of every kStep-th key; eight rows are looked up at a time)
+                constexpr int kStep = kThreads / Sh::kVecs, kRound = KT / kStep < 8 ? KT / kStep : 8;
+                const int c = tid % Sh::kVecs, key0 = tid / Sh::kVecs;
+                if (c < quads) {
+#pragma unroll 1
+                    for (int y = 0; y < 2 * KT; y += kRound * kStep) {
+                        const int which = y >= KT, at = key0 + y - which * KT;
+                        const T* const pool = static_cast<const T*>(which ? a.v : a.k) + c * 4;
+                        float* const to = which ? &sm.v[i & 1][at][c * 4] : &sm.k[i & 1][at][c * 4];
+                        const int pitch = (which ? Sh::kRow : Sh::kRow + 4) * kStep;
+                        long long off[kRound];
+#pragma unroll
+                        for (int x = 0; x < kRound; ++x) off[x] = sm.row[i % 3][which][at + x * kStep];
+                        if (sizeof(T) == 4 && aligned) {
+#pragma unroll
+                            for (int x = 0; x < kRound; ++x)
+                                if (off[x] >= 0) copy4(to + x * pitch, reinterpret_cast<const float*>(pool + off[x]));
+                        } else if (aligned) {
+                            float z[kRound][4];
+#pragma unroll
+                            for (int x = 0; x < kRound; ++x)
+                                if (off[x] >= 0) widen(pool + off[x], z[x]);
+#pragma unroll
+                            for (int x = 0; x < kRound; ++x)
+                                if (off[x] >= 0) *reinterpret_cast<float4*>(to + x * pitch) = make_float4(z[x][0], z[x][1], z[x][2], z[x][3]);
+                        } else {
+#pragma unroll 1
+                            for (int x = 0; x < kRound; ++x) {
+                                const long long o = sm.row[i % 3][which][at + x * kStep];
+                                for (int e = 0; e < 4; ++e)
+                                    if (o >= 0 && c * 4 + e < a.D) to[x * pitch + e] = to_float(pool[o + e]);
+                            }
                         }
                     }
-                    for (int e = 0; e < 4; ++e)
-                        if (c * 4 + e < a.D) dst[e] = to_float(src[e]);
                 }
             }
             cp_async_commit();
@@ -467,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
 #pragma unroll
                     for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
                     if (top > m[r] + kLag) {
-                        const float f = exp2f(m[r] - top);
+                        const float f = ex2(m[r] - top);
                         m[r] = top;
                         l[r] *= f;
                         if (tx == 0) sm.factor[2 * ty + r] = f;
@@ -477,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
                     }
 #pragma unroll
                     for (int x = 0; x < kI; ++x) {
-                        const float p = s[r][x] == -INFINITY ? 0.f : exp2f(s[r][x] - m[r]);
+                        const float p = s[r][x] == -INFINITY ? 0.f : ex2(s[r][x] - m[r]);
                         l[r] += p;
                         sm.p[tx + 16 * x][2 * ty + r] = p;
                     }

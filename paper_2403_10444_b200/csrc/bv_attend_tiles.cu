@@ -549,15 +549,19 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                     }
                     __syncwarp();
                 }
-                // k s - m, and whether any of them is too large
-                float most = -INFINITY;
-                load_columns<C>(s_at, s);
+                // k s - m, and whether any of them is too large (a unit's first tile has no m to be held to)
+                bool raise = i == 0;
+                if (!raise) {
+                    float most = -INFINITY;
+                    load_columns<C>(s_at, s);
 #pragma unroll
-                for (int c = 0; c < C; c += 8) wait_ld8(s + c);
-                weigh<C>(s, ts.nref + c0, a.kf, masked, lo, hi);
+                    for (int c = 0; c < C; c += 8) wait_ld8(s + c);
+                    weigh<C>(s, ts.nref + c0, a.kf, masked, lo, hi);
 #pragma unroll
-                for (int c = 0; c < C; ++c) most = fmaxf(most, s[c]);
-                if (team_any<kTeam>(bar, most > kLag || failed)) {
+                    for (int c = 0; c < C; ++c) most = fmaxf(most, s[c]);
+                    raise = team_any<kTeam>(bar, most > kLag || failed);
+                }
+                if (raise) {
 #pragma unroll 1
                     for (int c = 0; c < C; c += 8) {
                         float y[8];

@@ -139,10 +139,36 @@ __device__ __forceinline__ long long part_of(long long total, int c, int n) {
     const unsigned long long x = static_cast<unsigned long long>(total) * static_cast<unsigned>(c);
     return x >> 32 ? static_cast<long long>(x / static_cast<unsigned>(n)) : static_cast<long long>(static_cast<unsigned>(x) / static_cast<unsigned>(n));
 }
+// (At most 352 threads.  It holds the CTA's first barriers: what threads have set up before is there for all behind it.)
 __device__ __forceinline__ Share find_share(const AttendArgs& a, ShareSmem& sm, int threads) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int each = a.B <= threads ? 1 : (a.B + threads - 1) / threads;
     const int b0 = tid * each < a.B ? tid * each : a.B, b1 = b0 + each < a.B ? b0 + each : a.B;
+    Share s;
+    const int c = blockIdx.x;
+    auto cut = [&](long long total) {
+        s.total = total;
+        s.ctas = total < gridDim.x ? static_cast<int>(total) : gridDim.x;
+        s.begin = c < s.ctas ? part_of(total, c, s.ctas) : total;
+        s.end = c < s.ctas ? part_of(total, c + 1, s.ctas) : total;
+    };
+    if (a.B <= 32) {
+        // a lane a sequence, every warp for itself
+        const long long ph = lane < a.B ? head_tiles(a, seq_of(a, lane)) : 0, mine = a.Hkv * ph;
+        long long upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        cut(__shfl_sync(0xffffffffu, upto, 31));
+        const unsigned here = __ballot_sync(0xffffffffu, upto - mine <= s.begin && s.begin < upto);
+        s.b = here ? __ffs(here) - 1 : 0;
+        s.off = s.begin - __shfl_sync(0xffffffffu, upto - mine, s.b);
+        s.per_head = __shfl_sync(0xffffffffu, ph, s.b);
+        __syncthreads();
+        return s;
+    }
     long long mine = 0, per_head = 0;
 #pragma unroll 1
     for (int b = b0; b < b1; ++b) mine += a.Hkv * (per_head = head_tiles(a, seq_of(a, b)));
@@ -155,19 +181,14 @@ __device__ __forceinline__ Share find_share(const AttendArgs& a, ShareSmem& sm, 
     if (lane == 31) sm.sums[warp] = upto;
     __syncthreads();
     long long before = 0, total = 0;
-#pragma unroll 1
-    for (int w = 0; w < threads / 32; ++w) {
-        const long long x = sm.sums[w];
+#pragma unroll
+    for (int w = 0; w < 11; ++w) {
+        const long long x = w < threads / 32 ? sm.sums[w] : 0;
         before += w < warp ? x : 0;
         total += x;
     }
     before += upto - mine;
-    Share s;
-    s.total = total;
-    s.ctas = total < gridDim.x ? static_cast<int>(total) : gridDim.x;
-    const int c = blockIdx.x;
-    s.begin = c < s.ctas ? part_of(total, c, s.ctas) : total;
-    s.end = c < s.ctas ? part_of(total, c + 1, s.ctas) : total;
+    cut(total);
     if (s.begin < s.end && before <= s.begin && s.begin < before + mine) {
         int b = b0;
         if (each > 1) {
@@ -302,33 +323,55 @@ __device__ __forceinline__ void join_share(const AttendArgs& a, const Joint& u, 
         const int e = x + tid / lanes;
         const bool mine = e < e1;
         const int row = mine ? e / per_row : 0, d = mine ? (e - row * per_row) * W : 0;
-        float M = -INFINITY;
+        float M = -INFINITY, l = 0.f, o[W];
         bool nan = false;
-#pragma unroll 4
-        for (int c = sub; c < parts; c += lanes) {
-            const float m = __ldcg(base + (2 * c + (c == 0)) * stride + row);
-            nan |= m != m;
-            M = fmaxf(M, m);
-        }
-        for (int o = 1; o < lanes; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-        float l = 0.f, o[W];
 #pragma unroll
         for (int i = 0; i < W; ++i) o[i] = 0.f;
-#pragma unroll 4
-        for (int c = sub; c < parts; c += lanes) {
-            const float* p = base + (2 * c + (c == 0)) * stride;
-            const float m = __ldcg(p + row), pl = __ldcg(p + a.rows + row);
-            const float f = m == -INFINITY ? 0.f : exp2f(m - M);
-            l += m == -INFINITY ? pl : f * pl;              // (nothing visible there: zero; a page that is none: NaN)
-            float v[W];
-            if constexpr (W == 4) {
-                const float4 x4 = __ldcg(reinterpret_cast<const float4*>(p + 2 * a.rows + static_cast<size_t>(row) * a.D + d));
-                v[0] = x4.x; v[1] = x4.y; v[2] = x4.z; v[3] = x4.w;
-            } else {
-                v[0] = __ldcg(p + 2 * a.rows + static_cast<size_t>(row) * a.D + d);
-            }
+        // four parts at a time, all of their numbers under way together; what has been summed up is scaled where a larger m comes
+        for (int c0 = sub; c0 < parts; c0 += 4 * lanes) {
+            float m[4], pl[4], v[4][W];
 #pragma unroll
-            for (int i = 0; i < W; ++i) o[i] += f * v[i];
+            for (int y = 0; y < 4; ++y) {
+                const int c = c0 + y * lanes;
+                const bool there = c < parts;
+                const float* p = base + (there ? (2 * c + (c == 0)) * stride : 0);
+                m[y] = there ? __ldcg(p + row) : -INFINITY;
+                pl[y] = there ? __ldcg(p + a.rows + row) : 0.f;
+                const float* const at = p + 2 * a.rows + static_cast<size_t>(row) * a.D + d;
+                if constexpr (W == 4) {
+                    const float4 x4 = there ? __ldcg(reinterpret_cast<const float4*>(at)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    v[y][0] = x4.x; v[y][1] = x4.y; v[y][2] = x4.z; v[y][3] = x4.w;
+                } else {
+                    v[y][0] = there ? __ldcg(at) : 0.f;
+                }
+            }
+            float top = M;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                nan |= m[y] != m[y];
+                top = fmaxf(top, m[y]);
+            }
+            const float scale = M == -INFINITY ? 0.f : exp2f(M - top);
+            l = M == -INFINITY ? l : l * scale;               // (a sum of nothing: zero; of a page that is none: NaN)
+#pragma unroll
+            for (int i = 0; i < W; ++i) o[i] *= scale;
+            M = top;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const float f = m[y] == -INFINITY ? 0.f : exp2f(m[y] - M);
+                l += m[y] == -INFINITY ? pl[y] : f * pl[y];
+#pragma unroll
+                for (int i = 0; i < W; ++i) o[i] += f * v[y][i];
+            }
+        }
+        // the lanes' sums, on one m
+        float top = M;
+        for (int s = 1; s < lanes; s <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+        if (M != -INFINITY) {
+            const float scale = exp2f(M - top);
+            l *= scale;
+#pragma unroll
+            for (int i = 0; i < W; ++i) o[i] *= scale;
         }
         if (nan) l = NAN;
         for (int s = 1; s < lanes; s <<= 1) {
@@ -366,7 +409,6 @@ __device__ __forceinline__ void join_units(const AttendArgs& a, JointSmem& js, i
         }
         js.ok[tid] = v >= parts;
         if (v < parts) atomicExch(a.status, 1);
-        __threadfence();
     }
     __syncthreads();
     for (int j = 0; j < n; ++j) {
