@@ -627,10 +627,12 @@ void attend_rows_plan(AttendArgs* a) {
     if (few(a->D, rows)) {
         a->rows = few_each(a->D);
         a->span = kFewKeys;
+        a->extra = 6;                          // a unit's beginning and end, 8000 clocks, where a tile takes 1300
     } else {
         const int tiles = (rows + 31) / 32;
         a->rows = ((rows + tiles - 1) / tiles + 7) / 8 * 8;
         a->span = a->D <= 128 ? 64 : 32;
+        a->extra = 1;
     }
     a->per_page = 1;
 }

@@ -264,18 +264,19 @@ __device__ __forceinline__ void load_tiles(const AttendArgs& a, Smem<NP, N>& sm,
 
 // The products, by one thread: S of a tile before O of the one before it.
 template <int NP, int N>
-__device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>& sm, Walk w, int total, uint32_t tmem, uint32_t limit) {
+__device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>& sm, Walk w, uint32_t tmem, uint32_t limit) {
     using Sh = Shape<NP, N>;
     constexpr uint32_t qk = instruction(kTile, N, false, false), pv = instruction(64 * NP, N, true, true);
     const uint32_t ring = smem_u32(sm.ring), o_at = tmem + 2 * N;
     bool ok = true;
     auto wait = [&](unsigned long long& bar, int phase) { ok = ok && mbar_wait_now(smem_u32(&bar), phase & 1, a.status, limit); };
-    int unit = 0, left = w.upto - w.i;         // of the tile whose scores come next
+    int unit = 0, left = w.more ? w.upto - w.i : 0;      // of the tile whose scores come next
     unsigned starts = 0, ends = 0, teams = 0;  // bit t & 1: tile t is its unit's first, its last, its unit's team
-    auto scores = [&](int t) {
+    auto scores = [&](int t) {                 // false: there is no such tile
         const bool first = t == 0 || left == 0;
         if (left == 0) {
             walk_next(a, w);
+            if (!w.more) return false;
             left = w.upto - w.i;
             ++unit;
         }
@@ -288,7 +289,7 @@ __device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>&
         note(teams, team != 0);
         const int slot = 2 * t % Sh::kSlots;
         wait(sm.full[slot], 2 * t / Sh::kSlots);
-        if (!ok) return;
+        if (!ok) return false;
         fence_after();
         const uint32_t k_low = desc_low(ring + slot * Sh::kSlot, 16), q_low = desc_low(smem_u32(sm.q[team]), 16), s_at = tmem + bit * N;
 #pragma unroll
@@ -301,13 +302,14 @@ __device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>&
             if (first) commit(smem_u32(&sm.u_start[team]));
             commit(smem_u32(&sm.s_full[bit]));
         }
+        return true;
     };
-    if (total > 0) scores(0);
+    bool have = w.more && scores(0);
 #pragma unroll 1
-    for (int g = 0; g < total && ok; ++g) {
+    for (int g = 0; have && ok; ++g) {
         // (with one team the next unit's rows take the place of this one's when its last scores are there: its end does not wait for them)
         const bool later = Sh::kTeams == 1 && left == 0;
-        if (g + 1 < total && !later) scores(g + 1);
+        if (!later) have = scores(g + 1);
         const int x = 2 * g + 1, slot = x % Sh::kSlots, buffer = g % Sh::kBuffers, bit = g & 1, team = teams >> bit & 1;
         wait(sm.full[slot], x / Sh::kSlots);
         wait(sm.p_full[buffer], g / Sh::kBuffers);
@@ -321,7 +323,7 @@ __device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>&
         commit(smem_u32(&sm.empty[slot]));
         commit(smem_u32(&sm.p_done[buffer]));
         if (ends >> bit & 1) commit(smem_u32(&sm.u_done[team]));
-        if (g + 1 < total && later) scores(g + 1);
+        if (later) have = scores(g + 1);
     }
     if (!ok) {
         commit(smem_u32(&sm.drain));
@@ -430,7 +432,7 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
         // (the lane is elected, not chosen by its number, so that the compiler knows that it is one: a fourth less time an instruction)
         uint32_t one;
         asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
-        if (one) issue_products<NP, N>(a, sm, w, static_cast<int>(sh.end - sh.begin), tmem, limit);
+        if (one) issue_products<NP, N>(a, sm, w, tmem, limit);
         __syncwarp();
     } else {
         // ---- weights
@@ -660,11 +662,12 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
             team_sync<kTeam>(bar);
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + w.b * a.os[0] + w.h * a.group * a.os[2] + dim;
 #pragma unroll 1
-            for (int c = 0; c < C && c0 + c < v.count; c += 8) {
-                float o[8];
+            for (int c = 0; c < C && c0 + c < v.count; c += 16) {
+                float o[16];
                 __syncwarp();
-                ld8(o_at + c, o);
+                ld16(o_at + c, o);             // (of the last columns, where C is not a multiple of 16, some that are not the thread's)
                 wait_ld8(o);
+                wait_ld8(o + 8);
                 if (fix && has_dim) {
                     // what is not finite among the values that some rows see and others do not
 #pragma unroll 1
@@ -681,22 +684,22 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                             const float val = to_float((static_cast<const __nv_bfloat16*>(a.v) + page * a.vs[0] + w.h * a.vs[1] + (p - j * a.page) * a.vs[2])[dim]);
                             if (isfinite(val)) continue;
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) {
+                            for (int e = 0; e < 16; ++e) {
                                 const int pos = w.s.base + a.by_group(w.r0 + c0 + c + e);
                                 if (p <= pos && (p >= low_of(a, pos) || p < a.sinks)) o[e] += val;
                             }
                         }
                     }
                 }
-                const int left = has_dim ? v.count - c0 - c : 0;
+                const int mine = C - c < v.count - c0 - c ? C - c : v.count - c0 - c, left = has_dim ? mine : 0;
                 if (part) {
                     float* const at = part + 2 * a.rows + (c0 + c) * a.D + dim;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
+                    for (int e = 0; e < 16; ++e)
                         if (e < left) at[e * a.D] = o[e];
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
+                    for (int e = 0; e < 16; ++e)
                         if (e < left) out[ts.off[c0 + c + e]] = __float2bfloat16_rn(o[e] * ts.part[0][c0 + c + e]);
                 }
             }
@@ -772,6 +775,8 @@ void attend_tiles_plan(AttendArgs* a) {
     a->rows = ((rows + tiles - 1) / tiles + 15) / 16 * 16;
     a->span = a->page <= kTile ? kTile / a->page * a->page : kTile;
     a->per_page = a->page <= kTile ? 1 : (a->page + kTile - 1) / kTile;
+    // a unit's beginning and end: 7.2 us at 80 rows, where a tile takes 1.3; 1.3 us at 16, where teams overlap, and a tile takes 1.2
+    a->extra = a->rows >= 48 ? 5 : 1;
 }
 cudaError_t launch_attend_tiles(const AttendArgs& a, bool q_vec, int ctas, cudaStream_t stream, bool* taken) {
     CUtensorMap k, v;

@@ -208,11 +208,18 @@ int enqueue_attend(const StreamWork& work, void* ctx) {
     c.a.wait_limit = work.wait_limit;
     c.a.never_signal = work.never_signal;
     const int ctas = attend_ctas(work.sm_count);
+    // (fewer units than CTAs: the CTAs have parts of one or two, whose ends are as many everywhere)
+    auto few_units = [&] {
+        const long long units = static_cast<long long>(c.a.B) * c.a.Hkv * ((c.a.n * c.a.group + c.a.rows - 1) / c.a.rows);
+        if (units < ctas) c.a.extra = 0;
+    };
+    few_units();
     if (c.tiles) {
         bool taken = false;
         const cudaError_t e = launch_attend_tiles(c.a, c.q_vec, ctas, c.stream, &taken);
         if (e != cudaSuccess || taken) return done(e, 1);
         plan(&c, false);
+        few_units();
     }
     return done(launch_attend_rows(c.a, c.dtype, c.aligned, c.q_vec, ctas, c.stream), 1);
 }

@@ -28,7 +28,9 @@ inline Divider divider(unsigned by) {
 // keys; all tiles of all units, in that order, are one list that is cut into gridDim.x equal contiguous parts.  A CTA goes
 // through its part; what a unit has in several CTAs is left in `part` and joined by the one that finishes last.
 // (Lengths lie on the device and change from call to call, so the list is laid out by the kernel itself: equal parts keep
-// every SM at work whatever the lengths are, where a grid of (sequence, head, fixed pieces) waits for the longest sequence.)
+// every SM at work whatever the lengths are, where a grid of (sequence, head, fixed pieces) waits for the longest sequence.  Units of
+// different sequences are not equally long, so some CTAs have twelve ends of units where others have three: each counts as `extra` tiles in
+// front of its own.)
 struct AttendArgs {
     const void* q;
     void* out;
@@ -46,6 +48,7 @@ struct AttendArgs {
     int rows;                 // query rows of a unit, at most (row = token * group + head of the group)
     int span;                 // keys of a tile; for pages that are several tiles those of a tile but the last of a page
     int per_page;             // tiles of a page, where a page is more than one (else 1)
+    int extra;                // what a unit costs besides its tiles, in tiles: it counts as that many more when the list is cut
     float* part;              // [gridDim.x][2] partial results of part_floats(rows, D)
     unsigned* counters;       // [gridDim.x] by the first CTA of a unit that several have: those that have come, then gone; zero between launches
     int* status;              // set if a bounded wait gave up
@@ -110,24 +113,24 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, const Seq& s, int r
     u.tiles = u.sink + tile_of(a, p1) - u.first + 1;
     return u;
 }
-// Tiles of one key-value head of a sequence, over its tiles of rows.
-__device__ __forceinline__ long long head_tiles(const AttendArgs& a, const Seq& s) {
+// What one key-value head of a sequence takes of the list, over its tiles of rows.
+__device__ __forceinline__ long long head_cost(const AttendArgs& a, const Seq& s) {
     long long sum = 0;
     for (int r0 = 0; r0 < s.rows; r0 += a.rows) {
         const int r1 = (r0 + a.rows < s.rows ? r0 + a.rows : s.rows) - 1;
-        sum += span_of(a, s, r0, r1).tiles;
+        sum += span_of(a, s, r0, r1).tiles + a.extra;
     }
     return sum;
 }
 
 // Where a CTA's part of the list begins, as found by all its threads together.
 struct Share {
-    long long total;          // tiles of the list
-    int ctas;                 // CTAs that take part: no more than there are tiles, so that each has some
+    long long total;          // length of the list
+    int ctas;                 // CTAs that take part: no more than the list is long
     long long begin, end;     // the CTA's part
-    int b;                    // the sequence its first tile belongs to
-    long long off;            // ... and how many of that sequence's tiles come before it
-    long long per_head;       // tiles of one head of it
+    int b;                    // the sequence that it begins in
+    long long off;            // ... and how much of that sequence comes before it
+    long long per_head;       // what one head of it takes
 };
 struct ShareSmem {
     long long sums[32];
@@ -154,7 +157,7 @@ __device__ __forceinline__ Share find_share(const AttendArgs& a, ShareSmem& sm, 
     };
     if (a.B <= 32) {
         // a lane a sequence, every warp for itself
-        const long long ph = lane < a.B ? head_tiles(a, seq_of(a, lane)) : 0, mine = a.Hkv * ph;
+        const long long ph = lane < a.B ? head_cost(a, seq_of(a, lane)) : 0, mine = a.Hkv * ph;
         long long upto = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -171,7 +174,7 @@ __device__ __forceinline__ Share find_share(const AttendArgs& a, ShareSmem& sm, 
     }
     long long mine = 0, per_head = 0;
 #pragma unroll 1
-    for (int b = b0; b < b1; ++b) mine += a.Hkv * (per_head = head_tiles(a, seq_of(a, b)));
+    for (int b = b0; b < b1; ++b) mine += a.Hkv * (per_head = head_cost(a, seq_of(a, b)));
     long long upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -193,7 +196,7 @@ __device__ __forceinline__ Share find_share(const AttendArgs& a, ShareSmem& sm, 
         int b = b0;
         if (each > 1) {
             for (;; ++b) {
-                per_head = head_tiles(a, seq_of(a, b));
+                per_head = head_cost(a, seq_of(a, b));
                 if (s.begin < before + a.Hkv * per_head) break;
                 before += a.Hkv * per_head;
             }
@@ -209,14 +212,14 @@ __device__ __forceinline__ Share find_share(const AttendArgs& a, ShareSmem& sm, 
     return s;
 }
 
-// A walk over a CTA's part, unit by unit.
+// A walk over a CTA's part, unit by unit (those that it has tiles of).
 struct Walk {
-    long long at, end;        // the list's tile that comes next, the end of the part
+    long long at, end;        // the list's place of the tile that comes next, the end of the part
     int b, h, r0;             // the unit
     Seq s;
     Span u;
     int i, upto;              // its tiles [i, upto) are the CTA's
-    long long unit_at;        // the list's number of its tile 0
+    long long unit_at;        // the list's place of its tile 0
     bool more;
 };
 __device__ __forceinline__ void walk_unit(const AttendArgs& a, Walk& w) {
@@ -224,13 +227,13 @@ __device__ __forceinline__ void walk_unit(const AttendArgs& a, Walk& w) {
     w.u = span_of(a, w.s, w.r0, r1);
 }
 __device__ __forceinline__ void walk_cut(Walk& w) {
+    w.more = w.at < w.end;
     w.unit_at = w.at - w.i;
     const long long left = w.end - w.at;
     w.upto = left < w.u.tiles - w.i ? w.i + static_cast<int>(left) : w.u.tiles;
 }
 __device__ __forceinline__ Walk walk_begin(const AttendArgs& a, const Share& sh) {
     Walk w;
-    w.at = sh.begin;
     w.end = sh.end;
     w.more = sh.begin < sh.end;
     if (!w.more) return w;
@@ -246,15 +249,16 @@ __device__ __forceinline__ Walk walk_begin(const AttendArgs& a, const Share& sh)
     }
     for (w.r0 = 0;; w.r0 += a.rows) {
         walk_unit(a, w);
-        if (off < w.u.tiles) break;
-        off -= w.u.tiles;
+        if (off < w.u.tiles + a.extra) break;
+        off -= w.u.tiles + a.extra;
     }
-    w.i = static_cast<int>(off);
+    w.i = off > a.extra ? static_cast<int>(off) - a.extra : 0;
+    w.at = sh.begin + (off < a.extra ? a.extra - off : 0);
     walk_cut(w);
     return w;
 }
 __device__ __forceinline__ void walk_next(const AttendArgs& a, Walk& w) {
-    w.at += w.upto - w.i;
+    w.at += w.upto - w.i + a.extra;
     if (w.at >= w.end) { w.more = false; return; }
     w.i = 0;
     w.r0 += a.rows;
@@ -262,7 +266,7 @@ __device__ __forceinline__ void walk_next(const AttendArgs& a, Walk& w) {
         w.r0 = 0;
         if (++w.h >= a.Hkv) {
             w.h = 0;
-            do w.s = seq_of(a, ++w.b); while (w.s.rows == 0);     // (the list has tiles left, so there is one)
+            do w.s = seq_of(a, ++w.b); while (w.s.rows == 0);     // (the list goes on, so there is one)
         }
     }
     walk_unit(a, w);
@@ -270,9 +274,9 @@ __device__ __forceinline__ void walk_next(const AttendArgs& a, Walk& w) {
 }
 __device__ __forceinline__ int tile_at(const Span& u, int i) { return i < u.sink ? i : u.first + i - u.sink; }
 
-// The CTA that holds a tile of the list.
-__device__ __forceinline__ int holder_of(const Share& sh, long long tile) {
-    const unsigned long long x = static_cast<unsigned long long>(tile + 1) * static_cast<unsigned>(sh.ctas) - 1;
+// The CTA that holds a place of the list.
+__device__ __forceinline__ int holder_of(const Share& sh, long long place) {
+    const unsigned long long x = static_cast<unsigned long long>(place + 1) * static_cast<unsigned>(sh.ctas) - 1;
     return (x | sh.total) >> 32 ? static_cast<int>(x / sh.total) : static_cast<unsigned>(x) / static_cast<unsigned>(sh.total);
 }
 
