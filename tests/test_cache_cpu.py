@@ -1,7 +1,9 @@
 """The paged cache's entry points without a GPU: what they refuse before they touch a device, and the plain bookkeeping that the GPU
 tests compare with, pinned on cases worked out by hand."""
 import ctypes
+import os
 import struct
+import subprocess
 
 import pytest
 import torch
@@ -153,3 +155,72 @@ def test_the_plain_attention_on_a_case_by_hand():
     assert (out - 4).abs().max() < 1e-7 and written.all() and 0 < bound.max() < 1e-4
     assert (cp.attend(q, k, v, table, lens, scale=1.0, window=1)[0] == 5).all()
     assert ((cp.attend(q, k, v, table, lens, scale=1.0, window=1, sinks=1)[0] - 4).abs() < 1e-7).all()
+
+
+# ---- what the kernels are handed, over the runtime of tests/host_runtime.cu ----
+
+@pytest.fixture(scope="module")
+def host_so(tmp_path_factory):
+    here = os.path.dirname(os.path.abspath(__file__))
+    built = bv_build.build()
+    out = str(tmp_path_factory.mktemp("host") / "host_cache.so")
+    subprocess.check_call([os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"), "-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17",
+                           "-Xcompiler", "-fPIC", "-shared", "-I", bv_build.CSRC, os.path.join(here, "host_cache.cu"), "-o", out,
+                           "-Xlinker", "-Bsymbolic", "-Xlinker", "-rpath=" + os.path.dirname(built), built])
+    return ctypes.CDLL(out)
+
+
+@pytest.fixture
+def host(host_so):
+    host_so.bv_release()
+    host_so.host_errors.restype = ctypes.c_char_p
+    host_so.host_live_bytes.restype = ctypes.c_size_t
+    yield host_so
+    host_so.host_refuse_tiles(0)
+    host_so.bv_release()
+
+
+def on_host(host, B=3, n=1, q_heads=8, heads=2, D=128, page=16, dtype=1, offset=0, stream=None):
+    status = host.host_attend(B, n, q_heads, heads, D, page, dtype, ctypes.c_longlong(offset), ctypes.c_void_p(stream))
+    return status, host.host_attend_kernel()
+
+
+def test_the_parts_fit_the_workspace_whatever_the_shape(host):
+    for dtype in (0, 1):
+        for D in (8, 33, 64, 80, 128, 136, 256):
+            for n in (1, 2, 9, 17, 300):
+                for group in (1, 3, 8, 64):
+                    for page in (1, 16, 24, 200):
+                        assert on_host(host, n=n, q_heads=2 * group, D=D, page=page, dtype=dtype)[0] == 0
+                        assert host.host_errors() == b"", (dtype, D, n, group, page)
+
+
+def test_which_kernel_takes_a_call(host):
+    assert on_host(host)[1] == 1                                        # bf16 in whole vectors: the tensor cores
+    assert on_host(host, dtype=0)[1] == 2                               # 32 bits
+    assert on_host(host, offset=1)[1] == 2 and on_host(host, D=36)[1] == 2 and on_host(host, D=136)[1] == 2 and on_host(host, page=20)[1] == 2
+    assert on_host(host, D=72, page=24)[1] == 1 and on_host(host, D=16, page=8)[1] == 1 and on_host(host, page=1000)[1] == 1
+    host.host_refuse_tiles(1)                                           # no map of the pools: the other kernels, planned anew
+    for n in (1, 5, 40):
+        assert on_host(host, n=n) == (0, 2) and host.host_errors() == b""
+    host.host_refuse_tiles(0)
+    # rows of a unit: as even as multiples of 16 are, no more units than have to be
+    for rows, want in ((1, 16), (16, 16), (17, 32), (72, 80), (80, 80), (81, 48), (136, 80), (161, 64), (272, 80)):
+        on_host(host, n=rows, q_heads=1, heads=1)
+        assert host.host_attend_rows() == want, rows
+
+
+def test_calls_of_several_sizes_and_their_replays_share_a_workspace(host):
+    sizes = [dict(), dict(n=9, q_heads=64, heads=8), dict(n=300, q_heads=8), dict(dtype=0, n=5, q_heads=10, D=80, page=24)]
+    for a in sizes:
+        for b in sizes:
+            host.bv_release()
+            on_host(host)                                               # (the library is set up before any capture)
+            host.host_begin_capture(None)
+            assert on_host(host, **a)[0] == 0
+            graph = host.host_end_capture()
+            for step in (b, None, b, a, None, None, b):
+                host.host_replay(graph) if step is None else on_host(host, **step)
+                assert host.host_errors() == b"", (a, b)
+    host.bv_release()
+    assert host.host_live_bytes() == 0 and host.host_errors() == b""
