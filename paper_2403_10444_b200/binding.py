@@ -13,6 +13,11 @@ from typing import Optional, Tuple
 
 import torch
 
+try:
+    from . import _fast          # the cache's calls marshalled in C++ (build.build_fast); without it they are marshalled below
+except ImportError:
+    _fast = None
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libbv_b200.so")
 
@@ -79,6 +84,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.bv_status_string.argtypes = [ci]
     if path is None:
         _lib = lib
+        if _fast is not None:
+            _fast.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in
+                         ("bv_cache_attend", "bv_cache_append", "bv_pages_extend", "bv_pages_truncate", "bv_pages_fork", "bv_pages_compact", "bv_pages_copy")))
     return lib
 
 
@@ -442,8 +450,9 @@ def _lse_call(name, target_logits, draft_logits, draft_tokens, uniforms, draft_l
 
 # ---- the paged key-value cache (include/bv.h, struct bv_cache) ----
 #
-# A call of the cache takes some 10 us on the GPU and is made for every layer, so the checks are made on what each tensor is
-# asked once (an attribute costs 0.1 us); what a check finds wrong is put in words where it fails.
+# A call of the cache takes some 10 us on the GPU and is made for every layer.  What is in order goes through _fast (5 us of host time a
+# call, nearly all of it the launch); what it will not take, and everything where it is not built, is checked here, where what
+# a check finds wrong is put in words (7 us more).
 
 _CACHE = struct.Struct("@5Q6q8i")
 _STRIDES = struct.Struct("@3q")
@@ -530,6 +539,10 @@ def bv_cache_attend(q, k, v, table, lens, n_new=None, scale: Optional[float] = N
     ``table`` int32 [B, width], ``lens`` int32 [B] (the newest tokens counted in), ``n_new`` int32 [B] or None: every sequence
     brings n.  ``scale``: 1/sqrt(D) by default; ``window`` > 0: a token sees its last ``window`` positions and the first ``sinks``.
     Returns ``out`` [B, n, q_heads, D] (rows beyond n_new[b] are not written: zero in a tensor made here)."""
+    if _fast is not None:
+        r = _fast.attend(q, k, v, table, lens, n_new, scale, window, sinks, out, None if stream is None else stream.cuda_stream)
+        if r is not NotImplemented:
+            return r if r.__class__ is not int else _check(r)
     blob, B, _, D, dtype, dev = _cache(k, v, table, lens)
     n, heads, qs = _rows(q, B, 0, D, dtype, dev, "q")
     if out is None:
@@ -546,6 +559,10 @@ def bv_cache_attend(q, k, v, table, lens, n_new=None, scale: Optional[float] = N
 
 def bv_cache_append(k_new, v_new, k, v, table, lens, n_new=None, stream=None) -> None:
     """Stores the keys and values of the newest tokens [B, n, heads, D] in the pages of their positions (see include/bv.h)."""
+    if _fast is not None:
+        r = _fast.append(k_new, v_new, k, v, table, lens, n_new, None if stream is None else stream.cuda_stream)
+        if r is not NotImplemented:
+            return r if r.__class__ is not int else _check(r)
     blob, B, heads, D, dtype, dev = _cache(k, v, table, lens)
     n, _, ks = _rows(k_new, B, heads, D, dtype, dev, "k_new")
     n_v, _, vs = _rows(v_new, B, heads, D, dtype, dev, "v_new")
@@ -569,6 +586,10 @@ def bv_pages_extend(table, lens, refs, page_size: int, n: int, n_new=None, strea
     """Lengthens every sequence by n (or n_new[b] in 0 .. n) tokens, taking the lowest free pages (refs 0) in the sequences' order; table, lens and
     refs change in place.  Returns (new int32 [B]: the tokens, or -1 for a sequence left as it was; copies int32 [B, 2]: the pages that
     bv_pages_copy is to copy, or -1)."""
+    if _fast is not None:
+        r = _fast.extend(table, lens, refs, page_size, n, n_new, None if stream is None else stream.cuda_stream)
+        if r is not NotImplemented:
+            return r if r.__class__ is not int else _check(r)
     blob, B, dev = _book(table, lens, refs, page_size)
     given = None if n_new is None else _counted(n_new, B, dev, "n_new")
     new, copies = table.new_empty((B,)), table.new_empty((B, 2))
@@ -579,6 +600,10 @@ def bv_pages_extend(table, lens, refs, page_size: int, n: int, n_new=None, strea
 def bv_pages_truncate(table, lens, refs, page_size: int, keep, n: int = 0, n_new=None, stream=None) -> None:
     """Keeps the first keep[b] of the n (or n_new[b]) newest tokens of each sequence, with n = 0 of all its tokens, and gives back the pages
     that hold nothing any more.  ``keep`` may be the out_len of a verification."""
+    if _fast is not None:
+        r = _fast.truncate(table, lens, refs, page_size, keep, n, n_new, None if stream is None else stream.cuda_stream)
+        if r is not NotImplemented:
+            return r if r.__class__ is not int else _check(r)
     blob, B, dev = _book(table, lens, refs, page_size)
     kept, given = _counted(keep, B, dev, "keep"), None if n_new is None else _counted(n_new, B, dev, "n_new")
     _enqueue((_lib or load_library()).bv_pages_truncate, dev, stream, blob, kept, given, n)
@@ -586,6 +611,10 @@ def bv_pages_truncate(table, lens, refs, page_size: int, keep, n: int = 0, n_new
 
 def bv_pages_fork(table, lens, refs, page_size: int, src, dst, stream=None):
     """Makes sequence dst[i] a second copy of src[i] on the same pages.  Returns ok int32: 0, or -1 where a fork is refused."""
+    if _fast is not None:
+        r = _fast.fork(table, lens, refs, page_size, src, dst, None if stream is None else stream.cuda_stream)
+        if r is not NotImplemented:
+            return r if r.__class__ is not int else _check(r)
     blob, _, dev = _book(table, lens, refs, page_size)
     forks = src.shape[0] if src.dim() == 1 else -1
     s, d = _counted(src, forks, dev, "src"), _counted(dst, forks, dev, "dst")
@@ -599,6 +628,10 @@ def bv_pages_fork(table, lens, refs, page_size: int, src, dst, stream=None):
 def bv_pages_compact(table, lens, refs, page_size: int, stream=None):
     """Renumbers the pages so that those in use come first.  Returns (moves int32 [num_pages // 2, 2], count int32 [1]), which
     bv_pages_copy takes for each layer before anything else uses the cache."""
+    if _fast is not None:
+        r = _fast.compact(table, lens, refs, page_size, None if stream is None else stream.cuda_stream)
+        if r is not NotImplemented:
+            return r if r.__class__ is not int else _check(r)
     blob, _, dev = _book(table, lens, refs, page_size)
     moves, count = table.new_empty((refs.shape[0] // 2, 2)), table.new_empty((1,))
     # (a pool of one page has no moves, and no place for them)
@@ -608,6 +641,10 @@ def bv_pages_compact(table, lens, refs, page_size: int, stream=None):
 
 def bv_pages_copy(k, v, pairs, count=None, stream=None) -> None:
     """Copies pages, keys and values: pairs int32 [n, 2] of source and destination, of which the first count[0] are looked at."""
+    if _fast is not None:
+        r = _fast.copy(k, v, pairs, count, None if stream is None else stream.cuda_stream)
+        if r is not NotImplemented:
+            return r if r.__class__ is not int else _check(r)
     (P, heads, page, D), ks, vs, code, _, dev = _pools(k, v)
     _written(k, "k")
     _written(v, "v")
