@@ -4,7 +4,7 @@
 // same whatever the order in which its threads run.
 //
 // Taking needs the free pages' ranks: one cluster of up to 8 CTAs reads the counts in as many contiguous regions, the regions' sums
-// cross through distributed shared memory, and a second look at the counts hands out the pages.  (One CTA reads some 60 bytes a
+// cross through distributed shared memory, and a second look at the counts (the first 65536 of them kept in registers) hands out the pages.  (One CTA reads some 60 bytes a
 // clock: 100000 counts would take it 4 us twice, a cluster has them in one round of loads per CTA.)
 #include <cooperative_groups.h>
 
@@ -48,29 +48,55 @@ __device__ __forceinline__ unsigned zero_bits(const int32_t* refs, int first, in
     return bits;
 }
 struct ScanSmem {
-    int warp[kThreads / 32];
-    int pad;
+    int2 warp[kThreads / 32];
 };
-// Sum over the CTA, and what lies before this thread.
-__device__ __forceinline__ int scan(ScanSmem& sm, int mine, int* total) {
+// Two sums over the CTA at once, and what lies before this thread.
+__device__ __forceinline__ int2 scan(ScanSmem& sm, int2 mine, int2* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int upto = mine;
+    int2 upto = mine;
+#pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += x;
+        const int x = __shfl_up_sync(0xffffffffu, upto.x, o), y = __shfl_up_sync(0xffffffffu, upto.y, o);
+        if (lane >= o) {
+            upto.x += x;
+            upto.y += y;
+        }
     }
     __syncthreads();                          // (the last scan's readers)
     if (lane == 31) sm.warp[warp] = upto;
     __syncthreads();
-    int before = 0, all = 0;
+    int2 before{0, 0}, all{0, 0};
 #pragma unroll
     for (int w = 0; w < kThreads / 32; ++w) {
-        const int x = sm.warp[w];
-        before += w < warp ? x : 0;
-        all += x;
+        const int2 x = sm.warp[w];
+        before.x += w < warp ? x.x : 0;
+        before.y += w < warp ? x.y : 0;
+        all.x += x.x;
+        all.y += x.y;
     }
     *total = all;
-    return before + upto - mine;
+    return make_int2(before.x + upto.x - mine.x, before.y + upto.y - mine.y);
+}
+__device__ __forceinline__ int scan(ScanSmem& sm, int mine, int* total) {
+    int2 all;
+    const int2 before = scan(sm, make_int2(mine, 0), &all);
+    *total = all.x;
+    return before.x;
+}
+// All CTAs of the cluster have come here; a number of each, added up: what lies before this CTA, and all.
+__device__ __forceinline__ void come_together(cg::cluster_group& cluster, int ctas) {
+    if (ctas > 1) cluster.sync(); else __syncthreads();
+}
+__device__ __forceinline__ int2 across(cg::cluster_group& cluster, int* mine, int rank, int ctas) {
+    int x[8], before = 0, all = 0;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) x[r] = r < ctas ? *cluster.map_shared_rank(mine, r) : 0;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        before += r < rank ? x[r] : 0;
+        all += x[r];
+    }
+    return make_int2(before, all);
 }
 
 // A CTA's region of the counts: whole rounds of 16 but for the last.
@@ -120,41 +146,40 @@ __global__ void __launch_bounds__(kThreads, 1) extend_pages_kernel(const PagesAr
     int begin, end;
     region(a.num_pages, rank, ctas, &begin, &end);
 
-    // free pages of the region
-    int mine = 0, total;
-    for (int p = begin + tid * kEach; p < end; p += kRound) mine += __popc(zero_bits(a.refs, p, end, vec));
-    scan(sm.scan, mine, &total);
-    if (tid == 0) sm.free = total;
-    // what every sequence needs, summed up in their order (every CTA for itself: the pages it finds may be anybody's)
+    // The free pages of the region and what the sequences need, in their order (every CTA for itself: the pages it finds may be anybody's).
+    // The first round's loads, of counts and of sequences, are under way together; its counts are kept for the second look.
+    const int p0 = begin + tid * kEach;
+    const unsigned bits0 = p0 < end ? zero_bits(a.refs, p0, end, vec) : 0u;
+    int info = -1, want = tid < a.B ? need_of(a, tid, &info) : 0, mine = __popc(bits0);
+    for (int p = p0 + kRound; p < end; p += kRound) mine += __popc(zero_bits(a.refs, p, end, vec));
+    int2 all;                                 // (512 numbers of at most kMost + 1 each stay within 32 bits)
+    int2 ahead = scan(sm.scan, make_int2(mine, want), &all);
+    if (tid == 0) sm.free = all.x;
     int sum = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-        const int b = b0 + tid;
-        int info = -1;
-        const int want = b < a.B ? need_of(a, b, &info) : 0;
-        int all;                              // (512 numbers of at most kMost + 1 each stay within 32 bits)
-        const int before = scan(sm.scan, want, &all);
+    for (int b = tid, b0 = 0;;) {
         if (b < a.B) {
-            sm.upto[b] = min(sum + before + want, a.num_pages + 1);
+            sm.upto[b] = min(sum + ahead.y + want, a.num_pages + 1);
             sm.info[b] = info;
         }
-        sum = min(sum + all, a.num_pages + 1);
+        sum = min(sum + all.y, a.num_pages + 1);
+        b0 += kThreads;
+        b += kThreads;
+        if (b0 >= a.B) break;
+        want = b < a.B ? need_of(a, b, &info) : 0;
+        ahead = scan(sm.scan, make_int2(0, want), &all);
     }
-    cluster.sync();                           // everything that decides has been read, and nothing changed so far
-    int before = 0, free = 0;
-    for (int r = 0; r < ctas; ++r) {
-        const int f = *cluster.map_shared_rank(&sm.free, r);
-        if (r < rank) before += f;
-        free += f;
-    }
+    come_together(cluster, ctas);             // everything that decides has been read, and nothing changed so far
+    const int2 cut = across(cluster, &sm.free, rank, ctas);
+    const int free = cut.y;
     // the region's free pages, by rank, to the sequences
     const int wanted = min(sum, free);
-    int at = before;
-    for (int p0 = begin; p0 < end && at < wanted; p0 += kRound) {
-        const int p = p0 + tid * kEach;
-        unsigned bits = p < end ? zero_bits(a.refs, p, end, vec) : 0u;
-        int all;
-        int f = at + scan(sm.scan, __popc(bits), &all);
-        at += all;
+    int at = cut.x;
+    for (int first = begin; first < end && at < wanted; first += kRound) {
+        const int p = first + tid * kEach;
+        unsigned bits = first == begin ? bits0 : p < end ? zero_bits(a.refs, p, end, vec) : 0u;
+        int some;
+        int f = at + scan(sm.scan, __popc(bits), &some);
+        at += some;
         for (; bits && f < wanted; bits &= bits - 1, ++f) {
             const int page = p + __ffs(bits) - 1;
             int lo = 0, hi = a.B - 1;         // the first sequence whose sum is above f
@@ -163,9 +188,9 @@ __global__ void __launch_bounds__(kThreads, 1) extend_pages_kernel(const PagesAr
                 if (sm.upto[mid] > f) hi = mid; else lo = mid + 1;
             }
             if (sm.upto[lo] > free) continue; // it is not served, nor is any after it
-            const int slot = f - (lo > 0 ? sm.upto[lo - 1] : 0), info = sm.info[lo];
-            int32_t* entry = a.table + static_cast<long long>(lo) * a.width + info / kFirst + slot;
-            if (slot == 0 && (info & kReplace)) {
+            const int slot = f - (lo > 0 ? sm.upto[lo - 1] : 0), asked = sm.info[lo];
+            int32_t* entry = a.table + static_cast<long long>(lo) * a.width + asked / kFirst + slot;
+            if (slot == 0 && (asked & kReplace)) {
                 out_copies[2 * lo] = *entry;
                 out_copies[2 * lo + 1] = page;
             }
@@ -174,13 +199,13 @@ __global__ void __launch_bounds__(kThreads, 1) extend_pages_kernel(const PagesAr
         }
     }
     __threadfence();
-    cluster.sync();
+    come_together(cluster, ctas);
     // lengths, what was served, and the counts of the pages that were replaced (only now: one that comes to 0 is free for the next call)
     for (int b = rank * kThreads + tid; b < a.B; b += ctas * kThreads) {
-        const int info = sm.info[b];
-        const bool ok = info >= 0 && (!(info & kNeeds) || sm.upto[b] <= free);
+        const int asked = sm.info[b];
+        const bool ok = asked >= 0 && (!(asked & kNeeds) || sm.upto[b] <= free);
         const int m = a.n_new ? __ldg(a.n_new + b) : a.n;
-        if (ok && (info & kReplace)) atomicSub(a.refs + __ldcg(out_copies + 2 * b), 1);
+        if (ok && (asked & kReplace)) atomicSub(a.refs + __ldcg(out_copies + 2 * b), 1);
         else out_copies[2 * b] = out_copies[2 * b + 1] = -1;
         out_new[b] = ok ? m : -1;
         if (ok) a.lens[b] += m;
@@ -263,53 +288,54 @@ __global__ void __launch_bounds__(kThreads, 1) compact_pages_kernel(const PagesA
     const int rank = static_cast<int>(cluster.block_rank()), ctas = static_cast<int>(cluster.num_blocks()), tid = threadIdx.x;
     int begin, end;
     region(a.num_pages, rank, ctas, &begin, &end);
-    int mine = 0, all;
-    for (int p = begin + tid * kEach; p < end; p += kRound) mine += min(end - p, kEach) - __popc(zero_bits(a.refs, p, end, vec));
-    scan(sm.scan, mine, &all);
-    if (tid == 0) sm.used = all;
-    cluster.sync();
-    int live = 0;
-    for (int r = 0; r < ctas; ++r) live += *cluster.map_shared_rank(&sm.used, r);
+    // (the first round's counts are kept)
+    const int p0 = begin + tid * kEach;
+    const unsigned zero0 = p0 < end ? zero_bits(a.refs, p0, end, vec) : 0u;
+    auto zeros = [&](int p) { return p == p0 ? zero0 : zero_bits(a.refs, p, end, vec); };
+    int mine = 0, some;
+    for (int p = p0; p < end; p += kRound) mine += min(end - p, kEach) - __popc(zeros(p));
+    scan(sm.scan, mine, &some);
+    if (tid == 0) sm.used = some;
+    come_together(cluster, ctas);
+    const int live = across(cluster, &sm.used, rank, ctas).y;
     // free pages before `live`, pages in use from there on, as bits
     auto look = [&](int p, unsigned* holes, unsigned* sources) {
         *holes = *sources = 0;
         if (p >= end) return;
-        const unsigned zero = zero_bits(a.refs, p, end, vec), there = end - p >= kEach ? 0xffffu : (1u << (end - p)) - 1;
+        const unsigned zero = zeros(p), there = end - p >= kEach ? 0xffffu : (1u << (end - p)) - 1;
         const unsigned before = live - p >= kEach ? 0xffffu : live <= p ? 0u : (1u << (live - p)) - 1;
         *holes = zero & before;
         *sources = ~zero & there & ~before;
     };
-    int h = 0, s = 0;
-    for (int p = begin + tid * kEach; p < end; p += kRound) {
+    int2 found{0, 0}, all;
+    for (int p = p0; p < end; p += kRound) {
         unsigned hb, sb;
         look(p, &hb, &sb);
-        h += __popc(hb);
-        s += __popc(sb);
+        found.x += __popc(hb);
+        found.y += __popc(sb);
     }
-    scan(sm.scan, h, &all);
-    if (tid == 0) sm.holes = all;
-    scan(sm.scan, s, &all);
-    if (tid == 0) sm.sources = all;
-    cluster.sync();
-    int hole_at = 0, source_at = 0, count = 0;
-    for (int r = 0; r < ctas; ++r) {
-        const int x = *cluster.map_shared_rank(&sm.holes, r), y = *cluster.map_shared_rank(&sm.sources, r);
-        if (r < rank) { hole_at += x; source_at += y; }
-        count += y;
+    scan(sm.scan, found, &all);
+    if (tid == 0) {
+        sm.holes = all.x;
+        sm.sources = all.y;
     }
-    for (int p0 = begin; p0 < end; p0 += kRound) {
-        const int p = p0 + tid * kEach;
+    come_together(cluster, ctas);
+    const int2 holes = across(cluster, &sm.holes, rank, ctas), sources = across(cluster, &sm.sources, rank, ctas);
+    int hole_at = holes.x, source_at = sources.x;
+    const int count = sources.y;
+    for (int first = begin; first < end; first += kRound) {
+        const int p = first + tid * kEach;
         unsigned hb, sb;
         look(p, &hb, &sb);
-        int f = hole_at + scan(sm.scan, __popc(hb), &all);
-        hole_at += all;
-        int g = source_at + scan(sm.scan, __popc(sb), &all);
-        source_at += all;
+        const int2 ahead = scan(sm.scan, make_int2(__popc(hb), __popc(sb)), &all);
+        int f = hole_at + ahead.x, g = source_at + ahead.y;
+        hole_at += all.x;
+        source_at += all.y;
         for (; hb; hb &= hb - 1) moves[2 * f++ + 1] = p + __ffs(hb) - 1;
         for (; sb; sb &= sb - 1) moves[2 * g++] = p + __ffs(sb) - 1;
     }
     __threadfence();
-    cluster.sync();
+    come_together(cluster, ctas);
     for (int i = rank * kThreads + tid; i < a.num_pages / 2; i += ctas * kThreads) {
         if (i >= count) {
             moves[2 * i] = moves[2 * i + 1] = -1;
@@ -324,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) compact_pages_kernel(const PagesA
         *out_count = count;
         to[a.num_pages] = live;
     }
-    cluster.sync();                           // (the others' shared memory is read above)
+    come_together(cluster, ctas);             // (the others' shared memory is read above)
 }
 // Gives the pages of all tables their new numbers.
 __global__ void __launch_bounds__(256) rename_pages_kernel(const PagesArgs a, const int32_t* to) {
