@@ -460,15 +460,23 @@ _I32 = torch.int32
 _CODES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
 
 
-def _enqueue(fn, dev: int, stream, *args) -> None:
-    """Calls an entry point with device ``dev`` current (it nearly always is) and the stream as its last argument."""
+def _enqueue(fn, dev: int, *args) -> None:
+    """Calls an entry point with device ``dev`` current (it nearly always is) and its current stream as the last argument."""
     if torch._C._cuda_getDevice() == dev:
-        status = fn(*args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     else:
         with torch.cuda.device(dev):
-            status = fn(*args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     if status:
         _check(status)
+
+
+def _on_stream(stream, of, fn, *args):
+    """A call on a stream that is given: what it allocates and fills belongs to that stream too."""
+    if stream.device != of.device:
+        raise ValueError("the stream must be one of the cache's device")
+    with torch.cuda.stream(stream):
+        return fn(*args)
 
 
 def _pools(k, v):
@@ -539,8 +547,10 @@ def bv_cache_attend(q, k, v, table, lens, n_new=None, scale: Optional[float] = N
     ``table`` int32 [B, width], ``lens`` int32 [B] (the newest tokens counted in), ``n_new`` int32 [B] or None: every sequence
     brings n.  ``scale``: 1/sqrt(D) by default; ``window`` > 0: a token sees its last ``window`` positions and the first ``sinks``.
     Returns ``out`` [B, n, q_heads, D] (rows beyond n_new[b] are not written: zero in a tensor made here)."""
+    if stream is not None:
+        return _on_stream(stream, lens, bv_cache_attend, q, k, v, table, lens, n_new, scale, window, sinks, out)
     if _fast is not None:
-        r = _fast.attend(q, k, v, table, lens, n_new, scale, window, sinks, out, None if stream is None else stream.cuda_stream)
+        r = _fast.attend(q, k, v, table, lens, n_new, scale, window, sinks, out)
         if r is not NotImplemented:
             return r if r.__class__ is not int else _check(r)
     blob, B, _, D, dtype, dev = _cache(k, v, table, lens)
@@ -553,14 +563,16 @@ def bv_cache_attend(q, k, v, table, lens, n_new=None, scale: Optional[float] = N
     if n_out != n:
         raise ValueError("out must have the shape of q")
     new = None if n_new is None else _counted(n_new, B, dev, "n_new")
-    _enqueue((_lib or load_library()).bv_cache_attend, dev, stream, blob, q.data_ptr(), qs, new, n, heads, D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), os_)
+    _enqueue((_lib or load_library()).bv_cache_attend, dev, blob, q.data_ptr(), qs, new, n, heads, D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), os_)
     return out
 
 
 def bv_cache_append(k_new, v_new, k, v, table, lens, n_new=None, stream=None) -> None:
     """Stores the keys and values of the newest tokens [B, n, heads, D] in the pages of their positions (see include/bv.h)."""
+    if stream is not None:
+        return _on_stream(stream, lens, bv_cache_append, k_new, v_new, k, v, table, lens, n_new)
     if _fast is not None:
-        r = _fast.append(k_new, v_new, k, v, table, lens, n_new, None if stream is None else stream.cuda_stream)
+        r = _fast.append(k_new, v_new, k, v, table, lens, n_new)
         if r is not NotImplemented:
             return r if r.__class__ is not int else _check(r)
     blob, B, heads, D, dtype, dev = _cache(k, v, table, lens)
@@ -571,7 +583,7 @@ def bv_cache_append(k_new, v_new, k, v, table, lens, n_new=None, stream=None) ->
     _written(k, "k")
     _written(v, "v")
     new = None if n_new is None else _counted(n_new, B, dev, "n_new")
-    _enqueue((_lib or load_library()).bv_cache_append, dev, stream, blob, k_new.data_ptr(), ks, v_new.data_ptr(), vs, new, n)
+    _enqueue((_lib or load_library()).bv_cache_append, dev, blob, k_new.data_ptr(), ks, v_new.data_ptr(), vs, new, n)
 
 
 def _book(table, lens, refs, page_size: int):
@@ -586,33 +598,39 @@ def bv_pages_extend(table, lens, refs, page_size: int, n: int, n_new=None, strea
     """Lengthens every sequence by n (or n_new[b] in 0 .. n) tokens, taking the lowest free pages (refs 0) in the sequences' order; table, lens and
     refs change in place.  Returns (new int32 [B]: the tokens, or -1 for a sequence left as it was; copies int32 [B, 2]: the pages that
     bv_pages_copy is to copy, or -1)."""
+    if stream is not None:
+        return _on_stream(stream, lens, bv_pages_extend, table, lens, refs, page_size, n, n_new)
     if _fast is not None:
-        r = _fast.extend(table, lens, refs, page_size, n, n_new, None if stream is None else stream.cuda_stream)
+        r = _fast.extend(table, lens, refs, page_size, n, n_new)
         if r is not NotImplemented:
             return r if r.__class__ is not int else _check(r)
     blob, B, dev = _book(table, lens, refs, page_size)
     given = None if n_new is None else _counted(n_new, B, dev, "n_new")
     new, copies = table.new_empty((B,)), table.new_empty((B, 2))
-    _enqueue((_lib or load_library()).bv_pages_extend, dev, stream, blob, given, n, new.data_ptr(), copies.data_ptr())
+    _enqueue((_lib or load_library()).bv_pages_extend, dev, blob, given, n, new.data_ptr(), copies.data_ptr())
     return new, copies
 
 
 def bv_pages_truncate(table, lens, refs, page_size: int, keep, n: int = 0, n_new=None, stream=None) -> None:
     """Keeps the first keep[b] of the n (or n_new[b]) newest tokens of each sequence, with n = 0 of all its tokens, and gives back the pages
     that hold nothing any more.  ``keep`` may be the out_len of a verification."""
+    if stream is not None:
+        return _on_stream(stream, lens, bv_pages_truncate, table, lens, refs, page_size, keep, n, n_new)
     if _fast is not None:
-        r = _fast.truncate(table, lens, refs, page_size, keep, n, n_new, None if stream is None else stream.cuda_stream)
+        r = _fast.truncate(table, lens, refs, page_size, keep, n, n_new)
         if r is not NotImplemented:
             return r if r.__class__ is not int else _check(r)
     blob, B, dev = _book(table, lens, refs, page_size)
     kept, given = _counted(keep, B, dev, "keep"), None if n_new is None else _counted(n_new, B, dev, "n_new")
-    _enqueue((_lib or load_library()).bv_pages_truncate, dev, stream, blob, kept, given, n)
+    _enqueue((_lib or load_library()).bv_pages_truncate, dev, blob, kept, given, n)
 
 
 def bv_pages_fork(table, lens, refs, page_size: int, src, dst, stream=None):
     """Makes sequence dst[i] a second copy of src[i] on the same pages.  Returns ok int32: 0, or -1 where a fork is refused."""
+    if stream is not None:
+        return _on_stream(stream, lens, bv_pages_fork, table, lens, refs, page_size, src, dst)
     if _fast is not None:
-        r = _fast.fork(table, lens, refs, page_size, src, dst, None if stream is None else stream.cuda_stream)
+        r = _fast.fork(table, lens, refs, page_size, src, dst)
         if r is not NotImplemented:
             return r if r.__class__ is not int else _check(r)
     blob, _, dev = _book(table, lens, refs, page_size)
@@ -621,28 +639,32 @@ def bv_pages_fork(table, lens, refs, page_size: int, src, dst, stream=None):
     ok = table.new_empty((forks,))
     if forks == 0:
         return ok
-    _enqueue((_lib or load_library()).bv_pages_fork, dev, stream, blob, s, d, forks, ok.data_ptr())
+    _enqueue((_lib or load_library()).bv_pages_fork, dev, blob, s, d, forks, ok.data_ptr())
     return ok
 
 
 def bv_pages_compact(table, lens, refs, page_size: int, stream=None):
     """Renumbers the pages so that those in use come first.  Returns (moves int32 [num_pages // 2, 2], count int32 [1]), which
     bv_pages_copy takes for each layer before anything else uses the cache."""
+    if stream is not None:
+        return _on_stream(stream, lens, bv_pages_compact, table, lens, refs, page_size)
     if _fast is not None:
-        r = _fast.compact(table, lens, refs, page_size, None if stream is None else stream.cuda_stream)
+        r = _fast.compact(table, lens, refs, page_size)
         if r is not NotImplemented:
             return r if r.__class__ is not int else _check(r)
     blob, _, dev = _book(table, lens, refs, page_size)
     moves, count = table.new_empty((refs.shape[0] // 2, 2)), table.new_empty((1,))
     # (a pool of one page has no moves, and no place for them)
-    _enqueue((_lib or load_library()).bv_pages_compact, dev, stream, blob, moves.data_ptr() or count.data_ptr(), count.data_ptr())
+    _enqueue((_lib or load_library()).bv_pages_compact, dev, blob, moves.data_ptr() or count.data_ptr(), count.data_ptr())
     return moves, count
 
 
 def bv_pages_copy(k, v, pairs, count=None, stream=None) -> None:
     """Copies pages, keys and values: pairs int32 [n, 2] of source and destination, of which the first count[0] are looked at."""
+    if stream is not None:
+        return _on_stream(stream, k, bv_pages_copy, k, v, pairs, count)
     if _fast is not None:
-        r = _fast.copy(k, v, pairs, count, None if stream is None else stream.cuda_stream)
+        r = _fast.copy(k, v, pairs, count)
         if r is not NotImplemented:
             return r if r.__class__ is not int else _check(r)
     (P, heads, page, D), ks, vs, code, _, dev = _pools(k, v)
@@ -657,4 +679,4 @@ def bv_pages_copy(k, v, pairs, count=None, stream=None) -> None:
     if shape[0] == 0:
         return
     blob = _CACHE.pack(k.data_ptr(), v.data_ptr(), 0, 0, 0, ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], 0, 0, P, page, heads, D, code, 0)
-    _enqueue((_lib or load_library()).bv_pages_copy, dev, stream, blob, pairs.data_ptr(), shape[0], upto)
+    _enqueue((_lib or load_library()).bv_pages_copy, dev, blob, pairs.data_ptr(), shape[0], upto)

@@ -29,18 +29,11 @@ PyObject* other() { Py_RETURN_NOTIMPLEMENTED; }
 const at::Tensor* tensor(PyObject* o) { return THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr; }
 template <typename T> T* address(const at::Tensor& t) { return static_cast<T*>(t.data_ptr()); }
 
-// The stream of a call on `dev`: the address given, or torch's current one; false if another device is current.
-bool stream_of(PyObject* given, int dev, void** s) {
+// torch's current stream on `dev`; false if another device is current.
+bool stream_of(int dev, void** s) {
     if (c10::cuda::current_device() != dev) return false;
-    if (given == Py_None) {
-        *s = c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(dev)).stream();
-        return true;
-    }
-    if (!PyLong_Check(given)) return false;
-    *s = PyLong_AsVoidPtr(given);
-    if (!PyErr_Occurred()) return true;
-    PyErr_Clear();
-    return false;
+    *s = c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(dev)).stream();
+    return true;
 }
 // A contiguous int32 [n] on `dev`, or None if that may be.
 bool counted(PyObject* o, int64_t n, int dev, bool none, int32_t** p) {
@@ -137,9 +130,9 @@ template <typename F> int released(F f) {
     return status;
 }
 
-// q, k, v, table, lens, n_new, scale, window, sinks, out, stream
+// q, k, v, table, lens, n_new, scale, window, sinks, out
 PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 11 || !f_attend) return other();
+    if (n != 10 || !f_attend) return other();
     return guarded([&]() -> PyObject* {
         bv_cache c{};
         int dev, at, window, sinks;
@@ -148,7 +141,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int64_t qs[3], os[3];
         const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]), *v = tensor(a[2]);
         if (!pools(k, v, false, &c, &dev) || !sequences(a[3], a[4], &c, &at) || at != dev || !rows(q, c, *k, 0, dev, qs) || !counted(a[5], c.B, dev, true, &n_new) ||
-            !whole(a[7], &window) || !whole(a[8], &sinks) || !stream_of(a[10], dev, &s)) return other();
+            !whole(a[7], &window) || !whole(a[8], &sinks) || !stream_of(dev, &s)) return other();
         double scale = 1.0 / std::sqrt(static_cast<double>(c.D));
         if (a[6] != Py_None) {
             if (!PyFloat_Check(a[6])) return other();
@@ -171,9 +164,9 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return a[9] == Py_None ? THPVariable_Wrap(made) : Py_NewRef(a[9]);
     });
 }
-// k_new, v_new, k, v, table, lens, n_new, stream
+// k_new, v_new, k, v, table, lens, n_new
 PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 8 || !f_append) return other();
+    if (n != 7 || !f_append) return other();
     return guarded([&]() -> PyObject* {
         bv_cache c{};
         int dev, at;
@@ -182,19 +175,19 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int64_t ks[3], vs[3];
         const at::Tensor *kn = tensor(a[0]), *vn = tensor(a[1]), *k = tensor(a[2]), *v = tensor(a[3]);
         if (!pools(k, v, true, &c, &dev) || !sequences(a[4], a[5], &c, &at) || at != dev || !rows(kn, c, *k, c.heads, dev, ks) || !rows(vn, c, *k, c.heads, dev, vs) ||
-            vn->size(1) != kn->size(1) || !counted(a[6], c.B, dev, true, &n_new) || !stream_of(a[7], dev, &s)) return other();
+            vn->size(1) != kn->size(1) || !counted(a[6], c.B, dev, true, &n_new) || !stream_of(dev, &s)) return other();
         return answer(released([&] { return f_append(&c, kn->data_ptr(), ks, vn->data_ptr(), vs, n_new, static_cast<int>(kn->size(1)), s); }), none());
     });
 }
-// table, lens, refs, page_size, n, n_new, stream
+// table, lens, refs, page_size, n, n_new
 PyObject* extend(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 7 || !f_extend) return other();
+    if (n != 6 || !f_extend) return other();
     return guarded([&]() -> PyObject* {
         bv_cache c{};
         int dev, most;
         void* s;
         int32_t* n_new;
-        if (!book(a[0], a[1], a[2], a[3], &c, &dev) || !whole(a[4], &most) || !counted(a[5], c.B, dev, true, &n_new) || !stream_of(a[6], dev, &s)) return other();
+        if (!book(a[0], a[1], a[2], a[3], &c, &dev) || !whole(a[4], &most) || !counted(a[5], c.B, dev, true, &n_new) || !stream_of(dev, &s)) return other();
         const auto options = tensor(a[0])->options();
         const at::Tensor got = at::empty({c.B}, options), copies = at::empty({c.B, 2}, options);
         const int status = released([&] { return f_extend(&c, n_new, most, address<int32_t>(got), address<int32_t>(copies), s); });
@@ -206,22 +199,22 @@ PyObject* extend(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return both;
     });
 }
-// table, lens, refs, page_size, keep, n, n_new, stream
+// table, lens, refs, page_size, keep, n, n_new
 PyObject* truncate(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 8 || !f_truncate) return other();
+    if (n != 7 || !f_truncate) return other();
     return guarded([&]() -> PyObject* {
         bv_cache c{};
         int dev, most;
         void* s;
         int32_t *keep, *n_new;
         if (!book(a[0], a[1], a[2], a[3], &c, &dev) || !counted(a[4], c.B, dev, false, &keep) || !whole(a[5], &most) || !counted(a[6], c.B, dev, true, &n_new) ||
-            !stream_of(a[7], dev, &s)) return other();
+            !stream_of(dev, &s)) return other();
         return answer(released([&] { return f_truncate(&c, keep, n_new, most, s); }), none());
     });
 }
-// table, lens, refs, page_size, src, dst, stream
+// table, lens, refs, page_size, src, dst
 PyObject* fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 7 || !f_fork) return other();
+    if (n != 6 || !f_fork) return other();
     return guarded([&]() -> PyObject* {
         bv_cache c{};
         int dev;
@@ -230,20 +223,20 @@ PyObject* fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor* first = tensor(a[4]);
         if (!first || first->dim() != 1 || first->size(0) < 1 || first->size(0) > INT32_MAX) return other();
         const int forks = static_cast<int>(first->size(0));
-        if (!book(a[0], a[1], a[2], a[3], &c, &dev) || !counted(a[4], forks, dev, false, &src) || !counted(a[5], forks, dev, false, &dst) || !stream_of(a[6], dev, &s)) return other();
+        if (!book(a[0], a[1], a[2], a[3], &c, &dev) || !counted(a[4], forks, dev, false, &src) || !counted(a[5], forks, dev, false, &dst) || !stream_of(dev, &s)) return other();
         const at::Tensor ok = at::empty({forks}, tensor(a[0])->options());
         const int status = released([&] { return f_fork(&c, src, dst, forks, address<int32_t>(ok), s); });
         return status ? PyLong_FromLong(status) : THPVariable_Wrap(ok);
     });
 }
-// table, lens, refs, page_size, stream
+// table, lens, refs, page_size
 PyObject* compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 5 || !f_compact) return other();
+    if (n != 4 || !f_compact) return other();
     return guarded([&]() -> PyObject* {
         bv_cache c{};
         int dev;
         void* s;
-        if (!book(a[0], a[1], a[2], a[3], &c, &dev) || c.num_pages < 2 || !stream_of(a[4], dev, &s)) return other();
+        if (!book(a[0], a[1], a[2], a[3], &c, &dev) || c.num_pages < 2 || !stream_of(dev, &s)) return other();
         const auto options = tensor(a[0])->options();
         const at::Tensor moves = at::empty({c.num_pages / 2, 2}, options), count = at::empty({1}, options);
         const int status = released([&] { return f_compact(&c, address<int32_t>(moves), address<int32_t>(count), s); });
@@ -255,9 +248,9 @@ PyObject* compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return both;
     });
 }
-// k, v, pairs, count, stream
+// k, v, pairs, count
 PyObject* copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 5 || !f_copy) return other();
+    if (n != 4 || !f_copy) return other();
     return guarded([&]() -> PyObject* {
         bv_cache c{};
         int dev;
@@ -265,7 +258,7 @@ PyObject* copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int32_t* count;
         const at::Tensor* pairs = tensor(a[2]);
         if (!pools(tensor(a[0]), tensor(a[1]), true, &c, &dev) || !pairs || pairs->scalar_type() != at::kInt || pairs->dim() != 2 || pairs->size(1) != 2 || pairs->size(0) < 1 ||
-            pairs->size(0) > INT32_MAX || !pairs->is_contiguous() || !pairs->is_cuda() || pairs->get_device() != dev || !counted(a[3], 1, dev, true, &count) || !stream_of(a[4], dev, &s))
+            pairs->size(0) > INT32_MAX || !pairs->is_contiguous() || !pairs->is_cuda() || pairs->get_device() != dev || !counted(a[3], 1, dev, true, &count) || !stream_of(dev, &s))
             return other();
         return answer(released([&] { return f_copy(&c, address<int32_t>(*pairs), static_cast<int>(pairs->size(0)), count, s); }), none());
     });

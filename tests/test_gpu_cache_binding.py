@@ -90,3 +90,19 @@ def test_another_stream(way):
         again = bv.bv_cache_attend(c.q, c.k, c.v, c.table, c.lens)
     torch.cuda.synchronize()
     assert torch.equal(got, want) and torch.equal(again, want)
+
+
+def test_what_is_made_for_a_call_belongs_to_its_stream(way):
+    """The current stream is busy: neither the zeros of rows that a sequence does not bring, nor what lies in the memory before, may come after the result."""
+    c = cp.make(2, 3, 4, 2, 64, 16, [33, 160], spare=20, width=16)
+    new = torch.tensor([2, 3], dtype=torch.int32, device="cuda")
+    want = bv.bv_cache_attend(c.q, c.k, c.v, c.table, c.lens, n_new=new)
+    table, lens, refs = (x.clone() for x in (c.table, c.lens, c.refs))
+    want_new, want_copies = bv.bv_pages_extend(table, lens, refs, 16, 3)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(40_000_000)                                                       # some 20 ms
+    got = bv.bv_cache_attend(c.q, c.k, c.v, c.table, c.lens, n_new=new, stream=s)
+    got_new, got_copies = bv.bv_pages_extend(c.table, c.lens, c.refs, 16, 3, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(got_new, want_new) and torch.equal(got_copies, want_copies)
