@@ -89,7 +89,7 @@ __device__ __forceinline__ void put(const AttendArgs& a, const Walk& w, float* p
         T* const to = static_cast<T*>(a.out) + w.b * a.os[0] + t * a.os[1] + (w.h * a.group + r - t * a.group) * a.os[2] + d;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (d + e < a.D) to[e] = from_float<T>(l == 0.f ? 0.f : o[e] / l);
+            if (d + e < a.D) to[e] = from_float<T>(l == 0.f ? of_nothing(a, w.s, r) : o[e] / l);
     }
 }
 

@@ -657,7 +657,7 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                     part[member] = -ts.nref[member];
                     part[a.rows + member] = sum;
                 }
-                ts.part[0][member] = sum == 0.f ? 0.f : 1.f / sum;
+                ts.part[0][member] = sum == 0.f ? of_nothing(a, w.s, w.r0 + member) : 1.f / sum;
             }
             team_sync<kTeam>(bar);
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + w.b * a.os[0] + w.h * a.group * a.os[2] + dim;

@@ -87,6 +87,8 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int b) {
     s.rows = m * a.group;
     return s;
 }
+// What a row with the sum 0 gets: 0 where it sees nothing (its position is below 0), else 0 / 0 as the formula has it (all its scores are -inf).
+__device__ __forceinline__ float of_nothing(const AttendArgs& a, const Seq& s, int row) { return s.base + a.by_group(row) < 0 ? 0.f : NAN; }
 // The lowest position that a token at `pos` sees through its window.
 __device__ __forceinline__ int low_of(const AttendArgs& a, int pos) {
     if (a.window <= 0) return 0;
@@ -386,9 +388,9 @@ __device__ __forceinline__ void join_share(const AttendArgs& a, const Joint& u, 
         if (mine && sub == 0) {
             const int r = u.r0 + row, t = a.by_group(r);
             T* dst = static_cast<T*>(a.out) + u.b * a.os[0] + t * a.os[1] + (u.h * a.group + r - t * a.group) * a.os[2] + d;
-            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const float none = l == 0.f ? of_nothing(a, seq_of(a, u.b), r) : 0.f, inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-            for (int i = 0; i < W; ++i) dst[i] = from_float<T>(l == 0.f ? 0.f : o[i] * inv);
+            for (int i = 0; i < W; ++i) dst[i] = from_float<T>(l == 0.f ? none : o[i] * inv);
         }
     }
 }

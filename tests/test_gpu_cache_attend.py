@@ -169,6 +169,24 @@ def test_scores_far_apart(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,Hq,D", [(1, 2, 64), (3, 4, 64), (9, 16, 128), (2, 2, 33)])
+def test_a_row_of_scores_of_minus_infinity(dtype, n, Hq, D):
+    """Such a score weighs nothing beside others; a row of nothing else is 0 / 0."""
+    c = cp.make(3, n, Hq, 1, D, 16, [40, 900, n], dtype=dtype, seed=18)
+    c.q[..., 0] = 1.0
+    clean = bv.bv_cache_attend(c.q, c.k, c.v, c.table, c.lens).clone()
+    c.k[..., 0] = -math.inf
+    assert torch.isnan(bv.bv_cache_attend(c.q, c.k, c.v, c.table, c.lens)).all()
+    # one key of the last sequence's that is not: the rows that see it have its value, those before it do not
+    at = (c.table[2, (n - 1) // 16].item(), slice(None), (n - 1) % 16, 0)
+    c.k[at] = 1.0
+    got = bv.bv_cache_attend(c.q, c.k, c.v, c.table, c.lens)
+    assert torch.isnan(got[:2]).all() and torch.isnan(got[2, :n - 1]).all()
+    assert torch.equal(got[2, n - 1], c.v[c.table[2, (n - 1) // 16].item(), 0, (n - 1) % 16].expand(Hq, D))
+    assert not torch.isnan(clean).any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_strides_and_alignment(dtype):
     c = cp.make(3, 3, 4, 2, 64, 16, [50, 300, 129], dtype=dtype, seed=13)
     ref = bv.bv_cache_attend(c.q, c.k, c.v, c.table, c.lens)
