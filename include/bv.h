@@ -360,7 +360,7 @@ typedef struct bv_cache {
     void* k;               /* [num_pages, heads, page_size, D]  dtype, at k_stride between pages, heads, tokens */
     void* v;               /* the same, at v_stride                                                             */
     int32_t* table;        /* [B, width]  page numbers; entries at and beyond ceil(lens[b] / page_size) are not read */
-    int32_t* lens;         /* [B]         0 .. width page_size; anything else is a data fault of the sequence    */
+    int32_t* lens;         /* [B]         0 .. width page_size, 2^31 - 1024 at most; anything else is a data fault of the sequence */
     int32_t* refs;         /* [num_pages] table entries that name the page (bv_pages_* but bv_pages_copy)        */
     int64_t k_stride[3], v_stride[3];
     int32_t B, width, num_pages, page_size, heads, D, dtype, reserved;

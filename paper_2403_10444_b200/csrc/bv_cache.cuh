@@ -12,6 +12,9 @@
 
 namespace bv {
 
+// The longest sequence: a tile that begins in it ends below 2^31.
+constexpr int kLongest = 0x7fffffff - 1023;
+
 // Division of numbers below 2^31 by one that the host knows: (n mul / 2^32 + n) / 2^shift.  (A division of unknown integers is some
 // thirty instructions in a row, and the laying out of the work below is a chain of them.)
 struct Divider {
@@ -79,7 +82,7 @@ struct Seq {
 __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int b) {
     Seq s;
     s.len = __ldg(a.lens + b);
-    s.bad = s.len < 0 || s.len > static_cast<long long>(a.width) * a.page;
+    s.bad = s.len < 0 || s.len > kLongest || s.len > static_cast<long long>(a.width) * a.page;
     if (s.bad) s.len = 0;
     int m = a.n_new ? __ldg(a.n_new + b) : a.n;
     m = m < 0 ? 0 : m > a.n ? a.n : m;

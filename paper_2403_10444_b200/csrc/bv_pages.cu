@@ -29,7 +29,7 @@ struct PagesArgs {
 };
 
 __device__ __forceinline__ int pages_of(long long tokens, int page) { return static_cast<int>((tokens + page - 1) / page); }
-__device__ __forceinline__ bool length_ok(const PagesArgs& a, int len) { return len >= 0 && len <= static_cast<long long>(a.width) * a.page; }
+__device__ __forceinline__ bool length_ok(const PagesArgs& a, int len) { return len >= 0 && len <= kLongest && len <= static_cast<long long>(a.width) * a.page; }
 
 // The counts of pages first .. first + 15 of a region that ends at `end`, as bits: which are 0.
 __device__ __forceinline__ unsigned zero_bits(const int32_t* refs, int first, int end, bool vec) {
@@ -123,7 +123,7 @@ __device__ __forceinline__ int need_of(const PagesArgs& a, int b, int* info) {
     const int m = a.n_new ? __ldg(a.n_new + b) : a.n;
     const long long grown = static_cast<long long>(len) + m;
     *info = -1;
-    if (m < 0 || m > a.n || !length_ok(a, len) || grown > static_cast<long long>(a.width) * a.page || grown > 0x7fffffff) return 0;
+    if (m < 0 || m > a.n || !length_ok(a, len) || grown > static_cast<long long>(a.width) * a.page || grown > kLongest) return 0;
     int first = pages_of(len, a.page), pages = pages_of(grown, a.page) - first, replace = 0;
     if (m > 0 && len % a.page != 0) {
         const int last = __ldcg(a.table + static_cast<long long>(b) * a.width + first - 1);

@@ -257,6 +257,26 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(pool[1, 0, 6:8], c.k_new[0, :, 0])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [1, 9])
+def test_positions_next_to_2_to_the_31(dtype, n):
+    """The longest sequence there is, on one page named again and again, seen through a window: what a shorter one on that page sees.  A token
+    more is a length that is none."""
+    page, most = 1 << 20, 2**31 - 1024
+    c = cp.make(1, n, 2, 1, 16, page, [page - 1024], dtype=dtype, seed=19, spare=0)
+    want = bv.bv_cache_attend(c.q, c.k, c.v, c.table, c.lens, window=200, sinks=5)
+    table = c.table.expand(1, 2048).contiguous()
+    lens = torch.tensor([most], dtype=torch.int32, device="cuda")
+    got = bv.bv_cache_attend(c.q, c.k, c.v, table, lens, window=200, sinks=5)
+    assert torch.equal(got, want) and not torch.isnan(got).any()
+    assert torch.isnan(bv.bv_cache_attend(c.q, c.k, c.v, table, lens + 1, window=200, sinks=2000)).all()
+    k = c.k.clone()
+    bv.bv_cache_append(c.k_new, c.v_new, c.k, c.v, table, lens + 1)
+    assert torch.equal(c.k, k)
+    bv.bv_cache_append(c.k_new, c.v_new, c.k, c.v, table, lens)
+    assert torch.equal(c.k[0, 0, page - 1024 - n:page - 1024], c.k_new[0, :, 0]) and bv.bv_stream_status() == 0
+
+
 def test_many_short_sequences():
     lens = [1 + (i * 37) % 50 for i in range(700)]
     check(cp.make(700, 1, 2, 1, 64, 16, lens, seed=17))

@@ -173,6 +173,17 @@ def test_running_out_of_pages():
     assert (copies == -1).all()
 
 
+def test_lengths_next_to_2_to_the_31():
+    page, most = 1 << 20, 2**31 - 1024
+    table = torch.zeros((3, 2048), dtype=torch.int32, device="cuda")
+    lens = torch.tensor([most - 1, most, most + 1], dtype=torch.int32, device="cuda")
+    refs = torch.tensor([1, 0], dtype=torch.int32, device="cuda")
+    new, _ = bv.bv_pages_extend(table, lens, refs, page, 1)
+    assert new.tolist() == [1, -1, -1] and lens.tolist() == [most, most, most + 1]
+    bv.bv_pages_truncate(table, lens, refs, page, torch.tensor([0, 0, 0], dtype=torch.int32, device="cuda"), 1)
+    assert lens.tolist() == [most - 1, most - 1, most + 1] and refs.tolist() == [1, 0]
+
+
 def test_shared_pages_are_replaced():
     t, ln, rf = i32([[0, 1, -1], [0, 1, -1], [0, 1, -1]]), i32([6, 6, 4]), i32([3, 3, 0, 0, 0])
     got, copies = bv.bv_pages_extend(t, ln, rf, 4, 1)
