@@ -8,6 +8,7 @@
 namespace bv {
 namespace {
 
+constexpr double kLog2e = 1.4426950408889634073599246810019;
 bool on(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 int size_of(int dtype) { return dtype == BV_DTYPE_F32 ? 4 : 2; }
 // Are rows of D elements at these strides whole 16-byte vectors on 16-byte boundaries?
@@ -275,7 +276,7 @@ extern "C" int bv_cache_attend(const bv_cache* c, const void* q, const int64_t* 
     int rc = check_cache(c, true, false);
     if (rc != BV_OK) return rc;
     const int es = bv::size_of(c->dtype);
-    if (!q || !out || !q_stride || !out_stride || n < 1 || q_heads < 1 || q_heads % c->heads != 0 || window < 0 || sinks < 0 || !std::isfinite(scale) ||
+    if (!q || !out || !q_stride || !out_stride || n < 1 || q_heads < 1 || q_heads % c->heads != 0 || window < 0 || sinks < 0 || !std::isfinite(static_cast<float>(scale * bv::kLog2e)) ||
         !bv::on(q, es) || !bv::on(out, es) || (n_new && !bv::on(n_new, 4)) || !bv::none_negative(q_stride) || !bv::none_negative(out_stride)) return BV_ERR_INVALID_ARG;
     const int group = q_heads / c->heads;
     if (c->D > BV_MAX_HEAD_DIM || static_cast<long long>(n) * group > (1 << 30)) return BV_ERR_UNSUPPORTED;
@@ -287,7 +288,7 @@ extern "C" int bv_cache_attend(const bv_cache* c, const void* q, const int64_t* 
     a.table = c->table; a.lens = c->lens; a.n_new = n_new;
     for (int i = 0; i < 3; ++i) { a.qs[i] = q_stride[i]; a.os[i] = out_stride[i]; a.ks[i] = c->k_stride[i]; a.vs[i] = c->v_stride[i]; }
     a.B = c->B; a.n = n; a.Hkv = c->heads; a.group = group; a.D = c->D; a.page = c->page_size; a.num_pages = c->num_pages; a.width = c->width;
-    a.kf = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634073599246810019);
+    a.kf = static_cast<float>(static_cast<double>(scale) * bv::kLog2e);
     a.window = window;
     a.sinks = window > 0 ? sinks : 0;
     call.dtype = c->dtype;

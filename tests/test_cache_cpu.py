@@ -94,7 +94,7 @@ def test_refusals_before_a_device_is_touched(lib):
     neg = struct.pack("@3q", 32, -16, 8)
     for fn, bads in (
             (attend, POOLS + ROWS + [dict(q=None), dict(out=None), dict(qs=None), dict(os=None), dict(n=0), dict(heads=3), dict(q_heads=3), dict(q_heads=0), dict(window=-1), dict(sinks=-1),
-                                     dict(scale=float("nan")), dict(scale=float("inf")), dict(q=odd), dict(out=odd), dict(new=odd), dict(qs=neg), dict(os=neg)]),
+                                     dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38), dict(scale=-3e38), dict(q=odd), dict(out=odd), dict(new=odd), dict(qs=neg), dict(os=neg)]),
             (append, POOLS + ROWS + [dict(kn=None), dict(vn=None), dict(kns=None), dict(vns=None), dict(n=0), dict(kn=odd), dict(new=odd), dict(kns=neg)]),
             (extend, ROWS + COUNTS + [dict(n=0), dict(out=None), dict(copies=None), dict(out=odd), dict(new=odd)]),
             (truncate, ROWS + COUNTS + [dict(keep=None), dict(keep=odd), dict(n=-1), dict(new=odd)]),
