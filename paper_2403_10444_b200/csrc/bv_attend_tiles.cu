@@ -743,6 +743,7 @@ bool encode(const AttendArgs& a, const void* pool, const long long* stride, CUte
     const cuuint64_t dims[4] = {static_cast<cuuint64_t>(a.D), static_cast<cuuint64_t>(a.page), static_cast<cuuint64_t>(a.Hkv), static_cast<cuuint64_t>(a.num_pages)};
     // (the stride of an axis of one is nobody's concern, but has to be one that the map takes)
     cuuint64_t st[3] = {static_cast<cuuint64_t>(stride[2]) * 2, static_cast<cuuint64_t>(a.Hkv > 1 ? stride[1] : a.D) * 2, static_cast<cuuint64_t>(a.num_pages > 1 ? stride[0] : a.D) * 2};
+    if (st[0] == 0 || st[1] == 0 || st[2] == 0) return false;        // (heads or pages that are one and the same: not for a map)
     const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(a.page < kTile ? a.page : kTile), 1, 1}, ones[4] = {1, 1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), dims, st, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

@@ -207,6 +207,24 @@ def test_strides_and_alignment(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [1, 9])
+def test_pools_whose_heads_or_pages_are_one(dtype, n):
+    c = cp.make(2, n, 8, 2, 64, 16, [50, 300], dtype=dtype, seed=20)
+    k, v = c.k, c.v
+    c.k, c.v = k[:, :1].expand_as(k), v[:, :1].expand_as(v)
+    check(c)
+    c.k, c.v = k, v[3:4].expand_as(v)
+    check(c)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [40, 48, 49, 64, 65, 96, 128])
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_number_of_rows(dtype, rows, D):
+    check(cp.make(3, rows // 8 if rows % 8 == 0 else rows, 8 if rows % 8 == 0 else 1, 1, D, 16, [130, 700, 64], dtype=dtype, seed=21))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_the_same_bits_every_time(dtype):
     c = cp.make(9, 5, 16, 2, 128, 16, [2000, 5, 700, 31, 999, 1500, 64, 63, 3000], dtype=dtype, seed=14)
     ref = bv.bv_cache_attend(c.q, c.k, c.v, c.table, c.lens)
