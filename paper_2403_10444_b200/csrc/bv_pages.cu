@@ -281,8 +281,8 @@ struct CompactSmem {
     int used, holes, sources;
 };
 // The n pages in use are to lie at 0 .. n-1: those beyond move, in order, to the free pages before, in order.  Writes the moves, moves the
-// counts, and leaves in `to` where a page that moves goes, and n at to[num_pages].
-__global__ void __launch_bounds__(kThreads, 1) compact_pages_kernel(const PagesArgs a, int32_t* moves, int32_t* out_count, int32_t* to, const int vec) {
+// counts, and leaves in `moved` which move takes a page that moves (nothing for the others), and n at moved[num_pages].
+__global__ void __launch_bounds__(kThreads, 1) compact_pages_kernel(const PagesArgs a, int32_t* moves, int32_t* out_count, int32_t* moved, const int vec) {
     __shared__ CompactSmem sm;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = static_cast<int>(cluster.block_rank()), ctas = static_cast<int>(cluster.num_blocks()), tid = threadIdx.x;
@@ -344,25 +344,28 @@ __global__ void __launch_bounds__(kThreads, 1) compact_pages_kernel(const PagesA
         const int from = __ldcg(moves + 2 * i), into = __ldcg(moves + 2 * i + 1);
         a.refs[into] = __ldcg(a.refs + from);
         a.refs[from] = 0;
-        to[from] = into;
+        moved[from] = i;
     }
     if (rank == 0 && tid == 0) {
         *out_count = count;
-        to[a.num_pages] = live;
+        moved[a.num_pages] = live;
     }
     come_together(cluster, ctas);             // (the others' shared memory is read above)
 }
 // Gives the pages of all tables their new numbers.
-__global__ void __launch_bounds__(256) rename_pages_kernel(const PagesArgs a, const int32_t* to) {
-    const int live = __ldg(to + a.num_pages);
+__global__ void __launch_bounds__(256) rename_pages_kernel(const PagesArgs a, const int32_t* moves, const int32_t* count, const int32_t* moved) {
+    const int live = __ldg(moved + a.num_pages), n = __ldg(count);
     const int len = __ldg(a.lens + blockIdx.y);
     if (!length_ok(a, len)) return;
     int32_t* row = a.table + static_cast<long long>(blockIdx.y) * a.width;
     for (int j = blockIdx.x * 256 + threadIdx.x; j < pages_of(len, a.page); j += gridDim.x * 256) {
         const int page = row[j];
         if (page < live || page >= a.num_pages) continue;
-        const int now = __ldg(to + page);
-        if (now >= 0 && now < live) row[j] = now;     // (else no page in use: what it names was free)
+        // (a move that is this page's says so itself: `moved` holds anything for a page that the table names though its count is 0)
+        const int i = __ldg(moved + page);
+        if (i < 0 || i >= n) continue;
+        const int from = __ldg(moves + 2 * i), into = __ldg(moves + 2 * i + 1);
+        if (from == page) row[j] = into;
     }
 }
 
@@ -410,11 +413,11 @@ struct CompactCall {
 size_t compact_scratch(int, const void* ctx) { return (static_cast<const CompactCall*>(ctx)->a.num_pages + 1) * sizeof(int32_t); }
 int enqueue_compact(const StreamWork& work, void* ctx) {
     const CompactCall& c = *static_cast<const CompactCall*>(ctx);
-    int32_t* to = reinterpret_cast<int32_t*>(work.scratch);
-    cudaError_t e = one_cluster(compact_pages_kernel, c.a.num_pages, 0, c.stream, c.a, c.moves, c.count, to, static_cast<int>(on(c.a.refs, 16)));
+    int32_t* moved = reinterpret_cast<int32_t*>(work.scratch);
+    cudaError_t e = one_cluster(compact_pages_kernel, c.a.num_pages, 0, c.stream, c.a, c.moves, c.count, moved, static_cast<int>(on(c.a.refs, 16)));
     if (e == cudaSuccess && c.a.B > 0) {
         const int blocks = (c.a.width + 1023) / 1024;
-        rename_pages_kernel<<<dim3(blocks < 64 ? blocks : 64, c.a.B), 256, 0, c.stream>>>(c.a, to);
+        rename_pages_kernel<<<dim3(blocks < 64 ? blocks : 64, c.a.B), 256, 0, c.stream>>>(c.a, c.moves, c.count, moved);
         e = cudaGetLastError();
     }
     return done(e, c.a.B > 0 ? 2 : 1);

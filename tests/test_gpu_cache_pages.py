@@ -184,6 +184,31 @@ def test_lengths_next_to_2_to_the_31():
     assert lens.tolist() == [most - 1, most - 1, most + 1] and refs.tolist() == [1, 0]
 
 
+def test_a_table_that_names_a_free_page_keeps_it():
+    """Such an entry is a fault of its own: compacting gives it no other page, whatever an earlier call left in the workspace."""
+    for seed in range(3):
+        g = torch.Generator().manual_seed(seed)
+        refs = (torch.rand(500, generator=g) < 0.4).int()
+        before = torch.full((1, 500), -1, dtype=torch.int32)
+        used = refs.nonzero().squeeze(1).int()
+        before[0, :len(used)] = used
+        table, lens = before.cuda(), i32([len(used)])
+        bv.bv_pages_compact(table, lens, refs.cuda(), 1)               # leaves its moves in the workspace
+        free = (refs == 0).nonzero().squeeze(1).int()
+        wrong = torch.cat([used[:50], free[-100:]])[None].contiguous()
+        cleared = refs.clone()
+        cleared[used[50:]] = 0
+        book = cp.Book(wrong, torch.tensor([150]), cleared, 1)
+        moves, count = book.compact()
+        table, lens = wrong.cuda(), i32([150])
+        got_moves, got_count = bv.bv_pages_compact(table, lens, cleared.cuda(), 1)
+        assert got_count.item() == count and got_moves.tolist() == moves and table.tolist() == book.table
+        # pages that move now, and then come free while an entry still names them
+        table = i32([used[50:].tolist()])
+        bv.bv_pages_compact(table, i32([table.shape[1]]), cleared.cuda(), 1)
+        assert table.tolist() == [used[50:].tolist()]
+
+
 def test_shared_pages_are_replaced():
     t, ln, rf = i32([[0, 1, -1], [0, 1, -1], [0, 1, -1]]), i32([6, 6, 4]), i32([3, 3, 0, 0, 0])
     got, copies = bv.bv_pages_extend(t, ln, rf, 4, 1)
