@@ -563,6 +563,8 @@ def bv_cache_attend(q, k, v, table, lens, n_new=None, scale: Optional[float] = N
     if n_out != n:
         raise ValueError("out must have the shape of q")
     new = None if n_new is None else _counted(n_new, B, dev, "n_new")
+    if B == 0:
+        return out
     _enqueue((_lib or load_library()).bv_cache_attend, dev, blob, q.data_ptr(), qs, new, n, heads, D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), os_)
     return out
 
@@ -583,6 +585,8 @@ def bv_cache_append(k_new, v_new, k, v, table, lens, n_new=None, stream=None) ->
     _written(k, "k")
     _written(v, "v")
     new = None if n_new is None else _counted(n_new, B, dev, "n_new")
+    if B == 0:
+        return
     _enqueue((_lib or load_library()).bv_cache_append, dev, blob, k_new.data_ptr(), ks, v_new.data_ptr(), vs, new, n)
 
 
@@ -607,6 +611,8 @@ def bv_pages_extend(table, lens, refs, page_size: int, n: int, n_new=None, strea
     blob, B, dev = _book(table, lens, refs, page_size)
     given = None if n_new is None else _counted(n_new, B, dev, "n_new")
     new, copies = table.new_empty((B,)), table.new_empty((B, 2))
+    if B == 0:
+        return new, copies
     _enqueue((_lib or load_library()).bv_pages_extend, dev, blob, given, n, new.data_ptr(), copies.data_ptr())
     return new, copies
 
@@ -622,6 +628,8 @@ def bv_pages_truncate(table, lens, refs, page_size: int, keep, n: int = 0, n_new
             return r if r.__class__ is not int else _check(r)
     blob, B, dev = _book(table, lens, refs, page_size)
     kept, given = _counted(keep, B, dev, "keep"), None if n_new is None else _counted(n_new, B, dev, "n_new")
+    if B == 0:
+        return
     _enqueue((_lib or load_library()).bv_pages_truncate, dev, blob, kept, given, n)
 
 

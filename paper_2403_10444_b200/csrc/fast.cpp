@@ -1,6 +1,6 @@
 // The binding's calls of the paged cache in C++ (module _fast): the checks of binding.py on tensors of the ordinary kind, the library's call, and
 // nothing else.  A call of the cache takes some 5 us of GPU and driver time, and marshalling it in the interpreter another 7.
-// What is out of the ordinary (a tensor of the wrong type or shape, an output with gaps, another device than the current one) is
+// What is out of the ordinary (a tensor of the wrong type or shape, an empty batch, an output with gaps, another device than the current one) is
 // left to binding.py: NotImplemented.  A status that is not 0 comes back as an integer, for binding.py to raise.
 #include <Python.h>
 
@@ -48,7 +48,7 @@ bool sequences(PyObject* table, PyObject* lens, bv_cache* c, int* dev) {
     const at::Tensor *t = tensor(table), *l = tensor(lens);
     if (!t || !l || t->scalar_type() != at::kInt || l->scalar_type() != at::kInt || t->dim() != 2 || l->dim() != 1 || l->size(0) != t->size(0) || !t->is_contiguous() ||
         !l->is_contiguous() || !t->is_cuda() || !l->is_cuda() || l->get_device() != t->get_device()) return false;
-    if (t->size(0) > INT32_MAX || t->size(1) > INT32_MAX) return false;
+    if (t->size(0) > INT32_MAX || t->size(1) > INT32_MAX || t->size(0) == 0) return false;
     *dev = static_cast<int>(t->get_device());
     c->table = address<int32_t>(*t);
     c->lens = address<int32_t>(*l);

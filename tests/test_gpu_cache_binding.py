@@ -106,3 +106,17 @@ def test_what_is_made_for_a_call_belongs_to_its_stream(way):
     got_new, got_copies = bv.bv_pages_extend(c.table, c.lens, c.refs, 16, 3, stream=s)
     torch.cuda.synchronize()
     assert torch.equal(got, want) and torch.equal(got_new, want_new) and torch.equal(got_copies, want_copies)
+
+
+def test_an_empty_batch(way):
+    c = cp.make(2, 3, 4, 2, 64, 16, [33, 160])
+    table, lens, k = c.table[:0], c.lens[:0], c.k.clone()
+    assert bv.bv_cache_attend(c.q[:0], c.k, c.v, table, lens).shape == (0, 3, 4, 64)
+    assert bv.bv_cache_attend(c.q[:0], c.k, c.v, table, lens, n_new=lens).shape == (0, 3, 4, 64)
+    bv.bv_cache_append(c.k_new[:0], c.v_new[:0], c.k, c.v, table, lens)
+    new, copies = bv.bv_pages_extend(table, lens, c.refs, 16, 3)
+    assert new.shape == (0,) and copies.shape == (0, 2)
+    bv.bv_pages_truncate(table, lens, c.refs, 16, lens)
+    bv.bv_pages_copy(c.k, c.v, copies)
+    torch.cuda.synchronize()
+    assert torch.equal(c.k, k) and bv.bv_stream_status() == 0
