@@ -10,18 +10,18 @@
 // the rows, so the mask, the exponential and the rounding need no other lane.  Up to 32 rows the two fours are two teams that take
 // units in turn, so that one unit's end and the next one's beginning overlap; from 48 rows on, where the exponentials bound (80 x 128 of
 // them are 640 clocks of an SM), each four has half of the rows.  What softmax usually needs across lanes is avoided: each row has an
-// integer reference m in shared memory, weights are 2^{k s - m}, and only where some score exceeds its reference by more than 8
-// (a vote per tile) the new maxima are formed, and O and the sums scaled by the power of two between the old and the new
-// reference.  Sums stay per thread until a unit ends.  Weights are rounded to 16 bits for the second product, and the sums are taken of the rounded weights: a row of one
+// integer reference m in shared memory, weights are 2^{k s - m}, and only where some score exceeds its reference by more than 32
+// (a vote per tile; 32-bit sums and bf16 weights have the range) maxima are formed, and O and the sums scaled by the power of two between the
+// old and the new reference.  A unit's first references are the scores of one key, which are there without any look at the others.  Sums stay per thread until a unit ends.  Weights are rounded to 16 bits for the second product, and the sums are taken of the rounded weights: a row of one
 // key is that key's value exactly, and the error of a row, 2^-9 of its terms at most, is that of an output rounded once more.
 //
 // What a row may not see is taken out twice: its weight is 0 whatever the score is, and rows of V that no row of the unit sees (or that were never
 // loaded) are set to 0 in shared memory, since 0 times an infinity is not 0.  Rows of V that some see and others do not keep their finite
 // elements there; the others are added where they belong when the unit ends, from global memory.
 //
-// Steps that a CTA takes once or a few times (first maxima, masks, ends of units) are loops of 16 rows rather than code for N: fetching
-// instructions that ran never before costs a CTA more than running them (with everything unrolled a unit of 80 rows took 65000
-// clocks beyond its tiles).
+// What a unit takes besides its tiles is instructions that run once, at some four clocks each, since they are fetched for it: 65000 clocks with
+// everything unrolled, 13000 with loops of 16 rows, 8000 now (80 rows) that the first references are one key's, that values are cleared by all threads
+// a vector each, that results go out as whole vectors and that the next unit is looked up by one warp beside the first product.
 #include <cuda.h>
 
 #include "bv_cache.cuh"
@@ -32,7 +32,7 @@ namespace {
 
 constexpr int kTile = 128;
 constexpr float kNone = -3.0e38f;                               // the reference of a row that has seen no score
-constexpr float kLag = 8.f;                                     // how far a score may exceed its reference
+constexpr float kLag = 32.f;                                    // how far a score may exceed its reference (32-bit and bf16 range leave more)
 
 // ---- instructions ------------------------------------------------------------------------------------------------------
 
@@ -136,6 +136,11 @@ struct Shape {
     static_assert(kSlots >= 4, "two tiles in flight");
 };
 constexpr int kUnits = 8;                      // units that may be in flight: no more than slots
+// Sees of a unit: positions p0 to p1 are its rows', low0 and low1 the first positions of the first and the last row's windows.
+struct View {
+    int count, p0, p1, low0, low1;
+    int j0, j1, js;            // pages j0 .. j1, and those before js, hold what its rows see
+};
 template <int NP, int N>
 struct __align__(1024) Smem {
     using Sh = Shape<NP, N>;
@@ -147,6 +152,9 @@ struct __align__(1024) Smem {
         float part[4][N];                      // maxima by warp; then in part[0] what the move of the references scales by
         long long off[N];                      // where the rows' results go
         int abort, fix;
+        Walk next;                             // the team's next unit, the tiles of the other team's one before it
+        View next_view;
+        int skipped;
     } team[Sh::kTeams];
     unsigned long long full[8], empty[8], s_full[2], p_full[2], p_done[2], q_full[2], u_start[2], u_done[2], drain;
     ShareSmem share;
@@ -155,11 +163,6 @@ struct __align__(1024) Smem {
     int bad[kUnits];                           // units that name a page that is none
 };
 
-// Sees of a unit: positions p0 to p1 are its rows', low0 and low1 the first positions of the first and the last row's windows.
-struct View {
-    int count, p0, p1, low0, low1;
-    int j0, j1, js;            // pages j0 .. j1, and those before js, hold what its rows see
-};
 __device__ __forceinline__ View view_of(const AttendArgs& a, const Walk& w) {
     View v;
     v.count = w.r0 + a.rows < w.s.rows ? a.rows : w.s.rows - w.r0;
@@ -334,25 +337,34 @@ __device__ __forceinline__ void issue_products(const AttendArgs& a, Smem<NP, N>&
 // A unit's query rows, swizzled like the keys; zero beyond its rows and beyond D.  They are there when the copies are (fetched_queries).
 template <int NP, int N, int T>
 __device__ __forceinline__ void fetch_queries(const AttendArgs& a, char* to, const Walk& w, int count, int q_vec, int tid) {
-    constexpr int per_row = NP * 8;
+    constexpr int per_row = NP * 8, step = T / per_row;
     const int c = tid % per_row;
     const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + w.b * a.qs[0] + w.h * a.group * a.qs[2] + c * 8;
+    if (q_vec) {
+        const uint32_t dst = smem_u32(to) + c / 8 * (N * 128) + tid / per_row * 128 + ((c % 8) ^ (tid / per_row & 7)) * 16;
+        static_assert(step % 8 == 0, "the swizzle of a thread's rows is one");
+#pragma unroll
+        for (int x = 0; x < N; x += step) {
+            const int row = x + tid / per_row, r = w.r0 + row, t = a.by_group(r);
+            if (N % step != 0 && row >= N) break;
+            if (row < count && c * 8 < a.D)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + x * 128), "l"(src + t * a.qs[1] + (r - t * a.group) * a.qs[2]) : "memory");
+            else
+                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + x * 128), "r"(0) : "memory");
+        }
+        cp_async_commit();
+        return;
+    }
 #pragma unroll 1
-    for (int row = tid / per_row; row < N; row += T / per_row) {
+    for (int row = tid / per_row; row < N; row += step) {
         const uint32_t dst = smem_u32(to) + c / 8 * (N * 128) + row * 128 + ((c % 8) ^ (row & 7)) * 16;
         const int r = w.r0 + row, t = a.by_group(r);
-        const __nv_bfloat16* from = src + t * a.qs[1] + (r - t * a.group) * a.qs[2];
-        const bool there = row < count && c * 8 < a.D;
-        if (q_vec && there) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(from) : "memory");
-        } else {
-            uint4 val = make_uint4(0, 0, 0, 0);
-            if (there) {
-                const uint16_t* e = reinterpret_cast<const uint16_t*>(from);
-                val = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
-            }
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(val.x), "r"(val.y), "r"(val.z), "r"(val.w) : "memory");
+        uint4 val = make_uint4(0, 0, 0, 0);
+        if (row < count && c * 8 < a.D) {
+            const uint16_t* e = reinterpret_cast<const uint16_t*>(src + t * a.qs[1] + (r - t * a.group) * a.qs[2]);
+            val = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
         }
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(val.x), "r"(val.y), "r"(val.z), "r"(val.w) : "memory");
     }
     cp_async_commit();
 }
@@ -379,7 +391,7 @@ template <int C> __device__ __forceinline__ void weigh(float* s, const float* nr
 }
 
 template <int NP, int N>
-__global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const int q_vec) {
+__global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const int vec) {
     extern __shared__ __align__(1024) char raw[];
     using Sh = Shape<NP, N>;
     Smem<NP, N>& sm = *reinterpret_cast<Smem<NP, N>*>(raw);
@@ -450,14 +462,11 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
         // A wait that gives up: this thread asks for a vote from then on, and behind the vote all of them leave together (ts.abort is
         // set before a vote or after the barrier that follows the look at it, never between).
         bool failed = false, gone = false;
-        auto lane_wait = [&](unsigned long long& bar, int phase) {       // (for some lanes of a warp: no coming together in here)
+        auto wait = [&](unsigned long long& bar, int phase) {            // (by whole warps)
             if (!mbar_wait_now(smem_u32(&bar), phase & 1, a.status, limit)) {
                 failed = true;
                 atomicExch(&ts.abort, 1);
             }
-        };
-        auto wait = [&](unsigned long long& bar, int phase) {            // by whole warps
-            lane_wait(bar, phase);
             __syncwarp();
         };
         auto products = [&](int t) { wait(sm.p_done[t % Sh::kBuffers], t / Sh::kBuffers); };      // until tile t's are done
@@ -469,33 +478,33 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
         }
         if (w.more) {
             v = view_of(a, w);
-            fetch_queries<NP, N, kTeam>(a, sm.q[team], w, v.count, q_vec, member);
+            fetch_queries<NP, N, kTeam>(a, sm.q[team], w, v.count, vec & 1, member);
             fetched_queries(sm.q_full[team]);
         }
 #pragma unroll 1
         while (w.more) {
-            Walk next = w;
-            View nv{};
-            int skipped = 0;                   // tiles of the other team's unit
-            bool ahead = false;
-            auto look_ahead = [&] {
-                ahead = true;
-                walk_next(a, next);
-                if (Sh::kTeams > 1 && next.more) {
-                    skipped = next.upto - next.i;
-                    walk_next(a, next);
-                }
-                if (next.more) nv = view_of(a, next);
-            };
             float l[C];
 #pragma unroll
             for (int c = 0; c < C; ++c) l[c] = 0.f;
             if (member < N) {
                 const int r = w.r0 + member, t = a.by_group(r);
-                ts.nref[member] = -kNone;
                 ts.off[member] = t * a.os[1] + (r - t * a.group) * a.os[2];
             }
-            team_sync<kTeam>(bar);
+            // one warp looks ahead while the first scores are under way (here it costs nothing, and nobody has to keep the next unit in registers)
+            if (member < 32) {
+                Walk next = w;
+                int skipped = 0;
+                walk_next(a, next);
+                if (Sh::kTeams > 1 && next.more) {
+                    skipped = next.upto - next.i;
+                    walk_next(a, next);
+                }
+                if (lane == 0) {
+                    ts.next = next;
+                    if (next.more) ts.next_view = next.b == w.b && next.r0 == w.r0 ? v : view_of(a, next);
+                    ts.skipped = skipped;
+                }
+            }
             const int nt = w.upto - w.i;
 #pragma unroll 1
             for (int i = 0; i < nt && !gone; ++i, ++g) {
@@ -521,49 +530,57 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                     }
                     lo -= c0;
                     hi -= c0;
-                    // the value's row: zero where nobody sees it, its finite elements where some do not
-                    if (!all && key < a.span) {
-                        const int xv = 2 * g + 1;
-                        lane_wait(sm.full[xv % kSlots], xv / kSlots);
-                        char* row = sm.ring[xv % kSlots] + key * 128;
-                        if (!any) {
-#pragma unroll
-                            for (int e = 0; e < 8 * NP / Sh::kHalves; ++e) {
-                                const int x = half * 8 * NP / Sh::kHalves + e;
-                                *reinterpret_cast<uint4*>(row + x / 8 * Sh::kPanel + ((x + lane) % 8) * 16) = make_uint4(0, 0, 0, 0);
-                            }
-                        } else {
+                    // Values: zero where nobody sees them, their finite elements where some do not; the keys before `pre` and from `post` on, by all
+                    // threads, a vector at a time.
+                    const int pre = a.window > 0 && v.low1 > start ? (v.low1 - start < a.span ? v.low1 - start : a.span) : 0;
+                    const int sure = v.p0 + 1 - start < a.span ? v.p0 + 1 - start : a.span, post = sure > pre ? sure : pre;
+                    const int items = (pre + a.span - post) * (8 * NP);
+                    if (items > 0) wait(sm.full[(2 * g + 1) % kSlots], (2 * g + 1) / kSlots);
+                    bool odd = false;
 #pragma unroll 1
-                            for (int e = half * 8 * NP / Sh::kHalves; e < (half + 1) * 8 * NP / Sh::kHalves; ++e) {
-                                uint4* at = reinterpret_cast<uint4*>(row + e / 8 * Sh::kPanel + ((e + lane) % 8) * 16);
-                                uint4 val = *at;
-                                bool odd = false;
-                                auto finite = [&](uint32_t& x) {
-                                    if ((x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; odd = true; }
-                                    if ((x & 0x7f800000u) == 0x7f800000u) { x &= 0xffffu; odd = true; }
-                                };
-                                finite(val.x); finite(val.y); finite(val.z); finite(val.w);
-                                if (!odd) continue;
-                                ts.fix = 1;
-                                *at = val;
-                            }
+                    for (int x = member; x < items; x += kTeam) {
+                        const int e = x % (8 * NP), y = x / (8 * NP), z = y < pre ? y : y - pre + post, pz = start + z;
+                        const bool seen = z < keys && any_sees(a, v, pz);
+                        if (seen && all_see(a, v, pz)) continue;
+                        uint4* const at = reinterpret_cast<uint4*>(sm.ring[(2 * g + 1) % kSlots] + e / 8 * Sh::kPanel + z * 128 + e % 8 * 16);
+                        uint4 val = make_uint4(0, 0, 0, 0);
+                        if (seen) {
+                            val = *at;
+                            auto finite = [&](uint32_t& x) {
+                                const uint32_t low = (x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, high = (x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+                                x &= ~(low | high);
+                                odd |= (low | high) != 0;
+                            };
+                            finite(val.x); finite(val.y); finite(val.z); finite(val.w);
                         }
+                        *at = val;
                     }
+                    if (odd) ts.fix = 1;
                     __syncwarp();
                 }
-                // k s - m, and whether any of them is too large (a unit's first tile has no m to be held to)
-                bool raise = i == 0;
-                if (!raise) {
-                    float most = -INFINITY;
-                    load_columns<C>(s_at, s);
+                load_columns<C>(s_at, s);
 #pragma unroll
-                    for (int c = 0; c < C; c += 8) wait_ld8(s + c);
-                    weigh<C>(s, ts.nref + c0, a.kf, masked, lo, hi);
+                for (int c = 0; c < C; c += 8) wait_ld8(s + c);
+                if (i == 0) {
+                    // a unit's first references are the scores of a key that all its rows see, if one of the tile's two ends is such a key
+                    const int ref = all_see(a, v, start) ? 0 : all_see(a, v, start + keys - 1) ? keys - 1 : -1;
+                    if (key == ref) {
 #pragma unroll
-                    for (int c = 0; c < C; ++c) most = fmaxf(most, s[c]);
-                    raise = team_any<kTeam>(bar, most > kLag || failed);
+                        for (int c = 0; c < C; c += 4) *reinterpret_cast<float4*>(ts.part[0] + c0 + c) = make_float4(s[c], s[c + 1], s[c + 2], s[c + 3]);
+                    }
+                    team_sync<kTeam>(bar);
+                    if (member < N) {
+                        const float m = rintf(ts.part[0][member] * a.kf);
+                        ts.nref[member] = ref >= 0 && fabsf(m) < 1.0e30f ? -m : -kNone;
+                    }
+                    team_sync<kTeam>(bar);
                 }
-                if (raise) {
+                // k s - m, and whether any of them is too large
+                weigh<C>(s, ts.nref + c0, a.kf, masked, lo, hi);
+                float most = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < C; ++c) most = fmaxf(most, s[c]);
+                if (team_any<kTeam>(bar, most > kLag || failed)) {
 #pragma unroll 1
                     for (int c = 0; c < C; c += 8) {
                         float y[8];
@@ -628,9 +645,11 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                 mbar_arrive(smem_u32(&sm.p_full[g % Sh::kBuffers]));
             }
             // the next unit's rows, now that this one's have their scores
+            if (gone) team_sync<kTeam>(bar);   // (no tile was looked at, so nothing lies between ts.next and its readers)
+            const Walk next = ts.next;
+            const View nv = ts.next_view;
             if (!gone) {
-                look_ahead();
-                if (next.more) fetch_queries<NP, N, kTeam>(a, sm.q[team], next, nv.count, q_vec, member);
+                if (next.more) fetch_queries<NP, N, kTeam>(a, sm.q[team], next, nv.count, vec & 1, member);
                 wait(sm.u_done[team], unit / Sh::kTeams);
                 if (next.more) fetched_queries(sm.q_full[team]);
             }
@@ -660,14 +679,19 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                 ts.part[0][member] = sum == 0.f ? of_nothing(a, w.s, w.r0 + member) : 1.f / sum;
             }
             team_sync<kTeam>(bar);
-            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + w.b * a.os[0] + w.h * a.group * a.os[2] + dim;
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + w.b * a.os[0] + w.h * a.group * a.os[2];
+            // Eight rows at a time, in a loop: instructions are what this costs, and those of a loop are fetched once.  Two halves put their rows side
+            // by side where the weights lay (their products are done), from where they go out in whole vectors.
+            constexpr bool kStaged = Sh::kHalves == 2;
+            constexpr int kWide = 64 * NP;
+            __nv_bfloat16* const stage = reinterpret_cast<__nv_bfloat16*>(sm.p[0]);
+            static_assert(!kStaged || N * kWide * 2 <= Sh::kP, "rows in the place of weights");
 #pragma unroll 1
-            for (int c = 0; c < C && c0 + c < v.count; c += 16) {
-                float o[16];
+            for (int c = 0; c < C && c0 + c < v.count; c += 8) {
+                float o[8];
                 __syncwarp();
-                ld16(o_at + c, o);             // (of the last columns, where C is not a multiple of 16, some that are not the thread's)
+                ld8(o_at + c, o);
                 wait_ld8(o);
-                wait_ld8(o + 8);
                 if (fix && has_dim) {
                     // what is not finite among the values that some rows see and others do not
 #pragma unroll 1
@@ -684,26 +708,53 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                             const float val = to_float((static_cast<const __nv_bfloat16*>(a.v) + page * a.vs[0] + w.h * a.vs[1] + (p - j * a.page) * a.vs[2])[dim]);
                             if (isfinite(val)) continue;
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
+                            for (int e = 0; e < 8; ++e) {
                                 const int pos = w.s.base + a.by_group(w.r0 + c0 + c + e);
                                 if (p <= pos && (p >= low_of(a, pos) || p < a.sinks)) o[e] += val;
                             }
                         }
                     }
                 }
-                const int mine = C - c < v.count - c0 - c ? C - c : v.count - c0 - c, left = has_dim ? mine : 0;
+                const int left = has_dim ? v.count - c0 - c : 0;
                 if (part) {
-                    float* const at = part + 2 * a.rows + (c0 + c) * a.D + dim;
+                    float* at = part + 2 * a.rows + (c0 + c) * a.D + dim;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (e < left) at[e * a.D] = o[e];
+                    for (int e = 0; e < 8; ++e, at += a.D)
+                        if (e < left) *at = o[e];
+                    continue;
+                }
+                const float4 fa = *reinterpret_cast<const float4*>(ts.part[0] + c0 + c), fb = *reinterpret_cast<const float4*>(ts.part[0] + c0 + c + 4);
+                const float f[8] = {fa.x, fa.y, fa.z, fa.w, fb.x, fb.y, fb.z, fb.w};
+                if constexpr (kStaged) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (has_dim) stage[(c0 + c + e) * kWide + dim] = __float2bfloat16_rn(o[e] * f[e]);
                 } else {
+                    long long off[8];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (e < left) out[ts.off[c0 + c + e]] = __float2bfloat16_rn(o[e] * ts.part[0][c0 + c + e]);
+                    for (int e = 0; e < 8; ++e) off[e] = ts.off[c0 + c + e];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e < left) out[off[e] + dim] = __float2bfloat16_rn(o[e] * f[e]);
                 }
             }
-            if (!ahead) look_ahead();          // (a launch that gives up)
+            if (kStaged && !part) {
+                team_sync<kTeam>(bar);
+                constexpr int kPer = 8 * NP;
+                const int d = member % kPer * 8;
+                if (vec & 2) {
+#pragma unroll
+                    for (int x = 0; x < N; x += kTeam / kPer) {
+                        const int row = x + member / kPer;
+                        if (row < v.count && d < a.D) *reinterpret_cast<uint4*>(out + ts.off[row] + d) = *reinterpret_cast<const uint4*>(stage + row * kWide + d);
+                    }
+                } else {
+#pragma unroll 1
+                    for (int row = member / kPer; row < v.count; row += kTeam / kPer)
+                        for (int e = 0; e < 8 && d < a.D; ++e) out[ts.off[row] + d + e] = stage[row * kWide + d + e];
+                }
+            }
+            const int skipped = ts.skipped;
             fence_before();
             team_sync<kTeam>(bar);
             if (member == 0) ts.fix = sm.bad[unit % kUnits] = 0;
@@ -750,20 +801,20 @@ bool encode(const AttendArgs& a, const void* pool, const long long* stride, CUte
 }
 
 template <int NP, int N>
-cudaError_t launch(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, bool q_vec, int ctas, cudaStream_t stream) {
+cudaError_t launch(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, int vec, int ctas, cudaStream_t stream) {
     static std::atomic<unsigned long long> asked{0};
     const cudaError_t e = allow_shared(attend_tiles_kernel<NP, N>, Shape<NP, N>::kBytes, asked);
     if (e != cudaSuccess) return e;
-    return launch_together(attend_tiles_kernel<NP, N>, ctas, Shape<NP, N>::kThreads, Shape<NP, N>::kBytes, stream, a, k, v, static_cast<int>(q_vec));
+    return launch_together(attend_tiles_kernel<NP, N>, ctas, Shape<NP, N>::kThreads, Shape<NP, N>::kBytes, stream, a, k, v, vec);
 }
 template <int NP>
-cudaError_t pick(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, bool q_vec, int ctas, cudaStream_t stream) {
+cudaError_t pick(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, int vec, int ctas, cudaStream_t stream) {
     switch (a.rows) {
-        case 16: return launch<NP, 16>(a, k, v, q_vec, ctas, stream);
-        case 32: return launch<NP, 32>(a, k, v, q_vec, ctas, stream);
-        case 48: return launch<NP, 48>(a, k, v, q_vec, ctas, stream);
-        case 64: return launch<NP, 64>(a, k, v, q_vec, ctas, stream);
-        default: return launch<NP, 80>(a, k, v, q_vec, ctas, stream);
+        case 16: return launch<NP, 16>(a, k, v, vec, ctas, stream);
+        case 32: return launch<NP, 32>(a, k, v, vec, ctas, stream);
+        case 48: return launch<NP, 48>(a, k, v, vec, ctas, stream);
+        case 64: return launch<NP, 64>(a, k, v, vec, ctas, stream);
+        default: return launch<NP, 80>(a, k, v, vec, ctas, stream);
     }
 }
 
@@ -779,11 +830,12 @@ void attend_tiles_plan(AttendArgs* a) {
     // a unit's beginning and end: 7.2 us at 80 rows, where a tile takes 1.3; 1.3 us at 16, where teams overlap, and a tile takes 1.2
     a->extra = a->rows >= 48 ? 5 : 1;
 }
-cudaError_t launch_attend_tiles(const AttendArgs& a, bool q_vec, int ctas, cudaStream_t stream, bool* taken) {
+cudaError_t launch_attend_tiles(const AttendArgs& a, bool q_vec, bool out_vec, int ctas, cudaStream_t stream, bool* taken) {
+    const int vec = q_vec + 2 * out_vec;
     CUtensorMap k, v;
     *taken = encode(a, a.k, a.ks, &k) && encode(a, a.v, a.vs, &v);
     if (!*taken) return cudaSuccess;
-    return a.D <= 64 ? pick<1>(a, k, v, q_vec, ctas, stream) : pick<2>(a, k, v, q_vec, ctas, stream);
+    return a.D <= 64 ? pick<1>(a, k, v, vec, ctas, stream) : pick<2>(a, k, v, vec, ctas, stream);
 }
 
 }  // namespace bv

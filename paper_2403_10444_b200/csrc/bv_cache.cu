@@ -182,7 +182,7 @@ cudaError_t launch_copy(CopyArgs a, const bv_cache& c, cudaStream_t stream) {
 struct AttendCall {
     AttendArgs a;
     int dtype;
-    bool aligned, q_vec, tiles;
+    bool aligned, q_vec, out_vec, tiles;
     cudaStream_t stream;
 };
 // The kernels for every shape, or the one on the tensor cores.
@@ -217,7 +217,7 @@ int enqueue_attend(const StreamWork& work, void* ctx) {
     few_units();
     if (c.tiles) {
         bool taken = false;
-        const cudaError_t e = launch_attend_tiles(c.a, c.q_vec, ctas, c.stream, &taken);
+        const cudaError_t e = launch_attend_tiles(c.a, c.q_vec, c.out_vec, ctas, c.stream, &taken);
         if (e != cudaSuccess || taken) return done(e, 1);
         plan(&c, false);
         few_units();
@@ -294,6 +294,7 @@ extern "C" int bv_cache_attend(const bv_cache* c, const void* q, const int64_t* 
     call.dtype = c->dtype;
     call.aligned = bv::vectors(c->k, c->k_stride, c->D, es) && bv::vectors(c->v, c->v_stride, c->D, es);
     call.q_vec = bv::vectors(q, q_stride, c->D, es);
+    call.out_vec = bv::vectors(out, out_stride, c->D, es);
     bv::plan(&call, c->dtype == BV_DTYPE_BF16 && call.aligned && bv::attend_tiles_takes(a));
     call.stream = static_cast<cudaStream_t>(stream);
     return bv::with_stream_work(call.stream, bv::attend_scratch, bv::enqueue_attend, &call);

@@ -266,6 +266,7 @@ __device__ __forceinline__ void walk_next(const AttendArgs& a, Walk& w) {
     w.at += w.upto - w.i + a.extra;
     if (w.at >= w.end) { w.more = false; return; }
     w.i = 0;
+    const int b = w.b, r0 = w.r0;
     w.r0 += a.rows;
     if (w.r0 >= w.s.rows) {
         w.r0 = 0;
@@ -274,7 +275,7 @@ __device__ __forceinline__ void walk_next(const AttendArgs& a, Walk& w) {
             do w.s = seq_of(a, ++w.b); while (w.s.rows == 0);     // (the list goes on, so there is one)
         }
     }
-    walk_unit(a, w);
+    if (w.b != b || w.r0 != r0) walk_unit(a, w);                  // (the same rows of the next head see the same)
     walk_cut(w);
 }
 __device__ __forceinline__ int tile_at(const Span& u, int i) { return i < u.sink ? i : u.first + i - u.sink; }
@@ -465,7 +466,7 @@ int attend_rows_most();
 // The kernel on the tensor cores (bv_attend_tiles.cu), for calls that attend_tiles_takes; `taken` is false if no map of the pools could be had.
 bool attend_tiles_takes(const AttendArgs& a);
 void attend_tiles_plan(AttendArgs* a);
-cudaError_t launch_attend_tiles(const AttendArgs& a, bool q_vec, int ctas, cudaStream_t stream, bool* taken);
+cudaError_t launch_attend_tiles(const AttendArgs& a, bool q_vec, bool out_vec, int ctas, cudaStream_t stream, bool* taken);
 cudaError_t launch_attend_rows(const AttendArgs& a, int dtype, bool aligned, bool q_vec, int ctas, cudaStream_t stream);
 
 }  // namespace bv

@@ -20,7 +20,7 @@ cudaError_t attended(const bv::AttendArgs& a, int ctas, cudaStream_t st) {
 }
 }  // namespace
 namespace bv {
-cudaError_t fake_launch_attend_tiles(const AttendArgs& a, bool, int ctas, cudaStream_t st, bool* taken) {
+cudaError_t fake_launch_attend_tiles(const AttendArgs& a, bool, bool, int ctas, cudaStream_t st, bool* taken) {
     *taken = !g_refuse_tiles;
     if (!*taken) return cudaSuccess;
     g_kernel = 1;
