@@ -628,12 +628,15 @@ void attend_rows_plan(AttendArgs* a) {
         a->rows = few_each(a->D);
         a->span = kFewKeys;
         a->extra = 6;                          // a unit's beginning and end, 8000 clocks, where a tile takes 1300
+        a->whole = 6;                          // 4 tiles: 7.5 us by one CTA, 9.2 by four; 8 tiles: 9.8 (D = 64) and 12.5 (128) against 9.5 and 10.9 by eight
     } else {
         const int tiles = (rows + 31) / 32;
         a->rows = ((rows + tiles - 1) / tiles + 7) / 8 * 8;
         a->span = a->D <= 128 ? 64 : 32;
         a->extra = 1;
+        a->whole = 1;                          // (a tile takes longer than the join)
     }
+    a->slack = a->extra;
     a->per_page = 1;
 }
 int attend_rows_most() { return 32; }

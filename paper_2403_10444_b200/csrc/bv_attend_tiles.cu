@@ -827,8 +827,14 @@ void attend_tiles_plan(AttendArgs* a) {
     a->rows = ((rows + tiles - 1) / tiles + 15) / 16 * 16;
     a->span = a->page <= kTile ? kTile / a->page * a->page : kTile;
     a->per_page = a->page <= kTile ? 1 : (a->page + kTile - 1) / kTile;
-    // a unit's beginning and end: 7.2 us at 80 rows, where a tile takes 1.3; 1.3 us at 16, where teams overlap, and a tile takes 1.2
-    a->extra = a->rows >= 48 ? 5 : 1;
+    // A unit's beginning and end: 4.3 us at 72 rows, where a tile takes 1.4; at up to 32 rows, where teams overlap, 1 to 2 us, where a tile
+    // takes 0.75 (D = 64) or 1.5.  (128 blocks of 9 tokens over up to 4000 keys with 3, 4, 5: 121, 122, 128 us; 128 of 3 over up to 2000, D = 64,
+    // with 1, 2, 3: 54, 48, 47; D = 128 with 1, 2: 64, 66.)
+    a->extra = a->rows >= 48 ? 4 : a->D <= 64 ? 2 : 1;
+    // A second CTA for a unit costs a join, 2 to 3 us: 4 tiles take 9.7 and 13.6 us (4 and 72 rows) by one CTA, 10.4 and 14.7 by four, 8 tiles
+    // 12.8 and 18.6 against 10.8 and 14.3 by eight.
+    a->whole = 4;
+    a->slack = a->extra;
 }
 cudaError_t launch_attend_tiles(const AttendArgs& a, bool q_vec, bool out_vec, int ctas, cudaStream_t stream, bool* taken) {
     const int vec = q_vec + 2 * out_vec;

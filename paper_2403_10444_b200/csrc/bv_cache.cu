@@ -209,9 +209,10 @@ int enqueue_attend(const StreamWork& work, void* ctx) {
     c.a.wait_limit = work.wait_limit;
     c.a.never_signal = work.never_signal;
     const int ctas = attend_ctas(work.sm_count);
-    // (fewer units than CTAs: the CTAs have parts of one or two, whose ends are as many everywhere)
+    // (a CTA for each part of a unit where there are fewer units than CTAs: of up to 32 sequences, a lane looks at each of them, of three tiles of rows)
     auto few_units = [&] {
-        const long long units = static_cast<long long>(c.a.B) * c.a.Hkv * ((c.a.n * c.a.group + c.a.rows - 1) / c.a.rows);
+        const long long tiles = (c.a.n * c.a.group + c.a.rows - 1) / c.a.rows, units = static_cast<long long>(c.a.B) * c.a.Hkv * tiles;
+        if (units >= ctas || c.a.B > 32 || tiles > 3) c.a.whole = 0;
         if (units < ctas) c.a.extra = 0;
     };
     few_units();

@@ -69,6 +69,18 @@ def test_the_work_of_one_sequence_is_joined(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,Hq,Hkv", [(1, 2, 1), (1, 8, 4), (1, 16, 2), (5, 6, 1), (9, 16, 2), (13, 16, 1)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (150, 7)])
+def test_fewer_units_than_ctas(dtype, n, Hq, Hkv, window, sinks):
+    """Sequences of all lengths whose heads are shared out to the CTAs whole, in parts of their own, or as the list is cut."""
+    for lens in ([n], [700, n, 64], [1 + 130 * (i * 11 % 29) for i in range(29)], [30, 4000] + [20] * 30):
+        check(cp.make(len(lens), n, Hq, Hkv, 64, 16, lens, dtype=dtype, seed=len(lens)), window=window, sinks=sinks)
+    lens = [700, n, 64, 128]
+    c = cp.make(4, n, Hq, Hkv, 64, 16, lens, dtype=dtype, seed=22)
+    check(c, n_new=torch.tensor([n, 0, 1, n // 2], dtype=torch.int32, device="cuda"), window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_blocks_of_different_lengths_leave_the_other_rows(dtype):
     c = cp.make(6, 5, 8, 2, 64, 16, [40, 3, 0, 100, 17, 200], dtype=dtype, seed=7)
     new = torch.tensor([5, 3, 0, 1, -2, 9], dtype=torch.int32, device="cuda")
