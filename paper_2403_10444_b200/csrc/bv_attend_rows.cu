@@ -9,8 +9,10 @@
 // Two kernels.  Few query rows (a token of a group of up to 8 heads): the call is a matter of reading the cache.  Eight lanes share
 // a key, each with every 8th group of four of its D elements, of 4 query rows at a time, in registers; a warp has 4 keys of each tile
 // of 32, and every thread copies what it will read itself into a ring of cells of its own, several tiles ahead, so no thread
-// waits for another until the unit ends.  More rows: the FMAs bound.  A tile of 64 keys lies in shared memory, and both products
-// are tiled in registers: S by 2 rows x 4 keys a thread, O by 8 rows x 4 columns.
+// waits for another until the unit ends.  More rows: reading shared memory and the FMAs
+// bound (a 16-byte read takes a warp four clocks, wherever it goes).  A tile of 64 keys lies there, and both products are tiled in
+// registers: S by 4 rows x 8 keys a thread with a fourth of D each, O by 8 rows x 8 columns with every 4th or 8th key (2 x 4 and 8 x 4 with no
+// such splits: 206 us against 182 for 18 sequences of up to 8563 keys, 42 rows on 2 heads, D = 128).
 #include "bv_cache.cuh"
 #include "bv_launch.h"
 
@@ -317,15 +319,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_few_kernel(const AttendArg
 template <int NJ>
 struct ManyShape {
     static constexpr int kRows = 32, kKeys = NJ <= 4 ? 64 : 32, kRow = NJ * 32;
+    static constexpr int kPitch = kRow + 16;                           // of a key: two keys' groups of four quads lie in different banks
     static constexpr int kVecs = NJ <= 2 ? 16 : NJ <= 4 ? 32 : 64;     // groups of four of a row, to a power of two
-    static constexpr int kEach = NJ <= 4 ? 1 : 2;                      // ... that a thread has of O
-    static constexpr int kLanes = kVecs / kEach;                       // threads that share a row of O: 16 or 32
+    static constexpr int kLanes = kVecs / 2;                           // threads that share a row of O, two groups each
 };
 template <int NJ>
 struct ManySmem {
     using Sh = ManyShape<NJ>;
-    float k[2][Sh::kKeys][Sh::kRow + 4];
-    float v[2][Sh::kKeys][Sh::kRow];
+    float kv[2 * Sh::kKeys * (Sh::kPitch + Sh::kRow)];                 // two tiles of keys, two of values; at the end of a unit the splits of O
     float q[Sh::kRows][Sh::kRow + 4];
     float p[Sh::kKeys][Sh::kRows + 4];
     float m[Sh::kRows], l[Sh::kRows], factor[Sh::kRows];
@@ -339,16 +340,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
     extern __shared__ __align__(16) char raw[];
     using Sh = ManyShape<NJ>;
     ManySmem<NJ>& sm = *reinterpret_cast<ManySmem<NJ>*>(raw);
-    constexpr int KT = Sh::kKeys, kI = KT / 16, kEach = Sh::kEach;
+    constexpr int KT = Sh::kKeys, kI = KT / 8;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    // S: rows 2 ty, 2 ty + 1 and keys tx + 16 i;  O: rows of `rows8`, columns of `col`, every `kSplit`-th key
-    const int tx = lane & 15, ty = warp * 2 + (lane >> 4);
+    // S: a warp has 4 rows and all keys, a thread keys kg + 8 i and every fourth group of four of D, from part `dq` on; added up, row `mine`.
+    // O: rows of `rows8`, columns of `col`, every `kSplit`-th key
+    const int dq = lane & 3, kg = lane >> 2, mine = warp * 4 + dq;
     constexpr int kSplit = 2 * (32 / Sh::kLanes);
+    float* const keys = sm.kv;
+    float* const vals = sm.kv + 2 * KT * Sh::kPitch;
     const int rows8 = (warp & 3) * 8, col = lane % Sh::kLanes, split = (warp >> 2) + 2 * (lane / Sh::kLanes);
     const int quads = (a.D + 3) / 4;
 
     if (a.D % 4 != 0)                          // (columns D to the next multiple of four stay zero)
-        for (int x = tid; x < 2 * KT * (Sh::kRow + 4); x += kThreads) (&sm.k[0][0][0])[x] = 0.f;
+        for (int x = tid; x < 2 * KT * Sh::kPitch; x += kThreads) keys[x] = 0.f;
     if (tid == 0) sm.joint.n = 0;
     const Share sh = find_share(a, sm.share, kThreads);
     Walk w = walk_begin(a, sh);
@@ -375,8 +379,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
                     for (int y = 0; y < 2 * KT; y += kRound * kStep) {
                         const int which = y >= KT, at = key0 + y - which * KT;
                         const T* const pool = static_cast<const T*>(which ? a.v : a.k) + c * 4;
-                        float* const to = which ? &sm.v[i & 1][at][c * 4] : &sm.k[i & 1][at][c * 4];
-                        const int pitch = (which ? Sh::kRow : Sh::kRow + 4) * kStep;
+                        float* const to = which ? vals + ((i & 1) * KT + at) * Sh::kRow + c * 4 : keys + ((i & 1) * KT + at) * Sh::kPitch + c * 4;
+                        const int pitch = (which ? Sh::kRow : Sh::kPitch) * kStep;
                         long long off[kRound];
 #pragma unroll
                         for (int x = 0; x < kRound; ++x) off[x] = sm.row[i % 3][which][at + x * kStep];
@@ -430,19 +434,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
             sm.m[tid] = -INFINITY;
             sm.l[tid] = 0.f;
         }
-        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-        int pos[2], low[2];
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const bool valid = 2 * ty + r < v.count;
-            pos[r] = valid ? w.s.base + a.by_group(w.r0 + 2 * ty + r) : -1;
-            low[r] = valid ? low_of(a, pos[r]) : 0;
-        }
-        float acc[8][4 * kEach];
+        float m = -INFINITY, l = 0.f;
+        const int pos = mine < v.count ? w.s.base + a.by_group(w.r0 + mine) : -1, low = mine < v.count ? low_of(a, pos) : 0;
+        float acc[8][8];
 #pragma unroll
         for (int r = 0; r < 8; ++r)
 #pragma unroll
-            for (int x = 0; x < 4 * kEach; ++x) acc[r][x] = 0.f;
+            for (int x = 0; x < 8; ++x) acc[r][x] = 0.f;
         __syncthreads();
         fetch(0);
 #pragma unroll 1
@@ -455,49 +453,57 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
             const bool whole = whole_tile(a, v, start, KT);
             bool raised = false;
             if (warp * 4 < v.count) {
-                float s[2][kI];
+                float s[4][kI];
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
+                for (int r = 0; r < 4; ++r)
 #pragma unroll
                     for (int x = 0; x < kI; ++x) s[r][x] = 0.f;
-                const float* const kr = &sm.k[i & 1][tx][0];
-                const float* const qr = &sm.q[2 * ty][0];
-#pragma unroll 4
-                for (int d = 0; d < quads * 4; d += 4) {
-                    const float4 q0 = *reinterpret_cast<const float4*>(qr + d), q1 = *reinterpret_cast<const float4*>(qr + Sh::kRow + 4 + d);
+                const float* const kr = keys + ((i & 1) * KT + kg) * Sh::kPitch;
+                const float* const qr = &sm.q[warp * 4][0];
+#pragma unroll 2
+                for (int d = dq * 4; d < quads * 4; d += 16) {
+                    float4 q[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) q[r] = *reinterpret_cast<const float4*>(qr + r * (Sh::kRow + 4) + d);
 #pragma unroll
                     for (int x = 0; x < kI; ++x) {
-                        const float4 k = *reinterpret_cast<const float4*>(kr + x * 16 * (Sh::kRow + 4) + d);
-                        s[0][x] = fmaf(q0.x, k.x, fmaf(q0.y, k.y, fmaf(q0.z, k.z, fmaf(q0.w, k.w, s[0][x]))));
-                        s[1][x] = fmaf(q1.x, k.x, fmaf(q1.y, k.y, fmaf(q1.z, k.z, fmaf(q1.w, k.w, s[1][x]))));
+                        const float4 k = *reinterpret_cast<const float4*>(kr + x * 8 * Sh::kPitch + d);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[r][x] = fmaf(q[r].x, k.x, fmaf(q[r].y, k.y, fmaf(q[r].z, k.z, fmaf(q[r].w, k.w, s[r][x]))));
                     }
                 }
+                __syncwarp();
+                // the four parts of D: a thread keeps one row of four
+                float y[kI];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    float top = -INFINITY;
+                for (int x = 0; x < kI; ++x) {
+                    const bool up = dq & 2, odd = dq & 1;
+                    const float a0 = (up ? s[2][x] : s[0][x]) + __shfl_xor_sync(0xffffffffu, up ? s[0][x] : s[2][x], 2);
+                    const float a1 = (up ? s[3][x] : s[1][x]) + __shfl_xor_sync(0xffffffffu, up ? s[1][x] : s[3][x], 2);
+                    y[x] = (odd ? a1 : a0) + __shfl_xor_sync(0xffffffffu, odd ? a0 : a1, 1);
+                }
+                float top = -INFINITY;
 #pragma unroll
-                    for (int x = 0; x < kI; ++x) {
-                        const int p = start + tx + 16 * x;
-                        if (!whole && !(p <= pos[r] && (p >= low[r] || p < a.sinks))) s[r][x] = -INFINITY;
-                        top = fmaxf(top, s[r][x]);
-                    }
+                for (int x = 0; x < kI; ++x) {
+                    const int p = start + kg + 8 * x;
+                    if (!whole && !(p <= pos && (p >= low || p < a.sinks))) y[x] = -INFINITY;
+                    top = fmaxf(top, y[x]);
+                }
 #pragma unroll
-                    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    if (top > m[r] + kLag) {
-                        const float f = ex2(m[r] - top);
-                        m[r] = top;
-                        l[r] *= f;
-                        if (tx == 0) sm.factor[2 * ty + r] = f;
-                        raised = true;
-                    } else if (tx == 0) {
-                        sm.factor[2 * ty + r] = 1.f;
-                    }
+                for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                float f = 1.f;
+                if (top > m + kLag) {
+                    f = ex2(m - top);
+                    m = top;
+                    l *= f;
+                    raised = true;
+                }
+                if (kg == 0) sm.factor[mine] = f;
 #pragma unroll
-                    for (int x = 0; x < kI; ++x) {
-                        const float p = s[r][x] == -INFINITY ? 0.f : ex2(s[r][x] - m[r]);
-                        l[r] += p;
-                        sm.p[tx + 16 * x][2 * ty + r] = p;
-                    }
+                for (int x = 0; x < kI; ++x) {
+                    const float p = y[x] == -INFINITY ? 0.f : ex2(y[x] - m);
+                    l += p;
+                    sm.p[kg + 8 * x][mine] = p;
                 }
             }
             raised = __syncthreads_or(raised);
@@ -507,15 +513,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
                     for (int r = 0; r < 8; ++r) {
                         const float f = rows8 + r < v.count ? sm.factor[rows8 + r] : 1.f;
 #pragma unroll
-                        for (int x = 0; x < 4 * kEach; ++x) acc[r][x] *= f;
+                        for (int x = 0; x < 8; ++x) acc[r][x] *= f;
                     }
                 }
                 auto add = [&](int key, bool guard) {
                     const float4 pa = *reinterpret_cast<const float4*>(&sm.p[key][rows8]), pb = *reinterpret_cast<const float4*>(&sm.p[key][rows8 + 4]);
                     const float p[8] = {pa.x, pa.y, pa.z, pa.w, pb.x, pb.y, pb.z, pb.w};
 #pragma unroll
-                    for (int c = 0; c < kEach; ++c) {
-                        const float4 val = *reinterpret_cast<const float4*>(&sm.v[i & 1][key][(col + c * Sh::kLanes) * 4 < Sh::kRow ? (col + c * Sh::kLanes) * 4 : 0]);
+                    for (int c = 0; c < 2; ++c) {
+                        const float4 val = *reinterpret_cast<const float4*>(vals + ((i & 1) * KT + key) * Sh::kRow + ((col + c * Sh::kLanes) * 4 < Sh::kRow ? (col + c * Sh::kLanes) * 4 : 0));
 #pragma unroll
                         for (int r = 0; r < 8; ++r) {
                             if (guard && p[r] == 0.f) continue;
@@ -536,24 +542,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
             }
             __syncthreads();
         }
-        // the sums of the rows, and the splits of O, which lie in the keys' place
+        // the sums of the rows, and the splits of O, which lie in the place of keys and values
         cp_async_wait<0>();
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
-            if (tx == 0) {
-                sm.m[2 * ty + r] = m[r];
-                sm.l[2 * ty + r] = l[r];
-            }
+        for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        if (kg == 0) {
+            sm.m[mine] = m;
+            sm.l[mine] = l;
         }
-        float* const o_at = &sm.k[0][0][0];    // [kSplit][kRows][kRow]
-        static_assert(kSplit * Sh::kRows * Sh::kRow <= 2 * KT * (Sh::kRow + 4), "fits");
+        float* const o_at = sm.kv;             // [kSplit][kRows][kRow]
+        static_assert(kSplit * Sh::kRows * Sh::kRow <= static_cast<int>(sizeof(sm.kv) / sizeof(float)), "fits");
         if (rows8 < v.count) {
 #pragma unroll
             for (int r = 0; r < 8; ++r)
 #pragma unroll
-                for (int c = 0; c < kEach; ++c)
+                for (int c = 0; c < 2; ++c)
                     if ((col + c * Sh::kLanes) * 4 < Sh::kRow)
                         *reinterpret_cast<float4*>(o_at + (split * Sh::kRows + rows8 + r) * Sh::kRow + (col + c * Sh::kLanes) * 4) =
                             make_float4(acc[r][4 * c], acc[r][4 * c + 1], acc[r][4 * c + 2], acc[r][4 * c + 3]);
@@ -574,8 +577,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
         }
         __syncthreads();
         if (a.D % 4 != 0) {                    // (the keys' columns beyond D are zero again)
-            for (int x = tid; x < 2 * KT * (Sh::kRow + 4); x += kThreads)
-                if (x % (Sh::kRow + 4) >= a.D) o_at[x] = 0.f;
+            for (int x = tid; x < 2 * KT * Sh::kPitch; x += kThreads)
+                if (x % Sh::kPitch >= a.D) keys[x] = 0.f;
         }
         walk_next(a, w);
     }
