@@ -47,6 +47,7 @@ __device__ __forceinline__ unsigned zero_bits(const int32_t* refs, int first, in
     }
     return bits;
 }
+static_assert(kThreads / 32 == 16, "a half warp has the warps' sums");
 struct ScanSmem {
     int2 warp[kThreads / 32];
 };
@@ -65,15 +66,19 @@ __device__ __forceinline__ int2 scan(ScanSmem& sm, int2 mine, int2* total) {
     __syncthreads();                          // (the last scan's readers)
     if (lane == 31) sm.warp[warp] = upto;
     __syncthreads();
-    int2 before{0, 0}, all{0, 0};
+    // (the warps' sums, by a lane each, in every warp)
+    int2 sums = sm.warp[lane & 15];
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-        const int2 x = sm.warp[w];
-        before.x += w < warp ? x.x : 0;
-        before.y += w < warp ? x.y : 0;
-        all.x += x.x;
-        all.y += x.y;
+    for (int o = 1; o < kThreads / 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, sums.x, o, 16), y = __shfl_up_sync(0xffffffffu, sums.y, o, 16);
+        if ((lane & 15) >= o) {
+            sums.x += x;
+            sums.y += y;
+        }
     }
+    const int2 all = make_int2(__shfl_sync(0xffffffffu, sums.x, 15), __shfl_sync(0xffffffffu, sums.y, 15));
+    int2 before = make_int2(__shfl_sync(0xffffffffu, sums.x, (warp - 1) & 15), __shfl_sync(0xffffffffu, sums.y, (warp - 1) & 15));
+    if (warp == 0) before = make_int2(0, 0);
     *total = all;
     return make_int2(before.x + upto.x - mine.x, before.y + upto.y - mine.y);
 }
@@ -113,6 +118,7 @@ struct ExtendSmem {
     ScanSmem scan;
     int free;                 // free pages of this CTA's region
     int upto[kMaxSequences];  // pages needed by the sequences up to and including this one, at most one more than there are
+    int list[kRound];         // the free pages of a round, by rank
     int info[kMaxSequences];  // negative: refused whatever is free; else kReplace, kNeeds, and the first entry of its table row to be filled
 };
 enum : int { kReplace = 1, kNeeds = 2, kFirst = 4 };
@@ -178,17 +184,20 @@ __global__ void __launch_bounds__(kThreads, 1) extend_pages_kernel(const PagesAr
         const int p = first + tid * kEach;
         unsigned bits = first == begin ? bits0 : p < end ? zero_bits(a.refs, p, end, vec) : 0u;
         int some;
-        int f = at + scan(sm.scan, __popc(bits), &some);
-        at += some;
-        for (; bits && f < wanted; bits &= bits - 1, ++f) {
-            const int page = p + __ffs(bits) - 1;
-            int lo = 0, hi = a.B - 1;         // the first sequence whose sum is above f
+        int f = scan(sm.scan, __popc(bits), &some);
+        for (; bits && at + f < wanted; bits &= bits - 1, ++f) sm.list[f] = p + __ffs(bits) - 1;
+        __syncthreads();
+        // a thread a page (each thread with the free ones of its 16 took 13000 clocks for 256 sequences)
+        const int n = some < wanted - at ? some : wanted - at;
+        for (int x = tid; x < n; x += kThreads) {
+            const int page = sm.list[x], rank_of = at + x;
+            int lo = 0, hi = a.B - 1;         // the first sequence whose sum is above it
             while (lo < hi) {
                 const int mid = (lo + hi) / 2;
-                if (sm.upto[mid] > f) hi = mid; else lo = mid + 1;
+                if (sm.upto[mid] > rank_of) hi = mid; else lo = mid + 1;
             }
             if (sm.upto[lo] > free) continue; // it is not served, nor is any after it
-            const int slot = f - (lo > 0 ? sm.upto[lo - 1] : 0), asked = sm.info[lo];
+            const int slot = rank_of - (lo > 0 ? sm.upto[lo - 1] : 0), asked = sm.info[lo];
             int32_t* entry = a.table + static_cast<long long>(lo) * a.width + asked / kFirst + slot;
             if (slot == 0 && (asked & kReplace)) {
                 out_copies[2 * lo] = *entry;
@@ -197,6 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1) extend_pages_kernel(const PagesAr
             *entry = page;
             a.refs[page] = 1;
         }
+        at += some;
     }
     __threadfence();
     come_together(cluster, ctas);
