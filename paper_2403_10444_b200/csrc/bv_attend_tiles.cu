@@ -24,6 +24,8 @@
 // a vector each, that results go out as whole vectors and that the next unit is looked up by one warp beside the first product.
 #include <cuda.h>
 
+#include <numeric>
+
 #include "bv_cache.cuh"
 #include "bv_launch.h"
 
@@ -223,18 +225,18 @@ template <int NP, int N>
 __device__ __forceinline__ void load_tiles(const AttendArgs& a, Smem<NP, N>& sm, Walk w, const CUtensorMap* map, int which, uint32_t limit) {
     using Sh = Shape<NP, N>;
     const int lane = threadIdx.x & 31;
-    const int rows = a.page < kTile ? a.page : kTile;                    // of a box
-    const int per = a.per_page > 1 ? 1 : a.by_page(a.span);              // pages of a tile
+    const int boxes = a.per_page > 1 ? 1 : a.span / a.box;               // of a tile
     int x = which, unit = 0;                   // the slot's number in the ring's order
     bool ok = true;
 #pragma unroll 1
     for (; w.more && ok; walk_next(a, w), ++unit) {
         const View v = view_of(a, w);
         const int32_t* row = a.table + static_cast<long long>(w.b) * a.width;
+        int token = 0;                         // where in its page the lane's box begins
         auto entry = [&](int i) {              // this lane's page of tile i: -1 none to be seen, -2 none at all
-            if (i >= w.upto || lane >= per) return -1;
-            const int tile = tile_at(w.u, i);
-            const int j = a.per_page > 1 ? tile / a.per_page : tile * per + lane;
+            if (i >= w.upto || lane >= boxes) return -1;
+            const int p = tile_start(a, tile_at(w.u, i)) + lane * a.box, j = a.by_page(p);
+            token = p - j * a.page;
             if (j > v.j1 || (j < v.j0 && j >= v.js)) return -1;
             const int page = __ldg(row + j);
             return page < 0 || page >= a.num_pages ? -2 : page;
@@ -242,7 +244,7 @@ __device__ __forceinline__ void load_tiles(const AttendArgs& a, Smem<NP, N>& sm,
         int next = entry(w.i);
 #pragma unroll 1
         for (int i = w.i; i < w.upto && ok; ++i, x += 2) {
-            const int page = next;
+            const int page = next, at = token;
             next = entry(i + 1);
             const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
             if (__any_sync(0xffffffffu, page == -2) && lane == 0) sm.bad[unit % kUnits] = 1;
@@ -250,12 +252,11 @@ __device__ __forceinline__ void load_tiles(const AttendArgs& a, Smem<NP, N>& sm,
             ok = __all_sync(0xffffffffu, mbar_wait_now(smem_u32(&sm.empty[slot]), (x / Sh::kSlots & 1) ^ 1, a.status, limit));
             if (!ok) break;
             const uint32_t bar = smem_u32(&sm.full[slot]);
-            if (lane == 0) mbar_arrive_expect(bar, __popc(there) * rows * 128 * NP);
+            if (lane == 0) mbar_arrive_expect(bar, __popc(there) * a.box * 128 * NP);
             __syncwarp();
             if (page >= 0) {
-                const int token = a.per_page > 1 ? tile_at(w.u, i) % a.per_page * a.span : 0;
 #pragma unroll
-                for (int p = 0; p < NP; ++p) tma_load(smem_u32(sm.ring[slot]) + p * Sh::kPanel + lane * rows * 128, map, p * 64, token, w.h, page, bar);
+                for (int p = 0; p < NP; ++p) tma_load(smem_u32(sm.ring[slot]) + p * Sh::kPanel + lane * a.box * 128, map, p * 64, at, w.h, page, bar);
             }
         }
     }
@@ -795,7 +796,7 @@ bool encode(const AttendArgs& a, const void* pool, const long long* stride, CUte
     // (the stride of an axis of one is nobody's concern, but has to be one that the map takes)
     cuuint64_t st[3] = {static_cast<cuuint64_t>(stride[2]) * 2, static_cast<cuuint64_t>(a.Hkv > 1 ? stride[1] : a.D) * 2, static_cast<cuuint64_t>(a.num_pages > 1 ? stride[0] : a.D) * 2};
     if (st[0] == 0 || st[1] == 0 || st[2] == 0) return false;        // (heads or pages that are one and the same: not for a map)
-    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(a.page < kTile ? a.page : kTile), 1, 1}, ones[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(a.box), 1, 1}, ones[4] = {1, 1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), dims, st, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -825,8 +826,16 @@ void attend_tiles_plan(AttendArgs* a) {
     // the fewest tiles of rows, of sizes as even as multiples of 16 are
     const int rows = a->n * a->group, tiles = (rows + 79) / 80;
     a->rows = ((rows + tiles - 1) / tiles + 15) / 16 * 16;
+    // A box is a page, or a tile's share of one; where that leaves an eighth of the tiles' rows empty or more (pages of 48: 96 of 128) tiles go on
+    // across the pages, in boxes that divide both.
     a->span = a->page <= kTile ? kTile / a->page * a->page : kTile;
     a->per_page = a->page <= kTile ? 1 : (a->page + kTile - 1) / kTile;
+    a->box = a->page < kTile ? a->page : kTile;
+    if (8 * (a->per_page > 1 ? a->page : a->span) <= 7 * kTile * a->per_page) {
+        a->box = std::gcd(a->page, kTile);
+        a->span = kTile;
+        a->per_page = 1;
+    }
     // A unit's beginning and end: 4.3 us at 72 rows, where a tile takes 1.4; at up to 32 rows, where teams overlap, 1 to 2 us, where a tile
     // takes 0.75 (D = 64) or 1.5.  (128 blocks of 9 tokens over up to 4000 keys with 3, 4, 5: 121, 122, 128 us; 128 of 3 over up to 2000, D = 64,
     // with 1, 2, 3: 54, 48, 47; D = 128 with 1, 2: 64, 66.)

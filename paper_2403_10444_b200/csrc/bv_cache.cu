@@ -212,7 +212,7 @@ int enqueue_attend(const StreamWork& work, void* ctx) {
     // (a CTA for each part of a unit where there are fewer units than CTAs: of up to 32 sequences, a lane looks at each of them, of three tiles of rows)
     auto few_units = [&] {
         const long long tiles = (c.a.n * c.a.group + c.a.rows - 1) / c.a.rows, units = static_cast<long long>(c.a.B) * c.a.Hkv * tiles;
-        if (units >= ctas || c.a.B > 32 || tiles > 3) c.a.whole = 0;
+        if (units >= ctas || c.a.B > 32 || tiles > 3) c.a.slack = -1;
         if (units < ctas) c.a.extra = 0;
     };
     few_units();

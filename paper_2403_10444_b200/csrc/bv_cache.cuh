@@ -54,9 +54,11 @@ struct AttendArgs {
     int window, sinks;
     int rows;                 // query rows of a unit, at most (row = token * group + head of the group)
     int span;                 // keys of a tile; for pages that are several tiles those of a tile but the last of a page
+    int box;                  // ... as they are copied: tokens of a page at a time (on the tensor cores)
     int per_page;             // tiles of a page, where a page is more than one (else 1)
     int extra;                // what a unit costs besides its tiles, in tiles: it counts as that many more when the list is cut
-    int whole, slack;         // of a CTA for each unit's part; whole = 0: the list is cut
+    int whole;                // units of up to so many tiles are one CTA's
+    int slack;                // of a CTA for each unit's part; negative: the list is cut
     float* part;              // [gridDim.x][2] partial results of part_floats(rows, D)
     unsigned* counters;       // [gridDim.x] by the first CTA of a unit that several have: those that have come, then gone; zero between launches
     int* status;              // set if a bounded wait gave up
@@ -174,7 +176,7 @@ __device__ __forceinline__ Share find_share(const AttendArgs& a, ShareSmem& sm, 
     if (a.B <= 32) {
         // a lane a sequence, every warp for itself
         const Seq q = lane < a.B ? seq_of(a, lane) : Seq{0, 0, 0, false};
-        if (a.whole > 0) {
+        if (a.slack >= 0) {
             // (what is too long for 32 bits is for the list)
             const unsigned units = a.Hkv * row_tiles(a, q), t = units > 0 ? span_of(a, q, 0, q.rows - 1).tiles : 0;
             const bool fits = __all_sync(0xffffffffu, t <= 1u << 18);
@@ -272,11 +274,32 @@ __device__ __forceinline__ void walk_unit(const AttendArgs& a, Walk& w) {
     const int r1 = (w.r0 + a.rows < w.s.rows ? w.r0 + a.rows : w.s.rows) - 1;
     w.u = span_of(a, w.s, w.r0, r1);
 }
-__device__ __forceinline__ void walk_cut(Walk& w) {
+// (A cut through a unit of up to `whole` tiles gives it to the CTA that has the larger part, the first one of two halves.)
+__device__ __forceinline__ void walk_cut(const AttendArgs& a, Walk& w) {
     w.more = w.at < w.end;
     w.unit_at = w.at - w.i;
-    const long long left = w.end - w.at;
-    w.upto = left < w.u.tiles - w.i ? w.i + static_cast<int>(left) : w.u.tiles;
+    w.upto = w.u.tiles;
+    if (w.end - w.at < w.u.tiles - w.i) {
+        const int cut = w.i + static_cast<int>(w.end - w.at);
+        if (w.u.tiles > a.whole) w.upto = cut;
+        else if (2 * cut < w.u.tiles) w.more = false;
+    }
+}
+__device__ __forceinline__ void walk_next(const AttendArgs& a, Walk& w) {
+    w.at += w.upto - w.i + a.extra;
+    if (w.at >= w.end) { w.more = false; return; }
+    w.i = 0;
+    const int b = w.b, r0 = w.r0;
+    w.r0 += a.rows;
+    if (w.r0 >= w.s.rows) {
+        w.r0 = 0;
+        if (++w.h >= a.Hkv) {
+            w.h = 0;
+            do w.s = seq_of(a, ++w.b); while (w.s.rows == 0);     // (the list goes on, so there is one)
+        }
+    }
+    if (w.b != b || w.r0 != r0) walk_unit(a, w);                  // (the same rows of the next head see the same)
+    walk_cut(a, w);
 }
 __device__ __forceinline__ Walk walk_begin(const AttendArgs& a, const Share& sh) {
     Walk w;
@@ -314,24 +337,17 @@ __device__ __forceinline__ Walk walk_begin(const AttendArgs& a, const Share& sh)
     }
     w.i = off > a.extra ? static_cast<int>(off) - a.extra : 0;
     w.at = sh.begin + (off < a.extra ? a.extra - off : 0);
-    walk_cut(w);
-    return w;
-}
-__device__ __forceinline__ void walk_next(const AttendArgs& a, Walk& w) {
-    w.at += w.upto - w.i + a.extra;
-    if (w.at >= w.end) { w.more = false; return; }
-    w.i = 0;
-    const int b = w.b, r0 = w.r0;
-    w.r0 += a.rows;
-    if (w.r0 >= w.s.rows) {
-        w.r0 = 0;
-        if (++w.h >= a.Hkv) {
-            w.h = 0;
-            do w.s = seq_of(a, ++w.b); while (w.s.rows == 0);     // (the list goes on, so there is one)
+    if (w.i > 0 && w.u.tiles <= a.whole) {
+        if (2 * w.i >= w.u.tiles) {            // the CTA's before
+            w.upto = w.u.tiles;
+            walk_next(a, w);
+            return w;
         }
+        w.at -= w.i;
+        w.i = 0;
     }
-    if (w.b != b || w.r0 != r0) walk_unit(a, w);                  // (the same rows of the next head see the same)
-    walk_cut(w);
+    walk_cut(a, w);
+    return w;
 }
 __device__ __forceinline__ int tile_at(const Span& u, int i) { return i < u.sink ? i : u.first + i - u.sink; }
 

@@ -229,6 +229,21 @@ def test_pools_whose_heads_or_pages_are_one(dtype, n):
     check(c)
 
 
+@pytest.mark.parametrize("page", [8, 24, 40, 48, 56, 72, 80, 96, 104, 112, 120, 136, 160, 192, 200, 320, 1000])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (130, 50)])
+def test_every_kind_of_page(page, window, sinks):
+    """Pages that divide a tile, that tiles go across in smaller boxes, or that are several tiles themselves."""
+    for n, D in ((1, 128), (9, 64)):
+        c = cp.make(4, n, 16, 2, D, page, [n, 127, page, 900], seed=page)
+        clean = check(c, window=window, sinks=sinks).clone()
+        # rows behind the sequences, and pages of nobody
+        for b, L in enumerate([n, 127, page, 900]):
+            for j in range(L, cp.ceil_div(L, page) * page):
+                c.k[c.table[b, j // page].item(), :, j % page] = c.v[c.table[b, j // page].item(), :, j % page] = math.nan
+        c.k[c.refs == 0] = c.v[c.refs == 0] = math.nan
+        assert torch.equal(check(c, window=window, sinks=sinks), clean)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows", [40, 48, 49, 64, 65, 96, 128])
 @pytest.mark.parametrize("D", [64, 128])
