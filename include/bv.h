@@ -57,7 +57,7 @@ typedef enum bv_status {
     BV_OK = 0,
     BV_ERR_INVALID_ARG = -1,  /* null pointer, B < 0, gamma < 1, V < 1, T <= 0 or not finite,
                                  unknown dtype, pointer not aligned to its element size */
-    BV_ERR_UNSUPPORTED = -2,  /* gamma > BV_MAX_GAMMA, or no sm_100 device              */
+    BV_ERR_UNSUPPORTED = -2,  /* gamma > BV_MAX_GAMMA, a cache beyond the limits named at struct bv_cache, or no sm_100 device */
     BV_ERR_CUDA = -3,         /* a CUDA runtime call failed; see bv_last_cuda_error()   */
     BV_ERR_TIMEOUT = -4,      /* a bounded device-side wait gave up: reported by the
                                  host-buffer entry points and by bv_stream_status(),
@@ -355,6 +355,8 @@ int bv_decode_loop(const void* target_table, const void* draft_table, const int3
  * All pointers are DEVICE pointers.  Strides count elements and are 0 or more; the D elements of a row are contiguous.
  * Calls enqueue on `stream` and return without synchronising; lengths and tables are read on the device, so calls of one shape may be
  * captured and replayed.  Members that a call does not name are not looked at.
+ * Limits (BV_ERR_UNSUPPORTED beyond): bv_pages_* B 65535 (bv_pages_extend 8192), num_pages and width 2^22 - 2; bv_pages_copy heads
+ * page_size D below 2^30; bv_cache_attend D BV_MAX_HEAD_DIM, n q_heads / heads 2^30.
  */
 typedef struct bv_cache {
     void* k;               /* [num_pages, heads, page_size, D]  dtype, at k_stride between pages, heads, tokens */
@@ -378,8 +380,8 @@ typedef struct bv_cache {
  *   q, out  [B, n, q_heads, D] in the cache's dtype, at strides between sequences, tokens, heads; out must not overlap the inputs
  * Arithmetic: scores, weights and sums in fp32.  16-bit values are multiplied by weights rounded to 16 bits (their sum is taken of the same
  * rounded weights) where the tensor cores do it.  Results do not depend on the order in which CTAs finish.
- * Any D up to BV_MAX_HEAD_DIM, any page size, any alignment; D a multiple of 8 up to 128 at 16-byte strides with
- * pages of a multiple of 8 tokens, in bf16, goes through the tensor cores.
+ * Any D up to BV_MAX_HEAD_DIM, any page size, any alignment; D a multiple of 8 in 16 .. 128 at 16-byte strides with
+ * pages of a multiple of 8 tokens, in bf16, goes through the tensor cores.  scale log2(e) must be finite in 32 bits.
  */
 int bv_cache_attend(const bv_cache* cache, const void* q, const int64_t* q_stride, const int32_t* n_new, int n, int q_heads,
                     float scale, int window, int sinks, void* out, const int64_t* out_stride, void* stream);
@@ -462,8 +464,8 @@ int bv_stream_status(void* stream);
  *                   chunks that last target rows get, so that the launch ends on short items (default 0:
  *                   none; it helped only where most drafted tokens are accepted)
  *   "wait_limit"    polls after which a bounded device-side wait gives up (tests)
- *   "never_signal"  tests: 1: the kernels' workers never report what they have swept, so the waits
- *                   run out and the call ends with BV_ERR_TIMEOUT (2: only the phase kernel's second sweeps are not reported)
+ *   "never_signal"  tests: 1: the kernels' workers never report what they have swept (the cache's attention on the tensor cores: what has
+ *                   been multiplied), so the waits run out and the call ends with BV_ERR_TIMEOUT (2: only the phase kernel's second sweeps are not reported)
  * Their first values come from the environment variables BV_KERNEL (flow / cluster / stream / small / phase),
  * BV_CLUSTER, BV_MAX_CLUSTERS, BV_FLOW_CHUNKS, BV_FLOW_PIECES, BV_FLOW_CTAS, BV_FLOW_DEPTH, read once.
  * Returns BV_ERR_INVALID_ARG for an unknown name.

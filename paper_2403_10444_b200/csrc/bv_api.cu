@@ -909,6 +909,6 @@ const char* bv_status_string(int status) {
     }
 }
 
-int bv_version(void) { return 200; }
+int bv_version(void) { return 300; }
 
 }  // extern "C"

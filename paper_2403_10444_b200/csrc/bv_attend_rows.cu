@@ -6,7 +6,9 @@
 // that lags by up to 8 costs nothing in 32 bits (terms of up to 256 instead of 1) and saves nearly all of the scaling.
 // A weight of zero takes no value, whatever that is.
 //
-// Two kernels.  Few query rows (a token of a group of up to 8 heads): the call is a matter of reading the cache.  Eight lanes share
+// (18 sequences of up to 8563 tokens, blocks of 6 tokens, 14 heads on 2, D = 128: 182 us, 3.7 times the FMAs' floor; single tokens, 32 heads on 8, 16
+// sequences of up to 4096: 84 us, 3.7 TB/s.)
+// Two kernels.  Few query rows (a token of a group of up to 4 heads): the call is a matter of reading the cache.  Eight lanes share
 // a key, each with every 8th group of four of its D elements, of 4 query rows at a time, in registers; a warp has 4 keys of each tile
 // of 32, and every thread copies what it will read itself into a ring of cells of its own, several tiles ahead, so no thread
 // waits for another until the unit ends.  More rows: reading shared memory and the FMAs
@@ -605,9 +607,11 @@ cudaError_t launch_many(const AttendArgs& a, bool aligned, bool q_vec, int ctas,
     if (e != cudaSuccess) return e;
     return launch_together(attend_many_kernel<T, NJ>, ctas, kThreads, bytes, stream, a, static_cast<int>(aligned), static_cast<int>(q_vec));
 }
-// Up to 8 rows (4 where D is beyond 128) are taken 4 (2) at a time by the kernel that reads; the others by the one that multiplies.
+// Up to 4 rows (2 where D is beyond 128), which the kernel that reads takes in one pass, are its; the others the one's that multiplies.  16 sequences
+// of up to 4096 tokens, 4 key-value heads: 4 rows 52.7 and 72.1 us (D = 128), 36.4 and 45.8 (64), 8 rows 93.0 and 72.4, 64.4 and 46.2; D = 256:
+// 2 rows 92.5 and 126.7, 4 rows 149.9 and 126.7.
 constexpr int few_each(int D) { return D <= 128 ? 4 : 2; }
-bool few(int D, int rows) { return rows <= 2 * few_each(D); }
+bool few(int D, int rows) { return rows <= few_each(D); }
 template <typename T>
 cudaError_t pick(const AttendArgs& a, bool aligned, bool q_vec, int ctas, cudaStream_t stream) {
     const int nj = (a.D + 31) / 32;

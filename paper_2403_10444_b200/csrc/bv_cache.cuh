@@ -29,7 +29,7 @@ inline Divider divider(unsigned by) {
 
 // One call of bv_cache_attend.  Work is cut into units (sequence, key-value head, tile of query rows), a unit into tiles of
 // keys; all tiles of all units, in that order, are one list that is cut into gridDim.x equal contiguous parts.  A CTA goes
-// through its part; what a unit has in several CTAs is left in `part` and joined by the one that finishes last.
+// through its part; what a unit has in several CTAs is left in `part` and joined by those CTAs together.
 // (Lengths lie on the device and change from call to call, so the list is laid out by the kernel itself: equal parts keep
 // every SM at work whatever the lengths are, where a grid of (sequence, head, fixed pieces) waits for the longest sequence.  Units of
 // different sequences are not equally long, so some CTAs have twelve ends of units where others have three: each counts as `extra` tiles in
