@@ -331,26 +331,29 @@ struct ManySmem {
     float kv[2 * Sh::kKeys * (Sh::kPitch + Sh::kRow)];                 // two tiles of keys, two of values; at the end of a unit the splits of O
     float q[Sh::kRows][Sh::kRow + 4];
     float p[Sh::kKeys][Sh::kRows + 4];
-    float m[Sh::kRows], l[Sh::kRows], factor[Sh::kRows];
+    float m[Sh::kRows], l[4][Sh::kRows], factor[Sh::kRows], top[4][Sh::kRows];     // sums and maxima by the parts of the keys
     long long row[3][2][Sh::kKeys];            // where the keys' rows lie, of tiles i .. i + 2 (negative: nowhere)
     ShareSmem share;
     JointSmem joint;
 };
 
-template <typename T, int NJ>
+// PARTS: 32 / PARTS rows at most, whose keys are shared out to as many warps (8 rows of all keys would leave six of eight warps idle in either product:
+// 72.4 us against 56.8 for 16 sequences of up to 4096 tokens, 8 rows, D = 128; 16 rows 76.3 against 69.2).
+template <typename T, int NJ, int PARTS>
 __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendArgs a, const int aligned, const int q_vec) {
     extern __shared__ __align__(16) char raw[];
     using Sh = ManyShape<NJ>;
     ManySmem<NJ>& sm = *reinterpret_cast<ManySmem<NJ>*>(raw);
-    constexpr int KT = Sh::kKeys, kI = KT / 8;
+    constexpr int KT = Sh::kKeys, kI = KT / 8 / PARTS, kBlocks = 8 / PARTS, kGroups = 4 / PARTS, kHeld = 32 / PARTS;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    // S: a warp has 4 rows and all keys, a thread keys kg + 8 i and every fourth group of four of D, from part `dq` on; added up, row `mine`.
+    // S: a warp has 4 rows and its part of the keys, a thread keys 8 (PARTS i + part) + kg and every fourth group of four of D, from `dq` on; added
+    // up, row `mine`.
     // O: rows of `rows8`, columns of `col`, every `kSplit`-th key
-    const int dq = lane & 3, kg = lane >> 2, mine = warp * 4 + dq;
-    constexpr int kSplit = 2 * (32 / Sh::kLanes);
+    const int dq = lane & 3, kg = lane >> 2, mine = warp % kBlocks * 4 + dq, part_of_keys = warp / kBlocks;
+    constexpr int kSplit = 8 / kGroups * (32 / Sh::kLanes);
     float* const keys = sm.kv;
     float* const vals = sm.kv + 2 * KT * Sh::kPitch;
-    const int rows8 = (warp & 3) * 8, col = lane % Sh::kLanes, split = (warp >> 2) + 2 * (lane / Sh::kLanes);
+    const int rows8 = warp % kGroups * 8, col = lane % Sh::kLanes, split = warp / kGroups + 8 / kGroups * (lane / Sh::kLanes);
     const int quads = (a.D + 3) / 4;
 
     if (a.D % 4 != 0)                          // (columns D to the next multiple of four stay zero)
@@ -434,7 +437,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
         }
         if (tid < Sh::kRows) {
             sm.m[tid] = -INFINITY;
-            sm.l[tid] = 0.f;
         }
         float m = -INFINITY, l = 0.f;
         const int pos = mine < v.count ? w.s.base + a.by_group(w.r0 + mine) : -1, low = mine < v.count ? low_of(a, pos) : 0;
@@ -454,14 +456,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
             const int start = tile_at(w.u, w.i + i) * KT;
             const bool whole = whole_tile(a, v, start, KT);
             bool raised = false;
-            if (warp * 4 < v.count) {
+            const bool active = warp % kBlocks * 4 < v.count;
+            float y[kI], top = -INFINITY;
+            if (active) {
                 float s[4][kI];
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
 #pragma unroll
                     for (int x = 0; x < kI; ++x) s[r][x] = 0.f;
-                const float* const kr = keys + ((i & 1) * KT + kg) * Sh::kPitch;
-                const float* const qr = &sm.q[warp * 4][0];
+                const float* const kr = keys + ((i & 1) * KT + 8 * part_of_keys + kg) * Sh::kPitch;
+                const float* const qr = &sm.q[warp % kBlocks * 4][0];
 #pragma unroll 2
                 for (int d = dq * 4; d < quads * 4; d += 16) {
                     float4 q[4];
@@ -469,14 +473,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
                     for (int r = 0; r < 4; ++r) q[r] = *reinterpret_cast<const float4*>(qr + r * (Sh::kRow + 4) + d);
 #pragma unroll
                     for (int x = 0; x < kI; ++x) {
-                        const float4 k = *reinterpret_cast<const float4*>(kr + x * 8 * Sh::kPitch + d);
+                        const float4 k = *reinterpret_cast<const float4*>(kr + x * 8 * PARTS * Sh::kPitch + d);
 #pragma unroll
                         for (int r = 0; r < 4; ++r) s[r][x] = fmaf(q[r].x, k.x, fmaf(q[r].y, k.y, fmaf(q[r].z, k.z, fmaf(q[r].w, k.w, s[r][x]))));
                     }
                 }
                 __syncwarp();
                 // the four parts of D: a thread keeps one row of four
-                float y[kI];
 #pragma unroll
                 for (int x = 0; x < kI; ++x) {
                     const bool up = dq & 2, odd = dq & 1;
@@ -484,15 +487,22 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
                     const float a1 = (up ? s[3][x] : s[1][x]) + __shfl_xor_sync(0xffffffffu, up ? s[1][x] : s[3][x], 2);
                     y[x] = (odd ? a1 : a0) + __shfl_xor_sync(0xffffffffu, odd ? a0 : a1, 1);
                 }
-                float top = -INFINITY;
 #pragma unroll
                 for (int x = 0; x < kI; ++x) {
-                    const int p = start + kg + 8 * x;
+                    const int p = start + kg + 8 * (PARTS * x + part_of_keys);
                     if (!whole && !(p <= pos && (p >= low || p < a.sinks))) y[x] = -INFINITY;
                     top = fmaxf(top, y[x]);
                 }
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                if (PARTS > 1 && kg == 0) sm.top[part_of_keys][mine] = top;
+            }
+            if constexpr (PARTS > 1) __syncthreads();
+            if (active) {
+                if constexpr (PARTS > 1) {
+#pragma unroll
+                    for (int x = 0; x < PARTS; ++x) top = fmaxf(top, sm.top[x][mine]);
+                }
                 float f = 1.f;
                 if (top > m + kLag) {
                     f = ex2(m - top);
@@ -500,12 +510,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
                     l *= f;
                     raised = true;
                 }
-                if (kg == 0) sm.factor[mine] = f;
+                if (kg == 0 && part_of_keys == 0) sm.factor[mine] = f;
 #pragma unroll
                 for (int x = 0; x < kI; ++x) {
                     const float p = y[x] == -INFINITY ? 0.f : ex2(y[x] - m);
                     l += p;
-                    sm.p[kg + 8 * x][mine] = p;
+                    sm.p[kg + 8 * (PARTS * x + part_of_keys)][mine] = p;
                 }
             }
             raised = __syncthreads_or(raised);
@@ -549,18 +559,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
         if (kg == 0) {
-            sm.m[mine] = m;
-            sm.l[mine] = l;
+            if (part_of_keys == 0) sm.m[mine] = m;
+            sm.l[part_of_keys][mine] = l;
         }
-        float* const o_at = sm.kv;             // [kSplit][kRows][kRow]
-        static_assert(kSplit * Sh::kRows * Sh::kRow <= static_cast<int>(sizeof(sm.kv) / sizeof(float)), "fits");
+        float* const o_at = sm.kv;             // [kSplit][kHeld][kRow]
+        static_assert(kSplit * kHeld * Sh::kRow <= static_cast<int>(sizeof(sm.kv) / sizeof(float)), "fits");
         if (rows8 < v.count) {
 #pragma unroll
             for (int r = 0; r < 8; ++r)
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
                     if ((col + c * Sh::kLanes) * 4 < Sh::kRow)
-                        *reinterpret_cast<float4*>(o_at + (split * Sh::kRows + rows8 + r) * Sh::kRow + (col + c * Sh::kLanes) * 4) =
+                        *reinterpret_cast<float4*>(o_at + (split * kHeld + rows8 + r) * Sh::kRow + (col + c * Sh::kLanes) * 4) =
                             make_float4(acc[r][4 * c], acc[r][4 * c + 1], acc[r][4 * c + 2], acc[r][4 * c + 3]);
         }
         bad = __syncthreads_or(bad);
@@ -570,12 +580,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
             const int row = x / Sh::kVecs, c = x % Sh::kVecs;
             if (c >= quads) continue;
             float so[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
+#pragma unroll 4
             for (int s = 0; s < kSplit; ++s) {
-                const float4 y = *reinterpret_cast<const float4*>(o_at + (s * Sh::kRows + row) * Sh::kRow + c * 4);
+                const float4 y = *reinterpret_cast<const float4*>(o_at + (s * kHeld + row) * Sh::kRow + c * 4);
                 so[0] += y.x; so[1] += y.y; so[2] += y.z; so[3] += y.w;
             }
-            put<T>(a, w, part, row, c * 4, sm.m[row], bad ? NAN : sm.l[row], so);
+            float sum = 0.f;
+#pragma unroll
+            for (int x = 0; x < PARTS; ++x) sum += sm.l[x][row];
+            put<T>(a, w, part, row, c * 4, sm.m[row], bad ? NAN : sum, so);
         }
         __syncthreads();
         if (a.D % 4 != 0) {                    // (the keys' columns beyond D are zero again)
@@ -598,18 +611,26 @@ cudaError_t launch_few(const AttendArgs& a, bool aligned, bool q_vec, int ctas, 
     if (e != cudaSuccess) return e;
     return launch_together(attend_few_kernel<T, NJ, R>, ctas, kThreads, bytes, stream, a, static_cast<int>(aligned), static_cast<int>(q_vec));
 }
-template <typename T, int NJ>
+template <typename T, int NJ, int PARTS>
 cudaError_t launch_many(const AttendArgs& a, bool aligned, bool q_vec, int ctas, cudaStream_t stream) {
     constexpr int bytes = static_cast<int>(sizeof(ManySmem<NJ>));
     static_assert(bytes <= 227 * 1024, "fits an SM");
     static std::atomic<unsigned long long> asked{0};
-    const cudaError_t e = allow_shared(attend_many_kernel<T, NJ>, bytes, asked);
+    const cudaError_t e = allow_shared(attend_many_kernel<T, NJ, PARTS>, bytes, asked);
     if (e != cudaSuccess) return e;
-    return launch_together(attend_many_kernel<T, NJ>, ctas, kThreads, bytes, stream, a, static_cast<int>(aligned), static_cast<int>(q_vec));
+    return launch_together(attend_many_kernel<T, NJ, PARTS>, ctas, kThreads, bytes, stream, a, static_cast<int>(aligned), static_cast<int>(q_vec));
+}
+template <typename T, int NJ>
+cudaError_t pick_many(const AttendArgs& a, bool aligned, bool q_vec, int ctas, cudaStream_t stream) {
+    if constexpr (sizeof(T) == 4) {            // (16-bit shapes that the tensor cores do not take are too rare for kernels of their own)
+        if (a.rows <= 8) return launch_many<T, NJ, 4>(a, aligned, q_vec, ctas, stream);
+        if (a.rows <= 16) return launch_many<T, NJ, 2>(a, aligned, q_vec, ctas, stream);
+    }
+    return launch_many<T, NJ, 1>(a, aligned, q_vec, ctas, stream);
 }
 // Up to 4 rows (2 where D is beyond 128), which the kernel that reads takes in one pass, are its; the others the one's that multiplies.  16 sequences
-// of up to 4096 tokens, 4 key-value heads: 4 rows 52.7 and 72.1 us (D = 128), 36.4 and 45.8 (64), 8 rows 93.0 and 72.4, 64.4 and 46.2; D = 256:
-// 2 rows 92.5 and 126.7, 4 rows 149.9 and 126.7.
+// of up to 4096 tokens, 4 key-value heads: 4 rows 52.7 and 55.6 us (D = 128), 36.4 and 40.4 (64), 8 rows 93.0 and 56.8, 64.4 and 40.1; D = 256:
+// 2 rows 92.5 and 105.6, 4 rows 149.9 and 105.6.
 constexpr int few_each(int D) { return D <= 128 ? 4 : 2; }
 bool few(int D, int rows) { return rows <= few_each(D); }
 template <typename T>
@@ -621,10 +642,10 @@ cudaError_t pick(const AttendArgs& a, bool aligned, bool q_vec, int ctas, cudaSt
         if (nj <= 4) return launch_few<T, 4, 4>(a, aligned, q_vec, ctas, stream);
         return launch_few<T, 8, 2>(a, aligned, q_vec, ctas, stream);
     }
-    if (nj <= 2) return launch_many<T, 2>(a, aligned, q_vec, ctas, stream);
-    if (nj <= 3) return launch_many<T, 3>(a, aligned, q_vec, ctas, stream);
-    if (nj <= 4) return launch_many<T, 4>(a, aligned, q_vec, ctas, stream);
-    return launch_many<T, 8>(a, aligned, q_vec, ctas, stream);
+    if (nj <= 2) return pick_many<T, 2>(a, aligned, q_vec, ctas, stream);
+    if (nj <= 3) return pick_many<T, 3>(a, aligned, q_vec, ctas, stream);
+    if (nj <= 4) return pick_many<T, 4>(a, aligned, q_vec, ctas, stream);
+    return pick_many<T, 8>(a, aligned, q_vec, ctas, stream);
 }
 
 }  // namespace

@@ -245,8 +245,8 @@ def test_every_kind_of_page(page, window, sinks):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("rows", [40, 48, 49, 64, 65, 96, 128])
-@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows", [5, 7, 8, 12, 16, 17, 24, 40, 48, 49, 64, 65, 96, 128])
+@pytest.mark.parametrize("D", [36, 64, 128, 192])
 def test_every_number_of_rows(dtype, rows, D):
     check(cp.make(3, rows // 8 if rows % 8 == 0 else rows, 8 if rows % 8 == 0 else 1, 1, D, 16, [130, 700, 64], dtype=dtype, seed=21))
 
