@@ -14,7 +14,7 @@
 // the rows, so the mask, the exponential and the rounding need no other lane.  Up to 32 rows the two fours are two teams that take
 // units in turn, so that one unit's end and the next one's beginning overlap; from 48 rows on, where the exponentials bound (80 x 128 of
 // them are 640 clocks of an SM), each four has half of the rows.  What softmax usually needs across lanes is avoided: each row has an
-// integer reference m in shared memory, weights are 2^{k s - m}, and only where some score exceeds its reference by more than 32
+// integer reference m in shared memory, weights are 2^{k s - m}, and only where some score exceeds its reference by more than 16
 // (a vote per tile; 32-bit sums and bf16 weights have the range) maxima are formed, and O and the sums scaled by the power of two between the
 // old and the new reference.  A unit's first references are the scores of one key, which are there without any look at the others.  Sums stay per thread until a unit ends.  Weights are rounded to 16 bits for the second product, and the sums are taken of the rounded weights: a row of one
 // key is that key's value exactly, and the error of a row, 2^-9 of its terms at most, is that of an output rounded once more.
@@ -38,7 +38,7 @@ namespace {
 
 constexpr int kTile = 128;
 constexpr float kNone = -3.0e38f;                               // the reference of a row that has seen no score
-constexpr float kLag = 32.f;                                    // how far a score may exceed its reference (32-bit and bf16 range leave more)
+constexpr float kLag = 16.f;                                    // how far a score may exceed its reference (values up to 2^128 / 2^16 then stay finite)
 
 // ---- instructions ------------------------------------------------------------------------------------------------------
 

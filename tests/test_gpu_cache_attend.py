@@ -181,6 +181,21 @@ def test_scores_far_apart(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,Hq", [(1, 4), (9, 8)])
+def test_a_first_score_far_from_the_others(dtype, n, Hq):
+    """The first key, or the last of its tile, far below, far above and beside the others; values near the type's largest."""
+    for factor in (-30.0, -8.0, 0.0, 8.0, 30.0):
+        c = cp.make(2, n, Hq, 1, 64, 16, [1000, 140], dtype=dtype, seed=23)
+        c.q[..., 0] = 2.0
+        for b in range(2):
+            for j in (0, 127, 128):
+                c.k[c.table[b, j // 16].item(), :, j % 16, 0] = factor * 8
+        c.v *= 2.0 ** 100
+        check(c)
+        check(c, window=60, sinks=3)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("n,Hq,D", [(1, 2, 64), (3, 4, 64), (9, 16, 128), (2, 2, 33)])
 def test_a_row_of_scores_of_minus_infinity(dtype, n, Hq, D):
     """Such a score weighs nothing beside others; a row of nothing else is 0 / 0."""
