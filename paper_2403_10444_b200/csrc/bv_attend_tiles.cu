@@ -16,8 +16,10 @@
 // them are 640 clocks of an SM), each four has half of the rows.  What softmax usually needs across lanes is avoided: each row has an
 // integer reference m in shared memory, weights are 2^{k s - m}, and only where some score exceeds its reference by more than 16
 // (a vote per tile; 32-bit sums and bf16 weights have the range) maxima are formed, and O and the sums scaled by the power of two between the
-// old and the new reference.  A unit's first references are the scores of one key, which are there without any look at the others.  Sums stay per thread until a unit ends.  Weights are rounded to 16 bits for the second product, and the sums are taken of the rounded weights: a row of one
-// key is that key's value exactly, and the error of a row, 2^-9 of its terms at most, is that of an output rounded once more.
+// old and the new reference.  A unit's first references are the scores of one key, which are there without any look at the others.  Sums stay per
+// thread until a unit ends.  Weights are rounded to 16 bits for the second product, and the sums are taken of the rounded weights: a row of one key is
+// that key's value exactly, and the error of a row, 2^-8 of its terms at most, is that of an output rounded once more (0.0022 against 0.0017
+// on random values).
 //
 // What a row may not see is taken out twice: its weight is 0 whatever the score is, and rows of V that no row of the unit sees (or that were never
 // loaded) are set to 0 in shared memory, since 0 times an infinity is not 0.  Rows of V that some see and others do not keep their finite

@@ -481,14 +481,12 @@ __device__ __forceinline__ void join_units(const AttendArgs& a, JointSmem& js, i
     if (tid < n) {
         counter = a.counters + js.unit[tid].first;
         parts = js.unit[tid].last - js.unit[tid].first + 1;
-        __threadfence();
-        atomicInc(counter, 2 * parts - 1);    // `parts` have come, as many go: back to zero with the last one
+        // (`parts` come, as many go: back to zero with the last one)
         const unsigned limit = a.wait_limit ? a.wait_limit : 1u << 22;
-        unsigned v = 0;
-        for (unsigned i = 0; i <= limit; ++i) {
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
-            if (v >= parts) break;
-        }
+        unsigned v;
+        asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(v) : "l"(counter), "r"(2 * parts - 1) : "memory");
+        ++v;
+        for (unsigned i = 0; v < parts && i <= limit; ++i) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
         js.ok[tid] = v >= parts;
         if (v < parts) atomicExch(a.status, 1);
     }
