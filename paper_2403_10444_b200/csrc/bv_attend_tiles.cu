@@ -2,7 +2,7 @@
 // multiple of 8 tokens, rows at 16-byte strides.
 //
 // Bound by the cache's bytes: 64 sequences of up to 8192 tokens, 32 heads on 8, D = 128: 194 us, 5.9 TB/s (0.90 of the copy bandwidth); one of
-// 131072: 94 us, 5.7 TB/s; blocks of 9 tokens, 64 heads on 8, 64 sequences of up to 16384: 370 to 440 us by machine, 5.2 to 6.2 TB/s.  Small
+// 131072: 94 us, 5.7 TB/s; blocks of 9 tokens, 64 heads on 8, 64 sequences of up to 16384: 370 to 470 us by run and machine, 4.9 to 6.2 TB/s.  Small
 // calls by the chain of steps: 7.2 us for a tile of one unit, 11 with a join.
 //
 // A unit is one key-value head of a sequence with up to N query rows (the heads of its group times the block's tokens), a tile
@@ -686,6 +686,7 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                 ts.part[0][member] = sum == 0.f ? of_nothing(a, w.s, w.r0 + member) : 1.f / sum;
             }
             team_sync<kTeam>(bar);
+            if (member == 0) ts.fix = sm.bad[unit % kUnits] = 0;         // (everybody has read them; the unit's last barrier is still to come)
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + w.b * a.os[0] + w.h * a.group * a.os[2];
             // Eight rows at a time, in a loop: instructions are what this costs, and those of a loop are fetched once.  Two halves put their rows side
             // by side where the weights lay (their products are done), from where they go out in whole vectors.
@@ -764,7 +765,6 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
             const int skipped = ts.skipped;
             fence_before();
             team_sync<kTeam>(bar);
-            if (member == 0) ts.fix = sm.bad[unit % kUnits] = 0;
             w = next;
             v = nv;
             g += skipped;
