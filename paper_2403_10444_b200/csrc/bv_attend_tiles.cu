@@ -2,7 +2,8 @@
 // multiple of 8 tokens, rows at 16-byte strides.
 //
 // Bound by the cache's bytes: 64 sequences of up to 8192 tokens, 32 heads on 8, D = 128: 194 us, 5.9 TB/s (0.90 of the copy bandwidth); one of
-// 131072: 94 us, 5.7 TB/s; blocks of 9 tokens, 64 heads on 8, 64 sequences of up to 16384: 370 to 470 us by run and machine, 4.9 to 6.2 TB/s.  Small
+// 131072: 94 us, 5.7 TB/s; blocks of 9 tokens, 64 heads on 8, 64 sequences of up to 16384: 372 us, 6.2 TB/s, at 1965 MHz; called
+// without a pause the GPU reaches its 1000 W and 1560 MHz, and the call 447.  Small
 // calls by the chain of steps: 7.2 us for a tile of one unit, 11 with a join.
 //
 // A unit is one key-value head of a sequence with up to N query rows (the heads of its group times the block's tokens), a tile
