@@ -68,8 +68,8 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a, const I
         const int len = __ldg(a.lens + b);
         int m = a.n_new ? __ldg(a.n_new + b) : a.n;
         if (m > a.n) m = a.n;
-        const int pos = len - m + t;
-        if (t >= m || pos < 0 || len > kLongest || len > static_cast<long long>(a.width) * a.page) continue;
+        const int pos = place_of(len, m, t, a.width, a.page);
+        if (pos < 0) continue;
         const int j = a.by_page(pos), page = __ldg(a.table + static_cast<long long>(b) * a.width + j);
         if (page < 0 || page >= a.num_pages) continue;
         V val[2];

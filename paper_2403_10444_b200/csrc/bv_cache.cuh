@@ -15,6 +15,11 @@ namespace bv {
 // The longest sequence: a tile that begins in it ends below 2^31.
 constexpr int kLongest = 0x7fffffff - 1023;
 
+// Is it the length of a sequence whose row of the table has `width` pages?  Asked before anything is taken from it: -2^31 less one is positive.
+__host__ __device__ __forceinline__ bool length_ok(int len, int width, int page) { return len >= 0 && len <= kLongest && len <= static_cast<long long>(width) * page; }
+// The position that row t of the m newest tokens of a sequence is stored at; negative where there is none.
+__host__ __device__ __forceinline__ int place_of(int len, int m, int t, int width, int page) { return t < m && length_ok(len, width, page) ? len - m + t : -1; }
+
 // Division of numbers below 2^31 by one that the host knows: (n mul / 2^32 + n) / 2^shift.  (A division of unknown integers is some
 // thirty instructions in a row, and the laying out of the work below is a chain of them.)
 struct Divider {
@@ -89,7 +94,7 @@ struct Seq {
 __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int b) {
     Seq s;
     s.len = __ldg(a.lens + b);
-    s.bad = s.len < 0 || s.len > kLongest || s.len > static_cast<long long>(a.width) * a.page;
+    s.bad = !length_ok(s.len, a.width, a.page);
     if (s.bad) s.len = 0;
     int m = a.n_new ? __ldg(a.n_new + b) : a.n;
     m = m < 0 ? 0 : m > a.n ? a.n : m;

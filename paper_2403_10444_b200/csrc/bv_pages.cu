@@ -29,7 +29,7 @@ struct PagesArgs {
 };
 
 __device__ __forceinline__ int pages_of(long long tokens, int page) { return static_cast<int>((tokens + page - 1) / page); }
-__device__ __forceinline__ bool length_ok(const PagesArgs& a, int len) { return len >= 0 && len <= kLongest && len <= static_cast<long long>(a.width) * a.page; }
+__device__ __forceinline__ bool length_ok(const PagesArgs& a, int len) { return bv::length_ok(len, a.width, a.page); }
 
 // The counts of pages first .. first + 15 of a region that ends at `end`, as bits: which are 0.
 __device__ __forceinline__ unsigned zero_bits(const int32_t* refs, int first, int end, bool vec) {

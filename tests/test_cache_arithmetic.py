@@ -1,0 +1,34 @@
+"""Arithmetic that the cache's kernels share with the host, at the ends of its ranges."""
+import ctypes
+import itertools
+import os
+import subprocess
+
+import pytest
+
+from paper_2403_10444_b200 import build as bv_build
+
+MOST = 2**31 - 1024
+
+
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    here = os.path.dirname(os.path.abspath(__file__))
+    out = str(tmp_path_factory.mktemp("host") / "host_arithmetic.so")
+    subprocess.check_call([os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"), "-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-Xcompiler", "-fPIC",
+                           "-shared", "-I", bv_build.CSRC, os.path.join(here, "host_arithmetic.cu"), "-o", out])
+    return ctypes.CDLL(out)
+
+
+def test_a_token_is_stored_inside_its_sequence_or_nowhere(host):
+    """Lengths that are none, down to the lowest integer (one less than which is the largest), have no places."""
+    for (width, page), m in itertools.product(((3, 16), (1, 1), (1 << 22, 1 << 20), (100, 16)), (-2**31, -1, 0, 1, 2, 17, 2**30, 2**31 - 1)):
+        ends = (-2**31, -2**31 + 1, -2**31 + 16, -17, -1, 0, 1, 2, 16, 17, width * page, width * page + 1, MOST, MOST + 1, 2**31 - 1)
+        for length in {x for x in ends if -2**31 <= x < 2**31}:
+            for t in {0, 1, 16, max(0, m - 1), max(0, m)}:
+                if t >= 2**31:
+                    continue
+                fits = 0 <= length <= min(MOST, width * page) and t < m
+                want = length - m + t if fits and length - m + t >= 0 else None
+                got = host.host_place_of(length, m, t, width, page)
+                assert got == want if want is not None else got < 0, (length, m, t, width, page)
