@@ -32,6 +32,12 @@ inline Divider divider(unsigned by) {
     return Divider{by, static_cast<unsigned>(((1ull << 32) * ((1ull << shift) - by)) / by + 1), shift};
 }
 
+// A sum that is not let grow beyond `most`; `more` may be a whole round of numbers, which 32 bits hold but not the sum with them.
+__host__ __device__ __forceinline__ int sum_up_to(int most, int sum, int more) {
+    const long long x = static_cast<long long>(sum) + more;
+    return x < most ? static_cast<int>(x) : most;
+}
+
 // One call of bv_cache_attend.  Work is cut into units (sequence, key-value head, tile of query rows), a unit into tiles of
 // keys; all tiles of all units, in that order, are one list that is cut into gridDim.x equal contiguous parts.  A CTA goes
 // through its part; what a unit has in several CTAs is left in `part` and joined by those CTAs together.

@@ -158,16 +158,17 @@ __global__ void __launch_bounds__(kThreads, 1) extend_pages_kernel(const PagesAr
     const unsigned bits0 = p0 < end ? zero_bits(a.refs, p0, end, vec) : 0u;
     int info = -1, want = tid < a.B ? need_of(a, tid, &info) : 0, mine = __popc(bits0);
     for (int p = p0 + kRound; p < end; p += kRound) mine += __popc(zero_bits(a.refs, p, end, vec));
-    int2 all;                                 // (512 numbers of at most kMost + 1 each stay within 32 bits)
+    static_assert(static_cast<long long>(kThreads) * (kMost + 1) <= 0x7fffffff, "a round's numbers stay within 32 bits");
+    int2 all;
     int2 ahead = scan(sm.scan, make_int2(mine, want), &all);
     if (tid == 0) sm.free = all.x;
     int sum = 0;
     for (int b = tid, b0 = 0;;) {
         if (b < a.B) {
-            sm.upto[b] = min(sum + ahead.y + want, a.num_pages + 1);
+            sm.upto[b] = sum_up_to(a.num_pages + 1, sum, ahead.y + want);
             sm.info[b] = info;
         }
-        sum = min(sum + all.y, a.num_pages + 1);
+        sum = sum_up_to(a.num_pages + 1, sum, all.y);
         b0 += kThreads;
         b += kThreads;
         if (b0 >= a.B) break;

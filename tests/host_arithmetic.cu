@@ -3,4 +3,5 @@
 
 extern "C" {
 int host_place_of(int len, int m, int t, int width, int page) { return bv::place_of(len, m, t, width, page); }
+int host_sum_up_to(int most, int sum, int more) { return bv::sum_up_to(most, sum, more); }
 }

@@ -32,3 +32,15 @@ def test_a_token_is_stored_inside_its_sequence_or_nowhere(host):
                 want = length - m + t if fits and length - m + t >= 0 else None
                 got = host.host_place_of(length, m, t, width, page)
                 assert got == want if want is not None else got < 0, (length, m, t, width, page)
+
+
+def test_sums_of_pages_that_many_sequences_ask_for(host):
+    """In rounds of 512 sequences, as extending adds them up: never below what came before, never beyond a page more than there are."""
+    most = 2**22 - 2
+    for P in (1, 100, most - 9000, most):
+        for want in (0, 1, P // 2, P, P + 1):
+            carry = true = 0
+            for _ in range(16):
+                for i in (1, 2, 511, 512):
+                    assert host.host_sum_up_to(P + 1, carry, i * want) == min(true + i * want, P + 1), (P, want)
+                carry, true = host.host_sum_up_to(P + 1, carry, 512 * want), true + 512 * want

@@ -35,3 +35,30 @@ def test_the_lowest_lengths_have_no_tokens(dtype):
         got, _ = bv.bv_pages_extend(c.table, c.lens, c.refs, 16, 1, i32([1, 1, 1, 1, 1, 0]))
         assert got.tolist() == [-1] * 5 + [0]
     assert bv.bv_stream_status() == 0
+
+
+def test_sequences_that_ask_for_all_pages_of_the_largest_cache():
+    """1024 sequences of one-token pages, each of which would take the whole pool: the first gets it, the second half's sums are no fewer for
+    that.  With nothing free only those that ask for nothing are served."""
+    B, P = 1024, 2**22 - 2
+    if torch.cuda.mem_get_info()[0] < 4 * B * P + (1 << 32):
+        pytest.skip("a table of 17 GB")
+    table = torch.empty((B, P), dtype=torch.int32, device="cuda")
+    table[:, :2] = table[:, -2:] = -1
+    lens, refs = torch.zeros((B,), dtype=torch.int32, device="cuda"), torch.zeros((P,), dtype=torch.int32, device="cuda")
+    new, copies = bv.bv_pages_extend(table, lens, refs, 1, P)
+    assert new.tolist() == [P] + [-1] * (B - 1) and (copies == -1).all()
+    assert lens.tolist() == [P] + [0] * (B - 1) and (refs == 1).all()
+    assert torch.equal(table[0], torch.arange(P, dtype=torch.int32, device="cuda")) and (table[1:, :2] == -1).all() and (table[1:, -2:] == -1).all()
+    lens.zero_()
+    asked = torch.full((B,), P, dtype=torch.int32, device="cuda")
+    asked[::7] = 0
+    new, _ = bv.bv_pages_extend(table, lens, refs, 1, P, asked)
+    assert new.tolist() == [0 if b % 7 == 0 else -1 for b in range(B)] and (lens == 0).all() and (refs == 1).all()
+    # half of the pool free, the second half of the batch asks for it
+    refs[1::2] = 0
+    asked.fill_(0)
+    asked[600:] = P // 2
+    new, _ = bv.bv_pages_extend(table, lens, refs, 1, P, asked)
+    assert new.tolist() == [0] * 600 + [P // 2] + [-1] * 423 and (refs == 1).all()
+    assert torch.equal(table[600, :P // 2], torch.arange(1, P, 2, dtype=torch.int32, device="cuda"))
