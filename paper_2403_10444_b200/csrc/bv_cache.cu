@@ -66,8 +66,7 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a, const I
             c = static_cast<int>(x - y * a.vecs);
         }
         const int len = __ldg(a.lens + b);
-        int m = a.n_new ? __ldg(a.n_new + b) : a.n;
-        if (m > a.n) m = a.n;
+        const int m = a.n_new ? brought(__ldg(a.n_new + b), a.n) : a.n;
         const int pos = place_of(len, m, t, a.width, a.page);
         if (pos < 0) continue;
         const int j = a.by_page(pos), page = __ldg(a.table + static_cast<long long>(b) * a.width + j);

@@ -17,6 +17,8 @@ constexpr int kLongest = 0x7fffffff - 1023;
 
 // Is it the length of a sequence whose row of the table has `width` pages?  Asked before anything is taken from it: -2^31 less one is positive.
 __host__ __device__ __forceinline__ bool length_ok(int len, int width, int page) { return len >= 0 && len <= kLongest && len <= static_cast<long long>(width) * page; }
+// How many tokens a sequence brings where n_new says m: 0 .. n.
+__host__ __device__ __forceinline__ int brought(int m, int n) { return m < 0 ? 0 : m > n ? n : m; }
 // The position that row t of the m newest tokens of a sequence is stored at; negative where there is none.
 __host__ __device__ __forceinline__ int place_of(int len, int m, int t, int width, int page) { return t < m && length_ok(len, width, page) ? len - m + t : -1; }
 
@@ -102,8 +104,7 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int b) {
     s.len = __ldg(a.lens + b);
     s.bad = !length_ok(s.len, a.width, a.page);
     if (s.bad) s.len = 0;
-    int m = a.n_new ? __ldg(a.n_new + b) : a.n;
-    m = m < 0 ? 0 : m > a.n ? a.n : m;
+    const int m = a.n_new ? brought(__ldg(a.n_new + b), a.n) : a.n;
     s.base = s.len - m;
     s.rows = m * a.group;
     return s;

@@ -238,8 +238,8 @@ __global__ void __launch_bounds__(128) truncate_pages_kernel(const PagesArgs a, 
     if (!length_ok(a, len)) return;
     int m = len;
     if (a.n > 0) {
-        m = a.n_new ? __ldg(a.n_new + b) : a.n;
-        m = m < 0 ? 0 : m > len ? len : m;
+        m = a.n_new ? brought(__ldg(a.n_new + b), a.n) : a.n;
+        m = m > len ? len : m;
     }
     int k = __ldg(keep + b);
     k = k < 0 ? 0 : k > m ? m : k;

@@ -1,4 +1,6 @@
 """The paged cache at the ends of the ranges that its calls accept."""
+import random
+
 import pytest
 import torch
 
@@ -62,3 +64,36 @@ def test_sequences_that_ask_for_all_pages_of_the_largest_cache():
     new, _ = bv.bv_pages_extend(table, lens, refs, 1, P, asked)
     assert new.tolist() == [0] * 600 + [P // 2] + [-1] * 423 and (refs == 1).all()
     assert torch.equal(table[600, :P // 2], torch.arange(1, P, 2, dtype=torch.int32, device="cuda"))
+
+
+def cut_back(lens, table, refs, page, keep, n, n_new):
+    """What bv_pages_truncate leaves, by its contract: of the m newest tokens, n_new[b] held to 0 .. n, the first keep[b] stay."""
+    lens, table, refs = list(lens), [list(r) for r in table], list(refs)
+    for b, L in enumerate(lens):
+        m = min(L, max(0, min(n, n_new[b])))
+        lens[b] = L - m + max(0, min(m, keep[b]))
+        for j in range(cp.ceil_div(lens[b], page), cp.ceil_div(L, page)):
+            refs[table[b][j]] -= 1
+            table[b][j] = -1
+    return lens, table, refs
+
+
+def test_a_block_that_is_cut_back_has_n_tokens_at_most():
+    """More in n_new than n is n, as for the attention and for storing: tokens before the block stay."""
+    table, lens, refs = i32([[0, 1, 2], [3, 4, -1], [5, -1, -1]]), i32([10, 8, 2]), i32([1] * 6)
+    bv.bv_pages_truncate(table, lens, refs, 4, i32([1, 0, 0]), 3, i32([9, 2**31 - 1, 4]))
+    assert lens.tolist() == [8, 5, 0]
+    assert table.tolist() == [[0, 1, -1], [3, 4, -1], [-1, -1, -1]] and refs.tolist() == [1, 1, 0, 1, 1, 0]
+
+
+@pytest.mark.parametrize("seed", range(6))
+@pytest.mark.parametrize("page", [1, 3, 16])
+def test_blocks_cut_back_whatever_n_new_says(seed, page):
+    rng = random.Random(seed)
+    B, n = 40, rng.choice((1, 2, 5, 9))
+    lens = [rng.choice((0, 1, n, rng.randint(0, 6 * page))) for _ in range(B)]
+    c = cp.make(B, 1, 1, 1, 4, page, lens, dtype=F32, seed=seed)
+    keep, new = [rng.randint(-1, n + 3) for _ in range(B)], [rng.randint(-2, n + 3) for _ in range(B)]
+    want = cut_back(lens, c.table.tolist(), c.refs.tolist(), page, keep, n, new)
+    bv.bv_pages_truncate(c.table, c.lens, c.refs, page, i32(keep), n, i32(new))
+    assert (c.lens.tolist(), c.table.tolist(), c.refs.tolist()) == want
