@@ -144,7 +144,10 @@ struct Shape {
     static constexpr int kBytes = kSlots * kSlot + kTeams * kQ + kBuffers * kP + kRest;
     static_assert(kSlots >= 4, "two tiles in flight");
 };
-constexpr int kUnits = 8;                      // units that may be in flight: no more than slots
+// Marks of units (Smem::bad).  While a team has not yet read unit u's, the products may be at the scores of u + 3 (with two teams: each hands in the rows
+// of its next unit before it ends one, and scores go a tile ahead), so the keys' warp, which marks a unit when a slot is free for it, at u + 3 + half
+// of the slots.
+constexpr int kUnits = 8;
 // Sees of a unit: positions p0 to p1 are its rows', low0 and low1 the first positions of the first and the last row's windows.
 struct View {
     int count, p0, p1, low0, low1;
@@ -254,10 +257,11 @@ __device__ __forceinline__ void load_tiles(const AttendArgs& a, Smem<NP, N>& sm,
             const int page = next, at = token;
             next = entry(i + 1);
             const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
-            if (__any_sync(0xffffffffu, page == -2) && lane == 0) sm.bad[unit % kUnits] = 1;
+            const bool none = __any_sync(0xffffffffu, page == -2);
             const int slot = x % Sh::kSlots;
             ok = __all_sync(0xffffffffu, mbar_wait_now(smem_u32(&sm.empty[slot]), (x / Sh::kSlots & 1) ^ 1, a.status, limit));
             if (!ok) break;
+            if (none && lane == 0) sm.bad[unit % kUnits] = 1;        // (behind the wait: see kUnits)
             const uint32_t bar = smem_u32(&sm.full[slot]);
             if (lane == 0) mbar_arrive_expect(bar, __popc(there) * a.box * 128 * NP);
             __syncwarp();
@@ -404,6 +408,7 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
     using Sh = Shape<NP, N>;
     Smem<NP, N>& sm = *reinterpret_cast<Smem<NP, N>*>(raw);
     static_assert(sizeof(Smem<NP, N>) <= Sh::kBytes, "the rest fits");
+    static_assert(3 + Sh::kSlots / 2 < kUnits, "no two units with one mark");
     constexpr int kSlots = Sh::kSlots, kSoft = Sh::kSoft, C = Sh::kColumnsEach;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t limit = a.wait_limit ? a.wait_limit : 1u << 24;
