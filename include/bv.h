@@ -375,8 +375,8 @@ typedef struct bv_cache {
  * j > p - window or j < sinks.  m_b = n_new[b] held to 0 .. n (n_new null: n) tokens are the newest ones of the sequence and
  * already in the cache; rows t >= m_b of out are left as they were.  Query head h uses key-value head h / (q_heads / heads).
  * A row that sees nothing (a block longer than its sequence) is 0; one whose scores are all -inf is 0 / 0, NaN.  What a row does not
- * see does not count, whatever it holds (infinities and NaN too).  A sequence with a length that is none, or with a page outside 0 .. num_pages - 1 among
- * those it has to read, gets NaN; others are unaffected.
+ * see does not count, whatever it holds (infinities and NaN too).  The rows of a sequence with a length that is none are NaN, and so is a row that sees
+ * a position on a page outside 0 .. num_pages - 1; others are unaffected, those of the same block among them.
  *   q, out  [B, n, q_heads, D] in the cache's dtype, at strides between sequences, tokens, heads; out must not overlap the inputs
  * Arithmetic: scores, weights and sums in fp32.  16-bit values are multiplied by weights rounded to 16 bits (their sum is taken of the same
  * rounded weights) where the tensor cores do it.  Results do not depend on the order in which CTAs finish.

@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_few_kernel(const AttendArg
 #pragma unroll
                 for (int e = 0; e < 4; ++e) so[e] += sm.part[s][at][d + e] * f;
             }
-            put<T>(a, w, part, at, d, M, bad ? NAN : sl, so);
+            put<T>(a, w, part, at, d, M, bad && loses_row(a, w, at) ? NAN : sl, so);
         }
         cp_async_wait<0>();
         __syncthreads();
@@ -588,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendAr
             float sum = 0.f;
 #pragma unroll
             for (int x = 0; x < PARTS; ++x) sum += sm.l[x][row];
-            put<T>(a, w, part, row, c * 4, sm.m[row], bad ? NAN : sum, so);
+            put<T>(a, w, part, row, c * 4, sm.m[row], bad && loses_row(a, w, row) ? NAN : sum, so);
         }
         __syncthreads();
         if (a.D % 4 != 0) {                    // (the keys' columns beyond D are zero again)

@@ -189,13 +189,6 @@ __device__ __forceinline__ View view_of(const AttendArgs& a, const Walk& w) {
 }
 __device__ __forceinline__ bool any_sees(const AttendArgs& a, const View& v, int p) { return p <= v.p1 && (p >= v.low0 || p < a.sinks); }
 __device__ __forceinline__ bool all_see(const AttendArgs& a, const View& v, int p) { return p <= v.p0 && (p >= v.low1 || p < a.sinks); }
-// Keys of a tile, its first position.
-__device__ __forceinline__ int tile_keys(const AttendArgs& a, int tile, int* start) {
-    *start = tile_start(a, tile);
-    if (a.per_page == 1) return a.span;
-    const int left = a.page - tile % a.per_page * a.span;
-    return left < a.span ? left : a.span;
-}
 __device__ __forceinline__ bool whole_tile(const AttendArgs& a, const View& v, int start, int keys) {
     return start + keys - 1 <= v.p0 && (start >= v.low1 || start + keys <= a.sinks);
 }
@@ -680,11 +673,11 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                 const float x = across<8>(l + c32 + c16, lane);
                 if (lane < 8) sums[c32 + c16 + lane] = x;
             }
-            const bool bad = team_any<kTeam>(bar, w.s.bad || failed || gone) || *static_cast<volatile int*>(&sm.bad[unit % kUnits]) != 0;
+            const bool lost = team_any<kTeam>(bar, failed || gone), bad = w.s.bad || *static_cast<volatile int*>(&sm.bad[unit % kUnits]) != 0;
             const bool fix = *static_cast<volatile int*>(&ts.fix) != 0;
             float* part = leave_unit(a, sh, w, v.count, sm.joint, member);
             if (member < N) {
-                const float sum = bad ? NAN : ts.part[0][member] + ts.part[1][member] + ts.part[2][member] + ts.part[3][member];
+                const float sum = lost || (bad && member < v.count && loses_row(a, w, member)) ? NAN : ts.part[0][member] + ts.part[1][member] + ts.part[2][member] + ts.part[3][member];
                 if (part && member < v.count) {
                     part[member] = -ts.nref[member];
                     part[a.rows + member] = sum;

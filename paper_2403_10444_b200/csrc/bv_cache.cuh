@@ -118,6 +118,11 @@ __device__ __forceinline__ int low_of(const AttendArgs& a, int pos) {
     return low > 0 ? static_cast<int>(low) : 0;
 }
 
+// Does a token at `pos` see any of the positions x0 .. x1?
+__device__ __forceinline__ bool sees_any(const AttendArgs& a, int pos, int x0, int x1) {
+    if (x1 > pos) x1 = pos;
+    return x0 <= x1 && (x1 >= low_of(a, pos) || x0 < a.sinks);
+}
 // The tiles of keys that query rows [r0, r1] of a sequence can see any of: `sink` tiles from the front, then `tiles` - `sink` from
 // `first` on.  At least one: rows that see nothing are written too.
 struct Span {
@@ -362,6 +367,37 @@ __device__ __forceinline__ Walk walk_begin(const AttendArgs& a, const Share& sh)
     return w;
 }
 __device__ __forceinline__ int tile_at(const Span& u, int i) { return i < u.sink ? i : u.first + i - u.sink; }
+
+// Keys of a tile, its first position.
+__device__ __forceinline__ int tile_keys(const AttendArgs& a, int tile, int* start) {
+    *start = tile_start(a, tile);
+    if (a.per_page == 1) return a.span;
+    const int left = a.page - tile % a.per_page * a.span;
+    return left < a.span ? left : a.span;
+}
+
+// Is a row of a faulty unit lost: is its sequence's length none, or does it see a page that is none in the tiles that the CTA has of the unit?  (Looked up
+// when the unit ends, so that it costs nothing where all pages are some; a row that sees none of the faulty ones is as if they were, since what
+// a row does not see does not count.)
+__device__ __forceinline__ bool loses_row(const AttendArgs& a, const Walk& w, int row) {
+    if (w.s.bad) return true;
+    const int pos = w.s.base + a.by_group(w.r0 + row);
+#pragma unroll 1
+    for (int i = w.i; i < w.upto; ++i) {
+        int start;
+        const int end = tile_keys(a, tile_at(w.u, i), &start) + start;
+#pragma unroll 1
+        for (int x = start; x < end && x <= pos;) {
+            const int j = a.by_page(x), left = a.page - (x - j * a.page), upto = end - x < left ? end : x + left;       // positions x .. upto - 1 on page j
+            if (sees_any(a, pos, x, upto - 1)) {
+                const int page = __ldg(a.table + static_cast<long long>(w.b) * a.width + j);
+                if (page < 0 || page >= a.num_pages) return true;
+            }
+            x = upto;
+        }
+    }
+    return false;
+}
 
 // The CTA that holds a place of the list.
 __device__ __forceinline__ int holder_of(const Share& sh, long long place) {
