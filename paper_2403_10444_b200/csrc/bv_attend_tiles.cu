@@ -134,7 +134,7 @@ struct Shape {
     static constexpr int kKeys = 8, kValues = 9, kIssuer = 10;           // warps: loads of keys, of values, products
     static constexpr int kPanel = kTile * 128, kSlot = NP * kPanel;      // a slot: NP panels of 128 rows of 64 columns
     static constexpr int kQ = NP * N * 128, kP = N * kTile * 2;
-    static constexpr int kRest = 3 * 1024;
+    static constexpr int kRest = N > 64 ? 4096 : 3072;
     // two buffers for the weights (the next tile's are formed while the last one's are multiplied) where that leaves five slots
     static constexpr int kTwo = (227 * 1024 - kRest - kTeams * kQ - 2 * kP) / kSlot;
     static constexpr int kBuffers = kTwo >= 5 ? 2 : 1;
@@ -160,10 +160,10 @@ struct __align__(1024) Smem {
     char q[Sh::kTeams][Sh::kQ];
     char p[Sh::kBuffers][Sh::kP];
     struct __align__(16) {
-        float nref[N];                         // minus the references (read four at a time)
+        float nref[N], mref[N];                // minus the references (read four at a time): for the first look, and as they are
         float part[4][N];                      // maxima by warp; then in part[0] what the move of the references scales by
         long long off[N];                      // where the rows' results go
-        int abort, fix;
+        int abort, fix, far;                   // (far: some row's reference is)
         Walk next;                             // the team's next unit, the tiles of the other team's one before it
         View next_view;
         int skipped;
@@ -379,15 +379,22 @@ __device__ __forceinline__ void fetched_queries(unsigned long long& bar) {
     mbar_arrive(smem_u32(&bar));
 }
 
+// A reference differs from the exact product of its score by half of the product's last bit, which from 2^31 on is a hundred and more: the fused product less
+// the reference would overflow as a weight's exponent.  So rows of such references (from 2^20 on) are weighed by products that are rounded as the
+// reference was.  For the first look they count as rows without one, so that it always finds them.
+constexpr float kFar = 1048576.f;
+__device__ __forceinline__ bool far(float m) { return fabsf(m) >= kFar && fabsf(m) != -kNone; }
+
 // C columns of k s - m, those outside [lo, hi) at -inf.
-template <int C> __device__ __forceinline__ void weigh(float* s, const float* nref, float kf, bool masked, int lo, int hi) {
+template <int C, bool FAR = false> __device__ __forceinline__ void weigh(float* s, const float* nref, float kf, bool masked, int lo, int hi) {
+    auto one = [&](float x, float nr) { return FAR && far(nr) ? __fadd_rn(__fmul_rn(x, kf), nr) : fmaf(x, kf, nr); };
 #pragma unroll
     for (int c = 0; c < C; c += 4) {
         const float4 nr = *reinterpret_cast<const float4*>(nref + c);
-        s[c] = fmaf(s[c], kf, nr.x);
-        s[c + 1] = fmaf(s[c + 1], kf, nr.y);
-        s[c + 2] = fmaf(s[c + 2], kf, nr.z);
-        s[c + 3] = fmaf(s[c + 3], kf, nr.w);
+        s[c] = one(s[c], nr.x);
+        s[c + 1] = one(s[c + 1], nr.y);
+        s[c + 2] = one(s[c + 2], nr.z);
+        s[c + 3] = one(s[c + 3], nr.w);
     }
     if (masked) {
 #pragma unroll
@@ -426,7 +433,7 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
         mbar_init(smem_u32(&sm.drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         for (int i = 0; i < kUnits; ++i) sm.bad[i] = 0;
-        for (int i = 0; i < Sh::kTeams; ++i) sm.team[i].abort = sm.team[i].fix = 0;
+        for (int i = 0; i < Sh::kTeams; ++i) sm.team[i].abort = sm.team[i].fix = sm.team[i].far = 0;
         sm.joint.n = 0;
     } else if (warp < Sh::kKeys) {
         // (rows of a slot that no page reaches are never written: they stay zero)
@@ -577,7 +584,7 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                     team_sync<kTeam>(bar);
                     if (member < N) {
                         const float m = rintf(ts.part[0][member] * a.kf);
-                        ts.nref[member] = ref >= 0 && fabsf(m) < 1.0e30f ? -m : -kNone;
+                        ts.nref[member] = ts.mref[member] = ref >= 0 && fabsf(m) < kFar ? -m : -kNone;
                     }
                     team_sync<kTeam>(bar);
                 }
@@ -603,10 +610,12 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                     team_sync<kTeam>(bar);
                     if (member < N) {
                         const float top = fmaxf(fmaxf(ts.part[0][member], ts.part[1][member]), fmaxf(ts.part[2][member], ts.part[3][member]));
-                        const float old = -ts.nref[member];
+                        const float old = -ts.mref[member];
                         const float now = top - old > kLag ? rintf(top) : old;
                         ts.part[0][member] = now == old ? 1.f : exp2f(old - now);
-                        ts.nref[member] = -now;
+                        ts.mref[member] = -now;
+                        ts.nref[member] = fabsf(now) < kFar ? -now : -kNone;
+                        if (far(now)) ts.far = 1;
                     }
                     gone = *static_cast<volatile int*>(&ts.abort) != 0;
                     team_sync<kTeam>(bar);
@@ -630,7 +639,8 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
                     load_columns<C>(s_at, s);
 #pragma unroll
                     for (int c = 0; c < C; c += 8) wait_ld8(s + c);
-                    weigh<C>(s, ts.nref + c0, a.kf, masked, lo, hi);
+                    if (*static_cast<volatile int*>(&ts.far)) weigh<C, true>(s, ts.mref + c0, a.kf, masked, lo, hi);
+                    else weigh<C>(s, ts.mref + c0, a.kf, masked, lo, hi);
                 }
                 if (g >= Sh::kBuffers) products(g - Sh::kBuffers);       // (the weights that lie there have been multiplied)
                 char* const to = p_row + g % Sh::kBuffers * Sh::kP;
@@ -679,13 +689,13 @@ __global__ void __launch_bounds__((Shape<NP, N>::kThreads), 1) attend_tiles_kern
             if (member < N) {
                 const float sum = lost || (bad && member < v.count && loses_row(a, w, member)) ? NAN : ts.part[0][member] + ts.part[1][member] + ts.part[2][member] + ts.part[3][member];
                 if (part && member < v.count) {
-                    part[member] = -ts.nref[member];
+                    part[member] = -ts.mref[member];
                     part[a.rows + member] = sum;
                 }
                 ts.part[0][member] = sum == 0.f ? of_nothing(a, w.s, w.r0 + member) : 1.f / sum;
             }
             team_sync<kTeam>(bar);
-            if (member == 0) ts.fix = sm.bad[unit % kUnits] = 0;         // (everybody has read them; the unit's last barrier is still to come)
+            if (member == 0) ts.fix = ts.far = sm.bad[unit % kUnits] = 0;         // (everybody has read them; the unit's last barrier is still to come)
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + w.b * a.os[0] + w.h * a.group * a.os[2];
             // Eight rows at a time, in a loop: instructions are what this costs, and those of a loop are fetched once.  Two halves put their rows side
             // by side where the weights lay (their products are done), from where they go out in whole vectors.

@@ -97,3 +97,31 @@ def test_blocks_cut_back_whatever_n_new_says(seed, page):
     want = cut_back(lens, c.table.tolist(), c.refs.tolist(), page, keep, n, new)
     bv.bv_pages_truncate(c.table, c.lens, c.refs, page, i32(keep), n, i32(new))
     assert (c.lens.tolist(), c.table.tolist(), c.refs.tolist()) == want
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,Hq,D", [(1, 4, 64), (1, 8, 128), (9, 8, 128), (3, 4, 36)])
+@pytest.mark.parametrize("score", [1e5, 1e6, 3e7, 1e9, 3e10, 1e14, 1e25, 1e33])
+def test_scores_of_every_size(score, n, Hq, D, dtype):
+    """Two keys of the same large score, tiles and CTAs apart, among others far below: the mean of their values (weights of one and of nothing, so no
+    rounding but the result's).  Then keys that differ by little in all of them: some weighted mean of what a row sees."""
+    L = 3000
+    c = cp.make(2, n, Hq, 1, D, 16, [L, 700], dtype=dtype, seed=24)
+    size = (score / D ** 0.5) ** 0.5                             # of q's and of the keys' elements: the scaled score is their product times sqrt(D)
+    c.q.fill_(size)
+    c.k.fill_(-size)
+    for sign in (1, -1):
+        c.v[:, :, :, :] = 7.0
+        for b, tops in enumerate(((130, 2700), (0, 127))):
+            for j, val in zip(tops, (1.0, 3.0)):
+                at = (c.table[b, j // 16].item(), slice(None), j % 16)
+                c.k[at], c.v[at] = size * sign, val
+        got = bv.bv_cache_attend(c.q, c.k, c.v, c.table, c.lens, scale=sign * D ** -0.5)
+        assert (got == 2.0).all(), sign
+        c.k.mul_(-1)
+    g = torch.Generator().manual_seed(25)
+    c.k.copy_((size * (1 + 0.05 * torch.randn(c.k.shape, generator=g))).to(dtype))
+    c.v.copy_(torch.rand(c.v.shape, generator=g).to(dtype))
+    got = bv.bv_cache_attend(c.q, c.k, c.v, c.table, c.lens)
+    assert (got >= 0).all() and (got <= 1).all()
+    assert bv.bv_stream_status() == 0
