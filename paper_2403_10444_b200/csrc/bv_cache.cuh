@@ -532,6 +532,11 @@ __device__ __forceinline__ void join_units(const AttendArgs& a, JointSmem& js, i
         // (`parts` come, as many go: back to zero with the last one)
         const unsigned limit = a.wait_limit ? a.wait_limit : 1u << 22;
         unsigned v;
+        if (a.never_signal == 3 && static_cast<int>(blockIdx.x) == js.unit[tid].last) {
+            // (a test: the last CTA of a unit comes when another has given up, or after as many polls as anybody makes)
+            int gave_up = 0;
+            for (unsigned i = 0; !gave_up && i <= 1u << 22; ++i) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(gave_up) : "l"(a.status) : "memory");
+        }
         asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(v) : "l"(counter), "r"(2 * parts - 1) : "memory");
         ++v;
         for (unsigned i = 0; v < parts && i <= limit; ++i) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
