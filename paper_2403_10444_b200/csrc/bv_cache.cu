@@ -13,7 +13,7 @@ bool on(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 
 int size_of(int dtype) { return dtype == BV_DTYPE_F32 ? 4 : 2; }
 // Are rows of D elements at these strides whole 16-byte vectors on 16-byte boundaries?
 bool vectors(const void* p, const int64_t* stride, int D, int es) {
-    return on(p, 16) && D * es % 16 == 0 && stride[0] * es % 16 == 0 && stride[1] * es % 16 == 0 && stride[2] * es % 16 == 0;
+    return on(p, 16) && static_cast<int64_t>(D) * es % 16 == 0 && stride[0] * es % 16 == 0 && stride[1] * es % 16 == 0 && stride[2] * es % 16 == 0;
 }
 bool none_negative(const int64_t* stride) { return stride[0] >= 0 && stride[1] >= 0 && stride[2] >= 0; }
 
@@ -79,8 +79,8 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a, const I
     }
 }
 template <typename V>
-cudaError_t launch_append(AppendArgs a, int row_bytes, cudaStream_t stream) {
-    a.vecs = row_bytes / static_cast<int>(sizeof(V));
+cudaError_t launch_append(AppendArgs a, long long row_bytes, cudaStream_t stream) {
+    a.vecs = static_cast<int>(row_bytes / static_cast<int>(sizeof(V)));      // (no more than D)
     a.by_n = divider(a.n);
     a.by_heads = divider(a.heads);
     a.by_vecs = divider(a.vecs);
@@ -166,7 +166,7 @@ cudaError_t launch_copy(CopyArgs a, const bv_cache& c, cudaStream_t stream) {
         a.ts[w] = st[2] * es;
     }
     a.tokens = c.page_size;
-    a.vecs = c.D * es / static_cast<int>(sizeof(V));
+    a.vecs = static_cast<int>(static_cast<long long>(c.D) * es / static_cast<int>(sizeof(V)));
     a.all = a.vecs * c.heads * c.page_size;
     a.by_vecs = divider(a.vecs);
     a.by_tokens = divider(a.tokens);
@@ -250,7 +250,7 @@ extern "C" int bv_cache_append(const bv_cache* c, const void* k_new, const int64
     }
     a.table = c->table; a.lens = c->lens; a.n_new = n_new;
     a.B = c->B; a.n = n; a.heads = c->heads; a.page = c->page_size; a.num_pages = c->num_pages; a.width = c->width;
-    const int row_bytes = c->D * es;
+    const long long row_bytes = static_cast<long long>(c->D) * es;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     return bv::done(vec ? bv::launch_append<uint4>(a, row_bytes, s) : es == 4 ? bv::launch_append<uint32_t>(a, row_bytes, s) : bv::launch_append<uint16_t>(a, row_bytes, s), 1);
 }

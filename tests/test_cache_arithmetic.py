@@ -3,6 +3,7 @@ import ctypes
 import itertools
 import os
 import subprocess
+import sys
 
 import pytest
 
@@ -44,3 +45,19 @@ def test_sums_of_pages_that_many_sequences_ask_for(host):
                 for i in (1, 2, 511, 512):
                     assert host.host_sum_up_to(P + 1, carry, i * want) == min(true + i * want, P + 1), (P, want)
                 carry, true = host.host_sum_up_to(P + 1, carry, 512 * want), true + 512 * want
+
+
+def test_rows_of_as_many_bytes_as_32_bits_hold_and_more():
+    """Up to the launch, in a process of its own (a division by zero ends it); without a device the launch is what fails."""
+    code = ("import sys; sys.path[:0] = %r\n"
+            "import test_cache_cpu as t\n"
+            "from paper_2403_10444_b200 import build, binding\n"
+            "build.build(); lib = binding.load_library()\n"
+            "for D in (2**29, 2**30, 2**31 - 4, 2**31 - 1):\n"
+            "    for dtype in (0, 1):\n"
+            "        assert t.append(lib, D=D, B=0, dtype=dtype) == 0\n"
+            "        if not t.torch.cuda.is_available():\n"
+            "            assert t.append(lib, D=D, dtype=dtype) == -3\n"
+            "            assert t.copy(lib, D=D, heads=1, page=1, dtype=dtype) == (-3 if D < 2**30 else -2)\n")
+    here = os.path.dirname(os.path.abspath(__file__))
+    subprocess.check_call([sys.executable, "-c", code % [os.path.dirname(here), here]])

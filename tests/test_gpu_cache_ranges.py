@@ -125,3 +125,19 @@ def test_scores_of_every_size(score, n, Hq, D, dtype):
     got = bv.bv_cache_attend(c.q, c.k, c.v, c.table, c.lens)
     assert (got >= 0).all() and (got <= 1).all()
     assert bv.bv_stream_status() == 0
+
+
+@pytest.mark.parametrize("dtype,D", [(F32, 2**29), (BF16, 2**30 - 8)])
+def test_rows_of_2_to_the_31_bytes(dtype, D):
+    """Stored in a page and copied to another (one pool for keys and values: the same ones)."""
+    if torch.cuda.mem_get_info()[0] < 20 << 30:
+        pytest.skip("four rows of 2 GB")
+    pool = torch.zeros((3, 1, 1, D), dtype=dtype, device="cuda")
+    row = torch.zeros((1, 1, 1, D), dtype=dtype, device="cuda")
+    row.view(-1)[::1001] = 3.0
+    row.view(-1)[-1], row.view(-1)[0] = 5.0, 7.0
+    table, lens = i32([[1]]), i32([1])
+    bv.bv_cache_append(row, row, pool, pool, table, lens)
+    assert torch.equal(pool[1], row[0]) and not pool[0].any() and not pool[2].any()
+    bv.bv_pages_copy(pool, pool, i32([[1, 0]]))
+    assert torch.equal(pool[0], row[0]) and torch.equal(pool[1], row[0]) and not pool[2].any()
