@@ -66,9 +66,9 @@ class Decoder:
 
     def forward(self, tokens: torch.Tensor, lens: torch.Tensor, n_new=None) -> torch.Tensor:
         """Takes the newest tokens [B, n] (the cache has room for them; lens counts them in) through the layers; the logits
-        [B, n, V] after each."""
+        [B, n, V] after each.  What is no token of the vocabulary (padding beyond n_new, a fault's -1) is taken for the nearest one."""
         c, B, n = self.cache, tokens.shape[0], tokens.shape[1]
-        x = self.w["embed"][tokens.clamp_min(0)]
+        x = self.w["embed"][tokens.clamp(0, self.w["embed"].shape[0] - 1)]
         for layer, k, v in zip(self.w["layers"], c.k, c.v):
             qkv = (x @ layer["qkv"]).view(B, n, self.heads + 2 * self.kv_heads, self.D)
             q, kn, vn = qkv.split([self.heads, self.kv_heads, self.kv_heads], dim=2)
@@ -82,7 +82,7 @@ def run(target: Decoder, draft: Decoder, prompts: torch.Tensor, prompt_lens: tor
         gamma: int, temperature: float = 1.0, algo: str = "block_lse", graph: bool = False) -> Dict[str, torch.Tensor]:
     """Run ``u_draft.shape[0]`` iterations of Algorithm 3 on two decoders with empty caches.
 
-    prompts int32 [B, L] (CUDA), of which sequence b has prompt_lens[b] in 1 .. L; u_draft [N, gamma, B] and u_verify [N, B, gamma+2]: float32
+    prompts int32 [B, L] (CUDA), of which sequence b has prompt_lens[b] in 1 .. L (what lies beyond is not looked at); u_draft [N, gamma, B] and u_verify [N, B, gamma+2]: float32
     uniforms; algo as in ``specdec.run``.  Returns ``tokens`` int32 [B, N (gamma+1)] (generated tokens, then -1), ``lengths`` int64 [B], ``tau`` int32
     [N, B] and ``drafted`` int32 [N, B, gamma].  With ``graph`` the iterations after the first are replays of one captured one.
     """
@@ -94,6 +94,11 @@ def run(target: Decoder, draft: Decoder, prompts: torch.Tensor, prompt_lens: tor
         raise ValueError("prompts must be int32 [B, L] and prompt_lens int32 [B]")
     if tuple(u_draft.shape) != (N, gamma, B) or tuple(u_verify.shape) != (N, B, gamma + 2):
         raise ValueError("u_draft must be [N, gamma, B] and u_verify [N, B, gamma+2]")
+    # (one look of the host before anything is indexed by them: what is out of range would be a fault of the device)
+    held = torch.arange(prompts.shape[1], device=prompts.device)[None, :] < prompt_lens[:, None]
+    vocabulary = min(m.w["embed"].shape[0] for m in (target, draft))
+    if bool(((prompt_lens < 1) | (prompt_lens > prompts.shape[1])).any() | (held & ((prompts < 0) | (prompts >= vocabulary))).any()):
+        raise ValueError("prompt_lens must be in 1 .. %d, and tokens of the prompts in 0 .. %d" % (prompts.shape[1], vocabulary - 1))
     dev, width = prompts.device, N * (gamma + 1)
     V = target.w["unembed"].shape[1]
     fault = torch.zeros((1,), dtype=torch.int32, device=dev)
