@@ -212,7 +212,6 @@ int enqueue_attend(const StreamWork& work, void* ctx) {
     auto few_units = [&] {
         const long long tiles = (c.a.n * c.a.group + c.a.rows - 1) / c.a.rows, units = static_cast<long long>(c.a.B) * c.a.Hkv * tiles;
         if (units >= ctas || c.a.B > 32 || tiles > 3) c.a.slack = -1;
-        if (units < ctas) c.a.extra = 0;
     };
     few_units();
     if (c.tiles) {
