@@ -23,7 +23,9 @@ __host__ __device__ __forceinline__ int brought(int m, int n) { return m < 0 ? 0
 __host__ __device__ __forceinline__ int place_of(int len, int m, int t, int width, int page) { return t < m && length_ok(len, width, page) ? len - m + t : -1; }
 
 // Division of numbers below 2^31 by one that the host knows: (n mul / 2^32 + n) / 2^shift.  (A division of unknown integers is some
-// thirty instructions in a row, and the laying out of the work below is a chain of them.)
+// thirty instructions in a row, and the laying out of the work below is a chain of them.)  The method is that of Granlund and Montgomery, "Division by
+// Invariant Integers using Multiplication" (1994), section 4: shift = ceil(log2 by), mul = floor(2^32 (2^shift - by) / by) + 1; sums stay below 2^32
+// since n is below 2^31, which saves their correction step.
 struct Divider {
     unsigned by, mul, shift;
     __device__ __forceinline__ int operator()(int n) const { return static_cast<int>((__umulhi(static_cast<unsigned>(n), mul) + static_cast<unsigned>(n)) >> shift); }

@@ -2,6 +2,7 @@
 import ctypes
 import itertools
 import os
+import random
 import subprocess
 import sys
 
@@ -61,3 +62,15 @@ def test_rows_of_as_many_bytes_as_32_bits_hold_and_more():
             "            assert t.copy(lib, D=D, heads=1, page=1, dtype=dtype) == (-3 if D < 2**30 else -2)\n")
     here = os.path.dirname(os.path.abspath(__file__))
     subprocess.check_call([sys.executable, "-c", code % [os.path.dirname(here), here]])
+
+
+def test_divisions_by_what_the_host_knows(host):
+    """Quotients of everything below 2^31 at which they could differ: multiples of the divisor and their neighbours, the ends."""
+    rng = random.Random(1)
+    divisors = [1, 2, 3, 5, 7, 16, 24, 48, 127, 128, 641, 2**20, 2**30 - 1, 2**30, 2**30 + 1, 2**31 - 2, 2**31 - 1] + [rng.randrange(1, 2**rng.randint(1, 31)) for _ in range(300)]
+    for by in divisors:
+        top = (2**31 - 1) // by
+        near = {0, 1, top, max(0, top - 1), top // 2} | {rng.randint(0, top) for _ in range(20)}
+        for n in {q * by + d for q in near for d in (-1, 0, 1, by - 1)} | {2**31 - 1}:
+            if 0 <= n < 2**31:
+                assert host.host_divide(by, n) == n // by, (by, n)
