@@ -380,6 +380,7 @@ typedef struct bv_cache {
  *   q, out  [B, n, q_heads, D] in the cache's dtype, at strides between sequences, tokens, heads; out must not overlap the inputs
  * Arithmetic: scores, weights and sums in fp32.  16-bit values are multiplied by weights rounded to 16 bits (their sum is taken of the same
  * rounded weights) where the tensor cores do it.  Results do not depend on the order in which CTAs finish.
+ * Forward only: what a drafted block is scored with; there is no backward pass.
  * Any D up to BV_MAX_HEAD_DIM, any page size, any alignment; D a multiple of 8 in 16 .. 128 at 16-byte strides with
  * pages of a multiple of 8 tokens, in bf16, goes through the tensor cores.  scale log2(e) must be finite in 32 bits.
  */

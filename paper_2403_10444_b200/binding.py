@@ -546,7 +546,8 @@ def bv_cache_attend(q, k, v, table, lens, n_new=None, scale: Optional[float] = N
     ``q`` [B, n, q_heads, D]; ``k``, ``v`` [num_pages, heads, page_size, D] (float32 or bfloat16, any strides with contiguous rows);
     ``table`` int32 [B, width], ``lens`` int32 [B] (the newest tokens counted in), ``n_new`` int32 [B] or None: every sequence
     brings n.  ``scale``: 1/sqrt(D) by default; ``window`` > 0: a token sees its last ``window`` positions and the first ``sinks``.
-    Returns ``out`` [B, n, q_heads, D] (rows beyond n_new[b] are not written: zero in a tensor made here)."""
+    Returns ``out`` [B, n, q_heads, D] (rows beyond n_new[b] are not written: zero in a tensor made here).  Forward only: what is returned has no
+    autograd graph, whether or not ``q``, ``k`` or ``v`` require gradients."""
     if stream is not None:
         return _on_stream(stream, lens, bv_cache_attend, q, k, v, table, lens, n_new, scale, window, sinks, out)
     if _fast is not None:
@@ -570,7 +571,7 @@ def bv_cache_attend(q, k, v, table, lens, n_new=None, scale: Optional[float] = N
 
 
 def bv_cache_append(k_new, v_new, k, v, table, lens, n_new=None, stream=None) -> None:
-    """Stores the keys and values of the newest tokens [B, n, heads, D] in the pages of their positions (see include/bv.h)."""
+    """Stores the keys and values of the newest tokens [B, n, heads, D] in the pages of their positions (see include/bv.h); autograd does not see it."""
     if stream is not None:
         return _on_stream(stream, lens, bv_cache_append, k_new, v_new, k, v, table, lens, n_new)
     if _fast is not None:
