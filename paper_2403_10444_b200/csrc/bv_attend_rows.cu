@@ -6,15 +6,15 @@
 // that lags by up to 8 costs nothing in 32 bits (terms of up to 256 instead of 1) and saves nearly all of the scaling.
 // A weight of zero takes no value, whatever that is.
 //
-// (18 sequences of up to 8563 tokens, blocks of 6 tokens, 14 heads on 2, D = 128: 182 us, 3.7 times the FMAs' floor; single tokens, 32 heads on 8, 16
-// sequences of up to 4096: 84 us, 3.7 TB/s.)
+// (18 sequences of up to 8563 tokens, blocks of 6 tokens, 14 heads on 2, D = 128: 189 us, 3.9 times the FMAs' floor; single tokens, 32 heads on 8, 16
+// sequences of up to 4096: 71 us, 4.4 TB/s, 64 of up to 8192: 394 us, 5.8 TB/s.)
 // Two kernels.  Few query rows (a token of a group of up to 4 heads): the call is a matter of reading the cache.  Eight lanes share
 // a key, each with every 8th group of four of its D elements, of 4 query rows at a time, in registers; a warp has 4 keys of each tile
 // of 32, and every thread copies what it will read itself into a ring of cells of its own, several tiles ahead, so no thread
 // waits for another until the unit ends.  More rows: reading shared memory and the FMAs
 // bound (a 16-byte read takes a warp four clocks, wherever it goes).  A tile of 64 keys lies there, and both products are tiled in
 // registers: S by 4 rows x 8 keys a thread with a fourth of D each, O by 8 rows x 8 columns with every 4th or 8th key (2 x 4 and 8 x 4 with no
-// such splits: 206 us against 182 for 18 sequences of up to 8563 keys, 42 rows on 2 heads, D = 128).
+// such splits: 206 us against 182, when they were built, for 18 sequences of up to 8563 keys, 42 rows on 2 heads, D = 128).
 #include "bv_cache.cuh"
 #include "bv_launch.h"
 
@@ -338,7 +338,7 @@ struct ManySmem {
 };
 
 // PARTS: 32 / PARTS rows at most, whose keys are shared out to as many warps (8 rows of all keys would leave six of eight warps idle in either product:
-// 72.4 us against 56.8 for 16 sequences of up to 4096 tokens, 8 rows, D = 128; 16 rows 76.3 against 69.2).
+// 78.3 us against 59.6 for 16 sequences of up to 4096 tokens, 4 key-value heads, 8 rows, D = 128; 16 rows 81.4 against 73.2).
 template <typename T, int NJ, int PARTS>
 __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendArgs a, const int aligned, const int q_vec) {
     extern __shared__ __align__(16) char raw[];
@@ -629,8 +629,8 @@ cudaError_t pick_many(const AttendArgs& a, bool aligned, bool q_vec, int ctas, c
     return launch_many<T, NJ, 1>(a, aligned, q_vec, ctas, stream);
 }
 // Up to 4 rows (2 where D is beyond 128), which the kernel that reads takes in one pass, are its; the others the one's that multiplies.  16 sequences
-// of up to 4096 tokens, 4 key-value heads: 4 rows 52.7 and 55.6 us (D = 128), 36.4 and 40.4 (64), 8 rows 93.0 and 56.8, 64.4 and 40.1; D = 256:
-// 2 rows 92.5 and 105.6, 4 rows 149.9 and 105.6.
+// of up to 4096 tokens, 4 key-value heads: 4 rows 44.1 and 54.6 us (D = 128), 34.6 and 42.7 (64), 8 rows 69.8 and 59.6, 54.8 and 45.2; D = 256:
+// 2 rows 73.6 and 92.2, 4 rows 106.3 and 92.2.
 constexpr int few_each(int D) { return D <= 128 ? 4 : 2; }
 bool few(int D, int rows) { return rows <= few_each(D); }
 template <typename T>

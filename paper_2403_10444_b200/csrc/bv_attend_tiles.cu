@@ -1,10 +1,11 @@
 // Attention over a paged cache in 16 bits on the tensor cores: bv_cache_attend for bf16, D a multiple of 8 up to 128, pages of a
 // multiple of 8 tokens, rows at 16-byte strides.
 //
-// Bound by the cache's bytes: 64 sequences of up to 8192 tokens, 32 heads on 8, D = 128: 194 us, 5.9 TB/s (0.90 of the copy bandwidth); one of
-// 131072: 94 us, 5.7 TB/s; blocks of 9 tokens, 64 heads on 8, 64 sequences of up to 16384: 372 us, 6.2 TB/s, at 1965 MHz; called
-// without a pause the GPU reaches its 1000 W and 1560 MHz, and the call 447.  Small
-// calls by the chain of steps: 7.2 us for a tile of one unit, 11 with a join.
+// Bound by the cache's bytes: 64 sequences of up to 8192 tokens, 32 heads on 8, D = 128: 195 us, 5.9 TB/s (0.90 of the copy bandwidth); one of
+// 131072: 94 us, 5.7 TB/s; blocks of 9 tokens, 64 heads on 8, 64 sequences of up to 16384: 402 to 411 us, 5.7 TB/s, a few calls after a pause; called
+// in a loop the GPU reaches its 1000 W and 1560 MHz, and a call takes 449 to 483 (box by box).  Small
+// calls by the chain of steps: 7.2 us for a tile of one unit, 11 with a join.  Prompts by the products, of which a tile's keys feed 80 rows: 4 of 2048
+// tokens, 32 heads on 8, D = 128: 434 us, 320 TFLOP/s; of 8192: 4.4 ms, 500.
 //
 // A unit is one key-value head of a sequence with up to N query rows (the heads of its group times the block's tokens), a tile
 // 128 keys.  Keys are the large side, so they take the M side of the matrix instructions and nothing is padded but N, to 16:

@@ -48,11 +48,12 @@ __host__ __device__ __forceinline__ int sum_up_to(int most, int sum, int more) {
 // (Lengths lie on the device and change from call to call, so the list is laid out by the kernel itself: equal parts keep
 // every SM at work whatever the lengths are, where a grid of (sequence, head, fixed pieces) waits for the longest sequence.  Units of
 // different sequences are not equally long, so some CTAs have twelve ends of units where others have three: each counts as `extra` tiles in
-// front of its own; so too where the list is cut although units are fewer than CTAs, by which 150 such calls took 0.94 of the time on average, 0.70 to 1.05.)
+// front of its own; so too where the list is cut although units are fewer than CTAs, by which 250 such calls took 0.96 of the time on average, 0.70 to 1.05.)
 // With fewer units than CTAs the cuts of equal parts leave CTAs the end of one unit and the beginning of another, which they go through one
 // after the other.  There a CTA has a part of one unit instead: a unit of t tiles is one CTA's up to `whole` tiles and else cut into
 // ceil(t / T) equal parts, with the least T for which the CTAs suffice, if the longest part is at most `slack` tiles more than an equal one.
-// (8 sequences of 2000 tokens, 8 heads on 2, D = 128: 13.1 us against 15.0; in 32 bits 15.9 against 21.2.  250 tokens: 8.7 against 11.4.)
+// (8 sequences of 2000 tokens, 8 heads on 2, D = 128: 13.4 us against 14.0 for the list; in 32 bits 15.4 against 16.3.  250 tokens: 9.3 against 9.6, 10.9
+// against 11.9.)
 struct AttendArgs {
     const void* q;
     void* out;
