@@ -135,7 +135,7 @@ struct Shape {
     static constexpr int kKeys = 8, kValues = 9, kIssuer = 10;           // warps: loads of keys, of values, products
     static constexpr int kPanel = kTile * 128, kSlot = NP * kPanel;      // a slot: NP panels of 128 rows of 64 columns
     static constexpr int kQ = NP * N * 128, kP = N * kTile * 2;
-    static constexpr int kRest = N > 64 ? 4096 : 3072;
+    static constexpr int kRest = (N > 64 ? 4 : 3) * 1024;
     // two buffers for the weights (the next tile's are formed while the last one's are multiplied) where that leaves five slots
     static constexpr int kTwo = (227 * 1024 - kRest - kTeams * kQ - 2 * kP) / kSlot;
     static constexpr int kBuffers = kTwo >= 5 ? 2 : 1;
