@@ -6,8 +6,8 @@
 // that lags by up to 8 costs nothing in 32 bits (terms of up to 256 instead of 1) and saves nearly all of the scaling.
 // A weight of zero takes no value, whatever that is.
 //
-// (18 sequences of up to 8563 tokens, blocks of 6 tokens, 14 heads on 2, D = 128: 189 us, 3.9 times the FMAs' floor; single tokens, 32 heads on 8, 16
-// sequences of up to 4096: 71 us, 4.4 TB/s, 64 of up to 8192: 394 us, 5.8 TB/s.)
+// (18 sequences of up to 8563 tokens, blocks of 6 tokens, 14 heads on 2, D = 128: 186 us, 3.8 times the FMAs' floor; single tokens, 32 heads on 8, 16
+// sequences of up to 4096: 66 us, 4.7 TB/s, 64 of up to 8192: 387 us, 5.9 TB/s.)
 // Two kernels.  Few query rows (a token of a group of up to 4 heads): the call is a matter of reading the cache.  Eight lanes share
 // a key, each with every 8th group of four of its D elements, of 4 query rows at a time, in registers; a warp has 4 keys of each tile
 // of 32, and every thread copies what it will read itself into a ring of cells of its own, several tiles ahead, so no thread
@@ -341,7 +341,7 @@ struct ManySmem {
 };
 
 // PARTS: 32 / PARTS rows at most, whose keys are shared out to as many warps (8 rows of all keys would leave six of eight warps idle in either product:
-// 78.3 us against 59.6 for 16 sequences of up to 4096 tokens, 4 key-value heads, 8 rows, D = 128; 16 rows 81.4 against 73.2).
+// 76.8 us against 59.8 for 16 sequences of up to 4096 tokens, 4 key-value heads, 8 rows, D = 128; 16 rows 80.2 against 72.5).
 template <typename T, int NJ, int PARTS>
 __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const AttendArgs a, const int aligned, const int q_vec) {
     extern __shared__ __align__(16) char raw[];
@@ -632,8 +632,8 @@ cudaError_t pick_many(const AttendArgs& a, bool aligned, bool q_vec, int ctas, c
     return launch_many<T, NJ, 1>(a, aligned, q_vec, ctas, stream);
 }
 // Up to 4 rows (2 where D is beyond 128), which the kernel that reads takes in one pass, are its; the others the one's that multiplies.  16 sequences
-// of up to 4096 tokens, 4 key-value heads: 4 rows 44.1 and 54.6 us (D = 128), 34.6 and 42.7 (64), 8 rows 69.8 and 59.6, 54.8 and 45.2; D = 256:
-// 2 rows 73.6 and 92.2, 4 rows 106.3 and 92.2.
+// of up to 4096 tokens, 4 key-value heads: 4 rows 41.2 and 55.2 us (D = 128), 32.6 and 43.0 (64), 8 rows 67.0 and 59.8, 50.9 and 45.4; D = 256:
+// 2 rows 59.3 and 93.6, 4 rows 89.6 and 93.5 (64 sequences: 352.7 and 312.5).
 constexpr int few_each(int D) { return D <= 128 ? 4 : 2; }
 bool few(int D, int rows) { return rows <= few_each(D); }
 template <typename T>
