@@ -435,6 +435,79 @@ int bv_pages_compact(const bv_cache* cache, int32_t* out_moves, int32_t* out_cou
 int bv_pages_copy(const bv_cache* cache, const int32_t* pairs, int n_pairs, const int32_t* count, void* stream);
 
 /*
+ * bv_cache_append with rotary positions on the way: the queries and keys of the newest tokens are turned by the angles of their positions, keys
+ * and values go into their pages.  Of each head's first `rot` elements pair i becomes
+ *   mscale (x cos a - y sin a,  y cos a + x sin a),   a = position freq[i]
+ * where (x, y) are elements i and i + rot / 2, or (interleaved) 2 i and 2 i + 1; the other elements stay as they are.  Frequencies are the caller's, so
+ * any scaling for long contexts is one of freq and mscale.  The angle is formed in 64 bits; sine, cosine and products in 32; results are rounded once.
+ * Two layouts of the new tokens:
+ *   offsets null: [B, n, heads, D], row t < m_b (m_b as in bv_cache_attend) of sequence b, at strides between sequences, tokens, heads;
+ *   else packed:  [n, heads, D], rows offsets[b] .. offsets[b + 1] - 1 of sequence b, m_b = offsets[b + 1] - offsets[b] (offsets [B + 1], ascending, 0 or
+ *                 more, read on the device; n_new null; the first of the three strides is not looked at)
+ * and the token's position is lens[b] - m_b + t.  Rows that belong to no sequence's newest tokens are left as they were.
+ *   out_q  like q (may be q itself); q_heads 0: no queries (q and out_q are not looked at)
+ *   out_k  like k_new (may be k_new itself): the turned keys, as bv_prompt_attend takes them; null: only in the pages
+ * Where bv_cache_append stores nothing (a position below 0, a length that is none, a page that is none) nothing is stored; queries (and out_k) are
+ * turned by the position as it comes out in 32 bits.
+ * Limits (BV_ERR_UNSUPPORTED beyond): q_heads + 2 heads 65536, D 4096, rows 2^31 - 1.
+ */
+typedef struct bv_rotary {
+    const double* freq;       /* [rot / 2] DEVICE, radians per position */
+    int32_t rot;              /* elements of a head that turn: even, 2 .. D */
+    int32_t interleaved;      /* 0: pairs (i, i + rot / 2); else (2 i, 2 i + 1) */
+    float mscale;             /* what turned elements are multiplied by */
+    int32_t reserved;
+} bv_rotary;
+int bv_cache_append_rotary(const bv_cache* cache, const bv_rotary* rotary, const void* q, const int64_t* q_stride, int q_heads, const void* k_new,
+                           const int64_t* k_new_stride, const void* v_new, const int64_t* v_new_stride, const int32_t* n_new, const int32_t* offsets, int n,
+                           void* out_q, const int64_t* out_q_stride, void* out_k, const int64_t* out_k_stride, void* stream);
+
+/*
+ * Attention of whole prompts that lie one after the other: rows offsets[b] .. offsets[b + 1] - 1 are sequence b's (offsets [B + 1] int32, ascending,
+ * 0 or more, read on the device), and its token i sees the tokens j <= i of the same sequence, with window > 0 only j > i - window or j < sinks:
+ *   out[i, h] = sum_j w_j v[j, h'] / sum_j w_j,   w_j = exp(scale q[i, h] . k[j, h']),   h' = h / (q_heads / heads)
+ *   q, out [tokens, q_heads, D], k, v [tokens, heads, D] in `dtype`, DEVICE, at strides (elements, 0 or more) between tokens and heads, D contiguous;
+ *          out must not overlap the inputs
+ * Rows that belong to no sequence (behind the last, before the first) are left as they were; a sequence whose offsets are out of order or beyond
+ * `tokens` has no rows (rows that sequences share, where offsets do not ascend, get one's result or are left).  A row whose scores are all -inf is NaN.  What a row does not see does not count, whatever it holds (infinities and NaN too).
+ * Arithmetic and rounding as in bv_cache_attend.  Forward only.
+ * Any D up to BV_MAX_HEAD_DIM at any alignment; D a multiple of 8 in 16 .. 128 at 16-byte strides in bf16 goes through the tensor cores.
+ * scale log2(e) must be finite in 32 bits.  Limits (BV_ERR_UNSUPPORTED beyond): tokens 2^30, B 2^20.
+ */
+int bv_prompt_attend(const void* q, const int64_t* q_stride, const void* k, const int64_t* k_stride, const void* v, const int64_t* v_stride,
+                     const int32_t* offsets, int B, int tokens, int q_heads, int heads, int D, int dtype, float scale, int window, int sinks,
+                     void* out, const int64_t* out_stride, void* stream);
+
+/*
+ * Rows of logits cut to what a sampler keeps, and a token drawn from that.  Of a row's tokens in order, larger logits first and equal ones by
+ * index, with weights exp(z / temperature):
+ *   top_k  the first k (0 or less, or V and more: all)
+ *   top_p  of these, those before which less than top_p of their mass lies, the first always (1 and more: all)
+ *   min_p  those whose weight is at least min_p times the first one's (0: all)
+ * are kept.  Then, with uniforms (else out_tokens and out_lse are null):
+ *   out_tokens[r]  drawn from the kept weights by inverse CDF in vocabulary-index order with uniforms[r], the convention of bv_sample_draft
+ *   out_lse[r]     ln of the sum of the kept exp(z / temperature) (may be null)
+ * and with out_logits (may be null with uniforms; may be logits itself) the row with every other logit at -inf: what the verifications take, so a block
+ * that was drafted from cut rows is verified by cut rows of both models and `out_lse`.
+ *   logits [rows, V], out_logits [rows, V] in `dtype` at strides (elements) between rows, any V and alignment
+ * Weights and their sums are formed in 64 bits, so that borders lie where the formulas have them.  Each of a cut's numbers is one for all rows, or
+ * a DEVICE array [rows].  A row with a NaN or +inf logit or without a finite one gives the token -1 and the normaliser NaN and is copied as it is; one
+ * whose own numbers are out of range (temperature not positive or not finite, top_p or min_p negative or NaN, min_p above 1) the same, and becomes NaN.
+ * Limits (BV_ERR_UNSUPPORTED beyond): V 2^26, rows 2^27.
+ */
+typedef struct bv_cut {
+    const float* temperatures;    /* [rows] DEVICE, or null: temperature */
+    const int32_t* top_ks;        /* the same for the others             */
+    const float* top_ps;
+    const float* min_ps;
+    float temperature;
+    int32_t top_k;
+    float top_p, min_p;
+} bv_cut;
+int bv_sample_filtered(const void* logits, int64_t stride, const float* uniforms, int rows, int V, int dtype, const bv_cut* cut, int32_t* out_tokens,
+                       float* out_lse, void* out_logits, int64_t out_stride, void* stream);
+
+/*
  * Waits for `stream` and reports whether a device-side wait of any call enqueued on it since the
  * last query gave up: BV_ERR_TIMEOUT (the outputs of those calls are not to be used; the library's
  * state is intact and later calls work) or BV_OK.  Every device-side wait of this library is

@@ -7,6 +7,7 @@ point reports an error, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import struct
 from typing import Optional, Tuple
@@ -26,7 +27,7 @@ DTYPE_BF16 = 1
 
 # every symbol include/bv.h declares
 EXPORTS = ["bv_verify", "tv_verify", "bv_verify_ex", "tv_verify_ex", "bv_verify_host",
-           "tv_verify_host", "bv_verify_noalloc", "bv_verify_lse", "bv_verify_lse_ex", "tv_verify_lse", "tv_verify_lse_ex", "gbv_verify", "gbv_verify_ex", "bv_verify_probs", "tv_verify_probs", "bv_sample_draft", "bv_draft_chain", "bv_decode_loop", "bv_cache_attend", "bv_cache_append", "bv_pages_extend", "bv_pages_truncate", "bv_pages_fork", "bv_pages_compact", "bv_pages_copy", "bv_stream_status", "bv_set_option", "bv_release", "bv_last_launch_count", "bv_last_kernel", "bv_last_cuda_error",
+           "tv_verify_host", "bv_verify_noalloc", "bv_verify_lse", "bv_verify_lse_ex", "tv_verify_lse", "tv_verify_lse_ex", "gbv_verify", "gbv_verify_ex", "bv_verify_probs", "tv_verify_probs", "bv_sample_draft", "bv_draft_chain", "bv_decode_loop", "bv_cache_attend", "bv_cache_append", "bv_pages_extend", "bv_pages_truncate", "bv_pages_fork", "bv_pages_compact", "bv_pages_copy", "bv_cache_append_rotary", "bv_prompt_attend", "bv_sample_filtered", "bv_stream_status", "bv_set_option", "bv_release", "bv_last_launch_count", "bv_last_kernel", "bv_last_cuda_error",
            "bv_status_string", "bv_version"]
 
 
@@ -76,6 +77,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.bv_pages_fork.argtypes = [vp, vp, vp, ci, vp, vp]
     lib.bv_pages_compact.argtypes = [vp, vp, vp, vp]
     lib.bv_pages_copy.argtypes = [vp, vp, ci, vp, vp]
+    lib.bv_cache_append_rotary.argtypes = [vp, vp, vp, vp, ci, vp, vp, vp, vp, vp, vp, ci, vp, vp, vp, vp, vp]
+    lib.bv_prompt_attend.argtypes = [vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, cf, ci, ci, vp, vp, vp]
+    lib.bv_sample_filtered.argtypes = [vp, ctypes.c_int64, vp, ci, ci, ci, vp, vp, vp, vp, ctypes.c_int64, vp]
     for name in EXPORTS:
         getattr(lib, name).restype = ci
     lib.bv_stream_status.argtypes = [vp]
@@ -689,3 +693,213 @@ def bv_pages_copy(k, v, pairs, count=None, stream=None) -> None:
         return
     blob = _CACHE.pack(k.data_ptr(), v.data_ptr(), 0, 0, 0, ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], 0, 0, P, page, heads, D, code, 0)
     _enqueue((_lib or load_library()).bv_pages_copy, dev, blob, pairs.data_ptr(), shape[0], upto)
+
+
+# ---- prompts and rotary positions ----
+
+_ROTARY = struct.Struct("@Qiifi")
+
+
+def rotary_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, original: int = 0, low: float = 1.0, high: float = 32.0, device="cuda") -> torch.Tensor:
+    """Frequencies for bv_cache_append_rotary, float64 [rot / 2]: base^(-2 i / rot), radians per position.
+
+    ``factor`` > 1 stretches the context for which they were made: without ``original`` all of them are divided by it (positions interpolated
+    linearly); with ``original``, the context's length before, those that turn fewer than ``low`` times in it are, those that turn more than ``high``
+    times are not, and between the two is a ramp in the number of turns, linear in the index."""
+    if rot < 2 or rot % 2 or not base > 0 or not factor > 0:
+        raise ValueError("rot must be even and at least 2, base and factor positive")
+    f = torch.arange(rot // 2, dtype=torch.float64).mul_(-2.0 * math.log(base) / rot).exp_()
+    if original <= 0 or factor == 1.0:
+        return (f / factor).to(device)
+    if not 0 < low < high:
+        raise ValueError("low must be positive and below high")
+    # (the index at which a pair turns `turns` times over the original context)
+    at = lambda turns: rot * math.log(original / (turns * 2 * math.pi)) / (2 * math.log(base))
+    first, last = max(math.floor(at(high)), 0), min(math.ceil(at(low)), rot - 1)
+    ramp = ((torch.arange(rot // 2, dtype=torch.float64) - first) / max(last - first, 0.001)).clamp_(0, 1)
+    return (f * (1 - ramp) + f / factor * ramp).to(device)
+
+
+def _offsets(offsets, B: int, dev: int):
+    if B < 0 or offsets.dtype is not _I32 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.get_device() != dev:
+        raise ValueError("offsets must be a contiguous int32 tensor [B + 1] on the same device")
+    if offsets.shape[0] != B + 1:
+        raise ValueError("offsets must be [B + 1]")
+    return offsets.data_ptr()
+
+
+def _packed(t, heads: int, D: int, dtype, dev: int, name: str):
+    """(rows, heads, strides) of a tensor [tokens, heads, D] (heads = 0: any number)."""
+    shape, st = t.shape, t.stride()
+    if len(shape) != 3 or shape[2] != D or (heads and shape[1] != heads) or t.dtype is not dtype:
+        raise ValueError("%s must be [tokens, heads, D] of one dtype" % name)
+    if st[2] != 1 or t.get_device() != dev:
+        raise ValueError("%s must have contiguous rows of D on one device" % name)
+    return shape[0], shape[1], st
+
+
+def bv_cache_append_rotary(q, k_new, v_new, k, v, table, lens, freq, n_new=None, offsets=None, interleaved: bool = False, mscale: float = 1.0, out_q=None,
+                           out_k=None, stream=None):
+    """Turns the queries and keys of the newest tokens by the angles of their positions and stores keys and values in their pages (see
+    include/bv.h).
+
+    ``q``, ``k_new``, ``v_new``: [B, n, heads, D], of which sequence b brings n (or n_new[b]), or with ``offsets`` (int32 [B + 1]) packed, [tokens, heads, D].
+    ``q`` None: keys and values only.  ``freq`` float64 [rot / 2]: radians per position (``rotary_frequencies``); the first rot elements of a head turn,
+    in pairs (i, i + rot / 2) or, ``interleaved``, (2 i, 2 i + 1), and are multiplied by ``mscale``.  ``out_q`` (may be ``q``) takes the queries, a tensor made
+    here if None (rows that no sequence brings: zero in it); ``out_k`` (may be ``k_new``), if given, the keys.  Returns ``out_q``.  Autograd does not see it."""
+    if stream is not None:
+        return _on_stream(stream, lens, bv_cache_append_rotary, q, k_new, v_new, k, v, table, lens, freq, n_new, offsets, interleaved, mscale, out_q, out_k)
+    blob, B, heads, D, dtype, dev = _cache(k, v, table, lens)
+    if freq.dtype is not torch.float64 or freq.dim() != 1 or not freq.is_contiguous() or freq.get_device() != dev or freq.shape[0] < 1:
+        raise ValueError("freq must be a contiguous float64 tensor [rot / 2] on the cache's device")
+    if offsets is not None and n_new is not None:
+        raise ValueError("n_new goes with [B, n, heads, D], offsets with packed tokens")
+    at = None if offsets is None else _offsets(offsets, B, dev)
+
+    def rows(t, heads, name):
+        if offsets is None:
+            return _rows(t, B, heads, D, dtype, dev, name)
+        n, heads, st = _packed(t, heads, D, dtype, dev, name)
+        return n, heads, _STRIDES.pack(0, st[0], st[1])
+
+    n, _, ks = rows(k_new, heads, "k_new")
+    n_v, _, vs = rows(v_new, heads, "v_new")
+    q_at, q_heads, qs, out_at, os_, k_at, ok = None, 0, None, None, None, None, None
+    n_q = n
+    if q is not None:
+        n_q, q_heads, qs = rows(q, 0, "q")
+        q_at = q.data_ptr()
+        if out_q is None:
+            out_q = q.new_empty(q.shape) if n_new is None and offsets is None else q.new_zeros(q.shape)
+        else:
+            _written(out_q, "out_q")
+        n_o, _, os_ = rows(out_q, q_heads, "out_q")
+        out_at = out_q.data_ptr()
+        if n_o != n_q:
+            raise ValueError("out_q must have the shape of q")
+    elif out_q is not None:
+        raise ValueError("out_q without q")
+    if out_k is not None:
+        _written(out_k, "out_k")
+        n_o, _, ok = rows(out_k, heads, "out_k")
+        k_at = out_k.data_ptr()
+        if n_o != n:
+            raise ValueError("out_k must have the shape of k_new")
+    if n != n_v or n != n_q:
+        raise ValueError("q, k_new and v_new must have one number of tokens")
+    _written(k, "k")
+    _written(v, "v")
+    new = None if n_new is None else _counted(n_new, B, dev, "n_new")
+    if B == 0 or (offsets is not None and n == 0):
+        return out_q
+    rotary = _ROTARY.pack(freq.data_ptr(), 2 * freq.shape[0], bool(interleaved), mscale, 0)
+    _enqueue((_lib or load_library()).bv_cache_append_rotary, dev, blob, rotary, q_at, qs, q_heads, k_new.data_ptr(), ks, v_new.data_ptr(), vs, new, at, n, out_at, os_, k_at, ok)
+    return out_q
+
+
+def bv_prompt_attend(q, k, v, offsets, scale: Optional[float] = None, window: int = 0, sinks: int = 0, out=None, stream=None):
+    """Causal attention of whole prompts that lie one after the other (see include/bv.h).
+
+    ``q`` [tokens, q_heads, D], ``k``, ``v`` [tokens, heads, D] (float32 or bfloat16, any strides with contiguous rows); ``offsets`` int32 [B + 1]: sequence b is
+    rows offsets[b] .. offsets[b + 1] - 1.  ``scale``: 1/sqrt(D) by default; ``window`` > 0: a token sees its last ``window`` tokens and the first
+    ``sinks``.  Returns ``out`` [tokens, q_heads, D] (rows of no sequence are not written: zero in a tensor made here).  Forward only: what is returned has
+    no autograd graph."""
+    if stream is not None:
+        return _on_stream(stream, offsets, bv_prompt_attend, q, k, v, offsets, scale, window, sinks, out)
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q must be [tokens, q_heads, D], k and v [tokens, heads, D]")
+    D, dtype, dev = k.shape[2], k.dtype, k.get_device()
+    code = _CODES.get(dtype)
+    if code is None:
+        raise TypeError("queries, keys and values must be float32 or bfloat16, got %s" % dtype)
+    if dev < 0:
+        raise ValueError("expected CUDA tensors on one device")
+    n, heads, ks = _packed(k, 0, D, dtype, dev, "k")
+    n_v, _, vs = _packed(v, heads, D, dtype, dev, "v")
+    n_q, q_heads, qs = _packed(q, 0, D, dtype, dev, "q")
+    if n != n_v or n != n_q:
+        raise ValueError("q, k and v must have one number of tokens")
+    at = _offsets(offsets, offsets.shape[0] - 1 if offsets.dim() == 1 else -1, dev)
+    if out is None:
+        out = q.new_zeros((n, q_heads, D))
+    else:
+        _written(out, "out")
+    n_o, _, os_ = _packed(out, q_heads, D, dtype, dev, "out")
+    if n_o != n:
+        raise ValueError("out must have the shape of q")
+    if n == 0 or offsets.shape[0] == 1:
+        return out
+    pack = lambda st: _STRIDES.pack(st[0], st[1], 0)
+    _enqueue((_lib or load_library()).bv_prompt_attend, dev, q.data_ptr(), pack(qs), k.data_ptr(), pack(ks), v.data_ptr(), pack(vs), at, offsets.shape[0] - 1, n, q_heads, heads, D,
+             code, D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), pack(os_))
+    return out
+
+
+# ---- rows of logits, cut ----
+
+_CUT = struct.Struct("@4Qfiff")
+
+
+def _cut(logits, temperature, top_k, top_p, min_p):
+    """The packed settings: each a number, or a tensor with one for each row."""
+    rows, dev = logits.shape[0], logits.get_device()
+
+    def each(x, dtype, name):
+        if not isinstance(x, torch.Tensor):
+            return 0, x
+        if x.dtype is not dtype or tuple(x.shape) != (rows,) or not x.is_contiguous() or x.get_device() != dev:
+            raise ValueError("%s must be a number or a contiguous %s tensor [rows] on the logits' device" % (name, str(dtype)[6:]))
+        return x.data_ptr(), 0
+
+    t, k, p, m = each(temperature, torch.float32, "temperature"), each(top_k, _I32, "top_k"), each(top_p, torch.float32, "top_p"), each(min_p, torch.float32, "min_p")
+    return _CUT.pack(t[0], k[0], p[0], m[0], t[1], min(max(k[1], 0), 2**31 - 1), p[1], m[1])
+
+
+def _logits(t, name: str):
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be [rows, V] with contiguous rows" % name)
+    if not t.is_cuda:
+        raise ValueError("expected CUDA tensors")
+    return t.shape[0], t.shape[1]
+
+
+def _cut_call(logits, uniforms, tokens, lse, out, temperature, top_k, top_p, min_p) -> None:
+    rows, V = _logits(logits, "logits")
+    code, dev = _dtype_code(logits), logits.get_device()
+    if out is not None:
+        if _logits(out, "the filtered logits") != (rows, V) or out.dtype is not logits.dtype or out.get_device() != dev:
+            raise ValueError("the filtered logits must have the shape, dtype and device of the logits")
+        if rows > 1 and out.stride(0) < V:
+            raise ValueError("the filtered logits must not be an expanded tensor")
+    cut = _cut(logits, temperature, top_k, top_p, min_p)
+    if rows == 0:
+        return
+    ptr = lambda t: None if t is None else t.data_ptr()
+    _enqueue((_lib or load_library()).bv_sample_filtered, dev, logits.data_ptr(), logits.stride(0), ptr(uniforms), rows, V, code, cut, ptr(tokens), ptr(lse), ptr(out),
+             0 if out is None else out.stride(0))
+
+
+def bv_sample_filtered(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, want_lse: bool = True, out_logits=None, stream=None):
+    """The drafting step on cut rows (see include/bv.h): of ``logits`` [rows, V] (float32 or bfloat16, CUDA) the ``top_k`` largest (0: all), of these the smallest set
+    with ``top_p`` of their mass, and of these what is at least ``min_p`` times as likely as the first; a token of each row drawn from that with ``uniforms``
+    float32 [rows].  Each setting is a number or a tensor [rows] (float32; top_k int32).  Returns (tokens int32 [rows], lse float32 [rows] or None), lse of the kept
+    tokens; ``out_logits`` (may be ``logits``), if given, takes the rows with all other logits at -inf."""
+    if stream is not None:
+        return _on_stream(stream, logits, bv_sample_filtered, logits, uniforms, temperature, top_k, top_p, min_p, want_lse, out_logits)
+    rows, _ = _logits(logits, "logits")
+    if uniforms.shape != (rows,) or uniforms.dtype is not torch.float32 or not uniforms.is_contiguous() or uniforms.get_device() != logits.get_device():
+        raise ValueError("uniforms must be a contiguous float32 tensor [rows] on the logits' device")
+    tokens = torch.empty((rows,), dtype=torch.int32, device=logits.device)
+    lse = torch.empty((rows,), dtype=torch.float32, device=logits.device) if want_lse else None
+    _cut_call(logits, uniforms, tokens, lse, out_logits, temperature, top_k, top_p, min_p)
+    return tokens, lse
+
+
+def bv_filter_logits(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, stream=None):
+    """``logits`` [rows, V] with all that bv_sample_filtered would not keep at -inf, in ``out`` (may be ``logits``; None: a new tensor)."""
+    if stream is not None:
+        return _on_stream(stream, logits, bv_filter_logits, logits, temperature, top_k, top_p, min_p, out)
+    if out is None:
+        out = torch.empty(tuple(logits.shape), dtype=logits.dtype, device=logits.device)
+    _cut_call(logits, None, None, None, out, temperature, top_k, top_p, min_p)
+    return out
