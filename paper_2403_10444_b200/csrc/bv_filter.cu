@@ -14,6 +14,7 @@
 #include <cmath>
 #include <cstdint>
 
+#include "bv_cache.cuh"
 #include "bv_device.cuh"
 #include "bv_launch.h"
 
@@ -97,96 +98,245 @@ struct Border {
     __device__ __forceinline__ bool keeps(uint32_t k, int i) const { return k > key || (k == key && i <= last); }
 };
 
+constexpr int kBins = 4096;              // of a histogram over values
+constexpr int kList = 4096;              // tokens that are put in order one by one
+constexpr int kMostK = 1024;             // of a top-k by candidates
+constexpr int kFew = 2048;               // tokens of which all are candidates
+
 struct FilterSmem {
-    unsigned count[kDigits];
-    unsigned long long mass[kDigits];
-    double warp_mass[kFWarps];           // read by the other CTAs
-    unsigned warp_count[kFWarps];        // read by the other CTAs
-    float warp_top[kFWarps];             // read by the other CTAs
+    union {
+        unsigned bins[kBins];
+        struct {
+            unsigned count[kDigits];
+            unsigned long long mass[kDigits];
+        };
+        unsigned long long list[kList];  // key, then the index turned round: in order when they descend
+    };
+    double warp_mass[kFWarps], warp_above[kFWarps];      // read by the other CTAs, as are the next four
+    unsigned warp_count[kFWarps];
+    float cta_top, cta_low;
+    int cta_bad;
+    Border border;                       // from the first CTA
+    unsigned listed;                     // (the first CTA's: tokens in its list)
+    float warp_top[kFWarps], warp_low[kFWarps];
     int warp_bad[kFWarps];
     unsigned scan_count[kFWarps];
     unsigned long long scan_mass[kFWarps];
+    double scan_a[kFWarps], scan_b[kFWarps];
     // what a step found
     unsigned digit, found, above;
-    unsigned long long above_mass, total, digit_mass;
+    unsigned long long above_mass;
     int index;
-    double before, whole;
-    int segment;
 };
 
-// NV: vectors a thread holds; 0: it holds none and reads them anew in each pass.
-template <int DT, int NV>
-__global__ void __launch_bounds__(kFThreads, 1) filter_kernel(const FilterArgs a) {
+template <typename T> __device__ __forceinline__ T scanned(T x, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const T u = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += u;
+    }
+    return x;
+}
+__device__ __forceinline__ double summed(double x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+// The n numbers of a list in descending order, by all threads (size: the power of two that holds them; 0 behind them).
+__device__ __forceinline__ void sort_list(unsigned long long* list, int n) {
+    int size = 32;
+    while (size < n) size *= 2;
+    for (int i = n + threadIdx.x; i < size; i += kFThreads) list[i] = 0;
+    __syncthreads();
+    for (int k = 2; k <= size; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+            for (int x = threadIdx.x; x < size / 2; x += kFThreads) {
+                const int i = 2 * x - (x & (j - 1)), o = i + j;      // (i: the x-th index without bit j)
+                const unsigned long long u = list[i], v = list[o];
+                if ((u < v) == ((i & k) == 0)) { list[i] = v; list[o] = u; }
+            }
+            __syncthreads();
+        }
+}
+
+// A CTA's part of a row lies in shared memory where that holds it (RES), else it is read anew in each pass.
+template <int DT, bool RES>
+__global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a) {
     using R = Row<DT>;
     using E = typename R::E;
     constexpr int N = R::kN;
-    __shared__ FilterSmem sm;
+    extern __shared__ __align__(16) char raw[];
+    FilterSmem& sm = *reinterpret_cast<FilterSmem*>(raw);
+    uint4* const part = reinterpret_cast<uint4*>(raw + (sizeof(FilterSmem) + 15) / 16 * 16);
     cg::cluster_group cluster = cg::this_cluster();
     const int C = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
     const int row = static_cast<int>(blockIdx.x) / C;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const char* const in = a.logits + row * a.stride;
+    FilterSmem* const first_cta = cluster.map_shared_rank(&sm, 0);
 
     // a warp has nv runs of 32 vectors, one after the other
-    const int nv = NV ? NV : a.per_cta / (kFThreads * N);
+    const int nv = a.per_cta / (kFThreads * N);
     const int warp_first = rank * a.per_cta + warp * nv * 32 * N;
     auto index_of = [&](int j) { return warp_first + (j * 32 + lane) * N; };
     auto load = [&](int j) {
         const int i = index_of(j);
         uint4 v = make_uint4(R::kNegInf, R::kNegInf, R::kNegInf, R::kNegInf);
-        if (a.vec_in && i + N <= a.V) return *reinterpret_cast<const uint4*>(in + static_cast<long long>(i) * sizeof(E));
+        if (a.vec_in && i + N <= a.V) return ld_stream_v4(in + static_cast<long long>(i) * sizeof(E));
         E* e = reinterpret_cast<E*>(&v);
 #pragma unroll
         for (int x = 0; x < N; ++x)
             if (i + x < a.V) e[x] = reinterpret_cast<const E*>(in)[i + x];
         return v;
     };
-    uint4 held[NV ? NV : 1];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) held[j] = load(j);
+    uint4* const mine = part + warp * nv * 32 + lane;
     // f(vector, index of its first element), in the order of the row within a warp
     auto each = [&](auto&& f) {
-        if constexpr (NV > 0) {
-#pragma unroll
-            for (int j = 0; j < NV; ++j) f(held[j], index_of(j));
-        } else {
 #pragma unroll 1
-            for (int j = 0; j < nv; ++j) f(load(j), index_of(j));
-        }
+        for (int j = 0; j < nv; ++j) f(RES ? mine[j * 32] : load(j), index_of(j));
     };
 
-    // ---- the largest, and what cannot be read ----
+    // ---- the largest of all, the least of the threads' largest, and what cannot be read ----
     float top = -INFINITY;
     bool bad = false;
-    each([&](const uint4& v, int) {
+    {
+        constexpr int kAhead = 4;
+#pragma unroll 1
+        for (int j0 = 0; j0 < nv; j0 += kAhead) {
+            uint4 v[kAhead];
 #pragma unroll
-        for (int x = 0; x < N; ++x) {
-            const float z = R::get(v, x);
-            bad |= !(z < INFINITY);
-            top = fmaxf(top, z);
+            for (int j = 0; j < kAhead; ++j)
+                if (j0 + j < nv) v[j] = load(j0 + j);
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                if (j0 + j >= nv) break;
+                if (RES) mine[(j0 + j) * 32] = v[j];
+#pragma unroll
+                for (int x = 0; x < N; ++x) {
+                    const float z = R::get(v[j], x);
+                    bad |= !(z < INFINITY);
+                    top = fmaxf(top, z);
+                }
+            }
         }
-    });
+        // (threads without an element that is finite have no part in the least)
+        float low = top > -INFINITY ? top : INFINITY;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    bad = __any_sync(0xffffffffu, bad);
-    if (lane == 0) { sm.warp_top[warp] = top; sm.warp_bad[warp] = bad; }
-    cluster.sync();
-    for (int r = 0; r < C; ++r) {
-        const FilterSmem* o = cluster.map_shared_rank(&sm, r);
-        for (int w = 0; w < kFWarps; ++w) {
-            top = fmaxf(top, o->warp_top[w]);
-            bad |= o->warp_bad[w] != 0;
+        for (int o = 16; o > 0; o >>= 1) {
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
+        }
+        bad = __any_sync(0xffffffffu, bad);
+        if (lane == 0) { sm.warp_top[warp] = top; sm.warp_low[warp] = low; sm.warp_bad[warp] = bad; }
+        for (int x = tid; x < kBins; x += kFThreads) sm.bins[x] = 0;
+        if (tid == 0) sm.listed = 0;
+        __syncthreads();
+        if (warp == 0) {
+            top = lane < kFWarps ? sm.warp_top[lane] : -INFINITY;
+            low = lane < kFWarps ? sm.warp_low[lane] : INFINITY;
+            bad = lane < kFWarps && sm.warp_bad[lane];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
+            }
+            bad = __any_sync(0xffffffffu, bad);
+            if (lane == 0) { sm.cta_top = top; sm.cta_low = low; sm.cta_bad = bad; }
         }
     }
+    cluster.sync();
+    float low = INFINITY;
+    {
+        const FilterSmem* o = cluster.map_shared_rank(&sm, lane < C ? lane : 0);
+        top = o->cta_top;
+        low = o->cta_low;
+        bad = o->cta_bad != 0;
+#pragma unroll
+        for (int x = 4; x > 0; x >>= 1) {              // (8 CTAs at most; lanes beyond them have the first's)
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+            low = fminf(low, __shfl_xor_sync(0xffffffffu, low, x));
+            bad |= __shfl_xor_sync(0xffffffffu, static_cast<int>(bad), x) != 0;
+        }
+        top = __shfl_sync(0xffffffffu, top, 0);
+        low = __shfl_sync(0xffffffffu, low, 0);
+        bad = __shfl_sync(0xffffffffu, static_cast<int>(bad), 0) != 0;
+    }
     const float T = a.temperatures ? a.temperatures[row] : a.temperature, p = a.top_ps ? a.top_ps[row] : a.top_p, m = a.min_ps ? a.min_ps[row] : a.min_p;
-    const int k = a.top_ks ? a.top_ks[row] : a.top_k;
+    int k = a.top_ks ? a.top_ks[row] : a.top_k;
+    if (k <= 0 || k > a.V) k = a.V;
+    if (p == 0.f) k = 1;                               // (the first one always)
     const bool wrong = !(T > 0.f && T < INFINITY && p >= 0.f && m >= 0.f && m <= 1.f);
     bad |= top == -INFINITY || wrong;
-    const double scale = 1.4426950408889634073599246810019 / static_cast<double>(T), M = static_cast<double>(top);
+    const double scale = 1.4426950408889634073599246810019 / static_cast<double>(T), M = static_cast<double>(top), share = static_cast<double>(p);
     auto weight = [&](float z) { return pow2((static_cast<double>(z) - M) * scale); };
     auto fixed = [&](float z) { return static_cast<unsigned long long>(__double2ull_rn(weight(z) * static_cast<double>(1ull << a.fixed))); };
-
+    // min-p: the lowest value of the type that is not below its border
+    uint32_t least = 0;
+    if (m > 0.f) {
+        float x = __double2float_ru(M + static_cast<double>(T) * log(static_cast<double>(m)));
+        if constexpr (DT == kBF16) x = __bfloat162float(__float2bfloat16_ru(x));
+        least = key_of<DT>(x);
+    }
     Border border{kLowest<DT>, kAll};
+    // tokens, by whole warps, into the first CTA's list
+    auto enlist = [&](bool in, uint32_t key, int index) {
+        const unsigned who = __ballot_sync(0xffffffffu, in);
+        if (who == 0) return;
+        unsigned at = 0;
+        if (lane == 0) at = atomicAdd(&first_cta->listed, static_cast<unsigned>(__popc(who)));
+        at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1));
+        if (in && at < kList) first_cta->list[at] = static_cast<unsigned long long>(key) << 32 | (0xffffffffu - static_cast<unsigned>(index));
+    };
+    // This CTA's and the others' bins, eight a thread from 8 tid on.
+    auto gather = [&](unsigned (&c)[8]) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) c[x] = 0;
+        for (int r = 0; r < C; ++r) {
+            const uint4* o = reinterpret_cast<const uint4*>(cluster.map_shared_rank(&sm, r)->bins) + 2 * tid;
+            const uint4 u = o[0], v = o[1];
+            c[0] += u.x; c[1] += u.y; c[2] += u.z; c[3] += u.w;
+            c[4] += v.x; c[5] += v.y; c[6] += v.z; c[7] += v.w;
+        }
+    };
+    // The sum of x over the threads before this one; `all`: of all threads.
+    auto before_me = [&](double x, double* slots, double* all) {
+        const double inc = scanned(x, lane);
+        if (lane == 31) slots[warp] = inc;
+        __syncthreads();
+        double b = inc - x, total = 0.0;
+        for (int w = 0; w < kFWarps; ++w) {
+            if (w < warp) b += slots[w];
+            total += slots[w];
+        }
+        *all = total;
+        return b;
+    };
+    // In the first CTA: of its list of n in order, which are the row's first but for what has `above` of the mass, those before which there is less than
+    // `target`, at most `most` of them.
+    auto end_of_list = [&](int n, int most, double above, double target) {
+        if (n > most) n = most;
+        // a thread has consecutive ones
+        const int each_has = (n + kFThreads - 1) / kFThreads, i0 = tid * each_has;
+        double w = 0.0, all;
+        for (int x = i0; x < i0 + each_has && x < n; ++x) w += weight(value_of<DT>(static_cast<uint32_t>(sm.list[x] >> 32)));
+        double b = above + before_me(w, sm.scan_a, &all);
+        if (tid == 0) sm.found = 0;
+        __syncthreads();
+        const double limit = target < 0.0 ? share * (above + all) : target;
+        unsigned kept = 0;
+        for (int x = i0; x < i0 + each_has && x < n; ++x) {
+            if (p < 1.f && !(b < limit) && !(above == 0.0 && x == 0)) break;
+            kept = x + 1;
+            b += weight(value_of<DT>(static_cast<uint32_t>(sm.list[x] >> 32)));
+        }
+        if (kept) atomicMax(&sm.found, kept);
+        __syncthreads();
+        return static_cast<int>(sm.found);
+    };
+    auto entry = [&](int x) { return Border{static_cast<uint32_t>(sm.list[x] >> 32), static_cast<int>(0xffffffffu - static_cast<uint32_t>(sm.list[x]))}; };
+    auto announce = [&](Border b) {
+        if (tid < C) cluster.map_shared_rank(&sm, tid)->border = b;
+    };
     // One digit after the other, from the top: the largest key of which `enough` is true once all larger ones and its own are counted in.
     auto select = [&](bool by_mass, int k, double target_share) {
         const Border among = border;
@@ -291,20 +441,20 @@ __global__ void __launch_bounds__(kFThreads, 1) filter_kernel(const FilterArgs a
         border = Border{key, kAll};
         if (some == ties) return;
         // the index of the last of them: ties by warp, then in the warp that has it
-        unsigned mine = 0;
+        unsigned own = 0;
         each([&](const uint4& v, int) {
 #pragma unroll
-            for (int x = 0; x < N; ++x) mine += key_of<DT>(R::get(v, x)) == key;
+            for (int x = 0; x < N; ++x) own += key_of<DT>(R::get(v, x)) == key;
         });
-        mine = __reduce_add_sync(0xffffffffu, mine);
-        if (lane == 0) sm.warp_count[warp] = mine;
+        own = __reduce_add_sync(0xffffffffu, own);
+        if (lane == 0) sm.warp_count[warp] = own;
         cluster.sync();
         unsigned before = 0;
         for (int r = 0; r <= rank; ++r) {
             const FilterSmem* o = cluster.map_shared_rank(&sm, r);
             for (int x = 0; x < (r == rank ? warp : kFWarps); ++x) before += o->warp_count[x];
         }
-        if (before < some && before + mine >= some) {
+        if (before < some && before + own >= some) {
             unsigned need = some - before;
             int last = -1;
             each([&](const uint4& v, int i) {
@@ -332,35 +482,257 @@ __global__ void __launch_bounds__(kFThreads, 1) filter_kernel(const FilterArgs a
         cluster.sync();
         border.last = sm.index;
     };
-    if (!bad) {
-        if (k > 0 && k < a.V) select(false, k, 0.0);
-        if (p == 0.f) select(false, 1, 0.0);
-        else if (p < 1.f) select(true, 0, static_cast<double>(p));
-        if (m > 0.f) {
-            // (the lowest value of the type that is not below)
-            float low = __double2float_ru(M + static_cast<double>(T) * log(static_cast<double>(m)));
-            if constexpr (DT == kBF16) low = __bfloat162float(__float2bfloat16_ru(low));
-            const uint32_t least = key_of<DT>(low);
-            if (least > border.key) border = Border{least, kAll};
-        }
-    }
 
-    // ---- the token ----
-    if (a.uniforms) {
-        double mine = 0.0;
-        if (!bad) {
+    // Top-k of up to kMostK by candidates: what is not below the k-th largest of the vectors' maxima, or nearly so.  False: too many.
+    bool drew = false;
+    auto by_candidates = [&]() {
+        float limit = -INFINITY;
+        if (a.V > kFew) {
+            const float step = (kBins - 1) / (top - low);
+            if (!(step > 0.f && step < INFINITY)) return false;
+            each([&](const uint4& v, int) {
+                float z = R::get(v, 0);
+#pragma unroll
+                for (int x = 1; x < N; ++x) z = fmaxf(z, R::get(v, x));
+                const float d = (top - z) * step;
+                if (d < kBins) atomicAdd(&sm.bins[static_cast<int>(d)], 1u);
+            });
+            cluster.sync();
+            unsigned c[8], sum = 0;
+            gather(c);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) sum += c[x];
+            const unsigned inc = scanned(sum, lane);
+            if (lane == 31) sm.scan_count[warp] = inc;
+            if (tid == 0) sm.found = kBins;
+            __syncthreads();
+            unsigned upto = inc - sum;
+            for (int w = 0; w < warp; ++w) upto += sm.scan_count[w];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                if (upto < static_cast<unsigned>(k) && upto + c[x] >= static_cast<unsigned>(k)) sm.found = 8 * tid + x;
+                upto += c[x];
+            }
+            cluster.sync();                              // (the bins have been read)
+            const int bin = static_cast<int>(sm.found);
+            if (bin >= kBins) return false;
+            // every vector of the bins up to this one has a maximum whose distance comes out below bin + 1
+            limit = static_cast<float>(bin + 1);
+            const float step_ = step;
+            each([&](const uint4& v, int i) {
+                float z = R::get(v, 0);
+#pragma unroll
+                for (int x = 1; x < N; ++x) z = fmaxf(z, R::get(v, x));
+                if (!__any_sync(0xffffffffu, (top - z) * step_ < limit)) return;
+#pragma unroll
+                for (int x = 0; x < N; ++x) {
+                    const float y = R::get(v, x);
+                    enlist((top - y) * step_ < limit, key_of<DT>(y), i + x);
+                }
+            });
+        } else {
             each([&](const uint4& v, int i) {
 #pragma unroll
                 for (int x = 0; x < N; ++x) {
-                    const float z = R::get(v, x);
-                    const uint32_t key = key_of<DT>(z);
-                    if (key > kLowest<DT> && border.keeps(key, i + x)) mine += weight(z);
+                    const float y = R::get(v, x);
+                    enlist(y > -INFINITY, key_of<DT>(y), i + x);
                 }
             });
         }
+        cluster.sync();
+        const int n = static_cast<int>(first_cta->listed);
+        if (n > kList) return false;
+        if (rank == 0) {
+            sort_list(sm.list, n);
+            int kept = end_of_list(n, k, 0.0, -1.0);
+            // (of keys in order, those below min-p's border come last)
+            if (least > 0) {
+                __syncthreads();
+                if (tid == 0) sm.found = 0;
+                __syncthreads();
+                for (int x = tid; x < kept; x += kFThreads)
+                    if (static_cast<uint32_t>(sm.list[x] >> 32) >= least) atomicMax(&sm.found, static_cast<unsigned>(x + 1));
+                __syncthreads();
+                kept = static_cast<int>(sm.found);
+            }
+            announce(entry(kept - 1));
+            if (a.uniforms) {
+                // the kept ones in the order of the vocabulary: the same entries, turned round, their keys behind
+                __syncthreads();
+                for (int x = tid; x < kept; x += kFThreads) sm.list[x] = sm.list[x] << 32 | sm.list[x] >> 32;
+                sort_list(sm.list, kept);
+                const int each_has = (kept + kFThreads - 1) / kFThreads, i0 = tid * each_has;
+                double w = 0.0, W;
+                for (int x = i0; x < i0 + each_has && x < kept; ++x) w += weight(value_of<DT>(static_cast<uint32_t>(sm.list[x])));
+                double c = before_me(w, sm.scan_b, &W);
+                const double t = static_cast<double>(a.uniforms[row]) * W;
+                if (tid == 0) sm.found = 0xffffffffu;
+                __syncthreads();
+                for (int x = i0; x < i0 + each_has && x < kept; ++x) {
+                    const double y = weight(value_of<DT>(static_cast<uint32_t>(sm.list[x])));
+                    c += y;
+                    if (y > 0.0 && c > t) { atomicMin(&sm.found, static_cast<unsigned>(x)); break; }
+                }
+                __syncthreads();
+                if (tid == 0) {
+                    int x = static_cast<int>(sm.found);
+                    // (where rounding leaves none, the last that weighs anything)
+                    if (x < 0)
+                        for (x = kept - 1; x > 0 && weight(value_of<DT>(static_cast<uint32_t>(sm.list[x]))) == 0.0;) --x;
+                    a.tokens[row] = static_cast<int>(0xffffffffu - static_cast<uint32_t>(sm.list[x] >> 32));
+                    if (a.lse) a.lse[row] = static_cast<float>(M / static_cast<double>(T) + log(W));
+                }
+            }
+        }
+        cluster.sync();
+        border = sm.border;
+        drew = true;
+        return true;
+    };
+
+    // Top-p by a histogram over the distance from the largest, 1/128 of T a bin: counts bound the mass of each, so that only a few bins can hold the border;
+    // their tokens are put in order, what lies before them is summed up.  False: too many.
+    auto by_mass = [&]() {
+        const Border among = border;
+        const float among_z = value_of<DT>(among.key), step = 128.f / T;
+        if (!(step < INFINITY)) return false;
+        auto counts = [&](float z, int i) { return z > among_z || (z == among_z && i <= among.last && z > -INFINITY); };
+        auto bin_of = [&](float z) { return static_cast<int>(fminf((top - z) * step, static_cast<float>(kBins - 1))); };
+        each([&](const uint4& v, int i) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-        if (lane == 0) sm.warp_mass[warp] = mine;
+            for (int x = 0; x < N; ++x) {
+                const float z = R::get(v, x);
+                if (counts(z, i + x)) atomicAdd(&sm.bins[bin_of(z)], 1u);
+            }
+        });
+        cluster.sync();
+        unsigned c[8];
+        gather(c);
+        // (a bin's weights lie between these but for some 10^-5: roundings of distances up to 32, of exponentials)
+        double up[8], lo[8], u = 0.0, l = 0.0, all_u, all_l;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int b = 8 * tid + x;
+            up[x] = c[x] ? c[x] * static_cast<double>(1.00003f * exp2f(-1.44269504f / 128.f * b)) : 0.0;
+            lo[x] = c[x] && b < kBins - 1 ? c[x] * static_cast<double>(0.99997f * exp2f(-1.44269504f / 128.f * (b + 1))) : 0.0;
+            u += up[x];
+            l += lo[x];
+        }
+        double ub = before_me(u, sm.scan_a, &all_u), lb = before_me(l, sm.scan_b, &all_l);
+        if (tid == 0) { sm.digit = 0; sm.found = kBins; sm.above = 0; }
+        __syncthreads();
+        // Bins that are kept whole: prefix (1 - p) < p rest for the largest prefix and the least rest.  Bins of which nothing is kept: the prefix
+        // before them is enough in the worst case.
+        unsigned whole = 0, none = kBins;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            if (none == kBins && lb * (1.0 - share) >= share * (all_u - ub) * 1.0000001) none = 8 * tid + x;
+            ub += up[x];
+            lb += lo[x];
+            if (ub * (1.0 - share) < share * (all_l - lb) * 0.9999999) whole = 8 * tid + x + 1;
+        }
+        if (whole) atomicMax(&sm.digit, whole);
+        if (none < kBins) atomicMin(&sm.found, none);
+        __syncthreads();
+        const int b0 = static_cast<int>(sm.digit);
+        int b1 = static_cast<int>(sm.found) - 1;
+        if (b1 < b0) b1 = b0;
+        unsigned inside = 0;
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+            if (8 * tid + x >= b0 && 8 * tid + x <= b1) inside += c[x];
+        if (inside) atomicAdd(&sm.above, inside);
+        cluster.sync();                                  // (the bins have been read)
+        const unsigned n = sm.above;
+        if (n == 0 || n > kList) return false;
+        double above = 0.0, rest = 0.0;
+        each([&](const uint4& v, int i) {
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                const float z = R::get(v, x);
+                const bool in = counts(z, i + x);
+                const int b = bin_of(z);
+                enlist(in && b >= b0 && b <= b1, key_of<DT>(z), i + x);
+                if (in) {
+                    const double w = weight(z);
+                    if (b < b0) above += w;
+                    else rest += w;
+                }
+            }
+        });
+        above = summed(above);
+        rest = summed(rest);
+        if (lane == 0) { sm.warp_above[warp] = above; sm.warp_mass[warp] = rest; }
+        cluster.sync();
+        if (rank == 0) {
+            const FilterSmem* o = cluster.map_shared_rank(&sm, tid < C * kFWarps ? tid / kFWarps : 0);
+            const double x = tid < C * kFWarps ? o->warp_above[tid % kFWarps] : 0.0, y = tid < C * kFWarps ? o->warp_mass[tid % kFWarps] : 0.0;
+            before_me(x, sm.scan_a, &above);
+            before_me(y, sm.scan_b, &rest);
+            sort_list(sm.list, static_cast<int>(n));
+            const int kept = end_of_list(static_cast<int>(n), static_cast<int>(n), above, share * (above + rest));
+            // (none of them: the border lies before the first, whose index is the lowest of its value)
+            announce(kept > 0 ? entry(kept - 1) : Border{entry(0).key, -1});
+        }
+        cluster.sync();
+        border = sm.border;
+        return true;
+    };
+
+    if (!bad) {
+        bool dirty = false;                              // (something lies where the bins are)
+        auto clean = [&]() {
+            if (!dirty) return;
+            for (int x = tid; x < kBins; x += kFThreads) sm.bins[x] = 0;
+            if (tid == 0) sm.listed = 0;
+            cluster.sync();
+        };
+        if (k < a.V) {
+            if (k <= kMostK) {
+                dirty = true;
+                by_candidates();
+            }
+            if (!drew) {
+                dirty = true;
+                cluster.sync();
+                select(false, k, 0.0);
+            }
+        }
+        if (!drew) {
+            if (p < 1.f && p > 0.f) {
+                clean();
+                if (!by_mass()) {
+                    cluster.sync();
+                    select(true, 0, share);
+                }
+            }
+            if (least > border.key) border = Border{least, kAll};
+        }
+    }
+    const float border_z = value_of<DT>(border.key);
+    auto kept = [&](float z, int i) { return z > border_z || (z == border_z && i <= border.last); };
+
+    // ---- the token ----
+    if (a.uniforms && bad) {
+        if (rank == 0 && tid == 0) {
+            a.tokens[row] = -1;
+            if (a.lse) a.lse[row] = __int_as_float(0x7fc00000);
+        }
+    } else if (a.uniforms && !drew) {
+        double sum = 0.0;
+        each([&](const uint4& v, int i) {
+            bool any = false;
+#pragma unroll
+            for (int x = 0; x < N; ++x) any |= R::get(v, x) >= border_z;
+            if (!any) return;
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                const float z = R::get(v, x);
+                if (kept(z, i + x)) sum += weight(z);
+            }
+        });
+        sum = summed(sum);
+        if (lane == 0) sm.warp_mass[warp] = sum;
         cluster.sync();
         // every warp: the sums of all warps in order, four a lane
         double s[4], inc = 0.0;
@@ -370,20 +742,14 @@ __global__ void __launch_bounds__(kFThreads, 1) filter_kernel(const FilterArgs a
             s[x] = w < C * kFWarps ? cluster.map_shared_rank(&sm, w / kFWarps)->warp_mass[w % kFWarps] : 0.0;
             inc += s[x];
         }
-        const double own = inc;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const double u = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += u;
-        }
+        inc = scanned(inc, lane);
         const double W = __shfl_sync(0xffffffffu, inc, 31);
-        double before = __shfl_up_sync(0xffffffffu, inc, 1);
-        if (lane == 0) before = 0.0;
-        (void)own;
+        double c = __shfl_up_sync(0xffffffffu, inc, 1);
+        if (lane == 0) c = 0.0;
         const double t = static_cast<double>(a.uniforms[row]) * W;
         // the first segment with whose end the border is passed; where rounding leaves none, the last that holds anything
         int seg = -1, last = -1;
-        double at = 0.0, at_last = 0.0, c = before;
+        double at = 0.0, at_last = 0.0;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             if (s[x] > 0.0) {
@@ -394,38 +760,25 @@ __global__ void __launch_bounds__(kFThreads, 1) filter_kernel(const FilterArgs a
             c += s[x];
         }
         const unsigned hit = __ballot_sync(0xffffffffu, seg >= 0), some = __ballot_sync(0xffffffffu, last >= 0);
-        if (hit) {
-            const int src = __ffs(hit) - 1;
-            seg = __shfl_sync(0xffffffffu, seg, src);
-            at = __shfl_sync(0xffffffffu, at, src);
-        } else if (some) {
-            const int src = 31 - __clz(some);
-            seg = __shfl_sync(0xffffffffu, last, src);
-            at = __shfl_sync(0xffffffffu, at_last, src);
-        }
-        if (bad) {
-            if (rank == 0 && tid == 0) {
-                a.tokens[row] = -1;
-                if (a.lse) a.lse[row] = __int_as_float(0x7fc00000);
-            }
-        } else if (seg == rank * kFWarps + warp) {
+        const int src = hit ? __ffs(hit) - 1 : 31 - __clz(some);
+        seg = __shfl_sync(0xffffffffu, hit ? seg : last, src);
+        at = __shfl_sync(0xffffffffu, hit ? at : at_last, src);
+        if (seg == rank * kFWarps + warp) {
             int found = -1, latest = -1;
             double run = at;
             each([&](const uint4& v, int i) {
+                bool any = false;
+#pragma unroll
+                for (int x = 0; x < N; ++x) any |= kept(R::get(v, x), i + x);
+                if (found >= 0 || !__any_sync(0xffffffffu, any)) return;
                 double w[N], n = 0.0;
 #pragma unroll
                 for (int x = 0; x < N; ++x) {
                     const float z = R::get(v, x);
-                    const uint32_t key = key_of<DT>(z);
-                    w[x] = key > kLowest<DT> && border.keeps(key, i + x) ? weight(z) : 0.0;
+                    w[x] = kept(z, i + x) ? weight(z) : 0.0;
                     n += w[x];
                 }
-                double upto = n;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const double u = __shfl_up_sync(0xffffffffu, upto, o);
-                    if (lane >= o) upto += u;
-                }
+                const double upto = scanned(n, lane);
                 double c = run + (upto - n);
                 int here = -1;
 #pragma unroll
@@ -437,7 +790,7 @@ __global__ void __launch_bounds__(kFThreads, 1) filter_kernel(const FilterArgs a
                     }
                 }
                 const unsigned h = __ballot_sync(0xffffffffu, here >= 0);
-                if (found < 0 && h) found = __shfl_sync(0xffffffffu, here, __ffs(h) - 1);
+                if (h) found = __shfl_sync(0xffffffffu, here, __ffs(h) - 1);
                 run += __shfl_sync(0xffffffffu, upto, 31);
             });
             if (found < 0) found = __reduce_max_sync(0xffffffffu, latest);
@@ -456,10 +809,17 @@ __global__ void __launch_bounds__(kFThreads, 1) filter_kernel(const FilterArgs a
             if (wrong) {
                 w = make_uint4(R::kNaN, R::kNaN, R::kNaN, R::kNaN);
             } else if (!bad) {
-                E* e = reinterpret_cast<E*>(&w);
+                bool any = false;
 #pragma unroll
-                for (int x = 0; x < N; ++x)
-                    if (!border.keeps(key_of<DT>(R::get(v, x)), i + x)) e[x] = static_cast<E>(R::kNegInf >> (32 - 8 * sizeof(E)));
+                for (int x = 0; x < N; ++x) any |= R::get(v, x) >= border_z;
+                w = make_uint4(R::kNegInf, R::kNegInf, R::kNegInf, R::kNegInf);
+                if (any) {
+                    E* e = reinterpret_cast<E*>(&w);
+                    const E* f = reinterpret_cast<const E*>(&v);
+#pragma unroll
+                    for (int x = 0; x < N; ++x)
+                        if (kept(R::get(v, x), i + x)) e[x] = f[x];
+                }
             }
             if (a.vec_out && i + N <= a.V) {
                 *reinterpret_cast<uint4*>(out + static_cast<long long>(i) * sizeof(E)) = w;
@@ -474,8 +834,12 @@ __global__ void __launch_bounds__(kFThreads, 1) filter_kernel(const FilterArgs a
     cluster.sync();                       // (nobody leaves while its shared memory may be read)
 }
 
-template <int DT, int NV>
+constexpr int kSmall = static_cast<int>((sizeof(FilterSmem) + 15) / 16 * 16);
+template <int DT, bool RES>
 cudaError_t launch(FilterArgs a, int rows, int C, int nv, cudaStream_t stream) {
+    static std::atomic<unsigned long long> asked{0};
+    const cudaError_t e = allow_shared(filter_kernel<DT, RES>, 227 * 1024, asked);
+    if (e != cudaSuccess) return e;
     a.per_cta = nv * kFThreads * Row<DT>::kN;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeClusterDimension;
@@ -484,26 +848,22 @@ cudaError_t launch(FilterArgs a, int rows, int C, int nv, cudaStream_t stream) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(rows) * C);
     cfg.blockDim = dim3(kFThreads);
+    cfg.dynamicSmemBytes = kSmall + (RES ? nv * kFThreads * 16 : 0);
     cfg.stream = stream;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, filter_kernel<DT, NV>, a);
+    return cudaLaunchKernelEx(&cfg, filter_kernel<DT, RES>, a);
 }
 template <int DT>
 cudaError_t pick(const FilterArgs& a, int rows, int sms, cudaStream_t stream) {
-    constexpr int N = Row<DT>::kN, kMost = DT == kF32 ? 16 : 8;
+    constexpr int N = Row<DT>::kN;
     const long long vecs = (static_cast<long long>(a.V) + N - 1) / N, runs = (vecs + kFThreads - 1) / kFThreads;      // vectors a thread of one CTA would have
-    // the fewest CTAs that hold the row, and more where rows are fewer than SMs
+    // CTAs of a row: as many as leave two on an SM (8 vectors a thread), and more where rows are fewer than SMs
+    constexpr int kTwo = 8, kMost = (227 * 1024 - kSmall) / (kFThreads * 16);
     int C = 1;
-    while (C < 8 && (runs > static_cast<long long>(C) * kMost || (runs > C && 2LL * C * rows <= sms))) C *= 2;
+    while (C < 8 && (runs > static_cast<long long>(C) * kTwo || (runs > C && 2LL * C * rows <= sms))) C *= 2;
     const int nv = static_cast<int>((runs + C - 1) / C);
-    if (nv <= 1) return launch<DT, 1>(a, rows, C, 1, stream);
-    if (nv <= 2) return launch<DT, 2>(a, rows, C, 2, stream);
-    if (nv <= 4) return launch<DT, 4>(a, rows, C, 4, stream);
-    if (nv <= 8) return launch<DT, 8>(a, rows, C, 8, stream);
-    if constexpr (kMost == 16)
-        if (nv <= 16) return launch<DT, 16>(a, rows, C, 16, stream);
-    return launch<DT, 0>(a, rows, C, nv, stream);
+    return nv <= kMost ? launch<DT, true>(a, rows, C, nv, stream) : launch<DT, false>(a, rows, C, nv, stream);
 }
 
 bool on(const void* p, size_t x) { return reinterpret_cast<uintptr_t>(p) % x == 0; }
