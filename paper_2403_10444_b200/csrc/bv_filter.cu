@@ -44,11 +44,12 @@ struct FilterArgs {
     bool vec_in, vec_out;
 };
 
-// 2^y for y <= 0, to 64 bits but for some 10^-14: the series of e^(f ln 2) about the nearest integer.
+// 2^y for y <= 0, to 64 bits but for some 10^-14: the series of e^(f ln 2) about the nearest integer.  (No branch, so that a thread's
+// several are under way together: one after the other, the steps' latencies were six times the pipe's time.)
 __device__ __forceinline__ double pow2(double y) {
     const double magic = 6755399441055744.0;         // 1.5 2^52
-    if (!(y > -1000.0)) return 0.0;
-    const double t = y + magic, f = (y - (t - magic)) * 0.69314718055994530942;
+    const bool some = y > -1000.0;
+    const double t = (some ? y : 0.0) + magic, f = ((some ? y : 0.0) - (t - magic)) * 0.69314718055994530942;
     double s = 1.0 / 479001600.0;
     s = fma(s, f, 1.0 / 39916800.0);
     s = fma(s, f, 1.0 / 3628800.0);
@@ -62,7 +63,8 @@ __device__ __forceinline__ double pow2(double y) {
     s = fma(s, f, 0.5);
     s = fma(s, f, 1.0);
     s = fma(s, f, 1.0);
-    return __hiloint2double(__double2hiint(s) + (__double2loint(t) << 20), __double2loint(s));
+    const double w = __hiloint2double(__double2hiint(s) + (__double2loint(t) << 20), __double2loint(s));
+    return some ? w : 0.0;
 }
 
 template <int DT> struct Row;
@@ -98,8 +100,11 @@ struct Border {
     __device__ __forceinline__ bool keeps(uint32_t k, int i) const { return k > key || (k == key && i <= last); }
 };
 
-constexpr int kBins = 4096;              // of a histogram over values
+constexpr int kBins = 2048;              // of a histogram over values: four a thread
+constexpr float kPerNat = 64.f;          // bins of top-p's to a factor e of the weights
+static_assert(kBins == 4 * kFThreads, "");
 constexpr int kList = 4096;              // tokens that are put in order one by one
+constexpr int kShort = kList / 2;        // of a list that leaves room for buckets behind it
 constexpr int kMostK = 1024;             // of a top-k by candidates
 constexpr int kFew = 2048;               // tokens of which all are candidates
 
@@ -142,15 +147,65 @@ __device__ __forceinline__ double summed(double x) {
     for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
-// The n numbers of a list in descending order, by all threads (size: the power of two that holds them; 0 behind them).
-__device__ __forceinline__ void sort_list(unsigned long long* list, int n) {
-    int size = 32;
-    while (size < n) size *= 2;
-    for (int i = n + threadIdx.x; i < size; i += kFThreads) list[i] = 0;
+// The n numbers of a list in descending order, by all threads.  bucket(x) in 0 .. kShort - 1, not falling as x falls.  Up to kShort of them by buckets: counted,
+// placed, and within a bucket by comparison with the others there; more by a network.  (2048 by the network: 47000 clocks.)
+template <typename F> __device__ __forceinline__ void order_list(FilterSmem& sm, int n, F bucket) {
+    unsigned long long* const list = sm.list;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     __syncthreads();
-    for (int k = 2; k <= size; k *= 2)
+    if (n <= kShort) {
+        constexpr int kMine = kShort / kFThreads;
+        unsigned* const count = reinterpret_cast<unsigned*>(list + kShort);      // [kShort] how many, then where they begin
+        unsigned long long x[kMine];
+        unsigned at[kMine];
+        int in[kMine];
+        for (int i = tid; i < kShort; i += kFThreads) count[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            if (tid + i * kFThreads >= n) break;
+            x[i] = list[tid + i * kFThreads];
+            in[i] = bucket(x[i]);
+            at[i] = atomicAdd(&count[in[i]], 1u);
+        }
+        __syncthreads();
+        uint4& mine = reinterpret_cast<uint4*>(count)[tid];
+        static_assert(kShort == 4 * kFThreads, "four buckets a thread");
+        const uint4 c = mine;
+        unsigned b = scanned(c.x + c.y + c.z + c.w, lane);
+        if (lane == 31) sm.scan_count[warp] = b;
+        __syncthreads();
+        b -= c.x + c.y + c.z + c.w;
+        for (int w = 0; w < warp; ++w) b += sm.scan_count[w];
+        mine = make_uint4(b, b + c.x, b + c.x + c.y, b + c.x + c.y + c.z);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            if (tid + i * kFThreads >= n) break;
+            list[count[in[i]] + at[i]] = x[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            if (tid + i * kFThreads >= n) break;
+            const unsigned from = count[in[i]], to = in[i] + 1 < kShort ? count[in[i] + 1] : n;
+            at[i] = from;
+            for (unsigned o = from; o < to; ++o) at[i] += list[o] > x[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            if (tid + i * kFThreads >= n) break;
+            list[at[i]] = x[i];
+        }
+        __syncthreads();
+        return;
+    }
+    for (int i = n + tid; i < kList; i += kFThreads) list[i] = 0;
+    __syncthreads();
+    for (int k = 2; k <= kList; k *= 2)
         for (int j = k / 2; j > 0; j /= 2) {
-            for (int x = threadIdx.x; x < size / 2; x += kFThreads) {
+            for (int x = tid; x < kList / 2; x += kFThreads) {
                 const int i = 2 * x - (x & (j - 1)), o = i + j;      // (i: the x-th index without bit j)
                 const unsigned long long u = list[i], v = list[o];
                 if ((u < v) == ((i & k) == 0)) { list[i] = v; list[o] = u; }
@@ -278,25 +333,43 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         least = key_of<DT>(x);
     }
     Border border{kLowest<DT>, kAll};
-    // tokens, by whole warps, into the first CTA's list
-    auto enlist = [&](bool in, uint32_t key, int index) {
-        const unsigned who = __ballot_sync(0xffffffffu, in);
-        if (who == 0) return;
+    // Tokens of a vector (a bit each) into the CTA's list, by whole warps.
+    auto enlist = [&](unsigned which, const uint4& v, int i) {
+        const unsigned n = __popc(which), inc = scanned(n, lane), all = __shfl_sync(0xffffffffu, inc, 31);
+        if (all == 0) return;
         unsigned at = 0;
-        if (lane == 0) at = atomicAdd(&first_cta->listed, static_cast<unsigned>(__popc(who)));
-        at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1));
-        if (in && at < kList) first_cta->list[at] = static_cast<unsigned long long>(key) << 32 | (0xffffffffu - static_cast<unsigned>(index));
-    };
-    // This CTA's and the others' bins, eight a thread from 8 tid on.
-    auto gather = [&](unsigned (&c)[8]) {
+        if (lane == 0) at = atomicAdd(&sm.listed, all);
+        at = __shfl_sync(0xffffffffu, at, 0) + inc - n;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) c[x] = 0;
-        for (int r = 0; r < C; ++r) {
-            const uint4* o = reinterpret_cast<const uint4*>(cluster.map_shared_rank(&sm, r)->bins) + 2 * tid;
-            const uint4 u = o[0], v = o[1];
-            c[0] += u.x; c[1] += u.y; c[2] += u.z; c[3] += u.w;
-            c[4] += v.x; c[5] += v.y; c[6] += v.z; c[7] += v.w;
+        for (int x = 0; x < N; ++x)
+            if (which >> x & 1) {
+                if (at < kList) sm.list[at] = static_cast<unsigned long long>(key_of<DT>(R::get(v, x))) << 32 | (0xffffffffu - static_cast<unsigned>(i + x));
+                ++at;
+            }
+    };
+    // ... and all lists into the first CTA's, behind what it has; how many there are in all (more than kList: not all of them are there).
+    // (One remote addition a CTA: one for each of a warp's tokens was a microsecond each, 55 us for a row with 1300 candidates.)
+    auto collect = [&]() {
+        __syncthreads();
+        if (rank > 0) {
+            const unsigned n = sm.listed;
+            if (tid == 0) sm.above = n ? atomicAdd(&first_cta->listed, n) : 0;
+            __syncthreads();
+            const unsigned at = sm.above;
+            for (unsigned x = tid; x < n && x < kList && at + x < kList; x += kFThreads) first_cta->list[at + x] = sm.list[x];
         }
+        cluster.sync();
+        return first_cta->listed;
+    };
+    // This CTA's and the others' bins, four a thread from 4 tid on.
+    auto gather = [&](unsigned (&c)[4]) {
+        uint4 u[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) u[r] = r < C ? reinterpret_cast<const uint4*>(cluster.map_shared_rank(&sm, r)->bins)[tid] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) c[x] = 0;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) { c[0] += u[r].x; c[1] += u[r].y; c[2] += u[r].z; c[3] += u[r].w; }
     };
     // The sum of x over the threads before this one; `all`: of all threads.
     auto before_me = [&](double x, double* slots, double* all) {
@@ -332,6 +405,27 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         if (kept) atomicMax(&sm.found, kept);
         __syncthreads();
         return static_cast<int>(sm.found);
+    };
+    // The first CTA's list in order, by buckets between its largest and its smallest value.
+    auto order_by_value = [&](int n) {
+        if (tid == 0) { sm.digit = 0; sm.found = 0xffffffffu; }
+        __syncthreads();
+        unsigned hi = 0, lo = 0xffffffffu;
+        for (int x = tid; x < n; x += kFThreads) {
+            const unsigned key = static_cast<unsigned>(sm.list[x] >> 32);
+            hi = key > hi ? key : hi;
+            lo = key < lo ? key : lo;
+        }
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        if (lane == 0) { atomicMax(&sm.digit, hi); atomicMin(&sm.found, lo); }
+        __syncthreads();
+        const float from = value_of<DT>(sm.digit), wide = from - value_of<DT>(sm.found), fine = wide > 0.f ? (kShort - 1) / wide : 0.f;
+        // (a width that is infinite or next to nothing leaves buckets of any size, in order all the same)
+        order_list(sm, n, [&](unsigned long long x) {
+            const float d = (from - value_of<DT>(static_cast<uint32_t>(x >> 32))) * fine;
+            return d < static_cast<float>(kShort - 1) ? static_cast<int>(d) : kShort - 1;
+        });
     };
     auto entry = [&](int x) { return Border{static_cast<uint32_t>(sm.list[x] >> 32), static_cast<int>(0xffffffffu - static_cast<uint32_t>(sm.list[x]))}; };
     auto announce = [&](Border b) {
@@ -498,10 +592,10 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
                 if (d < kBins) atomicAdd(&sm.bins[static_cast<int>(d)], 1u);
             });
             cluster.sync();
-            unsigned c[8], sum = 0;
+            unsigned c[4], sum = 0;
             gather(c);
 #pragma unroll
-            for (int x = 0; x < 8; ++x) sum += c[x];
+            for (int x = 0; x < 4; ++x) sum += c[x];
             const unsigned inc = scanned(sum, lane);
             if (lane == 31) sm.scan_count[warp] = inc;
             if (tid == 0) sm.found = kBins;
@@ -509,8 +603,8 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             unsigned upto = inc - sum;
             for (int w = 0; w < warp; ++w) upto += sm.scan_count[w];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                if (upto < static_cast<unsigned>(k) && upto + c[x] >= static_cast<unsigned>(k)) sm.found = 8 * tid + x;
+            for (int x = 0; x < 4; ++x) {
+                if (upto < static_cast<unsigned>(k) && upto + c[x] >= static_cast<unsigned>(k)) sm.found = 4 * tid + x;
                 upto += c[x];
             }
             cluster.sync();                              // (the bins have been read)
@@ -524,27 +618,24 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
 #pragma unroll
                 for (int x = 1; x < N; ++x) z = fmaxf(z, R::get(v, x));
                 if (!__any_sync(0xffffffffu, (top - z) * step_ < limit)) return;
+                unsigned which = 0;
 #pragma unroll
-                for (int x = 0; x < N; ++x) {
-                    const float y = R::get(v, x);
-                    enlist((top - y) * step_ < limit, key_of<DT>(y), i + x);
-                }
+                for (int x = 0; x < N; ++x) which |= static_cast<unsigned>((top - R::get(v, x)) * step_ < limit) << x;
+                enlist(which, v, i);
             });
         } else {
             each([&](const uint4& v, int i) {
+                unsigned which = 0;
 #pragma unroll
-                for (int x = 0; x < N; ++x) {
-                    const float y = R::get(v, x);
-                    enlist(y > -INFINITY, key_of<DT>(y), i + x);
-                }
+                for (int x = 0; x < N; ++x) which |= static_cast<unsigned>(R::get(v, x) > -INFINITY) << x;
+                enlist(which, v, i);
             });
         }
-        cluster.sync();
-        const int n = static_cast<int>(first_cta->listed);
+        const unsigned n = collect();
         if (n > kList) return false;
         if (rank == 0) {
-            sort_list(sm.list, n);
-            int kept = end_of_list(n, k, 0.0, -1.0);
+            order_by_value(static_cast<int>(n));
+            int kept = end_of_list(static_cast<int>(n), k, 0.0, -1.0);
             // (of keys in order, those below min-p's border come last)
             if (least > 0) {
                 __syncthreads();
@@ -560,7 +651,8 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
                 // the kept ones in the order of the vocabulary: the same entries, turned round, their keys behind
                 __syncthreads();
                 for (int x = tid; x < kept; x += kFThreads) sm.list[x] = sm.list[x] << 32 | sm.list[x] >> 32;
-                sort_list(sm.list, kept);
+                const float share_of = static_cast<float>(kShort - 1) / static_cast<float>(a.V);
+                order_list(sm, kept, [&](unsigned long long x) { return static_cast<int>(static_cast<float>(0xffffffffu - static_cast<uint32_t>(x >> 32)) * share_of); });
                 const int each_has = (kept + kFThreads - 1) / kFThreads, i0 = tid * each_has;
                 double w = 0.0, W;
                 for (int x = i0; x < i0 + each_has && x < kept; ++x) w += weight(value_of<DT>(static_cast<uint32_t>(sm.list[x])));
@@ -590,11 +682,11 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         return true;
     };
 
-    // Top-p by a histogram over the distance from the largest, 1/128 of T a bin: counts bound the mass of each, so that only a few bins can hold the border;
+    // Top-p by a histogram over the distance from the largest, 1/64 of T a bin: counts bound the mass of each, so that only a few bins can hold the border;
     // their tokens are put in order, what lies before them is summed up.  False: too many.
     auto by_mass = [&]() {
         const Border among = border;
-        const float among_z = value_of<DT>(among.key), step = 128.f / T;
+        const float among_z = value_of<DT>(among.key), step = kPerNat / T;
         if (!(step < INFINITY)) return false;
         auto counts = [&](float z, int i) { return z > among_z || (z == among_z && i <= among.last && z > -INFINITY); };
         auto bin_of = [&](float z) { return static_cast<int>(fminf((top - z) * step, static_cast<float>(kBins - 1))); };
@@ -606,15 +698,15 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             }
         });
         cluster.sync();
-        unsigned c[8];
+        unsigned c[4];
         gather(c);
         // (a bin's weights lie between these but for some 10^-5: roundings of distances up to 32, of exponentials)
-        double up[8], lo[8], u = 0.0, l = 0.0, all_u, all_l;
+        double up[4], lo[4], u = 0.0, l = 0.0, all_u, all_l;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            const int b = 8 * tid + x;
-            up[x] = c[x] ? c[x] * static_cast<double>(1.00003f * exp2f(-1.44269504f / 128.f * b)) : 0.0;
-            lo[x] = c[x] && b < kBins - 1 ? c[x] * static_cast<double>(0.99997f * exp2f(-1.44269504f / 128.f * (b + 1))) : 0.0;
+        for (int x = 0; x < 4; ++x) {
+            const int b = 4 * tid + x;
+            up[x] = c[x] ? c[x] * static_cast<double>(1.00003f * exp2f(-1.44269504f / kPerNat * b)) : 0.0;
+            lo[x] = c[x] && b < kBins - 1 ? c[x] * static_cast<double>(0.99997f * exp2f(-1.44269504f / kPerNat * (b + 1))) : 0.0;
             u += up[x];
             l += lo[x];
         }
@@ -625,11 +717,11 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         // before them is enough in the worst case.
         unsigned whole = 0, none = kBins;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            if (none == kBins && lb * (1.0 - share) >= share * (all_u - ub) * 1.0000001) none = 8 * tid + x;
+        for (int x = 0; x < 4; ++x) {
+            if (none == kBins && lb * (1.0 - share) >= share * (all_u - ub) * 1.0000001) none = 4 * tid + x;
             ub += up[x];
             lb += lo[x];
-            if (ub * (1.0 - share) < share * (all_l - lb) * 0.9999999) whole = 8 * tid + x + 1;
+            if (ub * (1.0 - share) < share * (all_l - lb) * 0.9999999) whole = 4 * tid + x + 1;
         }
         if (whole) atomicMax(&sm.digit, whole);
         if (none < kBins) atomicMin(&sm.found, none);
@@ -639,37 +731,37 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         if (b1 < b0) b1 = b0;
         unsigned inside = 0;
 #pragma unroll
-        for (int x = 0; x < 8; ++x)
-            if (8 * tid + x >= b0 && 8 * tid + x <= b1) inside += c[x];
+        for (int x = 0; x < 4; ++x)
+            if (4 * tid + x >= b0 && 4 * tid + x <= b1) inside += c[x];
         if (inside) atomicAdd(&sm.above, inside);
         cluster.sync();                                  // (the bins have been read)
         const unsigned n = sm.above;
         if (n == 0 || n > kList) return false;
         double above = 0.0, rest = 0.0;
         each([&](const uint4& v, int i) {
+            unsigned which = 0;
 #pragma unroll
             for (int x = 0; x < N; ++x) {
                 const float z = R::get(v, x);
                 const bool in = counts(z, i + x);
                 const int b = bin_of(z);
-                enlist(in && b >= b0 && b <= b1, key_of<DT>(z), i + x);
-                if (in) {
-                    const double w = weight(z);
-                    if (b < b0) above += w;
-                    else rest += w;
-                }
+                const double w = in ? weight(z) : 0.0;
+                which |= static_cast<unsigned>(in && b >= b0 && b <= b1) << x;
+                above += b < b0 ? w : 0.0;
+                rest += b < b0 ? 0.0 : w;
             }
+            enlist(which, v, i);
         });
         above = summed(above);
         rest = summed(rest);
         if (lane == 0) { sm.warp_above[warp] = above; sm.warp_mass[warp] = rest; }
-        cluster.sync();
+        collect();
         if (rank == 0) {
             const FilterSmem* o = cluster.map_shared_rank(&sm, tid < C * kFWarps ? tid / kFWarps : 0);
             const double x = tid < C * kFWarps ? o->warp_above[tid % kFWarps] : 0.0, y = tid < C * kFWarps ? o->warp_mass[tid % kFWarps] : 0.0;
             before_me(x, sm.scan_a, &above);
             before_me(y, sm.scan_b, &rest);
-            sort_list(sm.list, static_cast<int>(n));
+            order_by_value(static_cast<int>(n));
             const int kept = end_of_list(static_cast<int>(n), static_cast<int>(n), above, share * (above + rest));
             // (none of them: the border lies before the first, whose index is the lowest of its value)
             announce(kept > 0 ? entry(kept - 1) : Border{entry(0).key, -1});
@@ -724,11 +816,11 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             bool any = false;
 #pragma unroll
             for (int x = 0; x < N; ++x) any |= R::get(v, x) >= border_z;
-            if (!any) return;
+            if (!__any_sync(0xffffffffu, any)) return;
 #pragma unroll
             for (int x = 0; x < N; ++x) {
                 const float z = R::get(v, x);
-                if (kept(z, i + x)) sum += weight(z);
+                sum += kept(z, i + x) ? weight(z) : 0.0;
             }
         });
         sum = summed(sum);
