@@ -44,26 +44,25 @@ struct FilterArgs {
     bool vec_in, vec_out;
 };
 
-// 2^y for y <= 0, to 64 bits but for some 10^-14: the series of e^(f ln 2) about the nearest integer.  (No branch, so that a thread's
-// several are under way together: one after the other, the steps' latencies were six times the pipe's time.)
-__device__ __forceinline__ double pow2(double y) {
+// 2^(y / 16) for y <= 0, but for some 10^-13: a sixteenth of a power of two from a table (roots[i] = 2^(i / 16), in shared memory, where no two of them
+// share a bank), the rest, at most half a sixteenth, by the series of the exponential.  Twelve operations with the sum, where a series about the nearest
+// integer takes 21, and the pipe for 64 bits is what a pass over a whole vocabulary waits for.  (No branch: a thread's several are under way together.)
+constexpr int kRoots = 16;
+__device__ __forceinline__ double pow2_16th(double y, const double* roots) {
     const double magic = 6755399441055744.0;         // 1.5 2^52
-    const bool some = y > -1000.0;
-    const double t = (some ? y : 0.0) + magic, f = ((some ? y : 0.0) - (t - magic)) * 0.69314718055994530942;
-    double s = 1.0 / 479001600.0;
-    s = fma(s, f, 1.0 / 39916800.0);
-    s = fma(s, f, 1.0 / 3628800.0);
-    s = fma(s, f, 1.0 / 362880.0);
-    s = fma(s, f, 1.0 / 40320.0);
-    s = fma(s, f, 1.0 / 5040.0);
-    s = fma(s, f, 1.0 / 720.0);
-    s = fma(s, f, 1.0 / 120.0);
-    s = fma(s, f, 1.0 / 24.0);
-    s = fma(s, f, 1.0 / 6.0);
-    s = fma(s, f, 0.5);
-    s = fma(s, f, 1.0);
-    s = fma(s, f, 1.0);
-    const double w = __hiloint2double(__double2hiint(s) + (__double2loint(t) << 20), __double2loint(s));
+    constexpr double c = 0.69314718055994530942 / kRoots;
+    const bool some = y > -1000.0 * kRoots;
+    y = some ? y : 0.0;
+    const double t = y + magic, f = y - (t - magic);
+    const int n = __double2loint(t);
+    double s = c * c * c * c * c / 120.0;
+    s = fma(s, f, c * c * c * c / 24.0);
+    s = fma(s, f, c * c * c / 6.0);
+    s = fma(s, f, c * c / 2.0);
+    s = fma(s, f, c);
+    const double r = roots[n & (kRoots - 1)];
+    s = fma(s * f, r, r);
+    const double w = __hiloint2double(__double2hiint(s) + (n >> 4 << 20), __double2loint(s));
     return some ? w : 0.0;
 }
 
@@ -117,6 +116,7 @@ struct FilterSmem {
         };
         unsigned long long list[kList];  // key, then the index turned round: in order when they descend
     };
+    double roots[kRoots];
     double warp_mass[kFWarps], warp_above[kFWarps];      // read by the other CTAs, as are the next four
     unsigned warp_count[kFWarps];
     float cta_top, cta_low;
@@ -285,6 +285,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         if (lane == 0) { sm.warp_top[warp] = top; sm.warp_low[warp] = low; sm.warp_bad[warp] = bad; }
         for (int x = tid; x < kBins; x += kFThreads) sm.bins[x] = 0;
         if (tid == 0) sm.listed = 0;
+        if (tid < kRoots) sm.roots[tid] = exp2(static_cast<double>(tid) / kRoots);
         __syncthreads();
         if (warp == 0) {
             top = lane < kFWarps ? sm.warp_top[lane] : -INFINITY;
@@ -322,8 +323,8 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
     if (p == 0.f) k = 1;                               // (the first one always)
     const bool wrong = !(T > 0.f && T < INFINITY && p >= 0.f && m >= 0.f && m <= 1.f);
     bad |= top == -INFINITY || wrong;
-    const double scale = 1.4426950408889634073599246810019 / static_cast<double>(T), M = static_cast<double>(top), share = static_cast<double>(p);
-    auto weight = [&](float z) { return pow2((static_cast<double>(z) - M) * scale); };
+    const double scale = kRoots * 1.4426950408889634073599246810019 / static_cast<double>(T), M = static_cast<double>(top), share = static_cast<double>(p);
+    auto weight = [&](float z) { return pow2_16th((static_cast<double>(z) - M) * scale, sm.roots); };
     auto fixed = [&](float z) { return static_cast<unsigned long long>(__double2ull_rn(weight(z) * static_cast<double>(1ull << a.fixed))); };
     // min-p: the lowest value of the type that is not below its border
     uint32_t least = 0;
@@ -333,19 +334,25 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         least = key_of<DT>(x);
     }
     Border border{kLowest<DT>, kAll};
-    // Tokens of a vector (a bit each) into the CTA's list, by whole warps.
-    auto enlist = [&](unsigned which, const uint4& v, int i) {
-        const unsigned n = __popc(which), inc = scanned(n, lane), all = __shfl_sync(0xffffffffu, inc, 31);
+    // Into the CTA's list: the tokens of which which(vector, index of its first) has a bit.  Counted first, so that a warp asks for room once.
+    auto enlist = [&](auto&& which) {
+        unsigned n = 0;
+        each([&](const uint4& v, int i) { n += __popc(which(v, i)); });
+        const unsigned inc = scanned(n, lane), all = __shfl_sync(0xffffffffu, inc, 31);
         if (all == 0) return;
         unsigned at = 0;
         if (lane == 0) at = atomicAdd(&sm.listed, all);
         at = __shfl_sync(0xffffffffu, at, 0) + inc - n;
+        each([&](const uint4& v, int i) {
+            const unsigned w = which(v, i);
+            if (w == 0) return;
 #pragma unroll
-        for (int x = 0; x < N; ++x)
-            if (which >> x & 1) {
-                if (at < kList) sm.list[at] = static_cast<unsigned long long>(key_of<DT>(R::get(v, x))) << 32 | (0xffffffffu - static_cast<unsigned>(i + x));
-                ++at;
-            }
+            for (int x = 0; x < N; ++x)
+                if (w >> x & 1) {
+                    if (at < kList) sm.list[at] = static_cast<unsigned long long>(key_of<DT>(R::get(v, x))) << 32 | (0xffffffffu - static_cast<unsigned>(i + x));
+                    ++at;
+                }
+        });
     };
     // ... and all lists into the first CTA's, behind what it has; how many there are in all (more than kList: not all of them are there).
     // (One remote addition a CTA: one for each of a warp's tokens was a microsecond each, 55 us for a row with 1300 candidates.)
@@ -577,13 +584,62 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         border.last = sm.index;
     };
 
+    // In the first CTA, which has a row's first n tokens in its list: what is kept of them, and the token.  target: the mass before which top-p keeps
+    // (negative: its share of the k first ones).
+    auto conclude = [&](int n, double target) {
+        order_by_value(n);
+        int kept = end_of_list(n, k, 0.0, target);
+        // (of keys in order, those below min-p's border come last)
+        if (least > 0) {
+            __syncthreads();
+            if (tid == 0) sm.found = 0;
+            __syncthreads();
+            for (int x = tid; x < kept; x += kFThreads)
+                if (static_cast<uint32_t>(sm.list[x] >> 32) >= least) atomicMax(&sm.found, static_cast<unsigned>(x + 1));
+            __syncthreads();
+            kept = static_cast<int>(sm.found);
+        }
+        announce(entry(kept - 1));
+        if (a.uniforms) {
+            // the kept ones in the order of the vocabulary: the same entries, turned round, their keys behind
+            __syncthreads();
+            for (int x = tid; x < kept; x += kFThreads) sm.list[x] = sm.list[x] << 32 | sm.list[x] >> 32;
+            const float share_of = static_cast<float>(kShort - 1) / static_cast<float>(a.V);
+            order_list(sm, kept, [&](unsigned long long x) { return static_cast<int>(static_cast<float>(0xffffffffu - static_cast<uint32_t>(x >> 32)) * share_of); });
+            const int each_has = (kept + kFThreads - 1) / kFThreads, i0 = tid * each_has;
+            double w = 0.0, W;
+            for (int x = i0; x < i0 + each_has && x < kept; ++x) w += weight(value_of<DT>(static_cast<uint32_t>(sm.list[x])));
+            double c = before_me(w, sm.scan_b, &W);
+            const double t = static_cast<double>(a.uniforms[row]) * W;
+            if (tid == 0) sm.found = 0xffffffffu;
+            __syncthreads();
+            for (int x = i0; x < i0 + each_has && x < kept; ++x) {
+                const double y = weight(value_of<DT>(static_cast<uint32_t>(sm.list[x])));
+                c += y;
+                if (y > 0.0 && c > t) { atomicMin(&sm.found, static_cast<unsigned>(x)); break; }
+            }
+            __syncthreads();
+            if (tid == 0) {
+                int x = static_cast<int>(sm.found);
+                // (where rounding leaves none, the last that weighs anything)
+                if (x < 0)
+                    for (x = kept - 1; x > 0 && weight(value_of<DT>(static_cast<uint32_t>(sm.list[x]))) == 0.0;) --x;
+                a.tokens[row] = static_cast<int>(0xffffffffu - static_cast<uint32_t>(sm.list[x] >> 32));
+                if (a.lse) a.lse[row] = static_cast<float>(M / static_cast<double>(T) + log(W));
+            }
+        }
+    };
     // Top-k of up to kMostK by candidates: what is not below the k-th largest of the vectors' maxima, or nearly so.  False: too many.
     bool drew = false;
     auto by_candidates = [&]() {
-        float limit = -INFINITY;
         if (a.V > kFew) {
-            const float step = (kBins - 1) / (top - low);
-            if (!(step > 0.f && step < INFINITY)) return false;
+            float limit;
+            // Each CTA's own k-th where those of all together are few (k = 50 of 8 CTAs: no histogram of all to wait for), else the row's.
+            const bool own = C == 1 || C * k <= kMostK;
+            float step = (kBins - 1) / (top - (own ? sm.cta_low : low));
+            const bool spread = step > 0.f && step < INFINITY;
+            if (!spread && !own) return false;
+            if (!spread) step = 0.f;
             each([&](const uint4& v, int) {
                 float z = R::get(v, 0);
 #pragma unroll
@@ -591,9 +647,15 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
                 const float d = (top - z) * step;
                 if (d < kBins) atomicAdd(&sm.bins[static_cast<int>(d)], 1u);
             });
-            cluster.sync();
             unsigned c[4], sum = 0;
-            gather(c);
+            if (own) {
+                __syncthreads();
+#pragma unroll
+                for (int x = 0; x < 4; ++x) c[x] = sm.bins[4 * tid + x];
+            } else {
+                cluster.sync();
+                gather(c);
+            }
 #pragma unroll
             for (int x = 0; x < 4; ++x) sum += c[x];
             const unsigned inc = scanned(sum, lane);
@@ -607,74 +669,32 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
                 if (upto < static_cast<unsigned>(k) && upto + c[x] >= static_cast<unsigned>(k)) sm.found = 4 * tid + x;
                 upto += c[x];
             }
-            cluster.sync();                              // (the bins have been read)
+            // (the bins have been read)
+            if (own) __syncthreads();
+            else cluster.sync();
             const int bin = static_cast<int>(sm.found);
-            if (bin >= kBins) return false;
-            // every vector of the bins up to this one has a maximum whose distance comes out below bin + 1
-            limit = static_cast<float>(bin + 1);
+            if (bin >= kBins && !own) return false;
+            // every vector of the bins up to this one has a maximum whose distance comes out below bin + 1 (a CTA with fewer than k: all of its own)
+            limit = bin < kBins && spread ? static_cast<float>(bin + 1) : INFINITY;
             const float step_ = step;
-            each([&](const uint4& v, int i) {
-                float z = R::get(v, 0);
-#pragma unroll
-                for (int x = 1; x < N; ++x) z = fmaxf(z, R::get(v, x));
-                if (!__any_sync(0xffffffffu, (top - z) * step_ < limit)) return;
+            enlist([&](const uint4& v, int) {
                 unsigned which = 0;
 #pragma unroll
                 for (int x = 0; x < N; ++x) which |= static_cast<unsigned>((top - R::get(v, x)) * step_ < limit) << x;
-                enlist(which, v, i);
+                return which;
             });
         } else {
-            each([&](const uint4& v, int i) {
+            enlist([&](const uint4& v, int) {
                 unsigned which = 0;
 #pragma unroll
                 for (int x = 0; x < N; ++x) which |= static_cast<unsigned>(R::get(v, x) > -INFINITY) << x;
-                enlist(which, v, i);
+                return which;
             });
         }
         const unsigned n = collect();
         if (n > kList) return false;
         if (rank == 0) {
-            order_by_value(static_cast<int>(n));
-            int kept = end_of_list(static_cast<int>(n), k, 0.0, -1.0);
-            // (of keys in order, those below min-p's border come last)
-            if (least > 0) {
-                __syncthreads();
-                if (tid == 0) sm.found = 0;
-                __syncthreads();
-                for (int x = tid; x < kept; x += kFThreads)
-                    if (static_cast<uint32_t>(sm.list[x] >> 32) >= least) atomicMax(&sm.found, static_cast<unsigned>(x + 1));
-                __syncthreads();
-                kept = static_cast<int>(sm.found);
-            }
-            announce(entry(kept - 1));
-            if (a.uniforms) {
-                // the kept ones in the order of the vocabulary: the same entries, turned round, their keys behind
-                __syncthreads();
-                for (int x = tid; x < kept; x += kFThreads) sm.list[x] = sm.list[x] << 32 | sm.list[x] >> 32;
-                const float share_of = static_cast<float>(kShort - 1) / static_cast<float>(a.V);
-                order_list(sm, kept, [&](unsigned long long x) { return static_cast<int>(static_cast<float>(0xffffffffu - static_cast<uint32_t>(x >> 32)) * share_of); });
-                const int each_has = (kept + kFThreads - 1) / kFThreads, i0 = tid * each_has;
-                double w = 0.0, W;
-                for (int x = i0; x < i0 + each_has && x < kept; ++x) w += weight(value_of<DT>(static_cast<uint32_t>(sm.list[x])));
-                double c = before_me(w, sm.scan_b, &W);
-                const double t = static_cast<double>(a.uniforms[row]) * W;
-                if (tid == 0) sm.found = 0xffffffffu;
-                __syncthreads();
-                for (int x = i0; x < i0 + each_has && x < kept; ++x) {
-                    const double y = weight(value_of<DT>(static_cast<uint32_t>(sm.list[x])));
-                    c += y;
-                    if (y > 0.0 && c > t) { atomicMin(&sm.found, static_cast<unsigned>(x)); break; }
-                }
-                __syncthreads();
-                if (tid == 0) {
-                    int x = static_cast<int>(sm.found);
-                    // (where rounding leaves none, the last that weighs anything)
-                    if (x < 0)
-                        for (x = kept - 1; x > 0 && weight(value_of<DT>(static_cast<uint32_t>(sm.list[x]))) == 0.0;) --x;
-                    a.tokens[row] = static_cast<int>(0xffffffffu - static_cast<uint32_t>(sm.list[x] >> 32));
-                    if (a.lse) a.lse[row] = static_cast<float>(M / static_cast<double>(T) + log(W));
-                }
-            }
+            conclude(static_cast<int>(n), -1.0);
         }
         cluster.sync();
         border = sm.border;
@@ -711,7 +731,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             l += lo[x];
         }
         double ub = before_me(u, sm.scan_a, &all_u), lb = before_me(l, sm.scan_b, &all_l);
-        if (tid == 0) { sm.digit = 0; sm.found = kBins; sm.above = 0; }
+        if (tid == 0) { sm.digit = 0; sm.found = kBins; sm.above = 0; sm.index = 0; }
         __syncthreads();
         // Bins that are kept whole: prefix (1 - p) < p rest for the largest prefix and the least rest.  Bins of which nothing is kept: the prefix
         // before them is enough in the worst case.
@@ -729,45 +749,66 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         const int b0 = static_cast<int>(sm.digit);
         int b1 = static_cast<int>(sm.found) - 1;
         if (b1 < b0) b1 = b0;
-        unsigned inside = 0;
+        unsigned inside = 0, before = 0;
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-            if (4 * tid + x >= b0 && 4 * tid + x <= b1) inside += c[x];
-        if (inside) atomicAdd(&sm.above, inside);
+        for (int x = 0; x < 4; ++x) {
+            if (4 * tid + x < b0) before += c[x];
+            else if (4 * tid + x <= b1) inside += c[x];
+        }
+        inside = __reduce_add_sync(0xffffffffu, inside);
+        before = __reduce_add_sync(0xffffffffu, before);
+        if (lane == 0) { atomicAdd(&sm.above, inside); atomicAdd(&sm.index, static_cast<int>(before)); }
         cluster.sync();                                  // (the bins have been read)
-        const unsigned n = sm.above;
+        unsigned n = sm.above;
         if (n == 0 || n > kList) return false;
+        // where all that may be kept is little, all of it goes into the list, and the token is drawn there
+        const bool all_of_it = n + static_cast<unsigned>(sm.index) <= kShort;
+        if (all_of_it) n += static_cast<unsigned>(sm.index);
         double above = 0.0, rest = 0.0;
         each([&](const uint4& v, int i) {
-            unsigned which = 0;
 #pragma unroll
             for (int x = 0; x < N; ++x) {
                 const float z = R::get(v, x);
-                const bool in = counts(z, i + x);
-                const int b = bin_of(z);
-                const double w = in ? weight(z) : 0.0;
-                which |= static_cast<unsigned>(in && b >= b0 && b <= b1) << x;
-                above += b < b0 ? w : 0.0;
-                rest += b < b0 ? 0.0 : w;
+                const double w = counts(z, i + x) ? weight(z) : 0.0;
+                const bool sure = bin_of(z) < b0;
+                above += sure ? w : 0.0;
+                rest += sure ? 0.0 : w;
             }
-            enlist(which, v, i);
         });
         above = summed(above);
         rest = summed(rest);
         if (lane == 0) { sm.warp_above[warp] = above; sm.warp_mass[warp] = rest; }
+        const int from = all_of_it ? 0 : b0;
+        enlist([&](const uint4& v, int i) {
+            unsigned which = 0;
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                const float z = R::get(v, x);
+                const int b = bin_of(z);
+                which |= static_cast<unsigned>(b >= from && b <= b1 && counts(z, i + x)) << x;
+            }
+            return which;
+        });
         collect();
         if (rank == 0) {
             const FilterSmem* o = cluster.map_shared_rank(&sm, tid < C * kFWarps ? tid / kFWarps : 0);
             const double x = tid < C * kFWarps ? o->warp_above[tid % kFWarps] : 0.0, y = tid < C * kFWarps ? o->warp_mass[tid % kFWarps] : 0.0;
             before_me(x, sm.scan_a, &above);
             before_me(y, sm.scan_b, &rest);
-            order_by_value(static_cast<int>(n));
-            const int kept = end_of_list(static_cast<int>(n), static_cast<int>(n), above, share * (above + rest));
-            // (none of them: the border lies before the first, whose index is the lowest of its value)
-            announce(kept > 0 ? entry(kept - 1) : Border{entry(0).key, -1});
+            const double target = share * (above + rest);
+            __syncthreads();
+            if (all_of_it) {
+                conclude(static_cast<int>(n), target);
+            } else {
+                order_by_value(static_cast<int>(n));
+                const int kept = end_of_list(static_cast<int>(n), static_cast<int>(n), above, target);
+                // (none of them: the border lies before the first, whose index is the lowest of its value)
+                announce(kept > 0 ? entry(kept - 1) : Border{entry(0).key, -1});
+            }
         }
         cluster.sync();
         border = sm.border;
+        drew = all_of_it;
         return true;
     };
 
