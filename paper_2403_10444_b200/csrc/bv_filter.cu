@@ -71,12 +71,28 @@ template <> struct Row<kF32> {
     using E = uint32_t;
     static constexpr int kN = 4;
     static constexpr uint32_t kNegInf = 0xff800000u, kNaN = 0x7fc00000u;
+    // The largest of a vector's, NaN if one is.
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        float r;
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
+        return __float_as_uint(r);
+    }
+    static __device__ __forceinline__ float top(const uint4& v) { return __uint_as_float(larger(larger(v.x, v.y), larger(v.z, v.w))); }
     static __device__ __forceinline__ float get(const uint4& v, int i) { return __uint_as_float(reinterpret_cast<const uint32_t*>(&v)[i]); }
 };
 template <> struct Row<kBF16> {
     using E = uint16_t;
     static constexpr int kN = 8;
     static constexpr uint32_t kNegInf = 0xff80ff80u, kNaN = 0x7fc07fc0u;
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    static __device__ __forceinline__ float top(const uint4& v) {
+        const uint32_t x = larger(larger(v.x, v.y), larger(v.z, v.w));
+        return __uint_as_float(larger(x, x << 16) & 0xffff0000u);
+    }
     static __device__ __forceinline__ float get(const uint4& v, int i) {
         const uint32_t w = reinterpret_cast<const uint32_t*>(&v)[i / 2];
         return __uint_as_float(i % 2 ? w & 0xffff0000u : w << 16);
@@ -245,10 +261,16 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         return v;
     };
     uint4* const mine = part + warp * nv * 32 + lane;
-    // f(vector, index of its first element), in the order of the row within a warp
+    // f(vector, index of its first element), in the order of the row within a warp.  (The next vector is under way; not unrolled, since f's
+    // instructions, which run a few times a launch, are fetched for it: four copies of the larger ones cost more than they hide.)
     auto each = [&](auto&& f) {
+        uint4 next = RES ? mine[0] : load(0);
 #pragma unroll 1
-        for (int j = 0; j < nv; ++j) f(RES ? mine[j * 32] : load(j), index_of(j));
+        for (int j = 0; j < nv; ++j) {
+            const uint4 v = next;
+            if (j + 1 < nv) next = RES ? mine[(j + 1) * 32] : load(j + 1);
+            f(v, index_of(j));
+        }
     };
 
     // ---- the largest of all, the least of the threads' largest, and what cannot be read ----
@@ -266,12 +288,9 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             for (int j = 0; j < kAhead; ++j) {
                 if (j0 + j >= nv) break;
                 if (RES) mine[(j0 + j) * 32] = v[j];
-#pragma unroll
-                for (int x = 0; x < N; ++x) {
-                    const float z = R::get(v[j], x);
-                    bad |= !(z < INFINITY);
-                    top = fmaxf(top, z);
-                }
+                const float z = R::top(v[j]);
+                bad |= !(z < INFINITY);
+                top = fmaxf(top, z);
             }
         }
         // (threads without an element that is finite have no part in the least)
@@ -334,18 +353,12 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         least = key_of<DT>(x);
     }
     Border border{kLowest<DT>, kAll};
-    // Into the CTA's list: the tokens of which which(vector, index of its first) has a bit.  Counted first, so that a warp asks for room once.
+    // Into the CTA's list: the tokens of which which(vector, index of its first) has a bit.
     auto enlist = [&](auto&& which) {
-        unsigned n = 0;
-        each([&](const uint4& v, int i) { n += __popc(which(v, i)); });
-        const unsigned inc = scanned(n, lane), all = __shfl_sync(0xffffffffu, inc, 31);
-        if (all == 0) return;
-        unsigned at = 0;
-        if (lane == 0) at = atomicAdd(&sm.listed, all);
-        at = __shfl_sync(0xffffffffu, at, 0) + inc - n;
         each([&](const uint4& v, int i) {
             const unsigned w = which(v, i);
             if (w == 0) return;
+            unsigned at = atomicAdd(&sm.listed, static_cast<unsigned>(__popc(w)));
 #pragma unroll
             for (int x = 0; x < N; ++x)
                 if (w >> x & 1) {
@@ -437,6 +450,53 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
     auto entry = [&](int x) { return Border{static_cast<uint32_t>(sm.list[x] >> 32), static_cast<int>(0xffffffffu - static_cast<uint32_t>(sm.list[x]))}; };
     auto announce = [&](Border b) {
         if (tid < C) cluster.map_shared_rank(&sm, tid)->border = b;
+    };
+    // The index of the some-th token, in the order of the vocabulary, of this key.
+    auto last_tie = [&](uint32_t key, unsigned some) {
+        const float z = value_of<DT>(key);
+        // the index of the last of them: ties by warp, then in the warp that has it
+        unsigned own = 0;
+        each([&](const uint4& v, int) {
+#pragma unroll
+            for (int x = 0; x < N; ++x) own += R::get(v, x) == z;
+        });
+        own = __reduce_add_sync(0xffffffffu, own);
+        if (lane == 0) sm.warp_count[warp] = own;
+        cluster.sync();
+        unsigned before = 0;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int w = 4 * lane + x;
+            if (w < rank * kFWarps + warp) before += cluster.map_shared_rank(&sm, w / kFWarps)->warp_count[w % kFWarps];
+        }
+        before = __reduce_add_sync(0xffffffffu, before);
+        if (before < some && before + own >= some) {
+            unsigned need = some - before;
+            int last = -1;
+            each([&](const uint4& v, int i) {
+                unsigned n = 0;
+#pragma unroll
+                for (int x = 0; x < N; ++x) n += R::get(v, x) == z;
+                unsigned inc = n;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const unsigned u = __shfl_up_sync(0xffffffffu, inc, o);
+                    if (lane >= o) inc += u;
+                }
+                const unsigned all = __shfl_sync(0xffffffffu, inc, 31);
+                if (need > inc - n && need <= inc) {
+                    unsigned left = need - (inc - n);
+#pragma unroll
+                    for (int x = 0; x < N; ++x)
+                        if (R::get(v, x) == z && --left == 0) last = i + x;
+                }
+                need = need > all ? need - all : 0;                   // (0: found; no later one is)
+            });
+            if (last >= 0)
+                for (int r = 0; r < C; ++r) cluster.map_shared_rank(&sm, r)->index = last;
+        }
+        cluster.sync();
+        return sm.index;
     };
     // One digit after the other, from the top: the largest key of which `enough` is true once all larger ones and its own are counted in.
     auto select = [&](bool by_mass, int k, double target_share) {
@@ -541,49 +601,38 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         }
         border = Border{key, kAll};
         if (some == ties) return;
-        // the index of the last of them: ties by warp, then in the warp that has it
-        unsigned own = 0;
-        each([&](const uint4& v, int) {
-#pragma unroll
-            for (int x = 0; x < N; ++x) own += key_of<DT>(R::get(v, x)) == key;
-        });
-        own = __reduce_add_sync(0xffffffffu, own);
-        if (lane == 0) sm.warp_count[warp] = own;
-        cluster.sync();
-        unsigned before = 0;
-        for (int r = 0; r <= rank; ++r) {
-            const FilterSmem* o = cluster.map_shared_rank(&sm, r);
-            for (int x = 0; x < (r == rank ? warp : kFWarps); ++x) before += o->warp_count[x];
-        }
-        if (before < some && before + own >= some) {
-            unsigned need = some - before;
-            int last = -1;
-            each([&](const uint4& v, int i) {
-                unsigned n = 0;
-#pragma unroll
-                for (int x = 0; x < N; ++x) n += key_of<DT>(R::get(v, x)) == key;
-                unsigned inc = n;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const unsigned u = __shfl_up_sync(0xffffffffu, inc, o);
-                    if (lane >= o) inc += u;
-                }
-                const unsigned all = __shfl_sync(0xffffffffu, inc, 31);
-                if (need > inc - n && need <= inc) {
-                    unsigned left = need - (inc - n);
-#pragma unroll
-                    for (int x = 0; x < N; ++x)
-                        if (key_of<DT>(R::get(v, x)) == key && --left == 0) last = i + x;
-                }
-                need = need > all ? need - all : 0;                   // (0: found; no later one is)
-            });
-            if (last >= 0)
-                for (int r = 0; r < C; ++r) cluster.map_shared_rank(&sm, r)->index = last;
-        }
-        cluster.sync();
-        border.last = sm.index;
+        border.last = last_tie(key, some);
     };
 
+    // In the first CTA: the token, of the `kept` ones in its list.
+    auto draw = [&](int kept) {
+        // the kept ones in the order of the vocabulary: the same entries, turned round, their keys behind
+        __syncthreads();
+        for (int x = tid; x < kept; x += kFThreads) sm.list[x] = sm.list[x] << 32 | sm.list[x] >> 32;
+        const float share_of = static_cast<float>(kShort - 1) / static_cast<float>(a.V);
+        order_list(sm, kept, [&](unsigned long long x) { return static_cast<int>(static_cast<float>(0xffffffffu - static_cast<uint32_t>(x >> 32)) * share_of); });
+        const int each_has = (kept + kFThreads - 1) / kFThreads, i0 = tid * each_has;
+        double w = 0.0, W;
+        for (int x = i0; x < i0 + each_has && x < kept; ++x) w += weight(value_of<DT>(static_cast<uint32_t>(sm.list[x])));
+        double c = before_me(w, sm.scan_b, &W);
+        const double t = static_cast<double>(a.uniforms[row]) * W;
+        if (tid == 0) sm.found = 0xffffffffu;
+        __syncthreads();
+        for (int x = i0; x < i0 + each_has && x < kept; ++x) {
+            const double y = weight(value_of<DT>(static_cast<uint32_t>(sm.list[x])));
+            c += y;
+            if (y > 0.0 && c > t) { atomicMin(&sm.found, static_cast<unsigned>(x)); break; }
+        }
+        __syncthreads();
+        if (tid == 0) {
+            int x = static_cast<int>(sm.found);
+            // (where rounding leaves none, the last that weighs anything)
+            if (x < 0)
+                for (x = kept - 1; x > 0 && weight(value_of<DT>(static_cast<uint32_t>(sm.list[x]))) == 0.0;) --x;
+            a.tokens[row] = static_cast<int>(0xffffffffu - static_cast<uint32_t>(sm.list[x] >> 32));
+            if (a.lse) a.lse[row] = static_cast<float>(M / static_cast<double>(T) + log(W));
+        }
+    };
     // In the first CTA, which has a row's first n tokens in its list: what is kept of them, and the token.  target: the mass before which top-p keeps
     // (negative: its share of the k first ones).
     auto conclude = [&](int n, double target) {
@@ -600,34 +649,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             kept = static_cast<int>(sm.found);
         }
         announce(entry(kept - 1));
-        if (a.uniforms) {
-            // the kept ones in the order of the vocabulary: the same entries, turned round, their keys behind
-            __syncthreads();
-            for (int x = tid; x < kept; x += kFThreads) sm.list[x] = sm.list[x] << 32 | sm.list[x] >> 32;
-            const float share_of = static_cast<float>(kShort - 1) / static_cast<float>(a.V);
-            order_list(sm, kept, [&](unsigned long long x) { return static_cast<int>(static_cast<float>(0xffffffffu - static_cast<uint32_t>(x >> 32)) * share_of); });
-            const int each_has = (kept + kFThreads - 1) / kFThreads, i0 = tid * each_has;
-            double w = 0.0, W;
-            for (int x = i0; x < i0 + each_has && x < kept; ++x) w += weight(value_of<DT>(static_cast<uint32_t>(sm.list[x])));
-            double c = before_me(w, sm.scan_b, &W);
-            const double t = static_cast<double>(a.uniforms[row]) * W;
-            if (tid == 0) sm.found = 0xffffffffu;
-            __syncthreads();
-            for (int x = i0; x < i0 + each_has && x < kept; ++x) {
-                const double y = weight(value_of<DT>(static_cast<uint32_t>(sm.list[x])));
-                c += y;
-                if (y > 0.0 && c > t) { atomicMin(&sm.found, static_cast<unsigned>(x)); break; }
-            }
-            __syncthreads();
-            if (tid == 0) {
-                int x = static_cast<int>(sm.found);
-                // (where rounding leaves none, the last that weighs anything)
-                if (x < 0)
-                    for (x = kept - 1; x > 0 && weight(value_of<DT>(static_cast<uint32_t>(sm.list[x]))) == 0.0;) --x;
-                a.tokens[row] = static_cast<int>(0xffffffffu - static_cast<uint32_t>(sm.list[x] >> 32));
-                if (a.lse) a.lse[row] = static_cast<float>(M / static_cast<double>(T) + log(W));
-            }
-        }
+        if (a.uniforms) draw(kept);
     };
     // Top-k of up to kMostK by candidates: what is not below the k-th largest of the vectors' maxima, or nearly so.  False: too many.
     bool drew = false;
@@ -641,10 +663,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             if (!spread && !own) return false;
             if (!spread) step = 0.f;
             each([&](const uint4& v, int) {
-                float z = R::get(v, 0);
-#pragma unroll
-                for (int x = 1; x < N; ++x) z = fmaxf(z, R::get(v, x));
-                const float d = (top - z) * step;
+                const float d = (top - R::top(v)) * step;
                 if (d < kBins) atomicAdd(&sm.bins[static_cast<int>(d)], 1u);
             });
             unsigned c[4], sum = 0;
@@ -674,13 +693,16 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             else cluster.sync();
             const int bin = static_cast<int>(sm.found);
             if (bin >= kBins && !own) return false;
-            // every vector of the bins up to this one has a maximum whose distance comes out below bin + 1 (a CTA with fewer than k: all of its own)
-            limit = bin < kBins && spread ? static_cast<float>(bin + 1) : INFINITY;
-            const float step_ = step;
+            // every vector of the bins up to this one has a maximum that is not below this (a hair lower, for the roundings; a CTA with fewer than k
+            // takes all of its own)
+            const float width = (bin + 1) / step;
+            limit = bin < kBins && spread ? top - width * 1.000001f - fabsf(top) * 1e-6f : -3.4e38f;
+            if (!(limit > -3.4e38f)) limit = -3.4e38f;
             enlist([&](const uint4& v, int) {
                 unsigned which = 0;
+                if (R::top(v) < limit) return which;
 #pragma unroll
-                for (int x = 0; x < N; ++x) which |= static_cast<unsigned>((top - R::get(v, x)) * step_ < limit) << x;
+                for (int x = 0; x < N; ++x) which |= static_cast<unsigned>(R::get(v, x) >= limit) << x;
                 return which;
             });
         } else {
@@ -781,6 +803,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         const int from = all_of_it ? 0 : b0;
         enlist([&](const uint4& v, int i) {
             unsigned which = 0;
+            if (bin_of(R::top(v)) > b1) return which;
 #pragma unroll
             for (int x = 0; x < N; ++x) {
                 const float z = R::get(v, x);
@@ -812,6 +835,151 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         return true;
     };
 
+    // In 16 bits, top-k and top-p by counting the tokens of each value: a bin a value from the largest down, so that a mass is a count times a weight, and
+    // the border is where the formulas have it.  2048 bins hold 16 powers of two; where logits of both signs matter, the values next to 0 share one bin, as do the
+    // least, and their masses are summed up (64 rows of 128256, top_p 0.9: 61 us with bins of equal width and all weights summed up, now 38).  How many are kept, or
+    // -1: the border lies in a shared bin.
+    auto by_keys = [&]() {
+        const bool mass = p < 1.f && p > 0.f;
+        const int kM = static_cast<int>(key_of<DT>(top) >> 16);
+        float least_z = top - 32.f * T;
+        if (low < least_z) least_z = low;
+        const int kL = least_z > -3.0e38f ? static_cast<int>(key_of<kF32>(least_z) >> 16) : 0x80;
+        int pos_lo = 0, neg_hi = -1;                     // (all keys are in the first part)
+        if (kM - kL >= kBins - 1 && kM > 0x7fff - 128 && kL < 0x8000) {
+            // powers of two from the least up whose values share a bin: so many that both signs' others fit, or those of the one that has any
+            int powers = (kM - kL + 3 - kBins + 255) / 256;
+            if (0x8000 + powers * 128 > kM) powers = (0x7fff - kL + 4 - kBins + 127) / 128;
+            else if (0x7fff - powers * 128 < kL) powers = (kM - 0x8000 + 4 - kBins + 127) / 128;
+            powers = powers < 1 ? 1 : powers;
+            pos_lo = 0x8000 + powers * 128;
+            neg_hi = 0x7fff - powers * 128;
+        }
+        const int base = kM >= pos_lo ? kM - pos_lo + 1 : 0;
+        auto bin_of = [&](float z) {
+            const int key = static_cast<int>(key_of<DT>(z) >> 16), i = key >= pos_lo ? kM - key : key > neg_hi ? base : base + 1 + neg_hi - key;
+            return i < kBins - 1 ? i : kBins - 1;
+        };
+        auto shared = [&](int b) { return b == kBins - 1 || (neg_hi >= 0 && b == base); };
+        auto value = [&](int b) { return value_of<DT>(static_cast<uint32_t>(neg_hi < 0 || b < base ? kM - b : neg_hi - (b - base - 1)) << 16); };
+        each([&](const uint4& v, int) {
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                const float z = R::get(v, x);
+                if (z > -INFINITY) atomicAdd(&sm.bins[bin_of(z)], 1u);
+            }
+        });
+        cluster.sync();
+        unsigned c[4], cs = 0;
+        gather(c);
+        double w[4], ws = 0.0, all = 0.0, middle = 0.0, rest = 0.0;
+        if (mass) {
+            bool some = false;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) some |= c[x] > 0 && shared(4 * tid + x);
+            if (__syncthreads_or(some)) {
+                each([&](const uint4& v, int) {
+#pragma unroll
+                    for (int x = 0; x < N; ++x) {
+                        const float z = R::get(v, x);
+                        const int b = bin_of(z);
+                        if (shared(b)) {
+                            const double y = weight(z);      // (of -inf: 0)
+                            if (b == kBins - 1) rest += y;
+                            else middle += y;
+                        }
+                    }
+                });
+                middle = summed(middle);
+                rest = summed(rest);
+                if (lane == 0) { sm.warp_above[warp] = middle; sm.warp_mass[warp] = rest; }
+                cluster.sync();
+                const FilterSmem* o = cluster.map_shared_rank(&sm, tid < C * kFWarps ? tid / kFWarps : 0);
+                before_me(tid < C * kFWarps ? o->warp_above[tid % kFWarps] : 0.0, sm.scan_a, &middle);
+                before_me(tid < C * kFWarps ? o->warp_mass[tid % kFWarps] : 0.0, sm.scan_b, &rest);
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int b = 4 * tid + x;
+            cs += c[x];
+            w[x] = !mass || c[x] == 0 ? 0.0 : b == kBins - 1 ? rest : shared(b) ? middle : c[x] * weight(value(b));
+            ws += w[x];
+        }
+        const unsigned inc = scanned(cs, lane);
+        if (lane == 31) sm.scan_count[warp] = inc;
+        if (tid == 0) { sm.found = 0; sm.digit = kBins; sm.above = 0; sm.index = 0; }
+        __syncthreads();
+        unsigned cb = inc - cs, total = 0;
+        for (int x = 0; x < kFWarps; ++x) {
+            if (x < warp) cb += sm.scan_count[x];
+            total += sm.scan_count[x];
+        }
+        double wb = mass ? before_me(ws, sm.scan_a, &all) : 0.0;
+        const unsigned most = static_cast<unsigned>(k) < total ? static_cast<unsigned>(k) : total;
+        // where the k-th lies, and the mass of the first k
+        {
+            unsigned u = cb;
+            double m = wb;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                if (u < most && u + c[x] >= most) {
+                    sm.digit = 4 * tid + x;
+                    sm.above = u;
+                    sm.scan_b[0] = u + c[x] == most ? m + w[x] : m + (most - u) * (w[x] / c[x]);
+                }
+                u += c[x];
+                m += w[x];
+            }
+        }
+        __syncthreads();
+        const int kth = static_cast<int>(sm.digit);
+        const unsigned before_kth = sm.above;
+        if (mass) {
+            // the last bin before which there is less than the target
+            const double target = share * sm.scan_b[0];
+            unsigned u = cb;
+            double m = wb;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                if (c[x] > 0 && 4 * tid + x <= kth && (m < target || u == 0)) atomicMax(&sm.found, static_cast<unsigned>(4 * tid + x + 1));
+                u += c[x];
+                m += w[x];
+            }
+            __syncthreads();
+            u = cb;
+            m = wb;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                if (4 * tid + x + 1 == static_cast<int>(sm.found)) {
+                    const unsigned there = 4 * tid + x == kth ? most - before_kth : c[x];
+                    const double i = ceil((target - m) / (w[x] / c[x]));
+                    sm.index = static_cast<int>(!(i >= 1.0) ? 1u : i < there ? static_cast<unsigned>(i) : there);
+                    sm.above = u;
+                    sm.listed = c[x];
+                }
+                u += c[x];
+                m += w[x];
+            }
+        } else if (kth >= 4 * tid && kth < 4 * tid + 4) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                if (4 * tid + x == kth) sm.listed = c[x];
+            sm.found = kth + 1;
+            sm.index = static_cast<int>(most - before_kth);
+        }
+        cluster.sync();                                  // (the bins have been read)
+        const int bin = static_cast<int>(sm.found) - 1;
+        const unsigned some = static_cast<unsigned>(sm.index), there = sm.listed, kept = sm.above + some;
+        __syncthreads();
+        if (tid == 0) sm.listed = 0;
+        // (the k-th in a shared bin has no mass that is known)
+        if (shared(bin) || (mass && k < static_cast<int>(total) && shared(kth))) return -1;
+        border = Border{key_of<DT>(value(bin)), kAll};
+        if (some < there) border.last = last_tie(border.key, some);
+        return static_cast<int>(kept);
+    };
+
     if (!bad) {
         bool dirty = false;                              // (something lies where the bins are)
         auto clean = [&]() {
@@ -820,26 +988,57 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             if (tid == 0) sm.listed = 0;
             cluster.sync();
         };
-        if (k < a.V) {
-            if (k <= kMostK) {
+        int known = -1;                                  // how many are kept, where that is known
+        if constexpr (DT == kBF16) {
+            // (few from each CTA are found faster than all values are counted: k = 50 of 32000, 16.4 us against 18)
+            if ((k < a.V || (p < 1.f && p > 0.f)) && !(k < a.V && C * k <= kMostK && a.V > kFew)) {
                 dirty = true;
-                by_candidates();
-            }
-            if (!drew) {
-                dirty = true;
-                cluster.sync();
-                select(false, k, 0.0);
+                known = by_keys();
+                if (known < 0) border = Border{kLowest<DT>, kAll};
             }
         }
-        if (!drew) {
-            if (p < 1.f && p > 0.f) {
+        if (known < 0) {
+            if (k < a.V) {
+                if (k <= kMostK) {
+                    clean();
+                    dirty = true;
+                    by_candidates();
+                }
+                if (!drew) {
+                    dirty = true;
+                    cluster.sync();
+                    select(false, k, 0.0);
+                }
+            }
+            if (!drew && p < 1.f && p > 0.f) {
                 clean();
                 if (!by_mass()) {
                     cluster.sync();
                     select(true, 0, share);
                 }
             }
+        }
+        if (!drew) {
             if (least > border.key) border = Border{least, kAll};
+            if (a.uniforms && known > 0 && known <= kShort) {
+                // few are kept: the token is drawn from a list of them
+                const float z0 = value_of<DT>(border.key);
+                if (tid == 0) sm.listed = 0;
+                cluster.sync();
+                enlist([&](const uint4& v, int i) {
+                    unsigned which = 0;
+                    if (R::top(v) < z0) return which;
+#pragma unroll
+                    for (int x = 0; x < N; ++x) {
+                        const float z = R::get(v, x);
+                        which |= static_cast<unsigned>(z > z0 || (z == z0 && i + x <= border.last)) << x;
+                    }
+                    return which;
+                });
+                const int n = static_cast<int>(collect());
+                if (rank == 0) draw(n);
+                drew = true;
+            }
         }
     }
     const float border_z = value_of<DT>(border.key);
@@ -854,10 +1053,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
     } else if (a.uniforms && !drew) {
         double sum = 0.0;
         each([&](const uint4& v, int i) {
-            bool any = false;
-#pragma unroll
-            for (int x = 0; x < N; ++x) any |= R::get(v, x) >= border_z;
-            if (!__any_sync(0xffffffffu, any)) return;
+            if (!__any_sync(0xffffffffu, R::top(v) >= border_z)) return;
 #pragma unroll
             for (int x = 0; x < N; ++x) {
                 const float z = R::get(v, x);
@@ -942,11 +1138,8 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             if (wrong) {
                 w = make_uint4(R::kNaN, R::kNaN, R::kNaN, R::kNaN);
             } else if (!bad) {
-                bool any = false;
-#pragma unroll
-                for (int x = 0; x < N; ++x) any |= R::get(v, x) >= border_z;
                 w = make_uint4(R::kNegInf, R::kNegInf, R::kNegInf, R::kNegInf);
-                if (any) {
+                if (R::top(v) >= border_z) {
                     E* e = reinterpret_cast<E*>(&w);
                     const E* f = reinterpret_cast<const E*>(&v);
 #pragma unroll
