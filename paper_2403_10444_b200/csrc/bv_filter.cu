@@ -123,6 +123,17 @@ constexpr int kShort = kList / 2;        // of a list that leaves room for bucke
 constexpr int kMostK = 1024;             // of a top-k by candidates
 constexpr int kFew = 2048;               // tokens of which all are candidates
 
+// Values of 16 bits to bins, a bin a value from the largest down: keys from kM down to pos_lo, one bin for those between pos_lo and neg_hi (values next to 0),
+// then from neg_hi down; the last bin takes all the rest.  neg_hi below 0: no such bin between.
+struct KeyBins {
+    int kM, pos_lo, neg_hi, base;
+    __device__ __forceinline__ int bin(float z) const {
+        const int key = static_cast<int>(key_of<kBF16>(z) >> 16), i = key >= pos_lo ? kM - key : key > neg_hi ? base : base + 1 + neg_hi - key;
+        return i < kBins - 1 ? i : kBins - 1;
+    }
+    __device__ __forceinline__ bool shared(int b) const { return b == kBins - 1 || (neg_hi >= 0 && b == base); }
+    __device__ __forceinline__ float value(int b) const { return value_of<kBF16>(static_cast<uint32_t>(neg_hi < 0 || b < base ? kM - b : neg_hi - (b - base - 1)) << 16); }
+};
 struct FilterSmem {
     union {
         unsigned bins[kBins];
@@ -261,19 +272,41 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         return v;
     };
     uint4* const mine = part + warp * nv * 32 + lane;
-    // f(vector, index of its first element), in the order of the row within a warp.  (The next vector is under way; not unrolled, since f's
-    // instructions, which run a few times a launch, are fetched for it: four copies of the larger ones cost more than they hide.)
+    // f(vector, index of its first element), in the order of the row within a warp.  From shared memory the next vector is under way (and f is there
+    // once: its instructions, which run a few times a launch, are fetched for it); from memory four vectors are.
     auto each = [&](auto&& f) {
-        uint4 next = RES ? mine[0] : load(0);
+        if constexpr (RES) {
+            uint4 next = mine[0];
 #pragma unroll 1
-        for (int j = 0; j < nv; ++j) {
-            const uint4 v = next;
-            if (j + 1 < nv) next = RES ? mine[(j + 1) * 32] : load(j + 1);
-            f(v, index_of(j));
+            for (int j = 0; j < nv; ++j) {
+                const uint4 v = next;
+                if (j + 1 < nv) next = mine[(j + 1) * 32];
+                f(v, index_of(j));
+            }
+        } else {
+#pragma unroll 1
+            for (int j0 = 0; j0 < nv; j0 += 4) {
+                uint4 v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j0 + j < nv) v[j] = load(j0 + j);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j0 + j < nv) f(v[j], index_of(j0 + j));
+            }
         }
     };
 
     // ---- the largest of all, the least of the threads' largest, and what cannot be read ----
+    const float T = a.temperatures ? a.temperatures[row] : a.temperature, p = a.top_ps ? a.top_ps[row] : a.top_p, m = a.min_ps ? a.min_ps[row] : a.min_p;
+    int k = a.top_ks ? a.top_ks[row] : a.top_k;
+    if (k <= 0 || k > a.V) k = a.V;
+    if (p == 0.f) k = 1;                               // (the first one always)
+    // (few from each CTA are found faster than all values are counted: k = 50 of 32000, 14.5 us against 18)
+    const bool counting = DT == kBF16 && (k < a.V || (p < 1.f && p > 0.f)) && !(k < a.V && C * k <= kMostK && a.V > kFew);
+    for (int x = tid; x < kBins; x += kFThreads) sm.bins[x] = 0;
+    if (tid == 0) sm.listed = 0;
+    if (tid < kRoots) sm.roots[tid] = exp2(static_cast<double>(tid) / kRoots);
     float top = -INFINITY;
     bool bad = false;
     {
@@ -302,9 +335,6 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         }
         bad = __any_sync(0xffffffffu, bad);
         if (lane == 0) { sm.warp_top[warp] = top; sm.warp_low[warp] = low; sm.warp_bad[warp] = bad; }
-        for (int x = tid; x < kBins; x += kFThreads) sm.bins[x] = 0;
-        if (tid == 0) sm.listed = 0;
-        if (tid < kRoots) sm.roots[tid] = exp2(static_cast<double>(tid) / kRoots);
         __syncthreads();
         if (warp == 0) {
             top = lane < kFWarps ? sm.warp_top[lane] : -INFINITY;
@@ -336,10 +366,6 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         low = __shfl_sync(0xffffffffu, low, 0);
         bad = __shfl_sync(0xffffffffu, static_cast<int>(bad), 0) != 0;
     }
-    const float T = a.temperatures ? a.temperatures[row] : a.temperature, p = a.top_ps ? a.top_ps[row] : a.top_p, m = a.min_ps ? a.min_ps[row] : a.min_p;
-    int k = a.top_ks ? a.top_ks[row] : a.top_k;
-    if (k <= 0 || k > a.V) k = a.V;
-    if (p == 0.f) k = 1;                               // (the first one always)
     const bool wrong = !(T > 0.f && T < INFINITY && p >= 0.f && m >= 0.f && m <= 1.f);
     bad |= top == -INFINITY || wrong;
     const double scale = kRoots * 1.4426950408889634073599246810019 / static_cast<double>(T), M = static_cast<double>(top), share = static_cast<double>(p);
@@ -633,11 +659,8 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             if (a.lse) a.lse[row] = static_cast<float>(M / static_cast<double>(T) + log(W));
         }
     };
-    // In the first CTA, which has a row's first n tokens in its list: what is kept of them, and the token.  target: the mass before which top-p keeps
-    // (negative: its share of the k first ones).
-    auto conclude = [&](int n, double target) {
-        order_by_value(n);
-        int kept = end_of_list(n, k, 0.0, target);
+    // In the first CTA, whose list begins with the `kept` first tokens in order: min-p, the border for all CTAs, the token.
+    auto finish = [&](int kept) {
         // (of keys in order, those below min-p's border come last)
         if (least > 0) {
             __syncthreads();
@@ -650,6 +673,12 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         }
         announce(entry(kept - 1));
         if (a.uniforms) draw(kept);
+    };
+    // In the first CTA, which has a row's first n tokens in its list: what is kept of them, and the token.  target: the mass before which top-p keeps
+    // (negative: its share of the k first ones).
+    auto conclude = [&](int n, double target) {
+        order_by_value(n);
+        finish(end_of_list(n, k, 0.0, target));
     };
     // Top-k of up to kMostK by candidates: what is not below the k-th largest of the vectors' maxima, or nearly so.  False: too many.
     bool drew = false;
@@ -845,31 +874,28 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         float least_z = top - 32.f * T;
         if (low < least_z) least_z = low;
         const int kL = least_z > -3.0e38f ? static_cast<int>(key_of<kF32>(least_z) >> 16) : 0x80;
-        int pos_lo = 0, neg_hi = -1;                     // (all keys are in the first part)
+        KeyBins bins{kM, 0, -1, 0};                // (all keys are in the first part)
         if (kM - kL >= kBins - 1 && kM > 0x7fff - 128 && kL < 0x8000) {
             // powers of two from the least up whose values share a bin: so many that both signs' others fit, or those of the one that has any
             int powers = (kM - kL + 3 - kBins + 255) / 256;
             if (0x8000 + powers * 128 > kM) powers = (0x7fff - kL + 4 - kBins + 127) / 128;
             else if (0x7fff - powers * 128 < kL) powers = (kM - 0x8000 + 4 - kBins + 127) / 128;
             powers = powers < 1 ? 1 : powers;
-            pos_lo = 0x8000 + powers * 128;
-            neg_hi = 0x7fff - powers * 128;
+            bins.pos_lo = 0x8000 + powers * 128;
+            bins.neg_hi = 0x7fff - powers * 128;
+            bins.base = kM >= bins.pos_lo ? kM - bins.pos_lo + 1 : 0;
         }
-        const int base = kM >= pos_lo ? kM - pos_lo + 1 : 0;
-        auto bin_of = [&](float z) {
-            const int key = static_cast<int>(key_of<DT>(z) >> 16), i = key >= pos_lo ? kM - key : key > neg_hi ? base : base + 1 + neg_hi - key;
-            return i < kBins - 1 ? i : kBins - 1;
-        };
-        auto shared = [&](int b) { return b == kBins - 1 || (neg_hi >= 0 && b == base); };
-        auto value = [&](int b) { return value_of<DT>(static_cast<uint32_t>(neg_hi < 0 || b < base ? kM - b : neg_hi - (b - base - 1)) << 16); };
         each([&](const uint4& v, int) {
 #pragma unroll
             for (int x = 0; x < N; ++x) {
                 const float z = R::get(v, x);
-                if (z > -INFINITY) atomicAdd(&sm.bins[bin_of(z)], 1u);
+                if (z > -INFINITY) atomicAdd(&sm.bins[bins.bin(z)], 1u);
             }
         });
         cluster.sync();
+        auto shared = [&](int b) { return bins.shared(b); };
+        auto value = [&](int b) { return bins.value(b); };
+        auto bin_of = [&](float z) { return bins.bin(z); };
         unsigned c[4], cs = 0;
         gather(c);
         double w[4], ws = 0.0, all = 0.0, middle = 0.0, rest = 0.0;
@@ -976,7 +1002,8 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         // (the k-th in a shared bin has no mass that is known)
         if (shared(bin) || (mass && k < static_cast<int>(total) && shared(kth))) return -1;
         border = Border{key_of<DT>(value(bin)), kAll};
-        if (some < there) border.last = last_tie(border.key, some);
+        // (a short list that a token is drawn from shows which of equal ones are kept)
+        if (some < there && !(a.uniforms && kept - some + there <= kShort)) border.last = last_tie(border.key, some);
         return static_cast<int>(kept);
     };
 
@@ -990,8 +1017,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         };
         int known = -1;                                  // how many are kept, where that is known
         if constexpr (DT == kBF16) {
-            // (few from each CTA are found faster than all values are counted: k = 50 of 32000, 16.4 us against 18)
-            if ((k < a.V || (p < 1.f && p > 0.f)) && !(k < a.V && C * k <= kMostK && a.V > kFew)) {
+            if (counting) {
                 dirty = true;
                 known = by_keys();
                 if (known < 0) border = Border{kLowest<DT>, kAll};
@@ -1019,9 +1045,8 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             }
         }
         if (!drew) {
-            if (least > border.key) border = Border{least, kAll};
             if (a.uniforms && known > 0 && known <= kShort) {
-                // few are kept: the token is drawn from a list of them
+                // Few are kept: they are listed, those equal to the last among them, put in order, and the token is drawn from the list.
                 const float z0 = value_of<DT>(border.key);
                 if (tid == 0) sm.listed = 0;
                 cluster.sync();
@@ -1036,8 +1061,15 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
                     return which;
                 });
                 const int n = static_cast<int>(collect());
-                if (rank == 0) draw(n);
+                if (rank == 0) {
+                    order_by_value(n);
+                    finish(known < n ? known : n);
+                }
+                cluster.sync();
+                border = sm.border;
                 drew = true;
+            } else if (least > border.key) {
+                border = Border{least, kAll};
             }
         }
     }
