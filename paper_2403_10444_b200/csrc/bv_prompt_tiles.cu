@@ -25,6 +25,7 @@ constexpr int kPromptThreads = 384, kSoftWarps = 8, kIssueWarp = 8, kLoadWarp = 
 constexpr int kUnits = 4;                      // marks of units: the cleaning warps are two units ahead of the weights at most
 constexpr float kNone = -3.0e38f;              // the reference of a row that has seen no score
 constexpr float kLag = 8.f;
+constexpr int kFirstKeys = 96;                 // of a tile, whose weights are multiplied while the others are formed
 constexpr int kMostPrompts = 1024;             // of a launch
 
 __device__ __forceinline__ void tma_load3(uint32_t dst, const CUtensorMap* map, int x, int head, int token, uint32_t bar) {
@@ -56,6 +57,12 @@ __device__ __forceinline__ void st32(uint32_t addr, const uint32_t* r) {
                  : "memory");
 }
 
+__device__ __forceinline__ void st16(uint32_t addr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+
 template <int NP>
 struct PromptShape {
     static constexpr int kPanel = kTile * 128, kSlot = NP * kPanel;        // a slot: NP panels of 128 rows of 64 columns
@@ -70,7 +77,7 @@ struct __align__(1024) PromptSmem {
     using Sh = PromptShape<NP>;
     char q[2][Sh::kSlot];
     char ring[Sh::kSlots][Sh::kSlot];
-    unsigned long long q_full[2], q_empty, full[8], empty[8], unclean[8], s_full[2], p_full[2], o_done[2], drain;
+    unsigned long long q_full[2], q_empty[2], full[8], empty[8], unclean[8], s_full[2], p_part[2], p_full[2], o_done[2], drain;
     uint32_t tmem;
     int abort;
     int fix[kUnits][2];                    // by unit, by cleaning warp: values that are not finite among those that some rows see
@@ -184,7 +191,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sm.q_full[i]), 1);
             mbar_init(smem_u32(&sm.s_full[i]), 1);
+            mbar_init(smem_u32(&sm.p_part[i]), kTile);
             mbar_init(smem_u32(&sm.p_full[i]), kTile);
+            mbar_init(smem_u32(&sm.q_empty[i]), 1);
             mbar_init(smem_u32(&sm.o_done[i]), 1);
         }
         for (int i = 0; i < kSlots; ++i) {
@@ -192,7 +201,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
             mbar_init(smem_u32(&sm.empty[i]), 1);
             mbar_init(smem_u32(&sm.unclean[i]), 1);
         }
-        mbar_init(smem_u32(&sm.q_empty), 1);
         mbar_init(smem_u32(&sm.drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         sm.abort = 0;
@@ -252,20 +260,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                 unsigned unclean = 0, phases = 0;      // by slot: does its last copy go through the cleaning warps, how many have (parity)
                 bool ok = true;
                 for (; ok && pair_at<NP>(a, sm, tokens_each, base, round, &p); ++round) {
-                    ok = wait_on<NP>(sm, sm.q_empty, (round & 1) ^ 1, a.status, limit);
-                    if (!ok) break;
                     const int tiles = list_length(p);
-                    for (int t = 0; t < (p.tiles[1] ? 2 : 1); ++t) {
-                        const uint32_t bar = smem_u32(&sm.q_full[t]);
-                        mbar_arrive_expect(bar, q_bytes);
-                        ++q_uses[t];
-#pragma unroll
-                        for (int c = 0; c < NP; ++c) tma_load3(smem_u32(sm.q[t]) + c * Sh::kPanel, &q_map, c * 64, p.h * a.group, p.first + p.t0 + t * tokens_each, bar);
-                    }
-                    for (int i = 0; i < 2 * tiles && ok; ++i, ++x) {
+                    auto fetch = [&](int i) {
                         const int slot = x % kSlots;
-                        ok = wait_on<NP>(sm, sm.empty[slot], (x / kSlots & 1) ^ 1, a.status, limit);
-                        if (!ok) break;
+                        ok = ok && wait_on<NP>(sm, sm.empty[slot], (x / kSlots & 1) ^ 1, a.status, limit);
+                        if (!ok) return;
                         // values that some rows do not see are handed on by the cleaning warps
                         const bool through = (i & 1) && !whole_tile(a, p.t0, p.p1, key_tile(p, i / 2));
                         const uint32_t bar = smem_u32(through ? &sm.unclean[slot] : &sm.full[slot]);
@@ -276,7 +275,20 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                         const CUtensorMap* map = i & 1 ? &v_map : &k_map;
 #pragma unroll
                         for (int c = 0; c < NP; ++c) tma_load3(smem_u32(sm.ring[slot]) + c * Sh::kPanel, map, c * 64, p.h, p.first + key_tile(p, i / 2) * kTile, bar);
+                        ++x;
+                    };
+                    // (the first keys need not wait until the unit before has its last scores, as the queries do)
+                    fetch(0);
+                    for (int t = 0; t < (p.tiles[1] ? 2 : 1) && ok; ++t) {
+                        ok = wait_on<NP>(sm, sm.q_empty[t], (q_uses[t] & 1) ^ 1, a.status, limit);
+                        if (!ok) break;
+                        const uint32_t bar = smem_u32(&sm.q_full[t]);
+                        mbar_arrive_expect(bar, q_bytes);
+                        ++q_uses[t];
+#pragma unroll
+                        for (int c = 0; c < NP; ++c) tma_load3(smem_u32(sm.q[t]) + c * Sh::kPanel, &q_map, c * 64, p.h * a.group, p.first + p.t0 + t * tokens_each, bar);
                     }
+                    for (int i = 1; i < 2 * tiles && ok; ++i) fetch(i);
                 }
                 // (a launch that gave up leaves when its copies are in)
                 if (*static_cast<volatile int*>(&sm.abort)) {
@@ -313,6 +325,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                                 mma(tmem + kS + t * kTile, desc(q_low + (s / 4 * Sh::kPanel + s % 4 * 32) / 16, desc_high(1024, 2)),
                                     desc(k_low + (s / 4 * Sh::kPanel + s % 4 * 32) / 16, desc_high(1024, 2)), qk, s > 0);
                         if (a.never_signal != 1) commit(smem_u32(&sm.s_full[t]));
+                        if (i + 1 == p.tiles[t]) commit(smem_u32(&sm.q_empty[t]));
                     };
                     wait(sm.full[x % kSlots], x / kSlots);
                     for (int t = 0; t < 2 && ok; ++t) {
@@ -324,19 +337,24 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                     }
                     if (!ok) break;
                     commit(smem_u32(&sm.empty[x % kSlots]));
-                    if (tiles == 1) commit(smem_u32(&sm.q_empty));
                     for (int i = 0; i < tiles && ok; ++i) {
                         const int v_at = x + 2 * i + 1, v_slot = v_at % kSlots, k_at = v_at + 1;
                         wait(sm.full[v_slot], v_at / kSlots);
                         bool next_in = false;
                         for (int t = 0; t < 2 && ok; ++t) {
                             if (i >= p.tiles[t]) continue;
-                            wait(sm.p_full[t], done[t]++);
+                            wait(sm.p_part[t], done[t]);
                             if (!ok) break;
                             fence_after();
                             const uint32_t v_low = desc_low(ring + v_slot * Sh::kSlot, Sh::kPanel);
 #pragma unroll
-                            for (int s = 0; s < kTile / 16; ++s)
+                            for (int s = 0; s < kFirstKeys / 16; ++s)
+                                mma_ts(tmem + kO + t * kTile, tmem + kS + t * kTile + s * 8, desc(v_low + s * 128, desc_high(1024, 2)), pv, i > 0 || s > 0);
+                            wait(sm.p_full[t], done[t]++);
+                            if (!ok) break;
+                            fence_after();
+#pragma unroll
+                            for (int s = kFirstKeys / 16; s < kTile / 16; ++s)
                                 mma_ts(tmem + kO + t * kTile, tmem + kS + t * kTile + s * 8, desc(v_low + s * 128, desc_high(1024, 2)), pv, i > 0 || s > 0);
                             commit(smem_u32(&sm.o_done[t]));
                             if (i + 1 < p.tiles[t]) {
@@ -350,7 +368,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                         if (!ok) break;
                         commit(smem_u32(&sm.empty[v_slot]));
                         if (i + 1 < tiles) commit(smem_u32(&sm.empty[k_at % kSlots]));
-                        if (i + 2 == tiles) commit(smem_u32(&sm.q_empty));
                     }
                     x += 2 * tiles;
                 }
@@ -435,7 +452,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                 if (!whole_tile(a, p0, last, j)) {
                     const int hi = pos - start, lo = low - start, sinks = a.sinks - start;         // seen: c <= hi and (c >= lo or c < sinks)
 #pragma unroll
-                    for (int c = 0; c < kTile; ++c) s[c] = c <= hi && (c >= lo || c < sinks) ? s[c] : -INFINITY;
+                    for (int c = 0; c < kTile; ++c) s[c] = c <= hi ? s[c] : -INFINITY;
+                    if (a.window > 0) {
+#pragma unroll
+                        for (int c = 0; c < kTile; ++c) s[c] = c >= lo || c < sinks ? s[c] : -INFINITY;
+                    }
                 }
                 float top[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
@@ -490,8 +511,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                     // (the sum is of the rounded weights: error of a row 0.0022 against 0.0023 with the others; a row of one key is its value)
                     sum[c / 2 & 1] = add2(sum[c / 2 & 1], pair2(__uint_as_float(w[c / 2] << 16), __uint_as_float(w[c / 2] & 0xffff0000u)));
                     if (c == 62) st32(s_at, w);
+                    if (c == kFirstKeys - 2) {
+                        st16(s_at + 32, w + 32);
+                        wait_st();
+                        fence_before();
+                        mbar_arrive(smem_u32(&sm.p_part[t]));
+                    }
                 }
-                st32(s_at + 32, w + 32);
+                st16(s_at + 48, w + 48);
                 float x, y;
                 unpair2(add2(sum[0], sum[1]), x, y);
                 l += x + y;
