@@ -139,6 +139,9 @@ __device__ __forceinline__ bool whole_tile(const PromptArgs& a, int p0, int p1, 
     return start + kTile - 1 <= p0 && (start >= low_of(a, p1) || start + kTile <= a.sinks);
 }
 
+// The lowest n bits.
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1; }
+
 // 2 floats at a time.
 __device__ __forceinline__ unsigned long long pair2(float x, float y) {
     unsigned long long r;
@@ -394,8 +397,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                     if (!ok) break;
                     phases ^= 1u << slot;
                     bool odd = false;
-                    for (int z = member; z < kTile * 8 * NP; z += kCleaners) {
-                        const int e = z % (8 * NP), row = z / (8 * NP), pos = start + row;
+                    // the keys before the last row's window, and those behind the first row
+                    const int pre = a.window > 0 && low1 > start ? (low1 - start < kTile ? low1 - start : kTile) : 0;
+                    const int sure = p.t0 + 1 - start < kTile ? p.t0 + 1 - start : kTile, post = sure > pre ? sure : pre;
+                    for (int z = member; z < (pre + kTile - post) * 8 * NP; z += kCleaners) {
+                        const int e = z % (8 * NP), y = z / (8 * NP), row = y < pre ? y : y - pre + post, pos = start + row;
                         const bool any = pos <= p.p1 && (pos >= p.low || pos < a.sinks);
                         if (any && pos <= p.t0 && (pos >= low1 || pos < a.sinks)) continue;       // (all see it)
                         uint4* const to = reinterpret_cast<uint4*>(sm.ring[slot] + e / 8 * Sh::kPanel + row * 128 + e % 8 * 16);
@@ -450,12 +456,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
 #pragma unroll
                 for (int c = 0; c < kTile; c += 8) wait_ld8(s + c);
                 if (!whole_tile(a, p0, last, j)) {
-                    const int hi = pos - start, lo = low - start, sinks = a.sinks - start;         // seen: c <= hi and (c >= lo or c < sinks)
+                    // seen: c <= hi and (c >= lo or c < sinks); a bit a key
+                    const int hi = pos - start, lo = low - start, sinks = a.sinks - start;
 #pragma unroll
-                    for (int c = 0; c < kTile; ++c) s[c] = c <= hi ? s[c] : -INFINITY;
-                    if (a.window > 0) {
+                    for (int w = 0; w < kTile; w += 32) {
+                        const uint32_t seen = below(hi + 1 - w) & (~below(lo - w) | below(sinks - w));
 #pragma unroll
-                        for (int c = 0; c < kTile; ++c) s[c] = c >= lo || c < sinks ? s[c] : -INFINITY;
+                        for (int c = 0; c < 32; ++c) s[w + c] = seen >> c & 1 ? s[w + c] : -INFINITY;
                     }
                 }
                 float top[4] = {s[0], s[1], s[2], s[3]};
@@ -533,18 +540,24 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
             const bool fix = (*static_cast<volatile int*>(&sm.fix[round % kUnits][0]) | *static_cast<volatile int*>(&sm.fix[round % kUnits][1])) != 0;
             const float f = l == 0.f ? NAN : 1.f / l;
             __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(a.out) + (p.first + static_cast<long long>(pos)) * a.os[0] + (p.h * a.group + head) * a.os[1];
+            // 32 columns at a time.  A lane has a row's 64 bytes; four lanes exchange them, so that a store of the warp is eight rows' whole sectors instead of
+            // 16 bytes of each of 32 (which were four times the time).
+            const long long out_at = reinterpret_cast<long long>(out);
+            const bool some = __any_sync(0xffffffffu, live);
 #pragma unroll 1
-            for (int c = 0; c < wide; c += 16) {
-                float o[16];
+            for (int c = 0; c < wide && some; c += 32) {
+                float o[32];
                 __syncwarp();
-                ld16(o_at + c, o);
-                wait_ld8(o);
-                wait_ld8(o + 8);
-                if (!live) continue;
-                if (fix) {
+                if (c + 16 < wide) {
+                    ld32(o_at + c, o);
+                } else {
+                    ld16(o_at + c, o);
+                }
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) wait_ld8(o + e);
+                if (fix && live) {
                     // what is not finite among the values that some rows of the unit see and others do not
-                    const int all = p.tiles[t];
-                    for (int i = 0; i < all; ++i) {
+                    for (int i = 0; i < p.tiles[t]; ++i) {
                         const int j = key_tile(p, i);
                         if (whole_tile(a, p.t0, p.p1, j)) continue;
                         for (int z = j * kTile; z < (j + 1) * kTile && z <= pos; ++z) {
@@ -552,7 +565,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                             // (those that all see have stayed where they were)
                             if (z <= p.t0 && (z >= low_of(a, p.p1) || z < a.sinks)) continue;
                             const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.v) + (p.first + static_cast<long long>(z)) * a.vs[0] + p.h * a.vs[1];
-                            for (int e = 0; e < 16; ++e) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
                                 if (c + e >= a.D) break;
                                 const float val = __bfloat162float(v[c + e]);
                                 if (!isfinite(val)) o[e] += val;
@@ -560,19 +574,49 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                         }
                     }
                 }
-                uint32_t w[8];
+                __syncwarp();
+                uint4 w[4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(o[2 * e] * f, o[2 * e + 1] * f);
-                    w[e] = *reinterpret_cast<const uint32_t*>(&h);
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t* const x = reinterpret_cast<uint32_t*>(&w[e]);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(o[8 * e + 2 * y] * f, o[8 * e + 2 * y + 1] * f);
+                        x[y] = *reinterpret_cast<const uint32_t*>(&h);
+                    }
                 }
                 if (out_vec) {
-                    if (c < a.D) *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
-                    if (c + 8 < a.D) *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-                } else {
+                    // w[e] of lane 4 r + l becomes w[l] of lane 4 r + e: bits of l and e are swapped one after the other
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (c + e < a.D) out[c + e] = __ushort_as_bfloat16(static_cast<unsigned short>(w[e / 2] >> (e % 2 * 16)));
+                    for (int step = 1; step < 4; step *= 2) {
+                        const bool up = lane & step;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (e & step) continue;
+                            uint4 &x = w[e], &y = w[e + step];
+                            const uint4 send = up ? x : y;
+                            uint4 got;
+                            got.x = __shfl_xor_sync(0xffffffffu, send.x, step);
+                            got.y = __shfl_xor_sync(0xffffffffu, send.y, step);
+                            got.z = __shfl_xor_sync(0xffffffffu, send.z, step);
+                            got.w = __shfl_xor_sync(0xffffffffu, send.w, step);
+                            if (up) x = got;
+                            else y = got;
+                        }
+                    }
+                    const int d = c + (lane & 3) * 8;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        // row e of the four
+                        const int from = (lane & ~3) + e;
+                        const long long to = __shfl_sync(0xffffffffu, out_at, from);
+                        const bool there = __shfl_sync(0xffffffffu, static_cast<int>(live), from);
+                        if (there && d < a.D) *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(to) + d) = w[e];
+                    }
+                } else if (live) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (c + e < a.D) out[c + e] = __ushort_as_bfloat16(static_cast<unsigned short>(reinterpret_cast<const uint32_t*>(&w[e / 8])[e % 8 / 2] >> (e % 2 * 16)));
                 }
             }
             fence_before();
