@@ -400,25 +400,37 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                     // the keys before the last row's window, and those behind the first row
                     const int pre = a.window > 0 && low1 > start ? (low1 - start < kTile ? low1 - start : kTile) : 0;
                     const int sure = p.t0 + 1 - start < kTile ? p.t0 + 1 - start : kTile, post = sure > pre ? sure : pre;
-                    for (int z = member; z < (pre + kTile - post) * 8 * NP; z += kCleaners) {
-                        const int e = z % (8 * NP), y = z / (8 * NP), row = y < pre ? y : y - pre + post, pos = start + row;
-                        const bool any = pos <= p.p1 && (pos >= p.low || pos < a.sinks);
-                        if (any && pos <= p.t0 && (pos >= low1 || pos < a.sinks)) continue;       // (all see it)
-                        uint4* const to = reinterpret_cast<uint4*>(sm.ring[slot] + e / 8 * Sh::kPanel + row * 128 + e % 8 * 16);
-                        uint4 val = make_uint4(0, 0, 0, 0);
-                        if (any) {
-                            val = *to;
-                            bool here = false;
-                            auto finite = [&](uint32_t& w) {
-                                const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-                                w &= ~(lo | hi);
-                                here |= (lo | hi) != 0;
-                            };
-                            finite(val.x); finite(val.y); finite(val.z); finite(val.w);
-                            odd |= here;
-                            if (!here) continue;
+                    // (four vectors on their way together: one after the other a tile's took 4000 clocks, which its products wait for)
+                    constexpr int kBatch = 4;
+                    const int items = (pre + kTile - post) * 8 * NP;
+                    for (int z0 = member; z0 < items; z0 += kBatch * kCleaners) {
+                        uint4 val[kBatch];
+                        uint4* to[kBatch];
+                        bool any[kBatch], some[kBatch];      // some row sees it; not all do
+#pragma unroll
+                        for (int u = 0; u < kBatch; ++u) {
+                            const int z = z0 + u * kCleaners, e = z % (8 * NP), y = z / (8 * NP), r = y < pre ? y : y - pre + post, pos = start + r;
+                            any[u] = pos <= p.p1 && (pos >= p.low || pos < a.sinks);
+                            some[u] = z < items && !(any[u] && pos <= p.t0 && (pos >= low1 || pos < a.sinks));
+                            to[u] = reinterpret_cast<uint4*>(sm.ring[slot] + e / 8 * Sh::kPanel + r * 128 + e % 8 * 16);
+                            val[u] = make_uint4(0, 0, 0, 0);
+                            if (some[u] && any[u]) val[u] = *to[u];
                         }
-                        *to = val;
+#pragma unroll
+                        for (int u = 0; u < kBatch; ++u) {
+                            // (exponents of ones carry into the sign's place)
+                            auto ones = [](uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };
+                            const bool here = (ones(val[u].x) | ones(val[u].y) | ones(val[u].z) | ones(val[u].w)) != 0;
+                            if (here) {
+                                auto finite = [&](uint32_t& w) {
+                                    const uint32_t x = ones(w);
+                                    w &= ~((x & 0x8000u ? 0xffffu : 0u) | (x & 0x80000000u ? 0xffff0000u : 0u));
+                                };
+                                finite(val[u].x); finite(val[u].y); finite(val[u].z); finite(val[u].w);
+                                odd = true;
+                            }
+                            if (some[u] && (here || !any[u])) *to[u] = val[u];
+                        }
                     }
                     if (odd) sm.fix[round % kUnits][member >> 5] = 1;
                     fence_async();
