@@ -90,7 +90,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         _lib = lib
         if _fast is not None:
             _fast.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in
-                         ("bv_cache_attend", "bv_cache_append", "bv_pages_extend", "bv_pages_truncate", "bv_pages_fork", "bv_pages_compact", "bv_pages_copy")))
+                         ("bv_cache_attend", "bv_cache_append", "bv_pages_extend", "bv_pages_truncate", "bv_pages_fork", "bv_pages_compact", "bv_pages_copy",
+                          "bv_cache_append_rotary", "bv_prompt_attend", "bv_sample_filtered")))
     return lib
 
 
@@ -749,6 +750,10 @@ def bv_cache_append_rotary(q, k_new, v_new, k, v, table, lens, freq, n_new=None,
     here if None (rows that no sequence brings: zero in it); ``out_k`` (may be ``k_new``), if given, the keys.  Returns ``out_q``.  Autograd does not see it."""
     if stream is not None:
         return _on_stream(stream, lens, bv_cache_append_rotary, q, k_new, v_new, k, v, table, lens, freq, n_new, offsets, interleaved, mscale, out_q, out_k)
+    if _fast is not None:
+        r = _fast.rotary(q, k_new, v_new, k, v, table, lens, freq, n_new, offsets, interleaved, mscale, out_q, out_k)
+        if r is not NotImplemented:
+            return r if r.__class__ is not int else _check(r)
     blob, B, heads, D, dtype, dev = _cache(k, v, table, lens)
     if freq.dtype is not torch.float64 or freq.dim() != 1 or not freq.is_contiguous() or freq.get_device() != dev or freq.shape[0] < 1:
         raise ValueError("freq must be a contiguous float64 tensor [rot / 2] on the cache's device")
@@ -806,6 +811,10 @@ def bv_prompt_attend(q, k, v, offsets, scale: Optional[float] = None, window: in
     no autograd graph."""
     if stream is not None:
         return _on_stream(stream, offsets, bv_prompt_attend, q, k, v, offsets, scale, window, sinks, out)
+    if _fast is not None:
+        r = _fast.prompt(q, k, v, offsets, scale, window, sinks, out)
+        if r is not NotImplemented:
+            return r if r.__class__ is not int else _check(r)
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q must be [tokens, q_heads, D], k and v [tokens, heads, D]")
     D, dtype, dev = k.shape[2], k.dtype, k.get_device()
@@ -886,6 +895,10 @@ def bv_sample_filtered(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, mi
     tokens; ``out_logits`` (may be ``logits``), if given, takes the rows with all other logits at -inf."""
     if stream is not None:
         return _on_stream(stream, logits, bv_sample_filtered, logits, uniforms, temperature, top_k, top_p, min_p, want_lse, out_logits)
+    if _fast is not None:
+        r = _fast.sample(logits, uniforms, temperature, top_k, top_p, min_p, want_lse, out_logits)
+        if r is not NotImplemented and uniforms is not None:
+            return r if r.__class__ is not int else _check(r)
     rows, _ = _logits(logits, "logits")
     if uniforms.shape != (rows,) or uniforms.dtype is not torch.float32 or not uniforms.is_contiguous() or uniforms.get_device() != logits.get_device():
         raise ValueError("uniforms must be a contiguous float32 tensor [rows] on the logits' device")
@@ -901,5 +914,9 @@ def bv_filter_logits(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out
         return _on_stream(stream, logits, bv_filter_logits, logits, temperature, top_k, top_p, min_p, out)
     if out is None:
         out = torch.empty(tuple(logits.shape), dtype=logits.dtype, device=logits.device)
+    if _fast is not None:
+        r = _fast.sample(logits, None, temperature, top_k, top_p, min_p, False, out)
+        if r is not NotImplemented:
+            return r if r.__class__ is not int else _check(r)
     _cut_call(logits, None, None, None, out, temperature, top_k, top_p, min_p)
     return out

@@ -1,18 +1,20 @@
 """The outer loop of speculative decoding (Algorithm 3) for models that attend to their context, on the library's paged
 key-value cache.
 
-    python -m paper_2403_10444_b200.specdec --context 512 [--V 32768] [--B 64] [--gammas 2,4,8] [--iterations 32] [--window 0 --sinks 0]
+    python -m paper_2403_10444_b200.specdec --context 512 [--V 32768] [--B 64] [--gammas 2,4,8] [--iterations 32] [--window 0 --sinks 0] [--rotary 10000]
+        [--packed] [--top-k 50 --top-p 0.9 --min-p 0.05]
 
 Two synthetic decoders (``workloads.attention_models``: token embedding, causal attention layers, unembedding; no weights of any
 real model) take the place of the two tables of ``specdec.run``.  Each keeps its keys and values in a cache of its own.  An iteration
 extends both caches by gamma + 1 tokens (``bv_pages_extend``), drafts gamma tokens one at a time, scores the block with one pass of the target over its
 gamma + 1 tokens (``bv_cache_append``, ``bv_cache_attend`` in every layer), verifies it, and takes what was not accepted out of
-both caches (``bv_pages_truncate`` with the verification's out_len).  Projections are torch products; attention, bookkeeping,
-sampling and verification run in the CUDA library.
+both caches (``bv_pages_truncate`` with the verification's out_len).  Prompts may go in packed (``Decoder.prefill``: ``bv_cache_append_rotary``,
+``bv_prompt_attend``), heads may be turned by their positions (``Rotary``) and both models' distributions cut (``Cut``: ``bv_sample_filtered``,
+``bv_filter_logits``).  Projections are torch products; attention, rotation, bookkeeping, sampling and verification run in the CUDA library.
 """
 from __future__ import annotations
 
-from typing import Dict, List
+from typing import Dict, List, NamedTuple, Optional
 
 import torch
 
@@ -55,11 +57,26 @@ class PagedCache:
             bv.bv_pages_copy(k, v, moves, count)
 
 
-class Decoder:
-    """A decoder (workloads.attention_models) and its cache.  ``window`` and ``sinks`` as in bv_cache_attend."""
+class Rotary(NamedTuple):
+    """Rotary positions of a decoder's queries and keys, as in bv_cache_append_rotary (``freq``: ``rotary_frequencies``)."""
+    freq: torch.Tensor
+    interleaved: bool = False
+    mscale: float = 1.0
 
-    def __init__(self, weights, B: int, capacity: int, page_size: int = 16, window: int = 0, sinks: int = 0):
-        self.w, self.window, self.sinks = weights, window, sinks
+
+class Cut(NamedTuple):
+    """What a sampler keeps of a distribution, as in bv_sample_filtered: numbers, the same for both models."""
+    top_k: int = 0
+    top_p: float = 1.0
+    min_p: float = 0.0
+
+
+class Decoder:
+    """A decoder (workloads.attention_models) and its cache.  ``window`` and ``sinks`` as in bv_cache_attend; ``rotary``: queries and keys are turned by their
+    positions."""
+
+    def __init__(self, weights, B: int, capacity: int, page_size: int = 16, window: int = 0, sinks: int = 0, rotary: Optional[Rotary] = None):
+        self.w, self.window, self.sinks, self.rotary = weights, window, sinks, rotary
         self.heads, self.kv_heads, self.D = weights["heads"], weights["kv_heads"], weights["head_dim"]
         e = weights["embed"]
         self.cache = PagedCache(len(weights["layers"]), B, capacity, self.kv_heads, self.D, page_size, e.dtype, e.device)
@@ -72,19 +89,42 @@ class Decoder:
         for layer, k, v in zip(self.w["layers"], c.k, c.v):
             qkv = (x @ layer["qkv"]).view(B, n, self.heads + 2 * self.kv_heads, self.D)
             q, kn, vn = qkv.split([self.heads, self.kv_heads, self.kv_heads], dim=2)
-            bv.bv_cache_append(kn, vn, k, v, c.table, lens, n_new=n_new)
+            if self.rotary is None:
+                bv.bv_cache_append(kn, vn, k, v, c.table, lens, n_new=n_new)
+            else:
+                r = self.rotary
+                q = bv.bv_cache_append_rotary(q, kn, vn, k, v, c.table, lens, r.freq, n_new=n_new, interleaved=r.interleaved, mscale=r.mscale)
             o = bv.bv_cache_attend(q, k, v, c.table, lens, n_new=n_new, window=self.window, sinks=self.sinks)
             x = x + o.reshape(B, n, self.heads * self.D) @ layer["out"]
         return x @ self.w["unembed"]
 
+    def prefill(self, tokens: torch.Tensor, offsets: torch.Tensor) -> torch.Tensor:
+        """Takes whole prompts that lie one after the other (tokens [T] of sequences that were empty, sequence b from offsets[b] on; the cache has room for
+        them and counts them in) through the layers: their keys and values go into the cache, their attention needs no cache.  What the last
+        layer leaves of each token [T, width]; ``@ w["unembed"]`` makes logits of it."""
+        c, T = self.cache, tokens.shape[0]
+        # (without rotary positions: pairs that turn by nothing)
+        r = self.rotary or Rotary(torch.zeros((1,), dtype=torch.float64, device=tokens.device))
+        x = self.w["embed"][tokens]
+        for layer, k, v in zip(self.w["layers"], c.k, c.v):
+            qkv = (x @ layer["qkv"]).view(T, self.heads + 2 * self.kv_heads, self.D)
+            q, kn, vn = qkv.split([self.heads, self.kv_heads, self.kv_heads], dim=1)
+            bv.bv_cache_append_rotary(q, kn, vn, k, v, c.table, c.lens, r.freq, offsets=offsets, interleaved=r.interleaved, mscale=r.mscale, out_q=q, out_k=kn)
+            o = bv.bv_prompt_attend(q, kn, vn, offsets, window=self.window, sinks=self.sinks)
+            x = x + o.reshape(T, self.heads * self.D) @ layer["out"]
+        return x
+
 
 def run(target: Decoder, draft: Decoder, prompts: torch.Tensor, prompt_lens: torch.Tensor, u_draft: torch.Tensor, u_verify: torch.Tensor,
-        gamma: int, temperature: float = 1.0, algo: str = "block_lse", graph: bool = False) -> Dict[str, torch.Tensor]:
+        gamma: int, temperature: float = 1.0, algo: str = "block_lse", graph: bool = False, packed: bool = False,
+        cut: Optional[Cut] = None) -> Dict[str, torch.Tensor]:
     """Run ``u_draft.shape[0]`` iterations of Algorithm 3 on two decoders with empty caches.
 
     prompts int32 [B, L] (CUDA), of which sequence b has prompt_lens[b] in 1 .. L (what lies beyond is not looked at); u_draft [N, gamma, B] and u_verify [N, B, gamma+2]: float32
     uniforms; algo as in ``specdec.run``.  Returns ``tokens`` int32 [B, N (gamma+1)] (generated tokens, then -1), ``lengths`` int64 [B], ``tau`` int32
     [N, B] and ``drafted`` int32 [N, B, gamma].  With ``graph`` the iterations after the first are replays of one captured one.
+    ``packed``: the prompts go through the layers one after the other instead of padded to the longest (``Decoder.prefill``).  ``cut``: both models' distributions
+    are cut before anything is drawn from them, so what is generated follows the target's cut distributions.
     """
     from .specdec import ALGOS
     if algo not in ALGOS:
@@ -108,7 +148,12 @@ def run(target: Decoder, draft: Decoder, prompts: torch.Tensor, prompt_lens: tor
         for m in (target, draft):
             new = m.cache.extend(prompts.shape[1] - 1, prompt_lens - 1)
             fault.add_((new < 0).any())
-            m.forward(prompts[:, :-1], m.cache.lens, new)
+            if not packed:
+                m.forward(prompts[:, :-1], m.cache.lens, new)
+                continue
+            offsets = torch.zeros((B + 1,), dtype=torch.int32, device=dev)
+            offsets[1:] = (prompt_lens - 1).cumsum(0)
+            m.prefill(prompts[:, :-1][held[:, 1:]], offsets)
     seq = torch.full((B, width + 1), -1, dtype=torch.int32, device=dev)
     pos = torch.zeros((B,), dtype=torch.int64, device=dev)
     taus = torch.empty((N, B), dtype=torch.int32, device=dev)
@@ -132,11 +177,17 @@ def run(target: Decoder, draft: Decoder, prompts: torch.Tensor, prompt_lens: tor
         for i in range(gamma + 1):
             logits = draft.forward(block[:, i:i + 1], at[i])[:, 0]
             if i < gamma:
-                draft_logits[:, i] = logits
-                tok, row_lse = bv.bv_sample_draft(logits.contiguous(), ud[i], temperature)
+                if cut is None:
+                    draft_logits[:, i] = logits
+                    tok, row_lse = bv.bv_sample_draft(logits.contiguous(), ud[i], temperature)
+                else:
+                    tok, row_lse = bv.bv_sample_filtered(logits, ud[i], temperature, *cut, out_logits=draft_logits[:, i])
                 block[:, i + 1] = tok
                 lse[:, i] = row_lse
         target_logits = target.forward(block, target.cache.lens).contiguous()
+        if cut is not None:
+            rows = target_logits.view(-1, V)
+            bv.bv_filter_logits(rows, temperature, *cut, out=rows)
         toks = block[:, 1:].contiguous()
         given = (lse,) if algo.endswith("lse") else ()
         out, out_len = verify(target_logits, draft_logits, toks, uv.contiguous(), *given, temperature)

@@ -171,18 +171,22 @@ def context_main(args):
     gen = torch.Generator(device="cuda").manual_seed(args.seed)
     prompts = torch.randint(args.V, (args.B, args.context), dtype=torch.int32, device="cuda", generator=gen)
     lens = torch.randint(max(1, args.context // 4), args.context + 1, (args.B,), dtype=torch.int32, device="cuda", generator=gen)
+    rotary = cached.Rotary(bv.rotary_frequencies(tw["head_dim"], args.rotary)) if args.rotary > 0 else None
+    cut = cached.Cut(args.top_k, args.top_p or 1.0, args.min_p)
+    cut = cut if cut != cached.Cut() else None
     for gamma in [int(x) for x in args.gammas.split(",")]:
         ud, uv = wl.loop_uniforms(args.iterations, args.B, gamma, args.seed + gamma, "cuda")
         for algo in ALGOS:
             spent = []
             for n in (2, args.iterations):                                                                           # warm-up, then all
-                models = [cached.Decoder(w, args.B, args.context + n * (gamma + 1), window=args.window, sinks=args.sinks) for w in (tw, dw)]
+                models = [cached.Decoder(w, args.B, args.context + n * (gamma + 1), window=args.window, sinks=args.sinks, rotary=rotary) for w in (tw, dw)]
                 torch.cuda.synchronize()
                 t0 = time.perf_counter()
-                res = cached.run(*models, prompts, lens, ud[:n], uv[:n], gamma, args.temperature, algo, args.graph)
+                res = cached.run(*models, prompts, lens, ud[:n], uv[:n], gamma, args.temperature, algo, args.graph, args.packed, cut)
                 torch.cuda.synchronize()
                 spent.append(time.perf_counter() - t0)
-            print(json.dumps({"V": args.V, "B": args.B, "gamma": gamma, "algo": algo, "context": args.context, "window": args.window or None,
+            print(json.dumps({"V": args.V, "B": args.B, "gamma": gamma, "algo": algo, "context": args.context, "window": args.window or None, "rotary": args.rotary or None,
+                              "packed": args.packed, "cut": cut and cut._asdict(),
                               "iterations": args.iterations, "temperature": args.temperature, "graph": args.graph,
                               "block_efficiency": round(block_efficiency(res), 4), "tokens": int(res["lengths"].sum().item()),
                               "ms_per_iteration": round(spent[1] / args.iterations * 1e3, 3),
@@ -198,12 +202,16 @@ def main():
     ap.add_argument("--draft-sigma", type=float, default=1.0)
     ap.add_argument("--temperature", type=float, default=1.0)
     ap.add_argument("--seed", type=int, default=7)
-    ap.add_argument("--top-p", type=float, default=0.0, help="mask both models' rows to their top-p nucleus")
+    ap.add_argument("--top-p", type=float, default=0.0, help="cut both models' rows to their top-p nucleus")
     ap.add_argument("--graph", action="store_true", help="replay one captured iteration as a CUDA graph")
     ap.add_argument("--no-chain", action="store_true", help="draft with gamma sampler calls instead of one chain launch")
     ap.add_argument("--context", type=int, default=0, help="models that attend to prompts of up to this many tokens (and what follows) on a paged cache")
     ap.add_argument("--window", type=int, default=0, help="with --context: how many positions a token sees (0: all)")
     ap.add_argument("--sinks", type=int, default=0, help="with --window: first positions that stay visible")
+    ap.add_argument("--rotary", type=float, default=0.0, help="with --context: base of rotary positions (0: none)")
+    ap.add_argument("--packed", action="store_true", help="with --context: prompts one after the other instead of padded to the longest")
+    ap.add_argument("--top-k", type=int, default=0, help="with --context: both models keep their top_k likeliest tokens (with --top-p: of those the nucleus)")
+    ap.add_argument("--min-p", type=float, default=0.0, help="with --context: and of these what is at least min_p times as likely as the first")
     args = ap.parse_args()
     bv.load_library()
     if args.context > 0:
