@@ -77,7 +77,7 @@ struct __align__(1024) PromptSmem {
     using Sh = PromptShape<NP>;
     char q[2][Sh::kSlot];
     char ring[Sh::kSlots][Sh::kSlot];
-    unsigned long long q_full[2], q_empty[2], full[8], empty[8], unclean[8], s_full[2], p_part[2], p_full[2], o_done[2], drain;
+    unsigned long long q_full[2], q_empty[2], full[8], empty[8], unclean[8], s_full[2], s_read[2], p_part[2], p_full[2], o_done[2], drain;
     uint32_t tmem;
     int abort;
     int fix[kUnits][2];                    // by unit, by cleaning warp: values that are not finite among those that some rows see
@@ -194,6 +194,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sm.q_full[i]), 1);
             mbar_init(smem_u32(&sm.s_full[i]), 1);
+            mbar_init(smem_u32(&sm.s_read[i]), kTile);
             mbar_init(smem_u32(&sm.p_part[i]), kTile);
             mbar_init(smem_u32(&sm.p_full[i]), kTile);
             mbar_init(smem_u32(&sm.q_empty[i]), 1);
@@ -251,7 +252,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
     }
     fence_after();
     const uint32_t tmem = sm.tmem;
-    constexpr uint32_t kS = 0, kO = 256;               // columns: S of both tiles, O of both
+    // Columns of tensor memory: S of both tiles, O of both, P of both, which has a place of its own where O is 64 columns wide (kOwn): there the next scores
+    // can be formed as soon as the last ones have been read, and nobody waits for them (windows of 1024, D = 64: 434 -> @@ us).
+    constexpr bool kOwn = NP == 1;
+    constexpr uint32_t kS = 0, kO = 256, kOStep = NP * 64, kP = kOwn ? kO + 2 * kOStep : kS, kPStep = kOwn ? 64 : kTile;
     Pair p;
 
     if (warp >= kSoftWarps) {
@@ -342,35 +346,46 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                     commit(smem_u32(&sm.empty[x % kSlots]));
                     for (int i = 0; i < tiles && ok; ++i) {
                         const int v_at = x + 2 * i + 1, v_slot = v_at % kSlots, k_at = v_at + 1;
-                        wait(sm.full[v_slot], v_at / kSlots);
                         bool next_in = false;
+                        auto next = [&](int t) {       // the scores of tile i + 1
+                            if (i + 1 >= p.tiles[t]) return;
+                            if (!next_in) wait(sm.full[k_at % kSlots], k_at / kSlots);
+                            next_in = true;
+                            if (kOwn) wait(sm.s_read[t], done[t]);
+                            if (!ok) return;
+                            fence_after();
+                            scores(t, i + 1);
+                        };
+                        if constexpr (kOwn) {
+                            for (int t = 0; t < 2; ++t) next(t);
+                            if (!ok) break;
+                            if (i + 1 < tiles) commit(smem_u32(&sm.empty[k_at % kSlots]));
+                        }
+                        wait(sm.full[v_slot], v_at / kSlots);
                         for (int t = 0; t < 2 && ok; ++t) {
                             if (i >= p.tiles[t]) continue;
+                            const uint32_t v_low = desc_low(ring + v_slot * Sh::kSlot, Sh::kPanel);
+                            auto products = [&](int from, int to) {
+                                fence_after();
+#pragma unroll
+                                for (int s = 0; s < kTile / 16; ++s)
+                                    if (s >= from && s < to)
+                                        mma_ts(tmem + kO + t * kOStep, tmem + kP + t * kPStep + s * 8, desc(v_low + s * 128, desc_high(1024, 2)), pv, i > 0 || s > 0);
+                            };
                             wait(sm.p_part[t], done[t]);
                             if (!ok) break;
-                            fence_after();
-                            const uint32_t v_low = desc_low(ring + v_slot * Sh::kSlot, Sh::kPanel);
-#pragma unroll
-                            for (int s = 0; s < kFirstKeys / 16; ++s)
-                                mma_ts(tmem + kO + t * kTile, tmem + kS + t * kTile + s * 8, desc(v_low + s * 128, desc_high(1024, 2)), pv, i > 0 || s > 0);
-                            wait(sm.p_full[t], done[t]++);
+                            products(0, kFirstKeys / 16);
+                            wait(sm.p_full[t], done[t]);
                             if (!ok) break;
-                            fence_after();
-#pragma unroll
-                            for (int s = kFirstKeys / 16; s < kTile / 16; ++s)
-                                mma_ts(tmem + kO + t * kTile, tmem + kS + t * kTile + s * 8, desc(v_low + s * 128, desc_high(1024, 2)), pv, i > 0 || s > 0);
+                            products(kFirstKeys / 16, kTile / 16);
                             commit(smem_u32(&sm.o_done[t]));
-                            if (i + 1 < p.tiles[t]) {
-                                if (!next_in) wait(sm.full[k_at % kSlots], k_at / kSlots);
-                                next_in = true;
-                                if (!ok) break;
-                                fence_after();
-                                scores(t, i + 1);
-                            }
+                            if (!kOwn) next(t);
+                            if (kOwn && i + 1 == p.tiles[t]) wait(sm.s_read[t], done[t]);      // (every phase is waited for)
+                            ++done[t];
                         }
                         if (!ok) break;
                         commit(smem_u32(&sm.empty[v_slot]));
-                        if (i + 1 < tiles) commit(smem_u32(&sm.empty[k_at % kSlots]));
+                        if (!kOwn && i + 1 < tiles) commit(smem_u32(&sm.empty[k_at % kSlots]));
                     }
                     x += 2 * tiles;
                 }
@@ -444,7 +459,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // ---- weights: a thread has a row ----
         const int t = warp >> 2, row = tid & (kTile - 1);
-        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16, s_at = tmem + lanes + kS + t * kTile, o_at = tmem + lanes + kO + t * kTile;
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16, s_at = tmem + lanes + kS + t * kTile, o_at = tmem + lanes + kO + t * kOStep, p_at = tmem + lanes + kP + t * kPStep;
         const int rows = tokens_each * a.group, token = a.by_group(row), head = row - token * a.group;
         const int wide = (a.D + 15) / 16 * 16;
         int done = 0;
@@ -467,6 +482,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                 for (int c = 0; c < kTile; c += 32) ld32(s_at + c, s + c);
 #pragma unroll
                 for (int c = 0; c < kTile; c += 8) wait_ld8(s + c);
+                if (kOwn) {
+                    fence_before();
+                    mbar_arrive(smem_u32(&sm.s_read[t]));
+                }
                 if (!whole_tile(a, p0, last, j)) {
                     // seen: c <= hi and (c >= lo or c < sinks); a bit a key
                     const int hi = pos - start, lo = low - start, sinks = a.sinks - start;
@@ -520,6 +539,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
 #pragma unroll
                     for (int c = 0; c < kTile; c += 2) unpair2(fma2(pair2(s[c], s[c + 1]), kf2, ref2), s[c], s[c + 1]);
                 }
+                // (the last weights have been multiplied: theirs is the place of these)
+                if (kOwn && done > 0) {
+                    ok = __all_sync(0xffffffffu, wait_on<NP>(sm, sm.o_done[t], done - 1, a.status, limit));
+                    if (!ok) break;
+                    fence_after();
+                }
                 uint32_t w[kTile / 2];
                 unsigned long long sum[2] = {0, 0};
 #pragma unroll
@@ -529,15 +554,15 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                     w[c / 2] = *reinterpret_cast<const uint32_t*>(&h);
                     // (the sum is of the rounded weights: error of a row 0.0022 against 0.0023 with the others; a row of one key is its value)
                     sum[c / 2 & 1] = add2(sum[c / 2 & 1], pair2(__uint_as_float(w[c / 2] << 16), __uint_as_float(w[c / 2] & 0xffff0000u)));
-                    if (c == 62) st32(s_at, w);
+                    if (c == 62) st32(p_at, w);
                     if (c == kFirstKeys - 2) {
-                        st16(s_at + 32, w + 32);
+                        st16(p_at + 32, w + 32);
                         wait_st();
                         fence_before();
                         mbar_arrive(smem_u32(&sm.p_part[t]));
                     }
                 }
-                st16(s_at + 48, w + 48);
+                st16(p_at + 48, w + 48);
                 float x, y;
                 unpair2(add2(sum[0], sum[1]), x, y);
                 l += x + y;
