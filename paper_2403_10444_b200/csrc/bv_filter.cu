@@ -630,6 +630,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         border.last = last_tie(key, some);
     };
 
+    int listed_kept = 0;                                 // (the first CTA's: with how many kept tokens its list begins)
     // In the first CTA: the token, of the `kept` ones in its list.
     auto draw = [&](int kept) {
         // the kept ones in the order of the vocabulary: the same entries, turned round, their keys behind
@@ -672,6 +673,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             kept = static_cast<int>(sm.found);
         }
         announce(entry(kept - 1));
+        listed_kept = kept;
         if (a.uniforms) draw(kept);
     };
     // In the first CTA, which has a row's first n tokens in its list: what is kept of them, and the token.  target: the mass before which top-p keeps
@@ -1163,7 +1165,34 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
     }
 
     // ---- the row ----
-    if (a.out) {
+    // Where a CTA has the whole row and a list of what is kept, the row is not read again: all of it becomes -inf, the kept ones are put back.
+    const bool place = !RES && C == 1 && drew && a.vec_out;
+    if (a.out && place) {
+        char* const out = a.out + row * a.out_stride;
+        constexpr int kMine = kList / kFThreads;
+        const int n = listed_kept;
+        int at[kMine];
+        E value[kMine];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int x = tid + i * kFThreads;
+            if (x >= n) break;
+            at[i] = static_cast<int>(0xffffffffu - static_cast<uint32_t>(a.uniforms ? sm.list[x] >> 32 : sm.list[x]));
+            value[i] = reinterpret_cast<const E*>(in)[at[i]];      // (before it is written: the row may be replaced where it lies)
+        }
+        __syncthreads();
+        const uint4 none = make_uint4(R::kNegInf, R::kNegInf, R::kNegInf, R::kNegInf);
+        const int whole = a.V / N;
+        for (int x = tid; x < whole; x += kFThreads) reinterpret_cast<uint4*>(out)[x] = none;
+        for (int x = whole * N + tid; x < a.V; x += kFThreads) reinterpret_cast<E*>(out)[x] = static_cast<E>(R::kNegInf >> (32 - 8 * sizeof(E)));
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            if (tid + i * kFThreads >= n) break;
+            reinterpret_cast<E*>(out)[at[i]] = value[i];
+        }
+    } else if (a.out) {
         char* const out = a.out + row * a.out_stride;
         each([&](const uint4& v, int i) {
             uint4 w = v;
