@@ -71,6 +71,7 @@ template <> struct Row<kF32> {
     using E = uint32_t;
     static constexpr int kN = 4;
     static constexpr uint32_t kNegInf = 0xff800000u, kNaN = 0x7fc00000u;
+    static constexpr float kLeast = -3.40282347e38f;
     // The largest of a vector's, NaN if one is.
     static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
         float r;
@@ -79,11 +80,18 @@ template <> struct Row<kF32> {
     }
     static __device__ __forceinline__ float top(const uint4& v) { return __uint_as_float(larger(larger(v.x, v.y), larger(v.z, v.w))); }
     static __device__ __forceinline__ float get(const uint4& v, int i) { return __uint_as_float(reinterpret_cast<const uint32_t*>(&v)[i]); }
+    // Which elements are not below z (at_least: of the type, rounded down), a bit each: element i is bit(i).
+    static constexpr __device__ __forceinline__ int bit(int i) { return i; }
+    static __device__ __forceinline__ float at_least(float z) { return z; }
+    static __device__ __forceinline__ unsigned from(const uint4& v, float z) {
+        return static_cast<unsigned>(get(v, 0) >= z) | static_cast<unsigned>(get(v, 1) >= z) << 1 | static_cast<unsigned>(get(v, 2) >= z) << 2 | static_cast<unsigned>(get(v, 3) >= z) << 3;
+    }
 };
 template <> struct Row<kBF16> {
     using E = uint16_t;
     static constexpr int kN = 8;
     static constexpr uint32_t kNegInf = 0xff80ff80u, kNaN = 0x7fc07fc0u;
+    static constexpr float kLeast = -3.38953139e38f;
     static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
         uint32_t r;
         asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -96,6 +104,13 @@ template <> struct Row<kBF16> {
     static __device__ __forceinline__ float get(const uint4& v, int i) {
         const uint32_t w = reinterpret_cast<const uint32_t*>(&v)[i / 2];
         return __uint_as_float(i % 2 ? w & 0xffff0000u : w << 16);
+    }
+    static constexpr __device__ __forceinline__ int bit(int i) { return i / 2 + i % 2 * 16; }
+    static __device__ __forceinline__ float at_least(float z) { return __bfloat162float(__float2bfloat16_rd(z)); }
+    static __device__ __forceinline__ unsigned from(const uint4& v, float z) {
+        const __nv_bfloat162 b = __float2bfloat162_rn(z);
+        auto pair = [&](uint32_t w) { return __hge2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w), b); };
+        return (pair(v.x) & 0x00010001u) | (pair(v.y) & 0x00020002u) | (pair(v.z) & 0x00040004u) | (pair(v.w) & 0x00080008u);
     }
 };
 
@@ -120,6 +135,7 @@ constexpr float kPerNat = 64.f;          // bins of top-p's to a factor e of the
 static_assert(kBins == 4 * kFThreads, "");
 constexpr int kList = 4096;              // tokens that are put in order one by one
 constexpr int kShort = kList / 2;        // of a list that leaves room for buckets behind it
+constexpr int kWide = 8192;              // bins by the upper 13 bits of keys: 16 to a power of two
 constexpr int kMostK = 1024;             // of a top-k by candidates
 constexpr int kFew = 2048;               // tokens of which all are candidates
 
@@ -142,6 +158,7 @@ struct FilterSmem {
             unsigned long long mass[kDigits];
         };
         unsigned long long list[kList];  // key, then the index turned round: in order when they descend
+        unsigned wide[kWide];
     };
     double roots[kRoots];
     double warp_mass[kFWarps], warp_above[kFWarps];      // read by the other CTAs, as are the next four
@@ -304,7 +321,10 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
     if (p == 0.f) k = 1;                               // (the first one always)
     // (few from each CTA are found faster than all values are counted: k = 50 of 32000, 14.5 us against 18)
     const bool counting = DT == kBF16 && (k < a.V || (p < 1.f && p > 0.f)) && !(k < a.V && C * k <= kMostK && a.V > kFew);
-    for (int x = tid; x < kBins; x += kFThreads) sm.bins[x] = 0;
+    // Each CTA's own k-th where those of all together are few: no histogram of all to wait for, and the vectors' maxima are counted while the row is read.
+    const bool own = k < a.V && k <= kMostK && (C == 1 || C * k <= kMostK) && a.V > kFew;
+    for (int x = tid; x < (own ? kWide : kBins); x += kFThreads) sm.wide[x] = 0;
+    if (own) __syncthreads();
     if (tid == 0) sm.listed = 0;
     if (tid < kRoots) sm.roots[tid] = exp2(static_cast<double>(tid) / kRoots);
     float top = -INFINITY;
@@ -324,6 +344,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
                 const float z = R::top(v[j]);
                 bad |= !(z < INFINITY);
                 top = fmaxf(top, z);
+                if (own) atomicAdd(&sm.wide[kWide - 1 - (key_of<DT>(z) >> 19)], 1u);
             }
         }
         // (threads without an element that is finite have no part in the least)
@@ -387,7 +408,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             unsigned at = atomicAdd(&sm.listed, static_cast<unsigned>(__popc(w)));
 #pragma unroll
             for (int x = 0; x < N; ++x)
-                if (w >> x & 1) {
+                if (w >> R::bit(x) & 1) {
                     if (at < kList) sm.list[at] = static_cast<unsigned long long>(key_of<DT>(R::get(v, x))) << 32 | (0xffffffffu - static_cast<unsigned>(i + x));
                     ++at;
                 }
@@ -687,60 +708,62 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
     auto by_candidates = [&]() {
         if (a.V > kFew) {
             float limit;
-            // Each CTA's own k-th where those of all together are few (k = 50 of 8 CTAs: no histogram of all to wait for), else the row's.
-            const bool own = C == 1 || C * k <= kMostK;
-            float step = (kBins - 1) / (top - (own ? sm.cta_low : low));
-            const bool spread = step > 0.f && step < INFINITY;
-            if (!spread && !own) return false;
-            if (!spread) step = 0.f;
-            each([&](const uint4& v, int) {
-                const float d = (top - R::top(v)) * step;
-                if (d < kBins) atomicAdd(&sm.bins[static_cast<int>(d)], 1u);
-            });
-            unsigned c[4], sum = 0;
             if (own) {
+                constexpr int kEach = kWide / kFThreads;
+                const uint4* const c = reinterpret_cast<const uint4*>(sm.wide) + tid * (kEach / 4);
+                unsigned sum = 0;
+                for (int x = 0; x < kEach / 4; ++x) { const uint4 u = c[x]; sum += u.x + u.y + u.z + u.w; }
+                const unsigned inc = scanned(sum, lane);
+                if (lane == 31) sm.scan_count[warp] = inc;
+                if (tid == 0) sm.found = kWide;
                 __syncthreads();
-#pragma unroll
-                for (int x = 0; x < 4; ++x) c[x] = sm.bins[4 * tid + x];
+                unsigned upto = inc - sum;
+                for (int w = 0; w < warp; ++w) upto += sm.scan_count[w];
+                if (upto < static_cast<unsigned>(k) && upto + sum >= static_cast<unsigned>(k)) {
+                    int x = tid * kEach;
+                    while ((upto += sm.wide[x]) < static_cast<unsigned>(k)) ++x;
+                    sm.found = x;
+                }
+                __syncthreads();                         // (the bins have been read)
+                // the lowest value of that bin (a CTA with fewer than k vectors takes all of its own)
+                const int bin = static_cast<int>(sm.found);
+                limit = bin < kWide ? value_of<kF32>(static_cast<uint32_t>(kWide - 1 - bin) << 19) : -INFINITY;
             } else {
+                const float step = (kBins - 1) / (top - low);
+                if (!(step > 0.f && step < INFINITY)) return false;
+                each([&](const uint4& v, int) {
+                    const float d = (top - R::top(v)) * step;
+                    if (d < kBins) atomicAdd(&sm.bins[static_cast<int>(d)], 1u);
+                });
                 cluster.sync();
+                unsigned c[4], sum = 0;
                 gather(c);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) sum += c[x];
+                const unsigned inc = scanned(sum, lane);
+                if (lane == 31) sm.scan_count[warp] = inc;
+                if (tid == 0) sm.found = kBins;
+                __syncthreads();
+                unsigned upto = inc - sum;
+                for (int w = 0; w < warp; ++w) upto += sm.scan_count[w];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    if (upto < static_cast<unsigned>(k) && upto + c[x] >= static_cast<unsigned>(k)) sm.found = 4 * tid + x;
+                    upto += c[x];
+                }
+                cluster.sync();                          // (the bins have been read)
+                const int bin = static_cast<int>(sm.found);
+                if (bin >= kBins) return false;
+                // every vector of the bins up to this one has a maximum that is not below this (a hair lower, for the roundings)
+                limit = top - (bin + 1) / step * 1.000001f - fabsf(top) * 1e-6f;
             }
-#pragma unroll
-            for (int x = 0; x < 4; ++x) sum += c[x];
-            const unsigned inc = scanned(sum, lane);
-            if (lane == 31) sm.scan_count[warp] = inc;
-            if (tid == 0) sm.found = kBins;
-            __syncthreads();
-            unsigned upto = inc - sum;
-            for (int w = 0; w < warp; ++w) upto += sm.scan_count[w];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                if (upto < static_cast<unsigned>(k) && upto + c[x] >= static_cast<unsigned>(k)) sm.found = 4 * tid + x;
-                upto += c[x];
-            }
-            // (the bins have been read)
-            if (own) __syncthreads();
-            else cluster.sync();
-            const int bin = static_cast<int>(sm.found);
-            if (bin >= kBins && !own) return false;
-            // every vector of the bins up to this one has a maximum that is not below this (a hair lower, for the roundings; a CTA with fewer than k
-            // takes all of its own)
-            const float width = (bin + 1) / step;
-            limit = bin < kBins && spread ? top - width * 1.000001f - fabsf(top) * 1e-6f : -3.4e38f;
-            if (!(limit > -3.4e38f)) limit = -3.4e38f;
-            enlist([&](const uint4& v, int) {
-                unsigned which = 0;
-                if (R::top(v) < limit) return which;
-#pragma unroll
-                for (int x = 0; x < N; ++x) which |= static_cast<unsigned>(R::get(v, x) >= limit) << x;
-                return which;
-            });
+            limit = R::at_least(limit > R::kLeast ? limit : R::kLeast);      // (-inf is nobody's candidate)
+            enlist([&](const uint4& v, int) { return R::from(v, limit); });
         } else {
             enlist([&](const uint4& v, int) {
                 unsigned which = 0;
 #pragma unroll
-                for (int x = 0; x < N; ++x) which |= static_cast<unsigned>(R::get(v, x) > -INFINITY) << x;
+                for (int x = 0; x < N; ++x) which |= static_cast<unsigned>(R::get(v, x) > -INFINITY) << R::bit(x);
                 return which;
             });
         }
@@ -839,7 +862,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             for (int x = 0; x < N; ++x) {
                 const float z = R::get(v, x);
                 const int b = bin_of(z);
-                which |= static_cast<unsigned>(b >= from && b <= b1 && counts(z, i + x)) << x;
+                which |= static_cast<unsigned>(b >= from && b <= b1 && counts(z, i + x)) << R::bit(x);
             }
             return which;
         });
@@ -1010,7 +1033,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
     };
 
     if (!bad) {
-        bool dirty = false;                              // (something lies where the bins are)
+        bool dirty = own;                                // (something lies where the bins are)
         auto clean = [&]() {
             if (!dirty) return;
             for (int x = tid; x < kBins; x += kFThreads) sm.bins[x] = 0;
@@ -1028,7 +1051,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         if (known < 0) {
             if (k < a.V) {
                 if (k <= kMostK) {
-                    clean();
+                    if (!own) clean();
                     dirty = true;
                     by_candidates();
                 }
@@ -1053,13 +1076,11 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
                 if (tid == 0) sm.listed = 0;
                 cluster.sync();
                 enlist([&](const uint4& v, int i) {
-                    unsigned which = 0;
-                    if (R::top(v) < z0) return which;
+                    unsigned which = R::from(v, z0);
+                    if (which == 0 || border.last == kAll) return which;
 #pragma unroll
-                    for (int x = 0; x < N; ++x) {
-                        const float z = R::get(v, x);
-                        which |= static_cast<unsigned>(z > z0 || (z == z0 && i + x <= border.last)) << x;
-                    }
+                    for (int x = 0; x < N; ++x)
+                        if (R::get(v, x) == z0 && i + x > border.last) which &= ~(1u << R::bit(x));
                     return which;
                 });
                 const int n = static_cast<int>(collect());
@@ -1248,6 +1269,9 @@ cudaError_t pick(const FilterArgs& a, int rows, int sms, cudaStream_t stream) {
     // CTAs of a row: as many as leave two on an SM (8 vectors a thread), and more where rows are fewer than SMs
     constexpr int kTwo = 8, kMost = (227 * 1024 - kSmall) / (kFThreads * 16);
     int C = 1;
+    // Many rows that are cut to few tokens: a CTA a row, which reads it twice (from the second level cache or memory) and writes it without another look. 576 rows of
+    // 128256, top_k 1000: @1 us, four CTAs that hold it 200; 150 rows @2 and @3.
+    if (!a.top_ks && a.top_k > 0 && a.top_k <= kMostK && a.V > kFew && runs > kTwo && 2LL * rows > 3LL * sms) return launch<DT, false>(a, rows, 1, static_cast<int>(runs), stream);
     while (C < 8 && (runs > static_cast<long long>(C) * kTwo || (runs > C && 2LL * C * rows <= sms))) C *= 2;
     const int nv = static_cast<int>((runs + C - 1) / C);
     return nv <= kMost ? launch<DT, true>(a, rows, C, nv, stream) : launch<DT, false>(a, rows, C, nv, stream);
