@@ -4,10 +4,20 @@
 // top-k largest: the first k.  top-p: those before which less than top_p of the mass of the k lies.  min-p: those not
 // below max + T ln(min_p).  So a row's outcome is one pair: a token is kept if its key is larger, or equal and its index not larger.
 //
-// A row is a cluster's, up to eight CTAs that hold it in registers from the one time it is read until it is written.  The last kept key is found digit
-// by digit (11, 11 and 10 bits of keys in the order of the logits), a histogram a digit: counts for top-k, and for top-p weights as integers of
-// up to 2^-45 of the largest, whose sums do not depend on the order of the additions.  Weights are exponentials in 64 bits: a
-// border between tokens of 10^-6 each is off by 10^-5 of a token for an error of 10^-11.
+// A row is a cluster's, up to eight CTAs that hold it in shared memory from the one time it is read until it is written (or one CTA's that reads it again).  The
+// last kept one is found by one of
+//   candidates   top-k of up to 1024: the k-th largest of the vectors' maxima, from a histogram, bounds the k-th token; what is not below goes into a list, which the
+//                first CTA puts in order, and the rest (top-p, min-p, the token) follows from the list
+//   values       16 bits: the tokens of each value are counted, so that a mass is a count times a weight
+//   masses       32 bits: a histogram over the distance from the largest bounds the masses, so that only the tokens of a few bins have to be put in order
+//   digits       whatever the others leave (lists that do not fit, infinities where the bins would be): 11, 11 and 10 bits of the keys, a histogram each, of counts or of
+//                weights as integers of up to 2^-45 of the largest, whose sums do not depend on the order of the additions
+// Weights are exponentials in 64 bits: a border between tokens of 10^-6 each is off by 10^-5 of a token for an error of 10^-11.
+//
+// One row of 32000, top_k 50, top_p 0.95: 14 us (13 on the GPU), a chain of barriers and exchanges between CTAs; 64 rows of 128256, top_p 0.9: 35 us, the same
+// chain and the histogram's additions (8 of 35); 576 rows, top_k 1000: 123 us, memory (each row is read twice); 37 rows of 50257 in 32 bits, all kinds of cuts: 31 us, the
+// pipe for 64 bits (a vocabulary's weights).
+// Measured and not kept: bins of fixed values counted while a row is read (64 rows 49 us against 39 then); a wider ring of loads for rows that are read again.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
@@ -891,7 +901,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
 
     // In 16 bits, top-k and top-p by counting the tokens of each value: a bin a value from the largest down, so that a mass is a count times a weight, and
     // the border is where the formulas have it.  2048 bins hold 16 powers of two; where logits of both signs matter, the values next to 0 share one bin, as do the
-    // least, and their masses are summed up (64 rows of 128256, top_p 0.9: 61 us with bins of equal width and all weights summed up, now 38).  How many are kept, or
+    // least, and their masses are summed up (64 rows of 128256, top_p 0.9: 61 us with bins of equal width and all weights summed up, then 39).  How many are kept, or
     // -1: the border lies in a shared bin.
     auto by_keys = [&]() {
         const bool mass = p < 1.f && p > 0.f;
@@ -1270,7 +1280,7 @@ cudaError_t pick(const FilterArgs& a, int rows, int sms, cudaStream_t stream) {
     constexpr int kTwo = 8, kMost = (227 * 1024 - kSmall) / (kFThreads * 16);
     int C = 1;
     // Many rows that are cut to few tokens: a CTA a row, which reads it twice (from the second level cache or memory) and writes it without another look. 576 rows of
-    // 128256, top_k 1000: @1 us, four CTAs that hold it 200; 150 rows @2 and @3.
+    // 128256, top_k 1000: 123 us, four CTAs that hold it 216.
     if (!a.top_ks && a.top_k > 0 && a.top_k <= kMostK && a.V > kFew && runs > kTwo && 2LL * rows > 3LL * sms) return launch<DT, false>(a, rows, 1, static_cast<int>(runs), stream);
     while (C < 8 && (runs > static_cast<long long>(C) * kTwo || (runs > C && 2LL * C * rows <= sms))) C *= 2;
     const int nv = static_cast<int>((runs + C - 1) / C);
