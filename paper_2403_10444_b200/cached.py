@@ -105,7 +105,7 @@ class Decoder:
         c, T = self.cache, tokens.shape[0]
         # (without rotary positions: pairs that turn by nothing)
         r = self.rotary or Rotary(torch.zeros((1,), dtype=torch.float64, device=tokens.device))
-        x = self.w["embed"][tokens]
+        x = self.w["embed"][tokens.clamp(0, self.w["embed"].shape[0] - 1)]
         for layer, k, v in zip(self.w["layers"], c.k, c.v):
             qkv = (x @ layer["qkv"]).view(T, self.heads + 2 * self.kv_heads, self.D)
             q, kn, vn = qkv.split([self.heads, self.kv_heads, self.kv_heads], dim=1)

@@ -1280,8 +1280,10 @@ cudaError_t pick(const FilterArgs& a, int rows, int sms, cudaStream_t stream) {
     constexpr int kTwo = 8, kMost = (227 * 1024 - kSmall) / (kFThreads * 16);
     int C = 1;
     // Many rows that are cut to few tokens: a CTA a row, which reads it twice (from the second level cache or memory) and writes it without another look.  Rows of
-    // 128256, top_k 1000: 104 of them 45 us, by four CTAs that hold each 53; 200: 59 and 80; 576: 123 and 216.
-    if (!a.top_ks && a.top_k > 0 && a.top_k <= kMostK && a.V > kFew && runs > kTwo && 10LL * rows > 7LL * sms) return launch<DT, false>(a, rows, 1, static_cast<int>(runs), stream);
+    // 128256, top_k 1000: 104 of them 45 us, by four CTAs that hold each 53; 200: 59 and 80; 576: 123 and 216.  In 16 bits also rows for every SM that are cut in any
+    // way: top_p 0.9, 148 of them 65 and 85, 300: 138 and 146.  (In 32 bits, 300 of 50257: 168 and 165.)
+    const bool few = !a.top_ks && a.top_k > 0 && a.top_k <= kMostK && a.V > kFew;
+    if (runs > kTwo && ((few && 10LL * rows > 7LL * sms) || (DT == kBF16 && rows >= sms))) return launch<DT, false>(a, rows, 1, static_cast<int>(runs), stream);
     while (C < 8 && (runs > static_cast<long long>(C) * kTwo || (runs > C && 2LL * C * rows <= sms))) C *= 2;
     const int nv = static_cast<int>((runs + C - 1) / C);
     return nv <= kMost ? launch<DT, true>(a, rows, C, nv, stream) : launch<DT, false>(a, rows, C, nv, stream);

@@ -267,7 +267,7 @@ int enqueue_prompt(const StreamWork& work, void* ctx) {
     if (c.tiles) e = launch_prompt_tiles(c.a, c.out_vec, work.sm_count, c.stream, &taken);
     if (e == cudaSuccess && !taken) e = launch_prompt_rows(c.a, c.dtype, c.aligned, c.stream);
     if (e != cudaSuccess) return note_cuda_error(e);
-    note_launches(1);
+    note_launches(taken ? prompt_tiles_launches(c.a.B) : 1);
     return BV_OK;
 }
 

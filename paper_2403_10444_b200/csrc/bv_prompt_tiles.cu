@@ -700,6 +700,7 @@ cudaError_t launch_tiles(const PromptArgs& a, const CUtensorMap& q, const CUtens
 
 }  // namespace
 
+int prompt_tiles_launches(int B) { return (B + kMostPrompts - 1) / kMostPrompts; }
 // (scores are multiplied by a number that keeps their order, and -inf as it is)
 bool prompt_tiles_takes(const PromptArgs& a) { return a.D >= 16 && a.D <= 128 && a.D % 8 == 0 && a.group <= kTile && a.kf > 0.f; }
 cudaError_t launch_prompt_tiles(const PromptArgs& a, bool out_vec, int ctas, cudaStream_t stream, bool* taken) {
