@@ -1,9 +1,10 @@
 // bv_prompt_attend: the entry point, and the kernel for 32 bits and every shape that the tensor cores do not take (bv_prompt_tiles.cu).
 //
-// Rows of a key-value head (a token's heads of the group one after the other) are cut into tiles of 64, a CTA takes one over the keys it sees, 64 at
-// a time, with a running maximum and sum for each row: scores by 4 x 4 values a thread from shared memory, weights through shared memory,
-// results in registers.  Bound by the FMAs of both products and what shared memory has to deliver for them, and where tiles are few by the
-// longest one's steps in a row: 7 prompts of up to 701 tokens, 10 heads on 2, D = 80: 169 us, 14 TFLOP/s.
+// Rows of a key-value head (a token's heads of the group one after the other) are cut into tiles of 64 or 128, a CTA takes one over the keys it
+// sees, 64 at a time, with a running maximum and sum for each row: scores by 4 x 4 or 8 x 4 values a thread from shared memory, weights through
+// shared memory, results in registers.  Bound by the FMAs of both products and what shared memory has to deliver for them (tiles of 128 read a key's
+// values half as often: 4 prompts of 2048 tokens, 32 heads on 8, D = 128: 3.8 ms, 36 TFLOP/s; with tiles of 64 5.0 ms), and where tiles are few by
+// the longest one's steps in a row: 7 prompts of up to 701 tokens, 10 heads on 2, D = 80: 172 us, 14 TFLOP/s.
 #include <cmath>
 
 #include "bv_launch.h"
@@ -12,7 +13,7 @@
 namespace bv {
 namespace {
 
-constexpr int kR = 64, kK = 64, kPThreads = 256;
+constexpr int kK = 64, kPThreads = 256;
 constexpr int kPStride = kK + 4;
 constexpr float kUnseen = -1.f;                // in the place of a weight: the row does not see the key
 
@@ -20,7 +21,7 @@ struct RowsLayout {
     int q_stride, v_stride;                    // floats
     // (an odd number of 16 bytes between rows: eight rows in a column are in eight different places)
     __host__ __device__ explicit RowsLayout(int D) : q_stride(((D + 3) / 4 | 1) * 4), v_stride((D + 63) / 64 * 64) {}
-    __host__ __device__ size_t bytes() const { return sizeof(float) * (static_cast<size_t>(kR + kK) * q_stride + static_cast<size_t>(kK) * v_stride + kR * kPStride); }
+    __host__ __device__ size_t bytes(int R) const { return sizeof(float) * (static_cast<size_t>(R + kK) * q_stride + static_cast<size_t>(kK) * v_stride + static_cast<size_t>(R) * kPStride); }
 };
 
 template <typename E> __device__ __forceinline__ float widen(E x);
@@ -30,20 +31,47 @@ template <typename E> __device__ __forceinline__ E narrow(float x);
 template <> __device__ __forceinline__ float narrow(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 narrow(float x) { return __float2bfloat16_rn(x); }
 
-// Rows to shared memory, widened; zero beyond D and beyond `count`.  from(row): its first element.
-template <typename E, bool VEC, typename F>
+// A vector to shared memory, widened.
+template <typename E>
+__device__ __forceinline__ void widen_to(float* to, const uint4& v, int c, int width) {
+    const E* e = reinterpret_cast<const E*>(&v);
+#pragma unroll
+    for (int i = 0; i < 16 / static_cast<int>(sizeof(E)); i += 4)
+        if (c + i < width) *reinterpret_cast<float4*>(to + c + i) = make_float4(widen<E>(e[i]), widen<E>(e[i + 1]), widen<E>(e[i + 2]), widen<E>(e[i + 3]));
+}
+
+// Rows to shared memory, widened; zero beyond D and beyond `count`.  from(row): its first element.  AHEAD: vectors of a thread under way together, with
+// their places counted on: 4 where a CTA is alone on its SM (4 prompts of 2048: 3.98 -> 3.79 ms); with two CTAs the plain loop is the faster (6000 tokens, 4 heads on 1: 1.38 and 1.57 ms).
+template <typename E, bool VEC, int AHEAD, typename F>
 __device__ __forceinline__ void stage(float* to, int stride, int width, int rows, int count, int D, F from) {
-    if constexpr (VEC) {
-        constexpr int N = 16 / sizeof(E);
+    constexpr int N = 16 / sizeof(E);
+    if constexpr (VEC && AHEAD == 1) {
         const int per = (width + N - 1) / N;
         for (int x = threadIdx.x; x < rows * per; x += kPThreads) {
             const int r = x / per, c = (x - r * per) * N;
             uint4 v = make_uint4(0, 0, 0, 0);
             if (r < count && c < D) v = __ldg(reinterpret_cast<const uint4*>(from(r) + c));      // (D is whole vectors)
-            const E* e = reinterpret_cast<const E*>(&v);
+            widen_to<E>(to + r * stride, v, c, width);
+        }
+    } else if constexpr (VEC) {
+        const int per = (width + N - 1) / N, step_r = kPThreads / per, step_c = kPThreads - step_r * per;
+        int r = threadIdx.x / per, c = threadIdx.x - r * per;
+        while (r < rows) {
+            uint4 v[AHEAD];
+            int rs[AHEAD], cs[AHEAD];
 #pragma unroll
-            for (int i = 0; i < N; i += 4)
-                if (c + i < width) *reinterpret_cast<float4*>(to + r * stride + c + i) = make_float4(widen<E>(e[i]), widen<E>(e[i + 1]), widen<E>(e[i + 2]), widen<E>(e[i + 3]));
+            for (int i = 0; i < AHEAD; ++i) {
+                rs[i] = r;
+                cs[i] = c * N;
+                v[i] = make_uint4(0, 0, 0, 0);
+                if (r < count && c * N < D) v[i] = __ldg(reinterpret_cast<const uint4*>(from(r) + c * N));
+                r += step_r;
+                c += step_c;
+                if (c >= per) { c -= per; ++r; }
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (rs[i] < rows) widen_to<E>(to + rs[i] * stride, v[i], cs[i], width);
         }
     } else {
         for (int x = threadIdx.x; x < rows * width; x += kPThreads) {
@@ -54,6 +82,7 @@ __device__ __forceinline__ void stage(float* to, int stride, int width, int rows
 }
 
 // The CTA's sequence and tile of rows: tiles of all sequences in order, a sequence's last ones (they see the most) first.
+template <int kR>
 __device__ __forceinline__ bool find_rows(const PromptArgs& a, int x, int* b, int* tile, Prompt* prompt) {
     __shared__ int sums[kPThreads / 32], found[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -93,9 +122,10 @@ __device__ __forceinline__ bool find_rows(const PromptArgs& a, int x, int* b, in
     return false;
 }
 
-// NC: 64-column parts of D.
-template <typename E, bool VEC, int NC>
-__global__ void __launch_bounds__(kPThreads, NC <= 2 ? 2 : 1) prompt_rows_kernel(const PromptArgs a) {
+// NC: 64-column parts of D.  RT: rows of a thread.
+template <typename E, bool VEC, int NC, int RT>
+__global__ void __launch_bounds__(kPThreads, NC <= 2 && RT == 4 ? 2 : 1) prompt_rows_kernel(const PromptArgs a) {
+    constexpr int kR = 16 * RT;                             // a tile's
     extern __shared__ __align__(16) float shared[];
     const RowsLayout lay(a.D);
     float* const sq = shared;
@@ -105,7 +135,7 @@ __global__ void __launch_bounds__(kPThreads, NC <= 2 ? 2 : 1) prompt_rows_kernel
     const int tid = threadIdx.x, tr = tid >> 4, tc = tid & 15;
     int b, tile;
     Prompt s;
-    if (!find_rows(a, static_cast<int>(blockIdx.x / a.Hkv), &b, &tile, &s)) return;
+    if (!find_rows<kR>(a, static_cast<int>(blockIdx.x / a.Hkv), &b, &tile, &s)) return;
     const int h = blockIdx.x % a.Hkv;
     const int r0 = tile * kR;                               // of length * group rows
     const long long all_rows = static_cast<long long>(s.length) * a.group;
@@ -113,18 +143,18 @@ __global__ void __launch_bounds__(kPThreads, NC <= 2 ? 2 : 1) prompt_rows_kernel
     const int wide = (a.D + 3) / 4 * 4;
     {
         const E* q = static_cast<const E*>(a.q) + s.first * a.qs[0] + h * a.group * a.qs[1];
-        stage<E, VEC>(sq, lay.q_stride, wide, kR, count, a.D, [&](int r) { const int t = a.by_group(r0 + r); return q + t * a.qs[0] + (r0 + r - t * a.group) * a.qs[1]; });
+        stage<E, VEC, RT == 8 ? 4 : 1>(sq, lay.q_stride, wide, kR, count, a.D, [&](int r) { const int t = a.by_group(r0 + r); return q + t * a.qs[0] + (r0 + r - t * a.group) * a.qs[1]; });
     }
-    int pos[4], low[4];
+    int pos[RT], low[RT];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        pos[i] = a.by_group(r0 + tr * 4 + i);
+    for (int i = 0; i < RT; ++i) {
+        pos[i] = a.by_group(r0 + tr * RT + i);
         low[i] = low_of(a, pos[i]);
     }
     const int p0 = a.by_group(r0), p1 = a.by_group(r0 + count - 1), low0 = low_of(a, p0), low1 = low_of(a, p1);
-    float m[4], l[4], o[4][NC * 4];
+    float m[RT], l[RT], o[RT][NC * 4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < RT; ++i) {
         m[i] = -INFINITY;
         l[i] = 0.f;
 #pragma unroll
@@ -138,29 +168,29 @@ __global__ void __launch_bounds__(kPThreads, NC <= 2 ? 2 : 1) prompt_rows_kernel
         const int keys = p1 + 1 - start < kK ? p1 + 1 - start : kK;
         const bool whole = start + kK - 1 <= p0 && (start >= low1 || start + kK <= a.sinks);
         __syncthreads();
-        stage<E, VEC>(sk, lay.q_stride, wide, kK, keys, a.D, [&](int j) { return k + (start + j) * a.ks[0]; });
-        stage<E, VEC>(sv, lay.v_stride, lay.v_stride, kK, keys, a.D, [&](int j) { return v + (start + j) * a.vs[0]; });
+        stage<E, VEC, RT == 8 ? 4 : 1>(sk, lay.q_stride, wide, kK, keys, a.D, [&](int j) { return k + (start + j) * a.ks[0]; });
+        stage<E, VEC, RT == 8 ? 4 : 1>(sv, lay.v_stride, lay.v_stride, kK, keys, a.D, [&](int j) { return v + (start + j) * a.vs[0]; });
         __syncthreads();
-        float x[4][4];
+        float x[RT][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < RT; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[i][j] = 0.f;
 #pragma unroll 2
         for (int d = 0; d < wide; d += 4) {
-            float4 qv[4], kv[4];
+            float4 qv[RT], kv[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) qv[i] = *reinterpret_cast<const float4*>(sq + (tr * 4 + i) * lay.q_stride + d);
+            for (int i = 0; i < RT; ++i) qv[i] = *reinterpret_cast<const float4*>(sq + (tr * RT + i) * lay.q_stride + d);
 #pragma unroll
             for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4*>(sk + (tc + 16 * j) * lay.q_stride + d);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < RT; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     x[i][j] = fmaf(qv[i].w, kv[j].w, fmaf(qv[i].z, kv[j].z, fmaf(qv[i].y, kv[j].y, fmaf(qv[i].x, kv[j].x, x[i][j]))));
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < RT; ++i) {
             float top = -INFINITY;
             bool sees[4];
 #pragma unroll
@@ -179,7 +209,7 @@ __global__ void __launch_bounds__(kPThreads, NC <= 2 ? 2 : 1) prompt_rows_kernel
             for (int j = 0; j < 4; ++j) {
                 const float w = ex2(__fsub_rn(x[i][j], ref));
                 sum += sees[j] ? w : 0.f;
-                sp[(tr * 4 + i) * kPStride + tc + 16 * j] = sees[j] ? w : kUnseen;
+                sp[(tr * RT + i) * kPStride + tc + 16 * j] = sees[j] ? w : kUnseen;
             }
             l[i] = l[i] * scale + sum;
 #pragma unroll
@@ -190,10 +220,10 @@ __global__ void __launch_bounds__(kPThreads, NC <= 2 ? 2 : 1) prompt_rows_kernel
         auto add = [&](auto checked) {
 #pragma unroll 2
             for (int j = 0; j < kK; j += 4) {
-                float w[4][4];
+                float w[RT][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float4 f = *reinterpret_cast<const float4*>(sp + (tr * 4 + i) * kPStride + j);
+                for (int i = 0; i < RT; ++i) {
+                    const float4 f = *reinterpret_cast<const float4*>(sp + (tr * RT + i) * kPStride + j);
                     w[i][0] = f.x; w[i][1] = f.y; w[i][2] = f.z; w[i][3] = f.w;
                 }
 #pragma unroll
@@ -202,7 +232,7 @@ __global__ void __launch_bounds__(kPThreads, NC <= 2 ? 2 : 1) prompt_rows_kernel
                     for (int c = 0; c < NC; ++c) {
                         const float4 f = *reinterpret_cast<const float4*>(sv + (j + y) * lay.v_stride + c * 64 + tc * 4);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
+                        for (int i = 0; i < RT; ++i) {
                             if (decltype(checked)::value && w[i][y] == kUnseen) continue;      // (0 times an infinity is not 0)
                             o[i][c * 4] = fmaf(w[i][y], f.x, o[i][c * 4]);
                             o[i][c * 4 + 1] = fmaf(w[i][y], f.y, o[i][c * 4 + 1]);
@@ -217,11 +247,11 @@ __global__ void __launch_bounds__(kPThreads, NC <= 2 ? 2 : 1) prompt_rows_kernel
     }
     E* const out = static_cast<E*>(a.out) + s.first * a.os[0] + h * a.group * a.os[1];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < RT; ++i) {
         float sum = l[i];
 #pragma unroll
         for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-        const int r = tr * 4 + i;
+        const int r = tr * RT + i;
         if (r >= count) continue;
         const float f = 1.f / sum;                          // (a row without weight: 0 / 0)
         E* to = out + pos[i] * a.os[0] + (r0 + r - pos[i] * a.group) * a.os[1];
@@ -233,21 +263,30 @@ __global__ void __launch_bounds__(kPThreads, NC <= 2 ? 2 : 1) prompt_rows_kernel
     }
 }
 
-template <typename E, bool VEC, int NC>
+// As many CTAs as there may be tiles (one more for each sequence than their rows would fill); those that find none leave.
+long long rows_ctas(const PromptArgs& a, int R) { return ((static_cast<long long>(a.tokens) * a.group + R - 1) / R + a.B) * a.Hkv; }
+
+template <typename E, bool VEC, int NC, int RT>
 cudaError_t launch_rows(const PromptArgs& a, cudaStream_t stream) {
     static std::atomic<unsigned long long> asked{0};
-    const size_t bytes = RowsLayout(a.D).bytes();
-    const cudaError_t e = allow_shared(prompt_rows_kernel<E, VEC, NC>, static_cast<int>(RowsLayout(NC * 64).bytes()), asked);
+    constexpr int kR = 16 * RT;
+    const size_t bytes = RowsLayout(a.D).bytes(kR);
+    const cudaError_t e = allow_shared(prompt_rows_kernel<E, VEC, NC, RT>, static_cast<int>(RowsLayout(NC * 64).bytes(kR)), asked);
     if (e != cudaSuccess) return e;
-    // as many CTAs as there may be tiles (one more for each sequence than their rows would fill); those that find none leave
-    const long long tiles = (static_cast<long long>(a.tokens) * a.group + kR - 1) / kR + a.B, ctas = tiles * a.Hkv;
+    const long long ctas = rows_ctas(a, kR);
     if (ctas > 0x7fffffff) return cudaErrorInvalidValue;
-    prompt_rows_kernel<E, VEC, NC><<<static_cast<unsigned>(ctas), kPThreads, bytes, stream>>>(a);
+    prompt_rows_kernel<E, VEC, NC, RT><<<static_cast<unsigned>(ctas), kPThreads, bytes, stream>>>(a);
     return cudaGetLastError();
 }
 template <typename E, bool VEC>
-cudaError_t pick_rows(const PromptArgs& a, cudaStream_t stream) {
-    return a.D <= 64 ? launch_rows<E, VEC, 1>(a, stream) : a.D <= 128 ? launch_rows<E, VEC, 2>(a, stream) : launch_rows<E, VEC, 4>(a, stream);
+cudaError_t pick_rows(const PromptArgs& a, int sms, cudaStream_t stream) {
+    // Tiles of 128 rows (one CTA an SM) where every SM gets two or more and a row has more than 64 columns: one prompt of 4096 tokens, 16 heads on 4,
+    // D = 128: 2.39 ms by 64 rows, 1.89 by 128; 16 of 300, 32 on 8: 650 and 527 us; D = 96: 1003 and 961 us.  With fewer tiles a wave of them is too
+    // long (6000 tokens, 4 heads on 1: 1.39 and 1.48 ms; 7 prompts of up to 701, 10 on 2, D = 80: 171 and 182 us; but 4096 tokens, 8 on 2: 1.23 and
+    // 1.01 ms), and up to 64 columns the loads take what the FMAs win (620 and 657 us).
+    if constexpr (sizeof(E) == 4 && VEC)
+        if (a.D > 64 && a.D <= 128 && rows_ctas(a, 128) - static_cast<long long>(a.B) * a.Hkv >= 2 * sms) return launch_rows<E, VEC, 2, 8>(a, stream);
+    return a.D <= 64 ? launch_rows<E, VEC, 1, 4>(a, stream) : a.D <= 128 ? launch_rows<E, VEC, 2, 4>(a, stream) : launch_rows<E, VEC, 4, 4>(a, stream);
 }
 
 struct PromptCall {
@@ -265,7 +304,7 @@ int enqueue_prompt(const StreamWork& work, void* ctx) {
     cudaError_t e = cudaSuccess;
     bool taken = false;
     if (c.tiles) e = launch_prompt_tiles(c.a, c.out_vec, work.sm_count, c.stream, &taken);
-    if (e == cudaSuccess && !taken) e = launch_prompt_rows(c.a, c.dtype, c.aligned, c.stream);
+    if (e == cudaSuccess && !taken) e = launch_prompt_rows(c.a, c.dtype, c.aligned, work.sm_count, c.stream);
     if (e != cudaSuccess) return note_cuda_error(e);
     note_launches(taken ? prompt_tiles_launches(c.a.B) : 1);
     return BV_OK;
@@ -273,9 +312,9 @@ int enqueue_prompt(const StreamWork& work, void* ctx) {
 
 }  // namespace
 
-cudaError_t launch_prompt_rows(const PromptArgs& a, int dtype, bool aligned, cudaStream_t stream) {
-    if (dtype == BV_DTYPE_F32) return aligned ? pick_rows<float, true>(a, stream) : pick_rows<float, false>(a, stream);
-    return aligned ? pick_rows<__nv_bfloat16, true>(a, stream) : pick_rows<__nv_bfloat16, false>(a, stream);
+cudaError_t launch_prompt_rows(const PromptArgs& a, int dtype, bool aligned, int sms, cudaStream_t stream) {
+    if (dtype == BV_DTYPE_F32) return aligned ? pick_rows<float, true>(a, sms, stream) : pick_rows<float, false>(a, sms, stream);
+    return aligned ? pick_rows<__nv_bfloat16, true>(a, sms, stream) : pick_rows<__nv_bfloat16, false>(a, sms, stream);
 }
 
 }  // namespace bv

@@ -35,7 +35,7 @@ __device__ __forceinline__ Prompt prompt_of(const PromptArgs& a, int b) {
 // The lowest position that a token at `pos` sees through its window.
 __device__ __forceinline__ int low_of(const PromptArgs& a, int pos) { return a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0; }
 
-cudaError_t launch_prompt_rows(const PromptArgs& a, int dtype, bool aligned, cudaStream_t stream);
+cudaError_t launch_prompt_rows(const PromptArgs& a, int dtype, bool aligned, int sms, cudaStream_t stream);
 bool prompt_tiles_takes(const PromptArgs& a);
 // (`taken` is false if no map of the tensors could be had)
 cudaError_t launch_prompt_tiles(const PromptArgs& a, bool out_vec, int ctas, cudaStream_t stream, bool* taken);

@@ -20,7 +20,8 @@
 // and its results, and CTAs' shares uneven by 12 %.
 // Measured and not kept: tiles of 64 keys with two S each, so that scores run ahead (products of 64 columns take as long as those of 128: 9.6 ms); a quarter of the
 // exponentials on the FMA pipe (more instructions: 8.8 ms, 361 us); warps that share a scheduler taking turns at exponentials (8.7 against 7.3 ms); one signal a
-// tile instead of two (8.95 ms); sums of weights before their rounding (7.9 against 7.6 ms, and less exact).
+// tile instead of two (8.95 ms); sums of weights before their rounding (7.9 against 7.6 ms, and less exact); two
+// threads a row, 16 warps at the softmax (88 registers a thread are too few: 21 ms, 714 us).
 #include "bv_launch.h"
 #include "bv_prompt.cuh"
 #include "bv_tensor.cuh"

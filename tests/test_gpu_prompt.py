@@ -273,3 +273,15 @@ def test_refusals():
     empty = torch.zeros((1,), dtype=torch.int32, device="cuda")
     assert not bv.bv_prompt_attend(q, k, v, empty).any()
     assert bv.bv_prompt_attend(q[:0], k[:0], v[:0], off).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,D", [([700, 1, 0, 333, 129], 39, 13, 128), ([1], 1, 1, 68), ([130] * 9 + [127, 5], 32, 32, 100), ([2500], 16, 16, 96)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 7)])
+def test_32_bits_with_tiles_for_every_multiprocessor(lens, Hq, Hkv, D, window, sinks):
+    """More than 64 columns and many tiles (and one that has few): whatever tile's size is taken, hidden values that are not finite stay hidden."""
+    q, k, v, off = make(lens, Hq, Hkv, D, dtype=F32, head=2, tail=3, seed=D)
+    for t in (k, v):
+        t[:2], t[-3:] = math.nan, math.inf
+    if window and lens[0] > 300:
+        v[2 + 50] = math.nan                       # rows 50 to 149 of the first sequence are NaN, no other
+    check(q, k, v, off, window=window, sinks=sinks)
