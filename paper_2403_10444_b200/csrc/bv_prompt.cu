@@ -303,7 +303,7 @@ int enqueue_prompt(const StreamWork& work, void* ctx) {
     c.a.never_signal = work.never_signal;
     cudaError_t e = cudaSuccess;
     bool taken = false;
-    if (c.tiles) e = launch_prompt_tiles(c.a, c.out_vec, work.sm_count, c.stream, &taken);
+    if (c.tiles) e = launch_prompt_tiles(c.a, c.out_vec, c.stream, &taken);
     if (e == cudaSuccess && !taken) e = launch_prompt_rows(c.a, c.dtype, c.aligned, work.sm_count, c.stream);
     if (e != cudaSuccess) return note_cuda_error(e);
     note_launches(taken ? prompt_tiles_launches(c.a.B) : 1);

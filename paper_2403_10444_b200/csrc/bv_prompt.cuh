@@ -38,7 +38,7 @@ __device__ __forceinline__ int low_of(const PromptArgs& a, int pos) { return a.w
 cudaError_t launch_prompt_rows(const PromptArgs& a, int dtype, bool aligned, int sms, cudaStream_t stream);
 bool prompt_tiles_takes(const PromptArgs& a);
 // (`taken` is false if no map of the tensors could be had)
-cudaError_t launch_prompt_tiles(const PromptArgs& a, bool out_vec, int ctas, cudaStream_t stream, bool* taken);
+cudaError_t launch_prompt_tiles(const PromptArgs& a, bool out_vec, cudaStream_t stream, bool* taken);
 int prompt_tiles_launches(int B);
 
 }  // namespace bv

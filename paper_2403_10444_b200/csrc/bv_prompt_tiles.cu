@@ -12,12 +12,14 @@
 // that some rows of the unit do not see: nobody's are set to 0 in shared memory, others keep their finite elements there, and what is
 // not finite is added where it belongs when the unit ends, from global memory.
 //
-// Units are in the order of their cost, largest first, and go to the CTAs in turn, forth and back.
+// Units are in the order of their cost, largest first.  The launch has a CTA for each of them, and a CTA that is at work asks for the next one that has not begun
+// and does its unit as well (cluster launch control), while it loads its own: memory, barriers and the order of the units are made once, loads go on from unit
+// to unit, and no counter has to be kept between launches (units handed out forth and back left shares uneven by 12 %: 16 prompts of up to 2048: 347 -> 307 us).
 //
-// One prompt of 32768 tokens, 32 heads on 8, D = 128: 8.67 ms, 1.01 PFLOP/s (7.3 to 7.9 ms, up to 1.2 PFLOP/s, a few calls after a pause); 16 prompts of up to 2048: 347 us,
-// 650 TFLOP/s.  A key tile of both tiles of rows takes 3700 clocks (2048 of products): 1800 in which a row's 128 scores become weights, some ten instructions each
+// One prompt of 32768 tokens, 32 heads on 8, D = 128: 8.44 ms, 1.04 PFLOP/s (7.3 to 7.9 ms, up to 1.2 PFLOP/s, a few calls after a pause); 16 prompts of up to 2048: 307 us,
+// 735 TFLOP/s.  A key tile of both tiles of rows takes 3700 clocks (2048 of products): 1800 in which a row's 128 scores become weights, some ten instructions each
 // by one warp a scheduler, 600 for reading them and their maximum, 1200 until the next scores are there.  Short prompts: 20 % more for a unit's first tile
-// and its results, and CTAs' shares uneven by 12 %.
+// and its results.
 // Measured and not kept: tiles of 64 keys with two S each, so that scores run ahead (products of 64 columns take as long as those of 128: 9.6 ms); a quarter of the
 // exponentials on the FMA pipe (more instructions: 8.8 ms, 361 us); warps that share a scheduler taking turns at exponentials (8.7 against 7.3 ms); one signal a
 // tile instead of two (8.95 ms); sums of weights before their rounding (7.9 against 7.6 ms, and less exact); two
@@ -36,6 +38,24 @@ constexpr float kNone = -3.0e38f;              // the reference of a row that ha
 constexpr float kLag = 8.f;
 constexpr int kFirstKeys = 96;                 // of a tile, whose weights are multiplied while the others are formed
 constexpr int kMostPrompts = 1024;             // of a launch
+constexpr int kTold = 4;                       // units that the loading thread may be ahead of who is last to hear of them
+
+// Asks for a CTA of the launch that has not begun, whose work this one then does; the answer is 16 bytes, signalled at bar.
+__device__ __forceinline__ void ask(uint32_t answer, uint32_t bar) {
+    fence_async();                             // (the last answer has been read)
+    mbar_arrive_expect(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(bar) : "memory");
+}
+// Its index, or -1.
+__device__ __forceinline__ int answered(uint32_t answer) {
+    uint32_t got, x = 0;
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b128 h;\n\t.reg .b32 y, z, w;\n\tld.shared.b128 h, [%2];\n\tclusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, y, z, w}, h;\n\t}"
+                 : "=r"(got), "+r"(x)
+                 : "r"(answer)
+                 : "memory");
+    return got ? static_cast<int>(x) : -1;
+}
 
 __device__ __forceinline__ void tma_load3(uint32_t dst, const CUtensorMap* map, int x, int head, int token, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(head),
@@ -86,6 +106,9 @@ struct __align__(1024) PromptSmem {
     using Sh = PromptShape<NP>;
     char q[2][Sh::kSlot];
     char ring[Sh::kSlots][Sh::kSlot];
+    ulonglong2 answer;                     // to the request for a unit that has not begun
+    unsigned long long asked, told[kTold], heard[kTold];
+    int next[kTold];                       // units after the first one, by their places in the CTA's order; -1: none
     unsigned long long q_full[2], q_empty[2], full[8], empty[8], unclean[8], s_full[2], s_read[2], p_part[2], p_full[2], o_done[2], drain;
     uint32_t tmem;
     int abort;
@@ -95,7 +118,7 @@ struct __align__(1024) PromptSmem {
     int before[kMostPrompts];              // pairs that come before the levels at which a sequence is the last
 };
 
-// Unit u of a CTA: a pair of tiles of a sequence's key-value head.
+// Unit u of the launch: a pair of tiles of a sequence's key-value head.
 struct Pair {
     int b, h, first, length;               // the sequence's first row and its rows
     int t0;                                // the first tile's first token
@@ -107,12 +130,10 @@ struct Pair {
 __device__ __forceinline__ int key_tile(const Pair& p, int i) { return i < p.sink_tiles ? i : i - p.sink_tiles + p.jump; }
 
 template <int NP>
-__device__ __forceinline__ bool pair_at(const PromptArgs& a, const PromptSmem<NP>& sm, int tokens_each, int base, int round, Pair* p) {
-    const int G = static_cast<int>(gridDim.x), c = static_cast<int>(blockIdx.x);
-    const long long u = static_cast<long long>(round) * G + (round & 1 ? G - 1 - c : c);
-    if (u >= static_cast<long long>(sm.units) * a.Hkv) return false;
-    const int x = static_cast<int>(u / a.Hkv);
-    p->h = static_cast<int>(u - static_cast<long long>(x) * a.Hkv);
+__device__ __forceinline__ bool pair_at(const PromptArgs& a, const PromptSmem<NP>& sm, int tokens_each, int base, int u, Pair* p) {
+    if (u < 0 || u >= static_cast<long long>(sm.units) * a.Hkv) return false;
+    const int x = u / a.Hkv;
+    p->h = u - x * a.Hkv;
     // the levels at which sequences 0 .. j have pairs: from the longest's down to one above the next one's
     int lo = 0, hi = sm.sequences;
     while (hi - lo > 1) {
@@ -183,6 +204,22 @@ template <int NP> __device__ __forceinline__ bool wait_on(PromptSmem<NP>& sm, un
     return true;
 }
 
+// The CTA's next unit, for one thread or a whole warp that is not the loading one: the first is the CTA's own, of the others that thread tells.
+template <int NP, bool WARP>
+__device__ __forceinline__ bool next_pair(const PromptArgs& a, PromptSmem<NP>& sm, int tokens_each, int base, int round, uint32_t limit, Pair* p) {
+    int u = static_cast<int>(blockIdx.x);
+    if (round > 0) {
+        const int slot = (round - 1) % kTold;
+        bool ok = wait_on<NP>(sm, sm.told[slot], (round - 1) / kTold, a.status, limit);
+        if (WARP) ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return false;
+        u = *static_cast<volatile int*>(&sm.next[slot]);
+        if (WARP) __syncwarp();
+        if (!WARP || (threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&sm.heard[slot]));
+    }
+    return pair_at<NP>(a, sm, tokens_each, base, u, p);
+}
+
 template <int NP>
 __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const PromptArgs a, const int base, const int sequences, const __grid_constant__ CUtensorMap q_map,
                                                                          const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const int tokens_each,
@@ -215,6 +252,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
             mbar_init(smem_u32(&sm.unclean[i]), 1);
         }
         mbar_init(smem_u32(&sm.drain), 1);
+        mbar_init(smem_u32(&sm.asked), 1);
+        for (int i = 0; i < kTold; ++i) {
+            mbar_init(smem_u32(&sm.told[i]), 1);
+            mbar_init(smem_u32(&sm.heard[i]), kSoftWarps + 3);      // (the issuing thread, two warps that clean)
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         sm.abort = 0;
     }
@@ -275,7 +317,15 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                 int x = 0, round = 0, q_uses[2] = {0, 0};
                 unsigned unclean = 0, phases = 0;      // by slot: does its last copy go through the cleaning warps, how many have (parity)
                 bool ok = true;
-                for (; ok && pair_at<NP>(a, sm, tokens_each, base, round, &p); ++round) {
+                int answers = 0;
+                auto answer = [&] {
+                    const bool in = mbar_wait_now(smem_u32(&sm.asked), answers++ & 1, a.status, limit);
+                    ok = ok && in;
+                    return in ? answered(smem_u32(&sm.answer)) : -1;
+                };
+                bool more = pair_at<NP>(a, sm, tokens_each, base, static_cast<int>(blockIdx.x), &p);
+                for (; ok && more; ++round) {
+                    ask(smem_u32(&sm.answer), smem_u32(&sm.asked));
                     const int tiles = list_length(p);
                     auto fetch = [&](int i) {
                         const int slot = x % kSlots;
@@ -305,6 +355,22 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                         for (int c = 0; c < NP; ++c) tma_load3(smem_u32(sm.q[t]) + c * Sh::kPanel, &q_map, c * 64, p.h * a.group, p.first + p.t0 + t * tokens_each, bar);
                     }
                     for (int i = 1; i < 2 * tiles && ok; ++i) fetch(i);
+                    // (there may be more CTAs than units; after a no there is no other request)
+                    auto another = [&] {
+                        ask(smem_u32(&sm.answer), smem_u32(&sm.asked));
+                        return answer();
+                    };
+                    int u = answer();
+                    while (ok && u >= 0 && !pair_at<NP>(a, sm, tokens_each, base, u, &p)) u = another();
+                    more = u >= 0;
+                    const int slot = round % kTold;
+                    ok = ok && wait_on<NP>(sm, sm.heard[slot], (round / kTold & 1) ^ 1, a.status, limit);
+                    if (ok) {
+                        *static_cast<volatile int*>(&sm.next[slot]) = u;
+                        mbar_arrive(smem_u32(&sm.told[slot]));
+                    }
+                    // (a launch that gave up takes all that has not begun with it)
+                    while (!ok && u >= 0) u = another();
                 }
                 // (a launch that gave up leaves when its copies are in)
                 if (*static_cast<volatile int*>(&sm.abort)) {
@@ -329,7 +395,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                 int x = 0, round = 0, done[2] = {0, 0}, q_uses[2] = {0, 0};      // slots used; tiles done by each of the two
                 bool ok = true;
                 auto wait = [&](unsigned long long& bar, int parity) { ok = ok && wait_on<NP>(sm, bar, parity, a.status, limit); };
-                for (; ok && pair_at<NP>(a, sm, tokens_each, base, round, &p); ++round) {
+                for (; ok && next_pair<NP, false>(a, sm, tokens_each, base, round, limit, &p); ++round) {
                     const int tiles = list_length(p);
                     // scores of tile i of the list for tile t of the pair
                     auto scores = [&](int t, int i) {
@@ -410,7 +476,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
             int x = 0;
             unsigned phases = 0;
             bool ok = true;
-            for (int round = 0; ok && pair_at<NP>(a, sm, tokens_each, base, round, &p); ++round) {
+            for (int round = 0; ok && next_pair<NP, true>(a, sm, tokens_each, base, round, limit, &p); ++round) {
                 const int tiles = list_length(p), low1 = low_of(a, p.p1);
                 if (lane == 0) sm.fix[round % kUnits][member >> 5] = 0;
                 __syncwarp();
@@ -473,7 +539,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
         const int wide = (a.D + 15) / 16 * 16;
         int done = 0;
         bool ok = true;
-        for (int round = 0; pair_at<NP>(a, sm, tokens_each, base, round, &p); ++round) {
+        for (int round = 0; next_pair<NP, true>(a, sm, tokens_each, base, round, limit, &p); ++round) {
             const int tiles = p.tiles[t];
             if (tiles == 0) continue;
             const int p0 = p.t0 + t * tokens_each, pos = p0 + token;
@@ -687,13 +753,13 @@ bool encode_rows(const PromptArgs& a, const void* at, const long long* stride, i
 }
 
 template <int NP>
-cudaError_t launch_tiles(const PromptArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int tokens_each, bool out_vec, int ctas, cudaStream_t stream) {
+cudaError_t launch_tiles(const PromptArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int tokens_each, bool out_vec, cudaStream_t stream) {
     static std::atomic<unsigned long long> asked{0};
     cudaError_t e = allow_shared(prompt_tiles_kernel<NP>, PromptShape<NP>::kBytes, asked);
     for (int base = 0; base < a.B && e == cudaSuccess; base += kMostPrompts) {
         const int n = a.B - base < kMostPrompts ? a.B - base : kMostPrompts;
         const long long pairs = static_cast<long long>(a.tokens) / (2 * tokens_each) + n, units = pairs * a.Hkv;      // (as many as there may be)
-        prompt_tiles_kernel<NP><<<static_cast<unsigned>(units < ctas ? units : ctas), kPromptThreads, PromptShape<NP>::kBytes, stream>>>(a, base, n, q, k, v, tokens_each, out_vec);
+        prompt_tiles_kernel<NP><<<static_cast<unsigned>(units), kPromptThreads, PromptShape<NP>::kBytes, stream>>>(a, base, n, q, k, v, tokens_each, out_vec);
         e = cudaGetLastError();
     }
     return e;
@@ -704,12 +770,12 @@ cudaError_t launch_tiles(const PromptArgs& a, const CUtensorMap& q, const CUtens
 int prompt_tiles_launches(int B) { return (B + kMostPrompts - 1) / kMostPrompts; }
 // (scores are multiplied by a number that keeps their order, and -inf as it is)
 bool prompt_tiles_takes(const PromptArgs& a) { return a.D >= 16 && a.D <= 128 && a.D % 8 == 0 && a.group <= kTile && a.kf > 0.f; }
-cudaError_t launch_prompt_tiles(const PromptArgs& a, bool out_vec, int ctas, cudaStream_t stream, bool* taken) {
+cudaError_t launch_prompt_tiles(const PromptArgs& a, bool out_vec, cudaStream_t stream, bool* taken) {
     const int tokens_each = kTile / a.group;
     CUtensorMap q, k, v;
     *taken = encode_rows(a, a.q, a.qs, a.Hkv * a.group, a.group, tokens_each, &q) && encode_rows(a, a.k, a.ks, a.Hkv, 1, kTile, &k) && encode_rows(a, a.v, a.vs, a.Hkv, 1, kTile, &v);
     if (!*taken) return cudaSuccess;
-    return a.D <= 64 ? launch_tiles<1>(a, q, k, v, tokens_each, out_vec, ctas, stream) : launch_tiles<2>(a, q, k, v, tokens_each, out_vec, ctas, stream);
+    return a.D <= 64 ? launch_tiles<1>(a, q, k, v, tokens_each, out_vec, stream) : launch_tiles<2>(a, q, k, v, tokens_each, out_vec, stream);
 }
 
 }  // namespace bv

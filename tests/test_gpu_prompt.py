@@ -285,3 +285,24 @@ def test_32_bits_with_tiles_for_every_multiprocessor(lens, Hq, Hkv, D, window, s
     if window and lens[0] > 300:
         v[2 + 50] = math.nan                       # rows 50 to 149 of the first sequence are NaN, no other
     check(q, k, v, off, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,D", [([1500, 3, 0, 2100, 64, 65, 900] + [7] * 40, 32, 8, 128), ([1] * 700, 16, 16, 64)])
+def test_more_units_than_multiprocessors(bv_options, lens, Hq, Hkv, D):
+    """Whichever CTA does a unit: the definition, the same bits every time, beside itself on another stream, and after a call that gave up."""
+    q, k, v, off = make(lens, Hq, Hkv, D, head=1, tail=2, seed=D)
+    want = check(q, k, v, off)
+    side, outs = torch.cuda.Stream(), [torch.full_like(want, 3.0) for _ in range(6)]
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        bv.bv_prompt_attend(q, k, v, off, out=out, stream=side if i % 2 else None)
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, want) for out in outs)
+    bv_options("wait_limit", 3000)
+    bv_options("never_signal", 1)
+    bv.bv_prompt_attend(q, k, v, off)
+    assert bv.bv_stream_status() == -4
+    bv.bv_set_option("never_signal", 0)
+    bv.bv_set_option("wait_limit", 0)
+    check(q, k, v, off)
+    assert bv.bv_stream_status() == 0
