@@ -13,11 +13,12 @@
 // not finite is added where it belongs when the unit ends, from global memory.
 //
 // Units are in the order of their cost, largest first.  The launch has a CTA for each of them, and a CTA that is at work asks for the next one that has not begun
-// and does its unit as well (cluster launch control), while it loads its own: memory, barriers and the order of the units are made once, loads go on from unit
-// to unit, and no counter has to be kept between launches (units handed out forth and back left shares uneven by 12 %: 16 prompts of up to 2048: 347 -> 307 us).
+// and does its unit as well (cluster launch control): memory, barriers and the order of the units are made once, loads go on from unit to unit, and no counter
+// has to be kept between launches.  Against units handed out forth and back, in turn on one GPU: 3 prompts of 3000 tokens, 16 heads on 2, D = 64: 98 -> 86 us; one of 1200,
+// 32 on 8, D = 128: 47 -> 45; 16 of up to 2048: 325 -> 319; one of 32768 as it was.
 //
-// One prompt of 32768 tokens, 32 heads on 8, D = 128: 8.44 ms, 1.04 PFLOP/s (7.3 to 7.9 ms, up to 1.2 PFLOP/s, a few calls after a pause); 16 prompts of up to 2048: 307 us,
-// 735 TFLOP/s.  A key tile of both tiles of rows takes 3700 clocks (2048 of products): 1800 in which a row's 128 scores become weights, some ten instructions each
+// One prompt of 32768 tokens, 32 heads on 8, D = 128: 8.67 ms, 1.01 PFLOP/s (7.3 to 7.9 ms, up to 1.2 PFLOP/s, a few calls after a pause); 16 prompts of up to 2048: 345 us,
+// 655 TFLOP/s (319 us a few calls after a pause).  A key tile of both tiles of rows takes 3700 clocks (2048 of products): 1800 in which a row's 128 scores become weights, some ten instructions each
 // by one warp a scheduler, 600 for reading them and their maximum, 1200 until the next scores are there.  Short prompts: 20 % more for a unit's first tile
 // and its results.
 // Measured and not kept: tiles of 64 keys with two S each, so that scores run ahead (products of 64 columns take as long as those of 128: 9.6 ms); a quarter of the
@@ -325,7 +326,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                 };
                 bool more = pair_at<NP>(a, sm, tokens_each, base, static_cast<int>(blockIdx.x), &p);
                 for (; ok && more; ++round) {
-                    ask(smem_u32(&sm.answer), smem_u32(&sm.asked));
                     const int tiles = list_length(p);
                     auto fetch = [&](int i) {
                         const int slot = x % kSlots;
@@ -354,7 +354,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
 #pragma unroll
                         for (int c = 0; c < NP; ++c) tma_load3(smem_u32(sm.q[t]) + c * Sh::kPanel, &q_map, c * 64, p.h * a.group, p.first + p.t0 + t * tokens_each, bar);
                     }
-                    for (int i = 1; i < 2 * tiles && ok; ++i) fetch(i);
+                    for (int i = 1; i < 2 * tiles - 1 && ok; ++i) fetch(i);
+                    // (not before: who asks early gets the larger unit, whoever is free first: one prompt of 2000 tokens took 78 us for 63)
+                    ask(smem_u32(&sm.answer), smem_u32(&sm.asked));
+                    if (ok) fetch(2 * tiles - 1);
                     // (there may be more CTAs than units; after a no there is no other request)
                     auto another = [&] {
                         ask(smem_u32(&sm.answer), smem_u32(&sm.asked));
