@@ -15,7 +15,8 @@
 // Units are in the order of their cost, largest first.  The launch has a CTA for each of them, and a CTA that is at work asks for the next one that has not begun
 // and does its unit as well (cluster launch control): memory, barriers and the order of the units are made once, loads go on from unit to unit, and no counter
 // has to be kept between launches.  Against units handed out forth and back, in turn on one GPU: 3 prompts of 3000 tokens, 16 heads on 2, D = 64: 98 -> 86 us; one of 1200,
-// 32 on 8, D = 128: 47 -> 45; 16 of up to 2048: 325 -> 319; one of 32768 as it was.
+// 32 on 8, D = 128: 47 -> 45; 16 of up to 2048: 325 -> 319; one of 32768 as it was.  Dearest where half of the
+// CTAs find no unit: 1000 prompts of 64 tokens, 32 heads on 8: 415 -> 421.
 //
 // One prompt of 32768 tokens, 32 heads on 8, D = 128: 8.67 ms, 1.01 PFLOP/s (7.3 to 7.9 ms, up to 1.2 PFLOP/s, a few calls after a pause); 16 prompts of up to 2048: 345 us,
 // 655 TFLOP/s (319 us a few calls after a pause).  A key tile of both tiles of rows takes 3700 clocks (2048 of products): 1800 in which a row's 128 scores become weights, some ten instructions each
