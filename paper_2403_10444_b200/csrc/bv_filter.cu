@@ -426,8 +426,11 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
     };
     // ... and all lists into the first CTA's, behind what it has; how many there are in all (more than kList: not all of them are there).
     // (One remote addition a CTA: one for each of a warp's tokens was a microsecond each, 55 us for a row with 1300 candidates.)
-    auto collect = [&]() {
+    // arrived: every thread has come to the cluster's barrier since it last read what the list lies over; the wait for the others is here, so that
+    // the listing between hides it.
+    auto collect = [&](bool arrived) {
         __syncthreads();
+        if (arrived) cluster.barrier_wait();
         if (rank > 0) {
             const unsigned n = sm.listed;
             if (tid == 0) sm.above = n ? atomicAdd(&first_cta->listed, n) : 0;
@@ -735,6 +738,8 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
                     sm.found = x;
                 }
                 __syncthreads();                         // (the bins have been read)
+                // (the others write into the first CTA's list, which lies where its bins are, when it is through with them and not before)
+                cluster.barrier_arrive();
                 // the lowest value of that bin (a CTA with fewer than k vectors takes all of its own)
                 const int bin = static_cast<int>(sm.found);
                 limit = bin < kWide ? value_of<kF32>(static_cast<uint32_t>(kWide - 1 - bin) << 19) : -INFINITY;
@@ -777,7 +782,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
                 return which;
             });
         }
-        const unsigned n = collect();
+        const unsigned n = collect(own);
         if (n > kList) return false;
         if (rank == 0) {
             conclude(static_cast<int>(n), -1.0);
@@ -876,7 +881,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             }
             return which;
         });
-        collect();
+        collect(false);
         if (rank == 0) {
             const FilterSmem* o = cluster.map_shared_rank(&sm, tid < C * kFWarps ? tid / kFWarps : 0);
             const double x = tid < C * kFWarps ? o->warp_above[tid % kFWarps] : 0.0, y = tid < C * kFWarps ? o->warp_mass[tid % kFWarps] : 0.0;
@@ -1093,7 +1098,7 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
                         if (R::get(v, x) == z0 && i + x > border.last) which &= ~(1u << R::bit(x));
                     return which;
                 });
-                const int n = static_cast<int>(collect());
+                const int n = static_cast<int>(collect(false));
                 if (rank == 0) {
                     order_by_value(n);
                     finish(known < n ? known : n);
