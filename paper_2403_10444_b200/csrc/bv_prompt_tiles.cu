@@ -35,12 +35,14 @@ namespace {
 
 constexpr int kTile = 128;
 constexpr int kPromptThreads = 384, kSoftWarps = 8, kIssueWarp = 8, kLoadWarp = 9, kCleanWarp = 10, kCleaners = 64;
-constexpr int kUnits = 4;                      // marks of units: the cleaning warps are two units ahead of the weights at most
 constexpr float kNone = -3.0e38f;              // the reference of a row that has seen no score
 constexpr float kLag = 8.f;
 constexpr int kFirstKeys = 96;                 // of a tile, whose weights are multiplied while the others are formed
 constexpr int kMostPrompts = 1024;             // of a launch
 constexpr int kTold = 4;                       // units that the loading thread may be ahead of who is last to hear of them
+// Marks of units: who is last to hear of units may still be at unit r (the second tile's weights, where later units have no such tile) when unit r + kTold is
+// told and the cleaning warps clear its mark.
+constexpr int kUnits = kTold + 1;
 
 // Asks for a CTA of the launch that has not begun, whose work this one then does; the answer is 16 bytes, signalled at bar.
 __device__ __forceinline__ void ask(uint32_t answer, uint32_t bar) {
