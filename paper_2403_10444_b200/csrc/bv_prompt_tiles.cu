@@ -583,7 +583,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
 #pragma unroll
                     for (int e = 0; e < 4; ++e) top[e] = fmaxf(top[e], s[c + e]);
                 }
-                const float most = __fmul_rn(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), a.kf);
+                // (a row that is nobody's holds another prompt's queries, or what an earlier unit left: it has no reference, and no say in what its warp does)
+                const float most = live ? __fmul_rn(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), a.kf) : -INFINITY;
                 // (a row without a reference takes the first it can have)
                 const bool need = most > m + kLag || (m == kNone && most > -INFINITY);
                 if (__any_sync(0xffffffffu, need)) {

@@ -26,3 +26,25 @@ def test_values_that_are_not_finite_in_units_of_one_tile(lens, Hq, Hkv, D, value
         got = torch.full_like(clean, 3.0)
         bv.bv_prompt_attend(q, k, bad, off, out=got)
         assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(7.0), want.nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 8), (14, 2), (65, 1)])
+def test_other_prompts_queries_and_what_ran_before_change_no_bit(Hq, Hkv, D):
+    """Rows of a tile that are nobody's hold another prompt's queries, or (where the group does not divide 128) what earlier calls left: large ones, not finite ones."""
+    lens = [45, 60, 3, 130]
+    q, k, v, off = make(lens, Hq, Hkv, D, seed=D + Hq)
+    want = check(q, k, v, off)
+    before = make([128 * 40], 4, 4, D, seed=1)
+    for size in (1e5, 1e20, math.inf, math.nan):
+        for b in (1, 3):
+            other = q.clone()
+            other[off[b]:off[b + 1]] *= size
+            got = bv.bv_prompt_attend(other, k, v, off)
+            mine = torch.ones(q.shape[0], dtype=torch.bool, device="cuda")
+            mine[off[b]:off[b + 1]] = False
+            assert torch.equal(got[mine], want[mine]), (size, b)
+        large = before[0].clone().mul_(size)
+        for _ in range(3):
+            bv.bv_prompt_attend(large, *before[1:])
+            assert torch.equal(bv.bv_prompt_attend(q, k, v, off), want), size
