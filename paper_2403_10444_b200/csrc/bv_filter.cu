@@ -798,7 +798,8 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
     auto by_mass = [&]() {
         const Border among = border;
         const float among_z = value_of<DT>(among.key), step = kPerNat / T;
-        if (!(step < INFINITY)) return false;
+        // (a distance that 32 bits do not hold counts as the last bin, where it belongs but for temperatures near the largest there are)
+        if (!(step < INFINITY) || T > 1e36f) return false;
         auto counts = [&](float z, int i) { return z > among_z || (z == among_z && i <= among.last && z > -INFINITY); };
         auto bin_of = [&](float z) { return static_cast<int>(fminf((top - z) * step, static_cast<float>(kBins - 1))); };
         each([&](const uint4& v, int i) {
