@@ -490,7 +490,8 @@ int bv_prompt_attend(const void* q, const int64_t* q_stride, const void* k, cons
  * and with out_logits (may be null with uniforms; may be logits itself) the row with every other logit at -inf: what the verifications take, so a block
  * that was drafted from cut rows is verified by cut rows of both models and `out_lse`.
  *   logits [rows, V], out_logits [rows, V] in `dtype` at strides (elements) between rows, any V and alignment
- * Weights and their sums are formed in 64 bits, so that borders lie where the formulas have them.  Each of a cut's numbers is one for all rows, or
+ * Weights are formed in 64 bits and summed in as many or more (what weighs less than 2^-69 of the row's largest may count as nothing), so that borders lie where the
+ * formulas have them.  Each of a cut's numbers is one for all rows, or
  * a DEVICE array [rows].  A row with a NaN or +inf logit or without a finite one gives the token -1 and the normaliser NaN and is copied as it is; one
  * whose own numbers are out of range (temperature not positive or not finite, top_p or min_p negative or NaN, min_p above 1) the same, and becomes NaN.
  * Limits (BV_ERR_UNSUPPORTED beyond): V 2^26, rows 2^27.

@@ -11,7 +11,8 @@
 //   values       16 bits: the tokens of each value are counted, so that a mass is a count times a weight
 //   masses       32 bits: a histogram over the distance from the largest bounds the masses, so that only the tokens of a few bins have to be put in order
 //   digits       whatever the others leave (lists that do not fit, infinities where the bins would be): 11, 11 and 10 bits of the keys, a histogram each, of counts or of
-//                weights as integers of up to 2^-45 of the largest, whose sums do not depend on the order of the additions
+//                weights as multiples of 2^-69 of the largest in 96 bits, whose sums do not depend on the order of the additions (64 bits held 2^-45 for 128256 tokens,
+//                2^-35 for 2^26, where a tail of lighter tokens was taken for nothing)
 // Weights are exponentials in 64 bits: a border between tokens of 10^-6 each is off by 10^-5 of a token for an error of 10^-11.
 //
 // One row of 32000, top_k 50, top_p 0.95: 14 us (13 on the GPU), a chain of barriers and exchanges between CTAs; 64 rows of 128256, top_p 0.9: 35 us, the same
@@ -50,7 +51,7 @@ struct FilterArgs {
     int32_t* tokens;
     float* lse;                          // null: not wanted
     char* out;                           // null: not wanted
-    int V, per_cta, fixed;               // elements of a CTA's part; bits of an integer weight
+    int V, per_cta;                      // elements of a CTA's part
     bool vec_in, vec_out;
 };
 
@@ -165,6 +166,7 @@ struct FilterSmem {
         unsigned bins[kBins];
         struct {
             unsigned count[kDigits];
+            unsigned carry[kDigits];     // of the masses: what is above 64 bits
             unsigned long long mass[kDigits];
         };
         unsigned long long list[kList];  // key, then the index turned round: in order when they descend
@@ -180,11 +182,10 @@ struct FilterSmem {
     float warp_top[kFWarps], warp_low[kFWarps];
     int warp_bad[kFWarps];
     unsigned scan_count[kFWarps];
-    unsigned long long scan_mass[kFWarps];
     double scan_a[kFWarps], scan_b[kFWarps];
     // what a step found
+    double above_mass;
     unsigned digit, found, above;
-    unsigned long long above_mass;
     int index;
 };
 
@@ -401,7 +402,6 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
     bad |= top == -INFINITY || wrong;
     const double scale = kRoots * 1.4426950408889634073599246810019 / static_cast<double>(T), M = static_cast<double>(top), share = static_cast<double>(p);
     auto weight = [&](float z) { return pow2_16th((static_cast<double>(z) - M) * scale, sm.roots); };
-    auto fixed = [&](float z) { return static_cast<unsigned long long>(__double2ull_rn(weight(z) * static_cast<double>(1ull << a.fixed))); };
     // min-p: the lowest value of the type that is not below its border
     uint32_t least = 0;
     if (m > 0.f) {
@@ -563,13 +563,12 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         const Border among = border;
         uint32_t prefix = 0;
         unsigned above = 0, ties = 0;
-        unsigned long long above_mass = 0;
-        double target = 0.0;
+        double above_mass = 0.0, target = 0.0;
         constexpr int kLevels = DT == kBF16 ? 2 : 3;
 #pragma unroll 1
         for (int level = 0; level < kLevels; ++level) {
             const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, digits = level == 2 ? 1024 : kDigits;
-            for (int x = tid; x < kDigits; x += kFThreads) { sm.count[x] = 0; sm.mass[x] = 0; }
+            for (int x = tid; x < kDigits; x += kFThreads) { sm.count[x] = 0; sm.carry[x] = 0; sm.mass[x] = 0; }
             __syncthreads();
             each([&](const uint4& v, int i) {
 #pragma unroll
@@ -580,50 +579,52 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
                     if (key > kLowest<DT> && in_range && among.keeps(key, i + x)) {
                         const int d = key >> shift & (digits - 1);
                         atomicAdd(&sm.count[d], 1u);
-                        if (by_mass) atomicAdd(&sm.mass[d], fixed(z));
+                        if (by_mass) {
+                            // (at most 32 wholes of 2^-5 and 2^64 parts of one; up to 2^26 of them stay below 2^96)
+                            const double w = 32.0 * weight(z);
+                            const unsigned whole = __double2uint_rz(w);
+                            const unsigned long long part = __double2ull_rz((w - whole) * 18446744073709551616.0), was = atomicAdd(&sm.mass[d], part);
+                            const unsigned over = whole + (was + part < was);
+                            if (over) atomicAdd(&sm.carry[d], over);
+                        }
                     }
                 }
             });
             cluster.sync();
             // four digits a thread, the largest first
             unsigned c[4], cs = 0;
-            unsigned long long w[4], ws = 0;
+            double w[4], ws = 0.0, all;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 const int d = kDigits - 1 - (4 * tid + x);
+                unsigned long long part = 0, whole = 0;
                 c[x] = 0;
-                w[x] = 0;
                 for (int r = 0; r < C; ++r) {
                     const FilterSmem* o = cluster.map_shared_rank(&sm, r);
                     c[x] += o->count[d];
-                    w[x] += o->mass[d];
+                    if (by_mass) {
+                        part += o->mass[d];
+                        whole += o->carry[d] + (part < o->mass[d]);
+                    }
                 }
+                // (one rounding; sums of these in one order, whatever that of the additions was)
+                w[x] = static_cast<double>(whole) / 32.0 + static_cast<double>(part) / 590295810358705651712.0;
                 cs += c[x];
                 ws += w[x];
             }
-            unsigned ci = cs;
-            unsigned long long wi = ws;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const unsigned cu = __shfl_up_sync(0xffffffffu, ci, o);
-                const unsigned long long wu = __shfl_up_sync(0xffffffffu, wi, o);
-                if (lane >= o) { ci += cu; wi += wu; }
-            }
-            if (lane == 31) { sm.scan_count[warp] = ci; sm.scan_mass[warp] = wi; }
+            const unsigned inc = scanned(cs, lane);
+            if (lane == 31) sm.scan_count[warp] = inc;
             if (tid == 0) sm.found = 0;
-            __syncthreads();
-            unsigned long long all = 0;
-            for (int x = 0; x < kFWarps; ++x) {
-                if (x < warp) { ci += sm.scan_count[x]; wi += sm.scan_mass[x]; }
-                all += sm.scan_mass[x];
-            }
-            if (level == 0) target = target_share * static_cast<double>(all);
-            unsigned cb = above + ci - cs;
-            unsigned long long wb = above_mass + wi - ws;
+            const double first = above_mass + before_me(ws, sm.scan_a, &all);      // (a barrier in it)
+            unsigned before = above + inc - cs;
+            for (int x = 0; x < warp; ++x) before += sm.scan_count[x];
+            if (level == 0) target = target_share * all;
+            unsigned cb = before;
+            double wb = first;
             // by count: the digit with which k is reached; by mass: the last digit before which there is less than the target
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const bool here = by_mass ? static_cast<double>(wb) < target : cb < static_cast<unsigned>(k);
+                const bool here = by_mass ? wb < target : cb < static_cast<unsigned>(k);
                 if (c[x] > 0 && here) atomicMax(&sm.found, 4u * tid + x + 1);
                 cb += c[x];
                 wb += w[x];
@@ -631,8 +632,8 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
             __syncthreads();
             const int found = static_cast<int>(sm.found) - 1;         // (there is one: the largest key's)
             if (found >= 4 * tid && found < 4 * tid + 4) {
-                cb = above + ci - cs;
-                wb = above_mass + wi - ws;
+                cb = before;
+                wb = first;
                 for (int x = 0; x < found - 4 * tid; ++x) { cb += c[x]; wb += w[x]; }
                 sm.digit = kDigits - 1 - found;
                 sm.above = cb;
@@ -652,9 +653,9 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
         if (!by_mass) {
             if (static_cast<unsigned>(k) - above < ties) some = static_cast<unsigned>(k) - above;
         } else {
-            const unsigned long long w = fixed(value_of<DT>(key));
-            if (w > 0) {
-                double i = ceil((target - static_cast<double>(above_mass)) / static_cast<double>(w));
+            const double w = weight(value_of<DT>(key));
+            if (w > 0.0) {
+                double i = ceil((target - above_mass) / w);
                 if (i < 1.0) i = 1.0;
                 if (i < static_cast<double>(ties)) some = static_cast<unsigned>(i);
             }
@@ -1328,8 +1329,6 @@ extern "C" int bv_sample_filtered(const void* logits, int64_t stride, const floa
     a.temperatures = cut->temperatures; a.top_ks = cut->top_ks; a.top_ps = cut->top_ps; a.min_ps = cut->min_ps;
     a.tokens = out_tokens; a.lse = out_lse; a.out = static_cast<char*>(out_logits);
     a.V = V;
-    a.fixed = 62;
-    while (static_cast<long long>(V) >> (62 - a.fixed)) --a.fixed;      // (a row's sum stays below 2^62)
     a.vec_in = on(logits, 16) && (rows == 1 || a.stride % 16 == 0);
     a.vec_out = on(out_logits, 16) && (rows == 1 || a.out_stride % 16 == 0);
     e = dtype == BV_DTYPE_F32 ? bv::pick<bv::kF32>(a, rows, sms, static_cast<cudaStream_t>(stream)) : bv::pick<bv::kBF16>(a, rows, sms, static_cast<cudaStream_t>(stream));
