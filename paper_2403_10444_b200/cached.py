@@ -8,7 +8,7 @@ Two synthetic decoders (``workloads.attention_models``: token embedding, causal 
 real model) take the place of the two tables of ``specdec.run``.  Each keeps its keys and values in a cache of its own.  An iteration
 extends both caches by gamma + 1 tokens (``bv_pages_extend``), drafts gamma tokens one at a time, scores the block with one pass of the target over its
 gamma + 1 tokens (``bv_cache_append``, ``bv_cache_attend`` in every layer), verifies it, and takes what was not accepted out of
-both caches (``bv_pages_truncate`` with the verification's out_len).  Prompts may go in packed (``Decoder.prefill``: ``bv_cache_append_rotary``,
+both caches (``bv_pages_truncate`` with the verification's out_len).  Prompts may go in packed (``Decoder.prefill``: ``bv_cache_append_rotary``, or without rotary positions ``bv_cache_append``, then
 ``bv_prompt_attend``), heads may be turned by their positions (``Rotary``) and both models' distributions cut (``Cut``: ``bv_sample_filtered``,
 ``bv_filter_logits``).  Projections are torch products; attention, rotation, bookkeeping, sampling and verification run in the CUDA library.
 """
@@ -98,18 +98,35 @@ class Decoder:
             x = x + o.reshape(B, n, self.heads * self.D) @ layer["out"]
         return x @ self.w["unembed"]
 
+    def _places(self, T: int, offsets: torch.Tensor):
+        """Where the T packed tokens of ``prefill`` go: (table int32 [T, 1], lens int32 [T]) of as many sequences of one token, each in its own page; length 0
+        where a token has no place (it belongs to no sequence, its position is none, its page is none)."""
+        c, page = self.cache, self.cache.page_size
+        B, room = c.table.shape[0], c.table.shape[1] * page
+        row = torch.arange(T, dtype=torch.int32, device=offsets.device)
+        b = (torch.searchsorted(offsets, row, right=True) - 1).clamp(0, B - 1)
+        first, end, length = offsets[b], offsets[b + 1], c.lens[b]
+        at = length - end + row
+        held = (first >= 0) & (row >= first) & (row < end) & (at >= 0) & (length <= room)
+        at = torch.where(held, at, 0)
+        return c.table[b, (at // page).long()][:, None].contiguous(), torch.where(held, at % page + 1, 0)
+
     def prefill(self, tokens: torch.Tensor, offsets: torch.Tensor) -> torch.Tensor:
         """Takes whole prompts that lie one after the other (tokens [T] of sequences that were empty, sequence b from offsets[b] on; the cache has room for
         them and counts them in) through the layers: their keys and values go into the cache, their attention needs no cache.  What the last
         layer leaves of each token [T, width]; ``@ w["unembed"]`` makes logits of it."""
         c, T = self.cache, tokens.shape[0]
-        # (without rotary positions: pairs that turn by nothing)
-        r = self.rotary or Rotary(torch.zeros((1,), dtype=torch.float64, device=tokens.device))
+        r = self.rotary
+        if r is None and c.table.shape[0] > 0:
+            pages, slots = self._places(T, offsets)
         x = self.w["embed"][tokens.clamp(0, self.w["embed"].shape[0] - 1)]
         for layer, k, v in zip(self.w["layers"], c.k, c.v):
             qkv = (x @ layer["qkv"]).view(T, self.heads + 2 * self.kv_heads, self.D)
             q, kn, vn = qkv.split([self.heads, self.kv_heads, self.kv_heads], dim=1)
-            bv.bv_cache_append_rotary(q, kn, vn, k, v, c.table, c.lens, r.freq, offsets=offsets, interleaved=r.interleaved, mscale=r.mscale, out_q=q, out_k=kn)
+            if r is not None:
+                bv.bv_cache_append_rotary(q, kn, vn, k, v, c.table, c.lens, r.freq, offsets=offsets, interleaved=r.interleaved, mscale=r.mscale, out_q=q, out_k=kn)
+            elif c.table.shape[0] > 0:
+                bv.bv_cache_append(kn[:, None], vn[:, None], k, v, pages, slots)
             o = bv.bv_prompt_attend(q, kn, vn, offsets, window=self.window, sinks=self.sinks)
             x = x + o.reshape(T, self.heads * self.D) @ layer["out"]
         return x
