@@ -213,6 +213,10 @@ def main():
     ap.add_argument("--top-k", type=int, default=0, help="with --context: both models keep their top_k likeliest tokens (with --top-p: of those the nucleus)")
     ap.add_argument("--min-p", type=float, default=0.0, help="with --context: and of these what is at least min_p times as likely as the first")
     args = ap.parse_args()
+    if args.context <= 0:
+        idle = ["--" + name.replace("_", "-") for name in ("rotary", "packed", "top_k", "min_p") if getattr(args, name) != ap.get_default(name)]
+        if idle:
+            ap.error("%s: only with --context" % ", ".join(idle))
     bv.load_library()
     if args.context > 0:
         return context_main(args)
