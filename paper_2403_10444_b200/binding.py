@@ -705,8 +705,9 @@ def rotary_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, ori
     """Frequencies for bv_cache_append_rotary, float64 [rot / 2]: base^(-2 i / rot), radians per position.
 
     ``factor`` > 1 stretches the context for which they were made: without ``original`` all of them are divided by it (positions interpolated
-    linearly); with ``original``, the context's length before, those that turn fewer than ``low`` times in it are, those that turn more than ``high``
-    times are not, and between the two is a ramp in the number of turns, linear in the index."""
+    linearly); with ``original``, the context's length before, by parts, as YaRN has it (Peng, Quesnelle, Fan, Shippole, 2023): those that turn fewer than
+    ``low`` times in it are divided, those that turn more than ``high`` times are not, and between the two is a ramp that is linear in the index, from the last
+    index with ``high`` turns or more to the first with ``low`` or fewer.  (The scale of queries and keys that goes with it is the caller's, ``mscale``.)"""
     if rot < 2 or rot % 2 or not base > 0 or not factor > 0:
         raise ValueError("rot must be even and at least 2, base and factor positive")
     f = torch.arange(rot // 2, dtype=torch.float64).mul_(-2.0 * math.log(base) / rot).exp_()
