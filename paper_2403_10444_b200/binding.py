@@ -896,9 +896,11 @@ def bv_sample_filtered(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, mi
     tokens; ``out_logits`` (may be ``logits``), if given, takes the rows with all other logits at -inf."""
     if stream is not None:
         return _on_stream(stream, logits, bv_sample_filtered, logits, uniforms, temperature, top_k, top_p, min_p, want_lse, out_logits)
+    if uniforms is None:
+        raise ValueError("a token is drawn with uniforms; rows alone are bv_filter_logits'")
     if _fast is not None:
         r = _fast.sample(logits, uniforms, temperature, top_k, top_p, min_p, want_lse, out_logits)
-        if r is not NotImplemented and uniforms is not None:
+        if r is not NotImplemented:
             return r if r.__class__ is not int else _check(r)
     rows, _ = _logits(logits, "logits")
     if uniforms.shape != (rows,) or uniforms.dtype is not torch.float32 or not uniforms.is_contiguous() or uniforms.get_device() != logits.get_device():
