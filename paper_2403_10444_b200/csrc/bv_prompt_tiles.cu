@@ -323,9 +323,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                 bool ok = true;
                 int answers = 0;
                 auto answer = [&] {
-                    const bool in = mbar_wait_now(smem_u32(&sm.asked), answers++ & 1, a.status, limit);
-                    ok = ok && in;
-                    return in ? answered(smem_u32(&sm.answer)) : -1;
+                    const uint32_t bar = smem_u32(&sm.asked), phase = answers++ & 1;
+                    if (mbar_wait_now(bar, phase, a.status, limit)) return answered(smem_u32(&sm.answer));
+                    // (given up: all others do too, and the answer is waited for once more, so that it does not come when the CTA has gone)
+                    ok = false;
+                    atomicExch(&sm.abort, 1);
+                    return mbar_wait_now(bar, phase, a.status, limit) ? answered(smem_u32(&sm.answer)) : -1;
                 };
                 bool more = pair_at<NP>(a, sm, tokens_each, base, static_cast<int>(blockIdx.x), &p);
                 for (; ok && more; ++round) {
