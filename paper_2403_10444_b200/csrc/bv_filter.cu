@@ -660,7 +660,8 @@ __global__ void __launch_bounds__(kFThreads, 2) filter_kernel(const FilterArgs a
                 if (i < static_cast<double>(ties)) some = static_cast<unsigned>(i);
             }
         }
-        border = Border{key, kAll};
+        // (all that are left of this key: an earlier cut may have taken some)
+        border = Border{key, key == among.key ? among.last : kAll};
         if (some == ties) return;
         border.last = last_tie(key, some);
     };
