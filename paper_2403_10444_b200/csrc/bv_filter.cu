@@ -15,9 +15,11 @@
 //                2^-35 for 2^26, where a tail of lighter tokens was taken for nothing)
 // Weights are exponentials in 64 bits: a border between tokens of 10^-6 each is off by 10^-5 of a token for an error of 10^-11.
 //
-// One row of 32000, top_k 50, top_p 0.95: 14 us (13 on the GPU), a chain of barriers and exchanges between CTAs; 64 rows of 128256, top_p 0.9: 35 us, the same
-// chain and the histogram's additions (8 of 35); 576 rows, top_k 1000: 123 us, memory (each row is read twice); 37 rows of 50257 in 32 bits, all kinds of cuts: 31 us, the
-// pipe for 64 bits (a vocabulary's weights).
+// One row of 32000, top_k 50, top_p 0.95: 14.5 us (13 on the GPU), a chain of barriers and exchanges between CTAs; 64 rows of 128256, top_p 0.9: 35 us, the same
+// chain and the histogram's additions (8 of 35); 576 rows, top_k 1000: 124 us, a row's sweeps one after the other (read, read again, filled) with two CTAs an SM, HBM at a
+// third; 37 rows of 50257 in 32 bits, all kinds of cuts: 31 us, of which those with top_p alone take longest (37 of one kind: top_p 0.9 36 us, nothing cut 21,
+// top_k of 1 to 200 with or without top_p 20 to 23, min_p 14): a third of the warps' waits is for barriers, the pipe for 64 bits is at 3 % (21 % on the busiest SM).  By digits, where
+// thousands of tokens about the border are nearly equal: 37 rows of 50257, top_p 0.9, equal logits 262 us, steps of a quarter 297, within some hundredths 158.
 // Measured and not kept: bins of fixed values counted while a row is read (64 rows 49 us against 39 then); a wider ring of loads for rows that are read again.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>

@@ -18,10 +18,10 @@
 // 32 on 8, D = 128: 47 -> 45; 16 of up to 2048: 325 -> 319; one of 32768 as it was.  Dearest where half of the
 // CTAs find no unit: 1000 prompts of 64 tokens, 32 heads on 8: 415 -> 421.
 //
-// One prompt of 32768 tokens, 32 heads on 8, D = 128: 8.67 ms, 1.01 PFLOP/s (7.3 to 7.9 ms, up to 1.2 PFLOP/s, a few calls after a pause); 16 prompts of up to 2048: 345 us,
+// One prompt of 32768 tokens, 32 heads on 8, D = 128: 8.6 ms, 1.02 PFLOP/s (7.3 to 7.9 ms, up to 1.2 PFLOP/s, a few calls after a pause); 16 prompts of up to 2048: 345 us,
 // 655 TFLOP/s (319 us a few calls after a pause).  A key tile of both tiles of rows takes 3700 clocks (2048 of products): 1800 in which a row's 128 scores become weights, some ten instructions each
-// by one warp a scheduler, 600 for reading them and their maximum, 1200 until the next scores are there.  Short prompts: 20 % more for a unit's first tile
-// and its results.
+// by one warp a scheduler, 600 for reading them and their maximum, 1200 until the next scores are there.  Short prompts: the 16 above have 102 such steps an SM, two thirds of
+// their time; the rest is units' first tiles and results, which the next unit's weights wait for.
 // Measured and not kept: tiles of 64 keys with two S each, so that scores run ahead (products of 64 columns take as long as those of 128: 9.6 ms); a quarter of the
 // exponentials on the FMA pipe (more instructions: 8.8 ms, 361 us); warps that share a scheduler taking turns at exponentials (8.7 against 7.3 ms); one signal a
 // tile instead of two (8.95 ms); sums of weights before their rounding (7.9 against 7.6 ms, and less exact); two
@@ -637,6 +637,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_tiles_kernel(const P
                     const float x = ex2(s[c]), y = ex2(s[c + 1]);
                     const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
                     w[c / 2] = *reinterpret_cast<const uint32_t*>(&h);
+                    // The weights' one rounding, to 16 bits: the tensor cores multiply bf16 values by bf16 alone.  A row's error becomes 0.0017 to 0.0021 with it where its
+                    // result's own rounding is 0.0016; the rest of a weight as a second operand would make half as many products again (2048 of a step's 3700 clocks).
                     // (the sum is of the rounded weights: error of a row 0.0022 against 0.0023 with the others; a row of one key is its value)
                     sum[c / 2 & 1] = add2(sum[c / 2 & 1], pair2(__uint_as_float(w[c / 2] << 16), __uint_as_float(w[c / 2] & 0xffff0000u)));
                     if (c == 62) st32(p_at, w);

@@ -1,12 +1,13 @@
 // bv_cache_append_rotary: queries and keys of the newest tokens turned by the angles of their positions, keys and values on into their pages.
 //
 // A pair (x, y) of a head becomes mscale (x cos a - y sin a, y cos a + x sin a), a = position freq[i].  The angle's turns, position freq / 2 pi, are
-// formed and cut down to one turn in 64 bits (at position 10^6 a 32-bit angle is off by 0.03), sine and cosine of the rest in 32; a
-// token's angles are those of all its heads, so a CTA forms them once, in shared memory, while the first vectors of its rows are under way.
+// formed and cut down to one turn in 64 bits (at position 10^6 a 32-bit angle is off by 0.03), sine and cosine of the rest in 32
+// (with the rest's rounding off by 2^-22 at most, a few roundings of a 32-bit result: rows of 32 bits are off by 3.7e-8 where those of 64-bit sines are by 2.9e-8, rows of
+// 16 bits by their own rounding either way); a token's angles are those of all its heads, so a CTA forms them once, in shared memory, while the first vectors of its rows are under way.
 //
-// Bound by the bytes of the rows, each of which is read once and written once (keys twice where they are wanted beside): 17500 tokens of 32 heads on 8, D =
-// 128, bf16, 506 MB in 105 us, 4.8 TB/s, reads and writes mixed; 64 blocks of 9 tokens, 64 heads on 8, 7.3 us; 7 blocks of 5, 32 bits, 3.2 us, launch and
-// three trips to memory in a row (offsets, length, page).
+// Each row is read once and written once (keys twice where they are wanted beside): 17500 tokens of 32 heads on 8, D =
+// 128, bf16, 506 MB in 105 us, 4.8 TB/s, reads and writes mixed (memory at 51 %, the SMs at 67 %: a unit's place is worked out for its load and again for its stores); 64 blocks of
+// 9 tokens, 64 heads on 8, 7.3 us; 7 blocks of 5, 32 bits, 3.4 us, launch and three trips to memory in a row (offsets, length, page).
 #include <cmath>
 
 #include "bv_cache.cuh"
