@@ -116,6 +116,8 @@ class Decoder:
         them and counts them in) through the layers: their keys and values go into the cache, their attention needs no cache.  What the last
         layer leaves of each token [T, width]; ``@ w["unembed"]`` makes logits of it."""
         c, T = self.cache, tokens.shape[0]
+        if tokens.dim() != 1 or offsets.dtype != torch.int32 or tuple(offsets.shape) != (c.table.shape[0] + 1,) or offsets.device != c.table.device:
+            raise ValueError("tokens must be [T] and offsets int32 [B + 1] on the cache's device")
         r = self.rotary
         if r is None and c.table.shape[0] > 0:
             pages, slots = self._places(T, offsets)

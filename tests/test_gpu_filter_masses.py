@@ -5,7 +5,6 @@ import pytest
 import torch
 
 import paper_2403_10444_b200 as bv
-import prompt_plain as pp
 from test_gpu_filter import check, uniforms
 
 pytestmark = pytest.mark.gpu
